@@ -312,6 +312,110 @@ idxc_status idxc_sparse_attention(const void* q, const void* kv, const int32_t* 
                                   int64_t n_q, int64_t n_kv, int H, int d_qk, int d_v, int k_top, float scale,
                                   void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Latent cache rows in bf16 or in 4 bits. (The paper prints no storage format for the latent cache that its sparse
+ * attention reads; bf16 is what idxc_sparse_attention takes, the 4-bit row is this library's own.) A row has 576 columns:
+ * 512 value columns, which are keys too, and 64 positional columns, which are keys only.
+ *   IDXC_LATENT_BF16  1152 bytes, the columns in order
+ *   IDXC_LATENT_Q4    IDXC_Q4_ROW_BYTES = 416 bytes, in order:
+ *       256 bytes  codes of the value columns: a nibble u = code + 8, code in -7 .. 7. The 4 bytes at 4 g hold columns
+ *                  8 g .. 8 g + 7; read as a little-endian word, its nibbles from the lowest are the columns
+ *                  0 2 4 6 1 3 5 7 of the eight
+ *        32 bytes  sixteen bf16 scales, one per 32 value columns
+ *       128 bytes  the 64 positional columns, bf16
+ *     A value column stands for code * scale. Scales written by idxc_quantize_q4 have 5 significant bits, so that
+ *     code * scale is exact in bf16 and every reader sees the same values.
+ * Caches are row-major arrays of rows without gaps, 16-byte aligned.
+ *
+ * idxc_quantize_q4 -- rows of bf16 into a 4-bit cache: a group's scale is the smallest number of 5 significant bits that is
+ * at least max|x| / 7 (and at least 2^-100); code = x / scale rounded to nearest, ties to even. Positional columns are copied.
+ *   x         [n_tokens, 576] bf16, 16-byte aligned
+ *   cache     [cache_rows, 416] bytes
+ *   dst_rows  NULL: token r is written at row r (n_tokens <= cache_rows). Otherwise DEVICE int64 [n_tokens]: token r is
+ *             written at row dst_rows[r]; a row outside [0, cache_rows) is not written. The rows must be distinct.
+ * idxc_dequantize_q4 -- the values that rows stand for: out [n_rows, 576] bf16, row r from cache row src_rows[r] (NULL: r);
+ * a source row outside the cache gives zeros. Exact for rows written by idxc_quantize_q4.
+ * ------------------------------------------------------------------------- */
+typedef enum { IDXC_LATENT_BF16 = 0, IDXC_LATENT_Q4 = 1 } idxc_latent_format;
+#define IDXC_Q4_ROW_BYTES 416
+
+idxc_status idxc_quantize_q4(const void* x, int64_t n_tokens, void* cache, int64_t cache_rows, const int64_t* dst_rows,
+                             void* cuda_stream);
+idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int64_t* src_rows, int64_t n_rows, void* out,
+                               void* cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Dense attention of new tokens over their sequences' latent rows, the form that idxc_sparse_attention computes over a
+ * selection: for sequence b, its new token i of n_step and head h
+ *     n(b, i)      = lens[b] - (n_step - 1 - i)                  (the new tokens are the last n_step rows)
+ *     x[s]         = scale * < q[b, i, h, :], row(kv_base[b] + s)[0:576] >          for 0 <= s < n(b, i)
+ *     out[b, i, h] = sum_s Softmax(x)[s] * row(kv_base[b] + s)[0:512],    lse[b, i, h] = log sum_s exp(x[s])
+ * A row that lies outside [0, n_kv) takes no part. A token that sees nothing gets out = 0 and lse = -inf.
+ *   q        DEVICE bf16 [B, n_step, H, 576], 16-byte aligned    kv  DEVICE [n_kv] rows of `fmt`
+ *   kv_base  NULL (0 for all) or DEVICE int64 [B]                lens DEVICE int32 [B], clamped to [0, max_len]
+ *   out      DEVICE bf16 [B, n_step, H, 512], 16-byte aligned    lse NULL or DEVICE fp32 [B, n_step, H]
+ *   workspace DEVICE, 256-byte aligned, idxc_latent_attention_workspace_bytes(B, n_step, max_len, H) bytes; scratch, one per
+ *            call in flight
+ * Supported: d_qk = 576, d_v = 512, 1 <= H <= 128, n_step >= 1, B * n_step * H < 2^31, max_len <= 2^30, n_kv < 2^31.
+ * Rows that no token sees are never read. Arithmetic: bf16 products with fp32 accumulation, fp32 softmax, probabilities
+ * rounded to bf16 for the second product, bf16 output. The result does not depend on what else runs.
+ *
+ * idxc_sparse_attention_q4 -- idxc_sparse_attention (same arguments, same rules) over a cache of 4-bit rows; its workspace is
+ * idxc_latent_attention_workspace_bytes(n_q, 1, k_top, H) bytes, 256-byte aligned.
+ * ------------------------------------------------------------------------- */
+size_t idxc_latent_attention_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H);
+
+idxc_status idxc_latent_attention(const void* q, const void* kv, idxc_latent_format fmt, int64_t n_kv, const int64_t* kv_base,
+                                  const int32_t* lens, int64_t B, int n_step, int64_t max_len, int H, int d_qk, int d_v,
+                                  float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                  void* cuda_stream);
+
+idxc_status idxc_sparse_attention_q4(const void* q, const void* kv_q4, const int32_t* topk, const int64_t* kv_base,
+                                     int64_t n_q, int64_t n_kv, int H, int d_qk, int d_v, int k_top, float scale, void* out,
+                                     float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention weight that cached positions received in a step, summed over heads and new tokens, for keeping the running
+ * sums by which a cache is cut. lse is the attention's own output for the same q.
+ *   dense (topk == NULL):  acc[b, s] = beta * acc[b, s] + sum_{i, h : s < n(b, i)} exp(x[b,i,h,s] - lse[b,i,h])   for
+ *                          s < lens[b] (clamped to [0, max_len]); other entries of the row are untouched. beta == 0: acc is
+ *                          not read. A row of the cache outside [0, n_kv) adds 0.
+ *   selected (topk = [B, k_top] int32, n_step == 1, beta == 1, lens == NULL): acc[b, topk[b,j]] += sum_h exp(x - lse[b,h]) for
+ *                          every usable entry (0 <= topk[b,j] < ld and its cache row inside [0, n_kv)); a position named
+ *                          twice is added twice.
+ * Tokens whose lse is -inf add nothing.
+ *   acc DEVICE fp32 [B, ld] (dense: ld >= max_len); lse DEVICE fp32 [B, n_step, H]; q, kv, kv_base, lens as above.
+ * Every entry of acc is written by one thread; the sums do not depend on what else runs.
+ * ------------------------------------------------------------------------- */
+idxc_status idxc_attention_weights(const void* q, const void* kv, idxc_latent_format fmt, int64_t n_kv, const int64_t* kv_base,
+                                   const int32_t* lens, const int32_t* topk, int k_top, int64_t B, int n_step,
+                                   int64_t max_len, int H, int d_qk, float scale, const float* lse, float beta, float* acc,
+                                   int64_t ld, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Cutting a cache to a budget by accumulated attention weight.
+ *
+ * idxc_evict_select -- the positions that stay. Sequence b has n = lens[b] positions (clamped to [0, ld]). n <= budget: all
+ * of them. Otherwise the last `recent` ones and the budget - recent of the others with the largest acc[b, s], ties to the
+ * lowest position. keep_out [B, budget] int32: ascending, padded with -1 (the format of topk_out: it can be passed to the
+ * sparse attention as it is); new_lens_out [B] int32: min(n, budget). 0 <= recent <= budget, 1 <= budget <= 2^30. NaN in
+ * acc: some positions are chosen, within range. new_lens_out must not be lens.
+ *
+ * idxc_compact_rows -- brings the rows that stay together: for j < n_keep[b], row dst_base[b] + j of dst becomes row
+ * src_base[b] + keep[b, j] of src. row_bytes is any multiple of 4 (bf16 or 4-bit latent rows, indexer keys, scales, the
+ * sums themselves with src_base[b] = b * ld). keep [B, ld_keep]; an entry that names no row of src, or whose place is
+ * no row of dst, moves nothing.
+ *   dst == src (then dst_base must be src_base): in place. keep[b] must be ascending without repeats, as written by
+ *   idxc_evict_select; entries that are not at or behind their own place are skipped. Sequences must not share rows.
+ *   Otherwise the two buffers must not overlap.
+ * ------------------------------------------------------------------------- */
+idxc_status idxc_evict_select(const float* acc, int64_t ld, const int32_t* lens, int64_t B, int budget, int recent,
+                              int32_t* keep_out, int32_t* new_lens_out, void* cuda_stream);
+
+idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t src_rows, int64_t dst_rows,
+                              const int64_t* src_base, const int64_t* dst_base, const int32_t* keep, int ld_keep,
+                              const int32_t* n_keep, int64_t B, void* cuda_stream);
+
 /* Synchronises the stream, then returns IDXC_OK, IDXC_ERR_CUDA, or
  * IDXC_ERR_DEVICE_TIMEOUT if any kernel of this library recorded a bounded wait that
  * ran out since the last poll (the record is cleared). */

@@ -17,6 +17,8 @@ _LIB_PATH = Path(__file__).resolve().parent / "libidxc.so"
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_PATTERN, ERR_CUDA, ERR_DEVICE_TIMEOUT = 1, 2, 3, 4, 5, 6
 BF16, FP8_E4M3 = 0, 1
+LATENT_BF16, LATENT_Q4 = 0, 1
+Q4_ROW_BYTES = 416
 FLAG_COPY_SHARED = 0x1
 FLAG_SIMT_SCORER = 0x2
 FLAG_FILL_MASKED = 0x4
@@ -29,6 +31,8 @@ EXPORTED_SYMBOLS = [
     "idxc_schedule_decode_layer", "idxc_poll_device_status", "idxc_launch_count", "idxc_indexer_decode_noalloc",
     "idxc_selftest_bounded_wait", "idxc_selftest_tmem_readout", "idxc_selftest_tmem_readout_under_mma", "idxc_selftest_issue_rates", "idxc_quantize_e4m3", "idxc_topk_overlap", "idxc_pattern_search_dp",
     "idxc_pattern_search_greedy", "idxc_distill_kl", "idxc_sparse_attention_workspace_bytes", "idxc_sparse_attention",
+    "idxc_quantize_q4", "idxc_dequantize_q4", "idxc_latent_attention_workspace_bytes", "idxc_latent_attention", "idxc_sparse_attention_q4",
+    "idxc_attention_weights", "idxc_evict_select", "idxc_compact_rows",
 ]
 NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -100,6 +104,23 @@ def lib() -> ctypes.CDLL:
         L.idxc_sparse_attention.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, sz, vp]
         L.idxc_quantize_e4m3.restype = i32
         L.idxc_quantize_e4m3.argtypes = [vp, i64, i32, vp, vp, vp, vp]
+        L.idxc_quantize_q4.restype = i32
+        L.idxc_quantize_q4.argtypes = [vp, i64, vp, i64, vp, vp]
+        L.idxc_dequantize_q4.restype = i32
+        L.idxc_dequantize_q4.argtypes = [vp, i64, vp, i64, vp, vp]
+        L.idxc_latent_attention_workspace_bytes.restype = sz
+        L.idxc_latent_attention_workspace_bytes.argtypes = [i64, i32, i64, i32]
+        L.idxc_latent_attention.restype = i32
+        L.idxc_latent_attention.argtypes = [vp, vp, i32, i64, vp, vp, i64, i32, i64, i32, i32, i32, ctypes.c_float, vp, vp, vp, sz, vp]
+        L.idxc_sparse_attention_q4.restype = i32
+        L.idxc_sparse_attention_q4.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, sz, vp]
+        L.idxc_attention_weights.restype = i32
+        L.idxc_attention_weights.argtypes = [vp, vp, i32, i64, vp, vp, vp, i32, i64, i32, i64, i32, i32, ctypes.c_float, vp, ctypes.c_float,
+                                             vp, i64, vp]
+        L.idxc_evict_select.restype = i32
+        L.idxc_evict_select.argtypes = [vp, i64, vp, i64, i32, i32, vp, vp, vp]
+        L.idxc_compact_rows.restype = i32
+        L.idxc_compact_rows.argtypes = [vp, vp, i32, i64, i64, vp, vp, vp, i32, vp, i64, vp]
         L.idxc_selftest_bounded_wait.restype = i32
         L.idxc_selftest_bounded_wait.argtypes = [u32, vp]
         L.idxc_selftest_tmem_readout.restype = i32
@@ -354,6 +375,180 @@ def sparse_attention(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, out=N
                                        ctypes.c_float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                        _stream(stream)), "idxc_sparse_attention")
     return out, lse
+
+
+# ------------------------------------------------------------------ latent cache: 4-bit rows, dense attention, eviction
+def _launch_on(stream, **tensors):
+    """Checks that the tensors (None allowed) are contiguous CUDA tensors of one device and returns (device guard, stream):
+    the call is made with that device current, on its current stream unless one is given."""
+    device = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        _dev(t, name)
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors are on {device}")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+    return torch.cuda.device(device), torch.cuda.current_stream(device) if stream is None else stream
+
+
+def _typed(t, name, dtype, shape=None):
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _latent_format(kv) -> int:
+    if kv.dim() == 2 and kv.dtype == torch.bfloat16 and kv.shape[1] == 576:
+        return LATENT_BF16
+    if kv.dim() == 2 and kv.dtype == torch.uint8 and kv.shape[1] == Q4_ROW_BYTES:
+        return LATENT_Q4
+    raise ValueError(f"kv must be [n_kv, 576] bfloat16 or [n_kv, {Q4_ROW_BYTES}] uint8, got {list(kv.shape)} {kv.dtype}")
+
+
+def _nbytes(t):
+    return t.numel() * t.element_size()
+
+
+def quantize_q4(x, cache_out, dst_rows=None, stream=None):
+    """idxc_quantize_q4: x [n, 576] bf16 -> rows of cache_out [rows, 416] uint8, row r or row dst_rows[r] (int64)."""
+    guard, stream = _launch_on(stream, x=x, cache_out=cache_out, dst_rows=dst_rows)
+    if x.dim() != 2 or cache_out.dim() != 2:
+        raise ValueError("x must be [n, 576] and cache_out [rows, 416]")
+    n = x.shape[0]
+    _typed(x, "x", torch.bfloat16, (n, 576)); _typed(cache_out, "cache_out", torch.uint8, (cache_out.shape[0], Q4_ROW_BYTES))
+    _typed(dst_rows, "dst_rows", torch.int64, (n,))
+    with guard:
+        _check(lib().idxc_quantize_q4(_ptr(x), n, _ptr(cache_out), cache_out.shape[0], _ptr(dst_rows), _stream(stream)), "idxc_quantize_q4")
+
+
+def dequantize_q4(cache, out, src_rows=None, stream=None):
+    """idxc_dequantize_q4: out [n, 576] bf16, row r = the values of cache row r, or of row src_rows[r] (int64)."""
+    guard, stream = _launch_on(stream, cache=cache, out=out, src_rows=src_rows)
+    if cache.dim() != 2 or out.dim() != 2:
+        raise ValueError("cache must be [rows, 416] and out [n, 576]")
+    n = out.shape[0]
+    _typed(out, "out", torch.bfloat16, (n, 576)); _typed(cache, "cache", torch.uint8, (cache.shape[0], Q4_ROW_BYTES))
+    _typed(src_rows, "src_rows", torch.int64, (n,))
+    with guard:
+        _check(lib().idxc_dequantize_q4(_ptr(cache), cache.shape[0], _ptr(src_rows), n, _ptr(out), _stream(stream)), "idxc_dequantize_q4")
+
+
+def latent_attention_workspace_bytes(B, n_step, max_len, H) -> int:
+    return int(lib().idxc_latent_attention_workspace_bytes(int(B), int(n_step), int(max_len), int(H)))
+
+
+def _latent_workspace(workspace, B, n_step, max_len, H, device):
+    if workspace is None:
+        workspace = alloc_workspace(latent_attention_workspace_bytes(B, n_step, max_len, H), device)
+    return workspace
+
+
+def latent_attention(q, kv, kv_base, lens, max_len, d_v, scale, want_lse=True, out=None, workspace=None, stream=None):
+    """idxc_latent_attention: q [B, n_step, H, 576] bf16 over each sequence's rows of kv ([n_kv, 576] bf16 or [n_kv, 416] uint8
+    4-bit rows), rows kv_base[b] .. kv_base[b] + lens[b] - 1 (kv_base None: 0). The n_step new tokens are the last rows; token i
+    sees lens[b] - (n_step - 1 - i) of them. ``max_len`` is a host upper bound on lens.
+    Returns (out [B, n_step, H, d_v] bf16, lse [B, n_step, H] fp32 or None)."""
+    guard, stream = _launch_on(stream, q=q, kv=kv, kv_base=kv_base, lens=lens, out=out, workspace=workspace)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, n_step, H, 576]")
+    fmt = _latent_format(kv)
+    B, n_step, H, d_qk = q.shape
+    _typed(q, "q", torch.bfloat16); _typed(kv_base, "kv_base", torch.int64, (B,)); _typed(lens, "lens", torch.int32, (B,))
+    _typed(out, "out", torch.bfloat16, (B, n_step, H, d_v))
+    with guard, torch.cuda.stream(stream):
+        if out is None:
+            out = torch.empty((B, n_step, H, d_v), dtype=torch.bfloat16, device=q.device)
+        lse = torch.empty((B, n_step, H), dtype=torch.float32, device=q.device) if want_lse else None
+        workspace = _latent_workspace(workspace, B, n_step, max_len, H, q.device)
+        _check(lib().idxc_latent_attention(_ptr(q), _ptr(kv), fmt, kv.shape[0], _ptr(kv_base), _ptr(lens), B, n_step, int(max_len), H, d_qk,
+                                           int(d_v), ctypes.c_float(scale), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
+                                           _stream(stream)), "idxc_latent_attention")
+    return out, lse
+
+
+def sparse_attention_q4(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, out=None, workspace=None, stream=None):
+    """idxc_sparse_attention_q4: sparse_attention over a cache of 4-bit rows, kv [n_kv, 416] uint8.
+    Returns (out [n_q, H, d_v] bf16, lse [n_q, H] fp32 or None)."""
+    guard, stream = _launch_on(stream, q=q, kv=kv, topk=topk, kv_base=kv_base, out=out, workspace=workspace)
+    if q.dim() != 3 or topk.dim() != 2 or _latent_format(kv) != LATENT_Q4:
+        raise ValueError("q must be [n_q, H, 576], topk [n_q, k_top] and kv [n_kv, 416] uint8")
+    n_q, H, d_qk = q.shape
+    k_top = topk.shape[1]
+    _typed(q, "q", torch.bfloat16); _typed(topk, "topk", torch.int32, (n_q, k_top)); _typed(kv_base, "kv_base", torch.int64, (n_q,))
+    _typed(out, "out", torch.bfloat16, (n_q, H, d_v))
+    with guard, torch.cuda.stream(stream):
+        if out is None:
+            out = torch.empty((n_q, H, d_v), dtype=torch.bfloat16, device=q.device)
+        lse = torch.empty((n_q, H), dtype=torch.float32, device=q.device) if want_lse else None
+        workspace = _latent_workspace(workspace, n_q, 1, k_top, H, q.device)
+        _check(lib().idxc_sparse_attention_q4(_ptr(q), _ptr(kv), _ptr(topk), _ptr(kv_base), n_q, kv.shape[0], H, d_qk, int(d_v), k_top,
+                                              ctypes.c_float(scale), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
+                                              _stream(stream)), "idxc_sparse_attention_q4")
+    return out, lse
+
+
+def attention_weights(q, kv, lse, acc, scale, kv_base=None, lens=None, max_len=None, topk=None, beta=1.0, stream=None):
+    """idxc_attention_weights: adds to acc [B, ld] fp32, in place, the probability every cached position received from
+    q [B, n_step, H, 576] (or [B, H, 576] for n_step = 1), given the attention's lse. Dense: lens and max_len; acc is scaled by beta first, over each sequence's own
+    positions. Selected: topk [B, k_top] int32, beta = 1."""
+    guard, stream = _launch_on(stream, q=q, kv=kv, lse=lse, acc=acc, kv_base=kv_base, lens=lens, topk=topk)
+    if q.dim() == 3:
+        q, lse = q.unsqueeze(1), lse.unsqueeze(1)
+    if q.dim() != 4 or acc.dim() != 2 or (topk is not None and topk.dim() != 2):
+        raise ValueError("q must be [B, n_step, H, 576], acc [B, ld] and topk [B, k_top]")
+    if (lens is None) == (topk is None) or (lens is not None and max_len is None):
+        raise ValueError("give either lens and max_len, or topk")
+    fmt = _latent_format(kv)
+    B, n_step, H, d_qk = q.shape
+    _typed(q, "q", torch.bfloat16); _typed(kv_base, "kv_base", torch.int64, (B,)); _typed(lens, "lens", torch.int32, (B,))
+    _typed(lse, "lse", torch.float32, (B, n_step, H)); _typed(acc, "acc", torch.float32, (B, acc.shape[1]))
+    k_top = 0 if topk is None else topk.shape[1]
+    _typed(topk, "topk", torch.int32, (B, k_top))
+    with guard:
+        _check(lib().idxc_attention_weights(_ptr(q), _ptr(kv), fmt, kv.shape[0], _ptr(kv_base), _ptr(lens), _ptr(topk), k_top, B, n_step,
+                                            0 if max_len is None else int(max_len), H, d_qk, ctypes.c_float(scale), _ptr(lse),
+                                            ctypes.c_float(beta), _ptr(acc), acc.shape[1], _stream(stream)), "idxc_attention_weights")
+
+
+def evict_select(acc, lens, budget, recent, keep_out, new_lens_out, stream=None):
+    """idxc_evict_select: acc [B, ld] fp32, lens [B] int32 -> keep_out [B, budget] int32 (ascending, -1 padded), new_lens_out [B]."""
+    guard, stream = _launch_on(stream, acc=acc, lens=lens, keep_out=keep_out, new_lens_out=new_lens_out)
+    if acc.dim() != 2:
+        raise ValueError("acc must be [B, ld]")
+    B, ld = acc.shape
+    _typed(acc, "acc", torch.float32); _typed(lens, "lens", torch.int32, (B,)); _typed(new_lens_out, "new_lens_out", torch.int32, (B,))
+    _typed(keep_out, "keep_out", torch.int32, (B, budget))
+    with guard:
+        _check(lib().idxc_evict_select(_ptr(acc), ld, _ptr(lens), B, int(budget), int(recent), _ptr(keep_out), _ptr(new_lens_out),
+                                       _stream(stream)), "idxc_evict_select")
+
+
+def compact_rows(src, dst, keep, n_keep, src_base, dst_base=None, stream=None):
+    """idxc_compact_rows: row dst_base[b] + j of dst <- row src_base[b] + keep[b, j] of src, j < n_keep[b]. dst may be src
+    itself (in place; dst_base must then be left out or be src_base)."""
+    if dst_base is None:
+        dst_base = src_base
+    guard, stream = _launch_on(stream, src=src, dst=dst, keep=keep, n_keep=n_keep, src_base=src_base, dst_base=dst_base)
+    if keep.dim() != 2:
+        raise ValueError("keep must be [B, ld_keep]")
+    B, ld_keep = keep.shape
+    if src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
+        raise ValueError("src and dst must have rows of the same type and shape")
+    row_bytes = src.element_size()
+    for n in src.shape[1:]:
+        row_bytes *= n
+    _typed(keep, "keep", torch.int32); _typed(n_keep, "n_keep", torch.int32, (B,))
+    _typed(src_base, "src_base", torch.int64, (B,)); _typed(dst_base, "dst_base", torch.int64, (B,))
+    with guard:
+        _check(lib().idxc_compact_rows(_ptr(src), _ptr(dst), row_bytes, src.shape[0], dst.shape[0], _ptr(src_base), _ptr(dst_base), _ptr(keep),
+                                       ld_keep, _ptr(n_keep), B, _stream(stream)), "idxc_compact_rows")
 
 
 def selftest_bounded_wait(wait_cycles: int = 1_000_000, stream=None):

@@ -520,6 +520,141 @@ idxc_status idxc_sparse_attention(const void* q, const void* kv, const int32_t* 
                ? IDXC_OK : IDXC_ERR_CUDA;
 }
 
+// ------------------------------------------------------------------ latent cache: 4-bit rows, dense attention, eviction
+
+idxc_status idxc_quantize_q4(const void* x, int64_t n_tokens, void* cache, int64_t cache_rows, const int64_t* dst_rows,
+                             void* cuda_stream) {
+    if (n_tokens < 0 || cache_rows < 0 || n_tokens > (int64_t(1) << 31) || (!dst_rows && n_tokens > cache_rows)) return IDXC_ERR_INVALID_ARG;
+    if (n_tokens == 0) return IDXC_OK;
+    if (!x || !cache || !aligned(x, 16) || !aligned(cache, 16) || (dst_rows && !aligned(dst_rows, 8))) return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_quantize_q4(x, n_tokens, cache, cache_rows, dst_rows, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+               ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int64_t* src_rows, int64_t n_rows, void* out,
+                               void* cuda_stream) {
+    if (n_rows < 0 || cache_rows < 0 || n_rows > (int64_t(1) << 31)) return IDXC_ERR_INVALID_ARG;
+    if (n_rows == 0) return IDXC_OK;
+    if (!out || !aligned(out, 16) || (cache_rows > 0 && !cache) || !aligned(cache, 16) || (src_rows && !aligned(src_rows, 8)))
+        return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_dequantize_q4(cache, cache_rows, src_rows, n_rows, out, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+               ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the calls over latent rows have in common. 0 means "go on" is IDXC_OK here; sizes first, then pointers.
+idxc_status check_latent(const LatentArgs& a, int d_qk) {
+    if (a.B < 0 || a.n_step < 1 || a.H < 1 || a.n_kv < 0 || a.max_len < 0 || d_qk < 1) return IDXC_ERR_INVALID_ARG;
+    if (a.max_len > (int64_t(1) << 30) || a.n_kv >= (int64_t(1) << 31)) return IDXC_ERR_INVALID_ARG;
+    if (d_qk != 576 || a.H > 128) return IDXC_ERR_UNSUPPORTED;
+    if (a.B >= (int64_t(1) << 31) || static_cast<int64_t>(a.n_step) * a.H >= (int64_t(1) << 31) ||
+        a.B * (static_cast<int64_t>(a.n_step) * a.H) >= (int64_t(1) << 31))
+        return IDXC_ERR_INVALID_ARG;
+    if (a.B == 0) return IDXC_OK;
+    if (!a.q || !aligned(a.q, 16) || (a.n_kv > 0 && !a.kv) || !aligned(a.kv, 16) || (a.kv_base && !aligned(a.kv_base, 8)))
+        return IDXC_ERR_INVALID_ARG;
+    if (a.topk ? !aligned(a.topk, 4) : (!a.lens || !aligned(a.lens, 4))) return IDXC_ERR_INVALID_ARG;
+    return IDXC_OK;
+}
+
+idxc_status run_latent_attn(const LatentArgs& a, int d_qk, int d_v, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* cuda_stream) {
+    if (d_v < 1 || d_v > d_qk) return IDXC_ERR_INVALID_ARG;
+    const idxc_status st = check_latent(a, d_qk);
+    if (st != IDXC_OK) return st;
+    if (d_v != 512) return IDXC_ERR_UNSUPPORTED;
+    if (a.B == 0) return IDXC_OK;
+    if (!out || !aligned(out, 16) || (lse && !aligned(lse, 4))) return IDXC_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < idxc_latent_attention_workspace_bytes(a.B, a.n_step, a.max_len, a.H))
+        return IDXC_ERR_WORKSPACE;
+    if (!device_info().ok) return IDXC_ERR_CUDA;
+    g_launches += 1;
+    return launch_latent_attn(a, out, lse, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t idxc_latent_attention_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H) {
+    if (B <= 0 || n_step < 1 || max_len < 0 || H < 1) return 0;
+    return 256;
+}
+
+idxc_status idxc_latent_attention(const void* q, const void* kv, idxc_latent_format fmt, int64_t n_kv, const int64_t* kv_base,
+                                  const int32_t* lens, int64_t B, int n_step, int64_t max_len, int H, int d_qk, int d_v,
+                                  float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (fmt != IDXC_LATENT_BF16 && fmt != IDXC_LATENT_Q4) return IDXC_ERR_INVALID_ARG;
+    const LatentArgs a{q, kv, fmt == IDXC_LATENT_Q4, n_kv, kv_base, lens, nullptr, 0, B, n_step, max_len, H, scale};
+    return run_latent_attn(a, d_qk, d_v, out, lse, workspace, workspace_bytes, cuda_stream);
+}
+
+idxc_status idxc_sparse_attention_q4(const void* q, const void* kv_q4, const int32_t* topk, const int64_t* kv_base, int64_t n_q,
+                                     int64_t n_kv, int H, int d_qk, int d_v, int k_top, float scale, void* out, float* lse,
+                                     void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (k_top < 1 || (n_q > 0 && !topk)) return IDXC_ERR_INVALID_ARG;
+    const LatentArgs a{q, kv_q4, 1, n_kv, kv_base, nullptr, topk, k_top, n_q, 1, k_top, H, scale};
+    return run_latent_attn(a, d_qk, d_v, out, lse, workspace, workspace_bytes, cuda_stream);
+}
+
+idxc_status idxc_attention_weights(const void* q, const void* kv, idxc_latent_format fmt, int64_t n_kv, const int64_t* kv_base,
+                                   const int32_t* lens, const int32_t* topk, int k_top, int64_t B, int n_step, int64_t max_len,
+                                   int H, int d_qk, float scale, const float* lse, float beta, float* acc, int64_t ld,
+                                   void* cuda_stream) {
+    if (fmt != IDXC_LATENT_BF16 && fmt != IDXC_LATENT_Q4) return IDXC_ERR_INVALID_ARG;
+    if (topk && (k_top < 1 || n_step != 1 || beta != 1.f || lens)) return IDXC_ERR_INVALID_ARG;
+    if (ld < 0 || (!topk && ld < max_len)) return IDXC_ERR_INVALID_ARG;
+    const LatentArgs a{q, kv, fmt == IDXC_LATENT_Q4, n_kv, kv_base, lens, topk, k_top, B, n_step, topk ? k_top : max_len, H, scale};
+    const idxc_status st = check_latent(a, d_qk);
+    if (st != IDXC_OK) return st;
+    if (B == 0) return IDXC_OK;
+    if (!lse || !acc || !aligned(lse, 4) || !aligned(acc, 4)) return IDXC_ERR_INVALID_ARG;
+    if (a.max_len == 0) return IDXC_OK;
+    if (!device_info().ok) return IDXC_ERR_CUDA;
+    g_launches += 1;
+    return launch_attn_weights(a, lse, beta, acc, ld, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_evict_select(const float* acc, int64_t ld, const int32_t* lens, int64_t B, int budget, int recent,
+                              int32_t* keep_out, int32_t* new_lens_out, void* cuda_stream) {
+    if (B < 0 || B > 65535 || ld < 0 || ld > (int64_t(1) << 30) || budget < 1 || budget > (1 << 30) || recent < 0 || recent > budget)
+        return IDXC_ERR_INVALID_ARG;
+    if (B == 0) return IDXC_OK;
+    if ((ld > 0 && !acc) || !lens || !keep_out || !new_lens_out || lens == new_lens_out || !aligned(acc, 4) || !aligned(lens, 4) ||
+        !aligned(keep_out, 4) || !aligned(new_lens_out, 4))
+        return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_evict_select(acc, ld, lens, static_cast<int>(B), budget, recent, keep_out, new_lens_out,
+                               static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t src_rows, int64_t dst_rows,
+                              const int64_t* src_base, const int64_t* dst_base, const int32_t* keep, int ld_keep,
+                              const int32_t* n_keep, int64_t B, void* cuda_stream) {
+    if (B < 0 || B > 65535 || row_bytes < 4 || (row_bytes & 3) || row_bytes > (1 << 20) || src_rows < 0 || dst_rows < 0 || ld_keep < 0 ||
+        src_rows > (int64_t(1) << 40) || dst_rows > (int64_t(1) << 40))
+        return IDXC_ERR_INVALID_ARG;
+    if (B == 0 || ld_keep == 0 || src_rows == 0 || dst_rows == 0) return IDXC_OK;
+    if (!src || !dst || !src_base || !dst_base || !keep || !n_keep || !aligned(src, 4) || !aligned(dst, 4) || !aligned(src_base, 8) ||
+        !aligned(dst_base, 8) || !aligned(keep, 4) || !aligned(n_keep, 4))
+        return IDXC_ERR_INVALID_ARG;
+    if (src == dst) {
+        if (src_base != dst_base || src_rows != dst_rows) return IDXC_ERR_INVALID_ARG;
+    } else {
+        const uintptr_t s0 = reinterpret_cast<uintptr_t>(src), d0 = reinterpret_cast<uintptr_t>(dst);
+        if (s0 < d0 + static_cast<uintptr_t>(dst_rows) * row_bytes && d0 < s0 + static_cast<uintptr_t>(src_rows) * row_bytes)
+            return IDXC_ERR_INVALID_ARG;
+    }
+    g_launches += 1;
+    return launch_compact_rows(src, dst, row_bytes, src_rows, dst_rows, src_base, dst_base, keep, ld_keep, n_keep, static_cast<int>(B),
+                               static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
 idxc_status idxc_selftest_bounded_wait(uint32_t wait_cycles, void* cuda_stream) {
     if (!device_info().ok) return IDXC_ERR_CUDA;
     const long long budget = wait_cycles > 100000000u ? 100000000LL : static_cast<long long>(wait_cycles);

@@ -116,6 +116,34 @@ cudaError_t launch_sparse_attn(const void* kv, const int32_t* topk, const int64_
                                const CUtensorMap& q_map, unsigned int* status, int sm_count,
                                cudaStream_t stream);
 
+// Attention over latent cache rows, dense or over a selection (latent_attn.cu, attn_weights.cu).
+struct LatentArgs {
+    const void* q;              // [B, n_step, H, 576] bf16
+    const void* kv;             // rows of 1152 (bf16) or 416 (4-bit) bytes
+    int q4;
+    int64_t n_kv;
+    const int64_t* kv_base;     // [B] or nullptr
+    const int32_t* lens;        // dense: [B]; selected: nullptr
+    const int32_t* topk;        // selected: [B, k_top]; dense: nullptr
+    int k_top;
+    int64_t B;
+    int n_step;
+    int64_t max_len;            // dense: host bound on lens; selected: k_top
+    int H;
+    float scale;
+};
+cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, cudaStream_t stream);
+cudaError_t launch_attn_weights(const LatentArgs& a, const float* lse, float beta, float* acc, int64_t ld, cudaStream_t stream);
+
+// latent_cache.cu
+cudaError_t launch_quantize_q4(const void* x, int64_t n, void* cache, int64_t cache_rows, const int64_t* dst_rows, cudaStream_t stream);
+cudaError_t launch_dequantize_q4(const void* cache, int64_t cache_rows, const int64_t* src_rows, int64_t n, void* out, cudaStream_t stream);
+cudaError_t launch_compact_rows(const void* src, void* dst, int row_bytes, int64_t src_rows, int64_t dst_rows, const int64_t* src_base,
+                                const int64_t* dst_base, const int32_t* keep, int ld_keep, const int32_t* n_keep, int B, cudaStream_t stream);
+// evict.cu
+cudaError_t launch_evict_select(const float* acc, int64_t ld, const int32_t* lens, int B, int budget, int recent, int32_t* keep,
+                                int32_t* new_lens, cudaStream_t stream);
+
 // selftest.cu: one tiny kernel whose only wait can never be satisfied; it must record a time-out in
 // `status` after `budget_cycles` and return.
 cudaError_t launch_selftest_bounded_wait(unsigned int* status, long long budget_cycles, cudaStream_t stream);

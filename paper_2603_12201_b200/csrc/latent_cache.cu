@@ -1,0 +1,206 @@
+// Rows of a latent cache: written in 4 bits (with append), read back, and moved when a cache is compacted.
+#include "kernels.h"
+#include "latent_format.cuh"
+
+namespace idxc {
+namespace {
+
+constexpr int kRowsPerWarp = 4;          // rows whose loads a warp keeps in flight
+constexpr int kRowThreads = 256;
+
+__device__ __forceinline__ float bf16_at(const uint4& v, int i) {
+    const uint32_t w = i < 2 ? v.x : (i < 4 ? v.y : (i < 6 ? v.z : v.w));
+    return __uint_as_float((i & 1) ? (w & 0xFFFF0000u) : (w << 16));
+}
+
+// The smallest scale of 5 significant bits that holds `amax` in 7 steps: amax / 7 rounded up past its top 4 mantissa bits.
+// At least 2^-100 (code * scale then stays far from the subnormals), at most 1.125 * 2^125 (7 steps stay finite).
+__device__ __forceinline__ float q4_scale(float amax) {
+    const float s = __fdiv_rn(fmaxf(amax, 7.f * 0x1p-100f), 7.f);
+    const float up = __uint_as_float((__float_as_uint(s) + 0x7FFFFu) & ~0x7FFFFu);
+    return fminf(up, 0x1.2p+125f);
+}
+
+// One word of codes from eight columns. The quotient is corrected by one residual step from the rounded reciprocal r of the
+// scale, which gives the correctly rounded x / scale (every product with a 5-bit scale is exact in the FMA), so that a value
+// halfway between two codes is seen as such and goes to the even one.
+__device__ __forceinline__ uint32_t q4_word(const uint4& v, float scale, float r) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = bf16_at(v, i);
+        const float q = x * r;
+        const float y = __fmaf_rn(-__fmaf_rn(q, scale, -x), r, q);
+        const int code = __float2int_rn(fminf(fmaxf(y, -7.f), 7.f));
+        const int nibble = (i & 1) * 4 + (i >> 1);
+        word |= static_cast<uint32_t>(code + 8) << (4 * nibble);
+    }
+    return word;
+}
+
+// A warp takes kRowsPerWarp rows; lane l holds the 8-column pieces l and l + 32 of a row's value columns, four lanes a group.
+__global__ void __launch_bounds__(kRowThreads)
+quantize_q4_kernel(const uint4* __restrict__ x, int64_t n, uint8_t* __restrict__ cache, int64_t cache_rows, const int64_t* __restrict__ dst_rows) {
+    const int lane = threadIdx.x & 31;
+    const int64_t row0 = (static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRowsPerWarp;
+    uint4 v[kRowsPerWarp][2], rope[kRowsPerWarp];
+    int64_t dst[kRowsPerWarp];
+#pragma unroll
+    for (int u = 0; u < kRowsPerWarp; ++u) {
+        const bool in = row0 + u < n;
+        const uint4* src = x + (row0 + u) * (kLatentCols / 8);
+        v[u][0] = in ? __ldg(src + lane) : make_uint4(0, 0, 0, 0);
+        v[u][1] = in ? __ldg(src + 32 + lane) : make_uint4(0, 0, 0, 0);
+        rope[u] = in && lane < 8 ? __ldg(src + 64 + lane) : make_uint4(0, 0, 0, 0);
+        dst[u] = in ? (dst_rows ? __ldg(dst_rows + row0 + u) : row0 + u) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsPerWarp; ++u) {
+        if (dst[u] < 0 || dst[u] >= cache_rows) continue;          // warp-uniform; a row outside the cache is not written
+        uint8_t* out = cache + dst[u] * kLatentQ4RowBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float amax = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(bf16_at(v[u][h], i)));
+            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+            const float s = q4_scale(amax);
+            reinterpret_cast<uint32_t*>(out)[h * 32 + lane] = q4_word(v[u][h], s, __frcp_rn(s));
+            if ((lane & 3) == 0)
+                reinterpret_cast<uint16_t*>(out + kLatentQ4ScaleOff)[h * 8 + (lane >> 2)] = static_cast<uint16_t>(__float_as_uint(s) >> 16);
+        }
+        if (lane < 8) reinterpret_cast<uint4*>(out + kLatentQ4RopeOff)[lane] = rope[u];
+    }
+}
+
+// src_rows == nullptr: row r of the output is cache row r. A source row outside the cache gives zeros.
+__global__ void __launch_bounds__(kRowThreads)
+dequantize_q4_kernel(const uint8_t* __restrict__ cache, int64_t cache_rows, const int64_t* __restrict__ src_rows, int64_t n, uint4* __restrict__ out) {
+    const int lane = threadIdx.x & 31;
+    const int64_t row0 = (static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRowsPerWarp;
+    uint32_t word[kRowsPerWarp][2];
+    uint16_t scale[kRowsPerWarp][2];
+    uint4 rope[kRowsPerWarp];
+#pragma unroll
+    for (int u = 0; u < kRowsPerWarp; ++u) {
+        const int64_t src = row0 + u < n ? (src_rows ? __ldg(src_rows + row0 + u) : row0 + u) : -1;
+        const bool in = src >= 0 && src < cache_rows;
+        const uint8_t* p = cache + (in ? src : 0) * kLatentQ4RowBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            word[u][h] = in ? __ldg(reinterpret_cast<const uint32_t*>(p) + h * 32 + lane) : 0x88888888u;
+            scale[u][h] = in ? __ldg(reinterpret_cast<const uint16_t*>(p + kLatentQ4ScaleOff) + h * 8 + (lane >> 2)) : static_cast<uint16_t>(0);
+        }
+        rope[u] = in && lane < 8 ? __ldg(reinterpret_cast<const uint4*>(p + kLatentQ4RopeOff) + lane) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsPerWarp; ++u) {
+        if (row0 + u >= n) continue;
+        uint4* dst = out + (row0 + u) * (kLatentCols / 8);
+        dst[lane] = dequant8_q4(word[u][0], scale_pair(scale[u][0]));
+        dst[32 + lane] = dequant8_q4(word[u][1], scale_pair(scale[u][1]));
+        if (lane < 8) dst[64 + lane] = rope[u];
+    }
+}
+
+// ---------------------------------------------------------------- compaction
+// Row j of sequence b of the destination <- row keep[b][j] of sequence b of the source, j < n_keep[b], in units of T.
+// Out of place the moves are independent.
+template <typename T>
+__global__ void __launch_bounds__(256)
+compact_copy_kernel(const T* __restrict__ src, T* __restrict__ dst, int units, int64_t src_rows, int64_t dst_rows,
+                    const int64_t* __restrict__ src_base, const int64_t* __restrict__ dst_base, const int32_t* __restrict__ keep, int ld_keep,
+                    const int32_t* __restrict__ n_keep) {
+    const int b = blockIdx.y;
+    const int n = min(max(__ldg(n_keep + b), 0), ld_keep);
+    const int64_t sb = __ldg(src_base + b), db = __ldg(dst_base + b);
+    const int64_t total = static_cast<int64_t>(n) * units;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const int j = static_cast<int>(i / units);
+        const int u = static_cast<int>(i - static_cast<int64_t>(j) * units);
+        const int64_t k = __ldg(keep + static_cast<int64_t>(b) * ld_keep + j);
+        const int64_t s = sb + k, d = db + j;
+        if (k < 0 || s < 0 || s >= src_rows || d < 0 || d >= dst_rows) continue;
+        dst[d * units + u] = src[s * units + u];
+    }
+}
+
+// In place: keep is ascending, so keep[j] >= j, and a chunk of destination rows [a, b) overwrites no source of a later chunk
+// (those are rows >= b). One CTA walks the chunks of one slice of a sequence's columns in order; within a chunk every load
+// is done before the first store. Slices of columns are independent, which is where the parallelism comes from.
+constexpr int kMoveThreads = 256;
+constexpr int kMoveRowsPerThread = 8;
+template <typename T>
+__global__ void __launch_bounds__(kMoveThreads)
+compact_in_place_kernel(T* __restrict__ rows, int units, int slice_units, int64_t n_rows, const int64_t* __restrict__ base,
+                        const int32_t* __restrict__ keep, int ld_keep, const int32_t* __restrict__ n_keep) {
+    const int b = blockIdx.y;
+    const int n = min(max(__ldg(n_keep + b), 0), ld_keep);
+    const int64_t sb = __ldg(base + b);
+    const int u0 = blockIdx.x * slice_units;
+    const int width = min(slice_units, units - u0);
+    const int per_pass = kMoveThreads / slice_units;          // rows that one pass of the CTA covers
+    const int my_row = threadIdx.x / slice_units, my_unit = threadIdx.x % slice_units;
+    const bool active = my_row < per_pass && my_unit < width;
+    const int32_t* k_row = keep + static_cast<int64_t>(b) * ld_keep;
+    for (int j0 = 0; j0 < n; j0 += per_pass * kMoveRowsPerThread) {
+        T v[kMoveRowsPerThread];
+        bool move[kMoveRowsPerThread];
+#pragma unroll
+        for (int i = 0; i < kMoveRowsPerThread; ++i) {
+            const int j = j0 + i * per_pass + my_row;
+            const int64_t k = active && j < n ? __ldg(k_row + j) : -1;
+            move[i] = k > j && sb + j >= 0 && sb + k < n_rows;       // keep[j] == j: the row is where it belongs
+            if (move[i]) v[i] = rows[(sb + k) * units + u0 + my_unit];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMoveRowsPerThread; ++i)
+            if (move[i]) rows[(sb + j0 + i * per_pass + my_row) * units + u0 + my_unit] = v[i];
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_quantize_q4(const void* x, int64_t n, void* cache, int64_t cache_rows, const int64_t* dst_rows, cudaStream_t stream) {
+    const int64_t per_cta = kRowThreads / 32 * kRowsPerWarp;
+    quantize_q4_kernel<<<static_cast<unsigned>((n + per_cta - 1) / per_cta), kRowThreads, 0, stream>>>(
+        static_cast<const uint4*>(x), n, static_cast<uint8_t*>(cache), cache_rows, dst_rows);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_dequantize_q4(const void* cache, int64_t cache_rows, const int64_t* src_rows, int64_t n, void* out, cudaStream_t stream) {
+    const int64_t per_cta = kRowThreads / 32 * kRowsPerWarp;
+    dequantize_q4_kernel<<<static_cast<unsigned>((n + per_cta - 1) / per_cta), kRowThreads, 0, stream>>>(
+        static_cast<const uint8_t*>(cache), cache_rows, src_rows, n, static_cast<uint4*>(out));
+    return cudaGetLastError();
+}
+
+template <typename T>
+static cudaError_t compact_as(const void* src, void* dst, int row_bytes, int64_t src_rows, int64_t dst_rows, const int64_t* src_base,
+                              const int64_t* dst_base, const int32_t* keep, int ld_keep, const int32_t* n_keep, int B, cudaStream_t stream) {
+    const int units = row_bytes / static_cast<int>(sizeof(T));
+    if (src == dst) {
+        const int slice = units < 8 ? units : 8;
+        const dim3 grid(static_cast<unsigned>((units + slice - 1) / slice), static_cast<unsigned>(B));
+        compact_in_place_kernel<T><<<grid, kMoveThreads, 0, stream>>>(static_cast<T*>(dst), units, slice, dst_rows, src_base, keep, ld_keep, n_keep);
+    } else {
+        int64_t blocks = (static_cast<int64_t>(ld_keep) * units + 1023) / 1024;
+        const int64_t cap = 2 * 8 * 148 / B + 1;
+        if (blocks > cap) blocks = cap;
+        compact_copy_kernel<T><<<dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(B)), 256, 0, stream>>>(
+            static_cast<const T*>(src), static_cast<T*>(dst), units, src_rows, dst_rows, src_base, dst_base, keep, ld_keep, n_keep);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_compact_rows(const void* src, void* dst, int row_bytes, int64_t src_rows, int64_t dst_rows, const int64_t* src_base,
+                                const int64_t* dst_base, const int32_t* keep, int ld_keep, const int32_t* n_keep, int B, cudaStream_t stream) {
+    const uintptr_t both = reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) | static_cast<uintptr_t>(row_bytes);
+    if ((both & 15) == 0)
+        return compact_as<uint4>(src, dst, row_bytes, src_rows, dst_rows, src_base, dst_base, keep, ld_keep, n_keep, B, stream);
+    return compact_as<uint32_t>(src, dst, row_bytes, src_rows, dst_rows, src_base, dst_base, keep, ld_keep, n_keep, B, stream);
+}
+
+}  // namespace idxc
