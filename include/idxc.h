@@ -356,7 +356,8 @@ idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int6
  *   out      DEVICE bf16 [B, n_step, H, 512], 16-byte aligned    lse NULL or DEVICE fp32 [B, n_step, H]
  *   workspace DEVICE, 256-byte aligned, idxc_latent_attention_workspace_bytes(B, n_step, max_len, H) bytes; scratch, one per
  *            call in flight
- * Supported: d_qk = 576, d_v = 512, 1 <= H <= 128, n_step >= 1, B * n_step * H < 2^31, max_len <= 2^30, n_kv < 2^31.
+ * Supported: d_qk = 576, d_v = 512, 1 <= H <= 128, n_step >= 1, B * n_step * H < 2^31, max_len <= 2^30, n_kv < 2^31,
+ * B * (n_step * H rounded up to 64s) * max_len below 2^42.
  * Rows that no token sees are never read. Arithmetic: bf16 products with fp32 accumulation, fp32 softmax, probabilities
  * rounded to bf16 for the second product, bf16 output. The result does not depend on what else runs.
  *

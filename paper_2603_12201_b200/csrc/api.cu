@@ -547,7 +547,7 @@ idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int6
 
 namespace {
 
-// What the calls over latent rows have in common. 0 means "go on" is IDXC_OK here; sizes first, then pointers.
+// What the calls over latent rows have in common: sizes first, then pointers.
 idxc_status check_latent(const LatentArgs& a, int d_qk) {
     if (a.B < 0 || a.n_step < 1 || a.H < 1 || a.n_kv < 0 || a.max_len < 0 || d_qk < 1) return IDXC_ERR_INVALID_ARG;
     if (a.max_len > (int64_t(1) << 30) || a.n_kv >= (int64_t(1) << 31)) return IDXC_ERR_INVALID_ARG;
@@ -569,12 +569,23 @@ idxc_status run_latent_attn(const LatentArgs& a, int d_qk, int d_v, void* out, f
     if (st != IDXC_OK) return st;
     if (d_v != 512) return IDXC_ERR_UNSUPPORTED;
     if (a.B == 0) return IDXC_OK;
+    if (!latent_attn_fits(a.B, a.n_step, a.max_len, a.H)) return IDXC_ERR_INVALID_ARG;
     if (!out || !aligned(out, 16) || (lse && !aligned(lse, 4))) return IDXC_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < idxc_latent_attention_workspace_bytes(a.B, a.n_step, a.max_len, a.H))
         return IDXC_ERR_WORKSPACE;
-    if (!device_info().ok) return IDXC_ERR_CUDA;
-    g_launches += 1;
-    return launch_latent_attn(a, out, lse, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+    DeviceInfo& di = device_info();
+    if (!di.ok) return IDXC_ERR_CUDA;
+    CUtensorMap q_map, kv_map;
+    if (!encode_operand_map(&q_map, a.q, a.B * a.n_step * a.H, 576, false, 64)) return IDXC_ERR_CUDA;
+    LatentArgs run = a;
+    if (a.n_kv == 0 && !a.topk) run.max_len = 0;               // no rows: every token sees nothing
+    if (a.q4 || a.n_kv == 0) kv_map = q_map;                   // not read
+    else if (!encode_operand_map(&kv_map, a.kv, a.n_kv, 576, false, 64)) return IDXC_ERR_CUDA;
+    int n_l = 0;
+    const cudaError_t e = launch_latent_attn(run, out, lse, workspace, q_map, kv_map, di.status_ptr, di.sm_count,
+                                             static_cast<cudaStream_t>(cuda_stream), &n_l);
+    g_launches += n_l;
+    return e == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
 }
 
 }  // namespace
@@ -582,8 +593,10 @@ idxc_status run_latent_attn(const LatentArgs& a, int d_qk, int d_v, void* out, f
 extern "C" {
 
 size_t idxc_latent_attention_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H) {
-    if (B <= 0 || n_step < 1 || max_len < 0 || H < 1) return 0;
-    return 256;
+    if (B <= 0 || n_step < 1 || max_len < 0 || H < 1 || max_len > (int64_t(1) << 30) || B >= (int64_t(1) << 31) ||
+        static_cast<int64_t>(n_step) * H >= (int64_t(1) << 31))
+        return 0;
+    return latent_attn_workspace_bytes(B, n_step, max_len, H);
 }
 
 idxc_status idxc_latent_attention(const void* q, const void* kv, idxc_latent_format fmt, int64_t n_kv, const int64_t* kv_base,

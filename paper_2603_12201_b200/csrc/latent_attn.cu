@@ -1,0 +1,839 @@
+// Attention over latent cache rows, one shared row per token for all heads (keys = its 576 columns, values = its first 512):
+// dense over a sequence's rows held in bf16 or 4 bits, and over a selection of 4-bit rows.
+//
+// One pass over the rows. A CTA holds 64 query rows (heads x new tokens of one sequence): its fp32 output, 64 x 512, is then
+// half of tensor memory, so scores, softmax and both halves of the output are done tile by tile with nothing saved or read
+// twice. tcgen05.mma with M = 64 puts row r on TMEM lane 32 (r / 16) + r % 16 (+ 16 with a lane offset of 16, measured), so
+// the two 256-column halves of O lie on top of each other in 256 columns. M = 64 issues at half the M = 128 rate (N = 64: 32
+// clocks, N = 256: 128), 2176 clocks of tensor pipe per 64-row tile; more than 64 query rows take two CTAs that walk
+// the same tiles side by side, the second reading them from the L2.
+//
+// Work: the tiles of all sequences, laid end to end, are cut into equal runs, one per CTA (pair). A run may start and end
+// inside a sequence: such a piece leaves a normalised fp32 result and its log-sum-exp in the workspace, and a merge kernel
+// weighs the pieces. A run has at most two of them, so the workspace does not grow with the work. A small plan kernel
+// computes the cuts from the lengths on the device.
+//
+// Shared memory: Q 9 blocks of [64 rows x 128 B] | 2 stages x 9 blocks of [64 cache rows x 128 B] | P [64 x 128 B], all in the
+// 128-byte swizzle. A block of cache rows is at once the K-major B operand of Q K^T and the MN-major B operand of P V. A stage
+// is two slots: "A" = blocks 0..3 (the first half of V), "B" = blocks 4..8.
+// TMEM: O [0, 256), both halves | S double-buffered [256, 320), [320, 384).
+// Order of the tensor pipe: S(i+1) | P(i) V(i), so that a tile's softmax runs under the next tile's scores.
+// bf16 rows come by TMA (the tail of a sequence is cleared in shared memory: rows behind it may hold NaN). 4-bit rows are read
+// into registers a tile ahead by eight warps and expanded into the stage (exact, see latent_format.cuh).
+#include <cuda_bf16.h>
+
+#include "kernels.h"
+#include "latent_format.cuh"
+#include "ptx_sm100.cuh"
+
+namespace idxc {
+namespace {
+
+constexpr int kTile = 64;                           // cache rows of a tile
+constexpr int kRows = 64;                           // query rows of a CTA
+constexpr int kBlocks = 9;                          // 64-column blocks of a row
+constexpr int kSlotA = 4;                           // blocks of slot A
+constexpr uint32_t kBlockBytes = kTile * 128;
+constexpr uint32_t kStageBytes = kBlocks * kBlockBytes;
+constexpr uint32_t kQBytes = kBlocks * kRows * 128;
+constexpr uint32_t kPBytes = kRows * 128;
+constexpr uint32_t kBarBytes = 512;
+constexpr uint32_t kSmemBytes = kQBytes + 2 * kStageBytes + kPBytes + kBarBytes + 1024;
+static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
+constexpr uint32_t kColS = 256;
+constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
+constexpr int kWarpsBf16 = 8;                       // 0 MMA | 1 rows (TMA) | 2 Q | 3 idle | 4..7 softmax
+constexpr int kWarpsQ4 = 16;                        // 0 MMA | 1 idle | 2 Q | 3 idle | 4..7 softmax | 8..15 rows
+constexpr int kLoadWarps = 8;
+
+struct Params {
+    LatentArgs a;
+    const int32_t* tiles;        // [units] tiles of every unit
+    const int2* starts;          // [groups + 1] (unit, tile) at which a group's run begins
+    const int32_t* runs;         // [groups + 1] first tile of the run in the end-to-end order
+    int64_t units;               // (sequence, block of 64 * ways query rows)
+    int blocks_per_seq;          // units of a sequence
+    int ways;                    // CTAs of a group: 1 or 2, each 64 rows
+    int groups;
+    float scale_log2;
+    __nv_bfloat16* out;
+    float* lse;
+    float* part_out;             // [groups][2][ways][64][512]
+    float* part_lse;             // [groups][2][ways][64]
+    unsigned int* status;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// ---------------------------------------------------------------- plan
+// Selected rows: tiles of query t up to its last usable entry.
+__global__ void __launch_bounds__(128)
+latent_count_kernel(const LatentArgs a, int32_t* __restrict__ tiles) {
+    __shared__ int s_last[4];
+    const int64_t t = blockIdx.x;
+    const int64_t base = a.kv_base ? __ldg(a.kv_base + t) : 0;
+    const int32_t* row = a.topk + t * a.k_top;
+    int last = 0;
+#pragma unroll 4
+    for (int j = threadIdx.x; j < a.k_top; j += 128) {
+        const int64_t i = __ldg(row + j);
+        if (i >= 0 && base + i >= 0 && base + i < a.n_kv) last = j + 1;
+    }
+    last = __reduce_max_sync(0xFFFFFFFFu, last);
+    if ((threadIdx.x & 31) == 0) s_last[threadIdx.x >> 5] = last;
+    __syncthreads();
+    if (threadIdx.x == 0) tiles[t] = (max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3])) + kTile - 1) / kTile;
+}
+
+// Tiles of every unit (dense; selected: already counted), their running sum, and where the equal runs of the groups begin.
+constexpr int kPlanThreads = 1024;
+__global__ void __launch_bounds__(kPlanThreads)
+latent_plan_kernel(const LatentArgs a, int64_t units, int blocks_per_seq, int groups, int32_t* __restrict__ tiles, int2* __restrict__ starts,
+                   int32_t* __restrict__ runs) {
+    __shared__ int s_sum[32];
+    const int64_t per = (units + kPlanThreads - 1) / kPlanThreads;
+    const int64_t u0 = threadIdx.x * per, u1 = min(u0 + per, units);
+    int sum = 0;
+    for (int64_t u = u0; u < u1; ++u) {
+        int n;
+        if (a.topk) {
+            n = tiles[u];
+        } else {
+            const int64_t len = __ldg(a.lens + u / blocks_per_seq);
+            n = static_cast<int>((min(max(len, int64_t(0)), a.max_len) + kTile - 1) / kTile);
+            tiles[u] = n;
+        }
+        sum += n;
+    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    int before = incl - sum, total = 0;
+    for (int w = 0; w < 32; ++w) {
+        if (w < warp) before += s_sum[w];
+        total += s_sum[w];
+    }
+    for (int g = threadIdx.x; g <= groups; g += kPlanThreads) runs[g] = static_cast<int>(static_cast<int64_t>(total) * g / groups);
+    if (total == 0) return;
+    for (int64_t u = u0; u < u1; ++u) {
+        const int n = tiles[u];
+        // groups whose first tile, total * g / groups rounded down, lies in this unit
+        for (int64_t g = (static_cast<int64_t>(before) * groups + total - 1) / total; g < groups; ++g) {
+            const int first = static_cast<int>(static_cast<int64_t>(total) * g / groups);
+            if (first >= before + n) break;
+            starts[g] = make_int2(static_cast<int>(u), first - before);
+        }
+        before += n;
+    }
+}
+
+// ---------------------------------------------------------------- the walk of a group over its run
+struct Piece {
+    int64_t unit;
+    int t0, n;            // first tile, number of tiles
+    bool whole;           // all tiles of the unit
+};
+struct Walk {
+    const int32_t* tiles;
+    int64_t unit;
+    int t, left;
+    __device__ __forceinline__ Walk(const Params& p, int group) : tiles(p.tiles), unit(0), t(0), left(__ldg(p.runs + group + 1) - __ldg(p.runs + group)) {
+        if (left > 0) {
+            const int2 s = __ldg(p.starts + group);
+            unit = s.x;
+            t = s.y;
+        }
+    }
+    __device__ __forceinline__ bool next(Piece& pc) {
+        if (left <= 0) return false;
+        int nt = __ldg(tiles + unit);
+        while (nt == 0) nt = __ldg(tiles + ++unit);         // left > 0: a unit with tiles follows
+        pc.unit = unit;
+        pc.t0 = t;
+        pc.n = min(nt - t, left);
+        pc.whole = t == 0 && pc.n == nt;
+        left -= pc.n;
+        ++unit;
+        t = 0;
+        return true;
+    }
+};
+
+// ---------------------------------------------------------------- main kernel
+template <bool Q4>
+__global__ void __launch_bounds__((Q4 ? kWarpsQ4 : kWarpsBf16) * 32, 1)
+latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map, const Params p) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* q_smem = smem;
+    uint8_t* stage_smem = smem + kQBytes;
+    uint8_t* p_smem = stage_smem + 2 * kStageBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(p_smem + kPBytes);
+    const uint32_t bar_q_full = smem_u32(bars + 0);
+    const uint32_t bar_q_empty = smem_u32(bars + 1);
+    const uint32_t bar_slot_full = smem_u32(bars + 2);       // [2 stages][A, B]
+    const uint32_t bar_slot_empty = smem_u32(bars + 6);
+    const uint32_t bar_s_full = smem_u32(bars + 10);         // [2]
+    const uint32_t bar_p_ready = smem_u32(bars + 12);
+    const uint32_t bar_pv_done = smem_u32(bars + 13);
+    const uint32_t bar_o_free = smem_u32(bars + 14);
+    const uint32_t bar_tail = smem_u32(bars + 15);
+    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 16);
+    volatile uint32_t* abort_flag = tmem_base_slot + 1;
+    uint8_t* mask_smem = reinterpret_cast<uint8_t*>(bars + 18);    // [2 stages][16]: usable rows 4k .. 4k+3 of the tile
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = blockIdx.x / p.ways, way = blockIdx.x - group * p.ways;
+    const int seq_rows = p.a.n_step * p.a.H;
+    // query rows of this CTA in a unit: first row within the sequence, and how many
+    auto rows_of = [&](int64_t unit, int64_t& seq, int& r0) -> int {
+        seq = unit / p.blocks_per_seq;
+        r0 = (static_cast<int>(unit - seq * p.blocks_per_seq) * p.ways + way) * kRows;
+        return min(kRows, seq_rows - r0);
+    };
+    auto seq_len = [&](int64_t seq) -> int64_t {
+        return p.a.topk ? p.a.k_top : min(max(static_cast<int64_t>(__ldg(p.a.lens + seq)), int64_t(0)), p.a.max_len);
+    };
+
+    if (threadIdx.x == 0) {
+        mbar_init(bar_q_full, 1);
+        mbar_init(bar_q_empty, 1);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(bar_slot_full + 8 * i, Q4 ? kLoadWarps : 1);
+            mbar_init(bar_slot_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) mbar_init(bar_s_full + 8 * i, 1);
+        mbar_init(bar_p_ready, 4);
+        mbar_init(bar_pv_done, 1);
+        mbar_init(bar_o_free, 4);
+        mbar_init(bar_tail, 1);
+        *abort_flag = 0u;
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(tmem_base_slot), 512);
+        tmem_relinquish_alloc_permit();
+    }
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    tcgen05_fence_after_sync();
+    const uint32_t tmem_base = *tmem_base_slot;
+
+    Walk walk(p, group);
+    Piece pc;
+    int64_t seq;
+    int r0;
+    bool ok = true;
+    uint32_t tile = 0, item = 0;          // counted over the whole kernel: stages, buffers and phases follow from them
+    auto give_up = [&](unsigned int code) {
+        *abort_flag = 1u;
+        atomicCAS(p.status, 0u, code);
+    };
+    auto wait_warp = [&](uint32_t bar, uint32_t parity, unsigned sleep_ns = 0) -> bool {
+        return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, kWaitCycleBudget, sleep_ns));
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ MMA issuer (warp-uniform, one elected lane issues)
+        constexpr uint32_t kIdescS = umma_idesc(1, 1, kRows, kTile);
+        constexpr uint32_t kIdescPV = umma_idesc(1, 1, kRows, 256) | kUmmaBMajorMN;
+        const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
+        const uint64_t p_desc = umma_smem_desc_sw128(smem_u32(p_smem));
+        auto issue_s = [&](uint32_t tl) -> bool {
+            const uint32_t st = tl & 1u, ph = (tl >> 1) & 1u;
+            const uint32_t d = tmem_base + kColS + st * 64;
+            uint64_t a_desc = q_desc, b_desc = umma_smem_desc_sw128(smem_u32(stage_smem + st * kStageBytes));
+#pragma unroll 1
+            for (int b = 0; b < kBlocks; ++b) {
+                if (b == 0 || b == kSlotA) {
+                    if (!wait_warp(bar_slot_full + 8 * (2 * st + (b != 0)), ph)) return false;
+                    tcgen05_fence_after_sync();
+                }
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) umma_f16_elect_acc(d, a_desc + ks * 2, b_desc + ks * 2, kIdescS, (b | ks) ? 1u : 0u);
+                a_desc += kRows * 128 / 16;
+                b_desc += kBlockBytes / 16;
+            }
+            umma_commit_elect(bar_s_full + 8 * st);
+            return true;
+        };
+        while (ok && walk.next(pc)) {
+            if (rows_of(pc.unit, seq, r0) <= 0) continue;
+            ok = wait_warp(bar_q_full, item & 1u) && issue_s(tile);
+            if (ok && pc.n == 1) umma_commit_elect(bar_q_empty);
+            for (int i = 0; i < pc.n && ok; ++i, ++tile) {
+                if (i + 1 < pc.n) {
+                    ok = issue_s(tile + 1);
+                    if (!ok) break;
+                    if (i + 2 == pc.n) umma_commit_elect(bar_q_empty);       // the piece's last scores
+                }
+                if (i == 0) ok = wait_warp(bar_o_free, (item & 1u) ^ 1u);    // the previous piece's output has been read
+                ok = ok && wait_warp(bar_p_ready, tile & 1u);
+                if (!ok) break;
+                tcgen05_fence_after_sync();
+                const uint32_t st = tile & 1u;
+                const uint64_t v_desc = umma_smem_desc_sw128_mn(smem_u32(stage_smem + st * kStageBytes), kBlockBytes);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int ks = 0; ks < kTile / 16; ++ks)
+                        umma_f16_elect_acc(tmem_base + (static_cast<uint32_t>(h * 16) << 16), p_desc + ks * 2,
+                                           v_desc + h * (kSlotA * kBlockBytes / 16) + ks * (16 * 128 / 16), kIdescPV, (i | ks) ? 1u : 0u);
+                    umma_commit_elect(bar_slot_empty + 8 * (2 * st + h));
+                }
+                umma_commit_elect(bar_pv_done);
+            }
+            ++item;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_MMA);
+    } else if (warp == 2) {
+        // ------------------------------------------------------------ Q
+        if (lane == 0) {
+            tma_prefetch_desc(&q_map);
+            while (ok && walk.next(pc)) {
+                if (rows_of(pc.unit, seq, r0) <= 0) continue;
+                ok = mbar_wait(bar_q_empty, (item & 1u) ^ 1u, abort_flag, kWaitCycleBudget, 200);
+                if (!ok) break;
+                mbar_arrive_expect_tx(bar_q_full, kQBytes);
+                for (int b = 0; b < kBlocks; ++b)
+                    tma_load_2d(smem_u32(q_smem + b * kRows * 128), &q_map, bar_q_full, b * 64, static_cast<int>(seq * seq_rows + r0));
+                ++item;
+            }
+            if (!ok) give_up(DEV_TIMEOUT_PRODUCER);
+        }
+    } else if (!Q4 && warp == 1) {
+        // ------------------------------------------------------------ bf16 rows
+        if (lane == 0) tma_prefetch_desc(&kv_map);
+        uint32_t tails = 0;
+        while (ok && walk.next(pc)) {
+            if (rows_of(pc.unit, seq, r0) <= 0) continue;
+            const int64_t len = seq_len(seq);
+            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            for (int i = 0; i < pc.n && ok; ++i, ++tile) {
+                const uint32_t st = tile & 1u, ph = ((tile >> 1) & 1u) ^ 1u;
+                uint8_t* dst = stage_smem + st * kStageBytes;
+                const int64_t at = static_cast<int64_t>(pc.t0 + i) * kTile;
+                // coordinates outside the cache read zeros; a base far outside is brought to the nearest such place
+                const int64_t first = min(max(base + at, static_cast<int64_t>(-kTile)), p.a.n_kv);
+                const bool tail = len - at < kTile;
+                ok = wait_warp(bar_slot_empty + 8 * (2 * st), ph, 20);
+                if (!ok) break;
+                if (!tail) {
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar_slot_full + 8 * (2 * st), kSlotA * kBlockBytes);
+                        for (int b = 0; b < kSlotA; ++b)
+                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &kv_map, bar_slot_full + 8 * (2 * st), b * 64, static_cast<int>(first));
+                    }
+                    ok = wait_warp(bar_slot_empty + 8 * (2 * st + 1), ph, 20);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar_slot_full + 8 * (2 * st + 1), (kBlocks - kSlotA) * kBlockBytes);
+                        for (int b = kSlotA; b < kBlocks; ++b)
+                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &kv_map, bar_slot_full + 8 * (2 * st + 1), b * 64, static_cast<int>(first));
+                    }
+                } else {
+                    // the sequence ends inside this tile: load, clear the rows behind its end, publish
+                    ok = wait_warp(bar_slot_empty + 8 * (2 * st + 1), ph, 20);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar_tail, kStageBytes);
+                        for (int b = 0; b < kBlocks; ++b)
+                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &kv_map, bar_tail, b * 64, static_cast<int>(first));
+                    }
+                    ok = wait_warp(bar_tail, tails & 1u);
+                    if (!ok) break;
+                    ++tails;
+                    const int valid = static_cast<int>(len - at);
+                    for (int b = 0; b < kBlocks; ++b)
+                        for (int o = valid * 128 + lane * 16; o < static_cast<int>(kBlockBytes); o += 512)
+                            *reinterpret_cast<uint4*>(dst + b * kBlockBytes + o) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar_slot_full + 8 * (2 * st));
+                        mbar_arrive(bar_slot_full + 8 * (2 * st + 1));
+                    }
+                }
+            }
+            ++item;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
+    } else if (Q4 && warp >= 8) {
+        // ------------------------------------------------------------ 4-bit rows
+        // A warp has rows 32 it + 4 w + rr (it = 0, 1; rr = 0..3) of every tile. Codes: lane = 8 block + 2 rr + half reads the 16
+        // bytes (one scale group) of column block `block` of the slot, half `half`, and stores four 16-byte chunks; eight
+        // consecutive lanes then store to eight different chunk positions (no bank conflicts). Positional columns: lane = 8 rr
+        // + chunk. Everything of the next tile is in registers before this tile's slot is free.
+        const int w = warp - 8;
+        const int blk = lane >> 3, rr = (lane >> 1) & 3, half = lane & 1;
+        const int rope_rr = lane >> 3, rope_ch = lane & 7;
+        const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
+        struct Tile { uint4 code[2][2]; uint16_t scale[2][2]; uint4 rope[2]; };      // [slot][it], [slot][it], [it]
+        Tile nx;
+        uint32_t nx_mask = 0;
+        int64_t len = 0, base = 0;
+        const int32_t* sel = nullptr;
+        int64_t src[2];                                       // cache rows of this lane's code rows in the tile being fetched, -1: none
+        auto locate = [&](int t) {                            // tile t of the piece's sequence
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                int64_t j = static_cast<int64_t>(t) * kTile + it * 32 + w * 4 + rr;
+                bool use = j < len;
+                if (sel != nullptr) {
+                    j = use ? __ldg(sel + j) : -1;
+                    use = j >= 0;
+                }
+                j += base;
+                src[it] = use && j >= 0 && j < p.a.n_kv ? j : -1;
+            }
+        };
+        auto fetch_codes = [&](int slot) {
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int cc = slot * 8 + blk * 2 + half;
+                const uint8_t* row = kv + (src[it] < 0 ? 0 : src[it]) * kLatentQ4RowBytes;
+                nx.code[slot][it] = src[it] < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(row) + cc);
+                nx.scale[slot][it] = src[it] < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(row + kLatentQ4ScaleOff) + cc);
+            }
+        };
+        auto fetch_rope = [&]() {
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int64_t s = __shfl_sync(0xFFFFFFFFu, src[it], rope_rr * 2);
+                nx.rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + rope_ch);
+            }
+        };
+        auto note_mask = [&]() {                              // bits 0..3: it = 0, bits 4..7: it = 1
+            uint32_t m = 0;
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const uint32_t v = __ballot_sync(0xFFFFFFFFu, src[it] >= 0);
+                m |= ((v & 1u) | ((v >> 1) & 2u) | ((v >> 2) & 4u) | ((v >> 3) & 8u)) << (4 * it);   // lanes 0, 2, 4, 6
+            }
+            nx_mask = m;
+        };
+        auto store_codes = [&](uint8_t* dst, int slot) {
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int r = it * 32 + w * 4 + rr;
+                uint8_t* row = dst + (slot * kSlotA + blk) * kBlockBytes + r * 128;
+                const __nv_bfloat162 s = scale_pair(nx.scale[slot][it]);
+                const uint4 c = nx.code[slot][it];
+                const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + (((half * 4 + v) ^ (r & 7)) << 4)) = dequant8_q4(word[v], s);
+            }
+        };
+        // the piece that the fetches are in runs ahead of the one whose tiles are stored
+        Walk ahead = walk;
+        Piece apc;
+        int ai = 0;
+        bool more = false;
+        auto ahead_piece = [&]() {
+            more = false;
+            while (ahead.next(apc)) {
+                int64_t s;
+                int rr0;
+                if (rows_of(apc.unit, s, rr0) <= 0) continue;
+                len = seq_len(s);
+                base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
+                sel = p.a.topk ? p.a.topk + s * p.a.k_top : nullptr;
+                ai = 0;
+                more = true;
+                return;
+            }
+        };
+        ahead_piece();
+        if (more) {
+            locate(apc.t0);
+            note_mask();
+            fetch_codes(0);
+            fetch_codes(1);
+            fetch_rope();
+        }
+        while (more && ok) {
+            // store tile `tile` (in registers), fetching the next as the registers come free
+            const uint32_t st = tile & 1u, ph = ((tile >> 1) & 1u) ^ 1u;
+            uint8_t* dst = stage_smem + st * kStageBytes;
+            const uint32_t mask = nx_mask;
+            if (++ai == apc.n) ahead_piece();
+            if (more) {
+                locate(apc.t0 + ai);
+                note_mask();
+            }
+            ok = wait_warp(bar_slot_empty + 8 * (2 * st), ph);
+            if (!ok) break;
+            store_codes(dst, 0);
+            if (lane == 0) {
+                mask_smem[st * 16 + w] = static_cast<uint8_t>(mask & 15u);
+                mask_smem[st * 16 + 8 + w] = static_cast<uint8_t>(mask >> 4);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_slot_full + 8 * (2 * st));
+            if (more) fetch_codes(0);
+            ok = wait_warp(bar_slot_empty + 8 * (2 * st + 1), ph);
+            if (!ok) break;
+            store_codes(dst, 1);
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int r = it * 32 + w * 4 + rope_rr;
+                *reinterpret_cast<uint4*>(dst + 8 * kBlockBytes + r * 128 + ((rope_ch ^ (r & 7)) << 4)) = nx.rope[it];
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_slot_full + 8 * (2 * st + 1));
+            if (more) {
+                fetch_codes(1);
+                fetch_rope();
+            }
+            ++tile;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
+    } else if (warp >= 4 && warp < 8) {
+        // ------------------------------------------------------------ softmax and output
+        // A warp has 16 query rows (its TMEM lane quarter). Scores are read as 16 x 256-bit fragments: with g = lane / 4 and
+        // j = lane % 4 a thread holds rows g and g + 8, columns 8i + 2j + {0, 1}; a row's maximum takes two shuffles.
+        const int quarter = warp & 3, g = lane >> 2, j = lane & 3;
+        const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+        const int row0 = quarter * 16 + g;
+        uint8_t* const p_row = p_smem + row0 * 128 + 4 * j;            // row g + 8 lies 1024 bytes further, same swizzle
+        // units without tiles: zeros (every CTA looks at its share, a lane each)
+        for (int64_t u0 = group; u0 < p.units; u0 += 32 * static_cast<int64_t>(p.groups)) {
+            const int64_t mine = u0 + lane * static_cast<int64_t>(p.groups);
+            uint32_t none = __ballot_sync(0xFFFFFFFFu, mine < p.units && __ldg(p.tiles + (mine < p.units ? mine : 0)) == 0);
+            for (; none; none &= none - 1) {
+                const int n = rows_of(u0 + (__ffs(none) - 1) * static_cast<int64_t>(p.groups), seq, r0);
+                for (int r = quarter; r < n; r += 4) {
+                    const int64_t at = seq * seq_rows + r0 + r;
+                    reinterpret_cast<uint4*>(p.out + at * 512)[lane] = make_uint4(0, 0, 0, 0);
+                    reinterpret_cast<uint4*>(p.out + at * 512)[32 + lane] = make_uint4(0, 0, 0, 0);
+                    if (p.lse && lane == 0) p.lse[at] = -INFINITY;
+                }
+            }
+        }
+        while (ok && walk.next(pc)) {
+            const int n_rows = rows_of(pc.unit, seq, r0);
+            if (n_rows <= 0) continue;
+            // keys that rows g and g + 8 see (dense): the sequence's length less the new tokens behind the row's own
+            const int64_t len = seq_len(seq);
+            int sees[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = row0 + 8 * h;
+                const int64_t n = p.a.topk ? len : len - (p.a.n_step - 1 - (r0 + r) / p.a.H);
+                sees[h] = r < n_rows ? static_cast<int>(max(n, int64_t(0))) : 0;
+            }
+            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            // rows [lo, hi) of the sequence lie inside the cache
+            const int lo = static_cast<int>(min(max(-base, int64_t(0)), int64_t(1) << 30));
+            const int hi = static_cast<int>(min(max(p.a.n_kv - base, int64_t(0)), int64_t(1) << 30));
+            if (!p.a.topk) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) sees[h] = min(sees[h], hi);
+            }
+            float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+            for (int i = 0; i < pc.n && ok; ++i, ++tile) {
+                const uint32_t st = tile & 1u;
+                ok = wait_warp(bar_s_full + 8 * st, (tile >> 1) & 1u);
+                if (!ok) break;
+                tcgen05_fence_after_sync();
+                uint32_t s[2][16];
+                tmem_ld_16x256b_x4(lane_base + kColS + st * 64, s[0]);
+                tmem_ld_16x256b_x4(lane_base + kColS + st * 64 + 32, s[1]);
+                tmem_ld_wait(s[0]);
+                tmem_ld_wait(s[1]);
+                const int at = (pc.t0 + i) * kTile;
+                float x[2][16];                                       // [row][8 column groups x 2]
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) x[h][2 * k + e] = __uint_as_float(s[k >> 2][4 * (k & 3) + 2 * h + e]) * p.scale_log2;
+                if (Q4 && p.a.topk) {
+                    // byte k of the stage's mask: rows 4k .. 4k + 3; this thread's columns 8i + 2j, + 1 are bits 2 (j & 1), + 1 of byte 2i + j / 2
+                    const uint4 mv = *reinterpret_cast<const uint4*>(mask_smem + st * 16);
+                    const uint32_t mw[4] = {mv.x, mv.y, mv.z, mv.w};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t two = mw[k >> 1] >> ((k & 1) * 16 + (j >> 1) * 8 + (j & 1) * 2);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const bool in = (two >> e) & 1u;
+                            x[0][2 * k + e] = in && sees[0] ? x[0][2 * k + e] : -INFINITY;
+                            x[1][2 * k + e] = in && sees[1] ? x[1][2 * k + e] : -INFINITY;
+                        }
+                    }
+                } else if (__any_sync(0xFFFFFFFFu, at + kTile > min(sees[0], sees[1]) || at < lo)) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const int c = at + 8 * (k >> 1) + 2 * j + (k & 1);
+                            if (c >= sees[h] || c < lo) x[h][k] = -INFINITY;
+                        }
+                }
+                float alpha[2];
+                bool move = false;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float mt = x[h][0];
+#pragma unroll
+                    for (int k = 1; k < 16; ++k) mt = fmaxf(mt, x[h][k]);
+                    mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, 1));
+                    mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, 2));
+                    alpha[h] = 1.f;
+                    if (mt > m_ref[h] + kMoveThreshold) {             // also the first usable score (m_ref = -inf)
+                        alpha[h] = m_ref[h] == -INFINITY ? 0.f : exp2_fast(m_ref[h] - mt);
+                        m_ref[h] = mt;
+                        l[h] *= alpha[h];
+                        move = true;
+                    }
+                }
+                uint32_t pk[2][8];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float ref = m_ref[h] == -INFINITY ? 0.f : m_ref[h];
+                    float sum = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float p0 = exp2_fast(x[h][2 * k] - ref), p1 = exp2_fast(x[h][2 * k + 1] - ref);
+                        sum += p0 + p1;
+                        pk[h][k] = pack2(p0, p1);
+                    }
+                    l[h] += sum;
+                }
+                const bool any_move = __any_sync(0xFFFFFFFFu, move);
+                // the previous tile's product has read P (and, for a rescale, written O); the piece's first tile: the product before it was
+                // waited for when that piece was written out
+                if (i > 0) {
+                    ok = wait_warp(bar_pv_done, (tile - 1u) & 1u);
+                    if (!ok) break;
+                    if (any_move) {
+                        tcgen05_fence_after_sync();
+                        const float a0 = __shfl_sync(0xFFFFFFFFu, alpha[0], (lane & 7) * 4), a1 = __shfl_sync(0xFFFFFFFFu, alpha[1], (lane & 7) * 4);
+                        const float f = (lane & 8) ? a1 : a0;             // lanes 0..15 and 16..31: rows 0..15 of the two halves of O
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t o[32];
+                            tmem_ld_32x32b_x32(lane_base + c * 32, o);
+                            tmem_ld_wait(o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st_32x32b_x32(lane_base + c * 32, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(p_row + h * 1024 + ((k ^ g) << 4)) = pk[h][k];
+                fence_proxy_async_smem();
+                tcgen05_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_p_ready);
+            }
+            if (!ok) break;
+            ok = wait_warp(bar_pv_done, (tile - 1u) & 1u);
+            if (!ok) break;
+            tcgen05_fence_after_sync();
+            // ---- this thread's rows' sums, then the output: lane = row (lane & 15) of half lane >> 4 of O
+            float inv[2], lse[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 1);
+                l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 2);
+                inv[h] = l[h] > 0.f ? 1.f / l[h] : 0.f;
+                lse[h] = l[h] > 0.f ? (m_ref[h] + log2f(l[h])) * 0.6931471805599453f : -INFINITY;
+            }
+            const float i0 = __shfl_sync(0xFFFFFFFFu, inv[0], (lane & 7) * 4), i1 = __shfl_sync(0xFFFFFFFFu, inv[1], (lane & 7) * 4);
+            const float f = (lane & 8) ? i1 : i0;
+            const int out_row = quarter * 16 + (lane & 15), col0 = (lane >> 4) * 256;
+            const int64_t at_row = seq * seq_rows + r0;
+            const int64_t slot = ((static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * p.ways + way) * kRows;
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+                uint32_t o[32];
+                tmem_ld_32x32b_x32(lane_base + c * 32, o);
+                tmem_ld_wait(o);
+                if (out_row >= n_rows) continue;
+                if (pc.whole) {
+                    uint4* dst = reinterpret_cast<uint4*>(p.out + (at_row + out_row) * 512 + col0 + c * 32);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        dst[v] = make_uint4(pack2(__uint_as_float(o[8 * v]) * f, __uint_as_float(o[8 * v + 1]) * f),
+                                            pack2(__uint_as_float(o[8 * v + 2]) * f, __uint_as_float(o[8 * v + 3]) * f),
+                                            pack2(__uint_as_float(o[8 * v + 4]) * f, __uint_as_float(o[8 * v + 5]) * f),
+                                            pack2(__uint_as_float(o[8 * v + 6]) * f, __uint_as_float(o[8 * v + 7]) * f));
+                } else {
+                    float4* dst = reinterpret_cast<float4*>(p.part_out + (slot + out_row) * 512 + col0 + c * 32);
+#pragma unroll
+                    for (int v = 0; v < 8; ++v)
+                        dst[v] = make_float4(__uint_as_float(o[4 * v]) * f, __uint_as_float(o[4 * v + 1]) * f, __uint_as_float(o[4 * v + 2]) * f,
+                                             __uint_as_float(o[4 * v + 3]) * f);
+                }
+            }
+            tcgen05_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_o_free);
+            if (j == 0) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = row0 + 8 * h;
+                    if (r >= n_rows) continue;
+                    if (!pc.whole) p.part_lse[slot + r] = lse[h];
+                    else if (p.lse) p.lse[at_row + r] = lse[h];
+                }
+            }
+            ++item;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_EPILOGUE);
+    }
+
+    // ---------------------------------------------------------------- teardown
+    __syncwarp();
+    if (*abort_flag) {                       // copies may still be in flight: let them land before the CTA's memory goes
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+    }
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) {
+        tcgen05_fence_after_sync();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// ---------------------------------------------------------------- merge
+// A unit cut by runs: group g - 1 holds its beginning (slot 1), groups g, g + 1, .. its continuations (slot 0). Block (g, y)
+// takes rows 4y .. 4y + 3 of the unit that group g is the first to start inside of; 128 threads a row, 4 columns each.
+__global__ void __launch_bounds__(512)
+latent_merge_kernel(const Params p) {
+    const int g = blockIdx.x;
+    if (p.runs[g + 1] == p.runs[g]) return;
+    const int2 s = p.starts[g];
+    if (s.y == 0) return;                                     // begins with its unit
+    // the run that holds tile 0 of the unit: the nearest earlier non-empty one must be it
+    int first = g - 1;
+    while (first > 0 && p.runs[first + 1] == p.runs[first]) --first;
+    if (p.starts[first].x == s.x && p.starts[first].y > 0) return;      // an earlier group starts inside this unit too
+    const int end = p.runs[g] - s.y + p.tiles[s.x];           // one past the unit's last tile, end to end
+    int last = g;
+    while (last + 1 < p.groups && p.runs[last + 1] < end) ++last;
+    const int64_t seq = s.x / p.blocks_per_seq;
+    const int seq_rows = p.a.n_step * p.a.H;
+    const int r = blockIdx.y * 4 + (threadIdx.x >> 7), c = threadIdx.x & 127;
+    const int r_seq = static_cast<int>(s.x - seq * p.blocks_per_seq) * p.ways * kRows + r;
+    if (r >= p.ways * kRows || r_seq >= seq_rows) return;
+    const int64_t stride = static_cast<int64_t>(2) * p.ways * kRows;            // rows of a group's two slots
+    const int64_t at1 = first * stride + p.ways * kRows + r, at0 = g * stride + r;
+    float m = p.part_lse[at1];
+    for (int k = g; k <= last; ++k) m = fmaxf(m, p.runs[k + 1] > p.runs[k] ? p.part_lse[at0 + (k - g) * stride] : -INFINITY);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float z = 0.f;
+    if (m > -INFINITY) {
+        auto add = [&](int64_t at) {
+            const float w = exp2_fast((p.part_lse[at] - m) * 1.4426950408889634f);
+            const float4 v = reinterpret_cast<const float4*>(p.part_out + at * 512)[c];
+            acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+            z += w;
+        };
+        add(at1);
+#pragma unroll 4
+        for (int k = g; k <= last; ++k)
+            if (p.runs[k + 1] > p.runs[k]) add(at0 + (k - g) * stride);
+    }
+    const float inv = z > 0.f ? 1.f / z : 0.f;
+    const int64_t out_row = seq * seq_rows + r_seq;
+    reinterpret_cast<uint2*>(p.out + out_row * 512)[c] = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    if (p.lse && c == 0) p.lse[out_row] = z > 0.f ? m + logf(z) : -INFINITY;
+}
+
+struct Layout {
+    int ways, blocks_per_seq, groups;
+    int64_t units;
+    size_t tiles_off, starts_off, runs_off, lse_off, out_off, bytes;
+};
+
+Layout layout_of(int64_t B, int n_step, int64_t max_len, int H, int sm_count) {
+    Layout y{};
+    const int64_t rows = static_cast<int64_t>(n_step) * H;
+    y.ways = rows > kRows ? 2 : 1;
+    y.blocks_per_seq = static_cast<int>((rows + y.ways * kRows - 1) / (y.ways * kRows));
+    y.units = B * y.blocks_per_seq;
+    const int64_t most = y.units * ((max_len + kTile - 1) / kTile);
+    const int64_t cap = sm_count / y.ways;
+    y.groups = static_cast<int>(most < 1 ? 1 : (most < cap ? most : cap));
+    auto take = [&](size_t bytes) { const size_t at = y.bytes; y.bytes += (bytes + 255) / 256 * 256; return at; };
+    y.tiles_off = take(static_cast<size_t>(y.units) * 4);
+    y.starts_off = take(static_cast<size_t>(y.groups + 1) * 8);
+    y.runs_off = take(static_cast<size_t>(y.groups + 1) * 4);
+    const size_t slots = static_cast<size_t>(y.groups) * 2 * y.ways * kRows;
+    y.lse_off = take(slots * 4);
+    y.out_off = take(slots * 512 * 4);
+    return y;
+}
+
+}  // namespace
+
+size_t latent_attn_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H) {
+    return layout_of(B, n_step, max_len, H, kLatentMaxGrid).bytes;
+}
+
+bool latent_attn_fits(int64_t B, int n_step, int64_t max_len, int H) {
+    const Layout y = layout_of(B, n_step, max_len, H, kLatentMaxGrid);
+    const int64_t tiles = (max_len + kTile - 1) / kTile;
+    return y.units < (int64_t(1) << 31) && (tiles == 0 || y.units <= ((int64_t(1) << 31) - 1) / tiles);
+}
+
+cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const CUtensorMap& q_map, const CUtensorMap& kv_map,
+                               unsigned int* status, int sm_count, cudaStream_t stream, int* launches) {
+    const Layout y = layout_of(a.B, a.n_step, a.max_len, a.H, sm_count < kLatentMaxGrid ? sm_count : kLatentMaxGrid);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    int32_t* tiles = reinterpret_cast<int32_t*>(ws + y.tiles_off);
+    int2* starts = reinterpret_cast<int2*>(ws + y.starts_off);
+    int32_t* runs = reinterpret_cast<int32_t*>(ws + y.runs_off);
+    const Params p{a, tiles, starts, runs, y.units, y.blocks_per_seq, y.ways, y.groups, a.scale * 1.4426950408889634f, static_cast<__nv_bfloat16*>(out), lse,
+                   reinterpret_cast<float*>(ws + y.out_off), reinterpret_cast<float*>(ws + y.lse_off), status};
+    cudaError_t e;
+    if (a.topk) {
+        ++*launches;
+        latent_count_kernel<<<static_cast<unsigned>(a.B), 128, 0, stream>>>(a, tiles);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    ++*launches;
+    latent_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, y.units, y.blocks_per_seq, y.groups, tiles, starts, runs);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const void* k = a.q4 ? reinterpret_cast<const void*>(latent_attn_kernel<true>) : reinterpret_cast<const void*>(latent_attn_kernel<false>);
+    if ((e = ensure_max_dynamic_smem(k, kSmemBytes)) != cudaSuccess) return e;
+    const unsigned grid = static_cast<unsigned>(y.groups * y.ways);
+    ++*launches;
+    if (a.q4) latent_attn_kernel<true><<<grid, kWarpsQ4 * 32, kSmemBytes, stream>>>(q_map, kv_map, p);
+    else latent_attn_kernel<false><<<grid, kWarpsBf16 * 32, kSmemBytes, stream>>>(q_map, kv_map, p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (y.groups > 1) {
+        ++*launches;
+        const int unit_rows = a.n_step * a.H < y.ways * kRows ? a.n_step * a.H : y.ways * kRows;
+        latent_merge_kernel<<<dim3(static_cast<unsigned>(y.groups), static_cast<unsigned>((unit_rows + 3) / 4)), 512, 0, stream>>>(p);
+        e = cudaGetLastError();
+    }
+    return e;
+}
+
+}  // namespace idxc

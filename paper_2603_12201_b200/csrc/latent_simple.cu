@@ -1,11 +1,10 @@
-// Plain CUDA-core forms of the attention over a latent cache and of the head-summed attention weights.
+// Head-summed attention weights over a latent cache, plain CUDA-core form.
 #include "kernels.h"
 #include "latent_format.cuh"
 
 namespace idxc {
 namespace {
 
-constexpr int kRows = 4;                  // query rows of a CTA
 constexpr int kPer = kLatentCols / 32;    // columns of a lane
 
 // Column lane + 32 i of a cache row, i < 18, as floats.
@@ -46,78 +45,6 @@ __device__ __forceinline__ int64_t entries(const LatentArgs& a, int b) {
     return n < 0 ? 0 : (n > a.max_len ? a.max_len : n);
 }
 
-__global__ void __launch_bounds__(256)
-latent_attn_simple_kernel(const LatentArgs a, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
-    __shared__ float q_s[kRows][kLatentCols];
-    __shared__ float o_s[kRows][kLatentValueCols];
-    __shared__ float m_s[8][kRows], l_s[8][kRows];
-    const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rows = a.n_step * a.H, r0 = blockIdx.y * kRows;
-    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
-    for (int i = threadIdx.x; i < kRows * kLatentCols; i += 256) {
-        const int r = r0 + i / kLatentCols;
-        q_s[i / kLatentCols][i % kLatentCols] = r < rows ? __bfloat162float(q[(static_cast<int64_t>(b) * rows + r) * kLatentCols + i % kLatentCols]) : 0.f;
-    }
-    for (int i = threadIdx.x; i < kRows * kLatentValueCols; i += 256) o_s[i / kLatentValueCols][i % kLatentValueCols] = 0.f;
-    __syncthreads();
-    const int64_t n = entries(a, b);
-    int64_t sees[kRows];
-    for (int r = 0; r < kRows; ++r) sees[r] = a.topk ? n : n - (a.n_step - 1 - (r0 + r) / a.H);
-    float m[kRows], l[kRows], acc[kRows][16];
-    for (int r = 0; r < kRows; ++r) {
-        m[r] = -INFINITY;
-        l[r] = 0.f;
-        for (int i = 0; i < 16; ++i) acc[r][i] = 0.f;
-    }
-    for (int64_t j = warp; j < n; j += 8) {
-        const int64_t row = cache_row(a, b, j);
-        if (row < 0) continue;
-        float v[kPer];
-        read_row(static_cast<const uint8_t*>(a.kv), a.q4 != 0, row, lane, v);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            float x = 0.f;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) x += q_s[r][lane + 32 * i] * v[i];
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-            x *= a.scale;
-            if (j >= sees[r]) continue;
-            const float mn = fmaxf(m[r], x);
-            const float f = expf(m[r] - mn), p = expf(x - mn);
-            m[r] = mn;
-            l[r] = l[r] * f + p;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[r][i] = acc[r][i] * f + p * v[i];
-        }
-    }
-    if (lane == 0)
-        for (int r = 0; r < kRows; ++r) { m_s[warp][r] = m[r]; l_s[warp][r] = l[r]; }
-    __syncthreads();
-    for (int w = 0; w < 8; ++w) {                  // one warp after the other: the order of the sums is fixed
-        if (w == warp) {
-            for (int r = 0; r < kRows; ++r) {
-                float top = -INFINITY;
-                for (int u = 0; u < 8; ++u) top = fmaxf(top, m_s[u][r]);
-                if (m[r] == -INFINITY) continue;
-                const float f = expf(m[r] - top);
-                for (int i = 0; i < 16; ++i) o_s[r][lane + 32 * i] += f * acc[r][i];
-            }
-        }
-        __syncthreads();
-    }
-    for (int i = threadIdx.x; i < kRows * kLatentValueCols; i += 256) {
-        const int r = i / kLatentValueCols, c = i % kLatentValueCols;
-        if (r0 + r >= rows) continue;
-        float top = -INFINITY, z = 0.f;
-        for (int u = 0; u < 8; ++u) top = fmaxf(top, m_s[u][r]);
-        for (int u = 0; u < 8; ++u) z += m_s[u][r] == -INFINITY ? 0.f : l_s[u][r] * expf(m_s[u][r] - top);
-        const int64_t at = static_cast<int64_t>(b) * rows + r0 + r;
-        out[at * kLatentValueCols + c] = __float2bfloat16(z > 0.f ? o_s[r][c] / z : 0.f);
-        if (c == 0 && lse) lse[at] = z > 0.f ? top + logf(z) : -INFINITY;
-    }
-}
-
 // One warp per position: its probability under every query row, summed.
 __global__ void __launch_bounds__(256)
 attn_weights_simple_kernel(const LatentArgs a, const float* __restrict__ lse, float beta, float* __restrict__ acc, int64_t ld) {
@@ -154,12 +81,6 @@ attn_weights_simple_kernel(const LatentArgs a, const float* __restrict__ lse, fl
 }
 
 }  // namespace
-
-cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, cudaStream_t stream) {
-    const dim3 grid(static_cast<unsigned>(a.B), static_cast<unsigned>((a.n_step * a.H + kRows - 1) / kRows));
-    latent_attn_simple_kernel<<<grid, 256, 0, stream>>>(a, static_cast<__nv_bfloat16*>(out), lse);
-    return cudaGetLastError();
-}
 
 cudaError_t launch_attn_weights(const LatentArgs& a, const float* lse, float beta, float* acc, int64_t ld, cudaStream_t stream) {
     const int64_t n = a.topk ? a.k_top : a.max_len;
