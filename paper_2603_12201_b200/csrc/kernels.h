@@ -132,13 +132,13 @@ struct LatentArgs {
     int H;
     float scale;
 };
-// latent_attn.cu. q_map: q as [B * n_step * H, 576] bf16, kv_map: kv as [n_kv, 576] bf16 (not used with q4), both with the 128-byte
-// swizzle and boxes of 64 columns x 64 rows. At most kLatentMaxGrid CTAs run. *launches is raised by the kernels launched.
+// latent_attn.cu. q_map: q as [B * n_step * H, 576] bf16, kv_map: kv as [n_kv, 576] bf16, both with the 128-byte swizzle and boxes of
+// 64 columns x 64 rows; value_map: kv's value columns as [8 blocks][n_kv][64], boxes of two blocks. The last two are not used with q4. At most kLatentMaxGrid CTAs run. *launches is raised by the kernels launched.
 constexpr int kLatentMaxGrid = 160;
 size_t latent_attn_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H);
 bool latent_attn_fits(int64_t B, int n_step, int64_t max_len, int H);      // the tile count of the call stays below 2^31
 cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const CUtensorMap& q_map, const CUtensorMap& kv_map,
-                               unsigned int* status, int sm_count, cudaStream_t stream, int* launches);
+                               const CUtensorMap& value_map, unsigned int* status, int sm_count, cudaStream_t stream, int* launches);
 cudaError_t launch_attn_weights(const LatentArgs& a, const float* lse, float beta, float* acc, int64_t ld, cudaStream_t stream);
 
 // latent_cache.cu

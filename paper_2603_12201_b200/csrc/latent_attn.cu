@@ -15,7 +15,10 @@
 //
 // Shared memory: Q 9 blocks of [64 rows x 128 B] | 2 stages x 9 blocks of [64 cache rows x 128 B] | P [64 x 128 B], all in the
 // 128-byte swizzle. A block of cache rows is at once the K-major B operand of Q K^T and the MN-major B operand of P V. A stage
-// is two slots: "A" = blocks 0..3 (the first half of V), "B" = blocks 4..8.
+// is five slots with barriers of their own: slots 0..3 = two blocks each (128 value columns, free again when their part of P V is
+// done), slot 4 = the positional block (free when its part of the scores is done). P V goes slot by slot, so that a stage is
+// being refilled from its front while its back is still multiplied; the scores of the next tile but one start with the
+// positional block and follow the refill. (With two slots a stage the refill was waited for: 5250 clocks a tile.)
 // TMEM: O [0, 256), both halves | S double-buffered [256, 320), [320, 384).
 // Order of the tensor pipe: S(i+1) | P(i) V(i), so that a tile's softmax runs under the next tile's scores.
 // bf16 rows come by TMA (the tail of a sequence is cleared in shared memory: rows behind it may hold NaN). 4-bit rows are read
@@ -32,7 +35,7 @@ namespace {
 constexpr int kTile = 64;                           // cache rows of a tile
 constexpr int kRows = 64;                           // query rows of a CTA
 constexpr int kBlocks = 9;                          // 64-column blocks of a row
-constexpr int kSlotA = 4;                           // blocks of slot A
+constexpr int kSlots = 5;                           // slots of a stage: blocks 2s, 2s + 1 for s < 4, block 8
 constexpr uint32_t kBlockBytes = kTile * 128;
 constexpr uint32_t kStageBytes = kBlocks * kBlockBytes;
 constexpr uint32_t kQBytes = kBlocks * kRows * 128;
@@ -176,7 +179,8 @@ struct Walk {
 // ---------------------------------------------------------------- main kernel
 template <bool Q4>
 __global__ void __launch_bounds__((Q4 ? kWarpsQ4 : kWarpsBf16) * 32, 1)
-latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map, const Params p) {
+latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map,
+                   const __grid_constant__ CUtensorMap value_map, const Params p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* q_smem = smem;
@@ -185,16 +189,17 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     uint64_t* bars = reinterpret_cast<uint64_t*>(p_smem + kPBytes);
     const uint32_t bar_q_full = smem_u32(bars + 0);
     const uint32_t bar_q_empty = smem_u32(bars + 1);
-    const uint32_t bar_slot_full = smem_u32(bars + 2);       // [2 stages][A, B]
-    const uint32_t bar_slot_empty = smem_u32(bars + 6);
-    const uint32_t bar_s_full = smem_u32(bars + 10);         // [2]
-    const uint32_t bar_p_ready = smem_u32(bars + 12);
-    const uint32_t bar_pv_done = smem_u32(bars + 13);
-    const uint32_t bar_o_free = smem_u32(bars + 14);
-    const uint32_t bar_tail = smem_u32(bars + 15);
-    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 16);
+    const uint32_t bar_slot_full = smem_u32(bars + 2);       // [2 stages][kSlots]
+    const uint32_t bar_slot_empty = smem_u32(bars + 12);
+    const uint32_t bar_s_full = smem_u32(bars + 22);         // [2]
+    const uint32_t bar_p_ready = smem_u32(bars + 24);
+    const uint32_t bar_pv_done = smem_u32(bars + 25);
+    const uint32_t bar_o_free = smem_u32(bars + 26);
+    const uint32_t bar_tail = smem_u32(bars + 27);
+    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 28);
     volatile uint32_t* abort_flag = tmem_base_slot + 1;
-    uint8_t* mask_smem = reinterpret_cast<uint8_t*>(bars + 18);    // [2 stages][16]: usable rows 4k .. 4k+3 of the tile
+    uint8_t* mask_smem = reinterpret_cast<uint8_t*>(bars + 30);    // [2 stages][8]: bit r of a stage's 64: row r of the tile is usable
+    static_assert(32 * 8 <= kBarBytes, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = blockIdx.x / p.ways, way = blockIdx.x - group * p.ways;
@@ -212,7 +217,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (threadIdx.x == 0) {
         mbar_init(bar_q_full, 1);
         mbar_init(bar_q_empty, 1);
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * kSlots; ++i) {
             mbar_init(bar_slot_full + 8 * i, Q4 ? kLoadWarps : 1);
             mbar_init(bar_slot_empty + 8 * i, 1);
         }
@@ -250,23 +255,27 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (warp == 0) {
         // ------------------------------------------------------------ MMA issuer (warp-uniform, one elected lane issues)
         constexpr uint32_t kIdescS = umma_idesc(1, 1, kRows, kTile);
-        constexpr uint32_t kIdescPV = umma_idesc(1, 1, kRows, 256) | kUmmaBMajorMN;
+        constexpr uint32_t kIdescPV = umma_idesc(1, 1, kRows, 128) | kUmmaBMajorMN;
         const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
         const uint64_t p_desc = umma_smem_desc_sw128(smem_u32(p_smem));
         auto issue_s = [&](uint32_t tl) -> bool {
             const uint32_t st = tl & 1u, ph = (tl >> 1) & 1u;
             const uint32_t d = tmem_base + kColS + st * 64;
-            uint64_t a_desc = q_desc, b_desc = umma_smem_desc_sw128(smem_u32(stage_smem + st * kStageBytes));
-#pragma unroll 1
-            for (int b = 0; b < kBlocks; ++b) {
-                if (b == 0 || b == kSlotA) {
-                    if (!wait_warp(bar_slot_full + 8 * (2 * st + (b != 0)), ph)) return false;
+            const uint64_t k_desc = umma_smem_desc_sw128(smem_u32(stage_smem + st * kStageBytes));
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n) {                      // block 8, then 0 .. 7
+                const int b = n == 0 ? 8 : n - 1;
+                if (n == 0 || (b & 1) == 0) {
+                    if (!wait_warp(bar_slot_full + 8 * (kSlots * st + (b >> 1)), ph)) return false;
                     tcgen05_fence_after_sync();
                 }
+                const uint64_t a_desc = q_desc + b * (kRows * 128 / 16), b_desc = k_desc + b * (kBlockBytes / 16);
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) umma_f16_elect_acc(d, a_desc + ks * 2, b_desc + ks * 2, kIdescS, (b | ks) ? 1u : 0u);
-                a_desc += kRows * 128 / 16;
-                b_desc += kBlockBytes / 16;
+                for (int ks = 0; ks < 4; ++ks) {
+                    if (n | ks) umma_f16_elect<true>(d, a_desc + ks * 2, b_desc + ks * 2, kIdescS);
+                    else umma_f16_elect<false>(d, a_desc, b_desc, kIdescS);
+                }
+                if (n == 0) umma_commit_elect(bar_slot_empty + 8 * (kSlots * st + 4));
             }
             umma_commit_elect(bar_s_full + 8 * st);
             return true;
@@ -287,13 +296,13 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 tcgen05_fence_after_sync();
                 const uint32_t st = tile & 1u;
                 const uint64_t v_desc = umma_smem_desc_sw128_mn(smem_u32(stage_smem + st * kStageBytes), kBlockBytes);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+                for (int sl = 0; sl < 4; ++sl) {                     // 128 value columns: half sl / 2 of O, columns 128 (sl % 2) ..
+                    const uint32_t d = tmem_base + (sl & 1) * 128 + (static_cast<uint32_t>((sl >> 1) * 16) << 16);
 #pragma unroll
                     for (int ks = 0; ks < kTile / 16; ++ks)
-                        umma_f16_elect_acc(tmem_base + (static_cast<uint32_t>(h * 16) << 16), p_desc + ks * 2,
-                                           v_desc + h * (kSlotA * kBlockBytes / 16) + ks * (16 * 128 / 16), kIdescPV, (i | ks) ? 1u : 0u);
-                    umma_commit_elect(bar_slot_empty + 8 * (2 * st + h));
+                        umma_f16_elect_acc(d, p_desc + ks * 2, v_desc + sl * (2 * kBlockBytes / 16) + ks * (16 * 128 / 16), kIdescPV, (i | ks) ? 1u : 0u);
+                    umma_commit_elect(bar_slot_empty + 8 * (kSlots * st + sl));
                 }
                 umma_commit_elect(bar_pv_done);
             }
@@ -317,7 +326,10 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
     } else if (!Q4 && warp == 1) {
         // ------------------------------------------------------------ bf16 rows
-        if (lane == 0) tma_prefetch_desc(&kv_map);
+        if (lane == 0) {
+            tma_prefetch_desc(&kv_map);
+            tma_prefetch_desc(&value_map);
+        }
         uint32_t tails = 0;
         while (ok && walk.next(pc)) {
             if (rows_of(pc.unit, seq, r0) <= 0) continue;
@@ -330,24 +342,26 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 // coordinates outside the cache read zeros; a base far outside is brought to the nearest such place
                 const int64_t first = min(max(base + at, static_cast<int64_t>(-kTile)), p.a.n_kv);
                 const bool tail = len - at < kTile;
-                ok = wait_warp(bar_slot_empty + 8 * (2 * st), ph, 20);
-                if (!ok) break;
+                // ask the L2 for the tile after the next (one CTA of the group: the other reads the same rows)
+                const int64_t soon = base + at + 2 * kTile;
+                if (lane == 0 && way == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                    l2_prefetch(static_cast<const uint8_t*>(p.a.kv) + soon * kLatentBf16RowBytes, kTile * kLatentBf16RowBytes);
                 if (!tail) {
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(bar_slot_full + 8 * (2 * st), kSlotA * kBlockBytes);
-                        for (int b = 0; b < kSlotA; ++b)
-                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &kv_map, bar_slot_full + 8 * (2 * st), b * 64, static_cast<int>(first));
+#pragma unroll
+                    for (int n = 0; n < kSlots; ++n) {
+                        const int sl = n == 0 ? 4 : n - 1;           // the order in which the scores take them
+                        const uint32_t full = bar_slot_full + 8 * (kSlots * st + sl), to = smem_u32(dst + 2 * sl * kBlockBytes);
+                        ok = ok && wait_warp(bar_slot_empty + 8 * (kSlots * st + sl), ph);
+                        if (ok && lane == 0) {
+                            mbar_arrive_expect_tx(full, (sl == 4 ? 1 : 2) * kBlockBytes);
+                            if (sl == 4) tma_load_2d(to, &kv_map, full, 512, static_cast<int>(first));
+                            else tma_load_3d(to, &value_map, full, 0, static_cast<int>(first), 2 * sl);
+                        }
                     }
-                    ok = wait_warp(bar_slot_empty + 8 * (2 * st + 1), ph, 20);
                     if (!ok) break;
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(bar_slot_full + 8 * (2 * st + 1), (kBlocks - kSlotA) * kBlockBytes);
-                        for (int b = kSlotA; b < kBlocks; ++b)
-                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &kv_map, bar_slot_full + 8 * (2 * st + 1), b * 64, static_cast<int>(first));
-                    }
                 } else {
                     // the sequence ends inside this tile: load, clear the rows behind its end, publish
-                    ok = wait_warp(bar_slot_empty + 8 * (2 * st + 1), ph, 20);
+                    for (int sl = 0; sl < kSlots && ok; ++sl) ok = wait_warp(bar_slot_empty + 8 * (kSlots * st + sl), ph, 20);
                     if (!ok) break;
                     if (lane == 0) {
                         mbar_arrive_expect_tx(bar_tail, kStageBytes);
@@ -363,10 +377,8 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             *reinterpret_cast<uint4*>(dst + b * kBlockBytes + o) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar_slot_full + 8 * (2 * st));
-                        mbar_arrive(bar_slot_full + 8 * (2 * st + 1));
-                    }
+                    if (lane == 0)
+                        for (int sl = 0; sl < kSlots; ++sl) mbar_arrive(bar_slot_full + 8 * (kSlots * st + sl));
                 }
             }
             ++item;
@@ -374,68 +386,42 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
     } else if (Q4 && warp >= 8) {
         // ------------------------------------------------------------ 4-bit rows
-        // A warp has rows 32 it + 4 w + rr (it = 0, 1; rr = 0..3) of every tile. Codes: lane = 8 block + 2 rr + half reads the 16
-        // bytes (one scale group) of column block `block` of the slot, half `half`, and stores four 16-byte chunks; eight
-        // consecutive lanes then store to eight different chunk positions (no bank conflicts). Positional columns: lane = 8 rr
-        // + chunk. Everything of the next tile is in registers before this tile's slot is free.
+        // A warp has rows 8w .. 8w + 7 of every tile. Codes: lane = 8 (2 block + half) + rr reads the 16 bytes (one scale group) of half
+        // `half` of a slot's block `block` of row rr, and stores four 16-byte chunks; eight consecutive lanes then store to eight
+        // different chunk positions (no bank conflicts). Positional columns: lane = 8 row + chunk, two rows a lane. Everything of the
+        // next tile is in registers before this tile's slot is free.
         const int w = warp - 8;
-        const int blk = lane >> 3, rr = (lane >> 1) & 3, half = lane & 1;
-        const int rope_rr = lane >> 3, rope_ch = lane & 7;
+        const int rr = lane & 7, blk = lane >> 4, half = (lane >> 3) & 1;
+        const int my_row = w * 8 + rr;
         const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
-        struct Tile { uint4 code[2][2]; uint16_t scale[2][2]; uint4 rope[2]; };      // [slot][it], [slot][it], [it]
-        Tile nx;
+        uint4 code[4], rope[2];                               // of the tile being fetched
+        uint16_t scale[4];
         uint32_t nx_mask = 0;
         int64_t len = 0, base = 0;
         const int32_t* sel = nullptr;
-        int64_t src[2];                                       // cache rows of this lane's code rows in the tile being fetched, -1: none
+        int64_t src;                                          // cache row of this lane's row in the tile being fetched, -1: none
         auto locate = [&](int t) {                            // tile t of the piece's sequence
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                int64_t j = static_cast<int64_t>(t) * kTile + it * 32 + w * 4 + rr;
-                bool use = j < len;
-                if (sel != nullptr) {
-                    j = use ? __ldg(sel + j) : -1;
-                    use = j >= 0;
-                }
-                j += base;
-                src[it] = use && j >= 0 && j < p.a.n_kv ? j : -1;
+            int64_t r = static_cast<int64_t>(t) * kTile + my_row;
+            bool use = r < len;
+            if (sel != nullptr) {
+                r = use ? __ldg(sel + r) : -1;
+                use = r >= 0;
             }
+            r += base;
+            src = use && r >= 0 && r < p.a.n_kv ? r : -1;
+            nx_mask = __ballot_sync(0xFFFFFFFFu, src >= 0) & 255u;
         };
-        auto fetch_codes = [&](int slot) {
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int cc = slot * 8 + blk * 2 + half;
-                const uint8_t* row = kv + (src[it] < 0 ? 0 : src[it]) * kLatentQ4RowBytes;
-                nx.code[slot][it] = src[it] < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(row) + cc);
-                nx.scale[slot][it] = src[it] < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(row + kLatentQ4ScaleOff) + cc);
-            }
+        auto fetch_codes = [&](int sl) {
+            const int cc = sl * 4 + blk * 2 + half;
+            const uint8_t* row = kv + (src < 0 ? 0 : src) * kLatentQ4RowBytes;
+            code[sl] = src < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(row) + cc);
+            scale[sl] = src < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(row + kLatentQ4ScaleOff) + cc);
         };
         auto fetch_rope = [&]() {
 #pragma unroll
             for (int it = 0; it < 2; ++it) {
-                const int64_t s = __shfl_sync(0xFFFFFFFFu, src[it], rope_rr * 2);
-                nx.rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + rope_ch);
-            }
-        };
-        auto note_mask = [&]() {                              // bits 0..3: it = 0, bits 4..7: it = 1
-            uint32_t m = 0;
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const uint32_t v = __ballot_sync(0xFFFFFFFFu, src[it] >= 0);
-                m |= ((v & 1u) | ((v >> 1) & 2u) | ((v >> 2) & 4u) | ((v >> 3) & 8u)) << (4 * it);   // lanes 0, 2, 4, 6
-            }
-            nx_mask = m;
-        };
-        auto store_codes = [&](uint8_t* dst, int slot) {
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int r = it * 32 + w * 4 + rr;
-                uint8_t* row = dst + (slot * kSlotA + blk) * kBlockBytes + r * 128;
-                const __nv_bfloat162 s = scale_pair(nx.scale[slot][it]);
-                const uint4 c = nx.code[slot][it];
-                const uint32_t word[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-                for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + (((half * 4 + v) ^ (r & 7)) << 4)) = dequant8_q4(word[v], s);
+                const int64_t s = __shfl_sync(0xFFFFFFFFu, src, it * 4 + (lane >> 3));
+                rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + (lane & 7));
             }
         };
         // the piece that the fetches are in runs ahead of the one whose tiles are stored
@@ -460,10 +446,9 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         ahead_piece();
         if (more) {
             locate(apc.t0);
-            note_mask();
-            fetch_codes(0);
-            fetch_codes(1);
             fetch_rope();
+#pragma unroll
+            for (int sl = 0; sl < 4; ++sl) fetch_codes(sl);
         }
         while (more && ok) {
             // store tile `tile` (in registers), fetching the next as the registers come free
@@ -471,35 +456,33 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             uint8_t* dst = stage_smem + st * kStageBytes;
             const uint32_t mask = nx_mask;
             if (++ai == apc.n) ahead_piece();
-            if (more) {
-                locate(apc.t0 + ai);
-                note_mask();
-            }
-            ok = wait_warp(bar_slot_empty + 8 * (2 * st), ph);
+            if (more) locate(apc.t0 + ai);
+            auto publish = [&](int sl) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_slot_full + 8 * (kSlots * st + sl));
+            };
+            ok = wait_warp(bar_slot_empty + 8 * (kSlots * st + 4), ph);
             if (!ok) break;
-            store_codes(dst, 0);
-            if (lane == 0) {
-                mask_smem[st * 16 + w] = static_cast<uint8_t>(mask & 15u);
-                mask_smem[st * 16 + 8 + w] = static_cast<uint8_t>(mask >> 4);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_slot_full + 8 * (2 * st));
-            if (more) fetch_codes(0);
-            ok = wait_warp(bar_slot_empty + 8 * (2 * st + 1), ph);
-            if (!ok) break;
-            store_codes(dst, 1);
 #pragma unroll
             for (int it = 0; it < 2; ++it) {
-                const int r = it * 32 + w * 4 + rope_rr;
-                *reinterpret_cast<uint4*>(dst + 8 * kBlockBytes + r * 128 + ((rope_ch ^ (r & 7)) << 4)) = nx.rope[it];
+                const int r = it * 4 + (lane >> 3);
+                *reinterpret_cast<uint4*>(dst + 8 * kBlockBytes + (w * 8 + r) * 128 + (((lane & 7) ^ r) << 4)) = rope[it];
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_slot_full + 8 * (2 * st + 1));
-            if (more) {
-                fetch_codes(1);
-                fetch_rope();
+            publish(4);
+            if (more) fetch_rope();
+#pragma unroll
+            for (int sl = 0; sl < 4; ++sl) {
+                ok = wait_warp(bar_slot_empty + 8 * (kSlots * st + sl), ph);
+                if (!ok) break;
+                uint8_t* row = dst + (2 * sl + blk) * kBlockBytes + my_row * 128;
+                const __nv_bfloat162 s2 = scale_pair(scale[sl]);
+                const uint32_t word[4] = {code[sl].x, code[sl].y, code[sl].z, code[sl].w};
+#pragma unroll
+                for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + (((half * 4 + v) ^ rr) << 4)) = dequant8_q4(word[v], s2);
+                if (sl == 0 && lane == 0) mask_smem[st * 8 + w] = static_cast<uint8_t>(mask);
+                publish(sl);
+                if (more) fetch_codes(sl);
             }
             ++tile;
         }
@@ -566,12 +549,10 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 #pragma unroll
                         for (int e = 0; e < 2; ++e) x[h][2 * k + e] = __uint_as_float(s[k >> 2][4 * (k & 3) + 2 * h + e]) * p.scale_log2;
                 if (Q4 && p.a.topk) {
-                    // byte k of the stage's mask: rows 4k .. 4k + 3; this thread's columns 8i + 2j, + 1 are bits 2 (j & 1), + 1 of byte 2i + j / 2
-                    const uint4 mv = *reinterpret_cast<const uint4*>(mask_smem + st * 16);
-                    const uint32_t mw[4] = {mv.x, mv.y, mv.z, mv.w};
+                    const uint2 mv = *reinterpret_cast<const uint2*>(mask_smem + st * 8);       // byte k: rows 8k .. 8k + 7
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const uint32_t two = mw[k >> 1] >> ((k & 1) * 16 + (j >> 1) * 8 + (j & 1) * 2);
+                        const uint32_t two = (k < 4 ? mv.x : mv.y) >> ((k & 3) * 8 + 2 * j);
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const bool in = (two >> e) & 1u;
@@ -803,7 +784,7 @@ bool latent_attn_fits(int64_t B, int n_step, int64_t max_len, int H) {
 }
 
 cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const CUtensorMap& q_map, const CUtensorMap& kv_map,
-                               unsigned int* status, int sm_count, cudaStream_t stream, int* launches) {
+                               const CUtensorMap& value_map, unsigned int* status, int sm_count, cudaStream_t stream, int* launches) {
     const Layout y = layout_of(a.B, a.n_step, a.max_len, a.H, sm_count < kLatentMaxGrid ? sm_count : kLatentMaxGrid);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     int32_t* tiles = reinterpret_cast<int32_t*>(ws + y.tiles_off);
@@ -824,8 +805,8 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     if ((e = ensure_max_dynamic_smem(k, kSmemBytes)) != cudaSuccess) return e;
     const unsigned grid = static_cast<unsigned>(y.groups * y.ways);
     ++*launches;
-    if (a.q4) latent_attn_kernel<true><<<grid, kWarpsQ4 * 32, kSmemBytes, stream>>>(q_map, kv_map, p);
-    else latent_attn_kernel<false><<<grid, kWarpsBf16 * 32, kSmemBytes, stream>>>(q_map, kv_map, p);
+    if (a.q4) latent_attn_kernel<true><<<grid, kWarpsQ4 * 32, kSmemBytes, stream>>>(q_map, kv_map, value_map, p);
+    else latent_attn_kernel<false><<<grid, kWarpsBf16 * 32, kSmemBytes, stream>>>(q_map, kv_map, value_map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if (y.groups > 1) {
         ++*launches;
