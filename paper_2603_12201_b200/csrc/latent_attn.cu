@@ -20,7 +20,8 @@
 // being refilled from its front while its back is still multiplied; the scores of the next tile but one start with the
 // positional block and follow the refill. (With two slots a stage the refill was waited for: 5250 clocks a tile.)
 // TMEM: O [0, 256), both halves | S double-buffered [256, 320), [320, 384).
-// Order of the tensor pipe: S(i+1) | P(i) V(i), so that a tile's softmax runs under the next tile's scores.
+// Scores and P V are issued by a warp each, so that a tile's softmax runs under the next tile's scores and neither waits for the
+// other's operands.
 // bf16 rows come by TMA (the tail of a sequence is cleared in shared memory: rows behind it may hold NaN). 4-bit rows are read
 // into registers a tile ahead by eight warps and expanded into the stage (exact, see latent_format.cuh).
 #include <cuda_bf16.h>
@@ -45,9 +46,9 @@ constexpr uint32_t kSmemBytes = kQBytes + 2 * kStageBytes + kPBytes + kBarBytes 
 static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
 constexpr uint32_t kColS = 256;
 constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
-constexpr int kWarpsBf16 = 8;                       // 0 MMA | 1 rows (TMA) | 2 Q | 3 idle | 4..7 softmax
-constexpr int kWarpsQ4 = 16;                        // 0 MMA | 1 idle | 2 Q | 3 idle | 4..7 softmax | 8..15 rows
-constexpr int kLoadWarps = 8;
+constexpr int kWarpsBf16 = 8;                       // 0 scores | 1 P V | 2 Q | 3 rows (TMA) | 4..7 softmax
+constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 idle | 4..7 softmax | 8..15 rows
+constexpr int kSlotWarps = 4;                       // warps that fill a slot (4-bit rows)
 
 struct Params {
     LatentArgs a;
@@ -58,7 +59,8 @@ struct Params {
     int blocks_per_seq;          // units of a sequence
     int ways;                    // CTAs of a group: 1 or 2, each 64 rows
     int groups;
-    float scale_log2;
+    float scale_log2;            // |scale| * log2(e), 1 for a zero scale
+    float sign;                  // 1, -1 or 0: scores are multiplied by it first
     __nv_bfloat16* out;
     float* lse;
     float* part_out;             // [groups][2][ways][64][512]
@@ -196,10 +198,11 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const uint32_t bar_pv_done = smem_u32(bars + 25);
     const uint32_t bar_o_free = smem_u32(bars + 26);
     const uint32_t bar_tail = smem_u32(bars + 27);
+    const uint32_t bar_s_free = smem_u32(bars + 32);         // [2]
     uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 28);
     volatile uint32_t* abort_flag = tmem_base_slot + 1;
     uint8_t* mask_smem = reinterpret_cast<uint8_t*>(bars + 30);    // [2 stages][8]: bit r of a stage's 64: row r of the tile is usable
-    static_assert(32 * 8 <= kBarBytes, "barrier area");
+    static_assert(34 * 8 <= kBarBytes, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = blockIdx.x / p.ways, way = blockIdx.x - group * p.ways;
@@ -218,10 +221,13 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         mbar_init(bar_q_full, 1);
         mbar_init(bar_q_empty, 1);
         for (int i = 0; i < 2 * kSlots; ++i) {
-            mbar_init(bar_slot_full + 8 * i, Q4 ? kLoadWarps : 1);
+            mbar_init(bar_slot_full + 8 * i, Q4 ? kSlotWarps : 1);
             mbar_init(bar_slot_empty + 8 * i, 1);
         }
-        for (int i = 0; i < 2; ++i) mbar_init(bar_s_full + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_s_full + 8 * i, 1);
+            mbar_init(bar_s_free + 8 * i, 4);
+        }
         mbar_init(bar_p_ready, 4);
         mbar_init(bar_pv_done, 1);
         mbar_init(bar_o_free, 4);
@@ -253,56 +259,70 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     };
 
     if (warp == 0) {
-        // ------------------------------------------------------------ MMA issuer (warp-uniform, one elected lane issues)
+        // ------------------------------------------------------------ scores (warp-uniform, one elected lane issues)
         constexpr uint32_t kIdescS = umma_idesc(1, 1, kRows, kTile);
-        constexpr uint32_t kIdescPV = umma_idesc(1, 1, kRows, 128) | kUmmaBMajorMN;
         const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
-        const uint64_t p_desc = umma_smem_desc_sw128(smem_u32(p_smem));
-        auto issue_s = [&](uint32_t tl) -> bool {
-            const uint32_t st = tl & 1u, ph = (tl >> 1) & 1u;
-            const uint32_t d = tmem_base + kColS + st * 64;
-            const uint64_t k_desc = umma_smem_desc_sw128(smem_u32(stage_smem + st * kStageBytes));
-#pragma unroll
-            for (int n = 0; n < kBlocks; ++n) {                      // block 8, then 0 .. 7
-                const int b = n == 0 ? 8 : n - 1;
-                if (n == 0 || (b & 1) == 0) {
-                    if (!wait_warp(bar_slot_full + 8 * (kSlots * st + (b >> 1)), ph)) return false;
-                    tcgen05_fence_after_sync();
-                }
-                const uint64_t a_desc = q_desc + b * (kRows * 128 / 16), b_desc = k_desc + b * (kBlockBytes / 16);
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks) {
-                    if (n | ks) umma_f16_elect<true>(d, a_desc + ks * 2, b_desc + ks * 2, kIdescS);
-                    else umma_f16_elect<false>(d, a_desc, b_desc, kIdescS);
-                }
-                if (n == 0) umma_commit_elect(bar_slot_empty + 8 * (kSlots * st + 4));
-            }
-            umma_commit_elect(bar_s_full + 8 * st);
-            return true;
-        };
         while (ok && walk.next(pc)) {
             if (rows_of(pc.unit, seq, r0) <= 0) continue;
-            ok = wait_warp(bar_q_full, item & 1u) && issue_s(tile);
-            if (ok && pc.n == 1) umma_commit_elect(bar_q_empty);
-            for (int i = 0; i < pc.n && ok; ++i, ++tile) {
-                if (i + 1 < pc.n) {
-                    ok = issue_s(tile + 1);
-                    if (!ok) break;
-                    if (i + 2 == pc.n) umma_commit_elect(bar_q_empty);       // the piece's last scores
-                }
-                if (i == 0) ok = wait_warp(bar_o_free, (item & 1u) ^ 1u);    // the previous piece's output has been read
-                ok = ok && wait_warp(bar_p_ready, tile & 1u);
+            ok = wait_warp(bar_q_full, item & 1u);
+            for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {      // (a vote: the compiler sees a uniform loop)
+                const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
+                const uint32_t d = tmem_base + kColS + st * 64;
+                const uint32_t full = bar_slot_full + 8 * kSlots * st;
+                const uint64_t k_desc = umma_smem_desc_sw128(smem_u32(stage_smem + st * kStageBytes));
+                // the softmax has read the scores that this buffer held
+                ok = wait_warp(bar_s_free + 8 * st, ph ^ 1u) && wait_warp(full + 8 * 4, ph);
                 if (!ok) break;
                 tcgen05_fence_after_sync();
-                const uint32_t st = tile & 1u;
-                const uint64_t v_desc = umma_smem_desc_sw128_mn(smem_u32(stage_smem + st * kStageBytes), kBlockBytes);
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) {                                         // the positional block first
+                    const uint64_t a_desc = q_desc + 8 * (kRows * 128 / 16) + ks * 2, b_desc = k_desc + 8 * (kBlockBytes / 16) + ks * 2;
+                    if (ks) umma_f16_elect<true>(d, a_desc, b_desc, kIdescS);
+                    else umma_f16_elect<false>(d, a_desc, b_desc, kIdescS);
+                }
+                umma_commit_elect(bar_slot_empty + 8 * (kSlots * st + 4));
+                uint64_t a_desc = q_desc, b_desc = k_desc;
 #pragma unroll 1
-                for (int sl = 0; sl < 4; ++sl) {                     // 128 value columns: half sl / 2 of O, columns 128 (sl % 2) ..
+                for (int sl = 0; sl < 4; ++sl) {                                         // rolled: the roles share an instruction cache
+                    ok = wait_warp(full + 8 * sl, ph);
+                    if (!ok) break;
+                    tcgen05_fence_after_sync();
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+                            umma_f16_elect<true>(d, a_desc + b * (kRows * 128 / 16) + ks * 2, b_desc + b * (kBlockBytes / 16) + ks * 2, kIdescS);
+                    a_desc += 2 * (kRows * 128 / 16);
+                    b_desc += 2 * (kBlockBytes / 16);
+                }
+                if (!ok) break;
+                umma_commit_elect(bar_s_full + 8 * st);
+            }
+            if (ok) umma_commit_elect(bar_q_empty);
+            ++item;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_MMA);
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ P V (a warp of its own: its waits do not hold up the scores)
+        constexpr uint32_t kIdescPV = umma_idesc(1, 1, kRows, 128) | kUmmaBMajorMN;
+        const uint64_t p_desc = umma_smem_desc_sw128(smem_u32(p_smem));
+        while (ok && walk.next(pc)) {
+            if (rows_of(pc.unit, seq, r0) <= 0) continue;
+            ok = wait_warp(bar_o_free, (item & 1u) ^ 1u);                // the previous piece's output has been read
+            for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {
+                const uint32_t st = tile & 1u;
+                uint64_t v_desc = umma_smem_desc_sw128_mn(smem_u32(stage_smem + st * kStageBytes), kBlockBytes);
+                ok = wait_warp(bar_p_ready, tile & 1u);
+                if (!ok) break;
+                tcgen05_fence_after_sync();
+#pragma unroll 1
+                for (int sl = 0; sl < 4; ++sl) {                         // 128 value columns: half sl / 2 of O, columns 128 (sl % 2) ..
                     const uint32_t d = tmem_base + (sl & 1) * 128 + (static_cast<uint32_t>((sl >> 1) * 16) << 16);
 #pragma unroll
                     for (int ks = 0; ks < kTile / 16; ++ks)
-                        umma_f16_elect_acc(d, p_desc + ks * 2, v_desc + sl * (2 * kBlockBytes / 16) + ks * (16 * 128 / 16), kIdescPV, (i | ks) ? 1u : 0u);
+                        umma_f16_elect_acc(d, p_desc + ks * 2, v_desc + ks * (16 * 128 / 16), kIdescPV, (i | ks) ? 1u : 0u);
                     umma_commit_elect(bar_slot_empty + 8 * (kSlots * st + sl));
+                    v_desc += 2 * kBlockBytes / 16;
                 }
                 umma_commit_elect(bar_pv_done);
             }
@@ -324,7 +344,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             }
             if (!ok) give_up(DEV_TIMEOUT_PRODUCER);
         }
-    } else if (!Q4 && warp == 1) {
+    } else if (!Q4 && warp == 3) {
         // ------------------------------------------------------------ bf16 rows
         if (lane == 0) {
             tma_prefetch_desc(&kv_map);
@@ -386,41 +406,49 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
     } else if (Q4 && warp >= 8) {
         // ------------------------------------------------------------ 4-bit rows
-        // A warp has rows 8w .. 8w + 7 of every tile. Codes: lane = 8 (2 block + half) + rr reads the 16 bytes (one scale group) of half
-        // `half` of a slot's block `block` of row rr, and stores four 16-byte chunks; eight consecutive lanes then store to eight
-        // different chunk positions (no bank conflicts). Positional columns: lane = 8 row + chunk, two rows a lane. Everything of the
-        // next tile is in registers before this tile's slot is free.
-        const int w = warp - 8;
+        // Warps 0..3 fill slots 0 and 2 of every tile, warps 4..7 slots 4 (positional columns), 1 and 3: a slot's hand-over (wait, fence,
+        // arrive) takes as long as its copying, so two slots are under way at a time. A warp has rows 16w .. 16w + 15: lane =
+        // 8 (2 block + half) + rr reads the 16 bytes (one scale group) of half `half` of a slot's block `block` of rows rr and rr + 8, and
+        // stores four 16-byte chunks of each; eight consecutive lanes then store to eight different chunk positions (no bank
+        // conflicts). Positional columns: lane = 8 row + chunk, four rows a lane. Everything of the next tile is in registers
+        // before this tile's slot is free, expanded before the wait for the slot.
+        const int w = (warp - 8) & 3, odd = (warp - 8) >> 2;
         const int rr = lane & 7, blk = lane >> 4, half = (lane >> 3) & 1;
-        const int my_row = w * 8 + rr;
         const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
-        uint4 code[4], rope[2];                               // of the tile being fetched
-        uint16_t scale[4];
+        uint4 code[2][2], rope[4];                            // [slot odd or odd + 2][row rr or rr + 8] of the tile being fetched
+        uint16_t scale[2][2];
         uint32_t nx_mask = 0;
         int64_t len = 0, base = 0;
         const int32_t* sel = nullptr;
-        int64_t src;                                          // cache row of this lane's row in the tile being fetched, -1: none
+        int64_t src[2];                                       // cache rows of this lane's rows in the tile being fetched, -1: none
         auto locate = [&](int t) {                            // tile t of the piece's sequence
-            int64_t r = static_cast<int64_t>(t) * kTile + my_row;
-            bool use = r < len;
-            if (sel != nullptr) {
-                r = use ? __ldg(sel + r) : -1;
-                use = r >= 0;
+            nx_mask = 0;
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                int64_t r = static_cast<int64_t>(t) * kTile + w * 16 + it * 8 + rr;
+                bool use = r < len;
+                if (sel != nullptr) {
+                    r = use ? __ldg(sel + r) : -1;
+                    use = r >= 0;
+                }
+                r += base;
+                src[it] = use && r >= 0 && r < p.a.n_kv ? r : -1;
+                nx_mask |= (__ballot_sync(0xFFFFFFFFu, src[it] >= 0) & 255u) << (8 * it);
             }
-            r += base;
-            src = use && r >= 0 && r < p.a.n_kv ? r : -1;
-            nx_mask = __ballot_sync(0xFFFFFFFFu, src >= 0) & 255u;
         };
-        auto fetch_codes = [&](int sl) {
-            const int cc = sl * 4 + blk * 2 + half;
-            const uint8_t* row = kv + (src < 0 ? 0 : src) * kLatentQ4RowBytes;
-            code[sl] = src < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(row) + cc);
-            scale[sl] = src < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(row + kLatentQ4ScaleOff) + cc);
+        auto fetch_codes = [&](int u) {
+            const int cc = (2 * u + odd) * 4 + blk * 2 + half;
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const uint8_t* row = kv + (src[it] < 0 ? 0 : src[it]) * kLatentQ4RowBytes;
+                code[u][it] = src[it] < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(row) + cc);
+                scale[u][it] = src[it] < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(row + kLatentQ4ScaleOff) + cc);
+            }
         };
         auto fetch_rope = [&]() {
 #pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int64_t s = __shfl_sync(0xFFFFFFFFu, src, it * 4 + (lane >> 3));
+            for (int it = 0; it < 4; ++it) {
+                const int64_t s = __shfl_sync(0xFFFFFFFFu, src[it >> 1], (it & 1) * 4 + (lane >> 3));
                 rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + (lane & 7));
             }
         };
@@ -446,9 +474,9 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         ahead_piece();
         if (more) {
             locate(apc.t0);
-            fetch_rope();
-#pragma unroll
-            for (int sl = 0; sl < 4; ++sl) fetch_codes(sl);
+            if (odd) fetch_rope();
+            fetch_codes(0);
+            fetch_codes(1);
         }
         while (more && ok) {
             // store tile `tile` (in registers), fetching the next as the registers come free
@@ -456,33 +484,52 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             uint8_t* dst = stage_smem + st * kStageBytes;
             const uint32_t mask = nx_mask;
             if (++ai == apc.n) ahead_piece();
-            if (more) locate(apc.t0 + ai);
+            if (more) {
+                locate(apc.t0 + ai);
+                // dense rows lie one behind the other: ask the L2 for a tile further ahead (one warp of one CTA of the group)
+                const int64_t soon = base + static_cast<int64_t>(apc.t0 + ai + 2) * kTile;
+                if (sel == nullptr && way == 0 && warp == 8 && lane == 0 && ai + 2 < apc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                    l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
+            }
             auto publish = [&](int sl) {
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_slot_full + 8 * (kSlots * st + sl));
             };
-            ok = wait_warp(bar_slot_empty + 8 * (kSlots * st + 4), ph);
-            if (!ok) break;
+            if (odd) {
+                ok = wait_warp(bar_slot_empty + 8 * (kSlots * st + 4), ph);
+                if (!ok) break;
 #pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int r = it * 4 + (lane >> 3);
-                *reinterpret_cast<uint4*>(dst + 8 * kBlockBytes + (w * 8 + r) * 128 + (((lane & 7) ^ r) << 4)) = rope[it];
+                for (int it = 0; it < 4; ++it) {
+                    const int r = w * 16 + it * 4 + (lane >> 3);
+                    *reinterpret_cast<uint4*>(dst + 8 * kBlockBytes + r * 128 + (((lane & 7) ^ (r & 7)) << 4)) = rope[it];
+                }
+                publish(4);
             }
-            publish(4);
-            if (more) fetch_rope();
 #pragma unroll
-            for (int sl = 0; sl < 4; ++sl) {
+            for (int u = 0; u < 2; ++u) {
+                const int sl = 2 * u + odd;
+                uint4 value[2][4];
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const __nv_bfloat162 s2 = scale_pair(scale[u][it]);
+                    const uint32_t word[4] = {code[u][it].x, code[u][it].y, code[u][it].z, code[u][it].w};
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) value[it][v] = dequant8_q4(word[v], s2);
+                }
+                if (more) {                                   // behind the expansion: it must not wait for loads younger than its own
+                    if (u == 0 && odd) fetch_rope();
+                    fetch_codes(u);
+                }
                 ok = wait_warp(bar_slot_empty + 8 * (kSlots * st + sl), ph);
                 if (!ok) break;
-                uint8_t* row = dst + (2 * sl + blk) * kBlockBytes + my_row * 128;
-                const __nv_bfloat162 s2 = scale_pair(scale[sl]);
-                const uint32_t word[4] = {code[sl].x, code[sl].y, code[sl].z, code[sl].w};
+                uint8_t* row = dst + (2 * sl + blk) * kBlockBytes + (w * 16 + rr) * 128;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + (((half * 4 + v) ^ rr) << 4)) = dequant8_q4(word[v], s2);
-                if (sl == 0 && lane == 0) mask_smem[st * 8 + w] = static_cast<uint8_t>(mask);
+                for (int it = 0; it < 2; ++it)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + it * 1024 + (((half * 4 + v) ^ rr) << 4)) = value[it][v];
+                if (sl == 0 && lane == 0) *reinterpret_cast<uint16_t*>(mask_smem + st * 8 + 2 * w) = static_cast<uint16_t>(mask);
                 publish(sl);
-                if (more) fetch_codes(sl);
             }
             ++tile;
         }
@@ -494,7 +541,8 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         const int quarter = warp & 3, g = lane >> 2, j = lane & 3;
         const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         const int row0 = quarter * 16 + g;
-        uint8_t* const p_row = p_smem + row0 * 128 + 4 * j;            // row g + 8 lies 1024 bytes further, same swizzle
+        // lane l gives the address of row l % 8 of matrix l / 8: rows 0..7 | 8..15 of an even chunk, then of the odd one
+        const uint32_t p_addr = smem_u32(p_smem) + (quarter * 16 + ((lane >> 3) & 1) * 8 + (lane & 7)) * 128;
         // units without tiles: zeros (every CTA looks at its share, a lane each)
         for (int64_t u0 = group; u0 < p.units; u0 += 32 * static_cast<int64_t>(p.groups)) {
             const int64_t mine = u0 + lane * static_cast<int64_t>(p.groups);
@@ -540,14 +588,24 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 tmem_ld_16x256b_x4(lane_base + kColS + st * 64 + 32, s[1]);
                 tmem_ld_wait(s[0]);
                 tmem_ld_wait(s[1]);
+                tcgen05_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_s_free + 8 * st);
                 const int at = (pc.t0 + i) * kTile;
-                float x[2][16];                                       // [row][8 column groups x 2]
+                float x[2][16];                                       // [row][8 column groups x 2], not yet scaled
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) x[h][2 * k + e] = __uint_as_float(s[k >> 2][4 * (k & 3) + 2 * h + e]) * p.scale_log2;
+                        for (int e = 0; e < 2; ++e) x[h][2 * k + e] = __uint_as_float(s[k >> 2][4 * (k & 3) + 2 * h + e]);
+                if (p.sign != 1.f) {                                  // a negative or zero scale: what is scaled grows with the score
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        x[0][k] *= p.sign;
+                        x[1][k] *= p.sign;
+                    }
+                }
                 if (Q4 && p.a.topk) {
                     const uint2 mv = *reinterpret_cast<const uint2*>(mask_smem + st * 8);       // byte k: rows 8k .. 8k + 7
 #pragma unroll
@@ -573,11 +631,12 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 bool move = false;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float mt = x[h][0];
+                    float m4[4];                                      // short chains
 #pragma unroll
-                    for (int k = 1; k < 16; ++k) mt = fmaxf(mt, x[h][k]);
+                    for (int k = 0; k < 4; ++k) m4[k] = fmaxf(fmaxf(x[h][k], x[h][k + 4]), fmaxf(x[h][k + 8], x[h][k + 12]));
+                    float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
                     mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, 1));
-                    mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, 2));
+                    mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, 2)) * p.scale_log2;
                     alpha[h] = 1.f;
                     if (mt > m_ref[h] + kMoveThreshold) {             // also the first usable score (m_ref = -inf)
                         alpha[h] = m_ref[h] == -INFINITY ? 0.f : exp2_fast(m_ref[h] - mt);
@@ -590,14 +649,14 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float ref = m_ref[h] == -INFINITY ? 0.f : m_ref[h];
-                    float sum = 0.f;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float p0 = exp2_fast(x[h][2 * k] - ref), p1 = exp2_fast(x[h][2 * k + 1] - ref);
-                        sum += p0 + p1;
+                        const float p0 = exp2_fast(__fmaf_rn(x[h][2 * k], p.scale_log2, -ref)), p1 = exp2_fast(__fmaf_rn(x[h][2 * k + 1], p.scale_log2, -ref));
+                        sum[k & 3] += p0 + p1;
                         pk[h][k] = pack2(p0, p1);
                     }
-                    l[h] += sum;
+                    l[h] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 }
                 const bool any_move = __any_sync(0xFFFFFFFFu, move);
                 // the previous tile's product has read P (and, for a rescale, written O); the piece's first tile: the product before it was
@@ -622,9 +681,8 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t*>(p_row + h * 1024 + ((k ^ g) << 4)) = pk[h][k];
+                for (int c = 0; c < 4; ++c)                           // chunks 2c, 2c + 1 of rows 0..7 and 8..15: four 8 x 8 matrices
+                    stmatrix_x4(p_addr + (((2 * c + (lane >> 4)) ^ (lane & 7)) << 4), pk[0][2 * c], pk[1][2 * c], pk[0][2 * c + 1], pk[1][2 * c + 1]);
                 fence_proxy_async_smem();
                 tcgen05_fence_before_sync();
                 __syncwarp();
@@ -790,7 +848,8 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     int32_t* tiles = reinterpret_cast<int32_t*>(ws + y.tiles_off);
     int2* starts = reinterpret_cast<int2*>(ws + y.starts_off);
     int32_t* runs = reinterpret_cast<int32_t*>(ws + y.runs_off);
-    const Params p{a, tiles, starts, runs, y.units, y.blocks_per_seq, y.ways, y.groups, a.scale * 1.4426950408889634f, static_cast<__nv_bfloat16*>(out), lse,
+    const Params p{a, tiles, starts, runs, y.units, y.blocks_per_seq, y.ways, y.groups, a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f,
+                   a.scale > 0.f ? 1.f : (a.scale < 0.f ? -1.f : 0.f), static_cast<__nv_bfloat16*>(out), lse,
                    reinterpret_cast<float*>(ws + y.out_off), reinterpret_cast<float*>(ws + y.lse_off), status};
     cudaError_t e;
     if (a.topk) {

@@ -309,6 +309,12 @@ __device__ __forceinline__ uint64_t umma_smem_desc_noswizzle(uint32_t smem_addr,
     return d;
 }
 
+// Four 8 x 8 matrices of 16-bit elements to shared memory; lane l addresses row l % 8 of matrix l / 8, and register i of lane
+// l holds elements 2 (l % 4), + 1 of row l / 4 of matrix i.
+__device__ __forceinline__ void stmatrix_x4(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
+}
+
 // ---------------------------------------------------------------- cp.async (16-byte gathers) and proxy fence
 __device__ __forceinline__ void cp_async_16(uint32_t dst_smem, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
