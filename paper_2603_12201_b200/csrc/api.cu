@@ -74,13 +74,13 @@ bool encode_operand_map(CUtensorMap* map, const void* base, int64_t rows, int d,
     return r == CUDA_SUCCESS;
 }
 
-// The value columns of latent rows [rows, 576] bf16 as [8 column blocks][rows][64]: a box of 64 columns, 64 rows and 2 blocks
-// lands as two swizzled operand blocks with one instruction.
-bool encode_value_map(CUtensorMap* map, const void* base, int64_t rows) {
+// The value columns of latent rows [rows, 576] bf16 as [8 column blocks][rows][64]: a box of 64 columns, box_rows rows and
+// box_blocks blocks lands as box_blocks swizzled operand blocks with one instruction.
+bool encode_value_map(CUtensorMap* map, const void* base, int64_t rows, int box_rows, int box_blocks) {
     DeviceInfo& di = device_info();
     const cuuint64_t gdim[3] = {64u, static_cast<cuuint64_t>(rows), 8u};
     const cuuint64_t gstride[2] = {1152u, 128u};
-    const cuuint32_t box[3] = {64u, 64u, 2u};
+    const cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(box_blocks)};
     const cuuint32_t estr[3] = {1u, 1u, 1u};
     return di.encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), gdim, gstride, box, estr,
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -588,14 +588,19 @@ idxc_status run_latent_attn(const LatentArgs& a, int d_qk, int d_v, void* out, f
         return IDXC_ERR_WORKSPACE;
     DeviceInfo& di = device_info();
     if (!di.ok) return IDXC_ERR_CUDA;
-    CUtensorMap q_map, kv_map, value_map;
-    if (!encode_operand_map(&q_map, a.q, a.B * a.n_step * a.H, 576, false, 64)) return IDXC_ERR_CUDA;
+    LatentMaps maps;
+    if (!encode_operand_map(&maps.q, a.q, a.B * a.n_step * a.H, 576, false, 64)) return IDXC_ERR_CUDA;
+    maps.rope = maps.k = maps.v = maps.q;                      // not read with 4-bit rows or without rows
     LatentArgs run = a;
     if (a.n_kv == 0 && !a.topk) run.max_len = 0;               // no rows: every token sees nothing
-    if (a.q4 || a.n_kv == 0) kv_map = value_map = q_map;       // not read
-    else if (!encode_operand_map(&kv_map, a.kv, a.n_kv, 576, false, 64) || !encode_value_map(&value_map, a.kv, a.n_kv)) return IDXC_ERR_CUDA;
+    if (!a.q4 && a.n_kv > 0) {
+        const bool pair = latent_attn_ways(a.n_step, a.H) == 2;
+        if (!encode_operand_map(&maps.rope, a.kv, a.n_kv, 576, false, pair ? 32 : 64) || !encode_value_map(&maps.v, a.kv, a.n_kv, 64, pair ? 4 : 2) ||
+            (pair && !encode_value_map(&maps.k, a.kv, a.n_kv, 32, 8)))
+            return IDXC_ERR_CUDA;
+    }
     int n_l = 0;
-    const cudaError_t e = launch_latent_attn(run, out, lse, workspace, q_map, kv_map, value_map, di.status_ptr, di.sm_count,
+    const cudaError_t e = launch_latent_attn(run, out, lse, workspace, maps, di.status_ptr, di.sm_count,
                                              static_cast<cudaStream_t>(cuda_stream), &n_l);
     g_launches += n_l;
     return e == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;

@@ -132,13 +132,20 @@ struct LatentArgs {
     int H;
     float scale;
 };
-// latent_attn.cu. q_map: q as [B * n_step * H, 576] bf16, kv_map: kv as [n_kv, 576] bf16, both with the 128-byte swizzle and boxes of
-// 64 columns x 64 rows; value_map: kv's value columns as [8 blocks][n_kv][64], boxes of two blocks. The last two are not used with q4. At most kLatentMaxGrid CTAs run. *launches is raised by the kernels launched.
+// Tensor maps of the attention over latent rows, all with the 128-byte swizzle. q: [B * n_step * H, 576], boxes of 64 columns x 64 rows.
+// With bf16 rows also, for one CTA a unit (latent_attn_ways == 1) | a pair (2):
+//   rope: [n_kv, 576], boxes of 64 columns x 64 | 32 rows
+//   v: value columns as [8 blocks][n_kv][64], boxes of 2 | 4 blocks x 64 rows          k: (pair) the same, boxes of 8 blocks x 32 rows
+struct LatentMaps {
+    CUtensorMap q, rope, k, v;
+};
+int latent_attn_ways(int n_step, int H);
+// latent_attn.cu. At most kLatentMaxGrid CTAs run. *launches is raised by the kernels launched.
 constexpr int kLatentMaxGrid = 160;
 size_t latent_attn_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H);
 bool latent_attn_fits(int64_t B, int n_step, int64_t max_len, int H);      // the tile count of the call stays below 2^31
-cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const CUtensorMap& q_map, const CUtensorMap& kv_map,
-                               const CUtensorMap& value_map, unsigned int* status, int sm_count, cudaStream_t stream, int* launches);
+cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const LatentMaps& maps, unsigned int* status, int sm_count,
+                               cudaStream_t stream, int* launches);
 cudaError_t launch_attn_weights(const LatentArgs& a, const float* lse, float beta, float* acc, int64_t ld, cudaStream_t stream);
 
 // latent_cache.cu

@@ -24,18 +24,12 @@
 // other's operands.
 // bf16 rows come by TMA (the tail of a sequence is cleared in shared memory: rows behind it may hold NaN). 4-bit rows are read
 // into registers a tile ahead by eight warps and expanded into the stage (exact, see latent_format.cuh).
-#include <cuda_bf16.h>
-
-#include "kernels.h"
-#include "latent_format.cuh"
-#include "ptx_sm100.cuh"
+#include "latent_attn.cuh"
 
 namespace idxc {
+using namespace latent;
 namespace {
 
-constexpr int kTile = 64;                           // cache rows of a tile
-constexpr int kRows = 64;                           // query rows of a CTA
-constexpr int kBlocks = 9;                          // 64-column blocks of a row
 constexpr int kSlots = 5;                           // slots of a stage: blocks 2s, 2s + 1 for s < 4, block 8
 constexpr uint32_t kBlockBytes = kTile * 128;
 constexpr uint32_t kStageBytes = kBlocks * kBlockBytes;
@@ -45,38 +39,9 @@ constexpr uint32_t kBarBytes = 512;
 constexpr uint32_t kSmemBytes = kQBytes + 2 * kStageBytes + kPBytes + kBarBytes + 1024;
 static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
 constexpr uint32_t kColS = 256;
-constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
 constexpr int kWarpsBf16 = 8;                       // 0 scores | 1 P V | 2 Q | 3 rows (TMA) | 4..7 softmax
 constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 idle | 4..7 softmax | 8..15 rows
 constexpr int kSlotWarps = 4;                       // warps that fill a slot (4-bit rows)
-
-struct Params {
-    LatentArgs a;
-    const int32_t* tiles;        // [units] tiles of every unit
-    const int2* starts;          // [groups + 1] (unit, tile) at which a group's run begins
-    const int32_t* runs;         // [groups + 1] first tile of the run in the end-to-end order
-    int64_t units;               // (sequence, block of 64 * ways query rows)
-    int blocks_per_seq;          // units of a sequence
-    int ways;                    // CTAs of a group: 1 or 2, each 64 rows
-    int groups;
-    float scale_log2;            // |scale| * log2(e), 1 for a zero scale
-    float sign;                  // 1, -1 or 0: scores are multiplied by it first
-    __nv_bfloat16* out;
-    float* lse;
-    float* part_out;             // [groups][2][ways][64][512]
-    float* part_lse;             // [groups][2][ways][64]
-    unsigned int* status;
-};
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
 
 // ---------------------------------------------------------------- plan
 // Selected rows: tiles of query t up to its last usable entry.
@@ -146,43 +111,11 @@ latent_plan_kernel(const LatentArgs a, int64_t units, int blocks_per_seq, int gr
     }
 }
 
-// ---------------------------------------------------------------- the walk of a group over its run
-struct Piece {
-    int64_t unit;
-    int t0, n;            // first tile, number of tiles
-    bool whole;           // all tiles of the unit
-};
-struct Walk {
-    const int32_t* tiles;
-    int64_t unit;
-    int t, left;
-    __device__ __forceinline__ Walk(const Params& p, int group) : tiles(p.tiles), unit(0), t(0), left(__ldg(p.runs + group + 1) - __ldg(p.runs + group)) {
-        if (left > 0) {
-            const int2 s = __ldg(p.starts + group);
-            unit = s.x;
-            t = s.y;
-        }
-    }
-    __device__ __forceinline__ bool next(Piece& pc) {
-        if (left <= 0) return false;
-        int nt = __ldg(tiles + unit);
-        while (nt == 0) nt = __ldg(tiles + ++unit);         // left > 0: a unit with tiles follows
-        pc.unit = unit;
-        pc.t0 = t;
-        pc.n = min(nt - t, left);
-        pc.whole = t == 0 && pc.n == nt;
-        left -= pc.n;
-        ++unit;
-        t = 0;
-        return true;
-    }
-};
-
 // ---------------------------------------------------------------- main kernel
 template <bool Q4>
 __global__ void __launch_bounds__((Q4 ? kWarpsQ4 : kWarpsBf16) * 32, 1)
-latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map,
-                   const __grid_constant__ CUtensorMap value_map, const Params p) {
+latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap rope_map,
+                   const __grid_constant__ CUtensorMap v_map, const Params p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* q_smem = smem;
@@ -205,12 +138,12 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     static_assert(34 * 8 <= kBarBytes, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int group = blockIdx.x / p.ways, way = blockIdx.x - group * p.ways;
+    const int group = blockIdx.x;
     const int seq_rows = p.a.n_step * p.a.H;
     // query rows of this CTA in a unit: first row within the sequence, and how many
     auto rows_of = [&](int64_t unit, int64_t& seq, int& r0) -> int {
         seq = unit / p.blocks_per_seq;
-        r0 = (static_cast<int>(unit - seq * p.blocks_per_seq) * p.ways + way) * kRows;
+        r0 = static_cast<int>(unit - seq * p.blocks_per_seq) * kRows;
         return min(kRows, seq_rows - r0);
     };
     auto seq_len = [&](int64_t seq) -> int64_t {
@@ -263,7 +196,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         constexpr uint32_t kIdescS = umma_idesc(1, 1, kRows, kTile);
         const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
         while (ok && walk.next(pc)) {
-            if (rows_of(pc.unit, seq, r0) <= 0) continue;
+            rows_of(pc.unit, seq, r0);
             ok = wait_warp(bar_q_full, item & 1u);
             for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {      // (a vote: the compiler sees a uniform loop)
                 const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
@@ -307,7 +240,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         constexpr uint32_t kIdescPV = umma_idesc(1, 1, kRows, 128) | kUmmaBMajorMN;
         const uint64_t p_desc = umma_smem_desc_sw128(smem_u32(p_smem));
         while (ok && walk.next(pc)) {
-            if (rows_of(pc.unit, seq, r0) <= 0) continue;
+            rows_of(pc.unit, seq, r0);
             ok = wait_warp(bar_o_free, (item & 1u) ^ 1u);                // the previous piece's output has been read
             for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {
                 const uint32_t st = tile & 1u;
@@ -334,7 +267,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         if (lane == 0) {
             tma_prefetch_desc(&q_map);
             while (ok && walk.next(pc)) {
-                if (rows_of(pc.unit, seq, r0) <= 0) continue;
+                rows_of(pc.unit, seq, r0);
                 ok = mbar_wait(bar_q_empty, (item & 1u) ^ 1u, abort_flag, kWaitCycleBudget, 200);
                 if (!ok) break;
                 mbar_arrive_expect_tx(bar_q_full, kQBytes);
@@ -347,12 +280,12 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     } else if (!Q4 && warp == 3) {
         // ------------------------------------------------------------ bf16 rows
         if (lane == 0) {
-            tma_prefetch_desc(&kv_map);
-            tma_prefetch_desc(&value_map);
+            tma_prefetch_desc(&rope_map);
+            tma_prefetch_desc(&v_map);
         }
         uint32_t tails = 0;
         while (ok && walk.next(pc)) {
-            if (rows_of(pc.unit, seq, r0) <= 0) continue;
+            rows_of(pc.unit, seq, r0);
             const int64_t len = seq_len(seq);
             const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
             for (int i = 0; i < pc.n && ok; ++i, ++tile) {
@@ -362,9 +295,9 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 // coordinates outside the cache read zeros; a base far outside is brought to the nearest such place
                 const int64_t first = min(max(base + at, static_cast<int64_t>(-kTile)), p.a.n_kv);
                 const bool tail = len - at < kTile;
-                // ask the L2 for the tile after the next (one CTA of the group: the other reads the same rows)
+                // ask the L2 for the tile after the next
                 const int64_t soon = base + at + 2 * kTile;
-                if (lane == 0 && way == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                if (lane == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
                     l2_prefetch(static_cast<const uint8_t*>(p.a.kv) + soon * kLatentBf16RowBytes, kTile * kLatentBf16RowBytes);
                 if (!tail) {
 #pragma unroll
@@ -374,8 +307,8 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         ok = ok && wait_warp(bar_slot_empty + 8 * (kSlots * st + sl), ph);
                         if (ok && lane == 0) {
                             mbar_arrive_expect_tx(full, (sl == 4 ? 1 : 2) * kBlockBytes);
-                            if (sl == 4) tma_load_2d(to, &kv_map, full, 512, static_cast<int>(first));
-                            else tma_load_3d(to, &value_map, full, 0, static_cast<int>(first), 2 * sl);
+                            if (sl == 4) tma_load_2d(to, &rope_map, full, 512, static_cast<int>(first));
+                            else tma_load_3d(to, &v_map, full, 0, static_cast<int>(first), 2 * sl);
                         }
                     }
                     if (!ok) break;
@@ -386,7 +319,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if (lane == 0) {
                         mbar_arrive_expect_tx(bar_tail, kStageBytes);
                         for (int b = 0; b < kBlocks; ++b)
-                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &kv_map, bar_tail, b * 64, static_cast<int>(first));
+                            tma_load_2d(smem_u32(dst + b * kBlockBytes), &rope_map, bar_tail, b * 64, static_cast<int>(first));
                     }
                     ok = wait_warp(bar_tail, tails & 1u);
                     if (!ok) break;
@@ -459,16 +392,13 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         bool more = false;
         auto ahead_piece = [&]() {
             more = false;
-            while (ahead.next(apc)) {
-                int64_t s;
-                int rr0;
-                if (rows_of(apc.unit, s, rr0) <= 0) continue;
+            if (ahead.next(apc)) {
+                const int64_t s = apc.unit / p.blocks_per_seq;
                 len = seq_len(s);
                 base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
                 sel = p.a.topk ? p.a.topk + s * p.a.k_top : nullptr;
                 ai = 0;
                 more = true;
-                return;
             }
         };
         ahead_piece();
@@ -486,9 +416,9 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             if (++ai == apc.n) ahead_piece();
             if (more) {
                 locate(apc.t0 + ai);
-                // dense rows lie one behind the other: ask the L2 for a tile further ahead (one warp of one CTA of the group)
+                // dense rows lie one behind the other: ask the L2 for a tile further ahead (one warp)
                 const int64_t soon = base + static_cast<int64_t>(apc.t0 + ai + 2) * kTile;
-                if (sel == nullptr && way == 0 && warp == 8 && lane == 0 && ai + 2 < apc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                if (sel == nullptr && warp == 8 && lane == 0 && ai + 2 < apc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
                     l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
             }
             auto publish = [&](int sl) {
@@ -543,23 +473,9 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         const int row0 = quarter * 16 + g;
         // lane l gives the address of row l % 8 of matrix l / 8: rows 0..7 | 8..15 of an even chunk, then of the odd one
         const uint32_t p_addr = smem_u32(p_smem) + (quarter * 16 + ((lane >> 3) & 1) * 8 + (lane & 7)) * 128;
-        // units without tiles: zeros (every CTA looks at its share, a lane each)
-        for (int64_t u0 = group; u0 < p.units; u0 += 32 * static_cast<int64_t>(p.groups)) {
-            const int64_t mine = u0 + lane * static_cast<int64_t>(p.groups);
-            uint32_t none = __ballot_sync(0xFFFFFFFFu, mine < p.units && __ldg(p.tiles + (mine < p.units ? mine : 0)) == 0);
-            for (; none; none &= none - 1) {
-                const int n = rows_of(u0 + (__ffs(none) - 1) * static_cast<int64_t>(p.groups), seq, r0);
-                for (int r = quarter; r < n; r += 4) {
-                    const int64_t at = seq * seq_rows + r0 + r;
-                    reinterpret_cast<uint4*>(p.out + at * 512)[lane] = make_uint4(0, 0, 0, 0);
-                    reinterpret_cast<uint4*>(p.out + at * 512)[32 + lane] = make_uint4(0, 0, 0, 0);
-                    if (p.lse && lane == 0) p.lse[at] = -INFINITY;
-                }
-            }
-        }
+        write_empty_units(p, group, quarter, lane, seq_rows, rows_of);
         while (ok && walk.next(pc)) {
             const int n_rows = rows_of(pc.unit, seq, r0);
-            if (n_rows <= 0) continue;
             // keys that rows g and g + 8 see (dense): the sequence's length less the new tokens behind the row's own
             const int64_t len = seq_len(seq);
             int sees[2];
@@ -705,14 +621,13 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const float f = (lane & 8) ? i1 : i0;
             const int out_row = quarter * 16 + (lane & 15), col0 = (lane >> 4) * 256;
             const int64_t at_row = seq * seq_rows + r0;
-            const int64_t slot = ((static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * p.ways + way) * kRows;
+            const int64_t slot = (static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * kRows;
 #pragma unroll 1
             for (int c = 0; c < 8; ++c) {
                 uint32_t o[32];
                 tmem_ld_32x32b_x32(lane_base + c * 32, o);
                 tmem_ld_wait(o);
-                if (out_row >= n_rows) continue;
-                if (pc.whole) {
+                if (out_row < n_rows && pc.whole) {
                     uint4* dst = reinterpret_cast<uint4*>(p.out + (at_row + out_row) * 512 + col0 + c * 32);
 #pragma unroll
                     for (int v = 0; v < 4; ++v)
@@ -720,13 +635,14 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                                             pack2(__uint_as_float(o[8 * v + 2]) * f, __uint_as_float(o[8 * v + 3]) * f),
                                             pack2(__uint_as_float(o[8 * v + 4]) * f, __uint_as_float(o[8 * v + 5]) * f),
                                             pack2(__uint_as_float(o[8 * v + 6]) * f, __uint_as_float(o[8 * v + 7]) * f));
-                } else {
+                } else if (out_row < n_rows) {
                     float4* dst = reinterpret_cast<float4*>(p.part_out + (slot + out_row) * 512 + col0 + c * 32);
 #pragma unroll
                     for (int v = 0; v < 8; ++v)
                         dst[v] = make_float4(__uint_as_float(o[4 * v]) * f, __uint_as_float(o[4 * v + 1]) * f, __uint_as_float(o[4 * v + 2]) * f,
                                              __uint_as_float(o[4 * v + 3]) * f);
                 }
+                __syncwarp();
             }
             tcgen05_fence_before_sync();
             __syncwarp();
@@ -804,6 +720,12 @@ latent_merge_kernel(const Params p) {
     if (p.lse && c == 0) p.lse[out_row] = z > 0.f ? m + logf(z) : -INFINITY;
 }
 
+}  // namespace
+
+int latent_attn_ways(int n_step, int H) { return static_cast<int64_t>(n_step) * H > kRows ? 2 : 1; }
+
+namespace {
+
 struct Layout {
     int ways, blocks_per_seq, groups;
     int64_t units;
@@ -813,7 +735,7 @@ struct Layout {
 Layout layout_of(int64_t B, int n_step, int64_t max_len, int H, int sm_count) {
     Layout y{};
     const int64_t rows = static_cast<int64_t>(n_step) * H;
-    y.ways = rows > kRows ? 2 : 1;
+    y.ways = latent_attn_ways(n_step, H);
     y.blocks_per_seq = static_cast<int>((rows + y.ways * kRows - 1) / (y.ways * kRows));
     y.units = B * y.blocks_per_seq;
     const int64_t most = y.units * ((max_len + kTile - 1) / kTile);
@@ -841,8 +763,8 @@ bool latent_attn_fits(int64_t B, int n_step, int64_t max_len, int H) {
     return y.units < (int64_t(1) << 31) && (tiles == 0 || y.units <= ((int64_t(1) << 31) - 1) / tiles);
 }
 
-cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const CUtensorMap& q_map, const CUtensorMap& kv_map,
-                               const CUtensorMap& value_map, unsigned int* status, int sm_count, cudaStream_t stream, int* launches) {
+cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const LatentMaps& maps, unsigned int* status, int sm_count,
+                               cudaStream_t stream, int* launches) {
     const Layout y = layout_of(a.B, a.n_step, a.max_len, a.H, sm_count < kLatentMaxGrid ? sm_count : kLatentMaxGrid);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     int32_t* tiles = reinterpret_cast<int32_t*>(ws + y.tiles_off);
@@ -860,13 +782,17 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     ++*launches;
     latent_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, y.units, y.blocks_per_seq, y.groups, tiles, starts, runs);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const void* k = a.q4 ? reinterpret_cast<const void*>(latent_attn_kernel<true>) : reinterpret_cast<const void*>(latent_attn_kernel<false>);
-    if ((e = ensure_max_dynamic_smem(k, kSmemBytes)) != cudaSuccess) return e;
-    const unsigned grid = static_cast<unsigned>(y.groups * y.ways);
     ++*launches;
-    if (a.q4) latent_attn_kernel<true><<<grid, kWarpsQ4 * 32, kSmemBytes, stream>>>(q_map, kv_map, value_map, p);
-    else latent_attn_kernel<false><<<grid, kWarpsBf16 * 32, kSmemBytes, stream>>>(q_map, kv_map, value_map, p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (y.ways == 2) {
+        e = launch_latent_attn_pair(maps, p, stream);
+    } else {
+        const void* k = a.q4 ? reinterpret_cast<const void*>(latent_attn_kernel<true>) : reinterpret_cast<const void*>(latent_attn_kernel<false>);
+        if ((e = ensure_max_dynamic_smem(k, kSmemBytes)) != cudaSuccess) return e;
+        if (a.q4) latent_attn_kernel<true><<<y.groups, kWarpsQ4 * 32, kSmemBytes, stream>>>(maps.q, maps.rope, maps.v, p);
+        else latent_attn_kernel<false><<<y.groups, kWarpsBf16 * 32, kSmemBytes, stream>>>(maps.q, maps.rope, maps.v, p);
+        e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return e;
     if (y.groups > 1) {
         ++*launches;
         const int unit_rows = a.n_step * a.H < y.ways * kRows ? a.n_step * a.H : y.ways * kRows;

@@ -1,0 +1,561 @@
+// Attention over latent cache rows for 65 to 128 query rows (all heads of a latent-attention model): a CTA pair on one tile.
+//
+// tcgen05.mma.cta_group::2 with M = 128 gives each CTA of the pair 64 query rows and issues at the full rate, where two CTAs with
+// M = 64 of their own issue at half of it (measured: N = 64 in 29 clocks, N = 256 in 64, against 32 and 128 for half the rows). Its
+// accumulator puts the first half of the N columns on TMEM lanes 0..63 and the second on lanes 64..127, so a CTA holds
+//   S: 32 columns, lane r = (row r, first 32 cache rows of the tile), lane 64 + r = (row r, last 32)
+//   O: 256 columns, lane r = (row r, value columns 0..255), lane 64 + r = (row r, value columns 256..511)
+// and 64 rows x 512 columns of fp32 output are half of tensor memory.
+// The B operand is split by columns of the product: for the scores CTA c holds the 576 columns of cache rows 32c .. 32c + 31 (K),
+// for P V the value columns 256c .. 256c + 255 of all 64 rows (V). The two overlap, but lie at the same shared-memory offset in both
+// CTAs, so they are two buffers, each double-buffered: K is free when the scores are done, V when the product is, and neither
+// waits for the other's tile. (One shared buffer a tile, as for up to 64 rows, refills only after the product: 2.8 K clocks a tile.)
+// The first CTA's warps 0 and 1 issue for both; loaders and softmax warps of both CTAs arrive on the first one's barriers, and
+// commits are multicast to both.
+// Shared memory of a CTA: Q 9 x [64 x 128 B] | K 2 x 9 x [32 x 128 B] | V 2 x 4 x [64 x 128 B] | P 2 x [64 x 128 B].
+#include "latent_attn.cuh"
+
+namespace idxc {
+using namespace latent;
+namespace {
+
+constexpr uint32_t kQBytes = kBlocks * kRows * 128;
+constexpr int kHalf = kTile / 2;                    // cache rows of a CTA's K
+constexpr uint32_t kKBlock = kHalf * 128;
+constexpr uint32_t kKBytes = kBlocks * kKBlock;
+constexpr uint32_t kVBlock = kTile * 128;
+constexpr uint32_t kVBytes = 4 * kVBlock;
+constexpr uint32_t kPBytes = kRows * 128;
+constexpr uint32_t kBarBytes = 512;
+constexpr uint32_t kSwapBytes = 3 * 4 * 32 * 4;     // what two warps exchange: row maxima, double-buffered, and at the end row sums
+constexpr uint32_t kSmemBytes = kQBytes + 2 * kKBytes + 2 * kVBytes + 2 * kPBytes + kBarBytes + kSwapBytes + 1024;
+static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
+constexpr uint32_t kColS = 256;                     // S buffer b at kColS + 32 b; O in [0, 256)
+constexpr int kWarpsBf16 = 9;                       // 0 scores | 1 P V | 2 Q | 3 K (TMA) | 4..7 softmax | 8 V (TMA)
+constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 idle | 4..7 softmax | 8..11 K | 12..15 V
+
+// barrier over the two warps of 64 threads that share query rows; returns whether both came with ok
+__device__ __forceinline__ bool pair_of_warps_ok(int id, bool ok) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %2, 0;\n\t"
+        "barrier.cta.red.and.pred p, %1, 64, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(ok)) : "memory");
+    return r != 0;
+}
+
+template <bool Q4>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((Q4 ? kWarpsQ4 : kWarpsBf16) * 32, 1)
+latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                        const __grid_constant__ CUtensorMap rope_map, const __grid_constant__ CUtensorMap v_map, const Params p) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* q_smem = smem;
+    uint8_t* k_smem = q_smem + kQBytes;
+    uint8_t* v_smem = k_smem + 2 * kKBytes;
+    uint8_t* p_smem = v_smem + 2 * kVBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(p_smem + 2 * kPBytes);
+    float* swap = reinterpret_cast<float*>(p_smem + 2 * kPBytes + kBarBytes);        // [3][4 warps][32]
+    // barriers that the first CTA's issuing warps wait on (both CTAs arrive there)
+    const uint32_t bar_q_full = smem_u32(bars + 0);
+    const uint32_t bar_k_full = smem_u32(bars + 1);          // [2]
+    const uint32_t bar_v_full = smem_u32(bars + 3);          // [2]
+    const uint32_t bar_s_free = smem_u32(bars + 5);          // [2]
+    const uint32_t bar_p_ready = smem_u32(bars + 7);         // [2]
+    const uint32_t bar_o_free = smem_u32(bars + 9);
+    // barriers that commits reach in both CTAs
+    const uint32_t bar_q_empty = smem_u32(bars + 10);
+    const uint32_t bar_s_full = smem_u32(bars + 11);         // [2] the scores of a tile are done (and its K is free)
+    const uint32_t bar_pv_done = smem_u32(bars + 13);        // [2] the product of a tile is done (and its V and P are free)
+    const uint32_t bar_tail = smem_u32(bars + 15);
+    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 16);
+    volatile uint32_t* abort_flag = tmem_base_slot + 1;
+    // [4 tiles][2]: usable rows of a tile. Four deep: K of tile i + 2 may land before the softmax has looked at tile i, but that of
+    // tile i + 4 follows the scores of tile i + 2, which waited for the softmax of tile i.
+    uint32_t* mask_smem = reinterpret_cast<uint32_t*>(bars + 18);
+    static_assert(22 * 8 <= kBarBytes, "barrier area");
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = static_cast<int>(cluster_ctarank());
+    const int group = blockIdx.x >> 1;
+    const int seq_rows = p.a.n_step * p.a.H;
+    auto rows_of = [&](int64_t unit, int64_t& seq, int& r0) -> int {
+        seq = unit / p.blocks_per_seq;
+        r0 = (static_cast<int>(unit - seq * p.blocks_per_seq) * 2 + rank) * kRows;
+        return min(kRows, seq_rows - r0);
+    };
+    auto seq_len = [&](int64_t seq) -> int64_t {
+        return p.a.topk ? p.a.k_top : min(max(static_cast<int64_t>(__ldg(p.a.lens + seq)), int64_t(0)), p.a.max_len);
+    };
+    auto in_first = [&](uint32_t bar) -> uint32_t { return map_to_cta(bar, 0); };
+
+    if (threadIdx.x == 0) {
+        mbar_init(bar_q_full, 2);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_k_full + 8 * i, Q4 ? 8 : 2);
+            mbar_init(bar_v_full + 8 * i, Q4 ? 8 : 2);
+            mbar_init(bar_s_free + 8 * i, 8);
+            mbar_init(bar_p_ready + 8 * i, 8);
+            mbar_init(bar_s_full + 8 * i, 1);
+            mbar_init(bar_pv_done + 8 * i, 1);
+        }
+        mbar_init(bar_o_free, 8);
+        mbar_init(bar_q_empty, 1);
+        mbar_init(bar_tail, 1);
+        *abort_flag = 0u;
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc_pair(smem_u32(tmem_base_slot), 512);
+        tmem_relinquish_pair();
+    }
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    cluster_sync();
+    tcgen05_fence_after_sync();
+    const uint32_t tmem_base = *tmem_base_slot;
+
+    Walk walk(p, group);
+    Piece pc;
+    int64_t seq;
+    int r0;
+    bool ok = true;
+    uint32_t tile = 0, item = 0;          // counted over the whole kernel: buffers and phases follow from them
+    auto give_up = [&](unsigned int code) {
+        *abort_flag = 1u;
+        st_cluster_u32(map_to_cta(smem_u32(const_cast<uint32_t*>(abort_flag)), static_cast<uint32_t>(rank ^ 1)), 1u);
+        atomicCAS(p.status, 0u, code);
+    };
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag)); };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ scores (first CTA, warp-uniform)
+        constexpr uint32_t kIdescS = umma_idesc(1, 1, 128, kTile);
+        const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
+        while (rank == 0 && ok && walk.next(pc)) {
+            ok = wait_warp(bar_q_full, item & 1u);
+            for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {      // (a vote: the compiler sees a uniform loop)
+                const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
+                ok = wait_warp(bar_s_free + 8 * st, ph ^ 1u) && wait_warp(bar_k_full + 8 * st, ph);
+                if (!ok) break;
+                tcgen05_fence_after_sync();
+                const uint32_t d = tmem_base + kColS + st * 32;
+                uint64_t a_desc = q_desc, b_desc = umma_smem_desc_sw128(smem_u32(k_smem + st * kKBytes));
+#pragma unroll 1
+                for (int b = 0; b < kBlocks; ++b) {
+                    umma_f16_pair_x4<2, 2>(d, a_desc, b_desc, kIdescS, b != 0 ? 1u : 0u);
+                    a_desc += kRows * 128 / 16;
+                    b_desc += kKBlock / 16;
+                }
+                umma_commit_pair_elect(bar_s_full + 8 * st);
+            }
+            if (ok) umma_commit_pair_elect(bar_q_empty);
+            ++item;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_MMA);
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ P V (first CTA)
+        constexpr uint32_t kIdescPV = umma_idesc(1, 1, 128, 256) | kUmmaBMajorMN;
+        while (rank == 0 && ok && walk.next(pc)) {
+            ok = wait_warp(bar_o_free, (item & 1u) ^ 1u);                // the previous piece's output has been read
+            for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {
+                const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
+                ok = wait_warp(bar_v_full + 8 * st, ph) && wait_warp(bar_p_ready + 8 * st, ph);
+                if (!ok) break;
+                tcgen05_fence_after_sync();
+                const uint64_t p_desc = umma_smem_desc_sw128(smem_u32(p_smem + st * kPBytes));
+                const uint64_t v_desc = umma_smem_desc_sw128_mn(smem_u32(v_smem + st * kVBytes), kVBlock);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)                              // 128 value columns of each CTA
+                    umma_f16_pair_x4<2, 16 * 128 / 16>(tmem_base + h * 128, p_desc, v_desc + h * (2 * kVBlock / 16), kIdescPV, i != 0 ? 1u : 0u);
+                umma_commit_pair_elect(bar_pv_done + 8 * st);
+            }
+            ++item;
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_MMA);
+    } else if (warp == 2) {
+        // ------------------------------------------------------------ Q
+        if (lane == 0) {
+            tma_prefetch_desc(&q_map);
+            while (ok && walk.next(pc)) {
+                rows_of(pc.unit, seq, r0);
+                ok = mbar_wait(bar_q_empty, (item & 1u) ^ 1u, abort_flag, kWaitCycleBudget, 200);
+                if (!ok) break;
+                const uint32_t full = in_first(bar_q_full);
+                mbar_arrive_expect_tx_cluster(full, kQBytes);
+                for (int b = 0; b < kBlocks; ++b)
+                    tma_load_2d_pair(smem_u32(q_smem + b * kRows * 128), &q_map, full, b * 64, static_cast<int>(seq * seq_rows + r0));
+                ++item;
+            }
+            if (!ok) give_up(DEV_TIMEOUT_PRODUCER);
+        }
+    } else if (!Q4 && warp == 3) {
+        // ------------------------------------------------------------ K, bf16: rows 32 rank .. of every tile. Rows behind the sequence's end
+        // may hold anything: they only reach scores that the softmax discards.
+        if (lane == 0) {
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&rope_map);
+            while (ok && walk.next(pc)) {
+                const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + pc.unit / p.blocks_per_seq) : 0;
+                for (int i = 0; i < pc.n && ok; ++i, ++tile) {
+                    const uint32_t st = tile & 1u;
+                    const int64_t at = base + static_cast<int64_t>(pc.t0 + i) * kTile;
+                    // ask the L2 for a tile further ahead
+                    const int64_t soon = at + 3 * kTile;
+                    if (rank == 0 && i + 3 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                        l2_prefetch(static_cast<const uint8_t*>(p.a.kv) + soon * kLatentBf16RowBytes, kTile * kLatentBf16RowBytes);
+                    ok = mbar_wait(bar_s_full + 8 * st, ((tile >> 1) & 1u) ^ 1u, abort_flag);
+                    if (!ok) break;
+                    const int first = static_cast<int>(min(max(at + rank * kHalf, static_cast<int64_t>(-kHalf)), p.a.n_kv));
+                    const uint32_t full = in_first(bar_k_full + 8 * st), to = smem_u32(k_smem + st * kKBytes);
+                    mbar_arrive_expect_tx_cluster(full, kKBytes);
+                    tma_load_3d_pair(to, &k_map, full, 0, first, 0);
+                    tma_load_2d_pair(to + 8 * kKBlock, &rope_map, full, 512, first);
+                }
+            }
+            if (!ok) give_up(DEV_TIMEOUT_GATHER);
+        }
+    } else if (!Q4 && warp == 8) {
+        // ------------------------------------------------------------ V, bf16: value columns 256 rank .. of every tile
+        if (lane == 0) tma_prefetch_desc(&v_map);
+        uint32_t tails = 0;
+        while (ok && walk.next(pc)) {
+            rows_of(pc.unit, seq, r0);
+            const int64_t len = seq_len(seq);
+            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            for (int i = 0; i < pc.n && ok; ++i, ++tile) {
+                const uint32_t st = tile & 1u;
+                const int64_t at = static_cast<int64_t>(pc.t0 + i) * kTile;
+                ok = wait_warp(bar_pv_done + 8 * st, ((tile >> 1) & 1u) ^ 1u);
+                if (!ok) break;
+                const int first = static_cast<int>(min(max(base + at, static_cast<int64_t>(-kTile)), p.a.n_kv));
+                uint8_t* dst = v_smem + st * kVBytes;
+                const uint32_t full = in_first(bar_v_full + 8 * st);
+                if (len - at >= kTile) {
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx_cluster(full, kVBytes);
+                        tma_load_3d_pair(smem_u32(dst), &v_map, full, 0, first, 4 * rank);
+                    }
+                } else {
+                    // the sequence ends inside this tile: load, clear the rows behind its end (0 x NaN would reach the output), publish
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar_tail, kVBytes);
+                        tma_load_3d(smem_u32(dst), &v_map, bar_tail, 0, first, 4 * rank);
+                    }
+                    ok = wait_warp(bar_tail, tails & 1u);
+                    if (!ok) break;
+                    ++tails;
+                    const int valid = static_cast<int>(len - at);
+                    for (int b = 0; b < 4; ++b)
+                        for (int o = valid * 128 + lane * 16; o < static_cast<int>(kVBlock); o += 512)
+                            *reinterpret_cast<uint4*>(dst + b * kVBlock + o) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(full);
+                }
+            }
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
+    } else if (Q4 && warp >= 8) {
+        // ------------------------------------------------------------ 4-bit rows, expanded by four warps for K and four for V
+        // Codes: lane = 8 c + rr reads the 16 bytes (one scale group) of a row rr at chunk c and stores four 16-byte pieces; eight
+        // consecutive lanes store to eight different positions of the swizzle (no bank conflicts). Everything of the next
+        // tile is in registers before this tile's buffer is free.
+        const bool is_v = warp >= 12;
+        const int w = warp & 3, rr = lane & 7, c4 = lane >> 3;
+        const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
+        int64_t len = 0, base = 0;
+        const int32_t* sel = nullptr;
+        auto cache_row = [&](int64_t r) -> int64_t {          // row r of the piece's sequence (or selection), -1: takes no part
+            bool use = r < len;
+            if (sel != nullptr) {
+                r = use ? __ldg(sel + r) : -1;
+                use = r >= 0;
+            }
+            r += base;
+            return use && r >= 0 && r < p.a.n_kv ? r : -1;
+        };
+        auto load_codes = [&](int64_t row, int chunk, uint4& code, uint16_t& scale) {
+            const uint8_t* at = kv + (row < 0 ? 0 : row) * kLatentQ4RowBytes;
+            code = row < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(at) + chunk);
+            scale = row < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(at + kLatentQ4ScaleOff) + chunk);
+        };
+        auto store_codes = [&](uint8_t* row, int half, const uint4& code, uint16_t scale) {        // row: start of the row in its block
+            const __nv_bfloat162 s2 = scale_pair(scale);
+            const uint32_t word[4] = {code.x, code.y, code.z, code.w};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + (((half * 4 + v) ^ rr) << 4)) = dequant8_q4(word[v], s2);
+        };
+        int i = 0;
+        bool more = false;
+        auto next_piece = [&]() {
+            more = walk.next(pc);
+            if (!more) return;
+            seq = pc.unit / p.blocks_per_seq;
+            len = seq_len(seq);
+            base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            sel = p.a.topk ? p.a.topk + seq * p.a.k_top : nullptr;
+            i = 0;
+        };
+        next_piece();
+        if (!is_v) {
+            // K: rows 8w .. 8w + 7 of this CTA's half, chunks c4 + 4 t; positional columns: lane = 8 row + chunk, two rows a lane
+            uint4 code[4], rope[2];
+            uint16_t scale[4];
+            uint32_t mask = 0;                                // bits 0..7: these rows of the first half of the tile, 8..15: of the second
+            auto fetch = [&]() {
+                const int64_t t0 = static_cast<int64_t>(pc.t0 + i) * kTile + w * 8 + rr;
+                const int64_t src = cache_row(t0 + rank * kHalf), other = cache_row(t0 + (rank ^ 1) * kHalf);
+                const uint32_t mine = __ballot_sync(0xFFFFFFFFu, src >= 0) & 255u, theirs = __ballot_sync(0xFFFFFFFFu, other >= 0) & 255u;
+                mask = rank == 0 ? mine | (theirs << 8) : theirs | (mine << 8);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) load_codes(src, c4 + 4 * t, code[t], scale[t]);
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const int64_t s = __shfl_sync(0xFFFFFFFFu, src, it * 4 + c4);
+                    rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + rr);
+                }
+                // dense rows lie one behind the other: ask the L2 for a tile further ahead
+                const int64_t soon = base + static_cast<int64_t>(pc.t0 + i + 2) * kTile;
+                if (sel == nullptr && rank == 0 && w == 0 && lane == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                    l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
+            };
+            if (more) fetch();
+            while (more && ok) {
+                const uint32_t st = tile & 1u;
+                uint8_t* dst = k_smem + st * kKBytes;
+                ok = wait_warp(bar_s_full + 8 * st, ((tile >> 1) & 1u) ^ 1u);
+                if (!ok) break;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int chunk = c4 + 4 * t;
+                    store_codes(dst + (chunk >> 1) * kKBlock + (w * 8 + rr) * 128, chunk & 1, code[t], scale[t]);
+                }
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const int r = it * 4 + c4;
+                    *reinterpret_cast<uint4*>(dst + 8 * kKBlock + (w * 8 + r) * 128 + ((rr ^ r) << 4)) = rope[it];
+                }
+                if (lane < 2) reinterpret_cast<uint8_t*>(mask_smem + (tile & 3u) * 2 + lane)[w] = static_cast<uint8_t>(mask >> (8 * lane));
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(in_first(bar_k_full + 8 * st));
+                ++tile;
+                if (++i == pc.n) next_piece();
+                if (more) fetch();
+            }
+        } else {
+            // V: rows 16w + rr and + 8 of the tile, chunks 8 rank + c4 + 4 t
+            uint4 code[2][2];
+            uint16_t scale[2][2];
+            auto fetch = [&]() {
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const int64_t src = cache_row(static_cast<int64_t>(pc.t0 + i) * kTile + w * 16 + it * 8 + rr);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) load_codes(src, 8 * rank + c4 + 4 * t, code[it][t], scale[it][t]);
+                }
+            };
+            if (more) fetch();
+            while (more && ok) {
+                const uint32_t st = tile & 1u;
+                uint8_t* dst = v_smem + st * kVBytes;
+                ok = wait_warp(bar_pv_done + 8 * st, ((tile >> 1) & 1u) ^ 1u);
+                if (!ok) break;
+#pragma unroll
+                for (int it = 0; it < 2; ++it)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int chunk = c4 + 4 * t;
+                        store_codes(dst + (chunk >> 1) * kVBlock + (w * 16 + it * 8 + rr) * 128, chunk & 1, code[it][t], scale[it][t]);
+                    }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(in_first(bar_v_full + 8 * st));
+                ++tile;
+                if (++i == pc.n) next_piece();
+                if (more) fetch();
+            }
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
+    } else if (warp >= 4 && warp < 8) {
+        // ------------------------------------------------------------ softmax and output
+        // Warps q and q ^ 2 share 32 query rows: this one has the tile's rows 32 half .. 32 half + 31 of each and, of the output, value
+        // columns 256 half .. 256 half + 255. They exchange the rows' maxima at every tile, so that both use the same reference.
+        const int q = warp & 3, half = q >> 1;
+        const int row = (q & 1) * 32 + lane;
+        const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
+        uint8_t* const p_row = p_smem + row * 128;
+        write_empty_units(p, group, q, lane, seq_rows, rows_of);
+        // Both warps of a row leave the tile loop at the same barrier or not at all: `ok` is only acted upon there.
+        while (walk.next(pc)) {
+            const int n_rows = rows_of(pc.unit, seq, r0);
+            const int64_t len = seq_len(seq);
+            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            // positions [lo, sees) are seen by this row: those inside the cache, up to the row's own new token
+            int sees = 0;
+            if (row < n_rows) {
+                int64_t n = len;
+                if (!p.a.topk) n = min(len - (p.a.n_step - 1 - (r0 + row) / p.a.H), p.a.n_kv - base);
+                sees = static_cast<int>(max(n, int64_t(0)));
+            }
+            const int lo = p.a.topk ? 0 : static_cast<int>(min(max(-base, int64_t(0)), int64_t(1) << 30));
+            float m_ref = -INFINITY, l = 0.f;
+            for (int i = 0; i < pc.n; ++i, ++tile) {
+                const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
+                ok = ok && wait_warp(bar_s_full + 8 * st, ph);
+                float x[32];
+                float mt = -INFINITY;
+                if (ok) {
+                    tcgen05_fence_after_sync();
+                    uint32_t s[32];
+                    tmem_ld_32x32b_x32(lane_base + kColS + st * 32, s);
+                    const uint32_t usable = Q4 && p.a.topk ? *const_cast<volatile uint32_t*>(mask_smem + (tile & 3u) * 2 + half) : 0xFFFFFFFFu;
+                    tmem_ld_wait(s);
+                    tcgen05_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(in_first(bar_s_free + 8 * st));
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(s[k]);
+                    if (p.sign != 1.f) {                                  // a negative or zero scale: what is scaled grows with the score
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] *= p.sign;
+                    }
+                    const int at = (pc.t0 + i) * kTile + half * kHalf;
+                    if (__any_sync(0xFFFFFFFFu, at + kHalf > sees || at < lo || usable != 0xFFFFFFFFu)) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (at + k >= sees || at + k < lo || !((usable >> k) & 1u)) x[k] = -INFINITY;
+                    }
+                    float m4[4];                                          // short chains
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        m4[k] = fmaxf(x[k], x[k + 4]);
+#pragma unroll
+                        for (int e = 8; e < 32; e += 8) m4[k] = fmaxf(m4[k], fmaxf(x[k + e], x[k + e + 4]));
+                    }
+                    mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;
+                }
+                swap[(st * 4 + q) * 32 + lane] = mt;
+                ok = pair_of_warps_ok(1 + (q & 1), ok);
+                if (!ok) break;
+                mt = fmaxf(mt, swap[(st * 4 + (q ^ 2)) * 32 + lane]);
+                float alpha = 1.f;
+                bool move = false;
+                if (mt > m_ref + kMoveThreshold) {                        // also the first usable score (m_ref = -inf)
+                    alpha = m_ref == -INFINITY ? 0.f : exp2_fast(m_ref - mt);
+                    m_ref = mt;
+                    l *= alpha;
+                    move = true;
+                }
+                const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                uint32_t pk[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float p0 = exp2_fast(__fmaf_rn(x[2 * k], p.scale_log2, -ref)), p1 = exp2_fast(__fmaf_rn(x[2 * k + 1], p.scale_log2, -ref));
+                    sum[k & 3] += p0 + p1;
+                    pk[k] = pack2(p0, p1);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                // P's buffer is free when the product of the tile before the last has read it; a rescale of O waits for the last product
+                ok = wait_warp(bar_pv_done + 8 * st, ph ^ 1u);
+                if (i > 0 && __any_sync(0xFFFFFFFFu, move)) {
+                    ok = ok && wait_warp(bar_pv_done + 8 * (st ^ 1u), ((tile - 1u) >> 1) & 1u);
+                    if (ok) {
+                        tcgen05_fence_after_sync();
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t o[32];
+                            tmem_ld_32x32b_x32(lane_base + c * 32, o);
+                            tmem_ld_wait(o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                            tmem_st_32x32b_x32(lane_base + c * 32, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                if (ok) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        *reinterpret_cast<uint4*>(p_row + st * kPBytes + (((half * 4 + v) ^ (row & 7)) << 4)) =
+                            make_uint4(pk[4 * v], pk[4 * v + 1], pk[4 * v + 2], pk[4 * v + 3]);
+                    fence_proxy_async_smem();
+                    tcgen05_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(in_first(bar_p_ready + 8 * st));
+                }
+            }
+            // the last product (tile - 1), and the other half's part of the sum
+            ok = ok && wait_warp(bar_pv_done + 8 * ((tile - 1u) & 1u), ((tile - 1u) >> 1) & 1u);
+            swap[(2 * 4 + q) * 32 + lane] = l;
+            ok = pair_of_warps_ok(1 + (q & 1), ok);
+            if (!ok) break;
+            tcgen05_fence_after_sync();
+            l += swap[(2 * 4 + (q ^ 2)) * 32 + lane];
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const int64_t at_row = seq * seq_rows + r0 + row;
+            const int64_t slot = ((static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * 2 + rank) * kRows + row;
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+                uint32_t o[32];
+                tmem_ld_32x32b_x32(lane_base + c * 32, o);
+                tmem_ld_wait(o);
+                if (row < n_rows && pc.whole) {
+                    uint4* dst = reinterpret_cast<uint4*>(p.out + at_row * 512 + half * 256 + c * 32);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        dst[v] = make_uint4(pack2(__uint_as_float(o[8 * v]) * inv, __uint_as_float(o[8 * v + 1]) * inv),
+                                            pack2(__uint_as_float(o[8 * v + 2]) * inv, __uint_as_float(o[8 * v + 3]) * inv),
+                                            pack2(__uint_as_float(o[8 * v + 4]) * inv, __uint_as_float(o[8 * v + 5]) * inv),
+                                            pack2(__uint_as_float(o[8 * v + 6]) * inv, __uint_as_float(o[8 * v + 7]) * inv));
+                } else if (row < n_rows) {
+                    float4* dst = reinterpret_cast<float4*>(p.part_out + slot * 512 + half * 256 + c * 32);
+#pragma unroll
+                    for (int v = 0; v < 8; ++v)
+                        dst[v] = make_float4(__uint_as_float(o[4 * v]) * inv, __uint_as_float(o[4 * v + 1]) * inv, __uint_as_float(o[4 * v + 2]) * inv,
+                                             __uint_as_float(o[4 * v + 3]) * inv);
+                }
+                __syncwarp();
+            }
+            tcgen05_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(in_first(bar_o_free));
+            if (half == 0 && row < n_rows) {
+                const float lse = l > 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                if (!pc.whole) p.part_lse[slot] = lse;
+                else if (p.lse) p.lse[at_row] = lse;
+            }
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_EPILOGUE);
+    }
+
+    // ---------------------------------------------------------------- teardown: neither CTA leaves while the other may still reach it
+    __syncwarp();
+    if (*abort_flag) {                       // copies may still be in flight: let them land before the CTA's memory goes
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+    }
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 0) {
+        tcgen05_fence_after_sync();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_latent_attn_pair(const LatentMaps& maps, const Params& p, cudaStream_t stream) {
+    const void* k = p.a.q4 ? reinterpret_cast<const void*>(latent_attn_pair_kernel<true>) : reinterpret_cast<const void*>(latent_attn_pair_kernel<false>);
+    if (cudaError_t e = ensure_max_dynamic_smem(k, kSmemBytes); e != cudaSuccess) return e;
+    const unsigned grid = static_cast<unsigned>(p.groups * 2);
+    if (p.a.q4) latent_attn_pair_kernel<true><<<grid, kWarpsQ4 * 32, kSmemBytes, stream>>>(maps.q, maps.k, maps.rope, maps.v, p);
+    else latent_attn_pair_kernel<false><<<grid, kWarpsBf16 * 32, kSmemBytes, stream>>>(maps.q, maps.k, maps.rope, maps.v, p);
+    return cudaGetLastError();
+}
+
+}  // namespace idxc
