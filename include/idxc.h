@@ -323,12 +323,12 @@ idxc_status idxc_sparse_attention(const void* q, const void* kv, const int32_t* 
  *                  0 2 4 6 1 3 5 7 of the eight
  *        32 bytes  sixteen bf16 scales, one per 32 value columns
  *       128 bytes  the 64 positional columns, bf16
- *     A value column stands for code * scale. Scales written by idxc_quantize_q4 have 5 significant bits, so that
+ *     A value column stands for code * scale (scales up to 1.3125 * 2^123). Scales written by idxc_quantize_q4 have 5 significant bits, so that
  *     code * scale is exact in bf16 and every reader sees the same values.
- * Caches are row-major arrays of rows without gaps, 16-byte aligned.
+ * Caches are row-major arrays of rows without gaps; bf16 rows 16-byte, 4-bit rows 32-byte aligned.
  *
  * idxc_quantize_q4 -- rows of bf16 into a 4-bit cache: a group's scale is the smallest number of 5 significant bits that is
- * at least max|x| / 7 (and at least 2^-100); code = x / scale rounded to nearest, ties to even. Positional columns are copied.
+ * at least max|x| / 7 (and at least 2^-100, at most 1.3125 * 2^123, where codes end at +-7); code = x / scale rounded to nearest, ties to even. Positional columns are copied.
  *   x         [n_tokens, 576] bf16, 16-byte aligned
  *   cache     [cache_rows, 416] bytes
  *   dst_rows  NULL: token r is written at row r (n_tokens <= cache_rows). Otherwise DEVICE int64 [n_tokens]: token r is

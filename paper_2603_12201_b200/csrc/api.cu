@@ -539,7 +539,7 @@ idxc_status idxc_quantize_q4(const void* x, int64_t n_tokens, void* cache, int64
                              void* cuda_stream) {
     if (n_tokens < 0 || cache_rows < 0 || n_tokens > (int64_t(1) << 31) || (!dst_rows && n_tokens > cache_rows)) return IDXC_ERR_INVALID_ARG;
     if (n_tokens == 0) return IDXC_OK;
-    if (!x || !cache || !aligned(x, 16) || !aligned(cache, 16) || (dst_rows && !aligned(dst_rows, 8))) return IDXC_ERR_INVALID_ARG;
+    if (!x || !cache || !aligned(x, 16) || !aligned(cache, 32) || (dst_rows && !aligned(dst_rows, 8))) return IDXC_ERR_INVALID_ARG;
     g_launches += 1;
     return launch_quantize_q4(x, n_tokens, cache, cache_rows, dst_rows, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
                ? IDXC_OK : IDXC_ERR_CUDA;
@@ -549,7 +549,7 @@ idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int6
                                void* cuda_stream) {
     if (n_rows < 0 || cache_rows < 0 || n_rows > (int64_t(1) << 31)) return IDXC_ERR_INVALID_ARG;
     if (n_rows == 0) return IDXC_OK;
-    if (!out || !aligned(out, 16) || (cache_rows > 0 && !cache) || !aligned(cache, 16) || (src_rows && !aligned(src_rows, 8)))
+    if (!out || !aligned(out, 16) || (cache_rows > 0 && !cache) || !aligned(cache, 32) || (src_rows && !aligned(src_rows, 8)))
         return IDXC_ERR_INVALID_ARG;
     g_launches += 1;
     return launch_dequantize_q4(cache, cache_rows, src_rows, n_rows, out, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
@@ -569,7 +569,7 @@ idxc_status check_latent(const LatentArgs& a, int d_qk) {
         a.B * (static_cast<int64_t>(a.n_step) * a.H) >= (int64_t(1) << 31))
         return IDXC_ERR_INVALID_ARG;
     if (a.B == 0) return IDXC_OK;
-    if (!a.q || !aligned(a.q, 16) || (a.n_kv > 0 && !a.kv) || !aligned(a.kv, 16) || (a.kv_base && !aligned(a.kv_base, 8)))
+    if (!a.q || !aligned(a.q, 16) || (a.n_kv > 0 && !a.kv) || !aligned(a.kv, a.q4 ? 32 : 16) || (a.kv_base && !aligned(a.kv_base, 8)))
         return IDXC_ERR_INVALID_ARG;
     if (a.topk ? !aligned(a.topk, 4) : (!a.lens || !aligned(a.lens, 4))) return IDXC_ERR_INVALID_ARG;
     return IDXC_OK;

@@ -10,8 +10,8 @@
 //
 // Work: the tiles of all sequences, laid end to end, are cut into equal runs, one per CTA (pair). A run may start and end
 // inside a sequence: such a piece leaves a normalised fp32 result and its log-sum-exp in the workspace, and a merge kernel
-// weighs the pieces. A run has at most two of them, so the workspace does not grow with the work. A small plan kernel
-// computes the cuts from the lengths on the device.
+// weighs the pieces. A run has at most two of them, so the workspace does not grow with the work. Every CTA works out the
+// cuts for itself from the lengths on the device.
 //
 // Shared memory: Q 9 blocks of [64 rows x 128 B] | 2 stages x 9 blocks of [64 cache rows x 128 B] | P [64 x 128 B], all in the
 // 128-byte swizzle. A block of cache rows is at once the K-major B operand of Q K^T and the MN-major B operand of P V. A stage
@@ -63,54 +63,6 @@ latent_count_kernel(const LatentArgs a, int32_t* __restrict__ tiles) {
     if (threadIdx.x == 0) tiles[t] = (max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3])) + kTile - 1) / kTile;
 }
 
-// Tiles of every unit (dense; selected: already counted), their running sum, and where the equal runs of the groups begin.
-constexpr int kPlanThreads = 1024;
-__global__ void __launch_bounds__(kPlanThreads)
-latent_plan_kernel(const LatentArgs a, int64_t units, int blocks_per_seq, int groups, int32_t* __restrict__ tiles, int2* __restrict__ starts,
-                   int32_t* __restrict__ runs) {
-    __shared__ int s_sum[32];
-    const int64_t per = (units + kPlanThreads - 1) / kPlanThreads;
-    const int64_t u0 = threadIdx.x * per, u1 = min(u0 + per, units);
-    int sum = 0;
-    for (int64_t u = u0; u < u1; ++u) {
-        int n;
-        if (a.topk) {
-            n = tiles[u];
-        } else {
-            const int64_t len = __ldg(a.lens + u / blocks_per_seq);
-            n = static_cast<int>((min(max(len, int64_t(0)), a.max_len) + kTile - 1) / kTile);
-            tiles[u] = n;
-        }
-        sum += n;
-    }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += y;
-    }
-    if (lane == 31) s_sum[warp] = incl;
-    __syncthreads();
-    int before = incl - sum, total = 0;
-    for (int w = 0; w < 32; ++w) {
-        if (w < warp) before += s_sum[w];
-        total += s_sum[w];
-    }
-    for (int g = threadIdx.x; g <= groups; g += kPlanThreads) runs[g] = static_cast<int>(static_cast<int64_t>(total) * g / groups);
-    if (total == 0) return;
-    for (int64_t u = u0; u < u1; ++u) {
-        const int n = tiles[u];
-        // groups whose first tile, total * g / groups rounded down, lies in this unit
-        for (int64_t g = (static_cast<int64_t>(before) * groups + total - 1) / total; g < groups; ++g) {
-            const int first = static_cast<int>(static_cast<int64_t>(total) * g / groups);
-            if (first >= before + n) break;
-            starts[g] = make_int2(static_cast<int>(u), first - before);
-        }
-        before += n;
-    }
-}
-
 // ---------------------------------------------------------------- main kernel
 template <bool Q4>
 __global__ void __launch_bounds__((Q4 ? kWarpsQ4 : kWarpsBf16) * 32, 1)
@@ -141,9 +93,10 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const int group = blockIdx.x;
     const int seq_rows = p.a.n_step * p.a.H;
     // query rows of this CTA in a unit: first row within the sequence, and how many
-    auto rows_of = [&](int64_t unit, int64_t& seq, int& r0) -> int {
-        seq = unit / p.blocks_per_seq;
-        r0 = static_cast<int>(unit - seq * p.blocks_per_seq) * kRows;
+    auto rows_of = [&](uint32_t unit, int64_t& seq, int& r0) -> int {
+        const uint32_t s = unit / static_cast<uint32_t>(p.blocks_per_seq);
+        seq = s;
+        r0 = static_cast<int>(unit - s * p.blocks_per_seq) * kRows;
         return min(kRows, seq_rows - r0);
     };
     auto seq_len = [&](int64_t seq) -> int64_t {
@@ -173,11 +126,18 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         tmem_relinquish_alloc_permit();
     }
     tcgen05_fence_before_sync();
+    const Run run = find_run(p.units, p.tiles, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
+    if (threadIdx.x == 0) {
+        p.starts[group] = make_int2(static_cast<int>(run.unit), run.t);
+        p.runs[group] = run.first;
+        if (group == p.groups - 1) p.runs[p.groups] = run.total;
+    }
+    fence_proxy_async_smem();                                // find_run's words before Q's copy over them
     __syncthreads();
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = *tmem_base_slot;
 
-    Walk walk(p, group);
+    Walk walk(p.tiles, run);
     Piece pc;
     int64_t seq;
     int r0;
@@ -393,7 +353,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         auto ahead_piece = [&]() {
             more = false;
             if (ahead.next(apc)) {
-                const int64_t s = apc.unit / p.blocks_per_seq;
+                const int64_t s = apc.unit / static_cast<uint32_t>(p.blocks_per_seq);
                 len = seq_len(s);
                 base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
                 sel = p.a.topk ? p.a.topk + s * p.a.k_top : nullptr;
@@ -442,7 +402,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 uint4 value[2][4];
 #pragma unroll
                 for (int it = 0; it < 2; ++it) {
-                    const __nv_bfloat162 s2 = scale_pair(scale[u][it]);
+                    const Q4Scale s2 = q4_scale_of(scale[u][it]);
                     const uint32_t word[4] = {code[u][it].x, code[u][it].y, code[u][it].z, code[u][it].w};
 #pragma unroll
                     for (int v = 0; v < 4; ++v) value[it][v] = dequant8_q4(word[v], s2);
@@ -681,41 +641,63 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 __global__ void __launch_bounds__(512)
 latent_merge_kernel(const Params p) {
     const int g = blockIdx.x;
-    if (p.runs[g + 1] == p.runs[g]) return;
     const int2 s = p.starts[g];
-    if (s.y == 0) return;                                     // begins with its unit
-    // the run that holds tile 0 of the unit: the nearest earlier non-empty one must be it
-    int first = g - 1;
-    while (first > 0 && p.runs[first + 1] == p.runs[first]) --first;
-    if (p.starts[first].x == s.x && p.starts[first].y > 0) return;      // an earlier group starts inside this unit too
-    const int end = p.runs[g] - s.y + p.tiles[s.x];           // one past the unit's last tile, end to end
-    int last = g;
-    while (last + 1 < p.groups && p.runs[last + 1] < end) ++last;
-    const int64_t seq = s.x / p.blocks_per_seq;
+    const int run = p.runs[g], run_end = p.runs[g + 1];
+    int first = g > 0 ? g - 1 : 0, first_run = p.runs[first];
+    int2 fs = p.starts[first];
+    if (run_end == run || s.y == 0) return;                   // no tiles, or begins with its unit
+    // the run that holds the tile before this one: the nearest earlier non-empty one
+    for (int next = run; first > 0 && first_run == next;) {
+        next = first_run;
+        first_run = p.runs[--first];
+        fs = p.starts[first];
+    }
+    if (fs.x == s.x && fs.y > 0) return;                      // an earlier group starts inside this unit too
+    const int end = run - s.y + p.tiles(static_cast<uint32_t>(s.x));      // one past the unit's last tile, end to end
+    const uint32_t seq = static_cast<uint32_t>(s.x) / static_cast<uint32_t>(p.blocks_per_seq);
     const int seq_rows = p.a.n_step * p.a.H;
     const int r = blockIdx.y * 4 + (threadIdx.x >> 7), c = threadIdx.x & 127;
     const int r_seq = static_cast<int>(s.x - seq * p.blocks_per_seq) * p.ways * kRows + r;
     if (r >= p.ways * kRows || r_seq >= seq_rows) return;
     const int64_t stride = static_cast<int64_t>(2) * p.ways * kRows;            // rows of a group's two slots
     const int64_t at1 = first * stride + p.ways * kRows + r, at0 = g * stride + r;
-    float m = p.part_lse[at1];
-    for (int k = g; k <= last; ++k) m = fmaxf(m, p.runs[k + 1] > p.runs[k] ? p.part_lse[at0 + (k - g) * stride] : -INFINITY);
+    float m = -INFINITY, z = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float z = 0.f;
-    if (m > -INFINITY) {
-        auto add = [&](int64_t at) {
-            const float w = exp2_fast((p.part_lse[at] - m) * 1.4426950408889634f);
-            const float4 v = reinterpret_cast<const float4*>(p.part_out + at * 512)[c];
-            acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+    // piece 0 is the beginning, piece k > 0 group g + k - 1's; eight at a time, all loads of the eight before their first use
+    bool more = true;
+    for (int k0 = 0; more; k0 += 8) {
+        float ls[8];
+        float4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = k0 + j, grp = g + k - 1;
+            bool in = k == 0;
+            if (k > 0) {
+                const int b0 = grp < p.groups ? p.runs[grp] : end;
+                more = b0 < end;
+                in = more && p.runs[grp + 1] > b0;
+            }
+            const int64_t at = k == 0 ? at1 : at0 + (k - 1) * stride;
+            ls[j] = in ? p.part_lse[at] : -INFINITY;
+            v[j] = in ? reinterpret_cast<const float4*>(p.part_out + at * 512)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, ls[j]);
+        if (top == -INFINITY) continue;
+        const float f = exp2_fast((m - top) * 1.4426950408889634f);
+        m = top;
+        z *= f;
+        acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float w = exp2_fast((ls[j] - top) * 1.4426950408889634f);
+            acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
             z += w;
-        };
-        add(at1);
-#pragma unroll 4
-        for (int k = g; k <= last; ++k)
-            if (p.runs[k + 1] > p.runs[k]) add(at0 + (k - g) * stride);
+        }
     }
     const float inv = z > 0.f ? 1.f / z : 0.f;
-    const int64_t out_row = seq * seq_rows + r_seq;
+    const int64_t out_row = static_cast<int64_t>(seq) * seq_rows + r_seq;
     reinterpret_cast<uint2*>(p.out + out_row * 512)[c] = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
     if (p.lse && c == 0) p.lse[out_row] = z > 0.f ? m + logf(z) : -INFINITY;
 }
@@ -742,7 +724,7 @@ Layout layout_of(int64_t B, int n_step, int64_t max_len, int H, int sm_count) {
     const int64_t cap = sm_count / y.ways;
     y.groups = static_cast<int>(most < 1 ? 1 : (most < cap ? most : cap));
     auto take = [&](size_t bytes) { const size_t at = y.bytes; y.bytes += (bytes + 255) / 256 * 256; return at; };
-    y.tiles_off = take(static_cast<size_t>(y.units) * 4);
+    y.tiles_off = take(static_cast<size_t>(B) * 4);            // counted tiles (selected rows)
     y.starts_off = take(static_cast<size_t>(y.groups + 1) * 8);
     y.runs_off = take(static_cast<size_t>(y.groups + 1) * 4);
     const size_t slots = static_cast<size_t>(y.groups) * 2 * y.ways * kRows;
@@ -770,7 +752,8 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     int32_t* tiles = reinterpret_cast<int32_t*>(ws + y.tiles_off);
     int2* starts = reinterpret_cast<int2*>(ws + y.starts_off);
     int32_t* runs = reinterpret_cast<int32_t*>(ws + y.runs_off);
-    const Params p{a, tiles, starts, runs, y.units, y.blocks_per_seq, y.ways, y.groups, a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f,
+    const UnitTiles unit_tiles{a.topk ? tiles : nullptr, a.lens, a.max_len, static_cast<uint32_t>(y.blocks_per_seq), kTile};
+    const Params p{a, unit_tiles, starts, runs, static_cast<uint32_t>(y.units), y.blocks_per_seq, y.ways, y.groups, a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f,
                    a.scale > 0.f ? 1.f : (a.scale < 0.f ? -1.f : 0.f), static_cast<__nv_bfloat16*>(out), lse,
                    reinterpret_cast<float*>(ws + y.out_off), reinterpret_cast<float*>(ws + y.lse_off), status};
     cudaError_t e;
@@ -779,9 +762,6 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
         latent_count_kernel<<<static_cast<unsigned>(a.B), 128, 0, stream>>>(a, tiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
-    ++*launches;
-    latent_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, y.units, y.blocks_per_seq, y.groups, tiles, starts, runs);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
     ++*launches;
     if (y.ways == 2) {
         e = launch_latent_attn_pair(maps, p, stream);

@@ -15,12 +15,26 @@ constexpr int kRows = 64;                           // query rows of a CTA
 constexpr int kBlocks = 9;                          // 64-column blocks of a row
 constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
 
+// Tiles of a unit: counted beforehand (selected rows), or from its sequence's length.
+struct UnitTiles {
+    const int32_t* counted;      // [units] or nullptr
+    const int32_t* lens;
+    int64_t max_len;
+    uint32_t blocks_per_seq;     // units of a sequence
+    int tile;                    // rows of a tile
+    __device__ __forceinline__ int operator()(uint32_t unit) const {
+        if (counted) return __ldg(counted + unit);
+        const int64_t len = __ldg(lens + unit / blocks_per_seq);
+        return static_cast<int>((min(max(len, int64_t(0)), max_len) + tile - 1) / tile);
+    }
+};
+
 struct Params {
     LatentArgs a;
-    const int32_t* tiles;        // [units] tiles of every unit
-    const int2* starts;          // [groups + 1] (unit, tile) at which a group's run begins
-    const int32_t* runs;         // [groups + 1] first tile of the run in the end-to-end order
-    int64_t units;               // (sequence, block of 64 * ways query rows)
+    UnitTiles tiles;
+    int2* starts;                // [groups] (unit, tile) at which a group's run begins
+    int32_t* runs;               // [groups + 1] first tile of the run in the end-to-end order (both written by the kernel for the merge)
+    uint32_t units;              // (sequence, block of 64 * ways query rows)
     int blocks_per_seq;          // units of a sequence
     int ways;                    // CTAs of a group: 1 or 2, each 64 rows
     int groups;
@@ -43,27 +57,79 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// ---------------------------------------------------------------- the walk of a group over its run
+// ---------------------------------------------------------------- the run of a group, and its walk over it
+// The tiles of all units, laid end to end, are cut into `groups` runs of equal length (to within one). Every CTA finds its own by a
+// scan over the units, which costs about a microsecond where a kernel of its own before this one costs five.
+struct Run {
+    uint32_t unit;        // where it begins
+    int t;
+    int first, n, total;  // first tile end to end, number of tiles, tiles of all units
+};
+__device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, int group, int groups, int* scratch /* shared, 40 words */) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+    const uint32_t n_thr = blockDim.x;
+    int mine = 0;                                    // this thread's unit of the first block of units
+    int sum = 0;
+    for (uint32_t u = threadIdx.x; u < units; u += n_thr) {
+        const int n = tiles(u);
+        if (u < n_thr) mine = n;
+        sum += n;
+    }
+    sum = __reduce_add_sync(0xFFFFFFFFu, sum);
+    if (lane == 0) scratch[warp] = sum;
+    __syncthreads();
+    Run r{0, 0, 0, 0, 0};
+    for (int w = 0; w < n_warps; ++w) r.total += scratch[w];
+    r.first = static_cast<int>(static_cast<int64_t>(r.total) * group / groups);
+    r.n = static_cast<int>(static_cast<int64_t>(r.total) * (group + 1) / groups) - r.first;
+    if (r.n > 0) {                                   // (uniform over the CTA)
+        int before_block = 0;
+        for (uint32_t u0 = 0; u0 < units; u0 += n_thr) {
+            const uint32_t u = u0 + threadIdx.x;
+            const int n = u0 == 0 ? mine : (u < units ? tiles(u) : 0);
+            int incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            __syncthreads();                         // (the last readers of scratch are done)
+            if (lane == 31) scratch[warp] = incl;
+            __syncthreads();
+            int before = before_block + incl - n, all = 0;
+            for (int w = 0; w < n_warps; ++w) {
+                if (w < warp) before += scratch[w];
+                all += scratch[w];
+            }
+            if (r.first >= before && r.first < before + n) {
+                scratch[32] = static_cast<int>(u);
+                scratch[33] = r.first - before;
+            }
+            before_block += all;
+            if (r.first < before_block) break;
+        }
+        __syncthreads();
+        r.unit = static_cast<uint32_t>(scratch[32]);
+        r.t = scratch[33];
+    }
+    __syncthreads();
+    return r;
+}
+
 struct Piece {
-    int64_t unit;
+    uint32_t unit;
     int t0, n;            // first tile, number of tiles
     bool whole;           // all tiles of the unit
 };
 struct Walk {
-    const int32_t* tiles;
-    int64_t unit;
+    const UnitTiles& tiles;
+    uint32_t unit;
     int t, left;
-    __device__ __forceinline__ Walk(const Params& p, int group) : tiles(p.tiles), unit(0), t(0), left(__ldg(p.runs + group + 1) - __ldg(p.runs + group)) {
-        if (left > 0) {
-            const int2 s = __ldg(p.starts + group);
-            unit = s.x;
-            t = s.y;
-        }
-    }
+    __device__ __forceinline__ Walk(const UnitTiles& tl, const Run& r) : tiles(tl), unit(r.unit), t(r.t), left(r.n) {}
     __device__ __forceinline__ bool next(Piece& pc) {
         if (left <= 0) return false;
-        int nt = __ldg(tiles + unit);
-        while (nt == 0) nt = __ldg(tiles + ++unit);         // left > 0: a unit with tiles follows
+        int nt = tiles(unit);
+        while (nt == 0) nt = tiles(++unit);                 // left > 0: a unit with tiles follows
         pc.unit = unit;
         pc.t0 = t;
         pc.n = min(nt - t, left);
@@ -80,11 +146,11 @@ template <typename RowsOf>
 __device__ __forceinline__ void write_empty_units(const Params& p, int group, int quarter, int lane, int seq_rows, RowsOf rows_of) {
     for (int64_t u0 = group; u0 < p.units; u0 += 32 * static_cast<int64_t>(p.groups)) {
         const int64_t mine = u0 + lane * static_cast<int64_t>(p.groups);
-        uint32_t none = __ballot_sync(0xFFFFFFFFu, mine < p.units && __ldg(p.tiles + (mine < p.units ? mine : 0)) == 0);
+        uint32_t none = __ballot_sync(0xFFFFFFFFu, mine < p.units && p.tiles(static_cast<uint32_t>(mine < p.units ? mine : 0)) == 0);
         for (; none; none &= none - 1) {
             int64_t seq;
             int r0;
-            const int n = rows_of(u0 + (__ffs(none) - 1) * static_cast<int64_t>(p.groups), seq, r0);
+            const int n = rows_of(static_cast<uint32_t>(u0 + (__ffs(none) - 1) * static_cast<int64_t>(p.groups)), seq, r0);
             for (int r = quarter; r < n; r += 4) {
                 const int64_t at = seq * seq_rows + r0 + r;
                 reinterpret_cast<uint4*>(p.out + at * 512)[lane] = make_uint4(0, 0, 0, 0);

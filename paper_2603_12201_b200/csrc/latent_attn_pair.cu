@@ -80,9 +80,10 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     const int rank = static_cast<int>(cluster_ctarank());
     const int group = blockIdx.x >> 1;
     const int seq_rows = p.a.n_step * p.a.H;
-    auto rows_of = [&](int64_t unit, int64_t& seq, int& r0) -> int {
-        seq = unit / p.blocks_per_seq;
-        r0 = (static_cast<int>(unit - seq * p.blocks_per_seq) * 2 + rank) * kRows;
+    auto rows_of = [&](uint32_t unit, int64_t& seq, int& r0) -> int {
+        const uint32_t s = unit / static_cast<uint32_t>(p.blocks_per_seq);
+        seq = s;
+        r0 = (static_cast<int>(unit - s * p.blocks_per_seq) * 2 + rank) * kRows;
         return min(kRows, seq_rows - r0);
     };
     auto seq_len = [&](int64_t seq) -> int64_t {
@@ -111,12 +112,19 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         tmem_relinquish_pair();
     }
     tcgen05_fence_before_sync();
+    const Run run = find_run(p.units, p.tiles, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
+    if (threadIdx.x == 0 && rank == 0) {
+        p.starts[group] = make_int2(static_cast<int>(run.unit), run.t);
+        p.runs[group] = run.first;
+        if (group == p.groups - 1) p.runs[p.groups] = run.total;
+    }
+    fence_proxy_async_smem();                                // find_run's words before Q's copy over them
     __syncthreads();
     cluster_sync();
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = *tmem_base_slot;
 
-    Walk walk(p, group);
+    Walk walk(p.tiles, run);
     Piece pc;
     int64_t seq;
     int r0;
@@ -197,7 +205,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             tma_prefetch_desc(&k_map);
             tma_prefetch_desc(&rope_map);
             while (ok && walk.next(pc)) {
-                const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + pc.unit / p.blocks_per_seq) : 0;
+                const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + pc.unit / static_cast<uint32_t>(p.blocks_per_seq)) : 0;
                 for (int i = 0; i < pc.n && ok; ++i, ++tile) {
                     const uint32_t st = tile & 1u;
                     const int64_t at = base + static_cast<int64_t>(pc.t0 + i) * kTile;
@@ -259,124 +267,103 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
     } else if (Q4 && warp >= 8) {
         // ------------------------------------------------------------ 4-bit rows, expanded by four warps for K and four for V
-        // Codes: lane = 8 c + rr reads the 16 bytes (one scale group) of a row rr at chunk c and stores four 16-byte pieces; eight
-        // consecutive lanes store to eight different positions of the swizzle (no bank conflicts). Everything of the next
-        // tile is in registers before this tile's buffer is free.
+        // Lane = 8 c + rr reads the 32 bytes of codes of 64-column block c (or c + 4) of a row rr and stores them as eight 16-byte pieces;
+        // eight consecutive lanes then store to eight different positions of the swizzle (no bank conflicts). The next
+        // tile is in registers and the rows of the one after are looked up while a tile is stored. The code is rolled and shared by
+        // the two kinds on purpose: unrolled over two tiles in registers the roles stalled on instruction fetch (3300 clocks a tile).
         const bool is_v = warp >= 12;
         const int w = warp & 3, rr = lane & 7, c4 = lane >> 3;
         const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
-        int64_t len = 0, base = 0;
+        // this lane's rows of a tile. K: one of this CTA's half, and (for the mask) the same one of the other half; V: two
+        const int off0 = is_v ? w * 16 + rr : rank * kHalf + w * 8 + rr, off1 = is_v ? off0 + 8 : (rank ^ 1) * kHalf + w * 8 + rr;
+        uint32_t code0[8], code1[8], scale0 = 0, scale1 = 0, mask = 0;
+        uint4 rope[2];
+        int64_t len = 0, base = 0, raw[2];                    // raw: position (or selected position) of this lane's rows in the next tile to fetch
         const int32_t* sel = nullptr;
-        auto cache_row = [&](int64_t r) -> int64_t {          // row r of the piece's sequence (or selection), -1: takes no part
-            bool use = r < len;
-            if (sel != nullptr) {
-                r = use ? __ldg(sel + r) : -1;
-                use = r >= 0;
-            }
-            r += base;
-            return use && r >= 0 && r < p.a.n_kv ? r : -1;
-        };
-        auto load_codes = [&](int64_t row, int chunk, uint4& code, uint16_t& scale) {
-            const uint8_t* at = kv + (row < 0 ? 0 : row) * kLatentQ4RowBytes;
-            code = row < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(at) + chunk);
-            scale = row < 0 ? static_cast<uint16_t>(0) : __ldg(reinterpret_cast<const uint16_t*>(at + kLatentQ4ScaleOff) + chunk);
-        };
-        auto store_codes = [&](uint8_t* row, int half, const uint4& code, uint16_t scale) {        // row: start of the row in its block
-            const __nv_bfloat162 s2 = scale_pair(scale);
-            const uint32_t word[4] = {code.x, code.y, code.z, code.w};
-#pragma unroll
-            for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4*>(row + (((half * 4 + v) ^ rr) << 4)) = dequant8_q4(word[v], s2);
-        };
         int i = 0;
-        bool more = false;
-        auto next_piece = [&]() {
-            more = walk.next(pc);
-            if (!more) return;
-            seq = pc.unit / p.blocks_per_seq;
+        auto open_piece = [&]() {
+            if (!walk.next(pc)) return;
+            seq = pc.unit / static_cast<uint32_t>(p.blocks_per_seq);
             len = seq_len(seq);
             base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
             sel = p.a.topk ? p.a.topk + seq * p.a.k_top : nullptr;
             i = 0;
         };
-        next_piece();
-        if (!is_v) {
-            // K: rows 8w .. 8w + 7 of this CTA's half, chunks c4 + 4 t; positional columns: lane = 8 row + chunk, two rows a lane
-            uint4 code[4], rope[2];
-            uint16_t scale[4];
-            uint32_t mask = 0;                                // bits 0..7: these rows of the first half of the tile, 8..15: of the second
-            auto fetch = [&]() {
-                const int64_t t0 = static_cast<int64_t>(pc.t0 + i) * kTile + w * 8 + rr;
-                const int64_t src = cache_row(t0 + rank * kHalf), other = cache_row(t0 + (rank ^ 1) * kHalf);
-                const uint32_t mine = __ballot_sync(0xFFFFFFFFu, src >= 0) & 255u, theirs = __ballot_sync(0xFFFFFFFFu, other >= 0) & 255u;
-                mask = rank == 0 ? mine | (theirs << 8) : theirs | (mine << 8);
+        auto look_up = [&]() {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) load_codes(src, c4 + 4 * t, code[t], scale[t]);
+            for (int e = 0; e < 2; ++e) {
+                const int64_t r = static_cast<int64_t>(pc.t0 + i) * kTile + (e == 0 ? off0 : off1);
+                raw[e] = r < len ? (sel != nullptr ? static_cast<int64_t>(__ldg(sel + r)) : r) : -1;
+            }
+        };
+        auto fetch = [&]() {                                  // the tile that was looked up; then looks up the next
+            int64_t src[2];
 #pragma unroll
-                for (int it = 0; it < 2; ++it) {
-                    const int64_t s = __shfl_sync(0xFFFFFFFFu, src, it * 4 + c4);
+            for (int e = 0; e < 2; ++e) {
+                const int64_t r = raw[e] + base;
+                src[e] = raw[e] >= 0 && r >= 0 && r < p.a.n_kv ? r : -1;
+            }
+            if (!is_v) {
+                const uint32_t mine = __ballot_sync(0xFFFFFFFFu, src[0] >= 0) & 255u, theirs = __ballot_sync(0xFFFFFFFFu, src[1] >= 0) & 255u;
+                mask = rank == 0 ? mine | (theirs << 8) : theirs | (mine << 8);       // bits 0..7: in the first half of the tile, 8..15: the second
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {              // positional columns: lane = 8 row + chunk, two rows a lane
+                    const int64_t s = __shfl_sync(0xFFFFFFFFu, src[0], it * 4 + c4);
                     rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + rr);
                 }
-                // dense rows lie one behind the other: ask the L2 for a tile further ahead
-                const int64_t soon = base + static_cast<int64_t>(pc.t0 + i + 2) * kTile;
-                if (sel == nullptr && rank == 0 && w == 0 && lane == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
-                    l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
-            };
-            if (more) fetch();
-            while (more && ok) {
-                const uint32_t st = tile & 1u;
-                uint8_t* dst = k_smem + st * kKBytes;
-                ok = wait_warp(bar_s_full + 8 * st, ((tile >> 1) & 1u) ^ 1u);
-                if (!ok) break;
+                src[1] = src[0];
+            }
+            const int block0 = is_v ? 4 * rank + c4 : c4, block1 = is_v ? block0 : c4 + 4;
+            const uint8_t* row0 = kv + (src[0] < 0 ? 0 : src[0]) * kLatentQ4RowBytes;
+            const uint8_t* row1 = kv + (src[1] < 0 ? 0 : src[1]) * kLatentQ4RowBytes;
+            load_nc_256(row0 + block0 * 32, src[0] >= 0, code0);
+            load_nc_256(row1 + block1 * 32, src[1] >= 0, code1);
+            scale0 = src[0] < 0 ? 0u : __ldg(reinterpret_cast<const uint32_t*>(row0 + kLatentQ4ScaleOff) + block0);
+            scale1 = src[1] < 0 ? 0u : __ldg(reinterpret_cast<const uint32_t*>(row1 + kLatentQ4ScaleOff) + block1);
+            // dense rows lie one behind the other: ask the L2 for a tile further ahead
+            const int64_t soon = base + static_cast<int64_t>(pc.t0 + i + 2) * kTile;
+            if (sel == nullptr && rank == 0 && warp == 8 && lane == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
+            if (++i == pc.n) open_piece();
+            look_up();
+        };
+        const uint32_t bar_free = is_v ? bar_pv_done : bar_s_full, bar_full = in_first(is_v ? bar_v_full : bar_k_full);
+        const uint32_t buf_bytes = is_v ? kVBytes : kKBytes, step = is_v ? 1024u : 4 * kKBlock;       // from the first 64 columns of this lane to the second
+        uint8_t* const my_dst = is_v ? v_smem + c4 * kVBlock + off0 * 128 : k_smem + c4 * kKBlock + (w * 8 + rr) * 128;
+        const int total = run.n;
+        if (total > 0) {
+            open_piece();
+            look_up();
+            fetch();
+        }
+        for (int t = 0; t < total; ++t) {
+            const uint32_t st = t & 1;
+            ok = wait_warp(bar_free + 8 * st, ((static_cast<uint32_t>(t) >> 1) & 1u) ^ 1u);
+            if (!ok) break;
+            uint8_t* dst = my_dst + st * buf_bytes;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const Q4Scale lo = q4_scale_of(scale0), hi = q4_scale_of(scale0 >> 16);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int chunk = c4 + 4 * t;
-                    store_codes(dst + (chunk >> 1) * kKBlock + (w * 8 + rr) * 128, chunk & 1, code[t], scale[t]);
-                }
+                for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4*>(dst + ((v ^ rr) << 4)) = dequant8_q4(code0[v], v < 4 ? lo : hi);
+#pragma unroll
+                for (int v = 0; v < 8; ++v) code0[v] = code1[v];
+                scale0 = scale1;
+                dst += step;
+            }
+            if (!is_v) {
+                dst = k_smem + st * kKBytes + 8 * kKBlock + w * 8 * 128;
 #pragma unroll
                 for (int it = 0; it < 2; ++it) {
                     const int r = it * 4 + c4;
-                    *reinterpret_cast<uint4*>(dst + 8 * kKBlock + (w * 8 + r) * 128 + ((rr ^ r) << 4)) = rope[it];
+                    *reinterpret_cast<uint4*>(dst + r * 128 + ((rr ^ r) << 4)) = rope[it];
                 }
-                if (lane < 2) reinterpret_cast<uint8_t*>(mask_smem + (tile & 3u) * 2 + lane)[w] = static_cast<uint8_t>(mask >> (8 * lane));
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(in_first(bar_k_full + 8 * st));
-                ++tile;
-                if (++i == pc.n) next_piece();
-                if (more) fetch();
+                if (lane < 2) reinterpret_cast<uint8_t*>(mask_smem + (t & 3) * 2 + lane)[w] = static_cast<uint8_t>(mask >> (8 * lane));
             }
-        } else {
-            // V: rows 16w + rr and + 8 of the tile, chunks 8 rank + c4 + 4 t
-            uint4 code[2][2];
-            uint16_t scale[2][2];
-            auto fetch = [&]() {
-#pragma unroll
-                for (int it = 0; it < 2; ++it) {
-                    const int64_t src = cache_row(static_cast<int64_t>(pc.t0 + i) * kTile + w * 16 + it * 8 + rr);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) load_codes(src, 8 * rank + c4 + 4 * t, code[it][t], scale[it][t]);
-                }
-            };
-            if (more) fetch();
-            while (more && ok) {
-                const uint32_t st = tile & 1u;
-                uint8_t* dst = v_smem + st * kVBytes;
-                ok = wait_warp(bar_pv_done + 8 * st, ((tile >> 1) & 1u) ^ 1u);
-                if (!ok) break;
-#pragma unroll
-                for (int it = 0; it < 2; ++it)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const int chunk = c4 + 4 * t;
-                        store_codes(dst + (chunk >> 1) * kVBlock + (w * 16 + it * 8 + rr) * 128, chunk & 1, code[it][t], scale[it][t]);
-                    }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(in_first(bar_v_full + 8 * st));
-                ++tile;
-                if (++i == pc.n) next_piece();
-                if (more) fetch();
-            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(bar_full + 8 * st);
+            if (t + 1 < total) fetch();
         }
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
     } else if (warp >= 4 && warp < 8) {

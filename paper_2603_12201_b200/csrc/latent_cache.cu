@@ -14,11 +14,12 @@ __device__ __forceinline__ float bf16_at(const uint4& v, int i) {
 }
 
 // The smallest scale of 5 significant bits that holds `amax` in 7 steps: amax / 7 rounded up past its top 4 mantissa bits.
-// At least 2^-100 (code * scale then stays far from the subnormals), at most 1.125 * 2^125 (7 steps stay finite).
+// At least 2^-100 (code * scale then stays far from the subnormals), at most 1.3125 * 2^123 (24 steps, which the reader
+// subtracts, stay finite).
 __device__ __forceinline__ float q4_scale(float amax) {
     const float s = __fdiv_rn(fmaxf(amax, 7.f * 0x1p-100f), 7.f);
     const float up = __uint_as_float((__float_as_uint(s) + 0x7FFFFu) & ~0x7FFFFu);
-    return fminf(up, 0x1.2p+125f);
+    return fminf(up, 0x1.5p+123f);
 }
 
 // One word of codes from eight columns. The quotient is corrected by one residual step from the rounded reciprocal r of the
@@ -98,8 +99,8 @@ dequantize_q4_kernel(const uint8_t* __restrict__ cache, int64_t cache_rows, cons
     for (int u = 0; u < kRowsPerWarp; ++u) {
         if (row0 + u >= n) continue;
         uint4* dst = out + (row0 + u) * (kLatentCols / 8);
-        dst[lane] = dequant8_q4(word[u][0], scale_pair(scale[u][0]));
-        dst[32 + lane] = dequant8_q4(word[u][1], scale_pair(scale[u][1]));
+        dst[lane] = dequant8_q4(word[u][0], q4_scale_of(scale[u][0]));
+        dst[32 + lane] = dequant8_q4(word[u][1], q4_scale_of(scale[u][1]));
         if (lane < 8) dst[64 + lane] = rope[u];
     }
 }

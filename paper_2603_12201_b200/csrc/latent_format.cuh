@@ -20,24 +20,40 @@ constexpr int kLatentQ4RowBytes = 416;
 constexpr int kLatentQ4ScaleOff = 256;
 constexpr int kLatentQ4RopeOff = 288;
 
-// Eight columns of a 4-bit row: `word` their codes, `scale2` the group's scale in both halves. 0x4300 | u is 128 + u in bf16
-// (unit step 1 there), so the subtraction of 136 leaves the code exactly.
-__device__ __forceinline__ uint4 dequant8_q4(uint32_t word, __nv_bfloat162 scale2) {
+// The scale of a group as the reader uses it, in both halves of a word: s and -24 s (3 s has at most 7 bits: exact).
+struct Q4Scale {
+    __nv_bfloat162 s, m24s;
+};
+__device__ __forceinline__ Q4Scale q4_scale_of(uint32_t bits) {      // the scale's bf16 bits in the low half
+    const uint32_t two = __byte_perm(bits, 0u, 0x1010), c = 0xC1C0C1C0u;      // -24 in both halves
+    Q4Scale r;
+    r.s = *reinterpret_cast<const __nv_bfloat162*>(&two);
+    r.m24s = __hmul2(r.s, *reinterpret_cast<const __nv_bfloat162*>(&c));
+    return r;
+}
+
+// Eight columns of a 4-bit row: `word` their codes. A nibble in the upper four mantissa bits of 0x4180 is 16 + u = 24 + code, so
+// (16 + u) s - 24 s = code * s with one FMA a pair, whose result is exact.
+__device__ __forceinline__ uint4 dequant8_q4(uint32_t word, const Q4Scale& q) {
     uint32_t r[4];
-    const uint32_t bias_bits = 0x43084308u;            // 136 in both halves
-    const __nv_bfloat162 bias = *reinterpret_cast<const __nv_bfloat162*>(&bias_bits);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t t = ((word >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-        const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&t), bias), scale2);
+        const uint32_t t = ((i == 0 ? word << 3 : word >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
+        const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&t), q.s, q.m24s);
         r[i] = *reinterpret_cast<const uint32_t*>(&v);
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-__device__ __forceinline__ __nv_bfloat162 scale_pair(uint16_t bits) {
-    const uint32_t two = static_cast<uint32_t>(bits) * 0x10001u;
-    return *reinterpret_cast<const __nv_bfloat162*>(&two);
+// 32 bytes from a 32-byte aligned address, zeros if !use (nothing is read then).
+__device__ __forceinline__ void load_nc_256(const uint8_t* at, bool use, uint32_t (&r)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = 0u;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %9, 0;\n\t"
+        "@p ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+        : "l"(at), "r"(static_cast<uint32_t>(use)));
 }
 
 }  // namespace idxc

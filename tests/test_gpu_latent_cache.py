@@ -72,9 +72,9 @@ def test_quantize_extreme_magnitudes(idxc):
     v = out.double().cpu().numpy()
     assert np.all(np.isfinite(v))
     assert np.array_equal(cache.cpu().numpy()[[0, 2, 3]], oracle.quantize_rows(x.double().numpy()[[0, 2, 3]]))
-    # the largest scale whose 7 steps are finite: half a step off at most, or the clipped end
+    # the largest scale, 1.3125 * 2^123: half a step off at most, or the clipped end
     xs = x.double().numpy()[1, :32]
-    assert np.all(np.abs(v[1, :32] - xs) <= np.maximum(0.5 * 1.125 * 2.0 ** 125, np.abs(xs) - 7 * 1.125 * 2.0 ** 125) * (1 + 1e-12))
+    assert np.all(np.abs(v[1, :32] - xs) <= np.maximum(0.5 * 1.3125 * 2.0 ** 123, np.abs(xs) - 7 * 1.3125 * 2.0 ** 123) * (1 + 1e-12))
 
 
 def test_scatter_writes_its_rows_only(idxc):
