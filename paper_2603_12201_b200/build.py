@@ -11,7 +11,7 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libidxc.so"
 SOURCES = ["api.cu", "topk.cu", "topk_cluster.cu", "topk_stream.cu", "scorer_simt.cu", "scorer_tc.cu", "noalloc.cu", "selftest.cu", "quantize.cu", "pattern_tools.cu", "distill.cu", "sparse_attn.cu",
-           "latent_cache.cu", "latent_attn.cu", "latent_attn_pair.cu", "latent_simple.cu", "evict.cu"]
+           "latent_cache.cu", "latent_attn.cu", "latent_attn_pair.cu", "attn_weights.cu", "evict.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",

@@ -646,9 +646,22 @@ idxc_status idxc_attention_weights(const void* q, const void* kv, idxc_latent_fo
     if (B == 0) return IDXC_OK;
     if (!lse || !acc || !aligned(lse, 4) || !aligned(acc, 4)) return IDXC_ERR_INVALID_ARG;
     if (a.max_len == 0) return IDXC_OK;
-    if (!device_info().ok) return IDXC_ERR_CUDA;
-    g_launches += 1;
-    return launch_attn_weights(a, lse, beta, acc, ld, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+    if (!latent_attn_fits(a.B, a.n_step, a.max_len, a.H)) return IDXC_ERR_INVALID_ARG;
+    DeviceInfo& di = device_info();
+    if (!di.ok) return IDXC_ERR_CUDA;
+    const int seq_rows = n_step * H;
+    CUtensorMap q_map, kv_map;
+    if (!a.q4 && !a.topk && a.n_kv > 0 && !encode_operand_map(&kv_map, a.kv, a.n_kv, 576, false, 128)) return IDXC_ERR_CUDA;
+    for (int row0 = 0; row0 < seq_rows; row0 += 128) {
+        const int rows = attn_weights_rows(n_step, H, row0);
+        if (!encode_operand_map(&q_map, a.q, a.B * seq_rows, 576, false, (rows + 15) / 16 * 16)) return IDXC_ERR_CUDA;
+        if (a.q4 || a.topk || a.n_kv == 0) kv_map = q_map;     // not read
+        g_launches += 1;
+        if (launch_attn_weights(a, row0, lse, row0 == 0 ? beta : 1.f, acc, ld, q_map, kv_map, di.status_ptr, di.sm_count,
+                                static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess)
+            return IDXC_ERR_CUDA;
+    }
+    return IDXC_OK;
 }
 
 idxc_status idxc_evict_select(const float* acc, int64_t ld, const int32_t* lens, int64_t B, int budget, int recent,

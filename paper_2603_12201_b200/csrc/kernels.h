@@ -146,7 +146,11 @@ size_t latent_attn_workspace_bytes(int64_t B, int n_step, int64_t max_len, int H
 bool latent_attn_fits(int64_t B, int n_step, int64_t max_len, int H);      // the tile count of the call stays below 2^31
 cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void* workspace, const LatentMaps& maps, unsigned int* status, int sm_count,
                                cudaStream_t stream, int* launches);
-cudaError_t launch_attn_weights(const LatentArgs& a, const float* lse, float beta, float* acc, int64_t ld, cudaStream_t stream);
+// attn_weights.cu: query rows row0 .. row0 + attn_weights_rows(..) - 1 of every sequence, one launch. q_map: q as [B * n_step * H, 576],
+// boxes of 64 columns x (the rows rounded up to 16); kv_map (bf16 rows in order): kv as [n_kv, 576], boxes of 64 columns x 128 rows.
+int attn_weights_rows(int n_step, int H, int row0);
+cudaError_t launch_attn_weights(const LatentArgs& a, int row0, const float* lse, float beta, float* acc, int64_t ld, const CUtensorMap& q_map,
+                                const CUtensorMap& kv_map, unsigned int* status, int sm_count, cudaStream_t stream);
 
 // latent_cache.cu
 cudaError_t launch_quantize_q4(const void* x, int64_t n, void* cache, int64_t cache_rows, const int64_t* dst_rows, cudaStream_t stream);

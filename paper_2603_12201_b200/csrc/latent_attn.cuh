@@ -15,7 +15,7 @@ constexpr int kRows = 64;                           // query rows of a CTA
 constexpr int kBlocks = 9;                          // 64-column blocks of a row
 constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
 
-// Tiles of a unit: counted beforehand (selected rows), or from its sequence's length.
+// Tiles of a unit: counted beforehand, or from its sequence's length (no lengths: max_len for all).
 struct UnitTiles {
     const int32_t* counted;      // [units] or nullptr
     const int32_t* lens;
@@ -24,7 +24,7 @@ struct UnitTiles {
     int tile;                    // rows of a tile
     __device__ __forceinline__ int operator()(uint32_t unit) const {
         if (counted) return __ldg(counted + unit);
-        const int64_t len = __ldg(lens + unit / blocks_per_seq);
+        const int64_t len = lens ? __ldg(lens + unit / blocks_per_seq) : max_len;
         return static_cast<int>((min(max(len, int64_t(0)), max_len) + tile - 1) / tile);
     }
 };

@@ -56,4 +56,10 @@ __device__ __forceinline__ void load_nc_256(const uint8_t* at, bool use, uint32_
         : "l"(at), "r"(static_cast<uint32_t>(use)));
 }
 
+__device__ __forceinline__ uint32_t load_nc_32(const uint8_t* at, bool use) {
+    uint32_t r = 0u;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.b32 %0, [%1];\n\t}" : "+r"(r) : "l"(at), "r"(static_cast<uint32_t>(use)));
+    return r;
+}
+
 }  // namespace idxc

@@ -153,6 +153,22 @@ __device__ __forceinline__ void umma_f16_elect_acc(uint32_t d_tmem, uint64_t a_d
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// Four K = 16 steps over one 64-column block with one election (an election each costs more issue time than a small MMA takes).
+// STEP_A, STEP_B: descriptor units between the steps.
+template <int STEP_A, int STEP_B>
+__device__ __forceinline__ void umma_f16_x4(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred e, p;\n\t"
+        "setp.ne.b32 p, %10, 0;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %5, %9, p;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %2, %6, %9, 1;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %3, %7, %9, 1;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %4, %8, %9, 1;\n\t}"
+        ::"r"(d_tmem), "l"(a), "l"(a + STEP_A), "l"(a + 2 * STEP_A), "l"(a + 3 * STEP_A), "l"(b), "l"(b + STEP_B), "l"(b + 2 * STEP_B),
+          "l"(b + 3 * STEP_B), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // A operand read from tensor memory: lane = row of A, one 32-bit column holds two consecutive bf16 elements of the row
 // (low half = even element), 8 columns per K = 16 step.
 __device__ __forceinline__ void umma_f16_ts_elect_acc(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -309,6 +325,9 @@ __device__ __forceinline__ uint64_t umma_smem_desc_noswizzle(uint32_t smem_addr,
     return d;
 }
 
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 // Four 8 x 8 matrices of 16-bit elements to shared memory; lane l addresses row l % 8 of matrix l / 8, and register i of lane
 // l holds elements 2 (l % 4), + 1 of row l / 4 of matrix i.
 __device__ __forceinline__ void stmatrix_x4(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {

@@ -287,6 +287,44 @@ def test_weights_of_a_selection(idxc, four):
     assert np.all(np.abs(acc.double().cpu().numpy() - want) <= bound + 2.0 ** -20 * want)
 
 
+@pytest.mark.parametrize("four", [False, True])
+def test_weights_without_visible_rows(idxc, four):
+    """An empty cache, sequences outside it and tokens that see nothing: the old sums are scaled, nothing is added."""
+    g = gen(33)
+    kv = cache_rows(70, four, g).to(DEV)
+    q = bf16_rows(3 * 2 * 5, g).reshape(3, 2, 5, 576).to(DEV)
+    lens = torch.tensor([60, 1, 0], dtype=torch.int32, device=DEV)
+    base = torch.tensor([-60, 70, 0], device=DEV)
+    start = torch.rand((3, 64), generator=g)
+    for rows, b in ((kv[:0], None), (kv, base)):
+        lse = torch.full((3, 2, 5), float("-inf"), device=DEV)
+        acc = start.clone().to(DEV)
+        idxc.attention_weights(q, rows, lse, acc, 0.05, kv_base=b, lens=lens, max_len=60, beta=0.25)
+        want = start.clone()
+        want[0, :60] *= 0.25
+        want[1, :1] *= 0.25
+        assert torch.equal(acc.cpu(), want)
+        lse.fill_(0.0)                                   # a finite lse of tokens whose rows do not exist
+        idxc.attention_weights(q, rows, lse, acc, 0.05, kv_base=b, lens=lens, max_len=60)
+        assert torch.equal(acc.cpu(), want)
+
+
+def test_weights_ignore_query_rows_of_the_next_sequence(idxc):
+    """The matrix product's padding reads query rows behind the sequence's own; whatever they hold adds nothing."""
+    g = gen(34)
+    kv = bf16_rows(200, g).to(DEV)
+    q = bf16_rows(2 * 5, g).reshape(2, 1, 5, 576)
+    q[1] = float("nan")
+    q = q.to(DEV)
+    lens = torch.tensor([200, 0], dtype=torch.int32, device=DEV)
+    out, lse = idxc.latent_attention(q, kv, None, lens, 200, 512, 0.05)
+    acc = torch.zeros((2, 200), device=DEV)
+    idxc.attention_weights(q, kv, lse, acc, 0.05, lens=lens, max_len=200)
+    o, l, spread, reach, p = oracle.attention(bits(q[0, 0]), stored(kv), 0.05, np.full(5, 200))
+    check_attention(out[0, 0], lse[0, 0], o, l, spread, reach)
+    assert np.allclose(acc[0].cpu().numpy(), p.sum(axis=0), rtol=1e-4)
+
+
 # ------------------------------------------------------------------ as a serving loop uses them
 def test_append_attend_weigh_evict_loop(idxc):
     """Prompt and steps into a 4-bit cache, dense attention, weights, eviction when full; against the same loop in float64."""
