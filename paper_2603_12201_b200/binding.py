@@ -7,6 +7,7 @@ Function names mirror ``include/idxc.h``.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from pathlib import Path
 
@@ -378,9 +379,12 @@ def sparse_attention(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, out=N
 
 
 # ------------------------------------------------------------------ latent cache: 4-bit rows, dense attention, eviction
+_NO_GUARD = contextlib.nullcontext()
+
+
 def _launch_on(stream, **tensors):
-    """Checks that the tensors (None allowed) are contiguous CUDA tensors of one device and returns (device guard, stream):
-    the call is made with that device current, on its current stream unless one is given."""
+    """Checks that the tensors (None allowed) are contiguous CUDA tensors of one device and returns (guard, stream): inside the
+    guard that device is current and so is the stream, which is the device's current one unless given."""
     device = None
     for name, t in tensors.items():
         if t is None:
@@ -390,9 +394,12 @@ def _launch_on(stream, **tensors):
             device = t.device
         elif t.device != device:
             raise ValueError(f"{name} is on {t.device}, the other tensors are on {device}")
-    if stream is not None and stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
-    return torch.cuda.device(device), torch.cuda.current_stream(device) if stream is None else stream
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+        return torch.cuda.stream(stream), stream
+    stream = torch.cuda.current_stream(device)
+    return (_NO_GUARD if torch.cuda.current_device() == device.index else torch.cuda.device(device)), stream
 
 
 def _typed(t, name, dtype, shape=None):
@@ -462,7 +469,7 @@ def latent_attention(q, kv, kv_base, lens, max_len, d_v, scale, want_lse=True, o
     B, n_step, H, d_qk = q.shape
     _typed(q, "q", torch.bfloat16); _typed(kv_base, "kv_base", torch.int64, (B,)); _typed(lens, "lens", torch.int32, (B,))
     _typed(out, "out", torch.bfloat16, (B, n_step, H, d_v))
-    with guard, torch.cuda.stream(stream):
+    with guard:
         if out is None:
             out = torch.empty((B, n_step, H, d_v), dtype=torch.bfloat16, device=q.device)
         lse = torch.empty((B, n_step, H), dtype=torch.float32, device=q.device) if want_lse else None
@@ -483,7 +490,7 @@ def sparse_attention_q4(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, ou
     k_top = topk.shape[1]
     _typed(q, "q", torch.bfloat16); _typed(topk, "topk", torch.int32, (n_q, k_top)); _typed(kv_base, "kv_base", torch.int64, (n_q,))
     _typed(out, "out", torch.bfloat16, (n_q, H, d_v))
-    with guard, torch.cuda.stream(stream):
+    with guard:
         if out is None:
             out = torch.empty((n_q, H, d_v), dtype=torch.bfloat16, device=q.device)
         lse = torch.empty((n_q, H), dtype=torch.float32, device=q.device) if want_lse else None

@@ -1,56 +1,98 @@
 // Which cached positions of a sequence stay when its cache is cut to a budget: the newest `recent` ones, and among the older
 // ones the budget - recent with the largest accumulated attention weight (ties: lowest position), in ascending order.
-// One CTA per sequence: three histogram passes (11 + 11 + 10 bits of an order-preserving key) find the weight of the last
-// one that stays exactly, and one ordered pass writes the positions.
+// A cluster of eight CTAs takes a sequence, each an eighth of its positions, whose keys stay in shared memory (up to 48K positions a
+// CTA; longer slices are read from global memory again). Three histogram passes (11 + 11 + 10 bits of an order-preserving key) find the
+// key of the last position that stays exactly; the CTAs add up their histograms through distributed shared memory. Then every
+// position's place in the output is the number of positions before it that stay, by prefix sums over lanes, warps and CTAs: no
+// atomics on the output, ascending order for free. Bound by latency (eight cluster barriers and sweeps of a few microseconds, 25 us at
+// 131072 positions), not by its bytes; one CTA per sequence took 313 us.
 #include "kernels.h"
+#include "ptx_sm100.cuh"
 
 namespace idxc {
 namespace {
 
-constexpr int kEvThreads = 1024;
+constexpr int kEvCtas = 8;
+constexpr int kEvThreads = 512;
+constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBins = 2048;
+constexpr int kEvKeys = 49152;                       // keys of a slice that fit into shared memory at most
+constexpr uint32_t kEvHistBytes = 2 * kEvBins * 4;
 
 // Larger float = larger key; -0 and +0 share a key.
 __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+__device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 ld_cluster_v2(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
+}
 
-__global__ void __launch_bounds__(kEvThreads)
-evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __restrict__ lens, int budget, int recent,
+__global__ void __cluster_dims__(kEvCtas, 1, 1) __launch_bounds__(kEvThreads)
+evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __restrict__ lens, int budget, int recent, int key_slots,
                     int32_t* __restrict__ keep, int32_t* __restrict__ new_lens) {
-    __shared__ uint32_t hist[kEvBins];
-    __shared__ uint32_t warp_sum[kEvThreads / 32];
+    extern __shared__ __align__(16) uint32_t ev_smem[];
+    uint32_t* hist = ev_smem;                        // [2][kEvBins]
+    uint32_t* keys = ev_smem + 2 * kEvBins;          // [key_slots]
+    __shared__ uint32_t warp_sum[kEvWarps];
+    __shared__ uint2 warp_count[kEvWarps];
     __shared__ uint32_t s_bin, s_left;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ __align__(8) uint2 cta_count;         // positions of this CTA that certainly stay, and those at the border key
+    const int rank = static_cast<int>(cluster_ctarank());
+    const int b = blockIdx.x / kEvCtas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int len = static_cast<int>(min(static_cast<int64_t>(max(__ldg(lens + b), 0)), ld));
     const float* row = acc + b * ld;
     int32_t* out = keep + static_cast<int64_t>(b) * budget;
     const int stay = min(len, budget);
-    if (tid == 0) new_lens[b] = stay;
-    for (int j = stay + tid; j < budget; j += kEvThreads) out[j] = -1;
-    if (len <= budget) {
-        for (int j = tid; j < len; j += kEvThreads) out[j] = j;
+    if (tid == 0 && rank == 0) new_lens[b] = stay;
+    for (int64_t j = stay + static_cast<int64_t>(rank) * kEvThreads + tid; j < budget; j += kEvCtas * kEvThreads) out[j] = -1;
+    if (len <= budget) {                             // (the whole cluster leaves here together)
+        for (int j = rank * kEvThreads + tid; j < len; j += kEvCtas * kEvThreads) out[j] = j;
         return;
     }
-    const int old = len - recent;                 // positions that compete
+    const int old = len - recent;                    // positions that compete
+    const int slice = ((len + kEvCtas - 1) / kEvCtas + 31) & ~31;
+    const int p0 = min(rank * slice, len), p1 = min(p0 + slice, len);
+    const int p1_old = min(p1, old);
+    const bool kept = slice <= key_slots;
+    if (kept)
+        for (int i = p0 + tid; i < p1_old; i += kEvThreads) keys[i - p0] = order_key(__ldg(row + i));
+    auto key_at = [&](int i) -> uint32_t { return kept ? keys[i - p0] : order_key(__ldg(row + i)); };
     uint32_t want = static_cast<uint32_t>(budget - recent);      // < old, since budget < len
+    const bool any_old = want > 0;
     uint32_t prefix = 0, mask = 0;
-    if (want > 0) {
+    for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
+    __syncthreads();
+    if (any_old) {
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
-            const int bins = pass == 2 ? 1024 : 2048;
-            for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
-            __syncthreads();
-            for (int i = tid; i < old; i += kEvThreads) {
-                const uint32_t k = order_key(__ldg(row + i));
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+            const uint32_t bins = pass == 2 ? 1024u : 2048u;
+            uint32_t* h = hist + (pass & 1) * kEvBins;
+            for (int i = p0 + tid; i < p1_old; i += kEvThreads) {
+                const uint32_t k = key_at(i);
+                if ((k & mask) == prefix) atomicAdd(&h[(k >> shift) & (bins - 1u)], 1u);
             }
-            __syncthreads();
-            // from the top bin down: the bin in which the count reaches `want`; thread t holds the two bins below the top 2t
-            const int hi = kEvBins - 1 - 2 * tid;
-            const uint32_t c0 = hist[hi], c1 = hist[hi - 1];
-            uint32_t run = c0 + c1;
+            cluster_sync();
+            // (every CTA has read the other buffer by now: it may be cleared for the next pass)
+            for (int i = tid; i < kEvBins; i += kEvThreads) hist[((pass + 1) & 1) * kEvBins + i] = 0;
+            // counts of all CTAs from the top bin down: the bin in which they reach `want`. Thread t has bins top .. top - 3.
+            const int top = kEvBins - 1 - 4 * tid;
+            const uint32_t at = smem_u32(h + top - 3);
+            uint32_t c[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < kEvCtas; ++r) {
+                const uint4 v = ld_cluster_v4(map_to_cta(at, r));
+                c[0] += v.w; c[1] += v.z; c[2] += v.y; c[3] += v.x;
+            }
+            const uint32_t mine = c[0] + c[1] + c[2] + c[3];
+            uint32_t run = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, run, o);
@@ -58,62 +100,77 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
             }
             if (lane == 31) warp_sum[warp] = run;
             __syncthreads();
-            uint32_t before = run - c0 - c1;
+            uint32_t before = run - mine;
             for (int w = 0; w < warp; ++w) before += warp_sum[w];
-            if (before < want && before + c0 >= want) { s_bin = hi; s_left = want - before; }
-            else if (before + c0 < want && before + c0 + c1 >= want) { s_bin = hi - 1; s_left = want - before - c0; }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (before < want && before + c[j] >= want) { s_bin = top - j; s_left = want - before; }
+                before += c[j];
+            }
             __syncthreads();
             prefix |= s_bin << shift;
-            mask |= static_cast<uint32_t>(bins - 1) << shift;
+            mask |= (bins - 1u) << shift;
             want = s_left;
             __syncthreads();
         }
     }
-    // `want` of the positions with key == prefix stay, the lowest first
-    uint32_t n_out = 0, n_equal = 0;
-    const bool any_old = budget > recent;
-    for (int i0 = 0; i0 < len; i0 += kEvThreads) {
-        const int i = i0 + tid;
-        uint32_t k = 0;
-        bool eq = false, above = false;
-        if (i < old && any_old) {
-            k = order_key(__ldg(row + i));
-            eq = k == prefix;
-            above = k > prefix;
+    // `want` of the positions with key == prefix stay, the lowest first. A warp has a run of its CTA's slice.
+    const int seg = (((slice + kEvWarps - 1) / kEvWarps) + 31) & ~31;
+    const int w0 = min(p0 + warp * seg, p1), w1 = min(w0 + seg, p1);
+    auto look = [&](int i, bool& sure, bool& border) {
+        sure = i >= old && i < w1;
+        border = false;
+        if (any_old && i < old && i < w1) {
+            const uint32_t k = key_at(i);
+            sure = k > prefix;
+            border = k == prefix;
         }
-        const bool rec = i >= old && i < len;
-        const uint32_t be = __ballot_sync(0xFFFFFFFFu, eq);
-        if (lane == 0) warp_sum[warp] = __popc(be);
-        __syncthreads();
-        uint32_t eq_before = n_equal, eq_all = 0;
-        for (int w = 0; w < kEvThreads / 32; ++w) {
-            if (w < warp) eq_before += warp_sum[w];
-            eq_all += warp_sum[w];
-        }
-        eq_before += __popc(be & ((1u << lane) - 1u));
-        __syncthreads();
-        const bool sel = rec || above || (eq && eq_before < want);
-        const uint32_t bs = __ballot_sync(0xFFFFFFFFu, sel);
-        if (lane == 0) warp_sum[warp] = __popc(bs);
-        __syncthreads();
-        uint32_t pos = n_out, all = 0;
-        for (int w = 0; w < kEvThreads / 32; ++w) {
-            if (w < warp) pos += warp_sum[w];
-            all += warp_sum[w];
-        }
-        pos += __popc(bs & ((1u << lane) - 1u));
-        if (sel && pos < static_cast<uint32_t>(budget)) out[pos] = i;
-        n_out += all;
-        n_equal += eq_all;
-        __syncthreads();
+    };
+    uint32_t n_sure = 0, n_border = 0;
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        bool sure, border;
+        look(i0 + lane, sure, border);
+        n_sure += __popc(__ballot_sync(0xFFFFFFFFu, sure));
+        n_border += __popc(__ballot_sync(0xFFFFFFFFu, border));
     }
+    if (lane == 0) warp_count[warp] = make_uint2(n_sure, n_border);
+    __syncthreads();
+    uint32_t sure_at = 0, border_at = 0;
+    for (int w = 0; w < kEvWarps; ++w) {
+        const uint2 v = warp_count[w];
+        if (w < warp) { sure_at += v.x; border_at += v.y; }
+        if (tid == 0) { n_sure = w == 0 ? v.x : n_sure + v.x; n_border = w == 0 ? v.y : n_border + v.y; }
+    }
+    if (tid == 0) cta_count = make_uint2(n_sure, n_border);
+    cluster_sync();
+    for (int r = 0; r < rank; ++r) {
+        const uint2 v = ld_cluster_v2(map_to_cta(smem_u32(&cta_count), r));
+        sure_at += v.x;
+        border_at += v.y;
+    }
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        bool sure, border;
+        look(i0 + lane, sure, border);
+        const uint32_t bs = __ballot_sync(0xFFFFFFFFu, sure), bb = __ballot_sync(0xFFFFFFFFu, border), below = (1u << lane) - 1u;
+        const uint32_t my_sure = sure_at + __popc(bs & below), my_border = border_at + __popc(bb & below);
+        const uint32_t place = my_sure + min(my_border, want);
+        if ((sure || (border && my_border < want)) && place < static_cast<uint32_t>(budget)) out[place] = i0 + lane;
+        sure_at += __popc(bs);
+        border_at += __popc(bb);
+    }
+    cluster_sync();                                  // no CTA leaves while another may still read its counts
 }
 
 }  // namespace
 
 cudaError_t launch_evict_select(const float* acc, int64_t ld, const int32_t* lens, int B, int budget, int recent, int32_t* keep,
                                 int32_t* new_lens, cudaStream_t stream) {
-    evict_select_kernel<<<static_cast<unsigned>(B), kEvThreads, 0, stream>>>(acc, ld, lens, budget, recent, keep, new_lens);
+    if (cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(evict_select_kernel), kEvHistBytes + kEvKeys * 4); e != cudaSuccess) return e;
+    // room for the longest slice that ld allows: short rows leave room for several CTAs on an SM
+    const int64_t slice = ((ld + kEvCtas - 1) / kEvCtas + 31) & ~int64_t(31);
+    const int slots = static_cast<int>(slice < kEvKeys ? slice : kEvKeys);
+    evict_select_kernel<<<static_cast<unsigned>(B) * kEvCtas, kEvThreads, kEvHistBytes + slots * 4, stream>>>(acc, ld, lens, budget, recent, slots, keep,
+                                                                                                             new_lens);
     return cudaGetLastError();
 }
 
