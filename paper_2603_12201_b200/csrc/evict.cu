@@ -12,7 +12,8 @@
 namespace idxc {
 namespace {
 
-constexpr int kEvCtas = 8;
+constexpr int kEvCtas = 8;                           // CTAs of a long sequence (short ones, up to kEvShort positions a row of acc: one)
+constexpr int kEvShort = 16384;
 constexpr int kEvThreads = 512;
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBins = 2048;
@@ -35,7 +36,8 @@ __device__ __forceinline__ uint2 ld_cluster_v2(uint32_t addr) {
     return v;
 }
 
-__global__ void __cluster_dims__(kEvCtas, 1, 1) __launch_bounds__(kEvThreads)
+template <int CTAS>
+__global__ void __launch_bounds__(kEvThreads)
 evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __restrict__ lens, int budget, int recent, int key_slots,
                     int32_t* __restrict__ keep, int32_t* __restrict__ new_lens) {
     extern __shared__ __align__(16) uint32_t ev_smem[];
@@ -45,20 +47,24 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
     __shared__ uint2 warp_count[kEvWarps];
     __shared__ uint32_t s_bin, s_left;
     __shared__ __align__(8) uint2 cta_count;         // positions of this CTA that certainly stay, and those at the border key
-    const int rank = static_cast<int>(cluster_ctarank());
-    const int b = blockIdx.x / kEvCtas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto sync_all = [&]() {                          // the CTAs of the sequence
+        if (CTAS > 1) cluster_sync();
+        else __syncthreads();
+    };
+    const int rank = CTAS > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+    const int b = blockIdx.x / CTAS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int len = static_cast<int>(min(static_cast<int64_t>(max(__ldg(lens + b), 0)), ld));
     const float* row = acc + b * ld;
     int32_t* out = keep + static_cast<int64_t>(b) * budget;
     const int stay = min(len, budget);
     if (tid == 0 && rank == 0) new_lens[b] = stay;
-    for (int64_t j = stay + static_cast<int64_t>(rank) * kEvThreads + tid; j < budget; j += kEvCtas * kEvThreads) out[j] = -1;
+    for (int64_t j = stay + static_cast<int64_t>(rank) * kEvThreads + tid; j < budget; j += CTAS * kEvThreads) out[j] = -1;
     if (len <= budget) {                             // (the whole cluster leaves here together)
-        for (int j = rank * kEvThreads + tid; j < len; j += kEvCtas * kEvThreads) out[j] = j;
+        for (int j = rank * kEvThreads + tid; j < len; j += CTAS * kEvThreads) out[j] = j;
         return;
     }
     const int old = len - recent;                    // positions that compete
-    const int slice = ((len + kEvCtas - 1) / kEvCtas + 31) & ~31;
+    const int slice = ((len + CTAS - 1) / CTAS + 31) & ~31;
     const int p0 = min(rank * slice, len), p1 = min(p0 + slice, len);
     const int p1_old = min(p1, old);
     const bool kept = slice <= key_slots;
@@ -79,7 +85,7 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
                 const uint32_t k = key_at(i);
                 if ((k & mask) == prefix) atomicAdd(&h[(k >> shift) & (bins - 1u)], 1u);
             }
-            cluster_sync();
+            sync_all();
             // (every CTA has read the other buffer by now: it may be cleared for the next pass)
             for (int i = tid; i < kEvBins; i += kEvThreads) hist[((pass + 1) & 1) * kEvBins + i] = 0;
             // counts of all CTAs from the top bin down: the bin in which they reach `want`. Thread t has bins top .. top - 3.
@@ -87,7 +93,7 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
             const uint32_t at = smem_u32(h + top - 3);
             uint32_t c[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < kEvCtas; ++r) {
+            for (int r = 0; r < CTAS; ++r) {
                 const uint4 v = ld_cluster_v4(map_to_cta(at, r));
                 c[0] += v.w; c[1] += v.z; c[2] += v.y; c[3] += v.x;
             }
@@ -142,7 +148,7 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
         if (tid == 0) { n_sure = w == 0 ? v.x : n_sure + v.x; n_border = w == 0 ? v.y : n_border + v.y; }
     }
     if (tid == 0) cta_count = make_uint2(n_sure, n_border);
-    cluster_sync();
+    sync_all();
     for (int r = 0; r < rank; ++r) {
         const uint2 v = ld_cluster_v2(map_to_cta(smem_u32(&cta_count), r));
         sure_at += v.x;
@@ -158,20 +164,37 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
         sure_at += __popc(bs);
         border_at += __popc(bb);
     }
-    cluster_sync();                                  // no CTA leaves while another may still read its counts
+    sync_all();                                  // no CTA leaves while another may still read its counts
 }
 
 }  // namespace
 
+template <int CTAS>
+static cudaError_t launch_as(const float* acc, int64_t ld, const int32_t* lens, int B, int budget, int recent, int32_t* keep, int32_t* new_lens,
+                             cudaStream_t stream) {
+    const void* kernel = reinterpret_cast<const void*>(evict_select_kernel<CTAS>);
+    if (cudaError_t e = ensure_max_dynamic_smem(kernel, kEvHistBytes + kEvKeys * 4); e != cudaSuccess) return e;
+    // room for the longest slice that ld allows: short rows leave room for several CTAs on an SM
+    const int64_t slice = ((ld + CTAS - 1) / CTAS + 31) & ~int64_t(31);
+    const int slots = static_cast<int>(slice < kEvKeys ? slice : kEvKeys);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(B) * CTAS);
+    cfg.blockDim = dim3(kEvThreads);
+    cfg.dynamicSmemBytes = kEvHistBytes + static_cast<size_t>(slots) * 4;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CTAS;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CTAS > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, evict_select_kernel<CTAS>, acc, ld, lens, budget, recent, slots, keep, new_lens);
+}
+
 cudaError_t launch_evict_select(const float* acc, int64_t ld, const int32_t* lens, int B, int budget, int recent, int32_t* keep,
                                 int32_t* new_lens, cudaStream_t stream) {
-    if (cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(evict_select_kernel), kEvHistBytes + kEvKeys * 4); e != cudaSuccess) return e;
-    // room for the longest slice that ld allows: short rows leave room for several CTAs on an SM
-    const int64_t slice = ((ld + kEvCtas - 1) / kEvCtas + 31) & ~int64_t(31);
-    const int slots = static_cast<int>(slice < kEvKeys ? slice : kEvKeys);
-    evict_select_kernel<<<static_cast<unsigned>(B) * kEvCtas, kEvThreads, kEvHistBytes + slots * 4, stream>>>(acc, ld, lens, budget, recent, slots, keep,
-                                                                                                             new_lens);
-    return cudaGetLastError();
+    return ld <= kEvShort ? launch_as<1>(acc, ld, lens, B, budget, recent, keep, new_lens, stream)
+                          : launch_as<kEvCtas>(acc, ld, lens, B, budget, recent, keep, new_lens, stream);
 }
 
 }  // namespace idxc

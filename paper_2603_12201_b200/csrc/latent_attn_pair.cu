@@ -268,102 +268,102 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     } else if (Q4 && warp >= 8) {
         // ------------------------------------------------------------ 4-bit rows, expanded by four warps for K and four for V
         // Lane = 8 c + rr reads the 32 bytes of codes of 64-column block c (or c + 4) of a row rr and stores them as eight 16-byte pieces;
-        // eight consecutive lanes then store to eight different positions of the swizzle (no bank conflicts). The next
-        // tile is in registers and the rows of the one after are looked up while a tile is stored. The code is rolled and shared by
-        // the two kinds on purpose: unrolled over two tiles in registers the roles stalled on instruction fetch (3300 clocks a tile).
+        // eight consecutive lanes then store to eight different positions of the swizzle (no bank conflicts). K's lanes also move 32 bytes of
+        // the positional columns. While a tile is stored the next is in registers or on its way there, and the rows of the one
+        // after are looked up (a load takes about 1000 clocks). The code is rolled and shared by the two kinds on purpose: unrolled over
+        // the tiles in registers the roles stalled on instruction fetch (3300 clocks a tile).
         const bool is_v = warp >= 12;
         const int w = warp & 3, rr = lane & 7, c4 = lane >> 3;
         const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
         // this lane's rows of a tile. K: one of this CTA's half, and (for the mask) the same one of the other half; V: two
         const int off0 = is_v ? w * 16 + rr : rank * kHalf + w * 8 + rr, off1 = is_v ? off0 + 8 : (rank ^ 1) * kHalf + w * 8 + rr;
-        uint32_t code0[8], code1[8], scale0 = 0, scale1 = 0, mask = 0;
-        uint4 rope[2];
-        int64_t len = 0, base = 0, raw[2];                    // raw: position (or selected position) of this lane's rows in the next tile to fetch
+        struct Share { uint32_t code0[8], code1[8], rope[8], scale0, scale1, mask; } cur, nxt;      // this lane's of a tile
+        int64_t base = 0;
+        int len = 0, raw0 = -1, raw1 = -1;                    // raw: position (or selected position) of this lane's rows in the next tile to fetch
         const int32_t* sel = nullptr;
         int i = 0;
         auto open_piece = [&]() {
             if (!walk.next(pc)) return;
             seq = pc.unit / static_cast<uint32_t>(p.blocks_per_seq);
-            len = seq_len(seq);
+            len = static_cast<int>(seq_len(seq));
             base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
             sel = p.a.topk ? p.a.topk + seq * p.a.k_top : nullptr;
             i = 0;
         };
         auto look_up = [&]() {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int64_t r = static_cast<int64_t>(pc.t0 + i) * kTile + (e == 0 ? off0 : off1);
-                raw[e] = r < len ? (sel != nullptr ? static_cast<int64_t>(__ldg(sel + r)) : r) : -1;
+            const int at = (pc.t0 + i) * kTile;
+            raw0 = at + off0 < len ? at + off0 : -1;
+            raw1 = at + off1 < len ? at + off1 : -1;
+            if (sel != nullptr) {
+                if (raw0 >= 0) raw0 = __ldg(sel + raw0);
+                if (raw1 >= 0) raw1 = __ldg(sel + raw1);
             }
         };
-        auto fetch = [&]() {                                  // the tile that was looked up; then looks up the next
-            int64_t src[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int64_t r = raw[e] + base;
-                src[e] = raw[e] >= 0 && r >= 0 && r < p.a.n_kv ? r : -1;
+        auto cache_row = [&](int raw) -> int {                // -1: takes no part
+            const int64_t r = base + raw;
+            return raw >= 0 && r >= 0 && r < p.a.n_kv ? static_cast<int>(r) : -1;
+        };
+        auto fetch = [&](Share& f) {                          // the tile that was looked up; then looks up the next
+            const int s0 = cache_row(raw0);
+            int s1 = cache_row(raw1);
+            if (sel != nullptr) {
+                const uint32_t mine = __ballot_sync(0xFFFFFFFFu, s0 >= 0) & 255u, theirs = __ballot_sync(0xFFFFFFFFu, s1 >= 0) & 255u;
+                f.mask = rank == 0 ? mine | (theirs << 8) : theirs | (mine << 8);     // K: bits 0..7: in the first half of the tile, 8..15: the second
             }
-            if (!is_v) {
-                const uint32_t mine = __ballot_sync(0xFFFFFFFFu, src[0] >= 0) & 255u, theirs = __ballot_sync(0xFFFFFFFFu, src[1] >= 0) & 255u;
-                mask = rank == 0 ? mine | (theirs << 8) : theirs | (mine << 8);       // bits 0..7: in the first half of the tile, 8..15: the second
-#pragma unroll
-                for (int it = 0; it < 2; ++it) {              // positional columns: lane = 8 row + chunk, two rows a lane
-                    const int64_t s = __shfl_sync(0xFFFFFFFFu, src[0], it * 4 + c4);
-                    rope[it] = s < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(kv + s * kLatentQ4RowBytes + kLatentQ4RopeOff) + rr);
-                }
-                src[1] = src[0];
-            }
+            s1 = is_v ? s1 : s0;
             const int block0 = is_v ? 4 * rank + c4 : c4, block1 = is_v ? block0 : c4 + 4;
-            const uint8_t* row0 = kv + (src[0] < 0 ? 0 : src[0]) * kLatentQ4RowBytes;
-            const uint8_t* row1 = kv + (src[1] < 0 ? 0 : src[1]) * kLatentQ4RowBytes;
-            load_nc_256(row0 + block0 * 32, src[0] >= 0, code0);
-            load_nc_256(row1 + block1 * 32, src[1] >= 0, code1);
-            scale0 = src[0] < 0 ? 0u : __ldg(reinterpret_cast<const uint32_t*>(row0 + kLatentQ4ScaleOff) + block0);
-            scale1 = src[1] < 0 ? 0u : __ldg(reinterpret_cast<const uint32_t*>(row1 + kLatentQ4ScaleOff) + block1);
+            const uint8_t* row0 = kv + static_cast<uint64_t>(static_cast<uint32_t>(max(s0, 0))) * kLatentQ4RowBytes;
+            const uint8_t* row1 = kv + static_cast<uint64_t>(static_cast<uint32_t>(max(s1, 0))) * kLatentQ4RowBytes;
+            load_nc_256(row0 + block0 * 32, s0 >= 0, f.code0);
+            load_nc_256(row1 + block1 * 32, s1 >= 0, f.code1);
+            load_nc_256(row0 + kLatentQ4RopeOff + c4 * 32, s0 >= 0 && !is_v, f.rope);
+            f.scale0 = load_nc_32(row0 + kLatentQ4ScaleOff + block0 * 4, s0 >= 0);
+            f.scale1 = load_nc_32(row1 + kLatentQ4ScaleOff + block1 * 4, s1 >= 0);
             // dense rows lie one behind the other: ask the L2 for a tile further ahead
-            const int64_t soon = base + static_cast<int64_t>(pc.t0 + i + 2) * kTile;
-            if (sel == nullptr && rank == 0 && warp == 8 && lane == 0 && i + 2 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
-                l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
+            if (sel == nullptr && rank == 0 && warp == 8 && lane == 0 && i + 3 < pc.n) {
+                const int64_t soon = base + static_cast<int64_t>(pc.t0 + i + 3) * kTile;
+                if (soon >= 0 && soon + kTile <= p.a.n_kv) l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
+            }
             if (++i == pc.n) open_piece();
             look_up();
         };
         const uint32_t bar_free = is_v ? bar_pv_done : bar_s_full, bar_full = in_first(is_v ? bar_v_full : bar_k_full);
         const uint32_t buf_bytes = is_v ? kVBytes : kKBytes, step = is_v ? 1024u : 4 * kKBlock;       // from the first 64 columns of this lane to the second
-        uint8_t* const my_dst = is_v ? v_smem + c4 * kVBlock + off0 * 128 : k_smem + c4 * kKBlock + (w * 8 + rr) * 128;
+        // piece v of a row goes to chunk v ^ rr of its 128 bytes: an exclusive or on the address, whose low seven bits hold rr
+        const uint32_t my_dst = (is_v ? smem_u32(v_smem) + c4 * kVBlock + off0 * 128 : smem_u32(k_smem) + c4 * kKBlock + (w * 8 + rr) * 128) + (rr << 4);
+        const uint32_t rope_dst = smem_u32(k_smem) + 8 * kKBlock + (w * 8 + rr) * 128 + (((2 * c4) ^ rr) << 4);
         const int total = run.n;
         if (total > 0) {
             open_piece();
             look_up();
-            fetch();
+            fetch(nxt);
         }
+#pragma unroll 1
         for (int t = 0; t < total; ++t) {
             const uint32_t st = t & 1;
+            cur = nxt;                                        // (waits for the loads: they were issued a tile ago)
+            if (t + 1 < total) fetch(nxt);
             ok = wait_warp(bar_free + 8 * st, ((static_cast<uint32_t>(t) >> 1) & 1u) ^ 1u);
             if (!ok) break;
-            uint8_t* dst = my_dst + st * buf_bytes;
+            uint32_t to = my_dst + st * buf_bytes;
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
-                const Q4Scale lo = q4_scale_of(scale0), hi = q4_scale_of(scale0 >> 16);
+                const Q4Scale lo = q4_scale_of(cur.scale0), hi = q4_scale_of(cur.scale0 >> 16);
 #pragma unroll
-                for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4*>(dst + ((v ^ rr) << 4)) = dequant8_q4(code0[v], v < 4 ? lo : hi);
+                for (int v = 0; v < 8; ++v) st_shared_v4(to ^ (v << 4), dequant8_q4(cur.code0[v], v < 4 ? lo : hi));
 #pragma unroll
-                for (int v = 0; v < 8; ++v) code0[v] = code1[v];
-                scale0 = scale1;
-                dst += step;
+                for (int v = 0; v < 8; ++v) cur.code0[v] = cur.code1[v];
+                cur.scale0 = cur.scale1;
+                to += step;
             }
             if (!is_v) {
-                dst = k_smem + st * kKBytes + 8 * kKBlock + w * 8 * 128;
-#pragma unroll
-                for (int it = 0; it < 2; ++it) {
-                    const int r = it * 4 + c4;
-                    *reinterpret_cast<uint4*>(dst + r * 128 + ((rr ^ r) << 4)) = rope[it];
-                }
-                if (lane < 2) reinterpret_cast<uint8_t*>(mask_smem + (t & 3) * 2 + lane)[w] = static_cast<uint8_t>(mask >> (8 * lane));
+                st_shared_v4(rope_dst + st * kKBytes, make_uint4(cur.rope[0], cur.rope[1], cur.rope[2], cur.rope[3]));
+                st_shared_v4((rope_dst + st * kKBytes) ^ 16u, make_uint4(cur.rope[4], cur.rope[5], cur.rope[6], cur.rope[7]));
+                if (lane < 2) reinterpret_cast<uint8_t*>(mask_smem + (t & 3) * 2 + lane)[w] = static_cast<uint8_t>(cur.mask >> (8 * lane));
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(bar_full + 8 * st);
-            if (t + 1 < total) fetch();
         }
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
     } else if (warp >= 4 && warp < 8) {
