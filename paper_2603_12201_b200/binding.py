@@ -383,31 +383,36 @@ _NO_GUARD = contextlib.nullcontext()
 
 
 def _launch_on(stream, **tensors):
-    """Checks that the tensors (None allowed) are contiguous CUDA tensors of one device and returns (guard, stream): inside the
-    guard that device is current and so is the stream, which is the device's current one unless given."""
+    """Checks that the tensors (None allowed, not the first) are contiguous CUDA tensors of one device and returns (guard, raw
+    stream): inside the guard that device is current and so is the stream, which is the device's current one unless given."""
     device = None
     for name, t in tensors.items():
         if t is None:
             continue
-        _dev(t, name)
         if device is None:
             device = t.device
-        elif t.device != device:
+        if t.device != device or device.type != "cuda" or not t.is_contiguous():
+            _dev(t, name)
             raise ValueError(f"{name} is on {t.device}, the other tensors are on {device}")
     if stream is not None:
         if stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
-        return torch.cuda.stream(stream), stream
-    stream = torch.cuda.current_stream(device)
-    return (_NO_GUARD if torch.cuda.current_device() == device.index else torch.cuda.device(device)), stream
+        return torch.cuda.stream(stream), stream.cuda_stream
+    raw = torch._C._cuda_getCurrentRawStream(device.index)       # (torch.cuda.current_stream builds an object: 2 us a call)
+    return (_NO_GUARD if torch.cuda.current_device() == device.index else torch.cuda.device(device)), raw
+
+
+def _at(t):
+    """The address of a tensor for a pointer argument."""
+    return None if t is None else t.data_ptr()
 
 
 def _typed(t, name, dtype, shape=None):
     if t is None:
         return
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
@@ -432,7 +437,7 @@ def quantize_q4(x, cache_out, dst_rows=None, stream=None):
     _typed(x, "x", torch.bfloat16, (n, 576)); _typed(cache_out, "cache_out", torch.uint8, (cache_out.shape[0], Q4_ROW_BYTES))
     _typed(dst_rows, "dst_rows", torch.int64, (n,))
     with guard:
-        _check(lib().idxc_quantize_q4(_ptr(x), n, _ptr(cache_out), cache_out.shape[0], _ptr(dst_rows), _stream(stream)), "idxc_quantize_q4")
+        _check(lib().idxc_quantize_q4(_at(x), n, _at(cache_out), cache_out.shape[0], _at(dst_rows), stream), "idxc_quantize_q4")
 
 
 def dequantize_q4(cache, out, src_rows=None, stream=None):
@@ -444,11 +449,11 @@ def dequantize_q4(cache, out, src_rows=None, stream=None):
     _typed(out, "out", torch.bfloat16, (n, 576)); _typed(cache, "cache", torch.uint8, (cache.shape[0], Q4_ROW_BYTES))
     _typed(src_rows, "src_rows", torch.int64, (n,))
     with guard:
-        _check(lib().idxc_dequantize_q4(_ptr(cache), cache.shape[0], _ptr(src_rows), n, _ptr(out), _stream(stream)), "idxc_dequantize_q4")
+        _check(lib().idxc_dequantize_q4(_at(cache), cache.shape[0], _at(src_rows), n, _at(out), stream), "idxc_dequantize_q4")
 
 
 def latent_attention_workspace_bytes(B, n_step, max_len, H) -> int:
-    return int(lib().idxc_latent_attention_workspace_bytes(int(B), int(n_step), int(max_len), int(H)))
+    return lib().idxc_latent_attention_workspace_bytes(int(B), int(n_step), int(max_len), int(H))
 
 
 def _latent_workspace(workspace, B, n_step, max_len, H, device):
@@ -474,9 +479,9 @@ def latent_attention(q, kv, kv_base, lens, max_len, d_v, scale, want_lse=True, o
             out = torch.empty((B, n_step, H, d_v), dtype=torch.bfloat16, device=q.device)
         lse = torch.empty((B, n_step, H), dtype=torch.float32, device=q.device) if want_lse else None
         workspace = _latent_workspace(workspace, B, n_step, max_len, H, q.device)
-        _check(lib().idxc_latent_attention(_ptr(q), _ptr(kv), fmt, kv.shape[0], _ptr(kv_base), _ptr(lens), B, n_step, int(max_len), H, d_qk,
-                                           int(d_v), ctypes.c_float(scale), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
-                                           _stream(stream)), "idxc_latent_attention")
+        _check(lib().idxc_latent_attention(_at(q), _at(kv), fmt, kv.shape[0], _at(kv_base), _at(lens), B, n_step, int(max_len), H, d_qk,
+                                           int(d_v), float(scale), _at(out), _at(lse), _at(workspace), _nbytes(workspace),
+                                           stream), "idxc_latent_attention")
     return out, lse
 
 
@@ -495,9 +500,9 @@ def sparse_attention_q4(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, ou
             out = torch.empty((n_q, H, d_v), dtype=torch.bfloat16, device=q.device)
         lse = torch.empty((n_q, H), dtype=torch.float32, device=q.device) if want_lse else None
         workspace = _latent_workspace(workspace, n_q, 1, k_top, H, q.device)
-        _check(lib().idxc_sparse_attention_q4(_ptr(q), _ptr(kv), _ptr(topk), _ptr(kv_base), n_q, kv.shape[0], H, d_qk, int(d_v), k_top,
-                                              ctypes.c_float(scale), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
-                                              _stream(stream)), "idxc_sparse_attention_q4")
+        _check(lib().idxc_sparse_attention_q4(_at(q), _at(kv), _at(topk), _at(kv_base), n_q, kv.shape[0], H, d_qk, int(d_v), k_top,
+                                              float(scale), _at(out), _at(lse), _at(workspace), _nbytes(workspace),
+                                              stream), "idxc_sparse_attention_q4")
     return out, lse
 
 
@@ -519,9 +524,9 @@ def attention_weights(q, kv, lse, acc, scale, kv_base=None, lens=None, max_len=N
     k_top = 0 if topk is None else topk.shape[1]
     _typed(topk, "topk", torch.int32, (B, k_top))
     with guard:
-        _check(lib().idxc_attention_weights(_ptr(q), _ptr(kv), fmt, kv.shape[0], _ptr(kv_base), _ptr(lens), _ptr(topk), k_top, B, n_step,
-                                            0 if max_len is None else int(max_len), H, d_qk, ctypes.c_float(scale), _ptr(lse),
-                                            ctypes.c_float(beta), _ptr(acc), acc.shape[1], _stream(stream)), "idxc_attention_weights")
+        _check(lib().idxc_attention_weights(_at(q), _at(kv), fmt, kv.shape[0], _at(kv_base), _at(lens), _at(topk), k_top, B, n_step,
+                                            0 if max_len is None else int(max_len), H, d_qk, float(scale), _at(lse),
+                                            float(beta), _at(acc), acc.shape[1], stream), "idxc_attention_weights")
 
 
 def evict_select(acc, lens, budget, recent, keep_out, new_lens_out, stream=None):
@@ -533,8 +538,8 @@ def evict_select(acc, lens, budget, recent, keep_out, new_lens_out, stream=None)
     _typed(acc, "acc", torch.float32); _typed(lens, "lens", torch.int32, (B,)); _typed(new_lens_out, "new_lens_out", torch.int32, (B,))
     _typed(keep_out, "keep_out", torch.int32, (B, budget))
     with guard:
-        _check(lib().idxc_evict_select(_ptr(acc), ld, _ptr(lens), B, int(budget), int(recent), _ptr(keep_out), _ptr(new_lens_out),
-                                       _stream(stream)), "idxc_evict_select")
+        _check(lib().idxc_evict_select(_at(acc), ld, _at(lens), B, int(budget), int(recent), _at(keep_out), _at(new_lens_out),
+                                       stream), "idxc_evict_select")
 
 
 def compact_rows(src, dst, keep, n_keep, src_base, dst_base=None, stream=None):
@@ -554,8 +559,8 @@ def compact_rows(src, dst, keep, n_keep, src_base, dst_base=None, stream=None):
     _typed(keep, "keep", torch.int32); _typed(n_keep, "n_keep", torch.int32, (B,))
     _typed(src_base, "src_base", torch.int64, (B,)); _typed(dst_base, "dst_base", torch.int64, (B,))
     with guard:
-        _check(lib().idxc_compact_rows(_ptr(src), _ptr(dst), row_bytes, src.shape[0], dst.shape[0], _ptr(src_base), _ptr(dst_base), _ptr(keep),
-                                       ld_keep, _ptr(n_keep), B, _stream(stream)), "idxc_compact_rows")
+        _check(lib().idxc_compact_rows(_at(src), _at(dst), row_bytes, src.shape[0], dst.shape[0], _at(src_base), _at(dst_base), _at(keep),
+                                       ld_keep, _at(n_keep), B, stream), "idxc_compact_rows")
 
 
 def selftest_bounded_wait(wait_cycles: int = 1_000_000, stream=None):

@@ -150,7 +150,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                 tcgen05_fence_after_sync();
                 const uint32_t d = tmem_base + kColS + st * 32;
                 uint64_t a_desc = q_desc, b_desc = umma_smem_desc_sw128(smem_u32(k_smem + st * kKBytes));
-#pragma unroll 1
+#pragma unroll 3
                 for (int b = 0; b < kBlocks; ++b) {
                     umma_f16_pair_x4<2, 2>(d, a_desc, b_desc, kIdescS, b != 0 ? 1u : 0u);
                     a_desc += kRows * 128 / 16;

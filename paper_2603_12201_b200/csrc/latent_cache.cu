@@ -5,7 +5,7 @@
 namespace idxc {
 namespace {
 
-constexpr int kRowsPerWarp = 4;          // rows whose loads a warp keeps in flight
+constexpr int kRowsPerWarp = 2;          // rows whose loads a warp keeps in flight
 constexpr int kRowThreads = 256;
 
 __device__ __forceinline__ float bf16_at(const uint4& v, int i) {
