@@ -101,7 +101,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     const uint32_t tmem_base = *tmem_base_slot;
 
     Walk walk(p.tiles, run);
-    Piece pc;
+    Piece pc{};
     bool ok = true;
     uint32_t tile = 0, item = 0, blk = 0;      // counted over the whole kernel; blk: column blocks (ring slot blk % 4)
     auto give_up = [&](unsigned int code) {

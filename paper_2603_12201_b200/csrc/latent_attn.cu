@@ -138,7 +138,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const uint32_t tmem_base = *tmem_base_slot;
 
     Walk walk(p.tiles, run);
-    Piece pc;
+    Piece pc{};
     int64_t seq;
     int r0;
     bool ok = true;

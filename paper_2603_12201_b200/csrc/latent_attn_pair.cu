@@ -12,14 +12,19 @@
 // waits for the other's tile. (One shared buffer a tile, as for up to 64 rows, refills only after the product: 2.8 K clocks a tile.)
 // The first CTA's warps 0 and 1 issue for both; loaders and softmax warps of both CTAs arrive on the first one's barriers, and
 // commits are multicast to both.
-// Shared memory of a CTA: Q 9 x [64 x 128 B] | K 2 x 9 x [32 x 128 B] | V 2 x 4 x [64 x 128 B] | P 2 x [64 x 128 B].
+// Shared memory of a CTA: Q 9 x [64 x 128 B] | K 2 x 9 x [32 x 128 B] | V 2 x 4 x [64 x 128 B] | P 2 x [64 x 128 B]. What an MMA reads and a
+// copy writes passes its 128 bytes a clock, and bf16 tiles keep that path busy to 1800 clocks, all there is.
+// 4-bit rows in order are copied as they are into a ring of half tiles (3 x 32 rows x 416 B, a bulk copy each), and eight warps expand
+// them into K and V. To make room, and to take their reads off the same path, 6 of Q's 9 blocks are then the A operand from
+// tensor memory, in both lane halves (each multiplies its own half of the N columns): 325 us at 8 x 131072 rows, 342 with the rows read
+// straight into registers and Q in shared memory. Selected rows are read straight into registers: at 2047 queries of 2048 rows 1.28 ms,
+// through the ring 2.1 ms (a copy a row, or 16 bytes at a time: the ring is too short for their latency).
 #include "latent_attn.cuh"
 
 namespace idxc {
 using namespace latent;
 namespace {
 
-constexpr uint32_t kQBytes = kBlocks * kRows * 128;
 constexpr int kHalf = kTile / 2;                    // cache rows of a CTA's K
 constexpr uint32_t kKBlock = kHalf * 128;
 constexpr uint32_t kKBytes = kBlocks * kKBlock;
@@ -28,11 +33,19 @@ constexpr uint32_t kVBytes = 4 * kVBlock;
 constexpr uint32_t kPBytes = kRows * 128;
 constexpr uint32_t kBarBytes = 512;
 constexpr uint32_t kSwapBytes = 3 * 4 * 32 * 4;     // what two warps exchange: row maxima, double-buffered, and at the end row sums
-constexpr uint32_t kSmemBytes = kQBytes + 2 * kKBytes + 2 * kVBytes + 2 * kPBytes + kBarBytes + kSwapBytes + 1024;
-static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
+constexpr int kQT = 6;                              // 4-bit rows: Q blocks in tensor memory
+constexpr int kRawSlots = 3;
+constexpr uint32_t kRawBytes = kHalf * kLatentQ4RowBytes;
+enum Rows { kBf16, kCodes, kPicked };               // bf16 rows in order, 4-bit rows in order, selected 4-bit rows
+constexpr uint32_t q_bytes(Rows r) { return (r == kCodes ? kBlocks - kQT : kBlocks) * kRows * 128; }
+constexpr uint32_t smem_bytes(Rows r) {
+    return q_bytes(r) + 2 * kKBytes + 2 * kVBytes + 2 * kPBytes + (r == kCodes ? kRawSlots * kRawBytes : 0) + kBarBytes + kSwapBytes + 1024;
+}
+static_assert(smem_bytes(kBf16) <= 232448 && smem_bytes(kCodes) <= 232448 && smem_bytes(kPicked) <= 232448, "shared memory of a CTA");
 constexpr uint32_t kColS = 256;                     // S buffer b at kColS + 32 b; O in [0, 256)
+constexpr uint32_t kColQ = 320;                     // 4-bit rows: Q blocks 0 .. kQT - 1, 32 columns each (two bf16 a column)
 constexpr int kWarpsBf16 = 9;                       // 0 scores | 1 P V | 2 Q | 3 K (TMA) | 4..7 softmax | 8 V (TMA)
-constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 idle | 4..7 softmax | 8..11 K | 12..15 V
+constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 rows in order | 4..7 softmax | 8..11 K | 12..15 V
 
 // barrier over the two warps of 64 threads that share query rows; returns whether both came with ok
 __device__ __forceinline__ bool pair_of_warps_ok(int id, bool ok) {
@@ -45,17 +58,18 @@ __device__ __forceinline__ bool pair_of_warps_ok(int id, bool ok) {
     return r != 0;
 }
 
-template <bool Q4>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((Q4 ? kWarpsQ4 : kWarpsBf16) * 32, 1)
+template <Rows ROWS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((ROWS == kBf16 ? kWarpsBf16 : kWarpsQ4) * 32, 1)
 latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                         const __grid_constant__ CUtensorMap rope_map, const __grid_constant__ CUtensorMap v_map, const Params p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* q_smem = smem;
-    uint8_t* k_smem = q_smem + kQBytes;
+    uint8_t* k_smem = q_smem + q_bytes(ROWS);
     uint8_t* v_smem = k_smem + 2 * kKBytes;
     uint8_t* p_smem = v_smem + 2 * kVBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(p_smem + 2 * kPBytes);
+    uint8_t* raw_smem = p_smem + 2 * kPBytes + kBarBytes + kSwapBytes;
     float* swap = reinterpret_cast<float*>(p_smem + 2 * kPBytes + kBarBytes);        // [3][4 warps][32]
     // barriers that the first CTA's issuing warps wait on (both CTAs arrive there)
     const uint32_t bar_q_full = smem_u32(bars + 0);
@@ -71,10 +85,15 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     const uint32_t bar_tail = smem_u32(bars + 15);
     uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(bars + 16);
     volatile uint32_t* abort_flag = tmem_base_slot + 1;
-    // [4 tiles][2]: usable rows of a tile. Four deep: K of tile i + 2 may land before the softmax has looked at tile i, but that of
-    // tile i + 4 follows the scores of tile i + 2, which waited for the softmax of tile i.
-    uint32_t* mask_smem = reinterpret_cast<uint32_t*>(bars + 18);
-    static_assert(22 * 8 <= kBarBytes, "barrier area");
+    // 4-bit rows: half tiles that have landed, and that were read; Q's first blocks are in tensor memory
+    const uint32_t bar_raw_full = smem_u32(bars + 18);       // [3]
+    const uint32_t bar_raw_empty = smem_u32(bars + 21);      // [3]
+    const uint32_t bar_q_ready = smem_u32(bars + 24);
+    volatile uint8_t* raw_mask = reinterpret_cast<volatile uint8_t*>(bars + 25);         // [3][8] usable rows of a half tile in the ring, four to a byte
+    // selected rows: [4 tiles][2 halves][4] usable rows of a tile, eight to a byte. Four deep: K of tile i + 2 may land before the softmax has
+    // looked at tile i, but that of tile i + 4 follows the scores of tile i + 2, which waited for the softmax of tile i.
+    volatile uint8_t* mask_smem = reinterpret_cast<volatile uint8_t*>(bars + 28);
+    static_assert(32 * 8 <= kBarBytes, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = static_cast<int>(cluster_ctarank());
@@ -94,8 +113,8 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     if (threadIdx.x == 0) {
         mbar_init(bar_q_full, 2);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar_k_full + 8 * i, Q4 ? 8 : 2);
-            mbar_init(bar_v_full + 8 * i, Q4 ? 8 : 2);
+            mbar_init(bar_k_full + 8 * i, ROWS == kBf16 ? 2 : 8);
+            mbar_init(bar_v_full + 8 * i, ROWS == kBf16 ? 2 : 8);
             mbar_init(bar_s_free + 8 * i, 8);
             mbar_init(bar_p_ready + 8 * i, 8);
             mbar_init(bar_s_full + 8 * i, 1);
@@ -104,6 +123,11 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         mbar_init(bar_o_free, 8);
         mbar_init(bar_q_empty, 1);
         mbar_init(bar_tail, 1);
+        mbar_init(bar_q_ready, 8);
+        for (int i = 0; i < kRawSlots; ++i) {
+            mbar_init(bar_raw_full + 8 * i, 1);
+            mbar_init(bar_raw_empty + 8 * i, 8);
+        }
         *abort_flag = 0u;
         fence_mbar_init();
     }
@@ -125,7 +149,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     const uint32_t tmem_base = *tmem_base_slot;
 
     Walk walk(p.tiles, run);
-    Piece pc;
+    Piece pc{};
     int64_t seq;
     int r0;
     bool ok = true;
@@ -142,7 +166,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         constexpr uint32_t kIdescS = umma_idesc(1, 1, 128, kTile);
         const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
         while (rank == 0 && ok && walk.next(pc)) {
-            ok = wait_warp(bar_q_full, item & 1u);
+            ok = wait_warp(bar_q_full, item & 1u) && (ROWS != kCodes || wait_warp(bar_q_ready, item & 1u));
             for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {      // (a vote: the compiler sees a uniform loop)
                 const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
                 ok = wait_warp(bar_s_free + 8 * st, ph ^ 1u) && wait_warp(bar_k_full + 8 * st, ph);
@@ -150,8 +174,17 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                 tcgen05_fence_after_sync();
                 const uint32_t d = tmem_base + kColS + st * 32;
                 uint64_t a_desc = q_desc, b_desc = umma_smem_desc_sw128(smem_u32(k_smem + st * kKBytes));
+                if (ROWS == kCodes) {
+                    uint32_t a_tmem = tmem_base + kColQ;
 #pragma unroll 3
-                for (int b = 0; b < kBlocks; ++b) {
+                    for (int b = 0; b < kQT; ++b) {
+                        umma_f16_pair_ts_x4<2>(d, a_tmem, b_desc, kIdescS, b != 0 ? 1u : 0u);
+                        a_tmem += 32;
+                        b_desc += kKBlock / 16;
+                    }
+                }
+#pragma unroll 3
+                for (int b = ROWS == kCodes ? kQT : 0; b < kBlocks; ++b) {
                     umma_f16_pair_x4<2, 2>(d, a_desc, b_desc, kIdescS, b != 0 ? 1u : 0u);
                     a_desc += kRows * 128 / 16;
                     b_desc += kKBlock / 16;
@@ -191,14 +224,15 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                 ok = mbar_wait(bar_q_empty, (item & 1u) ^ 1u, abort_flag, kWaitCycleBudget, 200);
                 if (!ok) break;
                 const uint32_t full = in_first(bar_q_full);
-                mbar_arrive_expect_tx_cluster(full, kQBytes);
-                for (int b = 0; b < kBlocks; ++b)
-                    tma_load_2d_pair(smem_u32(q_smem + b * kRows * 128), &q_map, full, b * 64, static_cast<int>(seq * seq_rows + r0));
+                mbar_arrive_expect_tx_cluster(full, q_bytes(ROWS));
+                constexpr int first = ROWS == kCodes ? kQT : 0;          // (the others go to tensor memory by the softmax warps)
+                for (int b = first; b < kBlocks; ++b)
+                    tma_load_2d_pair(smem_u32(q_smem + (b - first) * kRows * 128), &q_map, full, b * 64, static_cast<int>(seq * seq_rows + r0));
                 ++item;
             }
             if (!ok) give_up(DEV_TIMEOUT_PRODUCER);
         }
-    } else if (!Q4 && warp == 3) {
+    } else if (ROWS == kBf16 && warp == 3) {
         // ------------------------------------------------------------ K, bf16: rows 32 rank .. of every tile. Rows behind the sequence's end
         // may hold anything: they only reach scores that the softmax discards.
         if (lane == 0) {
@@ -224,7 +258,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             }
             if (!ok) give_up(DEV_TIMEOUT_GATHER);
         }
-    } else if (!Q4 && warp == 8) {
+    } else if (ROWS == kBf16 && warp == 8) {
         // ------------------------------------------------------------ V, bf16: value columns 256 rank .. of every tile
         if (lane == 0) tma_prefetch_desc(&v_map);
         uint32_t tails = 0;
@@ -265,8 +299,42 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             }
         }
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
-    } else if (Q4 && warp >= 8) {
-        // ------------------------------------------------------------ 4-bit rows, expanded by four warps for K and four for V
+    } else if (ROWS == kCodes && warp == 3) {
+        // ------------------------------------------------------------ 4-bit rows in order into the ring, one copy a half tile: of every tile this
+        // CTA's half, then the other
+        const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
+        uint32_t slot = 0, ph = 1;
+        while (ok && walk.next(pc)) {
+            const int64_t s = pc.unit / static_cast<uint32_t>(p.blocks_per_seq);
+            const int len = static_cast<int>(seq_len(s));
+            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
+            for (int x = 0; x < 2 * pc.n && ok; ++x) {
+                const int at = (pc.t0 + (x >> 1)) * kTile + ((x & 1) ^ rank) * kHalf + lane;
+                const int64_t r = base + at;
+                const uint32_t valid = __ballot_sync(0xFFFFFFFFu, at < len && r >= 0 && r < p.a.n_kv);
+                ok = wait_warp(bar_raw_empty + 8 * slot, ph);
+                if (!ok) break;
+                const uint32_t full = bar_raw_full + 8 * slot;
+                if (lane < 8) raw_mask[slot * 8 + lane] = static_cast<uint8_t>((valid >> (4 * lane)) & 15u);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_expect_tx(full, __popc(valid) * kLatentQ4RowBytes);
+                __syncwarp();
+                if (valid != 0 && lane == __ffs(valid) - 1)
+                    bulk_load_1d(smem_u32(raw_smem) + slot * kRawBytes + lane * kLatentQ4RowBytes, kv + r * kLatentQ4RowBytes,
+                                 __popc(valid) * kLatentQ4RowBytes, full);
+                // ask the L2 for a tile further ahead
+                const int64_t soon = base + static_cast<int64_t>(pc.t0 + (x >> 1) + 4) * kTile;
+                if (lane == 31 && (x & 1) == 0 && rank == 0 && (x >> 1) + 4 < pc.n && soon >= 0 && soon + kTile <= p.a.n_kv)
+                    l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
+                if (++slot == kRawSlots) {
+                    slot = 0;
+                    ph ^= 1u;
+                }
+            }
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_PRODUCER);
+    } else if (ROWS == kPicked && warp >= 8) {
+        // ------------------------------------------------------------ selected 4-bit rows, read and expanded by four warps for K and four for V
         // Lane = 8 c + rr reads the 32 bytes of codes of 64-column block c (or c + 4) of a row rr and stores them as eight 16-byte pieces;
         // eight consecutive lanes then store to eight different positions of the swizzle (no bank conflicts). K's lanes also move 32 bytes of
         // the positional columns. While a tile is stored the next is in registers or on its way there, and the rows of the one
@@ -279,7 +347,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         const int off0 = is_v ? w * 16 + rr : rank * kHalf + w * 8 + rr, off1 = is_v ? off0 + 8 : (rank ^ 1) * kHalf + w * 8 + rr;
         struct Share { uint32_t code0[8], code1[8], rope[8], scale0, scale1, mask; } cur, nxt;      // this lane's of a tile
         int64_t base = 0;
-        int len = 0, raw0 = -1, raw1 = -1;                    // raw: position (or selected position) of this lane's rows in the next tile to fetch
+        int len = 0, raw0 = -1, raw1 = -1;                    // raw: selected position of this lane's rows in the next tile to fetch
         const int32_t* sel = nullptr;
         int i = 0;
         auto open_piece = [&]() {
@@ -287,17 +355,15 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             seq = pc.unit / static_cast<uint32_t>(p.blocks_per_seq);
             len = static_cast<int>(seq_len(seq));
             base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
-            sel = p.a.topk ? p.a.topk + seq * p.a.k_top : nullptr;
+            sel = p.a.topk + seq * p.a.k_top;
             i = 0;
         };
         auto look_up = [&]() {
             const int at = (pc.t0 + i) * kTile;
             raw0 = at + off0 < len ? at + off0 : -1;
             raw1 = at + off1 < len ? at + off1 : -1;
-            if (sel != nullptr) {
-                if (raw0 >= 0) raw0 = __ldg(sel + raw0);
-                if (raw1 >= 0) raw1 = __ldg(sel + raw1);
-            }
+            if (raw0 >= 0) raw0 = __ldg(sel + raw0);
+            if (raw1 >= 0) raw1 = __ldg(sel + raw1);
         };
         auto cache_row = [&](int raw) -> int {                // -1: takes no part
             const int64_t r = base + raw;
@@ -306,7 +372,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         auto fetch = [&](Share& f) {                          // the tile that was looked up; then looks up the next
             const int s0 = cache_row(raw0);
             int s1 = cache_row(raw1);
-            if (sel != nullptr) {
+            {
                 const uint32_t mine = __ballot_sync(0xFFFFFFFFu, s0 >= 0) & 255u, theirs = __ballot_sync(0xFFFFFFFFu, s1 >= 0) & 255u;
                 f.mask = rank == 0 ? mine | (theirs << 8) : theirs | (mine << 8);     // K: bits 0..7: in the first half of the tile, 8..15: the second
             }
@@ -319,11 +385,6 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             load_nc_256(row0 + kLatentQ4RopeOff + c4 * 32, s0 >= 0 && !is_v, f.rope);
             f.scale0 = load_nc_32(row0 + kLatentQ4ScaleOff + block0 * 4, s0 >= 0);
             f.scale1 = load_nc_32(row1 + kLatentQ4ScaleOff + block1 * 4, s1 >= 0);
-            // dense rows lie one behind the other: ask the L2 for a tile further ahead
-            if (sel == nullptr && rank == 0 && warp == 8 && lane == 0 && i + 3 < pc.n) {
-                const int64_t soon = base + static_cast<int64_t>(pc.t0 + i + 3) * kTile;
-                if (soon >= 0 && soon + kTile <= p.a.n_kv) l2_prefetch(kv + soon * kLatentQ4RowBytes, kTile * kLatentQ4RowBytes);
-            }
             if (++i == pc.n) open_piece();
             look_up();
         };
@@ -359,11 +420,111 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             if (!is_v) {
                 st_shared_v4(rope_dst + st * kKBytes, make_uint4(cur.rope[0], cur.rope[1], cur.rope[2], cur.rope[3]));
                 st_shared_v4((rope_dst + st * kKBytes) ^ 16u, make_uint4(cur.rope[4], cur.rope[5], cur.rope[6], cur.rope[7]));
-                if (lane < 2) reinterpret_cast<uint8_t*>(mask_smem + (t & 3) * 2 + lane)[w] = static_cast<uint8_t>(cur.mask >> (8 * lane));
+                if (lane < 2) mask_smem[((t & 3) * 2 + lane) * 4 + w] = static_cast<uint8_t>(cur.mask >> (8 * lane));
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(bar_full + 8 * st);
+        }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
+    } else if (ROWS == kCodes && warp >= 8) {
+        // ------------------------------------------------------------ 4-bit rows, expanded by four warps for K and four for V
+        // A lane has four pieces of a tile, each the 16 bytes of codes under one scale, which become four 16-byte pieces of operand.
+        // lane = 8 g + 2 rr + half: 64-column block g (K: then g + 4; V: 4 rank + g), half `half` of it, row rr of four. Eight consecutive
+        // lanes then read 32 bytes of four rows, which lie 416 bytes apart (four different quarters of the banks), and store to eight
+        // different positions of the swizzle: neither side has bank conflicts. Pieces t = 0..3: rows 8w + 4 (t % 2) + rr of a half tile; K: all of
+        // this CTA's half, V: of its half and of the other. The code is rolled and shared by the two kinds on purpose: unrolled, the roles
+        // stalled on instruction fetch.
+        const bool is_v = warp >= 12;
+        const int w = warp & 3, g = lane >> 3, rr = (lane >> 1) & 3, half = lane & 1;
+        const uint32_t raw = smem_u32(raw_smem);
+        const uint32_t my_row = w * 8 + rr;                   // t even; t odd: 4 more
+        const uint32_t my_chunk = 2 * (is_v ? 4 * rank + g : g) + half;
+        const uint32_t bar_free = is_v ? bar_pv_done : bar_s_full, bar_full = in_first(is_v ? bar_v_full : bar_k_full);
+        const uint32_t buf_bytes = is_v ? kVBytes : kKBytes;
+        // piece v of a 32-column group goes to chunk (4 half + v) ^ (row % 8) of its 128 bytes: exclusive ors on an address whose low
+        // seven bits hold (4 half) ^ rr; rows of odd t have bit 2 of the row set
+        const uint32_t my_dst = (is_v ? smem_u32(v_smem) + g * kVBlock + rank * kHalf * 128 : smem_u32(k_smem) + g * kKBlock) + my_row * 128 + (((4 * half) ^ rr) << 4);
+        const int32_t to_second = is_v ? (rank == 0 ? 1 : -1) * kHalf * 128 : static_cast<int32_t>(4 * kKBlock);      // from t = 0, 1 to t = 2, 3
+        const uint32_t rope_src = (w * 8 + (lane >> 3)) * kLatentQ4RowBytes + kLatentQ4RopeOff + (lane & 7) * 16;
+        const uint32_t rope_dst = smem_u32(k_smem) + 8 * kKBlock + (w * 8 + (lane >> 3)) * 128 + (((lane & 7) ^ (lane >> 3)) << 4);
+        uint32_t slot = 0, raw_ph = 0;
+        auto next_slot = [&]() {
+            if (++slot == kRawSlots) {
+                slot = 0;
+                raw_ph ^= 1u;
+            }
+        };
+        auto done_with = [&](uint32_t s) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_raw_empty + 8 * s);
+        };
+        uint4 code[4], rope[2] = {};
+        uint32_t scale[4];
+        auto read = [&](uint4& c0, uint4& c1, uint32_t& s0, uint32_t& s1, uint32_t chunk) {        // pieces of rows my_row and my_row + 4
+            const uint32_t at = raw + slot * kRawBytes + my_row * kLatentQ4RowBytes;
+            const uint32_t valid = raw_mask[slot * 8 + 2 * w] >> rr, valid4 = raw_mask[slot * 8 + 2 * w + 1] >> rr;
+            c0 = ld_shared_v4(at + chunk * 16);
+            c1 = ld_shared_v4(at + 4 * kLatentQ4RowBytes + chunk * 16);
+            s0 = (valid & 1u) ? ld_shared_u16(at + kLatentQ4ScaleOff + chunk * 2) : 0u;
+            s1 = (valid4 & 1u) ? ld_shared_u16(at + 4 * kLatentQ4RowBytes + kLatentQ4ScaleOff + chunk * 2) : 0u;
+        };
+        const int total = run.n;
+#pragma unroll 1
+        for (int t = 0; t < total; ++t) {
+            const uint32_t st = t & 1;
+            ok = wait_warp(bar_raw_full + 8 * slot, raw_ph);
+            if (!ok) break;
+            read(code[0], code[1], scale[0], scale[1], my_chunk);
+            if (!is_v) {
+                read(code[2], code[3], scale[2], scale[3], my_chunk + 8);
+                const uint32_t valid = raw_mask[slot * 8 + 2 * w] >> (lane >> 3), valid4 = raw_mask[slot * 8 + 2 * w + 1] >> (lane >> 3);
+                rope[0] = (valid & 1u) ? ld_shared_v4(raw + slot * kRawBytes + rope_src) : make_uint4(0, 0, 0, 0);
+                rope[1] = (valid4 & 1u) ? ld_shared_v4(raw + slot * kRawBytes + rope_src + 4 * kLatentQ4RowBytes) : make_uint4(0, 0, 0, 0);
+            }
+            done_with(slot);
+            next_slot();
+            if (is_v) {
+                ok = wait_warp(bar_raw_full + 8 * slot, raw_ph);
+                if (!ok) break;
+                read(code[2], code[3], scale[2], scale[3], my_chunk);
+                done_with(slot);
+                next_slot();
+            }
+            ok = wait_warp(bar_free + 8 * st, ((static_cast<uint32_t>(t) >> 1) & 1u) ^ 1u);
+            if (!ok) break;
+            uint32_t to = my_dst + st * buf_bytes;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const Q4Scale s0 = q4_scale_of(scale[0]), s1 = q4_scale_of(scale[1]);
+                const uint32_t odd = (to + 4 * 128) ^ 64u;
+                st_shared_v4(to, dequant8_q4(code[0].x, s0));
+                st_shared_v4(to ^ 16u, dequant8_q4(code[0].y, s0));
+                st_shared_v4(to ^ 32u, dequant8_q4(code[0].z, s0));
+                st_shared_v4(to ^ 48u, dequant8_q4(code[0].w, s0));
+                st_shared_v4(odd, dequant8_q4(code[1].x, s1));
+                st_shared_v4(odd ^ 16u, dequant8_q4(code[1].y, s1));
+                st_shared_v4(odd ^ 32u, dequant8_q4(code[1].z, s1));
+                st_shared_v4(odd ^ 48u, dequant8_q4(code[1].w, s1));
+                code[0] = code[2];
+                code[1] = code[3];
+                scale[0] = scale[2];
+                scale[1] = scale[3];
+                to += to_second;
+            }
+            if (!is_v) {
+                st_shared_v4(rope_dst + st * kKBytes, rope[0]);
+                st_shared_v4((rope_dst + st * kKBytes + 4 * 128) ^ 64u, rope[1]);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(bar_full + 8 * st);
+            if (!is_v) {                                      // K has no use for the other half: its turn is passed when it has landed
+                ok = wait_warp(bar_raw_full + 8 * slot, raw_ph);
+                if (!ok) break;
+                done_with(slot);
+                next_slot();
+            }
         }
         if (!ok && lane == 0) give_up(DEV_TIMEOUT_GATHER);
     } else if (warp >= 4 && warp < 8) {
@@ -378,6 +539,33 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         // Both warps of a row leave the tile loop at the same barrier or not at all: `ok` is only acted upon there.
         while (walk.next(pc)) {
             const int n_rows = rows_of(pc.unit, seq, r0);
+            if (ROWS == kCodes) {
+                // Q's first blocks: this thread's row (both lane halves hold it) to tensor memory; the scores of the last piece are done. Rows
+                // that are not ours stay what they were: they only reach scores of rows that nobody reads.
+                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.a.q) + (seq * seq_rows + r0 + row) * (kLatentCols * 2));
+                auto load_block = [&](int b, uint32_t (&r)[32]) {
+#pragma unroll
+                    for (int ch = 0; ch < 8; ++ch) {
+                        const uint4 v = row < n_rows ? __ldg(src + b * 8 + ch) : make_uint4(0, 0, 0, 0);
+                        r[4 * ch] = v.x; r[4 * ch + 1] = v.y; r[4 * ch + 2] = v.z; r[4 * ch + 3] = v.w;
+                    }
+                };
+                uint32_t ra[32], rb[32];
+                load_block(0, ra);
+#pragma unroll 1
+                for (int b = 0; b < kQT; b += 2) {
+                    load_block(b + 1, rb);
+                    __syncwarp();
+                    tmem_st_32x32b_x32(lane_base + kColQ + b * 32, ra);
+                    if (b + 2 < kQT) load_block(b + 2, ra);
+                    __syncwarp();
+                    tmem_st_32x32b_x32(lane_base + kColQ + (b + 1) * 32, rb);
+                }
+                tmem_st_wait();
+                tcgen05_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(in_first(bar_q_ready));
+            }
             const int64_t len = seq_len(seq);
             const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
             // positions [lo, sees) are seen by this row: those inside the cache, up to the row's own new token
@@ -398,7 +586,9 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                     tcgen05_fence_after_sync();
                     uint32_t s[32];
                     tmem_ld_32x32b_x32(lane_base + kColS + st * 32, s);
-                    const uint32_t usable = Q4 && p.a.topk ? *const_cast<volatile uint32_t*>(mask_smem + (tile & 3u) * 2 + half) : 0xFFFFFFFFu;
+                    uint32_t usable = 0xFFFFFFFFu;
+                    if (ROWS == kPicked)
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(usable) : "r"(smem_u32(const_cast<uint8_t*>(mask_smem)) + ((tile & 3u) * 2 + half) * 4) : "memory");
                     tmem_ld_wait(s);
                     tcgen05_fence_before_sync();
                     __syncwarp();
@@ -537,12 +727,13 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
 }  // namespace
 
 cudaError_t launch_latent_attn_pair(const LatentMaps& maps, const Params& p, cudaStream_t stream) {
-    const void* k = p.a.q4 ? reinterpret_cast<const void*>(latent_attn_pair_kernel<true>) : reinterpret_cast<const void*>(latent_attn_pair_kernel<false>);
-    if (cudaError_t e = ensure_max_dynamic_smem(k, kSmemBytes); e != cudaSuccess) return e;
-    const unsigned grid = static_cast<unsigned>(p.groups * 2);
-    if (p.a.q4) latent_attn_pair_kernel<true><<<grid, kWarpsQ4 * 32, kSmemBytes, stream>>>(maps.q, maps.k, maps.rope, maps.v, p);
-    else latent_attn_pair_kernel<false><<<grid, kWarpsBf16 * 32, kSmemBytes, stream>>>(maps.q, maps.k, maps.rope, maps.v, p);
-    return cudaGetLastError();
+    auto go = [&](auto kernel, Rows rows, int warps) -> cudaError_t {
+        if (cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), smem_bytes(rows)); e != cudaSuccess) return e;
+        kernel<<<static_cast<unsigned>(p.groups * 2), warps * 32, smem_bytes(rows), stream>>>(maps.q, maps.k, maps.rope, maps.v, p);
+        return cudaGetLastError();
+    };
+    if (!p.a.q4) return go(latent_attn_pair_kernel<kBf16>, kBf16, kWarpsBf16);
+    return p.a.topk ? go(latent_attn_pair_kernel<kPicked>, kPicked, kWarpsQ4) : go(latent_attn_pair_kernel<kCodes>, kCodes, kWarpsQ4);
 }
 
 }  // namespace idxc

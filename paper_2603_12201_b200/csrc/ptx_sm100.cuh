@@ -328,6 +328,16 @@ __device__ __forceinline__ uint64_t umma_smem_desc_noswizzle(uint32_t smem_addr,
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_shared_u16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+    return v;
+}
 // Four 8 x 8 matrices of 16-bit elements to shared memory; lane l addresses row l % 8 of matrix l / 8, and register i of lane
 // l holds elements 2 (l % 4), + 1 of row l / 4 of matrix i.
 __device__ __forceinline__ void stmatrix_x4(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
@@ -415,6 +425,22 @@ __device__ __forceinline__ void umma_f16_pair_x4(uint32_t d_tmem, uint64_t a, ui
         "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %3, %7, %9, 1;\n\t"
         "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %4, %8, %9, 1;\n\t}"
         ::"r"(d_tmem), "l"(a), "l"(a + STEP_A), "l"(a + 2 * STEP_A), "l"(a + 3 * STEP_A), "l"(b), "l"(b + STEP_B), "l"(b + 2 * STEP_B),
+          "l"(b + 3 * STEP_B), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// The same with A from tensor memory: 8 columns a step, in each CTA the rows of its lanes 0..63 for the first half of the N columns and
+// of lanes 64..127 for the second.
+template <int STEP_B>
+__device__ __forceinline__ void umma_f16_pair_ts_x4(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred e, p;\n\t"
+        "setp.ne.b32 p, %10, 0;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %5, %9, p;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%2], %6, %9, 1;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%3], %7, %9, 1;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%4], %8, %9, 1;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(a_tmem + 8), "r"(a_tmem + 16), "r"(a_tmem + 24), "l"(b), "l"(b + STEP_B), "l"(b + 2 * STEP_B),
           "l"(b + 3 * STEP_B), "r"(idesc), "r"(accumulate)
         : "memory");
 }
