@@ -579,30 +579,40 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             }
             const float i0 = __shfl_sync(0xFFFFFFFFu, inv[0], (lane & 7) * 4), i1 = __shfl_sync(0xFFFFFFFFu, inv[1], (lane & 7) * 4);
             const float f = (lane & 8) ? i1 : i0;
-            const int out_row = quarter * 16 + (lane & 15), col0 = (lane >> 4) * 256;
             const int64_t at_row = seq * seq_rows + r0;
             const int64_t slot = (static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * kRows;
+            // this warp's rows of P, which it alone writes and the last product has read, are where it turns its rows
+            const uint32_t stage = smem_u32(p_smem) + quarter * 2048;
 #pragma unroll 1
             for (int c = 0; c < 8; ++c) {
                 uint32_t o[32];
                 tmem_ld_32x32b_x32(lane_base + c * 32, o);
                 tmem_ld_wait(o);
-                if (out_row < n_rows && pc.whole) {
-                    uint4* dst = reinterpret_cast<uint4*>(p.out + (at_row + out_row) * 512 + col0 + c * 32);
+                uint4 v[4];
+                if (pc.whole) {
 #pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        dst[v] = make_uint4(pack2(__uint_as_float(o[8 * v]) * f, __uint_as_float(o[8 * v + 1]) * f),
-                                            pack2(__uint_as_float(o[8 * v + 2]) * f, __uint_as_float(o[8 * v + 3]) * f),
-                                            pack2(__uint_as_float(o[8 * v + 4]) * f, __uint_as_float(o[8 * v + 5]) * f),
-                                            pack2(__uint_as_float(o[8 * v + 6]) * f, __uint_as_float(o[8 * v + 7]) * f));
-                } else if (out_row < n_rows) {
-                    float4* dst = reinterpret_cast<float4*>(p.part_out + (slot + out_row) * 512 + col0 + c * 32);
+                    for (int k = 0; k < 4; ++k)
+                        v[k] = make_uint4(pack2(__uint_as_float(o[8 * k]) * f, __uint_as_float(o[8 * k + 1]) * f),
+                                          pack2(__uint_as_float(o[8 * k + 2]) * f, __uint_as_float(o[8 * k + 3]) * f),
+                                          pack2(__uint_as_float(o[8 * k + 4]) * f, __uint_as_float(o[8 * k + 5]) * f),
+                                          pack2(__uint_as_float(o[8 * k + 6]) * f, __uint_as_float(o[8 * k + 7]) * f));
+                    store_rows(stage, lane, v, [&](int r, int i) -> uint4* {
+                        const int row = quarter * 16 + (r & 15);
+                        return row < n_rows ? reinterpret_cast<uint4*>(p.out + (at_row + row) * 512 + (r >> 4) * 256 + c * 32) + i : nullptr;
+                    });
+                } else {
 #pragma unroll
-                    for (int v = 0; v < 8; ++v)
-                        dst[v] = make_float4(__uint_as_float(o[4 * v]) * f, __uint_as_float(o[4 * v + 1]) * f, __uint_as_float(o[4 * v + 2]) * f,
-                                             __uint_as_float(o[4 * v + 3]) * f);
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[k] = make_uint4(__float_as_uint(__uint_as_float(o[16 * e + 4 * k]) * f), __float_as_uint(__uint_as_float(o[16 * e + 4 * k + 1]) * f),
+                                              __float_as_uint(__uint_as_float(o[16 * e + 4 * k + 2]) * f), __float_as_uint(__uint_as_float(o[16 * e + 4 * k + 3]) * f));
+                        store_rows(stage, lane, v, [&](int r, int i) -> uint4* {
+                            const int row = quarter * 16 + (r & 15);
+                            return row < n_rows ? reinterpret_cast<uint4*>(p.part_out + (slot + row) * 512 + (r >> 4) * 256 + c * 32 + e * 16) + i : nullptr;
+                        });
+                    }
                 }
-                __syncwarp();
             }
             tcgen05_fence_before_sync();
             __syncwarp();

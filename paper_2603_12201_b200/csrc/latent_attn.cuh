@@ -141,6 +141,25 @@ struct Walk {
     }
 };
 
+// A warp's 32 rows of 16 N bytes, a row in each lane's registers, to global memory through 512 N bytes of shared memory: an
+// instruction then writes 32 / N rows in contiguous pieces. (Stored straight from the registers, 16 bytes of 32 rows an instruction, the
+// output of a piece took 10 to 12 thousand clocks.) dst(r, i): where piece i of row r goes, nullptr: nowhere.
+template <int N, typename Dst>
+__device__ __forceinline__ void store_rows(uint32_t stage, int lane, const uint4 (&v)[N], Dst dst) {
+    auto swizzle = [](int r) -> int { return N == 8 ? (r & 7) : ((r >> 1) & 3); };
+#pragma unroll
+    for (int i = 0; i < N; ++i) st_shared_v4(stage + lane * (16 * N) + ((i ^ swizzle(lane)) << 4), v[i]);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int r = k * (32 / N) + lane / N, i = lane % N;
+        const uint4 w = ld_shared_v4(stage + r * (16 * N) + ((i ^ swizzle(r)) << 4));
+        uint4* to = dst(r, i);
+        if (to != nullptr) *to = w;
+    }
+    __syncwarp();
+}
+
 // Zeros and -inf for the units without tiles; every group looks at its share, a lane each. `quarter`: which of the four calling warps.
 template <typename RowsOf>
 __device__ __forceinline__ void write_empty_units(const Params& p, int group, int quarter, int lane, int seq_rows, RowsOf rows_of) {

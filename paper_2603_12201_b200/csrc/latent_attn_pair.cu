@@ -675,27 +675,44 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             const float inv = l > 0.f ? 1.f / l : 0.f;
             const int64_t at_row = seq * seq_rows + r0 + row;
             const int64_t slot = ((static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * 2 + rank) * kRows + row;
+            // P's buffers are free now, and until both warps of a row have met at the next tile: a quarter for each warp to turn its rows in
+            const uint32_t stage = smem_u32(p_smem) + q * 4096;
+            const int first_row = (q & 1) * 32;
+            if (pc.whole) {
 #pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
-                uint32_t o[32];
-                tmem_ld_32x32b_x32(lane_base + c * 32, o);
-                tmem_ld_wait(o);
-                if (row < n_rows && pc.whole) {
-                    uint4* dst = reinterpret_cast<uint4*>(p.out + at_row * 512 + half * 256 + c * 32);
+                for (int c = 0; c < 4; ++c) {
+                    uint4 v[8];
 #pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        dst[v] = make_uint4(pack2(__uint_as_float(o[8 * v]) * inv, __uint_as_float(o[8 * v + 1]) * inv),
-                                            pack2(__uint_as_float(o[8 * v + 2]) * inv, __uint_as_float(o[8 * v + 3]) * inv),
-                                            pack2(__uint_as_float(o[8 * v + 4]) * inv, __uint_as_float(o[8 * v + 5]) * inv),
-                                            pack2(__uint_as_float(o[8 * v + 6]) * inv, __uint_as_float(o[8 * v + 7]) * inv));
-                } else if (row < n_rows) {
-                    float4* dst = reinterpret_cast<float4*>(p.part_out + slot * 512 + half * 256 + c * 32);
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t o[32];
+                        tmem_ld_32x32b_x32(lane_base + c * 64 + e * 32, o);
+                        tmem_ld_wait(o);
 #pragma unroll
-                    for (int v = 0; v < 8; ++v)
-                        dst[v] = make_float4(__uint_as_float(o[4 * v]) * inv, __uint_as_float(o[4 * v + 1]) * inv, __uint_as_float(o[4 * v + 2]) * inv,
-                                             __uint_as_float(o[4 * v + 3]) * inv);
+                        for (int k = 0; k < 4; ++k)
+                            v[4 * e + k] = make_uint4(pack2(__uint_as_float(o[8 * k]) * inv, __uint_as_float(o[8 * k + 1]) * inv),
+                                                      pack2(__uint_as_float(o[8 * k + 2]) * inv, __uint_as_float(o[8 * k + 3]) * inv),
+                                                      pack2(__uint_as_float(o[8 * k + 4]) * inv, __uint_as_float(o[8 * k + 5]) * inv),
+                                                      pack2(__uint_as_float(o[8 * k + 6]) * inv, __uint_as_float(o[8 * k + 7]) * inv));
+                    }
+                    store_rows(stage, lane, v, [&](int r, int i) -> uint4* {
+                        return first_row + r < n_rows ? reinterpret_cast<uint4*>(p.out + (at_row - lane + r) * 512 + half * 256 + c * 64) + i : nullptr;
+                    });
                 }
-                __syncwarp();
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t o[32];
+                    tmem_ld_32x32b_x32(lane_base + c * 32, o);
+                    tmem_ld_wait(o);
+                    uint4 v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        v[k] = make_uint4(__float_as_uint(__uint_as_float(o[4 * k]) * inv), __float_as_uint(__uint_as_float(o[4 * k + 1]) * inv),
+                                          __float_as_uint(__uint_as_float(o[4 * k + 2]) * inv), __float_as_uint(__uint_as_float(o[4 * k + 3]) * inv));
+                    store_rows(stage, lane, v, [&](int r, int i) -> uint4* {
+                        return first_row + r < n_rows ? reinterpret_cast<uint4*>(p.part_out + (slot - lane + r) * 512 + half * 256 + c * 32) + i : nullptr;
+                    });
+                }
             }
             tcgen05_fence_before_sync();
             __syncwarp();
