@@ -358,8 +358,9 @@ idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int6
  *            call in flight
  * Supported: d_qk = 576, d_v = 512, 1 <= H <= 128, n_step >= 1, B * n_step * H < 2^31, max_len <= 2^30, n_kv < 2^31,
  * B * (n_step * H rounded up to 64s) * max_len below 2^42.
- * Rows that no token sees are never read. Arithmetic: bf16 products with fp32 accumulation, fp32 softmax, probabilities
- * rounded to bf16 for the second product, bf16 output. The result does not depend on what else runs.
+ * Rows that no token sees do not influence the result, whatever they hold (some behind a sequence's end are read). Arithmetic: bf16
+ * products with fp32 accumulation, fp32 softmax, probabilities rounded to bf16 for the second product, bf16 output. The result
+ * does not depend on what else runs.
  *
  * idxc_sparse_attention_q4 -- idxc_sparse_attention (same arguments, same rules) over a cache of 4-bit rows; its workspace is
  * idxc_latent_attention_workspace_bytes(n_q, 1, k_top, H) bytes, 256-byte aligned.

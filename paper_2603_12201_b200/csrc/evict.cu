@@ -14,9 +14,9 @@ namespace {
 
 constexpr int kEvCtas = 8;                           // CTAs of a long sequence (short ones, up to kEvShort positions a row of acc: one)
 constexpr int kEvShort = 16384;
-constexpr int kEvThreads = 512;
+constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
-constexpr int kEvBins = 2048;
+constexpr int kEvBins = 2 * kEvThreads;               // 2048, two a thread
 constexpr int kEvKeys = 49152;                       // keys of a slice that fit into shared memory at most
 constexpr uint32_t kEvHistBytes = 2 * kEvBins * 4;
 
@@ -24,11 +24,6 @@ constexpr uint32_t kEvHistBytes = 2 * kEvBins * 4;
 __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
-    uint4 v;
-    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
 }
 __device__ __forceinline__ uint2 ld_cluster_v2(uint32_t addr) {
     uint2 v;
@@ -88,16 +83,16 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
             sync_all();
             // (every CTA has read the other buffer by now: it may be cleared for the next pass)
             for (int i = tid; i < kEvBins; i += kEvThreads) hist[((pass + 1) & 1) * kEvBins + i] = 0;
-            // counts of all CTAs from the top bin down: the bin in which they reach `want`. Thread t has bins top .. top - 3.
-            const int top = kEvBins - 1 - 4 * tid;
-            const uint32_t at = smem_u32(h + top - 3);
-            uint32_t c[4] = {0, 0, 0, 0};
+            // counts of all CTAs from the top bin down: the bin in which they reach `want`. Thread t has bins top and top - 1.
+            const int top = kEvBins - 1 - 2 * tid;
+            const uint32_t at = smem_u32(h + top - 1);
+            uint32_t c[2] = {0, 0};
 #pragma unroll
             for (int r = 0; r < CTAS; ++r) {
-                const uint4 v = ld_cluster_v4(map_to_cta(at, r));
-                c[0] += v.w; c[1] += v.z; c[2] += v.y; c[3] += v.x;
+                const uint2 v = ld_cluster_v2(map_to_cta(at, r));
+                c[0] += v.y; c[1] += v.x;
             }
-            const uint32_t mine = c[0] + c[1] + c[2] + c[3];
+            const uint32_t mine = c[0] + c[1];
             uint32_t run = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -109,7 +104,7 @@ evict_select_kernel(const float* __restrict__ acc, int64_t ld, const int32_t* __
             uint32_t before = run - mine;
             for (int w = 0; w < warp; ++w) before += warp_sum[w];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 2; ++j) {
                 if (before < want && before + c[j] >= want) { s_bin = top - j; s_left = want - before; }
                 before += c[j];
             }

@@ -13,6 +13,8 @@ namespace latent {
 constexpr int kTile = 64;                           // cache rows of a tile
 constexpr int kRows = 64;                           // query rows of a CTA
 constexpr int kBlocks = 9;                          // 64-column blocks of a row
+// A loader of Q waits while the piece before is worked on: its bound grows with that piece (a tile takes a few thousand cycles).
+__device__ __forceinline__ long long piece_budget(int tiles) { return kWaitCycleBudget + 50000LL * tiles; }
 constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
 
 // Tiles of a unit: counted beforehand, or from its sequence's length (no lengths: max_len for all).

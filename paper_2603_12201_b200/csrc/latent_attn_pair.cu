@@ -219,9 +219,11 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         // ------------------------------------------------------------ Q
         if (lane == 0) {
             tma_prefetch_desc(&q_map);
+            int before = 0;                                  // tiles of the piece before
             while (ok && walk.next(pc)) {
                 rows_of(pc.unit, seq, r0);
-                ok = mbar_wait(bar_q_empty, (item & 1u) ^ 1u, abort_flag, kWaitCycleBudget, 200);
+                ok = mbar_wait(bar_q_empty, (item & 1u) ^ 1u, abort_flag, piece_budget(before), 200);
+                before = pc.n;
                 if (!ok) break;
                 const uint32_t full = in_first(bar_q_full);
                 mbar_arrive_expect_tx_cluster(full, q_bytes(ROWS));

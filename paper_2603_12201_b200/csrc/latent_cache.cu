@@ -13,30 +13,54 @@ __device__ __forceinline__ float bf16_at(const uint4& v, int i) {
     return __uint_as_float((i & 1) ? (w & 0xFFFF0000u) : (w << 16));
 }
 
+constexpr float kScaleMax = 0x1.5p+123f;
+
 // The smallest scale of 5 significant bits that holds `amax` in 7 steps: amax / 7 rounded up past its top 4 mantissa bits.
 // At least 2^-100 (code * scale then stays far from the subnormals), at most 1.3125 * 2^123 (24 steps, which the reader
 // subtracts, stay finite).
 __device__ __forceinline__ float q4_scale(float amax) {
     const float s = __fdiv_rn(fmaxf(amax, 7.f * 0x1p-100f), 7.f);
     const float up = __uint_as_float((__float_as_uint(s) + 0x7FFFFu) & ~0x7FFFFu);
-    return fminf(up, 0x1.5p+123f);
+    return fminf(up, kScaleMax);
 }
 
-// One word of codes from eight columns. The quotient is corrected by one residual step from the rounded reciprocal r of the
-// scale, which gives the correctly rounded x / scale (every product with a 5-bit scale is exact in the FMA), so that a value
-// halfway between two codes is seen as such and goes to the even one.
-__device__ __forceinline__ uint32_t q4_word(const uint4& v, float scale, float r) {
+// One word of codes from eight columns, four instructions a column. x times the rounded reciprocal r of the scale is off by less than
+// 2^-20, and an 8-bit number over a 5-bit one that is no half-integer is at least 2^-10 away from the next (below 7.5): so the sum with
+// 6144, whose unit is 2^-11, rounds the quotient to a value on the same side of every border and puts exact halves exactly. The
+// second sum rounds that to an integer, halves to even, in the low mantissa bits of 1.5 * 2^23 + 8 + code; the words' high
+// parts, the same for every column, drop out of the weighted sum modulo 2^32 as one constant.
+constexpr float kSnap = 6144.f;                          // 1.5 * 2^12
+constexpr float kCodeBias = 12582912.f + 8.f;            // 1.5 * 2^23 + 8
+constexpr uint32_t kWordBias = 0x4B400000u * 0x11111111u;
+__device__ __forceinline__ uint32_t q4_word(const uint4& v, float r) {
     uint32_t word = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float x = bf16_at(v, i);
-        const float q = x * r;
-        const float y = __fmaf_rn(-__fmaf_rn(q, scale, -x), r, q);
-        const int code = __float2int_rn(fminf(fmaxf(y, -7.f), 7.f));
-        const int nibble = (i & 1) * 4 + (i >> 1);
-        word |= static_cast<uint32_t>(code + 8) << (4 * nibble);
+        const float y = __fadd_rn(__fmaf_rn(bf16_at(v, i), r, kSnap), kCodeBias - kSnap);
+        word += __float_as_uint(y) << (4 * ((i & 1) * 4 + (i >> 1)));
+    }
+    return word - kWordBias;
+}
+
+// The same where codes may lie beyond +-7: the scale is at its upper limit, or x is not a number.
+__device__ __noinline__ uint32_t q4_word_clipped(uint4 v, float scale) {
+    uint32_t word = 0;
+    for (int i = 0; i < 8; ++i) {
+        const float y = rintf(__fdiv_rn(bf16_at(v, i), scale));
+        word |= static_cast<uint32_t>(__float2int_rn(fminf(fmaxf(y, -7.f), 7.f)) + 8) << (4 * ((i & 1) * 4 + (i >> 1)));
     }
     return word;
+}
+
+// Largest magnitude of eight bf16 values, as bf16 bits; not a number if one is none (its group is then written clipped).
+__device__ __forceinline__ uint32_t abs_max8(const uint4& v) {
+    auto two = [](uint32_t w) -> __nv_bfloat162 {
+        w &= 0x7FFF7FFFu;
+        return *reinterpret_cast<const __nv_bfloat162*>(&w);
+    };
+    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(two(v.x), two(v.y)), __hmax2_nan(two(v.z), two(v.w)));
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&m);
+    return max(w & 0xFFFFu, w >> 16);                    // (magnitudes: their bits are ordered as they are)
 }
 
 // A warp takes kRowsPerWarp rows; lane l holds the 8-column pieces l and l + 32 of a row's value columns, four lanes a group.
@@ -61,13 +85,12 @@ quantize_q4_kernel(const uint4* __restrict__ x, int64_t n, uint8_t* __restrict__
         uint8_t* out = cache + dst[u] * kLatentQ4RowBytes;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float amax = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(bf16_at(v[u][h], i)));
-            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+            uint32_t m = abs_max8(v[u][h]);
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+            const float amax = __uint_as_float(m << 16);
             const float s = q4_scale(amax);
-            reinterpret_cast<uint32_t*>(out)[h * 32 + lane] = q4_word(v[u][h], s, __frcp_rn(s));
+            reinterpret_cast<uint32_t*>(out)[h * 32 + lane] = amax <= 7.f * kScaleMax ? q4_word(v[u][h], __frcp_rn(s)) : q4_word_clipped(v[u][h], s);
             if ((lane & 3) == 0)
                 reinterpret_cast<uint16_t*>(out + kLatentQ4ScaleOff)[h * 8 + (lane >> 2)] = static_cast<uint16_t>(__float_as_uint(s) >> 16);
         }
@@ -107,23 +130,43 @@ dequantize_q4_kernel(const uint8_t* __restrict__ cache, int64_t cache_rows, cons
 
 // ---------------------------------------------------------------- compaction
 // Row j of sequence b of the destination <- row keep[b][j] of sequence b of the source, j < n_keep[b], in units of T.
-// Out of place the moves are independent.
+// Out of place the moves are independent: a block takes 1024 consecutive units of a sequence's rows, four a thread, whose four loads are in
+// flight together.
+constexpr int kCopyUnits = 1024;
 template <typename T>
 __global__ void __launch_bounds__(256)
-compact_copy_kernel(const T* __restrict__ src, T* __restrict__ dst, int units, int64_t src_rows, int64_t dst_rows,
+compact_copy_kernel(const T* __restrict__ src, T* __restrict__ dst, uint32_t units, int64_t src_rows, int64_t dst_rows,
                     const int64_t* __restrict__ src_base, const int64_t* __restrict__ dst_base, const int32_t* __restrict__ keep, int ld_keep,
                     const int32_t* __restrict__ n_keep) {
     const int b = blockIdx.y;
     const int n = min(max(__ldg(n_keep + b), 0), ld_keep);
     const int64_t sb = __ldg(src_base + b), db = __ldg(dst_base + b);
     const int64_t total = static_cast<int64_t>(n) * units;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
-        const int j = static_cast<int>(i / units);
-        const int u = static_cast<int>(i - static_cast<int64_t>(j) * units);
-        const int64_t k = __ldg(keep + static_cast<int64_t>(b) * ld_keep + j);
-        const int64_t s = sb + k, d = db + j;
-        if (k < 0 || s < 0 || s >= src_rows || d < 0 || d >= dst_rows) continue;
-        dst[d * units + u] = src[s * units + u];
+    const int32_t* k_row = keep + static_cast<int64_t>(b) * ld_keep;
+    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kCopyUnits; i0 < total; i0 += static_cast<int64_t>(gridDim.x) * kCopyUnits) {
+        const int64_t j0 = i0 / units;                            // one long division a block
+        const uint32_t u0 = static_cast<uint32_t>(i0 - j0 * units);
+        int64_t from[4], to[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t o = u0 + k * 256 + threadIdx.x, dj = o / units, u = o - dj * units;
+            const int64_t j = j0 + dj;
+            from[k] = -1;
+            if (j < n) {
+                const int64_t p = __ldg(k_row + j), s = sb + p, d = db + j;
+                if (p >= 0 && s >= 0 && s < src_rows && d >= 0 && d < dst_rows) {
+                    from[k] = s * units + u;
+                    to[k] = d * units + u;
+                }
+            }
+        }
+        T v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (from[k] >= 0) v[k] = __ldg(src + from[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (from[k] >= 0) dst[to[k]] = v[k];
     }
 }
 
@@ -187,11 +230,11 @@ static cudaError_t compact_as(const void* src, void* dst, int row_bytes, int64_t
         const dim3 grid(static_cast<unsigned>((units + slice - 1) / slice), static_cast<unsigned>(B));
         compact_in_place_kernel<T><<<grid, kMoveThreads, 0, stream>>>(static_cast<T*>(dst), units, slice, dst_rows, src_base, keep, ld_keep, n_keep);
     } else {
-        int64_t blocks = (static_cast<int64_t>(ld_keep) * units + 1023) / 1024;
-        const int64_t cap = 2 * 8 * 148 / B + 1;
+        int64_t blocks = (static_cast<int64_t>(ld_keep) * units + kCopyUnits - 1) / kCopyUnits;
+        const int64_t cap = 16 * 148 / B + 1;
         if (blocks > cap) blocks = cap;
         compact_copy_kernel<T><<<dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(B)), 256, 0, stream>>>(
-            static_cast<const T*>(src), static_cast<T*>(dst), units, src_rows, dst_rows, src_base, dst_base, keep, ld_keep, n_keep);
+            static_cast<const T*>(src), static_cast<T*>(dst), static_cast<uint32_t>(units), src_rows, dst_rows, src_base, dst_base, keep, ld_keep, n_keep);
     }
     return cudaGetLastError();
 }
