@@ -5,8 +5,8 @@
 // half of tensor memory, so scores, softmax and both halves of the output are done tile by tile with nothing saved or read
 // twice. tcgen05.mma with M = 64 puts row r on TMEM lane 32 (r / 16) + r % 16 (+ 16 with a lane offset of 16, measured), so
 // the two 256-column halves of O lie on top of each other in 256 columns. M = 64 issues at half the M = 128 rate (N = 64: 32
-// clocks, N = 256: 128), 2176 clocks of tensor pipe per 64-row tile; more than 64 query rows take two CTAs that walk
-// the same tiles side by side, the second reading them from the L2.
+// clocks, N = 256: 128), 2176 clocks of tensor pipe per 64-row tile. More than 64 query rows take a pair of CTAs
+// (latent_attn_pair.cu); what surrounds both kernels, the workspace, the count of selected tiles and the merge, is here.
 //
 // Work: the tiles of all sequences, laid end to end, are cut into equal runs, one per CTA (pair). A run may start and end
 // inside a sequence: such a piece leaves a normalised fp32 result and its log-sum-exp in the workspace, and a merge kernel
@@ -349,7 +349,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         };
         // the piece that the fetches are in runs ahead of the one whose tiles are stored
         Walk ahead = walk;
-        Piece apc;
+        Piece apc{};
         int ai = 0;
         bool more = false;
         auto ahead_piece = [&]() {
@@ -576,8 +576,8 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             for (int h = 0; h < 2; ++h) {
                 l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 1);
                 l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 2);
-                inv[h] = l[h] > 0.f ? 1.f / l[h] : 0.f;
-                lse[h] = l[h] > 0.f ? (m_ref[h] + log2f(l[h])) * 0.6931471805599453f : -INFINITY;
+                inv[h] = l[h] != 0.f ? 1.f / l[h] : 0.f;              // 0: the row saw nothing; a sum that is no number stays none
+                lse[h] = l[h] != 0.f ? (m_ref[h] + log2f(l[h])) * 0.6931471805599453f : -INFINITY;
             }
             const float i0 = __shfl_sync(0xFFFFFFFFu, inv[0], (lane & 7) * 4), i1 = __shfl_sync(0xFFFFFFFFu, inv[1], (lane & 7) * 4);
             const float f = (lane & 8) ? i1 : i0;
@@ -694,9 +694,14 @@ latent_merge_kernel(const Params p) {
             v[j] = in ? reinterpret_cast<const float4*>(p.part_out + at * 512)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         float top = m;
+        bool none = m == -INFINITY;                           // (fmaxf passes over what is no number; the weights do not)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, ls[j]);
-        if (top == -INFINITY) continue;
+        for (int j = 0; j < 8; ++j) {
+            top = fmaxf(top, ls[j]);
+            none = none && ls[j] == -INFINITY;
+        }
+        if (none) continue;
+        if (top == -INFINITY) top = 0.f;
         const float f = exp2_fast((m - top) * 1.4426950408889634f);
         m = top;
         z *= f;
@@ -708,10 +713,10 @@ latent_merge_kernel(const Params p) {
             z += w;
         }
     }
-    const float inv = z > 0.f ? 1.f / z : 0.f;
+    const float inv = z != 0.f ? 1.f / z : 0.f;
     const int64_t out_row = static_cast<int64_t>(seq) * seq_rows + r_seq;
     reinterpret_cast<uint2*>(p.out + out_row * 512)[c] = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-    if (p.lse && c == 0) p.lse[out_row] = z > 0.f ? m + logf(z) : -INFINITY;
+    if (p.lse && c == 0) p.lse[out_row] = z != 0.f ? m + logf(z) : -INFINITY;
 }
 
 }  // namespace

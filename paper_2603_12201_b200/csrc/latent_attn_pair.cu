@@ -674,7 +674,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             if (!ok) break;
             tcgen05_fence_after_sync();
             l += swap[(2 * 4 + (q ^ 2)) * 32 + lane];
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const float inv = l != 0.f ? 1.f / l : 0.f;                   // 0: the row saw nothing; a sum that is no number stays none
             const int64_t at_row = seq * seq_rows + r0 + row;
             const int64_t slot = ((static_cast<int64_t>(group) * 2 + (pc.t0 == 0 ? 1 : 0)) * 2 + rank) * kRows + row;
             // P's buffers are free now, and until both warps of a row have met at the next tile: a quarter for each warp to turn its rows in
@@ -720,7 +720,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(in_first(bar_o_free));
             if (half == 0 && row < n_rows) {
-                const float lse = l > 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                const float lse = l != 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
                 if (!pc.whole) p.part_lse[slot] = lse;
                 else if (p.lse) p.lse[at_row] = lse;
             }

@@ -1,0 +1,108 @@
+"""Latent-cache operators at the edges: scores that are no numbers, rows of sums too long for shared memory, pairs whose second half is empty."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import latent as oracle
+from tests.latent_util import bf16_rows, cache_rows, check_attention, oracle_sequence, q4_rows
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def idxc():
+    from paper_2603_12201_b200 import binding
+    return binding
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def set_nan(kv, row):
+    """A positional column of a cache row becomes NaN: its score is none for every head, its values stay what they are."""
+    if kv.dtype == torch.uint8:
+        kv[row, 288 + 2 * 5 + 1] = 0x7F
+        kv[row, 288 + 2 * 5] = 0xC0
+    else:
+        kv[row, 512 + 5] = float("nan")
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H", [16, 128])
+@pytest.mark.parametrize("lens,at", [([40, 70], 10), ([9000, 300], 0), ([9000, 300], 8999), ([64 * 300, 65], 9001)])
+def test_a_visible_row_that_is_no_number_shows(idxc, lens, at, H, four):
+    """In whichever piece of a cut sequence it lies; the other sequence does not notice."""
+    g = gen(lens[0] + at + H)
+    kv = cache_rows(sum(lens), four, g)
+    set_nan(kv, at)
+    q = bf16_rows(2 * H, g, 0.5).view(2, 1, H, 576)
+    base = torch.tensor([0, lens[0]], device=DEV)
+    out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), base, torch.tensor(lens, dtype=torch.int32, device=DEV), max(lens), 512, 1 / 24)
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    check_attention(out[1].reshape(H, 512), lse[1].reshape(H), *oracle_sequence(q[1], kv, lens[0], lens[1], 1, 1 / 24)[:4])
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H,head", [(16, 3), (128, 0), (128, 127), (100, 64)])
+def test_a_head_that_is_no_number_shows_alone(idxc, H, head, four):
+    n = 5000
+    g = gen(H + head)
+    kv = cache_rows(n, four, g)
+    q = bf16_rows(H, g, 0.5).view(1, 1, H, 576)
+    clean = q.clone()
+    q[0, 0, head, 100] = float("nan")
+    out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), None, torch.tensor([n], dtype=torch.int32, device=DEV), n, 512, 1 / 24)
+    assert torch.isnan(out[0, 0, head]).all() and torch.isnan(lse[0, 0, head])
+    others = [h for h in range(H) if h != head]
+    want = oracle_sequence(clean[0], kv, 0, n, 1, 1 / 24)[:4]
+    check_attention(out[0, 0, others], lse[0, 0, others], *(w[others] for w in want))
+
+
+def test_a_selected_row_that_is_no_number_shows(idxc):
+    g = gen(5)
+    kv = q4_rows(3000, g)
+    set_nan(kv, 1234)
+    for H, k_top in ((128, 2048), (16, 100)):
+        q = bf16_rows(2 * H, g, 0.5).view(2, H, 576)
+        topk = torch.stack([torch.arange(k_top), torch.arange(k_top)]).to(torch.int32)
+        topk[0, k_top - 1] = 1234
+        topk[1][topk[1] == 1234] = -1
+        out, lse = idxc.sparse_attention_q4(q.to(DEV), kv.to(DEV), topk.to(DEV), 512, 1 / 24)
+        assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+        assert torch.isfinite(out[1].float()).all() and torch.isfinite(lse[1]).all()
+        rows = topk[1][topk[1] >= 0].long()
+        sub = kv[rows]
+        check_attention(out[1], lse[1], *oracle_sequence(q[1:2], sub, 0, len(rows), 1, 1 / 24)[:4])
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H,n_step", [(50, 3), (65, 1), (33, 4), (128, 3), (43, 3)])
+def test_rows_that_end_inside_the_first_half_of_a_pair(idxc, H, n_step, four):
+    """H n_step = 150, 65, 132, 384, 129: the last pair of a sequence has its second 64 rows in part or not at all."""
+    lens = [700, 1, 130]
+    g = gen(H)
+    kv = cache_rows(sum(lens), four, g)
+    q = bf16_rows(3 * n_step * H, g, 0.5).view(3, n_step, H, 576)
+    base = torch.tensor(np.concatenate([[0], np.cumsum(lens)[:-1]]), device=DEV)
+    out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), base, torch.tensor(lens, dtype=torch.int32, device=DEV), max(lens), 512, 1 / 24)
+    for b, n in enumerate(lens):
+        check_attention(out[b].reshape(-1, 512), lse[b].reshape(-1), *oracle_sequence(q[b], kv, int(base[b]), n, n_step, 1 / 24)[:4], f"sequence {b}")
+
+
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal"])
+def test_select_in_rows_longer_than_shared_memory_holds(idxc, kind):
+    """Above 8 x 49152 positions a sequence the keys are read from global memory in every pass."""
+    ld, lens, budget, recent = 500001, [500001, 393217, 400000, 77], 70001, 333
+    rng = np.random.default_rng(11)
+    acc = {"spread": rng.random((4, ld)) ** 12, "ties": rng.integers(0, 5, (4, ld)) / 4.0, "equal": np.full((4, ld), 0.25)}[kind].astype(np.float32)
+    keep = torch.full((4, budget), -77, dtype=torch.int32, device=DEV)
+    new = torch.full((4,), -77, dtype=torch.int32, device=DEV)
+    idxc.evict_select(torch.from_numpy(acc).to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), budget, recent, keep, new)
+    for b, n in enumerate(lens):
+        want = oracle.evict(acc[b], n, budget, recent)
+        m = len(want)
+        assert int(new[b]) == m
+        assert np.array_equal(keep[b, :m].cpu().numpy(), want)
+        assert (keep[b, m:] == -1).all()
