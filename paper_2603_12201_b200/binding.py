@@ -385,21 +385,30 @@ _NO_GUARD = contextlib.nullcontext()
 def _launch_on(stream, **tensors):
     """Checks that the tensors (None allowed, not the first) are contiguous CUDA tensors of one device and returns (guard, raw
     stream): inside the guard that device is current and so is the stream, which is the device's current one unless given."""
-    device = None
+    index = None
     for name, t in tensors.items():
         if t is None:
             continue
-        if device is None:
-            device = t.device
-        if t.device != device or device.type != "cuda" or not t.is_contiguous():
+        if index is None:
+            index = t.get_device()                               # (-1: not on a GPU)
+        if index < 0 or t.get_device() != index or not t.is_contiguous():
             _dev(t, name)
-            raise ValueError(f"{name} is on {t.device}, the other tensors are on {device}")
+            raise ValueError(f"{name} is on {t.device}, the other tensors are on cuda:{index}")
     if stream is not None:
-        if stream.device != device:
-            raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+        if stream.device.index != index:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on cuda:{index}")
         return torch.cuda.stream(stream), stream.cuda_stream
-    raw = torch._C._cuda_getCurrentRawStream(device.index)       # (torch.cuda.current_stream builds an object: 2 us a call)
-    return (_NO_GUARD if torch.cuda.current_device() == device.index else torch.cuda.device(device)), raw
+    raw = torch._C._cuda_getCurrentRawStream(index)              # (torch.cuda.current_stream builds an object: 2 us a call)
+    return (_NO_GUARD if torch.cuda.current_device() == index else torch.cuda.device(index)), raw
+
+
+def _new(shape, dtype, device):
+    """torch.empty of a contiguous shape, a microsecond faster."""
+    strides, n = [], 1
+    for k in reversed(shape):
+        strides.append(n)
+        n *= max(k, 1)
+    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
 
 
 def _at(t):
@@ -422,10 +431,6 @@ def _latent_format(kv) -> int:
     if kv.dim() == 2 and kv.dtype == torch.uint8 and kv.shape[1] == Q4_ROW_BYTES:
         return LATENT_Q4
     raise ValueError(f"kv must be [n_kv, 576] bfloat16 or [n_kv, {Q4_ROW_BYTES}] uint8, got {list(kv.shape)} {kv.dtype}")
-
-
-def _nbytes(t):
-    return t.numel() * t.element_size()
 
 
 def quantize_q4(x, cache_out, dst_rows=None, stream=None):
@@ -458,7 +463,7 @@ def latent_attention_workspace_bytes(B, n_step, max_len, H) -> int:
 
 def _latent_workspace(workspace, B, n_step, max_len, H, device):
     if workspace is None:
-        workspace = alloc_workspace(latent_attention_workspace_bytes(B, n_step, max_len, H), device)
+        workspace = _new((max(latent_attention_workspace_bytes(B, n_step, max_len, H), 256),), torch.uint8, device)
     return workspace
 
 
@@ -476,11 +481,11 @@ def latent_attention(q, kv, kv_base, lens, max_len, d_v, scale, want_lse=True, o
     _typed(out, "out", torch.bfloat16, (B, n_step, H, d_v))
     with guard:
         if out is None:
-            out = torch.empty((B, n_step, H, d_v), dtype=torch.bfloat16, device=q.device)
-        lse = torch.empty((B, n_step, H), dtype=torch.float32, device=q.device) if want_lse else None
+            out = _new((B, n_step, H, d_v), torch.bfloat16, q.device)
+        lse = _new((B, n_step, H), torch.float32, q.device) if want_lse else None
         workspace = _latent_workspace(workspace, B, n_step, max_len, H, q.device)
         _check(lib().idxc_latent_attention(_at(q), _at(kv), fmt, kv.shape[0], _at(kv_base), _at(lens), B, n_step, int(max_len), H, d_qk,
-                                           int(d_v), float(scale), _at(out), _at(lse), _at(workspace), _nbytes(workspace),
+                                           int(d_v), float(scale), _at(out), _at(lse), _at(workspace), workspace.nbytes,
                                            stream), "idxc_latent_attention")
     return out, lse
 
@@ -497,11 +502,11 @@ def sparse_attention_q4(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, ou
     _typed(out, "out", torch.bfloat16, (n_q, H, d_v))
     with guard:
         if out is None:
-            out = torch.empty((n_q, H, d_v), dtype=torch.bfloat16, device=q.device)
-        lse = torch.empty((n_q, H), dtype=torch.float32, device=q.device) if want_lse else None
+            out = _new((n_q, H, d_v), torch.bfloat16, q.device)
+        lse = _new((n_q, H), torch.float32, q.device) if want_lse else None
         workspace = _latent_workspace(workspace, n_q, 1, k_top, H, q.device)
         _check(lib().idxc_sparse_attention_q4(_at(q), _at(kv), _at(topk), _at(kv_base), n_q, kv.shape[0], H, d_qk, int(d_v), k_top,
-                                              float(scale), _at(out), _at(lse), _at(workspace), _nbytes(workspace),
+                                              float(scale), _at(out), _at(lse), _at(workspace), workspace.nbytes,
                                               stream), "idxc_sparse_attention_q4")
     return out, lse
 

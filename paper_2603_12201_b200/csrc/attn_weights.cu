@@ -13,7 +13,7 @@ namespace idxc {
 using namespace latent;
 namespace {
 
-constexpr int kWTile = 128;                          // cache rows of a tile
+constexpr int kWTile = 128;                          // cache rows of a tile (2^7)
 constexpr int kWRows = 128;                          // query rows of a launch at most
 constexpr int kRing = 4;
 constexpr uint32_t kRingBytes = kWTile * 128;
@@ -76,6 +76,8 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     };
     auto seq_base = [&](uint32_t b) -> int64_t { return p.a.kv_base ? __ldg(p.a.kv_base + b) : 0; };
 
+    const EarlyTiles early = early_tiles(p.units, p.tiles);
+    early_bases(p.a.kv_base, p.a.B);
     if (threadIdx.x == 0) {
         mbar_init(bar_q_full, 1);
         mbar_init(bar_q_empty, 1);
@@ -95,7 +97,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         tmem_relinquish_alloc_permit();
     }
     tcgen05_fence_before_sync();
-    const Run run = find_run(p.units, p.tiles, blockIdx.x, p.groups, reinterpret_cast<int*>(tab));
+    const Run run = find_run(p.units, p.tiles, early, blockIdx.x, p.groups, reinterpret_cast<int*>(tab));
     __syncthreads();
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = *tmem_base_slot;
@@ -340,7 +342,7 @@ cudaError_t launch_attn_weights(const LatentArgs& a, int row0, const float* lse,
     const int rows = attn_weights_rows(a.n_step, a.H, row0);
     const int64_t tiles = a.B * ((a.max_len + kWTile - 1) / kWTile);
     const int groups = static_cast<int>(tiles < sm_count ? tiles : sm_count);
-    const UnitTiles ut{nullptr, a.lens, a.max_len, 1, kWTile};
+    const UnitTiles ut{nullptr, a.lens, a.max_len, 1, 7};
     const WParams p{a, ut, static_cast<uint32_t>(a.B), groups, row0, rows, static_cast<uint32_t>((rows + 15) / 16 * 16), a.scale * 1.4426950408889634f,
                     lse, beta, acc, ld, status};
     auto go = [&](auto kernel, int threads) -> cudaError_t {

@@ -11,6 +11,22 @@ namespace idxc {
 // Raises a kernel's dynamic shared-memory limit to `bytes` once per (kernel, device); thread-safe (api.cu).
 cudaError_t ensure_max_dynamic_smem(const void* kernel, int bytes);
 
+// Launches a kernel that may start while the kernel before it in the stream still runs, and waits for it itself (wait_for_previous).
+template <typename... Params, typename... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const Args&... args) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Row-wise top-k select (topk.cu). Row r has length lens[r] (device) if lens != nullptr,
 // else first_len + r * len_step, clamped to [0, ld]. row_mask: nullptr, or one byte per row: rows whose byte is 0 are
 // left alone (neither read nor written). launches: if given, receives the number of kernels launched (rows whose lengths

@@ -48,6 +48,7 @@ constexpr int kSlotWarps = 4;                       // warps that fill a slot (4
 __global__ void __launch_bounds__(128)
 latent_count_kernel(const LatentArgs a, int32_t* __restrict__ tiles) {
     __shared__ int s_last[4];
+    let_next_start();
     const int64_t t = blockIdx.x;
     const int64_t base = a.kv_base ? __ldg(a.kv_base + t) : 0;
     const int32_t* row = a.topk + t * a.k_top;
@@ -103,6 +104,15 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         return p.a.topk ? p.a.k_top : min(max(static_cast<int64_t>(__ldg(p.a.lens + seq)), int64_t(0)), p.a.max_len);
     };
 
+    let_next_start();                                        // the merge
+    EarlyTiles early{};
+    if (!p.tiles.counted) early = early_tiles(p.units, p.tiles);
+    early_bases(p.a.kv_base, p.a.B);
+    if (lane == 0 && warp == 2) tma_prefetch_desc(&q_map);
+    if (!Q4 && lane == 0 && warp == 3) {
+        tma_prefetch_desc(&rope_map);
+        tma_prefetch_desc(&v_map);
+    }
     if (threadIdx.x == 0) {
         mbar_init(bar_q_full, 1);
         mbar_init(bar_q_empty, 1);
@@ -126,7 +136,11 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         tmem_relinquish_alloc_permit();
     }
     tcgen05_fence_before_sync();
-    const Run run = find_run(p.units, p.tiles, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
+    if (p.tiles.counted) {
+        wait_for_previous();
+        early = early_tiles(p.units, p.tiles);
+    }
+    const Run run = find_run(p.units, p.tiles, early, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
     if (threadIdx.x == 0) {
         p.starts[group] = make_int2(static_cast<int>(run.unit), run.t);
         p.runs[group] = run.first;
@@ -225,7 +239,6 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     } else if (warp == 2) {
         // ------------------------------------------------------------ Q
         if (lane == 0) {
-            tma_prefetch_desc(&q_map);
             int before = 0;                                  // tiles of the piece before
             while (ok && walk.next(pc)) {
                 rows_of(pc.unit, seq, r0);
@@ -241,10 +254,6 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
     } else if (!Q4 && warp == 3) {
         // ------------------------------------------------------------ bf16 rows
-        if (lane == 0) {
-            tma_prefetch_desc(&rope_map);
-            tma_prefetch_desc(&v_map);
-        }
         uint32_t tails = 0;
         while (ok && walk.next(pc)) {
             rows_of(pc.unit, seq, r0);
@@ -652,6 +661,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 // takes rows 4y .. 4y + 3 of the unit that group g is the first to start inside of; 128 threads a row, 4 columns each.
 __global__ void __launch_bounds__(512)
 latent_merge_kernel(const Params p) {
+    wait_for_previous();
     const int g = blockIdx.x;
     const int2 s = p.starts[g];
     const int run = p.runs[g], run_end = p.runs[g + 1];
@@ -769,7 +779,7 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     int32_t* tiles = reinterpret_cast<int32_t*>(ws + y.tiles_off);
     int2* starts = reinterpret_cast<int2*>(ws + y.starts_off);
     int32_t* runs = reinterpret_cast<int32_t*>(ws + y.runs_off);
-    const UnitTiles unit_tiles{a.topk ? tiles : nullptr, a.lens, a.max_len, static_cast<uint32_t>(y.blocks_per_seq), kTile};
+    const UnitTiles unit_tiles{a.topk ? tiles : nullptr, a.lens, a.max_len, static_cast<uint32_t>(y.blocks_per_seq), 6};
     const Params p{a, unit_tiles, starts, runs, static_cast<uint32_t>(y.units), y.blocks_per_seq, y.ways, y.groups, a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f,
                    a.scale > 0.f ? 1.f : (a.scale < 0.f ? -1.f : 0.f), static_cast<__nv_bfloat16*>(out), lse,
                    reinterpret_cast<float*>(ws + y.out_off), reinterpret_cast<float*>(ws + y.lse_off), status};
@@ -785,16 +795,16 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     } else {
         const void* k = a.q4 ? reinterpret_cast<const void*>(latent_attn_kernel<true>) : reinterpret_cast<const void*>(latent_attn_kernel<false>);
         if ((e = ensure_max_dynamic_smem(k, kSmemBytes)) != cudaSuccess) return e;
-        if (a.q4) latent_attn_kernel<true><<<y.groups, kWarpsQ4 * 32, kSmemBytes, stream>>>(maps.q, maps.rope, maps.v, p);
+        if (a.topk) e = launch_behind(latent_attn_kernel<true>, y.groups, kWarpsQ4 * 32, kSmemBytes, stream, maps.q, maps.rope, maps.v, p);
+        else if (a.q4) latent_attn_kernel<true><<<y.groups, kWarpsQ4 * 32, kSmemBytes, stream>>>(maps.q, maps.rope, maps.v, p);
         else latent_attn_kernel<false><<<y.groups, kWarpsBf16 * 32, kSmemBytes, stream>>>(maps.q, maps.rope, maps.v, p);
-        e = cudaGetLastError();
+        if (!a.topk) e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
     if (y.groups > 1) {
         ++*launches;
         const int unit_rows = a.n_step * a.H < y.ways * kRows ? a.n_step * a.H : y.ways * kRows;
-        latent_merge_kernel<<<dim3(static_cast<unsigned>(y.groups), static_cast<unsigned>((unit_rows + 3) / 4)), 512, 0, stream>>>(p);
-        e = cudaGetLastError();
+        e = launch_behind(latent_merge_kernel, dim3(static_cast<unsigned>(y.groups), static_cast<unsigned>((unit_rows + 3) / 4)), 512, 0, stream, p);
     }
     return e;
 }

@@ -10,7 +10,7 @@
 namespace idxc {
 namespace latent {
 
-constexpr int kTile = 64;                           // cache rows of a tile
+constexpr int kTile = 64;                           // cache rows of a tile (2^6)
 constexpr int kRows = 64;                           // query rows of a CTA
 constexpr int kBlocks = 9;                          // 64-column blocks of a row
 // A loader of Q waits while the piece before is worked on: its bound grows with that piece (a tile takes a few thousand cycles).
@@ -23,11 +23,11 @@ struct UnitTiles {
     const int32_t* lens;
     int64_t max_len;
     uint32_t blocks_per_seq;     // units of a sequence
-    int tile;                    // rows of a tile
+    int tile_log2;               // rows of a tile
     __device__ __forceinline__ int operator()(uint32_t unit) const {
-        if (counted) return __ldg(counted + unit);
-        const int64_t len = lens ? __ldg(lens + unit / blocks_per_seq) : max_len;
-        return static_cast<int>((min(max(len, int64_t(0)), max_len) + tile - 1) / tile);
+        if (counted) return *static_cast<const volatile int32_t*>(counted + unit);      // (not __ldg: written while this kernel may already run)
+        const int most = static_cast<int>(max_len), len = lens ? __ldg(lens + unit / blocks_per_seq) : most;      // (max_len <= 2^30)
+        return (min(max(len, 0), most) + (1 << tile_log2) - 1) >> tile_log2;
     }
 };
 
@@ -62,19 +62,41 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // ---------------------------------------------------------------- the run of a group, and its walk over it
 // The tiles of all units, laid end to end, are cut into `groups` runs of equal length (to within one). Every CTA finds its own by a
 // scan over the units, which costs about a microsecond where a kernel of its own before this one costs five.
+// Up to 128 units every warp does that by itself, four units a lane, without a barrier: their loads (early_tiles) are under way while the
+// CTA sets itself up.
+constexpr uint32_t kFewUnits = 128;
+struct EarlyTiles { int n[4]; };
+__device__ __forceinline__ EarlyTiles early_tiles(uint32_t units, const UnitTiles& tiles) {
+    const uint32_t first = 4 * (threadIdx.x & 31);
+    EarlyTiles e;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e.n[k] = units <= kFewUnits && first + k < units ? tiles(first + k) : 0;
+    return e;
+}
+// Brings the first 4 KB of kv_base to the L1 (every role loads its sequence's when it starts).
+__device__ __forceinline__ void early_bases(const int64_t* kv_base, int64_t B) {
+    const int64_t at = 16 * static_cast<int64_t>(threadIdx.x & 31);
+    if (kv_base != nullptr && at < B) {
+        int64_t x;
+        asm volatile("ld.global.nc.b64 %0, [%1];" : "=l"(x) : "l"(kv_base + at));
+        static_cast<void>(x);
+    }
+}
 struct Run {
     uint32_t unit;        // where it begins
     int t;
     int first, n, total;  // first tile end to end, number of tiles, tiles of all units
 };
-__device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, int group, int groups, int* scratch /* shared, 40 words */) {
+__device__ __forceinline__ void cut_run(Run& r, int group, int groups) {
+    const int each = r.total / groups, more = r.total - each * groups;       // the first `more` runs have one tile more
+    r.first = group * each + min(group, more);
+    r.n = each + (group < more ? 1 : 0);
+}
+__device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, const EarlyTiles& early, int group, int groups,
+                                        int* scratch /* shared, 40 words */) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-    if (units <= 128) {                              // few units: every warp by itself, four units a lane, no barrier (3700 -> 2900 clocks)
-        int n[4], sum = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) n[k] = 4 * lane + k < units ? tiles(4 * lane + k) : 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sum += n[k];
+    if (units <= kFewUnits) {
+        const int sum = (early.n[0] + early.n[1]) + (early.n[2] + early.n[3]);
         int incl = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -83,16 +105,15 @@ __device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, 
         }
         Run r{0, 0, 0, 0, 0};
         r.total = __shfl_sync(0xFFFFFFFFu, incl, 31);
-        r.first = static_cast<int>(static_cast<int64_t>(r.total) * group / groups);
-        r.n = static_cast<int>(static_cast<int64_t>(r.total) * (group + 1) / groups) - r.first;
+        cut_run(r, group, groups);
         int before = incl - sum, unit = -1, t = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (r.first >= before && r.first < before + n[k]) {
+            if (r.first >= before && r.first < before + early.n[k]) {
                 unit = 4 * lane + k;
                 t = r.first - before;
             }
-            before += n[k];
+            before += early.n[k];
         }
         const uint32_t who = __ballot_sync(0xFFFFFFFFu, unit >= 0);
         if (who != 0) {
@@ -114,8 +135,7 @@ __device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, 
     __syncthreads();
     Run r{0, 0, 0, 0, 0};
     for (int w = 0; w < n_warps; ++w) r.total += scratch[w];
-    r.first = static_cast<int>(static_cast<int64_t>(r.total) * group / groups);
-    r.n = static_cast<int>(static_cast<int64_t>(r.total) * (group + 1) / groups) - r.first;
+    cut_run(r, group, groups);
     if (r.n > 0) {                                   // (uniform over the CTA)
         int before_block = 0;
         for (uint32_t u0 = 0; u0 < units; u0 += n_thr) {

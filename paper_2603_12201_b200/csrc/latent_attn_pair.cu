@@ -110,6 +110,16 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     };
     auto in_first = [&](uint32_t bar) -> uint32_t { return map_to_cta(bar, 0); };
 
+    let_next_start();                                        // the merge
+    EarlyTiles early{};
+    if (ROWS != kPicked) early = early_tiles(p.units, p.tiles);
+    early_bases(p.a.kv_base, p.a.B);
+    if (lane == 0 && warp == 2) tma_prefetch_desc(&q_map);
+    if (ROWS == kBf16 && lane == 0 && warp == 3) {
+        tma_prefetch_desc(&k_map);
+        tma_prefetch_desc(&rope_map);
+    }
+    if (ROWS == kBf16 && lane == 0 && warp == 8) tma_prefetch_desc(&v_map);
     if (threadIdx.x == 0) {
         mbar_init(bar_q_full, 2);
         for (int i = 0; i < 2; ++i) {
@@ -136,15 +146,21 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         tmem_relinquish_pair();
     }
     tcgen05_fence_before_sync();
-    const Run run = find_run(p.units, p.tiles, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
+    __syncwarp();
+    cluster_arrive();                                        // the other CTA's barriers are waited for below
+    if (ROWS == kPicked) {                                   // (counted by the kernel before)
+        wait_for_previous();
+        early = early_tiles(p.units, p.tiles);
+    }
+    const Run run = find_run(p.units, p.tiles, early, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
     if (threadIdx.x == 0 && rank == 0) {
         p.starts[group] = make_int2(static_cast<int>(run.unit), run.t);
         p.runs[group] = run.first;
         if (group == p.groups - 1) p.runs[p.groups] = run.total;
     }
     fence_proxy_async_smem();                                // find_run's words before Q's copy over them
-    __syncthreads();
-    cluster_sync();
+    if (p.units > kFewUnits) __syncthreads();
+    cluster_wait();
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = *tmem_base_slot;
 
@@ -218,7 +234,6 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     } else if (warp == 2) {
         // ------------------------------------------------------------ Q
         if (lane == 0) {
-            tma_prefetch_desc(&q_map);
             int before = 0;                                  // tiles of the piece before
             while (ok && walk.next(pc)) {
                 rows_of(pc.unit, seq, r0);
@@ -238,8 +253,6 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         // ------------------------------------------------------------ K, bf16: rows 32 rank .. of every tile. Rows behind the sequence's end
         // may hold anything: they only reach scores that the softmax discards.
         if (lane == 0) {
-            tma_prefetch_desc(&k_map);
-            tma_prefetch_desc(&rope_map);
             while (ok && walk.next(pc)) {
                 const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + pc.unit / static_cast<uint32_t>(p.blocks_per_seq)) : 0;
                 for (int i = 0; i < pc.n && ok; ++i, ++tile) {
@@ -262,7 +275,6 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         }
     } else if (ROWS == kBf16 && warp == 8) {
         // ------------------------------------------------------------ V, bf16: value columns 256 rank .. of every tile
-        if (lane == 0) tma_prefetch_desc(&v_map);
         uint32_t tails = 0;
         while (ok && walk.next(pc)) {
             rows_of(pc.unit, seq, r0);
@@ -748,6 +760,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
 cudaError_t launch_latent_attn_pair(const LatentMaps& maps, const Params& p, cudaStream_t stream) {
     auto go = [&](auto kernel, Rows rows, int warps) -> cudaError_t {
         if (cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), smem_bytes(rows)); e != cudaSuccess) return e;
+        if (rows == kPicked) return launch_behind(kernel, p.groups * 2, warps * 32, smem_bytes(rows), stream, maps.q, maps.k, maps.rope, maps.v, p);
         kernel<<<static_cast<unsigned>(p.groups * 2), warps * 32, smem_bytes(rows), stream>>>(maps.q, maps.k, maps.rope, maps.v, p);
         return cudaGetLastError();
     };
