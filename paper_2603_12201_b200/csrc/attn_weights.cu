@@ -97,7 +97,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
         tmem_relinquish_alloc_permit();
     }
     tcgen05_fence_before_sync();
-    const Run run = find_run(p.units, p.tiles, early, blockIdx.x, p.groups, reinterpret_cast<int*>(tab));
+    const Run run = find_run(p.units, p.tiles, early, blockIdx.x, p.groups, 0, reinterpret_cast<int*>(tab));
     __syncthreads();
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = *tmem_base_slot;

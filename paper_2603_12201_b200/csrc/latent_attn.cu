@@ -41,6 +41,7 @@ static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
 constexpr uint32_t kColS = 256;
 constexpr int kWarpsBf16 = 8;                       // 0 scores | 1 P V | 2 Q | 3 rows (TMA) | 4..7 softmax
 constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 idle | 4..7 softmax | 8..15 rows
+constexpr int kCutTiles = 4;                        // (see find_run) 74 queries of 32 selected tiles: 62 us cut even or apart, 100: 84 us and 103
 constexpr int kSlotWarps = 4;                       // warps that fill a slot (4-bit rows)
 
 // ---------------------------------------------------------------- plan
@@ -140,7 +141,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         wait_for_previous();
         early = early_tiles(p.units, p.tiles);
     }
-    const Run run = find_run(p.units, p.tiles, early, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
+    const Run run = find_run(p.units, p.tiles, early, group, p.groups, kCutTiles, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
     if (threadIdx.x == 0) {
         p.starts[group] = make_int2(static_cast<int>(run.unit), run.t);
         p.runs[group] = run.first;
@@ -658,7 +659,9 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 
 // ---------------------------------------------------------------- merge
 // A unit cut by runs: group g - 1 holds its beginning (slot 1), groups g, g + 1, .. its continuations (slot 0). Block (g, y)
-// takes rows 4y .. 4y + 3 of the unit that group g is the first to start inside of; 128 threads a row, 4 columns each.
+// takes rows 4 (y + k gridDim.y) .. + 3 of the unit that group g is the first to start inside of; 128 threads a row, 4 columns each. As
+// many blocks as run at a time where every unit needs them (32 queries of 2048 rows: 48 us, with a block for every four rows 50 us;
+// one query: 23.7 us, 29 with as many as run at a time of all groups).
 __global__ void __launch_bounds__(512)
 latent_merge_kernel(const Params p) {
     wait_for_previous();
@@ -677,56 +680,56 @@ latent_merge_kernel(const Params p) {
     if (fs.x == s.x && fs.y > 0) return;                      // an earlier group starts inside this unit too
     const int end = run - s.y + p.tiles(static_cast<uint32_t>(s.x));      // one past the unit's last tile, end to end
     const uint32_t seq = static_cast<uint32_t>(s.x) / static_cast<uint32_t>(p.blocks_per_seq);
-    const int seq_rows = p.a.n_step * p.a.H;
-    const int r = blockIdx.y * 4 + (threadIdx.x >> 7), c = threadIdx.x & 127;
-    const int r_seq = static_cast<int>(s.x - seq * p.blocks_per_seq) * p.ways * kRows + r;
-    if (r >= p.ways * kRows || r_seq >= seq_rows) return;
+    const int seq_rows = p.a.n_step * p.a.H, first_row = static_cast<int>(s.x - seq * p.blocks_per_seq) * p.ways * kRows;
+    const int n_rows = min(p.ways * kRows, seq_rows - first_row), c = threadIdx.x & 127;
     const int64_t stride = static_cast<int64_t>(2) * p.ways * kRows;            // rows of a group's two slots
-    const int64_t at1 = first * stride + p.ways * kRows + r, at0 = g * stride + r;
-    float m = -INFINITY, z = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    // piece 0 is the beginning, piece k > 0 group g + k - 1's; eight at a time, all loads of the eight before their first use
-    bool more = true;
-    for (int k0 = 0; more; k0 += 8) {
-        float ls[8];
-        float4 v[8];
+    for (int r = blockIdx.y * 4 + (threadIdx.x >> 7); r < n_rows; r += gridDim.y * 4) {
+        const int64_t at1 = first * stride + p.ways * kRows + r, at0 = g * stride + r;
+        float m = -INFINITY, z = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        // piece 0 is the beginning, piece k > 0 group g + k - 1's; eight at a time, all loads of the eight before their first use
+        bool more = true;
+        for (int k0 = 0; more; k0 += 8) {
+            float ls[8];
+            float4 v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int k = k0 + j, grp = g + k - 1;
-            bool in = k == 0;
-            if (k > 0) {
-                const int b0 = grp < p.groups ? p.runs[grp] : end;
-                more = b0 < end;
-                in = more && p.runs[grp + 1] > b0;
+            for (int j = 0; j < 8; ++j) {
+                const int k = k0 + j, grp = g + k - 1;
+                bool in = k == 0;
+                if (k > 0) {
+                    const int b0 = grp < p.groups ? p.runs[grp] : end;
+                    more = b0 < end;
+                    in = more && p.runs[grp + 1] > b0;
+                }
+                const int64_t at = k == 0 ? at1 : at0 + (k - 1) * stride;
+                ls[j] = in ? p.part_lse[at] : -INFINITY;
+                v[j] = in ? reinterpret_cast<const float4*>(p.part_out + at * 512)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            const int64_t at = k == 0 ? at1 : at0 + (k - 1) * stride;
-            ls[j] = in ? p.part_lse[at] : -INFINITY;
-            v[j] = in ? reinterpret_cast<const float4*>(p.part_out + at * 512)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        float top = m;
-        bool none = m == -INFINITY;                           // (fmaxf passes over what is no number; the weights do not)
+            float top = m;
+            bool none = m == -INFINITY;                       // (fmaxf passes over what is no number; the weights do not)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            top = fmaxf(top, ls[j]);
-            none = none && ls[j] == -INFINITY;
-        }
-        if (none) continue;
-        if (top == -INFINITY) top = 0.f;
-        const float f = exp2_fast((m - top) * 1.4426950408889634f);
-        m = top;
-        z *= f;
-        acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+            for (int j = 0; j < 8; ++j) {
+                top = fmaxf(top, ls[j]);
+                none = none && ls[j] == -INFINITY;
+            }
+            if (none) continue;
+            if (top == -INFINITY) top = 0.f;
+            const float f = exp2_fast((m - top) * 1.4426950408889634f);
+            m = top;
+            z *= f;
+            acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float w = exp2_fast((ls[j] - top) * 1.4426950408889634f);
-            acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
-            z += w;
+            for (int j = 0; j < 8; ++j) {
+                const float w = exp2_fast((ls[j] - top) * 1.4426950408889634f);
+                acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
+                z += w;
+            }
         }
+        const float inv = z != 0.f ? 1.f / z : 0.f;
+        const int64_t out_row = static_cast<int64_t>(seq) * seq_rows + first_row + r;
+        reinterpret_cast<uint2*>(p.out + out_row * 512)[c] = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+        if (p.lse && c == 0) p.lse[out_row] = z != 0.f ? m + logf(z) : -INFINITY;
     }
-    const float inv = z != 0.f ? 1.f / z : 0.f;
-    const int64_t out_row = static_cast<int64_t>(seq) * seq_rows + r_seq;
-    reinterpret_cast<uint2*>(p.out + out_row * 512)[c] = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-    if (p.lse && c == 0) p.lse[out_row] = z != 0.f ? m + logf(z) : -INFINITY;
 }
 
 }  // namespace
@@ -804,7 +807,9 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     if (y.groups > 1) {
         ++*launches;
         const int unit_rows = a.n_step * a.H < y.ways * kRows ? a.n_step * a.H : y.ways * kRows;
-        e = launch_behind(latent_merge_kernel, dim3(static_cast<unsigned>(y.groups), static_cast<unsigned>((unit_rows + 3) / 4)), 512, 0, stream, p);
+        const int64_t busy = y.units < y.groups ? y.units : y.groups;          // groups that may have a unit to merge
+        const int64_t at_once = 4 * sm_count / busy, blocks = (unit_rows + 3) / 4;
+        e = launch_behind(latent_merge_kernel, dim3(static_cast<unsigned>(y.groups), static_cast<unsigned>(blocks < at_once ? blocks : at_once)), 512, 0, stream, p);
     }
     return e;
 }

@@ -60,7 +60,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 // ---------------------------------------------------------------- the run of a group, and its walk over it
-// The tiles of all units, laid end to end, are cut into `groups` runs of equal length (to within one). Every CTA finds its own by a
+// The tiles of all units, laid end to end, are cut into `groups` runs, as a rule of equal length (to within one). Every CTA finds its own by a
 // scan over the units, which costs about a microsecond where a kernel of its own before this one costs five.
 // Up to 128 units every warp does that by itself, four units a lane, without a barrier: their loads (early_tiles) are under way while the
 // CTA sets itself up.
@@ -88,15 +88,19 @@ struct Run {
     int first, n, total;  // first tile end to end, number of tiles, tiles of all units
 };
 __device__ __forceinline__ void cut_run(Run& r, int group, int groups) {
-    const int each = r.total / groups, more = r.total - each * groups;       // the first `more` runs have one tile more
-    r.first = group * each + min(group, more);
-    r.n = each + (group < more ? 1 : 0);
+    const int each = r.total / groups, more = r.total - each * groups;       // total * group / groups without 64-bit divisions
+    r.first = each * group + more * group / groups;
+    r.n = each * (group + 1) + more * (group + 1) / groups - r.first;
 }
-__device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, const EarlyTiles& early, int group, int groups,
+// `cut_tiles`: what a run that begins or ends inside a unit costs more than one that does not, in tiles (its output goes out in fp32
+// and through the merge). Few units that are alike are therefore not cut evenly: with s = groups / units >= 1 each unit is cut by itself into s
+// runs, with s = 0 a run takes whole units, where the longest such run is no longer than an even one and that.
+__device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, const EarlyTiles& early, int group, int groups, int cut_tiles,
                                         int* scratch /* shared, 40 words */) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
     if (units <= kFewUnits) {
         const int sum = (early.n[0] + early.n[1]) + (early.n[2] + early.n[3]);
+        const int longest = __reduce_max_sync(0xFFFFFFFFu, max(max(early.n[0], early.n[1]), max(early.n[2], early.n[3])));
         int incl = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -105,6 +109,34 @@ __device__ __forceinline__ Run find_run(uint32_t units, const UnitTiles& tiles, 
         }
         Run r{0, 0, 0, 0, 0};
         r.total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+        // first tile of unit u, end to end, and its tiles
+        auto unit_at = [&](int u, int& n) -> int {
+            const int k = u & 3;
+            const int mine = incl - sum + (k > 0 ? early.n[0] : 0) + (k > 1 ? early.n[1] : 0) + (k > 2 ? early.n[2] : 0);
+            n = __shfl_sync(0xFFFFFFFFu, k == 0 ? early.n[0] : (k == 1 ? early.n[1] : (k == 2 ? early.n[2] : early.n[3])), (u >> 2) & 31);
+            return u < 4 * 32 ? __shfl_sync(0xFFFFFFFFu, mine, (u >> 2) & 31) : r.total;
+        };
+        const int n_units = static_cast<int>(units), s = groups / n_units;
+        const long long apart = s > 0 ? (longest + s - 1) / s : static_cast<long long>((n_units + groups - 1) / groups) * longest;
+        if (apart <= r.total / groups + cut_tiles) {
+            int n, n_end;
+            if (s > 0) {
+                const int u = group / s, p = group - u * s;
+                const int at = unit_at(min(u, n_units - 1), n);
+                const int t0 = static_cast<int>(static_cast<uint32_t>(n) * p / s), t1 = static_cast<int>(static_cast<uint32_t>(n) * (p + 1) / s);
+                const bool idle = u >= n_units;
+                r.unit = idle ? 0 : static_cast<uint32_t>(u);
+                r.t = idle ? 0 : t0;
+                r.first = idle ? r.total : at + t0;
+                r.n = idle ? 0 : t1 - t0;
+            } else {
+                const int u0 = group * n_units / groups, u1 = (group + 1) * n_units / groups;
+                r.unit = static_cast<uint32_t>(u0);
+                r.first = unit_at(u0, n);
+                r.n = unit_at(u1, n_end) - r.first;
+            }
+            return r;
+        }
         cut_run(r, group, groups);
         int before = incl - sum, unit = -1, t = 0;
 #pragma unroll

@@ -35,6 +35,7 @@ constexpr uint32_t kBarBytes = 512;
 constexpr uint32_t kSwapBytes = 3 * 4 * 32 * 4;     // what two warps exchange: row maxima, double-buffered, and at the end row sums
 constexpr int kQT = 6;                              // 4-bit rows: Q blocks in tensor memory
 constexpr int kRawSlots = 3;
+constexpr int kCutTiles = 13;                       // (see find_run) 64 queries of 32 selected tiles: 84 us cut even, 65 us apart; 38: 60 us and 65
 constexpr uint32_t kRawBytes = kHalf * kLatentQ4RowBytes;
 enum Rows { kBf16, kCodes, kPicked };               // bf16 rows in order, 4-bit rows in order, selected 4-bit rows
 constexpr uint32_t q_bytes(Rows r) { return (r == kCodes ? kBlocks - kQT : kBlocks) * kRows * 128; }
@@ -152,7 +153,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         wait_for_previous();
         early = early_tiles(p.units, p.tiles);
     }
-    const Run run = find_run(p.units, p.tiles, early, group, p.groups, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
+    const Run run = find_run(p.units, p.tiles, early, group, p.groups, kCutTiles, reinterpret_cast<int*>(q_smem));      // (Q has not been asked for yet)
     if (threadIdx.x == 0 && rank == 0) {
         p.starts[group] = make_int2(static_cast<int>(run.unit), run.t);
         p.runs[group] = run.first;

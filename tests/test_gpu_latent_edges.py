@@ -106,3 +106,22 @@ def test_select_in_rows_longer_than_shared_memory_holds(idxc, kind):
         assert int(new[b]) == m
         assert np.array_equal(keep[b, :m].cpu().numpy(), want)
         assert (keep[b, m:] == -1).all()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H", [8, 72])
+@pytest.mark.parametrize("B,n", [(2, 1700), (30, 300), (37, 500), (38, 300), (74, 65), (75, 64), (100, 129), (128, 64), (129, 200), (150, 70)])
+def test_sequences_of_one_length(idxc, B, n, H, four):
+    """Batches whose sequences are cut each by itself, or not at all, and every third batch with an empty and a longer one among them."""
+    lens = [n] * B
+    if B % 3 == 0:
+        lens[B // 2], lens[-1] = 0, n + 3
+    g = gen(B + H)
+    total = sum(lens)
+    kv = cache_rows(total, four, g)
+    q = bf16_rows(B * H, g, 0.5).view(B, 1, H, 576)
+    base = np.concatenate([[0], np.cumsum(lens)[:-1]])
+    out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), torch.tensor(base, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), max(lens), 512, 1 / 24)
+    for b in sorted({0, 1, B // 3, B // 2, B - 2, B - 1}):
+        check_attention(out[b, 0], lse[b, 0], *oracle_sequence(q[b], kv, int(base[b]), lens[b], 1, 1 / 24)[:4], f"sequence {b}")
+    assert torch.isfinite(out.float()).all()
