@@ -12,13 +12,17 @@
 // waits for the other's tile. (One shared buffer a tile, as for up to 64 rows, refills only after the product: 2.8 K clocks a tile.)
 // The first CTA's warps 0 and 1 issue for both; loaders and softmax warps of both CTAs arrive on the first one's barriers, and
 // commits are multicast to both.
-// Shared memory of a CTA: Q 9 x [64 x 128 B] | K 2 x 9 x [32 x 128 B] | V 2 x 4 x [64 x 128 B] | P 2 x [64 x 128 B]. What an MMA reads and a
-// copy writes passes its 128 bytes a clock, and bf16 tiles keep that path busy to 1800 clocks, all there is.
+// Shared memory of a CTA: Q 9 x [64 x 128 B] | K 2 x 9 x [32 x 128 B] | V 2 x 4 x [64 x 128 B] | P 2 x [64 x 128 B]. What MMAs read, copies
+// write and loads bring passes the same path at 128 bytes a clock, and that path bounds the kernel (selected 4-bit rows: 2800 of its
+// wavefronts in 2680 clocks a tile, a load taking one for every 32 bytes). So 6 of Q's 9 blocks are the A operand from tensor memory, in both
+// lane halves (each multiplies its own half of the N columns): 384 wavefronts a tile less, selected rows (2047 queries of 2048) 1.18 ->
+// 1.13 ms, bf16 rows (32 x 16K to 64K) 378 -> 369 us.
 // 4-bit rows in order are copied as they are into a ring of half tiles (3 x 32 rows x 416 B, a bulk copy each), and eight warps expand
-// them into K and V. To make room, and to take their reads off the same path, 6 of Q's 9 blocks are then the A operand from
-// tensor memory, in both lane halves (each multiplies its own half of the N columns): 325 us at 8 x 131072 rows, 342 with the rows read
-// straight into registers and Q in shared memory. Selected rows are read straight into registers: at 2047 queries of 2048 rows 1.28 ms,
-// through the ring 2.1 ms (a copy a row, or 16 bytes at a time: the ring is too short for their latency).
+// them into K and V; the ring lies where Q's 6 blocks would, so the softmax warps bring those from global to tensor memory themselves: 325 us
+// at 8 x 131072 rows, 342 with the rows read straight into registers and Q in shared memory. Selected rows are read straight into
+// registers: through the ring 2.1 ms (a copy a row, or 16 bytes at a time: the ring is too short for their latency).
+#include <type_traits>
+
 #include "latent_attn.cuh"
 
 namespace idxc {
@@ -33,7 +37,8 @@ constexpr uint32_t kVBytes = 4 * kVBlock;
 constexpr uint32_t kPBytes = kRows * 128;
 constexpr uint32_t kBarBytes = 512;
 constexpr uint32_t kSwapBytes = 3 * 4 * 32 * 4;     // what two warps exchange: row maxima, double-buffered, and at the end row sums
-constexpr int kQT = 6;                              // 4-bit rows: Q blocks in tensor memory
+constexpr int kQT = 6;                              // Q blocks that the scores take from tensor memory
+constexpr int kCopyTiles = 4;                       // they are copied there for pieces of that many tiles (860 clocks; one tile a piece: 0.5 us more)
 constexpr int kRawSlots = 3;
 constexpr int kCutTiles = 13;                       // (see find_run) 64 queries of 32 selected tiles: 84 us cut even, 65 us apart; 38: 60 us and 65
 constexpr uint32_t kRawBytes = kHalf * kLatentQ4RowBytes;
@@ -44,7 +49,7 @@ constexpr uint32_t smem_bytes(Rows r) {
 }
 static_assert(smem_bytes(kBf16) <= 232448 && smem_bytes(kCodes) <= 232448 && smem_bytes(kPicked) <= 232448, "shared memory of a CTA");
 constexpr uint32_t kColS = 256;                     // S buffer b at kColS + 32 b; O in [0, 256)
-constexpr uint32_t kColQ = 320;                     // 4-bit rows: Q blocks 0 .. kQT - 1, 32 columns each (two bf16 a column)
+constexpr uint32_t kColQ = 320;                     // Q blocks 0 .. kQT - 1, 32 columns each (two bf16 a column)
 constexpr int kWarpsBf16 = 9;                       // 0 scores | 1 P V | 2 Q | 3 K (TMA) | 4..7 softmax | 8 V (TMA)
 constexpr int kWarpsQ4 = 16;                        // 0 scores | 1 P V | 2 Q | 3 rows in order | 4..7 softmax | 8..11 K | 12..15 V
 
@@ -184,14 +189,28 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         const uint64_t q_desc = umma_smem_desc_sw128(smem_u32(q_smem));
         while (rank == 0 && ok && walk.next(pc)) {
             ok = wait_warp(bar_q_full, item & 1u) && (ROWS != kCodes || wait_warp(bar_q_ready, item & 1u));
+            const bool in_tmem = ROWS == kCodes || __all_sync(0xFFFFFFFFu, pc.n >= kCopyTiles);      // (a vote: uniform to the compiler)
+            if (ROWS != kCodes && __all_sync(0xFFFFFFFFu, ok && in_tmem)) {      // (Q came after the scores that read the last one were done)
+                tcgen05_fence_after_sync();
+#pragma unroll 1
+                for (int b = 0; b < kQT; ++b) tmem_copy_64x128_pair(tmem_base + kColQ + b * 32, q_desc + b * (kRows * 128 / 16));
+            }
             for (int i = 0; __all_sync(0xFFFFFFFFu, ok && i < pc.n); ++i, ++tile) {      // (a vote: the compiler sees a uniform loop)
                 const uint32_t st = tile & 1u, ph = (tile >> 1) & 1u;
                 ok = wait_warp(bar_s_free + 8 * st, ph ^ 1u) && wait_warp(bar_k_full + 8 * st, ph);
                 if (!ok) break;
                 tcgen05_fence_after_sync();
                 const uint32_t d = tmem_base + kColS + st * 32;
-                uint64_t a_desc = q_desc, b_desc = umma_smem_desc_sw128(smem_u32(k_smem + st * kKBytes));
-                if (ROWS == kCodes) {
+                uint64_t b_desc = umma_smem_desc_sw128(smem_u32(k_smem + st * kKBytes));
+                auto from_smem = [&](uint64_t a_desc, auto first) {      // blocks first .. 8 of Q
+#pragma unroll 3
+                    for (int b = first; b < kBlocks; ++b) {
+                        umma_f16_pair_x4<2, 2>(d, a_desc, b_desc, kIdescS, b != 0 ? 1u : 0u);
+                        a_desc += kRows * 128 / 16;
+                        b_desc += kKBlock / 16;
+                    }
+                };
+                if (in_tmem) {
                     uint32_t a_tmem = tmem_base + kColQ;
 #pragma unroll 3
                     for (int b = 0; b < kQT; ++b) {
@@ -199,12 +218,9 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                         a_tmem += 32;
                         b_desc += kKBlock / 16;
                     }
-                }
-#pragma unroll 3
-                for (int b = ROWS == kCodes ? kQT : 0; b < kBlocks; ++b) {
-                    umma_f16_pair_x4<2, 2>(d, a_desc, b_desc, kIdescS, b != 0 ? 1u : 0u);
-                    a_desc += kRows * 128 / 16;
-                    b_desc += kKBlock / 16;
+                    from_smem(q_desc + (ROWS == kCodes ? 0 : kQT * (kRows * 128 / 16)), std::integral_constant<int, kQT>());
+                } else {
+                    from_smem(q_desc, std::integral_constant<int, 0>());
                 }
                 umma_commit_pair_elect(bar_s_full + 8 * st);
             }

@@ -459,6 +459,23 @@ __device__ __forceinline__ void umma_commit_pair_elect(uint32_t bar) {
         ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
 }
 
+// 64 rows x 128 bytes of shared memory (128-byte swizzle) of each CTA of a pair into its tensor memory, 32 columns: row r on lanes r and
+// 64 + r, as the A operand of a pair's M = 128 MMAs wants it. In order with the MMAs that the same thread issues after it.
+__device__ __forceinline__ void tmem_copy_64x128_pair(uint32_t d, uint64_t s) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%0], %8;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%1], %9;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%2], %10;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%3], %11;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%4], %12;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%5], %13;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%6], %14;\n\t"
+        "@e tcgen05.cp.cta_group::2.64x128b.warpx2::02_13 [%7], %15;\n\t}"
+        ::"r"(d), "r"(d + 4), "r"(d + 8), "r"(d + 12), "r"(d + 16), "r"(d + 20), "r"(d + 24), "r"(d + 28),
+          "l"(s), "l"(s + 1), "l"(s + 2), "l"(s + 3), "l"(s + 4), "l"(s + 5), "l"(s + 6), "l"(s + 7) : "memory");
+}
+
 // ---------------------------------------------------------------- L2 residency hints
 // A policy word for the .L2::cache_hint forms: lines touched with evict_last are kept in preference to others,
 // lines touched with evict_first go first.
