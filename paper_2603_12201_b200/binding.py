@@ -402,13 +402,9 @@ def _launch_on(stream, **tensors):
     return (_NO_GUARD if torch.cuda.current_device() == index else torch.cuda.device(index)), raw
 
 
-def _new(shape, dtype, device):
-    """torch.empty of a contiguous shape, a microsecond faster."""
-    strides, n = [], 1
-    for k in reversed(shape):
-        strides.append(n)
-        n *= max(k, 1)
-    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
+def _new3(a, b, c, dtype, device):
+    """torch.empty((a, b, c)), a microsecond faster."""
+    return torch.empty_strided((a, b, c), (b * c, c, 1), dtype=dtype, device=device)
 
 
 def _at(t):
@@ -463,7 +459,7 @@ def latent_attention_workspace_bytes(B, n_step, max_len, H) -> int:
 
 def _latent_workspace(workspace, B, n_step, max_len, H, device):
     if workspace is None:
-        workspace = _new((max(latent_attention_workspace_bytes(B, n_step, max_len, H), 256),), torch.uint8, device)
+        workspace = torch.empty_strided((max(latent_attention_workspace_bytes(B, n_step, max_len, H), 256),), (1,), dtype=torch.uint8, device=device)
     return workspace
 
 
@@ -481,8 +477,8 @@ def latent_attention(q, kv, kv_base, lens, max_len, d_v, scale, want_lse=True, o
     _typed(out, "out", torch.bfloat16, (B, n_step, H, d_v))
     with guard:
         if out is None:
-            out = _new((B, n_step, H, d_v), torch.bfloat16, q.device)
-        lse = _new((B, n_step, H), torch.float32, q.device) if want_lse else None
+            out = torch.empty_strided((B, n_step, H, d_v), (n_step * H * d_v, H * d_v, d_v, 1), dtype=torch.bfloat16, device=q.device)
+        lse = _new3(B, n_step, H, torch.float32, q.device) if want_lse else None
         workspace = _latent_workspace(workspace, B, n_step, max_len, H, q.device)
         _check(lib().idxc_latent_attention(_at(q), _at(kv), fmt, kv.shape[0], _at(kv_base), _at(lens), B, n_step, int(max_len), H, d_qk,
                                            int(d_v), float(scale), _at(out), _at(lse), _at(workspace), workspace.nbytes,
@@ -502,8 +498,8 @@ def sparse_attention_q4(q, kv, topk, d_v, scale, kv_base=None, want_lse=True, ou
     _typed(out, "out", torch.bfloat16, (n_q, H, d_v))
     with guard:
         if out is None:
-            out = _new((n_q, H, d_v), torch.bfloat16, q.device)
-        lse = _new((n_q, H), torch.float32, q.device) if want_lse else None
+            out = _new3(n_q, H, d_v, torch.bfloat16, q.device)
+        lse = torch.empty_strided((n_q, H), (H, 1), dtype=torch.float32, device=q.device) if want_lse else None
         workspace = _latent_workspace(workspace, n_q, 1, k_top, H, q.device)
         _check(lib().idxc_sparse_attention_q4(_at(q), _at(kv), _at(topk), _at(kv_base), n_q, kv.shape[0], H, d_qk, int(d_v), k_top,
                                               float(scale), _at(out), _at(lse), _at(workspace), workspace.nbytes,

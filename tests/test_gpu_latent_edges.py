@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import latent as oracle
-from tests.latent_util import bf16_rows, cache_rows, check_attention, oracle_sequence, q4_rows
+from tests.latent_util import bf16_rows, cache_rows, check_attention, oracle_sequence, q4_rows, stored
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -125,3 +125,54 @@ def test_sequences_of_one_length(idxc, B, n, H, four):
     for b in sorted({0, 1, B // 3, B // 2, B - 2, B - 1}):
         check_attention(out[b, 0], lse[b, 0], *oracle_sequence(q[b], kv, int(base[b]), lens[b], 1, 1 / 24)[:4], f"sequence {b}")
     assert torch.isfinite(out.float()).all()
+
+
+def test_captured_run_with_copies_forks_and_joins(idxc):
+    """The cache's kernels behind a copy, a fill, each other and kernels of another stream, in a graph: every replay sees the inputs of its time."""
+    n, budget = 600, 128
+    g = gen(3)
+    src, x, kept = bf16_rows(n, g).to(DEV), torch.zeros(n, 576, dtype=torch.bfloat16, device=DEV), torch.empty(n, 576, dtype=torch.bfloat16, device=DEV)
+    cache, small = torch.zeros(n, 416, dtype=torch.uint8, device=DEV), torch.zeros(budget, 416, dtype=torch.uint8, device=DEV)
+    back, side = torch.empty(n, 576, dtype=torch.bfloat16, device=DEV), torch.empty(budget, 576, dtype=torch.bfloat16, device=DEV)
+    acc_src, acc = torch.rand(1, n, device=DEV), torch.zeros(1, n, device=DEV)
+    lens, zero = torch.tensor([n], dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV)
+    keep, new = torch.empty(1, budget, dtype=torch.int32, device=DEV), torch.empty(1, dtype=torch.int32, device=DEV)
+    q = bf16_rows(16, g, 0.5).view(1, 1, 16, 576).to(DEV)
+
+    def step():
+        main, other = torch.cuda.current_stream(), torch.cuda.Stream()
+        x.copy_(src)
+        idxc.quantize_q4(x, cache)
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            acc.copy_(acc_src)
+            idxc.evict_select(acc, lens, budget, 5, keep, new)
+        idxc.dequantize_q4(cache, back)
+        out, lse = idxc.latent_attention(q, cache, None, lens, n, 512, 1 / 24)
+        main.wait_stream(other)
+        idxc.compact_rows(cache, small, keep, new, zero)
+        idxc.dequantize_q4(small, side)
+        cache.zero_()
+        idxc.quantize_q4(x, cache)
+        idxc.dequantize_q4(cache, kept)
+        return out, lse
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for seed in range(3):
+        src.copy_(bf16_rows(n, gen(seed), 1 + seed))
+        acc_src.copy_(torch.rand(1, n, generator=gen(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(stored(cache), oracle.quantize_rows(src.double().cpu().numpy()))
+        for b in (back, kept):
+            assert np.array_equal(b.double().cpu().numpy(), oracle.row_values(stored(cache)))
+        want = oracle.evict(acc_src[0].cpu().numpy(), n, budget, 5)
+        assert np.array_equal(keep[0].cpu().numpy(), want)
+        assert torch.equal(side, back[torch.as_tensor(want, dtype=torch.int64, device=DEV)])
+        check_attention(got[0][0, 0], got[1][0, 0], *oracle_sequence(q[0], cache, 0, n, 1, 1 / 24)[:4])
