@@ -96,7 +96,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const int seq_rows = p.a.n_step * p.a.H;
     // query rows of this CTA in a unit: first row within the sequence, and how many
     auto rows_of = [&](uint32_t unit, int64_t& seq, int& r0) -> int {
-        const uint32_t s = unit / static_cast<uint32_t>(p.blocks_per_seq);
+        const uint32_t s = p.tiles.seq_of(unit);
         seq = s;
         r0 = static_cast<int>(unit - s * p.blocks_per_seq) * kRows;
         return min(kRows, seq_rows - r0);
@@ -365,7 +365,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         auto ahead_piece = [&]() {
             more = false;
             if (ahead.next(apc)) {
-                const int64_t s = apc.unit / static_cast<uint32_t>(p.blocks_per_seq);
+                const int64_t s = p.tiles.seq_of(apc.unit);
                 len = seq_len(s);
                 base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
                 sel = p.a.topk ? p.a.topk + s * p.a.k_top : nullptr;
@@ -660,9 +660,11 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 // ---------------------------------------------------------------- merge
 // A unit cut by runs: group g - 1 holds its beginning (slot 1), groups g, g + 1, .. its continuations (slot 0). Block (g, y)
 // takes rows 4 (y + k gridDim.y) .. + 3 of the unit that group g is the first to start inside of; 128 threads a row, 4 columns each. As
-// many blocks as run at a time where every unit needs them (32 queries of 2048 rows: 48 us, with a block for every four rows 50 us;
-// one query: 23.7 us, 29 with as many as run at a time of all groups).
-__global__ void __launch_bounds__(512)
+// many blocks as run at a time where every unit needs them. Bound by latency and by what is in flight: 32 queries of 32 tiles (the whole call) 44.9 us,
+// 64 sequences of 1 to 9 thousand rows 92.3 us; with eight pieces at a time 47.6 and 94.9, with three CTAs of four pieces 44.7 and 94.2, with a
+// block for every four rows 2 us more.
+constexpr int kMergePieces = 6, kMergeCtas = 2;
+__global__ void __launch_bounds__(512, kMergeCtas)
 latent_merge_kernel(const Params p) {
     wait_for_previous();
     const int g = blockIdx.x;
@@ -679,7 +681,7 @@ latent_merge_kernel(const Params p) {
     }
     if (fs.x == s.x && fs.y > 0) return;                      // an earlier group starts inside this unit too
     const int end = run - s.y + p.tiles(static_cast<uint32_t>(s.x));      // one past the unit's last tile, end to end
-    const uint32_t seq = static_cast<uint32_t>(s.x) / static_cast<uint32_t>(p.blocks_per_seq);
+    const uint32_t seq = p.tiles.seq_of(static_cast<uint32_t>(s.x));
     const int seq_rows = p.a.n_step * p.a.H, first_row = static_cast<int>(s.x - seq * p.blocks_per_seq) * p.ways * kRows;
     const int n_rows = min(p.ways * kRows, seq_rows - first_row), c = threadIdx.x & 127;
     const int64_t stride = static_cast<int64_t>(2) * p.ways * kRows;            // rows of a group's two slots
@@ -687,13 +689,13 @@ latent_merge_kernel(const Params p) {
         const int64_t at1 = first * stride + p.ways * kRows + r, at0 = g * stride + r;
         float m = -INFINITY, z = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        // piece 0 is the beginning, piece k > 0 group g + k - 1's; eight at a time, all loads of the eight before their first use
+        // piece 0 is the beginning, piece k > 0 group g + k - 1's; kMergePieces at a time, all their loads before their first use
         bool more = true;
-        for (int k0 = 0; more; k0 += 8) {
-            float ls[8];
-            float4 v[8];
+        for (int k0 = 0; more; k0 += kMergePieces) {
+            float ls[kMergePieces];
+            float4 v[kMergePieces];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < kMergePieces; ++j) {
                 const int k = k0 + j, grp = g + k - 1;
                 bool in = k == 0;
                 if (k > 0) {
@@ -708,7 +710,7 @@ latent_merge_kernel(const Params p) {
             float top = m;
             bool none = m == -INFINITY;                       // (fmaxf passes over what is no number; the weights do not)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < kMergePieces; ++j) {
                 top = fmaxf(top, ls[j]);
                 none = none && ls[j] == -INFINITY;
             }
@@ -719,7 +721,7 @@ latent_merge_kernel(const Params p) {
             z *= f;
             acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < kMergePieces; ++j) {
                 const float w = exp2_fast((ls[j] - top) * 1.4426950408889634f);
                 acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
                 z += w;
@@ -808,7 +810,7 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
         ++*launches;
         const int unit_rows = a.n_step * a.H < y.ways * kRows ? a.n_step * a.H : y.ways * kRows;
         const int64_t busy = y.units < y.groups ? y.units : y.groups;          // groups that may have a unit to merge
-        const int64_t at_once = 4 * sm_count / busy, blocks = (unit_rows + 3) / 4;
+        const int64_t at_once = kMergeCtas * sm_count / busy, blocks = (unit_rows + 3) / 4;
         e = launch_behind(latent_merge_kernel, dim3(static_cast<unsigned>(y.groups), static_cast<unsigned>(blocks < at_once ? blocks : at_once)), 512, 0, stream, p);
     }
     return e;

@@ -24,9 +24,10 @@ struct UnitTiles {
     int64_t max_len;
     uint32_t blocks_per_seq;     // units of a sequence
     int tile_log2;               // rows of a tile
+    __device__ __forceinline__ uint32_t seq_of(uint32_t unit) const { return blocks_per_seq == 1 ? unit : unit / blocks_per_seq; }
     __device__ __forceinline__ int operator()(uint32_t unit) const {
         if (counted) return *static_cast<const volatile int32_t*>(counted + unit);      // (not __ldg: written while this kernel may already run)
-        const int most = static_cast<int>(max_len), len = lens ? __ldg(lens + unit / blocks_per_seq) : most;      // (max_len <= 2^30)
+        const int most = static_cast<int>(max_len), len = lens ? __ldg(lens + seq_of(unit)) : most;      // (max_len <= 2^30)
         return (min(max(len, 0), most) + (1 << tile_log2) - 1) >> tile_log2;
     }
 };

@@ -106,7 +106,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
     const int group = blockIdx.x >> 1;
     const int seq_rows = p.a.n_step * p.a.H;
     auto rows_of = [&](uint32_t unit, int64_t& seq, int& r0) -> int {
-        const uint32_t s = unit / static_cast<uint32_t>(p.blocks_per_seq);
+        const uint32_t s = p.tiles.seq_of(unit);
         seq = s;
         r0 = (static_cast<int>(unit - s * p.blocks_per_seq) * 2 + rank) * kRows;
         return min(kRows, seq_rows - r0);
@@ -271,7 +271,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         // may hold anything: they only reach scores that the softmax discards.
         if (lane == 0) {
             while (ok && walk.next(pc)) {
-                const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + pc.unit / static_cast<uint32_t>(p.blocks_per_seq)) : 0;
+                const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + p.tiles.seq_of(pc.unit)) : 0;
                 for (int i = 0; i < pc.n && ok; ++i, ++tile) {
                     const uint32_t st = tile & 1u;
                     const int64_t at = base + static_cast<int64_t>(pc.t0 + i) * kTile;
@@ -336,7 +336,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         const uint8_t* kv = static_cast<const uint8_t*>(p.a.kv);
         uint32_t slot = 0, ph = 1;
         while (ok && walk.next(pc)) {
-            const int64_t s = pc.unit / static_cast<uint32_t>(p.blocks_per_seq);
+            const int64_t s = p.tiles.seq_of(pc.unit);
             const int len = static_cast<int>(seq_len(s));
             const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
             for (int x = 0; x < 2 * pc.n && ok; ++x) {
@@ -383,7 +383,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         int i = 0;
         auto open_piece = [&]() {
             if (!walk.next(pc)) return;
-            seq = pc.unit / static_cast<uint32_t>(p.blocks_per_seq);
+            seq = p.tiles.seq_of(pc.unit);
             len = static_cast<int>(seq_len(seq));
             base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
             sel = p.a.topk + seq * p.a.k_top;
