@@ -46,23 +46,30 @@ constexpr int kSlotWarps = 4;                       // warps that fill a slot (4
 
 // ---------------------------------------------------------------- plan
 // Selected rows: tiles of query t up to its last usable entry.
-__global__ void __launch_bounds__(128)
+constexpr int kCountThreads = 256;
+__global__ void __launch_bounds__(kCountThreads)
 latent_count_kernel(const LatentArgs a, int32_t* __restrict__ tiles) {
-    __shared__ int s_last[4];
+    __shared__ int s_last[kCountThreads / 32];
     let_next_start();
     const int64_t t = blockIdx.x;
     const int64_t base = a.kv_base ? __ldg(a.kv_base + t) : 0;
     const int32_t* row = a.topk + t * a.k_top;
     int last = 0;
-#pragma unroll 4
-    for (int j = threadIdx.x; j < a.k_top; j += 128) {
-        const int64_t i = __ldg(row + j);
-        if (i >= 0 && base + i >= 0 && base + i < a.n_kv) last = j + 1;
+    for (int j0 = threadIdx.x; j0 < a.k_top; j0 += 8 * kCountThreads) {          // eight loads under way at a time
+        int32_t i[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) i[k] = j0 + k * kCountThreads < a.k_top ? __ldg(row + j0 + k * kCountThreads) : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i[k] >= 0 && base + i[k] >= 0 && base + i[k] < a.n_kv) last = j0 + k * kCountThreads + 1;
     }
     last = __reduce_max_sync(0xFFFFFFFFu, last);
     if ((threadIdx.x & 31) == 0) s_last[threadIdx.x >> 5] = last;
     __syncthreads();
-    if (threadIdx.x == 0) tiles[t] = (max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3])) + kTile - 1) / kTile;
+    if (threadIdx.x < 32) {
+        last = __reduce_max_sync(0xFFFFFFFFu, threadIdx.x < kCountThreads / 32 ? s_last[threadIdx.x] : 0);
+        if (threadIdx.x == 0) tiles[t] = (last + kTile - 1) / kTile;
+    }
 }
 
 // ---------------------------------------------------------------- main kernel
@@ -791,7 +798,7 @@ cudaError_t launch_latent_attn(const LatentArgs& a, void* out, float* lse, void*
     cudaError_t e;
     if (a.topk) {
         ++*launches;
-        latent_count_kernel<<<static_cast<unsigned>(a.B), 128, 0, stream>>>(a, tiles);
+        latent_count_kernel<<<static_cast<unsigned>(a.B), kCountThreads, 0, stream>>>(a, tiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     ++*launches;
