@@ -176,3 +176,17 @@ def test_captured_run_with_copies_forks_and_joins(idxc):
         assert np.array_equal(keep[0].cpu().numpy(), want)
         assert torch.equal(side, back[torch.as_tensor(want, dtype=torch.int64, device=DEV)])
         check_attention(got[0][0, 0], got[1][0, 0], *oracle_sequence(q[0], cache, 0, n, 1, 1 / 24)[:4])
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("lens,H,n_step", [([260], 128, 200), ([77, 400], 20, 77), ([30, 150], 16, 130), ([193], 128, 2), ([64, 65, 3], 100, 5)])
+def test_chunks_of_a_prompt(idxc, lens, H, n_step, four):
+    """New tokens that fill many units, of which a prompt's first see few positions or none."""
+    B = len(lens)
+    g = gen(n_step + H)
+    kv = cache_rows(sum(lens), four, g)
+    q = bf16_rows(B * n_step * H, g, 0.5).view(B, n_step, H, 576)
+    base = np.concatenate([[0], np.cumsum(lens)[:-1]])
+    out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), torch.tensor(base, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), max(lens) + 9, 512, 1 / 24)
+    for b, n in enumerate(lens):
+        check_attention(out[b].reshape(-1, 512), lse[b].reshape(-1), *oracle_sequence(q[b], kv, int(base[b]), n, n_step, 1 / 24)[:4], f"sequence {b}")
