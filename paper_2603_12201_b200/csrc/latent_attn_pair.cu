@@ -40,7 +40,7 @@ constexpr uint32_t kSwapBytes = 3 * 4 * 32 * 4;     // what two warps exchange: 
 constexpr int kQT = 6;                              // Q blocks that the scores take from tensor memory
 constexpr int kCopyTiles = 4;                       // they are copied there for pieces of that many tiles (860 clocks; one tile a piece: 0.5 us more)
 constexpr int kRawSlots = 3;
-constexpr int kCutTiles = 13;                       // (see find_run) 64 queries of 32 selected tiles: 84 us cut even, 65 us apart; 38: 60 us and 65
+constexpr int kCutTiles = 13;                       // (see find_run) selected rows, 50 queries of 32 tiles: 64 us cut even, 58 us apart; 38 of 16: 41 us and 36
 constexpr uint32_t kRawBytes = kHalf * kLatentQ4RowBytes;
 enum Rows { kBf16, kCodes, kPicked };               // bf16 rows in order, 4-bit rows in order, selected 4-bit rows
 constexpr uint32_t q_bytes(Rows r) { return (r == kCodes ? kBlocks - kQT : kBlocks) * kRows * 128; }
