@@ -407,8 +407,8 @@ idxc_status idxc_attention_weights(const void* q, const void* kv, idxc_latent_fo
  *
  * idxc_compact_rows -- brings the rows that stay together: for j < n_keep[b], row dst_base[b] + j of dst becomes row
  * src_base[b] + keep[b, j] of src. row_bytes is any multiple of 4 (bf16 or 4-bit latent rows, indexer keys, scales, the
- * sums themselves with src_base[b] = b * ld). keep [B, ld_keep]; an entry that names no row of src, or whose place is
- * no row of dst, moves nothing.
+ * sums themselves with src_base[b] = b * ld). keep [B, ld_keep], ld_keep <= 2^30; an entry that names no row of src, or
+ * whose place is no row of dst, moves nothing.
  *   dst == src (then dst_base must be src_base): in place. keep[b] must be ascending without repeats, as written by
  *   idxc_evict_select; entries that are not at or behind their own place are skipped. Sequences must not share rows.
  *   Otherwise the two buffers must not overlap.

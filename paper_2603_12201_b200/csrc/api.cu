@@ -681,7 +681,7 @@ idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t
                               const int64_t* src_base, const int64_t* dst_base, const int32_t* keep, int ld_keep,
                               const int32_t* n_keep, int64_t B, void* cuda_stream) {
     if (B < 0 || B > 65535 || row_bytes < 4 || (row_bytes & 3) || row_bytes > (1 << 20) || src_rows < 0 || dst_rows < 0 || ld_keep < 0 ||
-        src_rows > (int64_t(1) << 40) || dst_rows > (int64_t(1) << 40))
+        ld_keep > (1 << 30) || src_rows > (int64_t(1) << 40) || dst_rows > (int64_t(1) << 40))
         return IDXC_ERR_INVALID_ARG;
     if (B == 0 || ld_keep == 0 || src_rows == 0 || dst_rows == 0) return IDXC_OK;
     if (!src || !dst || !src_base || !dst_base || !keep || !n_keep || !aligned(src, 4) || !aligned(dst, 4) || !aligned(src_base, 8) ||

@@ -116,3 +116,11 @@ def test_binding_takes_cuda_tensors_only(idxc):
         idxc.quantize_q4(kv, torch.zeros((4, 416), dtype=torch.uint8))
     with pytest.raises(ValueError):
         idxc.evict_select(torch.zeros(1, 4), torch.ones(1, dtype=torch.int32), 2, 1, torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
+
+
+def test_compaction_refuses_more_entries_than_it_can_count(idxc):
+    """Above 2^30 the row counter of the kernel in place would wrap; the same bound as the choice's budget."""
+    L, far = idxc.lib(), ctypes.c_void_p(1 << 30)
+    for dst, base in ((P, P), (far, P)):
+        for ld_keep in (2 ** 30 + 1, 2 ** 31 - 1):
+            assert L.idxc_compact_rows(P, dst, 4, 2 ** 32, 2 ** 32 if dst is P else 8, P, base, P, ld_keep, P, 1, None) == idxc.ERR_INVALID_ARG
