@@ -150,7 +150,7 @@ compact_copy_kernel(const T* src, T* dst, uint32_t units, int64_t src_rows, int6
     let_next_start();
     const int b = blockIdx.y;
     const int n = min(max(n_keep[b], 0), ld_keep);
-    const int64_t sb = src_base[b], db = dst_base[b];
+    const int64_t sb = near_base(src_base[b], src_rows), db = near_base(dst_base[b], dst_rows);
     const int64_t total = static_cast<int64_t>(n) * units;
     const int32_t* k_row = keep + static_cast<int64_t>(b) * ld_keep;
     for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kCopyUnits; i0 < total; i0 += static_cast<int64_t>(gridDim.x) * kCopyUnits) {
@@ -193,7 +193,7 @@ compact_in_place_kernel(T* rows, int units, int slice_units, int64_t n_rows, con
     let_next_start();
     const int b = blockIdx.y;
     const int n = min(max(n_keep[b], 0), ld_keep);
-    const int64_t sb = base[b];
+    const int64_t sb = near_base(base[b], n_rows);
     const int u0 = blockIdx.x * slice_units;
     const int width = min(slice_units, units - u0);
     const int per_pass = kMoveThreads / slice_units;          // rows that one pass of the CTA covers

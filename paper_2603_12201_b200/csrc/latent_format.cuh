@@ -20,6 +20,13 @@ constexpr int kLatentQ4RowBytes = 416;
 constexpr int kLatentQ4ScaleOff = 256;
 constexpr int kLatentQ4RopeOff = 288;
 
+// The first row of a sequence in an array of `rows` rows, brought into [-2^31, rows]: a position is below 2^31, so a base farther out names
+// no row of the array either, and no sum of a base and a position wraps around.
+__device__ __forceinline__ int64_t near_base(int64_t base, int64_t rows) {
+    const int64_t low = -(int64_t(1) << 31);
+    return base < low ? low : (base > rows ? rows : base);
+}
+
 // The scale of a group as the reader uses it, in both halves of a word: s and -24 s (3 s has at most 7 bits: exact).
 struct Q4Scale {
     __nv_bfloat162 s, m24s;

@@ -219,3 +219,27 @@ def test_evicted_cache_reads_as_the_selection(idxc):
     got, lse = idxc.latent_attention(q.unsqueeze(1), kv, base, new, budget, 512, 0.05)
     assert torch.allclose(lse.squeeze(1), want_lse, atol=1e-5)
     assert torch.allclose(got.squeeze(1).float(), want.float(), atol=2e-2, rtol=2e-2)
+
+
+@pytest.mark.parametrize("shape,dtype", [((416,), torch.uint8), ((), torch.float32)])
+def test_compaction_from_bases_far_outside_moves_nothing(idxc, shape, dtype):
+    """Bases near the ends of 64 bits, where a base plus a position would wrap around into the array or far in front of it."""
+    src = torch.arange(40, device=DEV).reshape(40, *[1] * len(shape)).expand(40, *shape).to(dtype).contiguous()
+    before = src.clone()
+    ends = [2 ** 63 - 1, 2 ** 63 - 3, 2 ** 63 - 10, -2 ** 63, -2 ** 63 + 2, -2 ** 31, -2 ** 31 - 1, 40, 2 ** 40]
+    base = torch.tensor(ends, dtype=torch.int64, device=DEV)
+    keep = torch.tensor([[1, 2, 5, 2 ** 31 - 1]], dtype=torch.int32, device=DEV).repeat(len(ends), 1)
+    n = torch.full((len(ends),), 4, dtype=torch.int32, device=DEV)
+    idxc.compact_rows(src, src, keep, n, base)
+    assert torch.equal(src, before)
+    dst = torch.full_like(src, 99)
+    want = dst.clone()
+    idxc.compact_rows(src, dst, keep, n, base, torch.zeros_like(base))
+    assert torch.equal(dst, want)
+    idxc.compact_rows(src, dst, keep, n, torch.zeros_like(base), base)
+    assert torch.equal(dst, want) and torch.equal(src, before)
+    # the edge itself: a base just in front of the array
+    base = torch.tensor([-3], dtype=torch.int64, device=DEV)
+    idxc.compact_rows(src, dst, keep[:1], n[:1], base, torch.zeros_like(base))
+    want[2] = before[2]
+    assert torch.equal(dst, want)
