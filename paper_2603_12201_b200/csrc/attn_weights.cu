@@ -74,7 +74,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
     auto seq_len = [&](uint32_t b) -> int {
         return p.a.topk ? p.a.k_top : static_cast<int>(min(max(static_cast<int64_t>(__ldg(p.a.lens + b)), int64_t(0)), p.a.max_len));
     };
-    auto seq_base = [&](uint32_t b) -> int64_t { return p.a.kv_base ? __ldg(p.a.kv_base + b) : 0; };
+    auto seq_base = [&](uint32_t b) -> int64_t { return first_row(p.a, b); };
 
     const EarlyTiles early = early_tiles(p.units, p.tiles);
     early_bases(p.a.kv_base, p.a.B);

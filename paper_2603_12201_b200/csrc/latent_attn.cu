@@ -52,7 +52,7 @@ latent_count_kernel(const LatentArgs a, int32_t* __restrict__ tiles) {
     __shared__ int s_last[kCountThreads / 32];
     let_next_start();
     const int64_t t = blockIdx.x;
-    const int64_t base = a.kv_base ? __ldg(a.kv_base + t) : 0;
+    const int64_t base = first_row(a, t);
     const int32_t* row = a.topk + t * a.k_top;
     int last = 0;
     for (int j0 = threadIdx.x; j0 < a.k_top; j0 += 8 * kCountThreads) {          // eight loads under way at a time
@@ -266,7 +266,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         while (ok && walk.next(pc)) {
             rows_of(pc.unit, seq, r0);
             const int64_t len = seq_len(seq);
-            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            const int64_t base = first_row(p.a, seq);
             for (int i = 0; i < pc.n && ok; ++i, ++tile) {
                 const uint32_t st = tile & 1u, ph = ((tile >> 1) & 1u) ^ 1u;
                 uint8_t* dst = stage_smem + st * kStageBytes;
@@ -374,7 +374,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             if (ahead.next(apc)) {
                 const int64_t s = p.tiles.seq_of(apc.unit);
                 len = seq_len(s);
-                base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
+                base = first_row(p.a, s);
                 sel = p.a.topk ? p.a.topk + s * p.a.k_top : nullptr;
                 ai = 0;
                 more = true;
@@ -464,7 +464,7 @@ latent_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 const int64_t n = p.a.topk ? len : len - (p.a.n_step - 1 - (r0 + r) / p.a.H);
                 sees[h] = r < n_rows ? static_cast<int>(max(n, int64_t(0))) : 0;
             }
-            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            const int64_t base = first_row(p.a, seq);
             // rows [lo, hi) of the sequence lie inside the cache
             const int lo = static_cast<int>(min(max(-base, int64_t(0)), int64_t(1) << 30));
             const int hi = static_cast<int>(min(max(p.a.n_kv - base, int64_t(0)), int64_t(1) << 30));

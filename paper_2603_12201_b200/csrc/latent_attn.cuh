@@ -15,6 +15,8 @@ constexpr int kRows = 64;                           // query rows of a CTA
 constexpr int kBlocks = 9;                          // 64-column blocks of a row
 // A loader of Q waits while the piece before is worked on: its bound grows with that piece (a tile takes a few thousand cycles).
 __device__ __forceinline__ long long piece_budget(int tiles) { return kWaitCycleBudget + 50000LL * tiles; }
+// First cache row of sequence b.
+__device__ __forceinline__ int64_t first_row(const LatentArgs& a, int64_t b) { return a.kv_base ? near_base(__ldg(a.kv_base + b), a.n_kv) : 0; }
 constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
 
 // Tiles of a unit: counted beforehand, or from its sequence's length (no lengths: max_len for all).

@@ -271,7 +271,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         // may hold anything: they only reach scores that the softmax discards.
         if (lane == 0) {
             while (ok && walk.next(pc)) {
-                const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + p.tiles.seq_of(pc.unit)) : 0;
+                const int64_t base = first_row(p.a, p.tiles.seq_of(pc.unit));
                 for (int i = 0; i < pc.n && ok; ++i, ++tile) {
                     const uint32_t st = tile & 1u;
                     const int64_t at = base + static_cast<int64_t>(pc.t0 + i) * kTile;
@@ -296,7 +296,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         while (ok && walk.next(pc)) {
             rows_of(pc.unit, seq, r0);
             const int64_t len = seq_len(seq);
-            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            const int64_t base = first_row(p.a, seq);
             for (int i = 0; i < pc.n && ok; ++i, ++tile) {
                 const uint32_t st = tile & 1u;
                 const int64_t at = static_cast<int64_t>(pc.t0 + i) * kTile;
@@ -338,7 +338,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
         while (ok && walk.next(pc)) {
             const int64_t s = p.tiles.seq_of(pc.unit);
             const int len = static_cast<int>(seq_len(s));
-            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + s) : 0;
+            const int64_t base = first_row(p.a, s);
             for (int x = 0; x < 2 * pc.n && ok; ++x) {
                 const int at = (pc.t0 + (x >> 1)) * kTile + ((x & 1) ^ rank) * kHalf + lane;
                 const int64_t r = base + at;
@@ -385,7 +385,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             if (!walk.next(pc)) return;
             seq = p.tiles.seq_of(pc.unit);
             len = static_cast<int>(seq_len(seq));
-            base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            base = first_row(p.a, seq);
             sel = p.a.topk + seq * p.a.k_top;
             i = 0;
         };
@@ -598,7 +598,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                 if (lane == 0) mbar_arrive_cluster(in_first(bar_q_ready));
             }
             const int64_t len = seq_len(seq);
-            const int64_t base = p.a.kv_base ? __ldg(p.a.kv_base + seq) : 0;
+            const int64_t base = first_row(p.a, seq);
             // positions [lo, sees) are seen by this row: those inside the cache, up to the row's own new token
             int sees = 0;
             if (row < n_rows) {

@@ -190,3 +190,30 @@ def test_chunks_of_a_prompt(idxc, lens, H, n_step, four):
     out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), torch.tensor(base, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), max(lens) + 9, 512, 1 / 24)
     for b, n in enumerate(lens):
         check_attention(out[b].reshape(-1, 512), lse[b].reshape(-1), *oracle_sequence(q[b], kv, int(base[b]), n, n_step, 1 / 24)[:4], f"sequence {b}")
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H", [16, 128])
+def test_bases_far_outside_name_no_row(idxc, H, four):
+    """Bases near the ends of 64 bits, where a base plus a position would wrap around: their sequences see nothing, the others everything."""
+    n_kv, n = 1000, 700
+    bases = [2 ** 63 - 1, 2 ** 63 - 151, 2 ** 63 - 300, 2 ** 63 - 700, -2 ** 63, -2 ** 63 + 200, -2 ** 31 - 1, -2 ** 31, 2 ** 40, n_kv, -n, 250]
+    B, g = len(bases), gen(H)
+    kv = cache_rows(n_kv, four, g).to(DEV)
+    q = bf16_rows(B * H, g).view(B, 1, H, 576).to(DEV)
+    base, lens = torch.tensor(bases, dtype=torch.int64, device=DEV), torch.full((B,), n, dtype=torch.int32, device=DEV)
+    out, lse = idxc.latent_attention(q, kv, base, lens, n, 512, 1 / 24)
+    topk = torch.arange(n, dtype=torch.int32, device=DEV).repeat(B, 1).contiguous()
+    topk[:, -1] = 2 ** 31 - 1
+    results = [(out[:, 0], lse[:, 0], n)]
+    if four:
+        results.append((*idxc.sparse_attention_q4(q[:, 0].contiguous(), kv, topk, 512, 1 / 24, kv_base=base), n - 1))
+    for o, l, seen in results:
+        assert bool((o[:-1] == 0).all()) and bool(torch.isneginf(l[:-1]).all())
+        check_attention(o[-1], l[-1], *oracle_sequence(q[-1], kv, 250, seen, 1, 1 / 24)[:4])
+    lse = lse.nan_to_num(neginf=0.0)
+    for how in (dict(lens=lens, max_len=n), dict(topk=topk)):
+        acc = torch.ones((B, n), device=DEV)
+        idxc.attention_weights(q, kv, lse, acc, 1 / 24, kv_base=base, **how)
+        assert bool((acc[:-1] == 1).all()) and bool((acc[-1, :n - 1] > 1).all())
+    idxc.poll_device_status()
