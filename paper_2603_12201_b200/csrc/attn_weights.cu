@@ -261,17 +261,20 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_cons
             const int len = seq_len(pc.unit);
             const int64_t base = seq_base(pc.unit);
             __syncwarp();
+            int least = len;                                                 // a row without a log-sum-exp counts nowhere, whatever its scores are
             for (int r = lane; r < kWRows; r += 32) {
-                const float v = r < p.rows ? __ldg(p.lse + b * seq_rows + p.row0 + r) : -INFINITY;
-                lse2[r] = v == -INFINITY ? INFINITY : v * 1.4426950408889634f;        // exp2(x - inf) = 0
-                sees[r] = p.a.topk ? len : len - (p.a.n_step - 1 - (p.row0 + r) / p.a.H);
+                const float v = r < p.rows ? __ldg(p.lse + b * seq_rows + p.row0 + r) : 0.f;
+                lse2[r] = v * 1.4426950408889634f;
+                sees[r] = v == -INFINITY ? 0 : (p.a.topk ? len : len - (p.a.n_step - 1 - (p.row0 + r) / p.a.H));
+                if (r < p.rows) least = min(least, sees[r]);
             }
+            const int seen_by_all = __reduce_min_sync(0xFFFFFFFFu, least);
             __syncwarp();
             for (int i = 0; i < pc.n && ok; ++i, ++tile) {
                 const uint32_t st = tile & 1u;
                 const int j = (pc.t0 + i) * kWTile + quarter * 32 + lane;
                 const bool use = entry_row(p.a, b, base, j, len) >= 0;
-                const bool tail = __any_sync(0xFFFFFFFFu, j >= len - (p.a.n_step - 1));       // some token may not see some position
+                const bool tail = __any_sync(0xFFFFFFFFu, j >= seen_by_all);       // some row may not count at some position
                 float* dst = p.acc + b * p.ld + j;
                 float old = 0.f;
                 if (!p.a.topk && j < len && p.beta != 0.f) old = p.beta * *dst;

@@ -5,6 +5,7 @@ import torch
 
 from oracle import latent as oracle
 from tests.latent_util import bf16_rows, cache_rows, check_attention, oracle_sequence, q4_rows, stored
+from tests.test_gpu_latent_attention import weights_bound
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -217,3 +218,61 @@ def test_bases_far_outside_name_no_row(idxc, H, four):
         idxc.attention_weights(q, kv, lse, acc, 1 / 24, kv_base=base, **how)
         assert bool((acc[:-1] == 1).all()) and bool((acc[-1, :n - 1] > 1).all())
     idxc.poll_device_status()
+
+
+# ------------------------------------------------------------------ weights of tokens and heads without a log-sum-exp
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("lens,H,n_step", [([300, 129], 20, 3), ([1000, 7], 128, 2), ([65, 200], 33, 4)])
+def test_tokens_without_a_log_sum_exp_add_nothing(idxc, lens, H, n_step, bad, four):
+    """A padding token (lse -inf) may hold anything in q, and so may a single head."""
+    g = gen(lens[0] + H)
+    kv, scale = cache_rows(sum(lens), four, g), 1 / 24
+    q = bf16_rows(2 * n_step * H, g).view(2, n_step, H, 576)
+    base = [0, lens[0]]
+    seq = [oracle_sequence(q[b], kv, base[b], lens[b], n_step, scale) for b in range(2)]
+    lse = torch.tensor(np.stack([s[1] for s in seq]), dtype=torch.float32).view(2, n_step, H)
+    off = torch.zeros((2, n_step, H), dtype=torch.bool)
+    off[0, n_step - 1] = True                            # the newest token, which sees every position
+    off[1, 0, H - 1] = True
+    off[1, 1, 0] = True
+    q[off] = bad
+    lse[off] = float("-inf")
+    start = torch.rand((2, max(lens) + 3), generator=g)
+    acc = start.clone().to(DEV)
+    idxc.attention_weights(q.to(DEV), kv.to(DEV), lse.to(DEV), acc, scale, kv_base=torch.tensor(base, device=DEV),
+                           lens=torch.tensor(lens, dtype=torch.int32, device=DEV), max_len=max(lens))
+    got = acc.double().cpu().numpy()
+    for b, n in enumerate(lens):
+        _, _, _, reach, p = seq[b]
+        p = np.where(off[b].reshape(-1, 1).numpy(), 0.0, p)
+        want = start[b, :n].double().numpy() + p.sum(axis=0)
+        # the launches of 128 query rows each round the sum once
+        assert np.all(np.abs(got[b, :n] - want) <= weights_bound(p, reach, n_step * H) + 2.0 ** -23 * want), f"sequence {b}"
+        assert np.array_equal(got[b, n:], start[b, n:].double().numpy())
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H", [9, 128])
+def test_heads_without_a_log_sum_exp_add_nothing_to_a_selection(idxc, H, four):
+    g = gen(H)
+    kv, k = cache_rows(400, four, g), 200
+    q = bf16_rows(2 * H, g).view(2, H, 576)
+    topk = torch.stack([torch.randperm(400, generator=g)[:k] for _ in range(2)]).to(torch.int32)
+    lse = torch.empty((2, H))
+    start = torch.rand((2, 400), generator=g)
+    want, bound = start.double().numpy().copy(), np.zeros((2, 400))
+    off = torch.zeros((2, H), dtype=torch.bool)
+    off[0, H // 2] = True
+    off[1, 1:] = True
+    for b in range(2):
+        rows = kv[topk[b].long()]
+        _, l, _, reach, p = oracle_sequence(q[b:b + 1], rows, 0, k, 1, 0.05)
+        lse[b] = torch.from_numpy(l).float()
+        p = np.where(off[b].reshape(-1, 1).numpy(), 0.0, p)
+        want[b, topk[b].numpy()] += p.sum(axis=0)
+        bound[b, topk[b].numpy()] = weights_bound(p, reach, H)
+    q[off], lse[off] = float("nan"), float("-inf")
+    acc = start.clone().to(DEV)
+    idxc.attention_weights(q.to(DEV), kv.to(DEV), lse.to(DEV), acc, 0.05, topk=topk.to(DEV))
+    assert np.all(np.abs(acc.double().cpu().numpy() - want) <= bound + 2.0 ** -23 * want)
