@@ -389,7 +389,8 @@ idxc_status idxc_sparse_attention_q4(const void* q, const void* kv_q4, const int
  *                          twice is added twice.
  * Tokens whose lse is -inf add nothing.
  *   acc DEVICE fp32 [B, ld] (dense: ld >= max_len); lse DEVICE fp32 [B, n_step, H]; q, kv, kv_base, lens as above.
- * Every entry of acc is written by one thread; the sums do not depend on what else runs.
+ * Dense, and selected without repeats, every entry of acc is written by one thread. Threads that meet at a position which a selection
+ * names again all add the same number, atomically, so that their order does not show. The sums repeat bit for bit.
  * ------------------------------------------------------------------------- */
 idxc_status idxc_attention_weights(const void* q, const void* kv, idxc_latent_format fmt, int64_t n_kv, const int64_t* kv_base,
                                    const int32_t* lens, const int32_t* topk, int k_top, int64_t B, int n_step,

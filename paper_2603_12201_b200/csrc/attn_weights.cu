@@ -2,7 +2,8 @@
 //     acc[b, s] = beta acc[b, s] + sum_r exp(scale <q_r, row_s> - lse_r)        r = (new token, head)
 // A score product with an exponential and a row sum behind it, no second product. The cache rows are the M of the MMAs (128 a tile), the
 // query rows the N, so a thread of the epilogue owns one position and sums over its accumulator row: no exchange between
-// threads, one writer per entry. Q stays in shared memory; the row blocks [128 rows x 128 B] stream through a ring of four, so
+// threads, one writer per entry (of a selection's entries that name a position again each adds the same number: same row, same order of
+// every sum). Q stays in shared memory; the row blocks [128 rows x 128 B] stream through a ring of four, so
 // a tile's scores start with its first 64 columns. HBM-bound with bf16 rows: 64 KB of the ring in flight per SM; the MMAs of a tile take
 // 2300 clocks at 128 query rows (64 each), the bytes of a tile 6400 at the copy rate.
 // bf16 rows of a sequence come by TMA, selected bf16 rows by 16-byte asynchronous copies, 4-bit rows through the registers of eight warps.

@@ -276,3 +276,33 @@ def test_heads_without_a_log_sum_exp_add_nothing_to_a_selection(idxc, H, four):
     acc = start.clone().to(DEV)
     idxc.attention_weights(q.to(DEV), kv.to(DEV), lse.to(DEV), acc, 0.05, topk=topk.to(DEV))
     assert np.all(np.abs(acc.double().cpu().numpy() - want) <= bound + 2.0 ** -23 * want)
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H", [5, 40, 128])
+def test_a_position_named_again_adds_the_same_number_in_any_order(idxc, H, four):
+    """Several threads add to a position that a selection names several times, but all of them the same number: the sum is that of
+    repeated fp32 additions, whichever tile, lane or block an entry falls to, and the same in every run."""
+    g = gen(H + four)
+    n, B, k = 3000, 3, 2001                              # the last tile is not full: its sums take the masked path
+    kv = cache_rows(n, four, g).to(DEV)
+    q = bf16_rows(B * H, g, 2.0).view(B, H, 576).to(DEV)
+    once = torch.stack([torch.randperm(n, generator=g)[:40] for _ in range(B)])
+    lse = torch.empty((B, H))
+    for b in range(B):
+        lse[b] = torch.from_numpy(oracle_sequence(q[b:b + 1].cpu(), kv[once[b].to(DEV)].cpu(), 0, 40, 1, 0.05)[1]).float()
+    lse = lse.to(DEV)
+    added = torch.zeros((B, n), device=DEV)
+    idxc.attention_weights(q, kv, lse, added, 0.05, topk=once.to(torch.int32).to(DEV))
+    added = added.cpu().numpy()                          # (0 + w is w)
+    times = torch.randint(0, 40, (B, k), generator=g)
+    topk = torch.gather(once, 1, times).to(torch.int32)
+    start = torch.rand((B, n), generator=g) * 100.0
+    want = start.numpy().copy()
+    for b in range(B):
+        for j in topk[b].tolist():
+            want[b, j] = np.float32(want[b, j] + added[b, j])
+    for _ in range(5):
+        acc = start.clone().to(DEV)
+        idxc.attention_weights(q, kv, lse, acc, 0.05, topk=topk.to(DEV))
+        assert np.array_equal(acc.cpu().numpy(), want)
