@@ -331,6 +331,7 @@ idxc_status idxc_sparse_attention(const void* q, const void* kv, const int32_t* 
  * at least max|x| / 7 (and at least 2^-100, at most 1.3125 * 2^123, where codes end at +-7); code = x / scale rounded to nearest, ties to even. Positional columns are copied.
  *   x         [n_tokens, 576] bf16, 16-byte aligned
  *   cache     [cache_rows, 416] bytes
+ *   n_tokens  at most 2^31 (n_rows below as well)
  *   dst_rows  NULL: token r is written at row r (n_tokens <= cache_rows). Otherwise DEVICE int64 [n_tokens]: token r is
  *             written at row dst_rows[r]; a row outside [0, cache_rows) is not written. The rows must be distinct.
  * idxc_dequantize_q4 -- the values that rows stand for: out [n_rows, 576] bf16, row r from cache row src_rows[r] (NULL: r);
@@ -403,13 +404,13 @@ idxc_status idxc_attention_weights(const void* q, const void* kv, idxc_latent_fo
  * idxc_evict_select -- the positions that stay. Sequence b has n = lens[b] positions (clamped to [0, ld]). n <= budget: all
  * of them. Otherwise the last `recent` ones and the budget - recent of the others with the largest acc[b, s], ties to the
  * lowest position. keep_out [B, budget] int32: ascending, padded with -1 (the format of topk_out: it can be passed to the
- * sparse attention as it is); new_lens_out [B] int32: min(n, budget). 0 <= recent <= budget, 1 <= budget <= 2^30. NaN in
- * acc: some positions are chosen, within range. new_lens_out must not be lens.
+ * sparse attention as it is); new_lens_out [B] int32: min(n, budget). 0 <= recent <= budget, 1 <= budget <= 2^30,
+ * ld <= 2^30, B <= 65535. NaN in acc: some positions are chosen, within range. new_lens_out must not be lens.
  *
  * idxc_compact_rows -- brings the rows that stay together: for j < n_keep[b], row dst_base[b] + j of dst becomes row
- * src_base[b] + keep[b, j] of src. row_bytes is any multiple of 4 (bf16 or 4-bit latent rows, indexer keys, scales, the
- * sums themselves with src_base[b] = b * ld). keep [B, ld_keep], ld_keep <= 2^30; an entry that names no row of src, or
- * whose place is no row of dst, moves nothing.
+ * src_base[b] + keep[b, j] of src. row_bytes is any multiple of 4 up to 2^20 (bf16 or 4-bit latent rows, indexer keys, scales,
+ * the sums themselves with src_base[b] = b * ld); B <= 65535, src_rows and dst_rows <= 2^40. keep [B, ld_keep], ld_keep <= 2^30;
+ * an entry that names no row of src, or whose place is no row of dst, moves nothing.
  *   dst == src (then dst_base must be src_base): in place. keep[b] must be ascending without repeats, as written by
  *   idxc_evict_select; entries that are not at or behind their own place are skipped. Sequences must not share rows.
  *   Otherwise the two buffers must not overlap.

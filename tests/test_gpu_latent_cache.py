@@ -243,3 +243,28 @@ def test_compaction_from_bases_far_outside_moves_nothing(idxc, shape, dtype):
     idxc.compact_rows(src, dst, keep[:1], n[:1], base, torch.zeros_like(base))
     want[2] = before[2]
     assert torch.equal(dst, want)
+
+
+def test_choice_and_compaction_at_their_limits(idxc):
+    """65535 sequences, and rows of 2^20 bytes."""
+    B, ld, budget = 65535, 5, 3
+    acc = torch.rand((B, ld), generator=gen(1)).to(DEV)
+    lens = torch.randint(0, ld + 1, (B,), generator=gen(2), dtype=torch.int32).to(DEV)
+    keep, new = torch.empty((B, budget), dtype=torch.int32, device=DEV), torch.empty((B,), dtype=torch.int32, device=DEV)
+    idxc.evict_select(acc, lens, budget, 1, keep, new)
+    base = torch.arange(B, device=DEV) * ld
+    moved = acc.clone().view(-1)
+    idxc.compact_rows(moved, moved, keep, new, base)
+    moved, k = moved.view(B, ld).cpu().numpy(), keep.cpu().numpy()
+    for b in list(range(0, B, 997)) + [B - 1]:
+        want = oracle.evict(acc[b].cpu().numpy(), int(lens[b]), budget, 1)
+        assert int(new[b]) == len(want) and np.array_equal(k[b, :len(want)], want)
+        assert np.array_equal(moved[b, :len(want)], acc[b].cpu().numpy()[want])
+    src = torch.randint(0, 2 ** 31 - 1, (9, 2 ** 18), generator=gen(3), dtype=torch.int32).to(DEV)
+    pick = torch.tensor([[0, 3, 4, 8]], dtype=torch.int32, device=DEV)
+    zero, n = torch.zeros(1, dtype=torch.int64, device=DEV), torch.tensor([4], dtype=torch.int32, device=DEV)
+    dst = torch.zeros((4, 2 ** 18), dtype=torch.int32, device=DEV)
+    idxc.compact_rows(src, dst, pick, n, zero)
+    assert torch.equal(dst, src[pick[0].long()])
+    idxc.compact_rows(src, src, pick, n, zero)
+    assert torch.equal(src[:4], dst)

@@ -124,3 +124,13 @@ def test_compaction_refuses_more_entries_than_it_can_count(idxc):
     for dst, base in ((P, P), (far, P)):
         for ld_keep in (2 ** 30 + 1, 2 ** 31 - 1):
             assert L.idxc_compact_rows(P, dst, 4, 2 ** 32, 2 ** 32 if dst is P else 8, P, base, P, ld_keep, P, 1, None) == idxc.ERR_INVALID_ARG
+
+
+def test_sizes_beyond_the_documented_limits(idxc):
+    L, bad, Q, far = idxc.lib(), idxc.ERR_INVALID_ARG, ctypes.c_void_p(8192), ctypes.c_void_p(1 << 52)
+    assert L.idxc_quantize_q4(P, 2 ** 31 + 1, P, 2 ** 40, None, None) == bad
+    assert L.idxc_dequantize_q4(P, 2 ** 40, None, 2 ** 31 + 1, P, None) == bad
+    for ld, B, budget in ((2 ** 30 + 1, 1, 4), (10, 65536, 4), (10, 1, 2 ** 30 + 1)):
+        assert L.idxc_evict_select(P, ld, P, B, budget, 0, P, Q, None) == bad
+    for rb, sr, dr, B in ((2 ** 20 + 4, 8, 8, 1), (16, 8, 8, 65536), (16, 2 ** 40 + 1, 8, 1), (16, 8, 2 ** 40 + 1, 1)):
+        assert L.idxc_compact_rows(P, far, rb, sr, dr, P, Q, P, 4, P, B, None) == bad
