@@ -361,7 +361,8 @@ idxc_status idxc_dequantize_q4(const void* cache, int64_t cache_rows, const int6
  * B * (n_step * H rounded up to 64s) * max_len below 2^42.
  * Rows that no token sees do not influence the result, whatever they hold (some behind a sequence's end are read). A sequence's newest
  * n_step - 1 rows, which some of its tokens see and others do not, meet the others with weight 0 and have to be finite. A visible score that
- * is no number makes its row of out and lse none, as in the formula. Arithmetic: bf16
+ * is no number makes its row of out and lse none, as in the formula; a token all of whose visible scores are -inf is as one that sees
+ * nothing. Arithmetic: bf16
  * products with fp32 accumulation, fp32 softmax, probabilities rounded to bf16 for the second product, bf16 output. The result
  * does not depend on what else runs.
  *

@@ -306,3 +306,35 @@ def test_a_position_named_again_adds_the_same_number_in_any_order(idxc, H, four)
         acc = start.clone().to(DEV)
         idxc.attention_weights(q, kv, lse, acc, 0.05, topk=topk.to(DEV))
         assert np.array_equal(acc.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("H,n", [(16, 70), (16, 9000), (128, 70), (128, 9000)])
+def test_scores_of_minus_infinity(idxc, H, n, four):
+    """They have no weight; a token all of whose scores are -inf is as one that sees nothing, in a sequence that is cut as in one that is not."""
+    g = gen(H + n)
+    kv = cache_rows(2 * n, four, g)
+    low = torch.zeros(2 * n, dtype=torch.bool)
+    low[:n:3] = True
+    low[n - 200 if n > 200 else 0:n] = True              # the first sequence's last rows, a whole tile and more; every row of the second
+    low[n:] = True
+    if n == 70:
+        low[:64] = False
+    rows = torch.nonzero(low)[:, 0]
+    if four:
+        kv[rows, 288 + 2 * 7], kv[rows, 288 + 2 * 7 + 1] = 0x80, 0xFF
+    else:
+        kv[rows, 512 + 7] = float("-inf")
+    q = bf16_rows(2 * H, g, 0.5).view(2, 1, H, 576)
+    q[..., 512 + 7] = 0.5
+    out, lse = idxc.latent_attention(q.to(DEV), kv.to(DEV), torch.tensor([0, n], device=DEV), torch.tensor([n, n], dtype=torch.int32, device=DEV), n, 512, 1 / 24)
+    assert bool((out[1] == 0).all()) and bool(torch.isneginf(lse[1]).all())
+    seen = torch.nonzero(~low[:n])[:, 0]
+    check_attention(out[0, 0], lse[0, 0], *oracle_sequence(q[0], kv[seen], 0, len(seen), 1, 1 / 24)[:4])
+    if four:
+        topk = torch.stack([torch.randperm(n, generator=g), torch.randperm(n, generator=g)])[:, :min(n, 2048)].to(torch.int32)
+        out, lse = idxc.sparse_attention_q4(q[:, 0].contiguous().to(DEV), kv.to(DEV), topk.to(DEV), 512, 1 / 24, kv_base=torch.tensor([0, n], device=DEV))
+        assert bool((out[1] == 0).all()) and bool(torch.isneginf(lse[1]).all())
+        pick = topk[0].long()
+        pick = pick[~low[pick]]
+        check_attention(out[0], lse[0], *oracle_sequence(q[:1, 0], kv[pick], 0, len(pick), 1, 1 / 24)[:4])
