@@ -268,3 +268,35 @@ def test_choice_and_compaction_at_their_limits(idxc):
     assert torch.equal(dst, src[pick[0].long()])
     idxc.compact_rows(src, src, pick, n, zero)
     assert torch.equal(src[:4], dst)
+
+
+@pytest.mark.parametrize("binade", [0, -95, 60])
+def test_quantize_every_quotient(idxc, binade):
+    """Every bf16 magnitude of both signs that a 5-bit scale holds, down to 1/64 of the scale's binade, under all sixteen scales of a binade:
+    31 values a group, and in the last column 7 steps, which make the scale."""
+    m = torch.arange(128, 256, dtype=torch.float64) / 128.0
+    mags = torch.cat([m * 2.0 ** e for e in range(-6, 4)])
+    groups, scales, pairs = [], [], 0
+    for s in range(16, 32):
+        v = mags[mags <= 7 * s / 16]
+        pairs += v.numel()
+        v = torch.cat([v, -v])
+        v = torch.cat([v, torch.zeros(-v.numel() % 31, dtype=torch.float64)]).view(-1, 31)
+        groups.append(torch.cat([v, torch.full((v.shape[0], 1), 7 * s / 16, dtype=torch.float64)], dim=1))
+        scales += [s / 16] * v.shape[0]
+    rows = -(-len(scales) // 16)
+    scales += [1.0] * (16 * rows - len(scales))
+    last = torch.zeros((16 * rows, 32), dtype=torch.float64)
+    last[:, 31] = 7.0
+    every = torch.cat(groups)
+    last[:every.shape[0]] = every
+    x = torch.cat([last.view(rows, 512), torch.zeros((rows, 64), dtype=torch.float64)], dim=1) * 2.0 ** binade
+    assert torch.equal(x.to(torch.bfloat16).double(), x)
+    cache = torch.empty((rows, 416), dtype=torch.uint8, device=DEV)
+    idxc.quantize_q4(x.to(torch.bfloat16).to(DEV), cache)
+    got = cache.cpu()
+    stored_scales = got[:, 256:288].contiguous().view(torch.bfloat16).double().reshape(-1)
+    assert torch.equal(stored_scales, torch.tensor(scales, dtype=torch.float64) * 2.0 ** binade)
+    met = torch.stack([torch.tensor(scales, dtype=torch.float64).repeat_interleave(31), (x[:, :512].reshape(-1, 32)[:, :31] * 2.0 ** -binade).reshape(-1)])
+    assert torch.unique(met[:, met[1] != 0], dim=1).shape[1] == 2 * pairs
+    assert np.array_equal(got.numpy(), oracle.quantize_rows(x.numpy()))
