@@ -79,11 +79,8 @@ __device__ __forceinline__ EarlyTiles early_tiles(uint32_t units, const UnitTile
 // Brings the first 4 KB of kv_base to the L1 (every role loads its sequence's when it starts).
 __device__ __forceinline__ void early_bases(const int64_t* kv_base, int64_t B) {
     const int64_t at = 16 * static_cast<int64_t>(threadIdx.x & 31);
-    if (kv_base != nullptr && at < B) {
-        int64_t x;
-        asm volatile("ld.global.nc.b64 %0, [%1];" : "=l"(x) : "l"(kv_base + at));
-        static_cast<void>(x);
-    }
+    if (kv_base != nullptr && at < B)
+        asm volatile("{\n\t.reg .b64 x;\n\tld.global.nc.b64 x, [%0];\n\t}" ::"l"(kv_base + at));
 }
 struct Run {
     uint32_t unit;        // where it begins

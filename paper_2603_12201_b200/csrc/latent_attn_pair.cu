@@ -572,7 +572,7 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
             const int n_rows = rows_of(pc.unit, seq, r0);
             if (ROWS == kCodes) {
                 // Q's first blocks: this thread's row (both lane halves hold it) to tensor memory; the scores of the last piece are done. Rows
-                // that are not ours stay what they were: they only reach scores of rows that nobody reads.
+                // that are not ours become zeros: they only reach scores of rows that nobody reads.
                 const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.a.q) + (seq * seq_rows + r0 + row) * (kLatentCols * 2));
                 auto load_block = [&](int b, uint32_t (&r)[32]) {
 #pragma unroll
