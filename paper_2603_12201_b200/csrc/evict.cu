@@ -1,12 +1,12 @@
 // Which cached positions of a sequence stay when its cache is cut to a budget: the newest `recent` ones, and among the older
 // ones the budget - recent with the largest accumulated attention weight (ties: lowest position), in ascending order.
-// A cluster of eight CTAs takes a sequence, each an eighth of its positions, whose keys stay in shared memory (up to 48K positions a
+// A cluster of eight CTAs (or one, see the launch) takes a sequence, each an eighth of its positions, whose keys stay in shared memory (up to 48K positions a
 // CTA; longer slices are read from global memory again). Three histogram passes (11 + 11 + 10 bits of an order-preserving key) find the
 // key of the last position that stays exactly. The CTAs' counts are added up through distributed shared memory by one warp each, 64 bins at
 // a time first and then the bins of one such group: 3 KB a pass, where all bins of all CTAs took 5000 clocks. Then every
 // position's place in the output is the number of positions before it that stay, by prefix sums over lanes, warps and CTAs: no
 // atomics on the output, ascending order for free. Bound by latency (five cluster barriers, and sweeps of a few microseconds that are
-// instructions, not bytes): 8 sequences of 131072 positions 19 us, 24 of 900 to 6000 12 us.
+// instructions, not bytes): 8 sequences of 131072 positions 16 us, 24 of 6007 7 us (replayed back to back; 19 and 12 with cold caches).
 #include "kernels.h"
 #include "ptx_sm100.cuh"
 
@@ -15,8 +15,7 @@ namespace {
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
-constexpr int kEvCtas = 8;                           // CTAs of a long sequence (short ones, up to kEvShort positions a row of acc: one)
-constexpr int kEvShort = 16384;
+constexpr int kEvCtas = 8;                           // CTAs of a sequence, or one: see one_cta_each
 constexpr int kEvBins = 2 * kEvThreads;               // 2048, two a thread
 constexpr int kEvKeys = 49152;                       // keys of a slice that fit into shared memory at most
 constexpr uint32_t kEvHistBytes = 2 * kEvBins * 4;
@@ -259,10 +258,24 @@ static cudaError_t launch_as(const float* acc, int64_t ld, const int32_t* lens, 
     return cudaLaunchKernelEx(&cfg, evict_select_kernel<CTAS>, acc, ld, lens, budget, recent, slots, keep, new_lens);
 }
 
+// One CTA a sequence or a cluster of eight. A cluster costs about 4 us more to start and sweeps eight times as fast, but few clusters run at a time.
+// Measured (us, one CTA | cluster; B sequences of ld positions, a quarter kept):
+//   ld       B = 1         24            54            148           149
+//   8192     8.3 |  8.5    8.4 | 11.0    8.4 | 20.8    8.6 | 49.3   13.9 | 49.6
+//   16384   12.5 |  8.7   12.6 | 12.0   12.7 | 23.1   12.9 | 53.6   22.1 | 53.9
+//   49152   29.0 | 10.9   29.5 | 15.8   29.5 | 30.5   29.7 | 71.6   56.9 | 72.2
+//   65536   61.1 | 11.6   61.8 | 19.4   61.9 | 36.0   62.1 | 81.4  121.7 | 82.2      (the keys no longer fit one CTA's shared memory)
+//   131072   117 | 16.0    118 | 29.6    118 | 52.4    127 | 124     236 | 125
+// The border rises by about 512 positions with every sequence that runs at the same time as the others.
+static bool one_cta_each(int64_t ld, int B) {
+    const int waves = (B + 147) / 148;
+    return ld <= 8192 + 512 * static_cast<int64_t>(B / waves);
+}
+
 cudaError_t launch_evict_select(const float* acc, int64_t ld, const int32_t* lens, int B, int budget, int recent, int32_t* keep,
                                 int32_t* new_lens, cudaStream_t stream) {
-    return ld <= kEvShort ? launch_as<1>(acc, ld, lens, B, budget, recent, keep, new_lens, stream)
-                          : launch_as<kEvCtas>(acc, ld, lens, B, budget, recent, keep, new_lens, stream);
+    return one_cta_each(ld, B) ? launch_as<1>(acc, ld, lens, B, budget, recent, keep, new_lens, stream)
+                               : launch_as<kEvCtas>(acc, ld, lens, B, budget, recent, keep, new_lens, stream);
 }
 
 }  // namespace idxc

@@ -300,3 +300,18 @@ def test_quantize_every_quotient(idxc, binade):
     met = torch.stack([torch.tensor(scales, dtype=torch.float64).repeat_interleave(31), (x[:, :512].reshape(-1, 32)[:, :31] * 2.0 ** -binade).reshape(-1)])
     assert torch.unique(met[:, met[1] != 0], dim=1).shape[1] == 2 * pairs
     assert np.array_equal(got.numpy(), oracle.quantize_rows(x.numpy()))
+
+
+@pytest.mark.parametrize("B,ld", [(1, 8704), (1, 8705), (37, 27136), (37, 27137), (148, 60000), (148, 83969), (149, 46081), (300, 9000)])
+def test_select_on_both_sides_of_its_rule(idxc, B, ld):
+    """One block a sequence or eight, with keys that fit one block's shared memory and keys that do not."""
+    g = gen(B + ld)
+    lens = [ld - 13 * (b % 5) for b in range(B)]
+    acc = torch.rand((B, ld), generator=g) ** 12
+    acc[:, ::3] = 0.0                                    # ties, more of them than stay
+    budget = ld // 3
+    keep, new = select(idxc, acc, lens, budget, 100)
+    for b in sorted({0, 1 % B, B // 2, B - 1}):
+        want = oracle.evict(acc[b].numpy(), lens[b], budget, 100)
+        assert new[b] == budget and np.array_equal(keep[b], want)
+    assert np.all(np.diff(keep, axis=1) > 0) and np.all(new == budget)
