@@ -329,6 +329,7 @@ idxc_status idxc_sparse_attention(const void* q, const void* kv, const int32_t* 
  *
  * idxc_quantize_q4 -- rows of bf16 into a 4-bit cache: a group's scale is the smallest number of 5 significant bits that is
  * at least max|x| / 7 (and at least 2^-100, at most 1.3125 * 2^123, where codes end at +-7); code = x / scale rounded to nearest, ties to even. Positional columns are copied.
+ * Value columns are assumed finite: one that is not spoils its own group of 32, which then stands for finite numbers.
  *   x         [n_tokens, 576] bf16, 16-byte aligned
  *   cache     [cache_rows, 416] bytes
  *   n_tokens  at most 2^31 (n_rows below as well)
@@ -389,7 +390,7 @@ idxc_status idxc_sparse_attention_q4(const void* q, const void* kv_q4, const int
  *   selected (topk = [B, k_top] int32, n_step == 1, beta == 1, lens == NULL): acc[b, topk[b,j]] += sum_h exp(x - lse[b,h]) for
  *                          every usable entry (0 <= topk[b,j] < ld and its cache row inside [0, n_kv)); a position named
  *                          twice is added twice.
- * Tokens whose lse is -inf add nothing.
+ * Tokens whose lse is -inf add nothing. More than 128 query rows (n_step * H) are taken 128 at a time, and the cache is read for each.
  *   acc DEVICE fp32 [B, ld] (dense: ld >= max_len); lse DEVICE fp32 [B, n_step, H]; q, kv, kv_base, lens as above.
  * Dense, and selected without repeats, every entry of acc is written by one thread. Threads that meet at a position which a selection
  * names again all add the same number, atomically, so that their order does not show. The sums repeat bit for bit.

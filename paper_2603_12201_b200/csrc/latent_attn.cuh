@@ -19,7 +19,9 @@ __device__ __forceinline__ long long piece_budget(int tiles) { return kWaitCycle
 __device__ __forceinline__ int64_t first_row(const LatentArgs& a, int64_t b) { return a.kv_base ? near_base(__ldg(a.kv_base + b), a.n_kv) : 0; }
 constexpr float kMoveThreshold = 8.f;               // log2 units: probabilities stay below 2^8 of the reference
 
-// Tiles of a unit: counted beforehand, or from its sequence's length (no lengths: max_len for all).
+// Tiles of a unit: counted beforehand, or from its sequence's length (no lengths: max_len for all). A unit of a prompt chunk walks all tiles of its
+// sequence, those behind its last token's position too: their scores are masked away. (Units that stop there had half the tiles of a whole prompt and were no
+// faster, 1061 -> 1088 us for 2048 tokens: equal runs of tiles then give short units to the first groups, and each costs a piece's end.)
 struct UnitTiles {
     const int32_t* counted;      // [units] or nullptr
     const int32_t* lens;

