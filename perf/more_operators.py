@@ -521,7 +521,7 @@ def exact(case, seed):
         for name in ("k", "v"):
             x = s["new_" + name].double()
             if s[name + "_scale"] is not None:
-                scale = (s["new_" + name].float().abs().amax(dim=-1).clamp_min(1e-12) / 448.0)[..., None]
+                scale = (s["new_" + name].float().abs().amax(dim=-1).clamp_min(1e-12).double() / 448.0).float()[..., None]
                 code = (s["new_" + name].float() / scale).to(torch.float8_e4m3fn).double()
                 s[name + "_scale"][slots // P, :, slots % P] = scale[..., 0]
                 s[name].view(torch.uint8)[slots // P, slots % P] = code.to(torch.float8_e4m3fn).view(torch.uint8)
@@ -539,7 +539,7 @@ def exact(case, seed):
             for p0 in range(0, pages.numel(), 4096):
                 pg = pages[p0:p0 + 4096]
                 at = (pg[:, None] * P + torch.arange(P, device=DEV)).reshape(-1)
-                rows = _rows64(s, "k", at, head).to(BF16).double().reshape(pg.numel(), P, -1)
+                rows = _rows64(s, "k", at, head).reshape(pg.numel(), P, -1)
                 inside = (torch.arange(P, device=DEV)[None, :] <= upto[p0:p0 + 4096, None])[:, :, None]
                 bounds[pg, head, 0] = torch.where(inside, rows, math.inf).amin(dim=1)
                 bounds[pg, head, 1] = torch.where(inside, rows, -math.inf).amax(dim=1)
