@@ -424,6 +424,107 @@ idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t
                               const int64_t* src_base, const int64_t* dst_base, const int32_t* keep, int ld_keep,
                               const int32_t* n_keep, int64_t B, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Serving from a paged key/value cache. (The paper has no counterpart: its serving system keeps its caches in pages. These calls keep the
+ * pages, write and read them, and attend over them, whole or over the pages that a score selects.)
+ *
+ * A page holds P = page_size positions of a request. Request b's logical page p is physical page table[b, p]; the slot of a position s is
+ * table[b, s / P] * P + s % P: the row of that position in a cache of n_pages * P rows. Slots are the dst_rows of idxc_quantize_e4m3 and
+ * idxc_quantize_q4, so indexer keys and latent rows are appended to paged caches by the calls that are there.
+ *   table    DEVICE int32 [B, ld_table]; entries behind a request's pages are not looked at
+ *   lens     DEVICE int32 [B], positions of every request (negative: 0)
+ *   page_size a multiple of 16, 16 .. 1024; B <= 65535; B * ld_table < 2^31
+ *
+ * idxc_page_tables -- pages and slots for the new tokens of a batch of requests. Request b wants n = new_tokens[b] positions more, and so
+ * ceil((lens[b] + n) / P) - ceil(lens[b] / P) pages, which are taken from the top of the stack free_pages[0 .. *free_count - 1]: in the order of
+ * requests and of their pages, free_pages[count - 1] first. A request is refused, and all behind it, when the stack does not hold what it and
+ * those in front of it want, when its pages would not fit ld_table, or its tokens not n_slots. For a request that is served, the table gets its pages, lens[b]
+ * grows by n, and start_out[b] is its length before; for one that is refused start_out[b] = -1 and nothing changes.
+ *   free_pages DEVICE int32 [free_capacity] (read), free_count DEVICE int32 [1] (taken as at most free_capacity; lowered by the pages taken)
+ *   token_begin_out DEVICE int32 [B + 1]: tokens in front of each request, refused ones included (sums above 2^31 - 1 are given as that)
+ *   slots_out DEVICE int64 [n_slots]: token j of request b at token_begin_out[b] + j; -1 for tokens of refused requests and behind the last token
+ *   seq_out   NULL or DEVICE int32 [n_slots]: the token's request, -1 behind the last token
+ * idxc_page_release -- requests cut to their first keep_lens[b] positions (NULL or negative: 0, finished requests): lens[b] = min(lens[b], keep_lens[b]), and the pages that
+ * hold none of them return to the stack, in the reverse of the order above, so that giving back what idxc_page_tables has just handed out leaves the
+ * stack as it was. Their table entries become -1. Pages for which the stack has no room (free_capacity) are dropped.
+ * idxc_page_rows -- positions (such as topk_out) as rows of a paged cache: out[r, j] = the slot of positions[r, j] in the request of row r, which is seq[r] (NULL: r);
+ * -1 for positions below 0 or behind the table, for table entries below 0 and for requests outside [0, B). The rows serve idxc_sparse_attention
+ * and idxc_sparse_attention_q4 over a paged latent cache with kv_base = NULL. positions, out: DEVICE int32 [n_rows, k]; out may be positions.
+ * ------------------------------------------------------------------------- */
+idxc_status idxc_page_tables(int32_t* table, int64_t ld_table, int32_t* lens, const int32_t* new_tokens, int64_t B, int page_size,
+                             const int32_t* free_pages, int64_t free_capacity, int32_t* free_count, int32_t* token_begin_out, int32_t* start_out,
+                             int64_t* slots_out, int64_t n_slots, int32_t* seq_out, void* cuda_stream);
+idxc_status idxc_page_release(int32_t* table, int64_t ld_table, int32_t* lens, const int32_t* keep_lens, int64_t B, int page_size,
+                              int32_t* free_pages, int64_t free_capacity, int32_t* free_count, void* cuda_stream);
+idxc_status idxc_page_rows(const int32_t* table, int64_t ld_table, int64_t B, const int32_t* seq, const int32_t* positions, int64_t n_rows, int k,
+                           int page_size, int32_t* out, void* cuda_stream);
+
+/* A paged cache of keys and values, [n_pages, page_size, H_kv, d] by strides in elements (so either order of tokens and heads, and keys and values side
+ * by side in one array). HOST struct of DEVICE pointers.
+ *   IDXC_BF16      k, v bf16; no scales
+ *   IDXC_FP8_E4M3  k, v e4m3 codes; k_scale, v_scale fp32 [n_pages, H_kv, page_size], value = code * scale (16-byte aligned). Value scales are
+ *                  positive and at most 2^60.
+ *   bounds         NULL, or bf16 [n_pages, H_kv, 2, d], 16-byte aligned: the smallest (0) and largest (1) value of every key column of a page
+ * d in {64, 128}; k, v 16-byte aligned, strides multiples of 16 bytes, at least 16 bytes and below 2^39 bytes; 1 <= H_kv <= 1024; n_pages * page_size < 2^31. */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    void* bounds;
+    int64_t n_pages;
+    int64_t page_stride, token_stride, head_stride;
+    int32_t page_size, H_kv, d;
+    int32_t dtype;               /* idxc_dtype */
+} idxc_paged_cache;
+
+/* ---------------------------------------------------------------------------
+ * idxc_paged_append -- keys and values of n tokens written to their slots (a slot outside the cache: not written; slots distinct). In 8 bits every
+ * (token, head) gets scale = max(max|x|, 1e-12) / 448 and codes as idxc_quantize_e4m3 writes them. With bounds, those of every page written to
+ * become the bounds of its rows 0 .. the last one written, as they read back in bf16. For that, the tokens of one page follow each other, in ascending slots
+ * without gaps (as idxc_page_tables gives them), and its rows in front of them hold the request's earlier tokens.
+ *   k, v     DEVICE bf16 [n, H_kv, d], 16-byte aligned, k_stride and v_stride elements between tokens (multiples of 8, at least H_kv * d: a projection's
+ *            output may hold queries, keys and values side by side)
+ * idxc_paged_gather -- rows read back: k_out, v_out DEVICE bf16 [n, H_kv, d] without gaps, 16-byte aligned; zeros for slots outside the cache.
+ * n * H_kv * d < 2^40.
+ * ------------------------------------------------------------------------- */
+idxc_status idxc_paged_append(const idxc_paged_cache* cache /* HOST */, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                              const int64_t* slots, int64_t n, void* cuda_stream);
+idxc_status idxc_paged_gather(const idxc_paged_cache* cache /* HOST */, const int64_t* slots, int64_t n, void* k_out, void* v_out, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention of new tokens over their requests' pages: query head h reads key head h / (H / H_kv); for request b and its new token i of n_step
+ *     n(b, i)      = lens[b] - (n_step - 1 - i)                  (the new tokens are the last n_step positions, and are in the cache)
+ *     x[s]         = scale * < q[b, i, h, :], k[s] >             for 0 <= s < n(b, i)
+ *     out[b, i, h] = sum_s Softmax(x)[s] * v[s],    lse[b, i, h] = log sum_s exp(x[s])
+ * With pages (DEVICE int32 [B, H_kv, n_sel], the format of topk_out: logical pages first, then -1) only positions of the pages named by the first
+ * min(n_sel, ceil(lens[b] / P)) entries of (b, key head) take part; entries below 0 or behind the request's pages are skipped, a page named twice
+ * counts twice. Positions whose page is no page of the cache take no part. A token that sees nothing gets out = 0 and lse = -inf.
+ *   q        DEVICE bf16 [B, n_step, H, d], 16-byte aligned; q_stride elements between tokens (a multiple of 8, at least H * d)
+ *   max_len  HOST bound on lens (longer ones are cut to it), at most ld_table * page_size and 2^30
+ *   out      DEVICE bf16 [B, n_step, H, d], 16-byte aligned; lse NULL or DEVICE fp32 [B, n_step, H]
+ *   workspace DEVICE, 256-byte aligned, idxc_paged_attention_workspace_bytes(n_step, H, H_kv, d) bytes; scratch, one per call in flight
+ * H a multiple of H_kv, H / H_kv <= 128, n_step <= 1024. Rows of a page that no token sees do not influence the result, whatever they hold. A
+ * request's newest n_step - 1 rows, which some of its tokens see and others do not, meet the others with weight 0 and have to be finite. A visible
+ * score that is no number makes its row of out and lse none. Arithmetic: bf16 products (8-bit rows: f16, exact codes, q as f16 times a power of two) with fp32
+ * accumulation, fp32 softmax, probabilities rounded to bf16 (f16) for the second product, bf16 output. The result does not depend on what else runs.
+ *
+ * idxc_page_scores -- the largest score that any key between a page's bounds could reach, for choosing pages:
+ *     scores[b * H_kv + g, p] = scale * max over i and the heads h of key head g of  sum_d max(q[b,i,h,d] * lo[d], q[b,i,h,d] * hi[d])
+ * for the pages p < n_pages_out[b * H_kv + g] = min(ceil(lens[b] / P), ld_table) of the request; other entries of the row are left as they are. The first keep_first
+ * and the last keep_last pages get 3e38, pages that are none of the cache's -3e38. With k_top pages wanted,
+ * idxc_topk_rows(scores, ld_scores, B * H_kv, 0, 0, n_pages_out, k_top, pages) gives the selection that idxc_paged_attention takes.
+ *   bounds   DEVICE bf16 [n_pages, H_kv, 2, d], 16-byte aligned; scores DEVICE fp32 [B * H_kv, ld_scores], ld_scores >= ld_table
+ *   scale    positive and finite
+ * ------------------------------------------------------------------------- */
+size_t idxc_paged_attention_workspace_bytes(int n_step, int H, int H_kv, int d);
+idxc_status idxc_paged_attention(const idxc_paged_cache* cache /* HOST */, const void* q, int64_t q_stride, const int32_t* table, int64_t ld_table,
+                                 const int32_t* lens, int64_t B, int n_step, int64_t max_len, int H, const int32_t* pages, int n_sel, float scale,
+                                 void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+idxc_status idxc_page_scores(const void* bounds, int64_t n_pages, int page_size, int H_kv, int d, const void* q, int64_t q_stride, const int32_t* table,
+                             int64_t ld_table, const int32_t* lens, int64_t B, int n_step, int H, int keep_first, int keep_last, float scale,
+                             float* scores, int64_t ld_scores, int32_t* n_pages_out, void* cuda_stream);
+
 /* Synchronises the stream, then returns IDXC_OK, IDXC_ERR_CUDA, or
  * IDXC_ERR_DEVICE_TIMEOUT if any kernel of this library recorded a bounded wait that
  * ran out since the last poll (the record is cleared). */

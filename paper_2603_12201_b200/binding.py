@@ -34,6 +34,8 @@ EXPORTED_SYMBOLS = [
     "idxc_pattern_search_greedy", "idxc_distill_kl", "idxc_sparse_attention_workspace_bytes", "idxc_sparse_attention",
     "idxc_quantize_q4", "idxc_dequantize_q4", "idxc_latent_attention_workspace_bytes", "idxc_latent_attention", "idxc_sparse_attention_q4",
     "idxc_attention_weights", "idxc_evict_select", "idxc_compact_rows",
+    "idxc_page_tables", "idxc_page_release", "idxc_page_rows", "idxc_paged_append", "idxc_paged_gather", "idxc_paged_attention_workspace_bytes",
+    "idxc_paged_attention", "idxc_page_scores",
 ]
 NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -122,6 +124,23 @@ def lib() -> ctypes.CDLL:
         L.idxc_evict_select.argtypes = [vp, i64, vp, i64, i32, i32, vp, vp, vp]
         L.idxc_compact_rows.restype = i32
         L.idxc_compact_rows.argtypes = [vp, vp, i32, i64, i64, vp, vp, vp, i32, vp, i64, vp]
+        f32 = ctypes.c_float
+        L.idxc_page_tables.restype = i32
+        L.idxc_page_tables.argtypes = [vp, i64, vp, vp, i64, i32, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+        L.idxc_page_release.restype = i32
+        L.idxc_page_release.argtypes = [vp, i64, vp, vp, i64, i32, vp, i64, vp, vp]
+        L.idxc_page_rows.restype = i32
+        L.idxc_page_rows.argtypes = [vp, i64, i64, vp, vp, i64, i32, i32, vp, vp]
+        L.idxc_paged_append.restype = i32
+        L.idxc_paged_append.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp]
+        L.idxc_paged_gather.restype = i32
+        L.idxc_paged_gather.argtypes = [vp, vp, i64, vp, vp, vp]
+        L.idxc_paged_attention_workspace_bytes.restype = sz
+        L.idxc_paged_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.idxc_paged_attention.restype = i32
+        L.idxc_paged_attention.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i64, i32, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.idxc_page_scores.restype = i32
+        L.idxc_page_scores.argtypes = [vp, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, f32, vp, i64, vp, vp]
         L.idxc_selftest_bounded_wait.restype = i32
         L.idxc_selftest_bounded_wait.argtypes = [u32, vp]
         L.idxc_selftest_tmem_readout.restype = i32
@@ -562,6 +581,213 @@ def compact_rows(src, dst, keep, n_keep, src_base, dst_base=None, stream=None):
     with guard:
         _check(lib().idxc_compact_rows(_at(src), _at(dst), row_bytes, src.shape[0], dst.shape[0], _at(src_base), _at(dst_base), _at(keep),
                                        ld_keep, _at(n_keep), B, stream), "idxc_compact_rows")
+
+
+# ------------------------------------------------------------------ paged key/value cache
+def page_tables(table, lens, new_tokens, free_pages, free_count, page_size, slots_out, token_begin_out, start_out, seq_out=None, stream=None):
+    """idxc_page_tables: pages for new_tokens[b] more positions of every request, taken from the stack free_pages[:free_count]. table [B, ld]
+    int32, lens [B] int32 and free_count [1] int32 are brought up to date in place; slots_out [n] int64 (and seq_out [n] int32) get one
+    entry per new token, requests one after the other, -1 behind the last; token_begin_out [B + 1] int32; start_out [B] int32: a request's length
+    before, or -1 if it is refused (the stack, the table or slots_out too small for it and those in front of it)."""
+    guard, stream = _launch_on(stream, table=table, lens=lens, new_tokens=new_tokens, free_pages=free_pages, free_count=free_count, slots_out=slots_out,
+                               token_begin_out=token_begin_out, start_out=start_out, seq_out=seq_out)
+    if table.dim() != 2 or free_pages.dim() != 1 or slots_out.dim() != 1:
+        raise ValueError("table must be [B, ld], free_pages [capacity] and slots_out [n]")
+    B, ld = table.shape
+    n = slots_out.shape[0]
+    _typed(table, "table", torch.int32); _typed(lens, "lens", torch.int32, (B,)); _typed(new_tokens, "new_tokens", torch.int32, (B,))
+    _typed(free_pages, "free_pages", torch.int32); _typed(free_count, "free_count", torch.int32, (1,)); _typed(slots_out, "slots_out", torch.int64)
+    _typed(token_begin_out, "token_begin_out", torch.int32, (B + 1,)); _typed(start_out, "start_out", torch.int32, (B,))
+    _typed(seq_out, "seq_out", torch.int32, (n,))
+    with guard:
+        _check(lib().idxc_page_tables(_at(table), ld, _at(lens), _at(new_tokens), B, int(page_size), _at(free_pages), free_pages.shape[0], _at(free_count),
+                                      _at(token_begin_out), _at(start_out), _at(slots_out), n, _at(seq_out), stream), "idxc_page_tables")
+
+
+def page_release(table, lens, keep_lens, free_pages, free_count, page_size, stream=None):
+    """idxc_page_release: every request cut to its first keep_lens[b] positions (None: 0); pages that hold none of them go back to the stack.
+    table, lens, free_pages and free_count change in place."""
+    guard, stream = _launch_on(stream, table=table, lens=lens, keep_lens=keep_lens, free_pages=free_pages, free_count=free_count)
+    if table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("table must be [B, ld] and free_pages [capacity]")
+    B, ld = table.shape
+    _typed(table, "table", torch.int32); _typed(lens, "lens", torch.int32, (B,)); _typed(keep_lens, "keep_lens", torch.int32, (B,))
+    _typed(free_pages, "free_pages", torch.int32); _typed(free_count, "free_count", torch.int32, (1,))
+    with guard:
+        _check(lib().idxc_page_release(_at(table), ld, _at(lens), _at(keep_lens), B, int(page_size), _at(free_pages), free_pages.shape[0], _at(free_count),
+                                       stream), "idxc_page_release")
+
+
+def page_rows(table, positions, page_size, out, seq=None, stream=None):
+    """idxc_page_rows: out [n, k] int32 = rows of a paged cache for positions [n, k] int32 of request seq[r] (None: r); -1 stays -1. With it
+    sparse_attention and sparse_attention_q4 read paged latent caches: topk = out, kv_base = None."""
+    guard, stream = _launch_on(stream, table=table, positions=positions, out=out, seq=seq)
+    if table.dim() != 2 or positions.dim() != 2:
+        raise ValueError("table must be [B, ld] and positions [n, k]")
+    n, k = positions.shape
+    _typed(table, "table", torch.int32); _typed(positions, "positions", torch.int32); _typed(out, "out", torch.int32, (n, k))
+    _typed(seq, "seq", torch.int32, (n,))
+    with guard:
+        _check(lib().idxc_page_rows(_at(table), table.shape[1], table.shape[0], _at(seq), _at(positions), n, k, int(page_size), _at(out), stream),
+               "idxc_page_rows")
+
+
+class _PagedCacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("bounds", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class PagedCache:
+    """idxc_paged_cache: keys and values [n_pages, page_size, H_kv, d] of one paged cache, bf16, or float8_e4m3fn with k_scale and v_scale
+    [n_pages, H_kv, page_size] fp32; optionally the pages' bounds [n_pages, H_kv, 2, d] bf16. k and v may be strided views with the same strides
+    (heads in front of tokens, keys and values interleaved), as long as the d columns lie side by side. Holds the tensors, copies nothing."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, bounds=None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be [n_pages, page_size, H_kv, d] of one type")
+        dt = _dtype_of(k)
+        n_pages, page_size, H_kv, d = k.shape
+        if not k.is_cuda:
+            raise ValueError("k must live on a CUDA device (this library has no CPU path)")
+        for name, t in (("v", v), ("k_scale", k_scale), ("v_scale", v_scale), ("bounds", bounds)):
+            if t is not None and t.device != k.device:
+                raise ValueError(f"{name} is on {t.device}, k is on {k.device}")
+        strides = []
+        for t in (k, v):
+            row, own = d, list(t.stride())
+            if own[3] != 1 and d > 1:
+                raise ValueError("the columns of k and v must lie side by side")
+            for axis in (2, 1, 0):              # an axis of length 1 may have any stride: it gets the one it would have without gaps
+                if t.shape[axis] == 1:
+                    own[axis] = row
+                row = max(row, own[axis] * t.shape[axis])
+            strides.append(own)
+        if strides[0] != strides[1]:
+            raise ValueError(f"k and v must have the same strides, got {k.stride()} and {v.stride()}")
+        if (dt == FP8_E4M3) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("float8_e4m3fn rows need k_scale and v_scale, bf16 rows have none")
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            _typed(t, name, torch.float32, (n_pages, H_kv, page_size))
+        _typed(bounds, "bounds", torch.bfloat16, (n_pages, H_kv, 2, d))
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale), ("bounds", bounds)):
+            if t is not None and not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        self.k, self.v, self.k_scale, self.v_scale, self.bounds = k, v, k_scale, v_scale, bounds
+        self.n_pages, self.page_size, self.H_kv, self.d = n_pages, page_size, H_kv, d
+        self.device_index = k.get_device()
+        self._c = _PagedCacheStruct(_at(k), _at(v), _at(k_scale), _at(v_scale), _at(bounds), n_pages, *strides[0][:3], page_size, H_kv, d, dt)
+        self._p = ctypes.addressof(self._c)
+
+
+def _token_stride(t, name, heads, d, index):
+    """Checks that t [..., heads, d] is bf16 on the device, with heads and columns side by side and one stride for all its tokens, and returns that stride."""
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the cache is on cuda:{index}")
+    shape, stride = t.shape, t.stride()
+    if shape[-2:] != (heads, d):
+        raise ValueError(f"{name} must be [..., {heads}, {d}], got {list(shape)}")
+    if t.is_contiguous():
+        return heads * d
+    if stride[-1] != 1 or (heads > 1 and stride[-2] != d):
+        raise ValueError(f"the heads and columns of {name} must lie side by side")
+    step, n = heads * d, 1                                      # tokens of the inner axes so far, and their stride
+    for axis in range(t.dim() - 3, -1, -1):
+        if shape[axis] == 1:
+            continue
+        if n == 1:
+            step = stride[axis]
+        elif stride[axis] != step * n:
+            raise ValueError(f"the tokens of {name} must be one stride apart")
+        n *= shape[axis]
+    return step if n > 1 else max(step, heads * d)
+
+
+def _on_cache(cache, stream, **tensors):
+    """_launch_on for calls whose device is the cache's."""
+    guard, stream = _launch_on(stream, **tensors)
+    for name, t in tensors.items():
+        if t is not None:
+            if t.get_device() != cache.device_index:
+                raise ValueError(f"{name} is on {t.device}, the cache is on cuda:{cache.device_index}")
+            break
+    return guard, stream
+
+
+def paged_append(cache, k, v, slots, stream=None):
+    """idxc_paged_append: k, v [n, H_kv, d] bf16 (tokens any stride apart) written to slots [n] int64 of a PagedCache, in 8 bits with their scales; the
+    bounds of the pages written to are brought up to date if the cache has them. Slots outside the cache are skipped."""
+    guard, stream = _on_cache(cache, stream, slots=slots)
+    n = slots.shape[0]
+    _typed(slots, "slots", torch.int64, (n,))
+    if k.dim() != 3 or v.dim() != 3 or k.shape[0] != n or v.shape[0] != n:
+        raise ValueError(f"k and v must be [{n}, {cache.H_kv}, {cache.d}]")
+    k_stride = _token_stride(k, "k", cache.H_kv, cache.d, cache.device_index)
+    v_stride = _token_stride(v, "v", cache.H_kv, cache.d, cache.device_index)
+    with guard:
+        _check(lib().idxc_paged_append(cache._p, _at(k), k_stride, _at(v), v_stride, _at(slots), n, stream), "idxc_paged_append")
+
+
+def paged_gather(cache, slots, k_out, v_out, stream=None):
+    """idxc_paged_gather: rows slots [n] int64 of a PagedCache read into k_out, v_out [n, H_kv, d] bf16; zeros for slots outside the cache."""
+    guard, stream = _on_cache(cache, stream, slots=slots, k_out=k_out, v_out=v_out)
+    n = slots.shape[0]
+    _typed(slots, "slots", torch.int64, (n,))
+    _typed(k_out, "k_out", torch.bfloat16, (n, cache.H_kv, cache.d)); _typed(v_out, "v_out", torch.bfloat16, (n, cache.H_kv, cache.d))
+    with guard:
+        _check(lib().idxc_paged_gather(cache._p, _at(slots), n, _at(k_out), _at(v_out), stream), "idxc_paged_gather")
+
+
+def paged_attention_workspace_bytes(n_step, H, H_kv, d) -> int:
+    return lib().idxc_paged_attention_workspace_bytes(int(n_step), int(H), int(H_kv), int(d))
+
+
+def paged_attention(cache, q, table, lens, max_len, scale, pages=None, want_lse=True, out=None, workspace=None, stream=None):
+    """idxc_paged_attention: q [B, n_step, H, d] bf16 (tokens any one stride apart) over the requests' pages of a PagedCache, H / H_kv query heads to a
+    key head; the n_step new tokens are the last positions, and token i sees lens[b] - (n_step - 1 - i) of them. table [B, ld] int32, lens [B] int32,
+    ``max_len`` a host bound on lens. pages [B, H_kv, n_sel] (or [B * H_kv, n_sel]) int32: only the positions of these logical pages.
+    Returns (out [B, n_step, H, d] bf16, lse [B, n_step, H] fp32 or None)."""
+    guard, stream = _on_cache(cache, stream, table=table, lens=lens, pages=pages, out=out, workspace=workspace)
+    if q.dim() != 4 or table.dim() != 2:
+        raise ValueError("q must be [B, n_step, H, d] and table [B, ld]")
+    B, n_step, H, d = q.shape
+    q_stride = _token_stride(q, "q", H, cache.d, cache.device_index)
+    ld = table.shape[1]
+    _typed(table, "table", torch.int32, (B, ld)); _typed(lens, "lens", torch.int32, (B,)); _typed(out, "out", torch.bfloat16, (B, n_step, H, d))
+    n_sel = 0
+    if pages is not None:
+        n_sel = pages.shape[-1]
+        _typed(pages, "pages", torch.int32, (B, cache.H_kv, n_sel) if pages.dim() == 3 else (B * cache.H_kv, n_sel))
+    with guard:
+        if out is None:
+            out = torch.empty_strided((B, n_step, H, d), (n_step * H * d, H * d, d, 1), dtype=torch.bfloat16, device=q.device)
+        lse = _new3(B, n_step, H, torch.float32, q.device) if want_lse else None
+        if workspace is None:
+            workspace = torch.empty_strided((max(paged_attention_workspace_bytes(n_step, H, cache.H_kv, d), 256),), (1,), dtype=torch.uint8, device=q.device)
+        _check(lib().idxc_paged_attention(cache._p, _at(q), q_stride, _at(table), ld, _at(lens), B, n_step, int(max_len), H, _at(pages), n_sel, float(scale),
+                                          _at(out), _at(lse), _at(workspace), workspace.nbytes, stream), "idxc_paged_attention")
+    return out, lse
+
+
+def page_scores(bounds, q, table, lens, page_size, scale, scores_out, n_pages_out, keep_first=1, keep_last=1, stream=None):
+    """idxc_page_scores: the largest score that a key between a page's bounds could reach, for every page of every request and key head. bounds
+    [n_pages, H_kv, 2, d] bf16, q [B, n_step, H, d] bf16 -> scores_out [B * H_kv, ld] fp32, n_pages_out [B * H_kv] int32, which topk_rows takes as
+    scores and lens; its selection is paged_attention's pages. The first keep_first and last keep_last pages score 3e38."""
+    guard, stream = _launch_on(stream, bounds=bounds, table=table, lens=lens, scores_out=scores_out, n_pages_out=n_pages_out)
+    if q.dim() != 4 or table.dim() != 2 or bounds.dim() != 4 or scores_out.dim() != 2:
+        raise ValueError("bounds must be [n_pages, H_kv, 2, d], q [B, n_step, H, d], table [B, ld] and scores_out [B * H_kv, ld]")
+    n_pages, H_kv, _, d = bounds.shape
+    B, n_step, H, _ = q.shape
+    _typed(bounds, "bounds", torch.bfloat16, (n_pages, H_kv, 2, d))
+    q_stride = _token_stride(q, "q", H, d, bounds.get_device())
+    _typed(table, "table", torch.int32, (B, table.shape[1])); _typed(lens, "lens", torch.int32, (B,))
+    _typed(scores_out, "scores_out", torch.float32, (B * H_kv, scores_out.shape[1])); _typed(n_pages_out, "n_pages_out", torch.int32, (B * H_kv,))
+    with guard:
+        _check(lib().idxc_page_scores(_at(bounds), n_pages, int(page_size), H_kv, d, _at(q), q_stride, _at(table), table.shape[1], _at(lens), B, n_step, H,
+                                      int(keep_first), int(keep_last), float(scale), _at(scores_out), scores_out.shape[1], _at(n_pages_out), stream),
+               "idxc_page_scores")
 
 
 def selftest_bounded_wait(wait_cycles: int = 1_000_000, stream=None):

@@ -699,6 +699,192 @@ idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t
                                static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
 }
 
+// ------------------------------------------------------------------ paged key/value cache
+
+}  // extern "C"
+
+namespace {
+
+// What the calls over block tables have in common.
+bool page_sizes_ok(int64_t B, int64_t ld_table, int page_size) {
+    return B >= 0 && B <= 65535 && ld_table >= 0 && ld_table < (int64_t(1) << 31) && B * ld_table < (int64_t(1) << 31) && page_size >= 16 &&
+           page_size <= 1024 && page_size % 16 == 0;
+}
+
+idxc_status check_paged(const idxc_paged_cache* c, PagedCache& out) {
+    if (!c || (c->dtype != IDXC_BF16 && c->dtype != IDXC_FP8_E4M3) || c->n_pages < 0 || c->H_kv < 1 || c->H_kv > 1024 || c->d < 1 ||
+        c->page_size < 16 || c->page_size > 1024 || c->page_size % 16 || c->n_pages >= (int64_t(1) << 31) ||
+        c->n_pages * c->page_size >= (int64_t(1) << 31))
+        return IDXC_ERR_INVALID_ARG;
+    if (c->d != 64 && c->d != 128) return IDXC_ERR_UNSUPPORTED;
+    const bool fp8 = c->dtype == IDXC_FP8_E4M3;
+    const int64_t bytes = fp8 ? 1 : 2;
+    for (const int64_t stride : {c->page_stride, c->token_stride, c->head_stride})
+        if (stride < 16 / bytes || stride >= (int64_t(1) << 39) / bytes || stride * bytes % 16) return IDXC_ERR_INVALID_ARG;
+    if (c->n_pages > 0 && (!c->k || !c->v || (fp8 && (!c->k_scale || !c->v_scale)))) return IDXC_ERR_INVALID_ARG;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->bounds, 16) || (fp8 && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))))
+        return IDXC_ERR_INVALID_ARG;
+    out = PagedCache{c->k, c->v, c->k_scale, c->v_scale, c->bounds, c->n_pages, c->page_stride, c->token_stride, c->head_stride,
+                     c->page_size, c->H_kv, c->d, fp8};
+    return IDXC_OK;
+}
+
+// Keys or values as [n_pages][H_kv][page_size][d], boxes of `box` tokens of one head and page.
+bool encode_paged_map(CUtensorMap* map, const void* base, const PagedCache& c, int box) {
+    const cuuint64_t bytes = c.fp8 ? 1 : 2;
+    const cuuint32_t inner = c.fp8 ? static_cast<cuuint32_t>(c.d) : 64u;      // a box is 128 bytes wide, 64 with d = 64 in 8 bits
+    const cuuint64_t gdim[4] = {static_cast<cuuint64_t>(c.d), static_cast<cuuint64_t>(c.page_size), static_cast<cuuint64_t>(c.H_kv),
+                                static_cast<cuuint64_t>(c.n_pages)};
+    const cuuint64_t gstride[3] = {static_cast<cuuint64_t>(c.token_stride) * bytes, static_cast<cuuint64_t>(c.head_stride) * bytes,
+                                   static_cast<cuuint64_t>(c.page_stride) * bytes};
+    const cuuint32_t dims[4] = {inner, static_cast<cuuint32_t>(box), 1u, 1u};
+    const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+    return device_info().encode(map, c.fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), gdim, gstride,
+                                dims, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                inner * bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                                c.d * bytes >= 256 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+idxc_status idxc_page_tables(int32_t* table, int64_t ld_table, int32_t* lens, const int32_t* new_tokens, int64_t B, int page_size,
+                             const int32_t* free_pages, int64_t free_capacity, int32_t* free_count, int32_t* token_begin_out, int32_t* start_out,
+                             int64_t* slots_out, int64_t n_slots, int32_t* seq_out, void* cuda_stream) {
+    if (!page_sizes_ok(B, ld_table, page_size) || free_capacity < 0 || free_capacity >= (int64_t(1) << 31) || n_slots < 0 || n_slots >= (int64_t(1) << 31))
+        return IDXC_ERR_INVALID_ARG;
+    if (!free_count || !token_begin_out || !aligned(free_count, 4) || !aligned(token_begin_out, 4) || (free_capacity > 0 && !free_pages) ||
+        !aligned(free_pages, 4) || (n_slots > 0 && !slots_out) || !aligned(slots_out, 8) || !aligned(seq_out, 4))
+        return IDXC_ERR_INVALID_ARG;
+    if (B > 0 && ((ld_table > 0 && !table) || !lens || !new_tokens || !start_out || lens == new_tokens || lens == start_out || new_tokens == start_out ||
+                  !aligned(table, 4) || !aligned(lens, 4) || !aligned(new_tokens, 4) || !aligned(start_out, 4)))
+        return IDXC_ERR_INVALID_ARG;
+    int n_l = 0;
+    const cudaError_t e = launch_page_tables(table, ld_table, lens, new_tokens, static_cast<int>(B), page_size, free_pages, free_capacity, free_count,
+                                             token_begin_out, start_out, slots_out, n_slots, seq_out, static_cast<cudaStream_t>(cuda_stream), &n_l);
+    g_launches += n_l;
+    return e == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_page_release(int32_t* table, int64_t ld_table, int32_t* lens, const int32_t* keep_lens, int64_t B, int page_size, int32_t* free_pages,
+                              int64_t free_capacity, int32_t* free_count, void* cuda_stream) {
+    if (!page_sizes_ok(B, ld_table, page_size) || free_capacity < 0 || free_capacity >= (int64_t(1) << 31)) return IDXC_ERR_INVALID_ARG;
+    if (B == 0) return IDXC_OK;
+    if ((ld_table > 0 && !table) || !lens || !free_count || lens == keep_lens || (free_capacity > 0 && !free_pages) || !aligned(table, 4) ||
+        !aligned(lens, 4) || !aligned(keep_lens, 4) || !aligned(free_pages, 4) || !aligned(free_count, 4))
+        return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_page_release(table, ld_table, lens, keep_lens, static_cast<int>(B), page_size, free_pages, free_capacity, free_count,
+                               static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_page_rows(const int32_t* table, int64_t ld_table, int64_t B, const int32_t* seq, const int32_t* positions, int64_t n_rows, int k,
+                           int page_size, int32_t* out, void* cuda_stream) {
+    if (!page_sizes_ok(B, ld_table, page_size) || n_rows < 0 || k < 0 || n_rows >= (int64_t(1) << 31) || (!seq && n_rows > B)) return IDXC_ERR_INVALID_ARG;
+    if (n_rows == 0 || k == 0) return IDXC_OK;
+    if ((B * ld_table > 0 && !table) || !positions || !out || !aligned(table, 4) || !aligned(seq, 4) || !aligned(positions, 4) || !aligned(out, 4))
+        return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_page_rows(table, ld_table, seq, static_cast<int>(B), positions, n_rows, k, page_size, out, static_cast<cudaStream_t>(cuda_stream)) ==
+                   cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_paged_append(const idxc_paged_cache* cache, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* slots,
+                              int64_t n, void* cuda_stream) {
+    PagedCache c;
+    const idxc_status st = check_paged(cache, c);
+    if (st != IDXC_OK) return st;
+    const int64_t row = static_cast<int64_t>(c.H_kv) * c.d;
+    if (n < 0 || n >= (int64_t(1) << 31) || n * row >= (int64_t(1) << 40) || k_stride < row || v_stride < row || k_stride % 8 || v_stride % 8 ||
+        k_stride >= (int64_t(1) << 39) || v_stride >= (int64_t(1) << 39))
+        return IDXC_ERR_INVALID_ARG;
+    if (n == 0 || c.n_pages == 0) return IDXC_OK;
+    if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_paged_append(c, k, k_stride, v, v_stride, slots, n, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_paged_gather(const idxc_paged_cache* cache, const int64_t* slots, int64_t n, void* k_out, void* v_out, void* cuda_stream) {
+    PagedCache c;
+    const idxc_status st = check_paged(cache, c);
+    if (st != IDXC_OK) return st;
+    if (n < 0 || n >= (int64_t(1) << 31) || n * c.H_kv * c.d >= (int64_t(1) << 40)) return IDXC_ERR_INVALID_ARG;
+    if (n == 0) return IDXC_OK;
+    if (!slots || !k_out || !v_out || !aligned(slots, 8) || !aligned(k_out, 16) || !aligned(v_out, 16)) return IDXC_ERR_INVALID_ARG;
+    g_launches += 1;
+    return launch_paged_gather(c, slots, n, k_out, v_out, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+size_t idxc_paged_attention_workspace_bytes(int n_step, int H, int H_kv, int d) {
+    if (n_step < 1 || n_step > 1024 || H_kv < 1 || H < H_kv || H % H_kv || H / H_kv > 128 || (d != 64 && d != 128)) return 0;
+    return paged_attn_workspace_bytes(n_step, H / H_kv, d);
+}
+
+idxc_status idxc_paged_attention(const idxc_paged_cache* cache, const void* q, int64_t q_stride, const int32_t* table, int64_t ld_table,
+                                 const int32_t* lens, int64_t B, int n_step, int64_t max_len, int H, const int32_t* pages, int n_sel, float scale,
+                                 void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    PagedAttnArgs a;
+    const idxc_status st = check_paged(cache, a.c);
+    if (st != IDXC_OK) return st;
+    if (!page_sizes_ok(B, ld_table, a.c.page_size) || n_step < 1 || n_step > 1024 || H < a.c.H_kv || H % a.c.H_kv || H / a.c.H_kv > 128 || max_len < 0 ||
+        max_len > (int64_t(1) << 30) || max_len > ld_table * a.c.page_size || (pages && n_sel < 1) || q_stride < static_cast<int64_t>(H) * a.c.d ||
+        q_stride % 8 || q_stride >= (int64_t(1) << 39) || B * n_step * H >= (int64_t(1) << 31))
+        return IDXC_ERR_INVALID_ARG;
+    if (B == 0) return IDXC_OK;
+    if (!q || !lens || !out || (max_len > 0 && !table) || !aligned(q, 16) || !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) ||
+        !aligned(pages, 4) || !aligned(lse, 4))
+        return IDXC_ERR_INVALID_ARG;
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.q_stride = q_stride;
+    a.H = H;
+    a.group = H / a.c.H_kv;
+    a.n_step = n_step;
+    a.table = table;
+    a.ld_table = ld_table;
+    a.lens = lens;
+    a.B = static_cast<int>(B);
+    a.max_len = a.c.n_pages > 0 ? max_len : 0;                 // no pages: every token sees nothing
+    a.pages = pages;
+    a.n_sel = pages ? n_sel : 0;
+    a.scale = scale;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.lse = lse;
+    if (!paged_attn_fits(a)) return IDXC_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < idxc_paged_attention_workspace_bytes(n_step, H, a.c.H_kv, a.c.d)) return IDXC_ERR_WORKSPACE;
+    DeviceInfo& di = device_info();
+    if (!di.ok) return IDXC_ERR_CUDA;
+    CUtensorMap k_map{}, v_map{};
+    const int box = a.c.page_size % 64 == 0 ? 64 : (a.c.page_size % 32 == 0 ? 32 : 16);
+    if (a.c.n_pages > 0 && (!encode_paged_map(&k_map, a.c.k, a.c, box) || !encode_paged_map(&v_map, a.c.v, a.c, box))) return IDXC_ERR_CUDA;
+    int n_l = 0;
+    const cudaError_t e = launch_paged_attn(a, workspace, k_map, v_map, di.status_ptr, di.sm_count, static_cast<cudaStream_t>(cuda_stream), &n_l);
+    g_launches += n_l;
+    return e == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
+idxc_status idxc_page_scores(const void* bounds, int64_t n_pages, int page_size, int H_kv, int d, const void* q, int64_t q_stride, const int32_t* table,
+                             int64_t ld_table, const int32_t* lens, int64_t B, int n_step, int H, int keep_first, int keep_last, float scale,
+                             float* scores, int64_t ld_scores, int32_t* n_pages_out, void* cuda_stream) {
+    if (!page_sizes_ok(B, ld_table, page_size) || n_pages < 0 || n_pages >= (int64_t(1) << 31) || H_kv < 1 || H_kv > 1024 || d < 1 || n_step < 1 ||
+        n_step > 1024 || H < H_kv || H % H_kv || H / H_kv > 128 || keep_first < 0 || keep_last < 0 || ld_scores < ld_table || !(scale > 0.f) ||
+        !(scale <= 3.4028234663852886e38f) || B * n_step * H >= (int64_t(1) << 31))
+        return IDXC_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return IDXC_ERR_UNSUPPORTED;
+    if (q_stride < static_cast<int64_t>(H) * d || q_stride % 8 || q_stride >= (int64_t(1) << 39)) return IDXC_ERR_INVALID_ARG;
+    if (B == 0) return IDXC_OK;
+    if (!q || !lens || !n_pages_out || lens == n_pages_out || (n_pages > 0 && !bounds) || (ld_table > 0 && (!table || !scores)) || !aligned(bounds, 16) ||
+        !aligned(q, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(scores, 4) || !aligned(n_pages_out, 4))
+        return IDXC_ERR_INVALID_ARG;
+    DeviceInfo& di = device_info();
+    if (!di.ok) return IDXC_ERR_CUDA;
+    g_launches += 1;
+    return launch_page_scores(bounds, n_pages, page_size, H_kv, d, q, q_stride, n_step, H / H_kv, table, ld_table, lens, static_cast<int>(B), keep_first,
+                              keep_last, scale, scores, ld_scores, n_pages_out, di.sm_count, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+               ? IDXC_OK : IDXC_ERR_CUDA;
+}
+
 idxc_status idxc_selftest_bounded_wait(uint32_t wait_cycles, void* cuda_stream) {
     if (!device_info().ok) return IDXC_ERR_CUDA;
     const long long budget = wait_cycles > 100000000u ? 100000000LL : static_cast<long long>(wait_cycles);

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -176,6 +177,58 @@ cudaError_t launch_compact_rows(const void* src, void* dst, int row_bytes, int64
 // evict.cu
 cudaError_t launch_evict_select(const float* acc, int64_t ld, const int32_t* lens, int B, int budget, int recent, int32_t* keep,
                                 int32_t* new_lens, cudaStream_t stream);
+
+// A paged key/value cache: [n_pages, page_size, H_kv, d] by strides (in elements), and what goes with it.
+struct PagedCache {
+    void* k;                    // bf16, or e4m3 codes
+    void* v;
+    float* k_scale;             // e4m3: [n_pages, H_kv, page_size]
+    float* v_scale;
+    void* bounds;               // nullptr, or bf16 [n_pages, H_kv, 2, d]
+    int64_t n_pages;
+    int64_t page_stride, token_stride, head_stride;
+    int page_size, H_kv, d;
+    int fp8;
+};
+// page_tables.cu
+cudaError_t launch_page_tables(int32_t* table, int64_t ld, int32_t* lens, const int32_t* new_tokens, int B, int P, const int32_t* free_pages,
+                               int64_t free_cap, int32_t* free_count, int32_t* token_begin, int32_t* start, int64_t* slots, int64_t n_slots,
+                               int32_t* seq, cudaStream_t stream, int* launches);
+cudaError_t launch_page_release(int32_t* table, int64_t ld, int32_t* lens, const int32_t* keep_lens, int B, int P, int32_t* free_pages,
+                                int64_t free_cap, int32_t* free_count, cudaStream_t stream);
+cudaError_t launch_page_rows(const int32_t* table, int64_t ld, const int32_t* seq, int B, const int32_t* positions, int64_t n_rows, int k, int P,
+                             int32_t* rows, cudaStream_t stream);
+// paged_cache.cu (k_stride, v_stride: elements between the tokens of the input)
+cudaError_t launch_paged_append(const PagedCache& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* slots, int64_t n,
+                                cudaStream_t stream);
+cudaError_t launch_paged_gather(const PagedCache& c, const int64_t* slots, int64_t n, void* k_out, void* v_out, cudaStream_t stream);
+// page_scores.cu
+cudaError_t launch_page_scores(const void* bounds, int64_t n_pages, int P, int H_kv, int d, const void* q, int64_t q_stride, int n_step, int group,
+                               const int32_t* table, int64_t ld_table, const int32_t* lens, int B, int keep_first, int keep_last, float scale,
+                               float* scores, int64_t ld, int32_t* n_out, int sm_count, cudaStream_t stream);
+// paged_attn.cu. k_map, v_map: the cache as [n_pages][H_kv][page_size][d], boxes of 128 bytes (d = 64 in 8 bits: 64) x 64, 32 or 16 tokens
+// (the most that divides page_size), swizzled over their own width.
+struct PagedAttnArgs {
+    PagedCache c;
+    const __nv_bfloat16* q;     // [B, n_step, H, d]; q_stride elements between tokens
+    int64_t q_stride;
+    int H, group, n_step;       // group = H / H_kv
+    const int32_t* table;       // [B, ld_table]
+    int64_t ld_table;
+    const int32_t* lens;        // [B]
+    int B;
+    int64_t max_len;            // host bound on lens, at most ld_table * page_size
+    const int32_t* pages;       // nullptr, or [B, H_kv, n_sel] logical pages
+    int n_sel;
+    float scale;
+    __nv_bfloat16* out;         // [B, n_step, H, d]
+    float* lse;                 // nullptr, or [B, n_step, H]
+};
+constexpr int kPagedMaxGrid = 160;
+size_t paged_attn_workspace_bytes(int n_step, int group, int d);
+bool paged_attn_fits(const PagedAttnArgs& a);           // the tile count of the call stays below 2^31
+cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
+                              int sm_count, cudaStream_t stream, int* launches);
 
 // selftest.cu: one tiny kernel whose only wait can never be satisfied; it must record a time-out in
 // `status` after `budget_cycles` and return.

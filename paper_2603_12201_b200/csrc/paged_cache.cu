@@ -1,0 +1,237 @@
+// Writing and reading rows of a paged key/value cache, and the bounds of its pages: for every page, head and key column the smallest and the
+// largest value among the rows 0 .. (newest written), as the rows read back in bf16.
+//
+// Append. Tokens that follow each other into one page are a run; the CTA that holds a run's first token walks the page's rows once: those in
+// front of the run come from the cache, the run's from the input, and go to the cache on the way. So a page's bounds come from its rows alone
+// (never from what they were), one thread owns a column's bounds, and nothing is read twice. A thread owns 8 columns (16 bytes) of a head; what
+// a head's 8 or 16 threads share is only the row's maximum in front of the e4m3 codes. HBM-bound: 8 bytes moved per element of k and v in bf16
+// (read, written), 6 in e4m3, and for a decode step the latency of one page's rows.
+#include "e4m3_rows.cuh"
+#include "kernels.h"
+#include "ptx_sm100.cuh"
+
+namespace idxc {
+namespace {
+
+constexpr int kAppendThreads = 128;
+
+// Values of 8 e4m3 codes and their row's scale, rounded to bf16.
+__device__ __forceinline__ uint4 codes_to_bf16(uint2 codes, float scale) {
+    uint4 out;
+    uint32_t* o = &out.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t two = (i < 2 ? codes.x : codes.y) >> (16 * (i & 1)) & 0xFFFFu;
+        const uint32_t h = e4m3x2_to_f16x2(two);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        const __nv_bfloat162 v = __floats2bfloat162_rn(f.x * scale, f.y * scale);
+        o[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return out;
+}
+__device__ __forceinline__ void widen(uint4 v, uint4& lo, uint4& hi) {
+    const uint32_t* x = &v.x;
+    uint32_t *l = &lo.x, *h = &hi.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162*>(x + i);
+        __nv_bfloat162 a = __hmin2(*reinterpret_cast<__nv_bfloat162*>(l + i), y), b = __hmax2(*reinterpret_cast<__nv_bfloat162*>(h + i), y);
+        l[i] = *reinterpret_cast<uint32_t*>(&a);
+        h[i] = *reinterpret_cast<uint32_t*>(&b);
+    }
+}
+constexpr uint32_t kBf16PosInf2 = 0x7F807F80u, kBf16NegInf2 = 0xFF80FF80u;
+
+struct AppendArgs {
+    PagedCache c;
+    const uint4* k;              // rows of H_kv * d bf16, k_stride / v_stride vectors of 8 apart
+    const uint4* v;
+    int64_t k_stride, v_stride;
+    const int64_t* slots;
+    int64_t n;
+    int chunk;                   // tokens a CTA looks at for the beginnings of runs
+};
+
+template <bool FP8>
+__global__ void __launch_bounds__(kAppendThreads)
+paged_append_kernel(const AppendArgs a) {
+    __shared__ int run_len;
+    __shared__ uint4 part[2][kAppendThreads];
+    let_next_start();
+    wait_for_previous();
+    const PagedCache& c = a.c;
+    const int vecs = c.H_kv * (c.d / 8), per_head = c.d / 8;
+    const int cols = min(vecs, kAppendThreads), lanes = kAppendThreads / cols;       // threads of a row, rows at a time
+    const int lane = threadIdx.x / cols;
+    const int col = blockIdx.y * kAppendThreads + threadIdx.x % cols;
+    const bool works = lane < lanes && col < vecs;
+    const int head = col / per_head, d0 = (col % per_head) * 8;
+    const int64_t n_slots = c.n_pages * c.page_size;
+    const int64_t t_end = min(a.n, (static_cast<int64_t>(blockIdx.x) + 1) * a.chunk);
+    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.chunk; t0 < t_end; ++t0) {
+        const int64_t slot = a.slots[t0];
+        if (slot < 0 || slot >= n_slots) continue;                                   // (uniform over the CTA, as all that follows)
+        const int64_t page = slot / c.page_size;
+        const int off = static_cast<int>(slot - page * c.page_size);
+        if (t0 > 0 && off > 0 && a.slots[t0 - 1] == slot - 1) continue;              // inside a run
+        __syncthreads();
+        if (threadIdx.x == 0) run_len = c.page_size - off;
+        __syncthreads();
+        for (int i = threadIdx.x; i < c.page_size - off; i += kAppendThreads)
+            if (t0 + i >= a.n || a.slots[t0 + i] != slot + i) {
+                atomicMin(&run_len, i);
+                break;
+            }
+        __syncthreads();
+        const int n_new = run_len, rows = off + n_new;
+        uint4 lo = make_uint4(kBf16PosInf2, kBf16PosInf2, kBf16PosInf2, kBf16PosInf2);
+        uint4 hi = make_uint4(kBf16NegInf2, kBf16NegInf2, kBf16NegInf2, kBf16NegInf2);
+        const int64_t base = page * c.page_stride + head * c.head_stride + d0;        // elements
+        const int64_t scale_base = (page * c.H_kv + head) * c.page_size;
+        constexpr int U = 4;                                                          // rows in flight a thread
+        if (c.bounds)
+            for (int r0 = lane; r0 < off; r0 += U * lanes) {                          // rows that are there
+                uint4 x[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int r = r0 + u * lanes;
+                    if (!works || r >= off) continue;
+                    const int64_t at = base + r * c.token_stride;
+                    if (FP8)
+                        x[u] = codes_to_bf16(*reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + at), c.k_scale[scale_base + r]);
+                    else
+                        x[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + at);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (works && r0 + u * lanes < off) widen(x[u], lo, hi);
+            }
+        for (int i0 = 0; i0 < n_new; i0 += U * lanes) {                               // (all threads: they shuffle)
+            Vec8 k[U], v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * lanes + lane;
+                const bool in = works && i < n_new;
+                k[u].raw = in ? __ldg(a.k + (t0 + i) * a.k_stride + col) : make_uint4(0u, 0u, 0u, 0u);
+                v[u].raw = in ? __ldg(a.v + (t0 + i) * a.v_stride + col) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * lanes + lane;
+                const bool in = works && i < n_new;
+                const int64_t at = base + (off + i) * c.token_stride;
+                if (!FP8) {
+                    if (in) {
+                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(c.k) + at) = k[u].raw;
+                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(c.v) + at) = v[u].raw;
+                        widen(k[u].raw, lo, hi);
+                    }
+                    continue;
+                }
+                float k_max = 0.f, v_max = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    k_max = fmaxf(k_max, fabsf(k[u].get(e)));
+                    v_max = fmaxf(v_max, fabsf(v[u].get(e)));
+                }
+                for (int o = per_head / 2; o > 0; o >>= 1) {                          // (a head's threads are aligned within a warp)
+                    k_max = fmaxf(k_max, __shfl_xor_sync(0xFFFFFFFFu, k_max, o));
+                    v_max = fmaxf(v_max, __shfl_xor_sync(0xFFFFFFFFu, v_max, o));
+                }
+                if (in) {
+                    const float ks = __fdiv_rn(fmaxf(k_max, 1e-12f), kE4m3Max), vs = __fdiv_rn(fmaxf(v_max, 1e-12f), kE4m3Max);
+                    const uint2 kc = quantize8(k[u], ks);
+                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.k) + at) = kc;
+                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.v) + at) = quantize8(v[u], vs);
+                    if (d0 == 0) {
+                        c.k_scale[scale_base + off + i] = ks;
+                        c.v_scale[scale_base + off + i] = vs;
+                    }
+                    if (c.bounds) widen(codes_to_bf16(kc, ks), lo, hi);
+                }
+            }
+        }
+        if (!c.bounds) continue;
+        if (lanes > 1) {                                                              // columns meet from the rows that went side by side
+            part[0][threadIdx.x] = lo;
+            part[1][threadIdx.x] = hi;
+            __syncthreads();
+            if (lane == 0)
+                for (int l = 1; l < lanes; ++l) {
+                    uint4 dummy = hi;
+                    widen(part[0][l * cols + threadIdx.x], lo, dummy);
+                    dummy = lo;
+                    widen(part[1][l * cols + threadIdx.x], dummy, hi);
+                }
+        }
+        if (works && lane == 0 && rows > 0) {
+            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(c.bounds) + (page * c.H_kv + head) * 2 * c.d + d0;
+            *reinterpret_cast<uint4*>(to) = lo;
+            *reinterpret_cast<uint4*>(to + c.d) = hi;
+        }
+    }
+}
+
+// Rows of the cache in bf16, a 16-byte vector of k and of v a thread and step; slots outside the cache give zeros.
+template <bool FP8>
+__global__ void __launch_bounds__(256)
+paged_gather_kernel(const PagedCache c, const int64_t* slots, int64_t n, uint4* k_out, uint4* v_out) {
+    let_next_start();
+    wait_for_previous();
+    const int per_head = c.d / 8, vecs = c.H_kv * per_head;
+    const int64_t n_slots = c.n_pages * c.page_size, all = n * vecs, step = gridDim.x * int64_t(256);
+    constexpr int U = 2;
+    for (int64_t i0 = blockIdx.x * int64_t(256) + threadIdx.x; i0 < all; i0 += U * step) {
+        uint4 k[U], v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * step;
+            k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (i >= all) continue;
+            const int64_t t = i / vecs;
+            const int col = static_cast<int>(i - t * vecs), head = col / per_head, d0 = (col - head * per_head) * 8;
+            const int64_t slot = slots[t];
+            if (slot < 0 || slot >= n_slots) continue;
+            const int64_t page = slot / c.page_size;
+            const int off = static_cast<int>(slot - page * c.page_size);
+            const int64_t at = page * c.page_stride + off * c.token_stride + head * c.head_stride + d0;
+            if (FP8) {
+                const int64_t s = (page * c.H_kv + head) * c.page_size + off;
+                k[u] = codes_to_bf16(*reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + at), c.k_scale[s]);
+                v[u] = codes_to_bf16(*reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.v) + at), c.v_scale[s]);
+            } else {
+                k[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + at);
+                v[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.v) + at);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * step < all) {
+                k_out[i0 + u * step] = k[u];
+                v_out[i0 + u * step] = v[u];
+            }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_paged_append(const PagedCache& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* slots, int64_t n,
+                                cudaStream_t stream) {
+    // A CTA for every token as long as that fills the GPU a few times over (a decode step's pages then go side by side); longer inputs are
+    // prompts, whose runs are as long as pages.
+    const int chunk = n <= 4096 ? 1 : 16;
+    const AppendArgs a{c, static_cast<const uint4*>(k), static_cast<const uint4*>(v), k_stride / 8, v_stride / 8, slots, n, chunk};
+    const int vecs = c.H_kv * (c.d / 8);
+    const dim3 grid(static_cast<unsigned>((n + chunk - 1) / chunk), static_cast<unsigned>((vecs + kAppendThreads - 1) / kAppendThreads));
+    return c.fp8 ? launch_behind(paged_append_kernel<true>, grid, kAppendThreads, 0, stream, a)
+                 : launch_behind(paged_append_kernel<false>, grid, kAppendThreads, 0, stream, a);
+}
+
+cudaError_t launch_paged_gather(const PagedCache& c, const int64_t* slots, int64_t n, void* k_out, void* v_out, cudaStream_t stream) {
+    const int64_t all = n * c.H_kv * (c.d / 8), blocks = (all + 511) / 512;
+    const unsigned grid = static_cast<unsigned>(blocks < 148 * 64 ? blocks : 148 * 64);
+    return c.fp8 ? launch_behind(paged_gather_kernel<true>, dim3(grid), 256, 0, stream, c, slots, n, static_cast<uint4*>(k_out), static_cast<uint4*>(v_out))
+                 : launch_behind(paged_gather_kernel<false>, dim3(grid), 256, 0, stream, c, slots, n, static_cast<uint4*>(k_out), static_cast<uint4*>(v_out));
+}
+
+}  // namespace idxc
