@@ -9,8 +9,8 @@
 // the tensor cores issue several times what the copies deliver. (A tile is the M = 16 rows of up to 16 query rows; tcgen05's M = 64 or 128 would
 // be mostly padding, and its accumulators would cross tensor memory twice a tile.)
 //
-// Each of 8 warps works on a tile of its own (with more than 32 query rows 2 or 4 warps share one, 32 rows each) with its own running maximum and
-// sum; the warps meet once at a segment's end. The tiles of all (request, key head, block of rows), end to end, are cut into equal runs, a run a
+// Each of 8 warps takes 16 or 32 keys of a tile and up to 32 query rows (with more rows, 2 or 4 warps the same keys) with its own running
+// maximum and sum; the warps meet once at a segment's end. The tiles of all (request, key head, block of rows), end to end, are cut into equal runs, a run a
 // CTA, which finds it from the lengths on the device; segments cut by a run's end go to the workspace in fp32 and through a merge kernel. All sums
 // have an order fixed by the sizes, so results repeat bit for bit.
 //
@@ -185,7 +185,10 @@ struct Walk {
 template <int D, bool FP8, int MT, int RG>
 struct Layout {
     static constexpr int kRows = 16 * MT * RG;                         // query rows of a CTA
-    static constexpr int kSlots = kWarps / RG;                         // tiles worked on at a time
+    static constexpr int kParts = kWarps / RG;                         // warps that share a row
+    static constexpr int kKeys = D == 128 && !FP8 && RG < 4 ? 16 : 32; // keys of a tile that a warp takes
+    static constexpr int kSplit = kTile / kKeys;                       // warps (of a row) that share a tile
+    static constexpr int kSlots = kParts / kSplit;                     // tiles worked on at a time
     static constexpr int kTileBytes = kTile * D * (FP8 ? 1 : 2);
     static constexpr int kStageBytes = 2 * kTileBytes + (FP8 ? 1024 : 0);      // K, V, scales of K and of V (256 bytes each)
     static constexpr int kQBytes = kRows * D * 2;
@@ -193,9 +196,12 @@ struct Layout {
     static constexpr int kMlBytes = kWarps * MT * 16 * 8;
     static constexpr int kSmall = 1024 + 4096;                         // alignment of the stages; barriers, positions, scales of q
     static constexpr int kFit = (kSmemLimit - kSmall - kQBytes - kRedBytes - kMlBytes) / kStageBytes;
-    static constexpr int kStages = kFit > 24 ? 24 : kFit;
+    // A stage belongs to one slot, whose warps see every phase of its barrier: were the stages no multiple of the slots, a warp could come to
+    // a stage's barrier while the tile before its own is still on the way, and take the parity of the one before that for its own.
+    static constexpr int kStages = (kFit > 24 ? 24 : kFit) / kSlots * kSlots;
     static constexpr int kBytes = kSmall + kStages * kStageBytes + kQBytes + kRedBytes + kMlBytes;
-    static_assert(kStages >= 3, "a ring of at least three tiles");
+    static_assert(kParts >= kSplit, "the warps of a row take a whole tile");
+    static_assert(kStages >= 3 && kStages % kSlots == 0, "a ring of at least three tiles, each stage one slot's");
     static_assert(kStages * (16 + 16) + kRows * 4 + 96 <= 4096, "small words");
 };
 
@@ -229,7 +235,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
             mbar_init(bars + 8 * s, 1);
-            mbar_init(bars + 8 * (NS + s), RG);
+            mbar_init(bars + 8 * (NS + s), RG * L::kSplit);
         }
         *abort_flag = 0;
         fence_mbar_init();
@@ -333,10 +339,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
     // ---------------------------------------------------------------- consumers
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
-    const int rg = warp % RG, slot = warp / RG;
+    const int rg = warp % RG, part = warp / RG;
+    const int slot = part / L::kSplit, key0 = (part % L::kSplit) * L::kKeys;      // this warp's keys of its slot's tiles
     const int g = lane >> 2, j = lane & 3;       // row and column pair of the fragments
     const int rows_all = a.n_step * a.group;
-    constexpr int KS = MT == 1 ? 64 : 32;        // keys of a step: the scores of 32 rows and 64 keys would not fit beside the output
+    constexpr int KS = L::kKeys;
     constexpr int NT = D / 8;                    // output fragments of 8 columns
     int it = 0;
     bool ok = true;
@@ -433,35 +440,30 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             const uint32_t k_at = stages + st * L::kStageBytes, v_at = k_at + L::kTileBytes, sc_at = v_at + L::kTileBytes;
-            const uint4 where = ld_shared_v4(pos_s + st * 16);
-            int at[4];                           // position of the first key of each 16
-            {
-                const int w4[4] = {static_cast<int>(where.x), static_cast<int>(where.y), static_cast<int>(where.z), static_cast<int>(where.w)};
+            int at[KS / 16];                     // position of the first key of each 16
+            int last = 0;
 #pragma unroll
-                for (int q16 = 0; q16 < 4; ++q16) {
-                    const int pc = (q16 * 16) >> p.piece_log2;
-                    const int first = pc == 0 ? w4[0] : (pc == 1 ? w4[1] : (pc == 2 ? w4[2] : w4[3]));
-                    at[q16] = first < 0 ? INT32_MAX / 2 : first + (q16 * 16 - (pc << p.piece_log2));
-                }
+            for (int i = 0; i < KS / 16; ++i) {
+                const int key = key0 + i * 16, pc = key >> p.piece_log2;
+                int first;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(first) : "r"(pos_s + st * 16 + pc * 4) : "memory");
+                at[i] = first < 0 ? INT32_MAX / 2 : first + (key - (pc << p.piece_log2));
+                last = max(last, at[i] + 16);
             }
-            const bool clean = max(max(at[0], at[1]), max(at[2], at[3])) + 16 <= sees_least;
+            const bool clean = last <= sees_least;
             if (!clean) {
                 // Rows of V that no token sees meet probability 0 and may hold anything: they are cleared.
-                bool any = false;
-                for (int r = lane; r < kTile; r += 32) {
-                    const int q16 = r >> 4, first = q16 == 0 ? at[0] : (q16 == 1 ? at[1] : (q16 == 2 ? at[2] : at[3]));
-                    if (first + (r & 15) >= len) {
+                const int r = key0 + (lane & (KS - 1)), i = (lane & (KS - 1)) >> 4;
+                const int first = KS == 16 || i == 0 ? at[0] : at[KS / 16 - 1];
+                if (first + (r & 15) >= len) {
 #pragma unroll
-                        for (int c = 0; c < ROWB / 16; ++c) st_shared_v4(v_at + chunk_at<ROWB>(r, c), make_uint4(0u, 0u, 0u, 0u));
-                        if (FP8) asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc_at + 256 + r * 4), "f"(1.f) : "memory");
-                        any = true;
-                    }
+                    for (int c = lane / KS; c < ROWB / 16; c += 32 / KS) st_shared_v4(v_at + chunk_at<ROWB>(r, c), make_uint4(0u, 0u, 0u, 0u));
+                    if (FP8) asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc_at + 256 + r * 4), "f"(1.f) : "memory");
+                    fence_proxy_async_smem();    // (the next copy into these rows comes from the asynchronous proxy)
                 }
-                if (any) fence_proxy_async_smem();        // (the next copy into these rows comes from the asynchronous proxy)
                 __syncwarp();
             }
-#pragma unroll
-            for (int k0 = 0; k0 < kTile; k0 += KS) {
+            {
                 float x[MT][KS / 8][4];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
@@ -488,7 +490,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
                     for (int n = 0; n < KS / 8; ++n) {
                         uint32_t kb[4];
-                        ldmatrix_x4(k_at + chunk_at<ROWB>(k0 + n * 8 + (lane & 7), c4 * 4 + (lane >> 3)), kb);
+                        ldmatrix_x4(k_at + chunk_at<ROWB>(key0 + n * 8 + (lane & 7), c4 * 4 + (lane >> 3)), kb);
 #pragma unroll
                         for (int u = 0; u < STEPS; ++u) {
                             uint32_t b0, b1;
@@ -510,8 +512,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 for (int n = 0; n < KS / 8; ++n) {
                     float2 k_sc = make_float2(1.f, 1.f);
                     if (FP8) {
-                        k_sc = ld_shared_f32x2(sc_at + (k0 + n * 8 + 2 * j) * 4);
-                        const float2 v2 = ld_shared_f32x2(sc_at + 256 + (k0 + n * 8 + 2 * j) * 4);
+                        k_sc = ld_shared_f32x2(sc_at + (key0 + n * 8 + 2 * j) * 4);
+                        const float2 v2 = ld_shared_f32x2(sc_at + 256 + (key0 + n * 8 + 2 * j) * 4);
                         vs[FP8 ? n : 0][0] = v2.x;
                         vs[FP8 ? n : 0][1] = v2.y;
                     }
@@ -521,7 +523,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         for (int e = 0; e < 4; ++e) {
                             float v = x[mt][n][e] * row_scale[mt][e >> 1];
                             if (FP8) v *= e & 1 ? k_sc.y : k_sc.x;
-                            if (!clean && at[(k0 + n * 8) >> 4] + ((n & 1) * 8 + 2 * j + (e & 1)) >= sees[mt][e >> 1]) v = -INFINITY;
+                            if (!clean && at[n >> 1] + ((n & 1) * 8 + 2 * j + (e & 1)) >= sees[mt][e >> 1]) v = -INFINITY;
                             x[mt][n][e] = v;
                         }
                 }
@@ -574,7 +576,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                             const float lo = x[mt][2 * kk + (e >> 1)][2 * (e & 1)], hi = x[mt][2 * kk + (e >> 1)][2 * (e & 1) + 1];
                             pa[mt][e] = FP8 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
                         }
-                    const int r = k0 + kk * 16 + (lane & 15);      // matrices (keys 0-7, 8-15) x two 16-byte chunks
+                    const int r = key0 + kk * 16 + (lane & 15);      // matrices (keys 0-7, 8-15) x two 16-byte chunks
 #pragma unroll
                     for (int c2 = 0; c2 < ROWB / 32; ++c2) {
                         uint32_t vb[4];
@@ -614,23 +616,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             for (int h = 0; h < 2; ++h) {
                 l[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][h], 1);
                 l[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][h], 2);
-                if (j == 0) st_shared_f32x2(ml_s + ((slot * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * 8, m[mt][h], l[mt][h]);
+                if (j == 0) st_shared_f32x2(ml_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * 8, m[mt][h], l[mt][h]);
             }
         consumers_sync();
-        const int64_t part = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * L::kRows;
+        const int64_t out_part = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * L::kRows;
         auto joined = [&](int r, float& top, float& sum) {          // r: row of the CTA
             const int of = r / (16 * MT), in = r % (16 * MT);
             top = -INFINITY;
             sum = 0.f;
-            float2 v[L::kSlots];
+            float2 v[L::kParts];
 #pragma unroll
-            for (int w = 0; w < L::kSlots; ++w) {
+            for (int w = 0; w < L::kParts; ++w) {
                 v[w] = ld_shared_f32x2(ml_s + ((w * RG + of) * MT * 16 + in) * 8);
                 top = fmaxf(top, v[w].x);
             }
             const float use = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int w = 0; w < L::kSlots; ++w) sum += v[w].y * exp2_fast(v[w].x - use);
+            for (int w = 0; w < L::kParts; ++w) sum += v[w].y * exp2_fast(v[w].x - use);
         };
         float f[MT][2];
 #pragma unroll
@@ -647,7 +649,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const float over = sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum;
             asm volatile("st.shared.f32 [%0], %1;" ::"r"(qs_s + r * 4), "f"(over) : "memory");      // (q's scales are in registers)
             if (!whole) {
-                p.part_ml[part + r] = make_float2(top, sum);
+                p.part_ml[out_part + r] = make_float2(top, sum);
             } else if (a.lse) {
                 const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
                 a.lse[(static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h] =
@@ -663,7 +665,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float v[2] = {o[mt][c0 / 8 + n0][2 * h] * f[mt][h], o[mt][c0 / 8 + n0][2 * h + 1] * f[mt][h]};
-                        const uint32_t row = red_s + ((slot * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * (kPitch * 4);
+                        const uint32_t row = red_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * (kPitch * 4);
                         if (!FP8) {
                             st_shared_f32x2(row + (n0 * 8 + 2 * j) * 4, v[0], v[1]);
                         } else {                 // fragment 2 c + odd holds columns 16 c + 2 n + odd
@@ -677,13 +679,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 const int r = i >> 4, c = (i & 15) * 2, of = r / (16 * MT), in = r % (16 * MT);
                 float2 v = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < L::kSlots; ++w) {
+                for (int w = 0; w < L::kParts; ++w) {
                     const float2 y = ld_shared_f32x2(red_s + ((w * RG + of) * MT * 16 + in) * (kPitch * 4) + c * 4);
                     v.x += y.x;
                     v.y += y.y;
                 }
                 if (!whole) {
-                    *reinterpret_cast<float2*>(p.part_o + (part + r) * D + c0 + c) = v;
+                    *reinterpret_cast<float2*>(p.part_o + (out_part + r) * D + c0 + c) = v;
                 } else {
                     const float over = ld_shared_f32(qs_s + r * 4);
                     const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
