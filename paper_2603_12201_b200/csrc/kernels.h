@@ -224,7 +224,7 @@ struct PagedAttnArgs {
     __nv_bfloat16* out;         // [B, n_step, H, d]
     float* lse;                 // nullptr, or [B, n_step, H]
 };
-constexpr int kPagedMaxGrid = 160;
+constexpr int kPagedMaxSms = 160;
 size_t paged_attn_workspace_bytes(int n_step, int group, int d);
 bool paged_attn_fits(const PagedAttnArgs& a);           // the tile count of the call stays below 2^31
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,

@@ -27,13 +27,7 @@ namespace idxc {
 namespace {
 
 constexpr int kTile = 64;                       // keys of a tile
-constexpr int kWarps = 8;                       // consumer warps; warp 8 is the producer, three more fill up its warpgroup
-constexpr int kThreads = (kWarps + 4) * 32;
-// Registers: a launch of 384 threads has 168 each, 64512 in all; the producer's warpgroup keeps 40 (5120), the consumers take 232 (59392).
-constexpr int kProducerRegs = 40, kConsumerRegs = 232;
-static_assert(128 * kProducerRegs + 256 * kConsumerRegs <= kThreads * 168, "shares of the launch's registers");
-constexpr int kSmemLimit = 232448 - 128;          // (static shared memory beside it)
-constexpr int kPitch = 40;                      // floats between the rows of a warp's 32-column slice: no bank conflicts on float2 and float4
+constexpr int kProducerRegs = 40;
 constexpr float kF16Head = 16384.f;             // probabilities times scale reach 1; f16 holds them times 2^14
 
 struct Params {
@@ -81,7 +75,8 @@ __device__ __forceinline__ void st_shared_v2(uint32_t addr, uint32_t x, uint32_t
 __device__ __forceinline__ float log2_above(float scale) {
     return static_cast<float>(min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 126, -60), 60));
 }
-__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); }
+template <int WARPS>
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
 
 // ---------------------------------------------------------------- work
 // Keys of request b that the call knows of.
@@ -107,24 +102,23 @@ __device__ __forceinline__ int run_begin(int total, int cta, int grid) {
 }
 __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared, 16 words */) {
     const int units = p.a.c.H_kv * p.row_blocks;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_thr = blockDim.x, n_warps = n_thr >> 5;
     int sum = 0, mine = 0;
-    for (int b = threadIdx.x; b < p.a.B; b += kThreads) {
+    for (int b = threadIdx.x; b < p.a.B; b += n_thr) {
         const int n = tiles_of(p.a, b) * units;
-        if (b < kThreads) mine = n;
+        if (b < n_thr) mine = n;
         sum += n;
     }
     sum = __reduce_add_sync(0xFFFFFFFFu, sum);
     if (lane == 0) scratch[warp] = sum;
     __syncthreads();
     Run r{0, 0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) r.total += scratch[w];
+    for (int w = 0; w < n_warps; ++w) r.total += scratch[w];
     const int first = run_begin(r.total, blockIdx.x, gridDim.x);
     r.n = run_begin(r.total, blockIdx.x + 1, gridDim.x) - first;
     if (r.n > 0) {                               // (uniform over the CTA)
         int before_block = 0;
-        for (int b0 = 0; b0 < p.a.B; b0 += kThreads) {
+        for (int b0 = 0; b0 < p.a.B; b0 += n_thr) {
             const int b = b0 + threadIdx.x;
             const int n = b0 == 0 ? mine : (b < p.a.B ? tiles_of(p.a, b) * units : 0);
             int incl = n;
@@ -137,8 +131,7 @@ __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared,
             if (lane == 31) scratch[warp] = incl;
             __syncthreads();
             int before = before_block + incl - n, all = 0;
-#pragma unroll
-            for (int w = 0; w < kThreads / 32; ++w) {
+            for (int w = 0; w < n_warps; ++w) {
                 if (w < warp) before += scratch[w];
                 all += scratch[w];
             }
@@ -182,8 +175,16 @@ struct Walk {
 };
 
 // ---------------------------------------------------------------- shared memory
+// Up to 32 query rows: 4 consumer warps a CTA and two CTAs an SM, so that one's segment end hides behind the other's tiles. More rows: 8 and
+// one. A fifth (ninth) warp is the producer; three more fill up its warpgroup, because registers are handed out by warpgroups: the launch's
+// 128 (168) a thread, of which the producer's keeps 40.
 template <int D, bool FP8, int MT, int RG>
 struct Layout {
+    static constexpr int kWarps = RG == 1 ? 4 : 8;
+    static constexpr int kThreads = (kWarps + 4) * 32;
+    static constexpr int kCtas = RG == 1 ? 2 : 1;                      // of an SM
+    static constexpr int kConsumerRegs = RG == 1 ? 216 : 232;
+    static_assert(128 * kProducerRegs + kWarps * 32 * kConsumerRegs <= kThreads * (RG == 1 ? 128 : 168), "shares of the launch's registers");
     static constexpr int kRows = 16 * MT * RG;                         // query rows of a CTA
     static constexpr int kParts = kWarps / RG;                         // warps that share a row
     static constexpr int kKeys = D == 128 && !FP8 && RG < 4 ? 16 : 32; // keys of a tile that a warp takes
@@ -191,18 +192,22 @@ struct Layout {
     static constexpr int kSlots = kParts / kSplit;                     // tiles worked on at a time
     static constexpr int kTileBytes = kTile * D * (FP8 ? 1 : 2);
     static constexpr int kStageBytes = 2 * kTileBytes + (FP8 ? 1024 : 0);      // K, V, scales of K and of V (256 bytes each)
+    static constexpr int kSlice = MT == 1 ? 32 : 16;                   // columns of the output that go through shared memory at a time
+    static constexpr int kPitch = kSlice + 8;                          // floats between rows there: no bank conflicts on float2
     static constexpr int kQBytes = kRows * D * 2;
     static constexpr int kRedBytes = kWarps * MT * 16 * kPitch * 4;
+    static constexpr int kShared = kQBytes > kRedBytes ? kQBytes : kRedBytes;  // q, and the output's slices when q is done with
     static constexpr int kMlBytes = kWarps * MT * 16 * 8;
-    static constexpr int kSmall = 1024 + 4096;                         // alignment of the stages; barriers, positions, scales of q
-    static constexpr int kFit = (kSmemLimit - kSmall - kQBytes - kRedBytes - kMlBytes) / kStageBytes;
+    static constexpr int kSmall = 1024 + 1536;                         // alignment of the stages; barriers, positions, scales of q
+    static constexpr int kLimit = (233472 - kCtas * (1024 + 128)) / kCtas;     // an SM's, without what the system and static arrays take
+    static constexpr int kFit = (kLimit - kSmall - kShared - kMlBytes) / kStageBytes;
     // A stage belongs to one slot, whose warps see every phase of its barrier: were the stages no multiple of the slots, a warp could come to
     // a stage's barrier while the tile before its own is still on the way, and take the parity of the one before that for its own.
     static constexpr int kStages = (kFit > 24 ? 24 : kFit) / kSlots * kSlots;
-    static constexpr int kBytes = kSmall + kStages * kStageBytes + kQBytes + kRedBytes + kMlBytes;
+    static constexpr int kBytes = kSmall + kStages * kStageBytes + kShared + kMlBytes;
     static_assert(kParts >= kSplit, "the warps of a row take a whole tile");
     static_assert(kStages >= 3 && kStages % kSlots == 0, "a ring of at least three tiles, each stage one slot's");
-    static_assert(kStages * (16 + 16) + kRows * 4 + 96 <= 4096, "small words");
+    static_assert(kStages * (16 + 16) + kRows * 4 + 16 <= 1536, "small words");
 };
 
 // Byte offset of 16-byte chunk `c` of row `r` in a tile whose rows are at most 128 bytes (wider ones lie in blocks of 128).
@@ -213,17 +218,17 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
 }
 
 template <int D, bool FP8, int MT, int RG>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__((Layout<D, FP8, MT, RG>::kThreads), (Layout<D, FP8, MT, RG>::kCtas))
 paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ Params p) {
     using L = Layout<D, FP8, MT, RG>;
     constexpr int ROWB = D * (FP8 ? 1 : 2);      // bytes of a cached row
-    constexpr int NS = L::kStages;
+    constexpr int NS = L::kStages, W = L::kWarps;
     extern __shared__ uint8_t raw[];
     const uint32_t base = smem_u32(raw);
     const uint32_t stages = (base + 1023u) & ~1023u;
     const uint32_t q_s = stages + NS * L::kStageBytes;
-    const uint32_t red_s = q_s + L::kQBytes;
-    const uint32_t ml_s = red_s + L::kRedBytes;
+    const uint32_t red_s = q_s;
+    const uint32_t ml_s = q_s + L::kShared;
     const uint32_t bars = ml_s + L::kMlBytes;    // full[NS], empty[NS]
     const uint32_t pos_s = bars + NS * 16;       // [NS][4] position of the first key of each piece, -1: none
     const uint32_t qs_s = pos_s + NS * 16;       // [kRows] power of two taken out of a row of q
@@ -248,9 +253,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const PagedAttnArgs& a = p.a;
     if (threadIdx.x == 0 && blockIdx.x == 0) *p.total = run.total;
 
-    if (warp >= kWarps) {
+    if (warp >= W) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
-        if (warp > kWarps) return;
+        if (warp > W) return;
         // ------------------------------------------------------------ producer: pieces of pages into the ring
         const int piece = 1 << p.piece_log2, per_tile_log2 = 6 - p.piece_log2, per_tile = 1 << per_tile_log2;
         const uint32_t piece_bytes = static_cast<uint32_t>(piece) * (2 * ROWB + (FP8 ? 8 : 0));
@@ -338,7 +343,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 
     // ---------------------------------------------------------------- consumers
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kConsumerRegs));
     const int rg = warp % RG, part = warp / RG;
     const int slot = part / L::kSplit, key0 = (part % L::kSplit) * L::kKeys;      // this warp's keys of its slot's tiles
     const int g = lane >> 2, j = lane & 3;       // row and column pair of the fragments
@@ -356,7 +361,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         const int n_rows = min(rows_all - row0, L::kRows);
         const bool whole = s.t0 == 0 && s.n == s.nt;
         // q of the segment, zeros behind the last row
-        for (int i = threadIdx.x; i < L::kRows * (D / 8); i += kWarps * 32) {
+        for (int i = threadIdx.x; i < L::kRows * (D / 8); i += W * 32) {
             const int r = i / (D / 8), c = i - r * (D / 8);
             uint4 x = make_uint4(0u, 0u, 0u, 0u);
             if (r < n_rows) {
@@ -392,7 +397,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 st_shared_v2(hi, h[1], h[3]);
             }
         }
-        consumers_sync();
+        consumers_sync<W>();
 
         // Address of this lane's row for an A fragment of q: matrices (rows 0-7, 8-15) x (columns 0-7, 8-15).
         auto q_frag = [&](int mt, int ks, uint32_t(&f)[4]) {
@@ -618,7 +623,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 l[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][h], 2);
                 if (j == 0) st_shared_f32x2(ml_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * 8, m[mt][h], l[mt][h]);
             }
-        consumers_sync();
+        consumers_sync<W>();
         const int64_t out_part = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * L::kRows;
         auto joined = [&](int r, float& top, float& sum) {          // r: row of the CTA
             const int of = r / (16 * MT), in = r % (16 * MT);
@@ -643,7 +648,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 joined((rg * MT + mt) * 16 + h * 8 + g, top, sum);
                 f[mt][h] = exp2_fast(m[mt][h] - (top == -INFINITY ? 0.f : top));
             }
-        for (int r = threadIdx.x; r < n_rows; r += kWarps * 32) {
+        for (int r = threadIdx.x; r < n_rows; r += W * 32) {
             float top, sum;
             joined(r, top, sum);
             const float over = sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum;
@@ -657,15 +662,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
         }
 #pragma unroll
-        for (int c0 = 0; c0 < D; c0 += 32) {
+        for (int c0 = 0; c0 < D; c0 += L::kSlice) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int n0 = 0; n0 < 4; ++n0)
+                for (int n0 = 0; n0 < L::kSlice / 8; ++n0)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float v[2] = {o[mt][c0 / 8 + n0][2 * h] * f[mt][h], o[mt][c0 / 8 + n0][2 * h + 1] * f[mt][h]};
-                        const uint32_t row = red_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * (kPitch * 4);
+                        const uint32_t row = red_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * (L::kPitch * 4);
                         if (!FP8) {
                             st_shared_f32x2(row + (n0 * 8 + 2 * j) * 4, v[0], v[1]);
                         } else {                 // fragment 2 c + odd holds columns 16 c + 2 n + odd
@@ -674,13 +679,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                             asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(v[1]) : "memory");
                         }
                     }
-            consumers_sync();
-            for (int i = threadIdx.x; i < n_rows * 16; i += kWarps * 32) {
-                const int r = i >> 4, c = (i & 15) * 2, of = r / (16 * MT), in = r % (16 * MT);
+            consumers_sync<W>();
+            for (int i = threadIdx.x; i < n_rows * (L::kSlice / 2); i += W * 32) {
+                const int r = i / (L::kSlice / 2), c = i % (L::kSlice / 2) * 2, of = r / (16 * MT), in = r % (16 * MT);
                 float2 v = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < L::kParts; ++w) {
-                    const float2 y = ld_shared_f32x2(red_s + ((w * RG + of) * MT * 16 + in) * (kPitch * 4) + c * 4);
+                    const float2 y = ld_shared_f32x2(red_s + ((w * RG + of) * MT * 16 + in) * (L::kPitch * 4) + c * 4);
                     v.x += y.x;
                     v.y += y.y;
                 }
@@ -693,7 +698,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     *reinterpret_cast<uint32_t*>(a.out + to) = pack_bf16(v.x * over, v.y * over);
                 }
             }
-            consumers_sync();
+            consumers_sync<W>();
         }
         if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.unit, s.n, s.nt);
     }
@@ -704,9 +709,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (tiles_of(a, b) != 0) continue;
         const int64_t n_vec = static_cast<int64_t>(a.n_step) * a.H * (D / 8);
         uint4* to = reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(b) * a.n_step * a.H * D);
-        for (int64_t i = threadIdx.x; i < n_vec; i += kWarps * 32) to[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int64_t i = threadIdx.x; i < n_vec; i += W * 32) to[i] = make_uint4(0u, 0u, 0u, 0u);
         if (a.lse)
-            for (int i = threadIdx.x; i < a.n_step * a.H; i += kWarps * 32) a.lse[static_cast<int64_t>(b) * a.n_step * a.H + i] = -INFINITY;
+            for (int i = threadIdx.x; i < a.n_step * a.H; i += W * 32) a.lse[static_cast<int64_t>(b) * a.n_step * a.H + i] = -INFINITY;
     }
 }
 
@@ -776,15 +781,17 @@ paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) 
     if (p.a.lse && lane == 0) p.a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
+int max_grid(int cta_rows) { return cta_rows <= 32 ? 2 * kPagedMaxSms : kPagedMaxSms; }
 int rows_of_cta(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128)); }
 
 template <int D, bool FP8, int MT, int RG>
-cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, int grid, cudaStream_t stream, int* launches) {
+cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, int sm_count, cudaStream_t stream, int* launches) {
     using L = Layout<D, FP8, MT, RG>;
+    const int grid = sm_count * L::kCtas < max_grid(L::kRows) ? sm_count * L::kCtas : max_grid(L::kRows);
     auto kernel = paged_attn_kernel<D, FP8, MT, RG>;
     cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes);
     if (e != cudaSuccess) return e;
-    e = launch_behind(kernel, dim3(grid), kThreads, L::kBytes, stream, k_map, v_map, p);
+    e = launch_behind(kernel, dim3(grid), L::kThreads, L::kBytes, stream, k_map, v_map, p);
     *launches += 1;
     if (e != cudaSuccess) return e;
     const int rows = p.a.n_step * p.a.group < L::kRows ? p.a.n_step * p.a.group : L::kRows;
@@ -796,8 +803,8 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
 
 // owners and total, the pieces' maxima and sums, the pieces
 size_t paged_attn_workspace_bytes(int n_step, int group, int d) {
-    const size_t rows = static_cast<size_t>(rows_of_cta(n_step * group));
-    return kPagedMaxGrid * 16 + 256 + kPagedMaxGrid * 2 * rows * (8 + static_cast<size_t>(d) * 4);
+    const size_t rows = static_cast<size_t>(rows_of_cta(n_step * group)), grid = static_cast<size_t>(max_grid(static_cast<int>(rows)));
+    return grid * 16 + 256 + grid * 2 * rows * (8 + static_cast<size_t>(d) * 4);
 }
 bool paged_attn_fits(const PagedAttnArgs& a) {
     const int64_t rows = static_cast<int64_t>(a.n_step) * a.group, cta = rows_of_cta(a.n_step * a.group);
@@ -819,16 +826,16 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUt
     p.scale_log2 = a.scale * 1.4426950408889634f;
     uint8_t* w = static_cast<uint8_t*>(workspace);
     p.owners = reinterpret_cast<int4*>(w);
-    p.total = reinterpret_cast<int*>(w + kPagedMaxGrid * 16);
-    p.part_ml = reinterpret_cast<float2*>(w + kPagedMaxGrid * 16 + 256);
-    p.part_o = reinterpret_cast<float*>(w + kPagedMaxGrid * 16 + 256 + static_cast<size_t>(kPagedMaxGrid) * 2 * cta_rows * 8);
+    const size_t grid = static_cast<size_t>(max_grid(cta_rows));
+    p.total = reinterpret_cast<int*>(w + grid * 16);
+    p.part_ml = reinterpret_cast<float2*>(w + grid * 16 + 256);
+    p.part_o = reinterpret_cast<float*>(w + grid * 16 + 256 + grid * 2 * cta_rows * 8);
     p.status = status;
-    const int grid = sm_count < kPagedMaxGrid ? sm_count : kPagedMaxGrid;
 #define IDXC_RUN(D_, F_)                                                                                   \
-    (cta_rows == 16   ? run<D_, F_, 1, 1>(k_map, v_map, p, grid, stream, launches)                          \
-     : cta_rows == 32 ? run<D_, F_, 2, 1>(k_map, v_map, p, grid, stream, launches)                          \
-     : cta_rows == 64 ? run<D_, F_, 2, 2>(k_map, v_map, p, grid, stream, launches)                          \
-                      : run<D_, F_, 2, 4>(k_map, v_map, p, grid, stream, launches))
+    (cta_rows == 16   ? run<D_, F_, 1, 1>(k_map, v_map, p, sm_count, stream, launches)                          \
+     : cta_rows == 32 ? run<D_, F_, 2, 1>(k_map, v_map, p, sm_count, stream, launches)                          \
+     : cta_rows == 64 ? run<D_, F_, 2, 2>(k_map, v_map, p, sm_count, stream, launches)                          \
+                      : run<D_, F_, 2, 4>(k_map, v_map, p, sm_count, stream, launches))
     if (a.c.d == 128) return a.c.fp8 ? IDXC_RUN(128, true) : IDXC_RUN(128, false);
     return a.c.fp8 ? IDXC_RUN(64, true) : IDXC_RUN(64, false);
 #undef IDXC_RUN
