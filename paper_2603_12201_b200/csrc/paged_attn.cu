@@ -3,16 +3,19 @@
 // over all pages of a request, or over the pages that a selection names for each (request, key head).
 //
 // What bounds it: a key and a value of d columns are 4 d bytes (bf16) and 4 d flops a query row; with the 1 to 32 rows that share a key head
-// in a decode step that is 1 to 32 flops a byte, far below the tensor cores' 200: HBM. So the design serves the copies. One CTA an SM, a ring of
-// 64-key tiles of K and V (32 KB in bf16 with d = 128) filled by TMA from whole pages or 16-key pieces of them, and warp-level MMAs, which take
-// their operands from shared memory with one ldmatrix each and keep scores, softmax and output in registers: 128 MMAs a tile and 16 rows, of which
-// the tensor cores issue several times what the copies deliver. (A tile is the M = 16 rows of up to 16 query rows; tcgen05's M = 64 or 128 would
-// be mostly padding, and its accumulators would cross tensor memory twice a tile.)
+// in a decode step that is 1 to 32 flops a byte, far below the tensor cores' 200: HBM. So the design serves the copies: a ring of 64-key tiles of K
+// and V (32 KB in bf16 with d = 128), filled by TMA with whole pages or 16-key pieces of them, and as few instructions a tile as will do.
 //
-// Each of 8 warps takes 16 or 32 keys of a tile and up to 32 query rows (with more rows, 2 or 4 warps the same keys) with its own running
-// maximum and sum; the warps meet once at a segment's end. The tiles of all (request, key head, block of rows), end to end, are cut into equal runs, a run a
-// CTA, which finds it from the lengths on the device; segments cut by a run's end go to the workspace in fp32 and through a merge kernel. All sums
-// have an order fixed by the sizes, so results repeat bit for bit.
+// Keys are the M = 16 of the matrix instructions, query rows their N = 8: S^T = K Q^T and O^T = V^T P^T. Up to 8 rows (a group of 8 heads) then waste
+// nothing, K and V are read from shared memory once for any number of rows, and scores, softmax and output stay in registers. (With rows as M, 8 rows were half
+// padding, and 8-bit tiles took 1740 instructions instead of ~1000. tcgen05's M = 64 or 128 with rows as N would fit too, but its scores would cross
+// tensor memory twice a tile, a latency that several resident CTAs would have to hide.) P^T comes out of the scores' registers by an 8 x 8 transposition.
+//
+// Up to 32 rows: 4 warps, each 16 keys of a tile with its own running reference and sum; 2 or 3 CTAs an SM hide each other's segment ends. More rows:
+// 8 warps, of which 2 or 4 share the keys and take 32 rows each. The warps' parts meet once at a segment's end, in shared memory. The tiles of all
+// (request, key head, block of rows), end to end, are cut into runs of equal cost, a run a CTA, which finds it from the lengths on the device;
+// segments cut by a run's end go to the workspace in fp32 and through a merge kernel. All sums have an order fixed by the sizes, so results
+// repeat bit for bit.
 //
 // e4m3 rows: codes become f16 (exact) on the way to the registers, with q as f16 times a power of two a row (its largest element in [1, 2); what
 // falls below f16's range is below 2^-25 of that, an fp32 rounding). The value's scale goes into the probability, whose reference is the running
@@ -28,7 +31,9 @@ namespace {
 
 constexpr int kTile = 64;                       // keys of a tile
 constexpr int kProducerRegs = 40;
-constexpr float kF16Head = 16384.f;             // probabilities times scale reach 1; f16 holds them times 2^14
+constexpr int kSegmentTiles = 4;                // what a segment's beginning and end cost, in tiles
+constexpr float kSlack = 8.f;                   // log2 units by which a score may pass its row's reference before that moves
+constexpr float kF16Head = 64.f;                // probabilities times scale reach 2^kSlack; f16 holds them times 2^6
 
 struct Params {
     PagedAttnArgs a;
@@ -65,6 +70,23 @@ __device__ __forceinline__ float2 ld_shared_f32x2(uint32_t addr) {
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ float4 ld_shared_f32x4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_shared_u32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_shared_f32(uint32_t addr, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory"); }
+// An 8 x 8 matrix of 16-bit elements, lane 4 g + j holding elements 2 j, + 1 of row g, transposed.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
 __device__ __forceinline__ void st_shared_f32x2(uint32_t addr, float x, float y) {
     asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y) : "memory");
 }
@@ -88,12 +110,15 @@ __device__ __forceinline__ int tiles_of(const PagedAttnArgs& a, int b) {
     const int pages = (len + a.c.page_size - 1) / a.c.page_size;
     return static_cast<int>((static_cast<int64_t>(min(a.n_sel, pages)) * a.c.page_size + kTile - 1) / kTile);
 }
+// The units (request, key head, block of rows) lie end to end, each kSegmentTiles and its tiles long, and are cut into runs of equal length: a
+// run with many short segments gets fewer tiles. A run that ends among the first kSegmentTiles of a unit has none of its tiles.
 struct Run {
-    int b, x;             // request, tile among all of the request's units
-    int n;                // tiles
-    int total;
+    int b, x;             // request, place among all of the request's units
+    int n;                // length
+    int total;            // of all units
 };
-// First tile of a CTA's run: total * cta / n, cut among n = min(grid, total) CTAs so that no run in front of another is empty.
+__device__ __forceinline__ int length_of_unit(int tiles) { return tiles > 0 ? tiles + kSegmentTiles : 0; }
+// Beginning of a CTA's run: total * cta / n, cut among n = min(grid, total) CTAs so that no run in front of another is empty.
 __device__ __forceinline__ int run_begin(int total, int cta, int grid) {
     const int n = min(grid, total);
     if (cta >= n) return total;
@@ -105,7 +130,7 @@ __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared,
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_thr = blockDim.x, n_warps = n_thr >> 5;
     int sum = 0, mine = 0;
     for (int b = threadIdx.x; b < p.a.B; b += n_thr) {
-        const int n = tiles_of(p.a, b) * units;
+        const int n = length_of_unit(tiles_of(p.a, b)) * units;
         if (b < n_thr) mine = n;
         sum += n;
     }
@@ -120,7 +145,7 @@ __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared,
         int before_block = 0;
         for (int b0 = 0; b0 < p.a.B; b0 += n_thr) {
             const int b = b0 + threadIdx.x;
-            const int n = b0 == 0 ? mine : (b < p.a.B ? tiles_of(p.a, b) * units : 0);
+            const int n = b0 == 0 ? mine : (b < p.a.B ? length_of_unit(tiles_of(p.a, b)) * units : 0);
             int incl = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -157,56 +182,58 @@ struct Walk {
     int b, x, left, nt;
     __device__ __forceinline__ Walk(const Params& q, const Run& r) : p(q), b(r.b), x(r.x), left(r.n), nt(r.n > 0 ? tiles_of(q.a, r.b) : 0) {}
     __device__ __forceinline__ bool next(Segment& s) {
-        if (left <= 0) return false;
         const int units = p.a.c.H_kv * p.row_blocks;
-        while (x == nt * units) {                // the request's end (or one without tiles); more tiles follow
-            nt = tiles_of(p.a, ++b);
-            x = 0;
+        while (left > 0) {
+            while (x == length_of_unit(nt) * units) {       // the request's end (or one without tiles); more follow
+                nt = tiles_of(p.a, ++b);
+                x = 0;
+            }
+            const int len = nt + kSegmentTiles;
+            s.b = b;
+            s.unit = x / len;
+            const int from = x - s.unit * len, n = min(len - from, left);
+            x += n;
+            left -= n;
+            s.t0 = max(from - kSegmentTiles, 0);
+            s.n = max(from + n - kSegmentTiles, 0) - s.t0;
+            s.nt = nt;
+            if (s.n > 0) return true;
         }
-        s.b = b;
-        s.unit = x / nt;
-        s.t0 = x - s.unit * nt;
-        s.n = min(nt - s.t0, left);
-        s.nt = nt;
-        x += s.n;
-        left -= s.n;
-        return true;
+        return false;
     }
 };
 
 // ---------------------------------------------------------------- shared memory
-// Up to 32 query rows: 4 consumer warps a CTA and two CTAs an SM, so that one's segment end hides behind the other's tiles. More rows: 8 and
-// one. A fifth (ninth) warp is the producer; three more fill up its warpgroup, because registers are handed out by warpgroups: the launch's
-// 128 (168) a thread, of which the producer's keeps 40.
-template <int D, bool FP8, int MT, int RG>
+// NR blocks of 8 query rows a warp, RG warps side by side over the rows.
+// With 32 rows a warp the output alone is 128 registers of d = 128: registers are then handed out unevenly, by warpgroups (three idle warps fill
+// up the producer's): the launch's 128 (168) a thread, of which the producer's warpgroup keeps 40.
+template <int D, bool FP8, int NR, int RG>
 struct Layout {
-    static constexpr int kWarps = RG == 1 ? 4 : 8;
-    static constexpr int kThreads = (kWarps + 4) * 32;
-    static constexpr int kCtas = RG == 1 ? 2 : 1;                      // of an SM
+    static constexpr int kWarps = RG == 1 ? 4 : 8;                     // consumers
+    static constexpr bool kUneven = NR == 4;
+    static constexpr int kThreads = (kWarps + (kUneven ? 4 : 1)) * 32;
+    static constexpr int kCtas = RG > 1 ? 1 : (NR == 1 && (FP8 || D == 64) ? 3 : 2);      // of an SM
     static constexpr int kConsumerRegs = RG == 1 ? 216 : 232;
-    static_assert(128 * kProducerRegs + kWarps * 32 * kConsumerRegs <= kThreads * (RG == 1 ? 128 : 168), "shares of the launch's registers");
-    static constexpr int kRows = 16 * MT * RG;                         // query rows of a CTA
-    static constexpr int kParts = kWarps / RG;                         // warps that share a row
-    static constexpr int kKeys = D == 128 && !FP8 && RG < 4 ? 16 : 32; // keys of a tile that a warp takes
-    static constexpr int kSplit = kTile / kKeys;                       // warps (of a row) that share a tile
-    static constexpr int kSlots = kParts / kSplit;                     // tiles worked on at a time
+    static_assert(128 * kProducerRegs + kWarps * 32 * kConsumerRegs <= (kWarps + 4) * 32 * (RG == 1 ? 128 : 168), "shares of the launch's registers");
+    static constexpr int kRows = 8 * NR * RG;                          // query rows of a CTA
+    static constexpr int kParts = kWarps / RG;                         // warps that share a row; they share every tile
+    static constexpr int kKeys = kTile / kParts;                       // keys of a tile that a warp takes
     static constexpr int kTileBytes = kTile * D * (FP8 ? 1 : 2);
     static constexpr int kStageBytes = 2 * kTileBytes + (FP8 ? 1024 : 0);      // K, V, scales of K and of V (256 bytes each)
-    static constexpr int kSlice = MT == 1 ? 32 : 16;                   // columns of the output that go through shared memory at a time
-    static constexpr int kPitch = kSlice + 8;                          // floats between rows there: no bank conflicts on float2
+    static constexpr int kSlice = NR == 1 ? 64 : (NR == 2 ? 32 : 16);  // columns of the output that go through shared memory at a time
+    static constexpr int kPitch = kSlice + 4;                          // floats between rows there: no bank conflicts
     static constexpr int kQBytes = kRows * D * 2;
-    static constexpr int kRedBytes = kWarps * MT * 16 * kPitch * 4;
+    static constexpr int kRedBytes = kParts * kRows * kPitch * 4;
     static constexpr int kShared = kQBytes > kRedBytes ? kQBytes : kRedBytes;  // q, and the output's slices when q is done with
-    static constexpr int kMlBytes = kWarps * MT * 16 * 8;
-    static constexpr int kSmall = 1024 + 1536;                         // alignment of the stages; barriers, positions, scales of q
+    static constexpr int kMlBytes = kParts * kRows * 8;
+    static constexpr int kSmall = 1024 + 1536;                         // alignment of the stages; barriers, positions, a number per row
     static constexpr int kLimit = (233472 - kCtas * (1024 + 128)) / kCtas;     // an SM's, without what the system and static arrays take
     static constexpr int kFit = (kLimit - kSmall - kShared - kMlBytes) / kStageBytes;
-    // A stage belongs to one slot, whose warps see every phase of its barrier: were the stages no multiple of the slots, a warp could come to
-    // a stage's barrier while the tile before its own is still on the way, and take the parity of the one before that for its own.
-    static constexpr int kStages = (kFit > 24 ? 24 : kFit) / kSlots * kSlots;
+    // Every warp sees every phase of every stage's barrier. (If warps took tiles in turn, one could come to a stage's barrier while the tile
+    // before its own is still on the way, and take the parity of the one before that for its own.)
+    static constexpr int kStages = kFit > 24 ? 24 : kFit;
     static constexpr int kBytes = kSmall + kStages * kStageBytes + kShared + kMlBytes;
-    static_assert(kParts >= kSplit, "the warps of a row take a whole tile");
-    static_assert(kStages >= 3 && kStages % kSlots == 0, "a ring of at least three tiles, each stage one slot's");
+    static_assert(kKeys % 16 == 0 && kStages >= 3, "whole steps of 16 keys, a ring of at least three tiles");
     static_assert(kStages * (16 + 16) + kRows * 4 + 16 <= 1536, "small words");
 };
 
@@ -217,10 +244,10 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
     return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
 }
 
-template <int D, bool FP8, int MT, int RG>
-__global__ void __launch_bounds__((Layout<D, FP8, MT, RG>::kThreads), (Layout<D, FP8, MT, RG>::kCtas))
+template <int D, bool FP8, int NR, int RG>
+__global__ void __launch_bounds__((Layout<D, FP8, NR, RG>::kThreads), (Layout<D, FP8, NR, RG>::kCtas))
 paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ Params p) {
-    using L = Layout<D, FP8, MT, RG>;
+    using L = Layout<D, FP8, NR, RG>;
     constexpr int ROWB = D * (FP8 ? 1 : 2);      // bytes of a cached row
     constexpr int NS = L::kStages, W = L::kWarps;
     extern __shared__ uint8_t raw[];
@@ -228,11 +255,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const uint32_t stages = (base + 1023u) & ~1023u;
     const uint32_t q_s = stages + NS * L::kStageBytes;
     const uint32_t red_s = q_s;
-    const uint32_t ml_s = q_s + L::kShared;
+    const uint32_t ml_s = q_s + L::kShared;      // [parts][rows] (maximum, sum) of a warp, then (factor, -)
     const uint32_t bars = ml_s + L::kMlBytes;    // full[NS], empty[NS]
     const uint32_t pos_s = bars + NS * 16;       // [NS][4] position of the first key of each piece, -1: none
-    const uint32_t qs_s = pos_s + NS * 16;       // [kRows] power of two taken out of a row of q
-    const uint32_t flag_s = qs_s + L::kRows * 4;
+    const uint32_t row_s = pos_s + NS * 16;      // [rows] power of two taken out of a row of q; at the end what the row is multiplied by
+    const uint32_t flag_s = row_s + L::kRows * 4;
     __shared__ int scratch[16];
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(raw + (flag_s - base));
 
@@ -240,7 +267,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
             mbar_init(bars + 8 * s, 1);
-            mbar_init(bars + 8 * (NS + s), RG * L::kSplit);
+            mbar_init(bars + 8 * (NS + s), W);
         }
         *abort_flag = 0;
         fence_mbar_init();
@@ -254,7 +281,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     if (threadIdx.x == 0 && blockIdx.x == 0) *p.total = run.total;
 
     if (warp >= W) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
+        if (L::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
         if (warp > W) return;
         // ------------------------------------------------------------ producer: pieces of pages into the ring
         const int piece = 1 << p.piece_log2, per_tile_log2 = 6 - p.piece_log2, per_tile = 1 << per_tile_log2;
@@ -343,97 +370,113 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 
     // ---------------------------------------------------------------- consumers
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kConsumerRegs));
+    if (L::kUneven) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kConsumerRegs));
     const int rg = warp % RG, part = warp / RG;
-    const int slot = part / L::kSplit, key0 = (part % L::kSplit) * L::kKeys;      // this warp's keys of its slot's tiles
-    const int g = lane >> 2, j = lane & 3;       // row and column pair of the fragments
+    const int g = lane >> 2, j = lane & 3;       // of a fragment: key (or output column) g and g + 8, query rows 2 j and 2 j + 1
+    const int warp_row = rg * NR * 8;            // first row of the CTA's that is this warp's
     const int rows_all = a.n_step * a.group;
-    constexpr int KS = L::kKeys;
-    constexpr int NT = D / 8;                    // output fragments of 8 columns
+    constexpr int NT = D / 16;                   // output fragments of 16 columns
+    constexpr bool kQRegs = NR < 4;              // q's fragments stay in registers, and the next segment's q is on its way early
+    constexpr int QV = L::kRows * (D / 8) / (W * 32) > 0 ? L::kRows * (D / 8) / (W * 32) : 1;      // vectors of q a thread brings
+    constexpr int Q_THREADS = L::kRows * (D / 8) < W * 32 ? L::kRows * (D / 8) : W * 32;
+
+    auto load_q = [&](const Segment& s, uint4(&q)[QV]) {              // zeros behind the last row
+        const int head = s.unit / p.row_blocks, row0 = (s.unit - head * p.row_blocks) * L::kRows;
+#pragma unroll
+        for (int u = 0; u < QV; ++u) {
+            const int i = threadIdx.x + u * W * 32, r = i / (D / 8), c = i - r * (D / 8);
+            q[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (threadIdx.x < Q_THREADS && row0 + r < rows_all) {
+                const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
+                q[u] = __ldg(reinterpret_cast<const uint4*>(a.q + (static_cast<int64_t>(s.b) * a.n_step + step) * a.q_stride +
+                                                            static_cast<int64_t>(head * a.group + h) * D) + c);
+            }
+        }
+    };
     int it = 0;
     bool ok = true;
     Walk walk(p, run);
-    Segment s;
+    Segment s, after;
     int4 owner = make_int4(-1, 0, 0, 0);
-    while (walk.next(s)) {
+    uint4 q_next[QV];
+    bool more = walk.next(after);
+    if (kQRegs && more) load_q(after, q_next);
+    while (more) {
+        s = after;
+        if (!kQRegs) load_q(s, q_next);
         const int len = length_of(a, s.b);
         const int head = s.unit / p.row_blocks, row0 = (s.unit - head * p.row_blocks) * L::kRows;
         const int n_rows = min(rows_all - row0, L::kRows);
         const bool whole = s.t0 == 0 && s.n == s.nt;
-        // q of the segment, zeros behind the last row
-        for (int i = threadIdx.x; i < L::kRows * (D / 8); i += W * 32) {
-            const int r = i / (D / 8), c = i - r * (D / 8);
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (r < n_rows) {
-                const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
-                x = __ldg(reinterpret_cast<const uint4*>(a.q + (static_cast<int64_t>(s.b) * a.n_step + step) * a.q_stride +
-                                                         static_cast<int64_t>(head * a.group + h) * D) + c);
-            }
-            const uint32_t row_at = q_s + r * (D * 2);
-            if (!FP8) {
-                st_shared_v4(row_at + ((c ^ (r & 7)) << 4), x);
-            } else {
-                // the D / 8 threads of a row are neighbours in a warp
-                const uint32_t* w = &x.x;
-                float f[8], top = 0.f;
+        if (threadIdx.x < Q_THREADS) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    f[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
-                    top = fmaxf(top, fabsf(f[e]));
+            for (int u = 0; u < QV; ++u) {
+                const int i = threadIdx.x + u * W * 32, r = i / (D / 8), c = i - r * (D / 8);
+                const uint32_t row_at = q_s + r * (D * 2);
+                const uint4 x = q_next[u];
+                if (!FP8) {
+                    st_shared_v4(row_at + ((c ^ (r & 7)) << 4), x);
+                } else {
+                    // the D / 8 threads of a row are neighbours in a warp
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    float f[8], top = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        f[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+                        top = fmaxf(top, fabsf(f[e]));
+                    }
+#pragma unroll
+                    for (int o = D / 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                    const int exponent = min(max(static_cast<int>(__float_as_uint(top) >> 23), 1), 253);      // top in [2^(exponent - 127), 2 of that)
+                    const float down = __uint_as_float(static_cast<uint32_t>(254 - exponent) << 23);
+                    if (c == 0) st_shared_f32(row_s + r * 4, __uint_as_float(static_cast<uint32_t>(exponent) << 23));
+                    uint32_t h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[e] = pack_f16(f[2 * e] * down, f[2 * e + 1] * down);
+                    // Of 16 columns lane j of a fragment takes 4 j .. 4 j + 3 (the four codes of a register of K): pairs 0 and 1 of each four
+                    // go to places 2 j and 2 j + 8.
+                    const int block = c >> 1, odd = c & 1;             // 16 columns; the second eight of them
+                    st_shared_v2(row_at + (((2 * block) ^ (r & 7)) << 4) + odd * 8, h[0], h[2]);
+                    st_shared_v2(row_at + (((2 * block + 1) ^ (r & 7)) << 4) + odd * 8, h[1], h[3]);
                 }
-#pragma unroll
-                for (int o = D / 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                const int exponent = min(max(static_cast<int>(__float_as_uint(top) >> 23), 1), 253);      // top in [2^(exponent - 127), 2 of that)
-                const float down = __uint_as_float(static_cast<uint32_t>(254 - exponent) << 23);
-                if (c == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(qs_s + r * 4), "f"(__uint_as_float(static_cast<uint32_t>(exponent) << 23)) : "memory");
-                uint32_t h[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = pack_f16(f[2 * e] * down, f[2 * e + 1] * down);
-                // Of 16 columns lane j of a fragment takes 4 j .. 4 j + 3 (the four codes of a register of K): pairs 0 and 1 of each four
-                // go to places 2 j and 2 j + 8.
-                const int block = c >> 1, odd = c & 1;                 // 16 columns; the second eight of them
-                const uint32_t lo = row_at + (((2 * block) ^ (r & 7)) << 4) + odd * 8, hi = row_at + (((2 * block + 1) ^ (r & 7)) << 4) + odd * 8;
-                st_shared_v2(lo, h[0], h[2]);
-                st_shared_v2(hi, h[1], h[3]);
             }
         }
         consumers_sync<W>();
 
-        // Address of this lane's row for an A fragment of q: matrices (rows 0-7, 8-15) x (columns 0-7, 8-15).
-        auto q_frag = [&](int mt, int ks, uint32_t(&f)[4]) {
-            const int r = (rg * MT + mt) * 16 + (lane & 15), c = 2 * ks + (lane >> 4);
+        // B fragments of q for two steps of 16 columns and a block of 8 rows: matrices of 8 rows x 8 columns side by side.
+        auto q_frag = [&](int nr, int c4, uint32_t(&f)[4]) {
+            const int r = warp_row + nr * 8 + (lane & 7), c = c4 * 4 + (lane >> 3);
             ldmatrix_x4(q_s + r * (D * 2) + ((c ^ (r & 7)) << 4), f);
         };
-        uint32_t qf[MT == 1 ? D / 16 : 1][4];
-        if (MT == 1) {
+        uint32_t qf[kQRegs ? NR : 1][kQRegs ? D / 32 : 1][4];
+        if (kQRegs) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) q_frag(0, ks, qf[MT == 1 ? ks : 0]);
+            for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                for (int c4 = 0; c4 < D / 32; ++c4) q_frag(nr, c4, qf[kQRegs ? nr : 0][kQRegs ? c4 : 0]);
         }
-        int sees[MT][2];                         // keys that the row of fragment half h sees
-        float row_scale[MT][2];
-        float m[MT][2], l[MT][2];
-        float o[MT][NT][4];
-        int sees_least = len;
+        int sees[NR][2];                         // keys that rows 2 j, 2 j + 1 see
+        float row_scale[NR][2], m[NR][2], l[NR][2];
+        float o[NR][NT][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = (rg * MT + mt) * 16 + h * 8 + g;
-                sees[mt][h] = len - (a.n_step - 1 - min((row0 + r) / a.group, a.n_step - 1));
-                row_scale[mt][h] = FP8 ? p.scale_log2 * ld_shared_f32(qs_s + r * 4) : p.scale_log2;
-                m[mt][h] = -INFINITY;
-                l[mt][h] = 0.f;
+            for (int e = 0; e < 2; ++e) {
+                const int r = warp_row + nr * 8 + 2 * j + e;
+                sees[nr][e] = len - (a.n_step - 1 - min((row0 + r) / a.group, a.n_step - 1));
+                row_scale[nr][e] = FP8 ? p.scale_log2 * ld_shared_f32(row_s + r * 4) : p.scale_log2;
+                m[nr][e] = -INFINITY;
+                l[nr][e] = 0.f;
             }
-        sees_least = len - (a.n_step - 1);       // (of the request's first token)
+        const int sees_least = len - (a.n_step - 1);      // (of the request's first token)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[mt][n][e] = 0.f;
+                for (int e = 0; e < 4; ++e) o[nr][n][e] = 0.f;
 
-        // first tile of the segment whose place in the run is this warp's
-        for (int t = (slot - it % L::kSlots + L::kSlots) % L::kSlots; t < s.n; t += L::kSlots) {
+        for (int t = 0; t < s.n; ++t) {
             const int st = (it + t) % NS;
             if (ok && !mbar_wait(bars + 8 * st, ((it + t) / NS) & 1, abort_flag)) {
                 if (lane == 0) {
@@ -445,166 +488,144 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             const uint32_t k_at = stages + st * L::kStageBytes, v_at = k_at + L::kTileBytes, sc_at = v_at + L::kTileBytes;
-            int at[KS / 16];                     // position of the first key of each 16
-            int last = 0;
 #pragma unroll
-            for (int i = 0; i < KS / 16; ++i) {
-                const int key = key0 + i * 16, pc = key >> p.piece_log2;
-                int first;
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(first) : "r"(pos_s + st * 16 + pc * 4) : "memory");
-                at[i] = first < 0 ? INT32_MAX / 2 : first + (key - (pc << p.piece_log2));
-                last = max(last, at[i] + 16);
-            }
-            const bool clean = last <= sees_least;
-            if (!clean) {
-                // Rows of V that no token sees meet probability 0 and may hold anything: they are cleared.
-                const int r = key0 + (lane & (KS - 1)), i = (lane & (KS - 1)) >> 4;
-                const int first = KS == 16 || i == 0 ? at[0] : at[KS / 16 - 1];
-                if (first + (r & 15) >= len) {
+            for (int step = 0; step < L::kKeys / 16; ++step) {
+                const int key0 = (part * (L::kKeys / 16) + step) * 16;
+                const int pc = key0 >> p.piece_log2;
+                int at = static_cast<int>(ld_shared_u32(pos_s + st * 16 + pc * 4));      // position of the first of the 16 keys
+                at = at < 0 ? INT32_MAX / 2 : at + (key0 - (pc << p.piece_log2));
+                const bool clean = at + 16 <= sees_least;
+                if (!clean) {
+                    // Rows of V that no token sees meet probability 0 and may hold anything: they are cleared. (Warps that share keys clear them alike.)
+                    const int r = key0 + (lane & 15);
+                    if (at + (lane & 15) >= len) {
 #pragma unroll
-                    for (int c = lane / KS; c < ROWB / 16; c += 32 / KS) st_shared_v4(v_at + chunk_at<ROWB>(r, c), make_uint4(0u, 0u, 0u, 0u));
-                    if (FP8) asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc_at + 256 + r * 4), "f"(1.f) : "memory");
-                    fence_proxy_async_smem();    // (the next copy into these rows comes from the asynchronous proxy)
+                        for (int c = 0; c < ROWB / 16; c += 2) st_shared_v4(v_at + chunk_at<ROWB>(r, c + (lane >> 4)), make_uint4(0u, 0u, 0u, 0u));
+                        if (FP8) st_shared_f32(sc_at + 256 + r * 4, 1.f);
+                        fence_proxy_async_smem();          // (the next copy into these rows comes from the asynchronous proxy)
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
-            }
-            {
-                float x[MT][KS / 8][4];
+                // scores of 16 keys: A fragments straight from K's rows, (keys 0-7, 8-15) x two 16-byte chunks an ldmatrix; two sums a block
+                // halve the chain of dependent instructions
+                float x[NR][2][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-                    for (int n = 0; n < KS / 8; ++n)
+                    for (int e = 0; e < 8; ++e) x[nr][e >> 2][e & 3] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][n][e] = 0.f;
-                // scores: an ldmatrix takes 8 keys x 64 bytes
-                constexpr int STEPS = FP8 ? 4 : 2;        // 16-column steps in 64 bytes
+                for (int c4 = 0; c4 < D / 32; ++c4) {                  // 32 columns: two steps of 16
+                    uint32_t ka[2][4];
+                    if (!FP8) {
 #pragma unroll
-                for (int c4 = 0; c4 < ROWB / 64; ++c4) {
-                    uint32_t qa[STEPS][MT][4];
-#pragma unroll
-                    for (int u = 0; u < STEPS; ++u)
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            if (MT == 1) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) qa[u][mt][e] = qf[MT == 1 ? c4 * STEPS + u : 0][e];
-                            } else {
-                                q_frag(mt, c4 * STEPS + u, qa[u][mt]);
-                            }
-                        }
-#pragma unroll
-                    for (int n = 0; n < KS / 8; ++n) {
+                        for (int u = 0; u < 2; ++u)
+                            ldmatrix_x4(k_at + chunk_at<ROWB>(key0 + (lane & 15), c4 * 4 + 2 * u + (lane >> 4)), ka[u]);
+                    } else {
                         uint32_t kb[4];
-                        ldmatrix_x4(k_at + chunk_at<ROWB>(key0 + n * 8 + (lane & 7), c4 * 4 + (lane >> 3)), kb);
+                        ldmatrix_x4(k_at + chunk_at<ROWB>(key0 + (lane & 15), c4 * 2 + (lane >> 4)), kb);
 #pragma unroll
-                        for (int u = 0; u < STEPS; ++u) {
-                            uint32_t b0, b1;
-                            if (FP8) {
-                                b0 = e4m3x2_to_f16x2(kb[u] & 0xFFFFu);
-                                b1 = e4m3x2_to_f16x2(kb[u] >> 16);
-                            } else {
-                                b0 = kb[(2 * u) & 3];
-                                b1 = kb[(2 * u + 1) & 3];
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {              // keys g and g + 8: four codes each
+                                ka[u][h] = e4m3x2_to_f16x2(kb[2 * u + h] & 0xFFFFu);
+                                ka[u][2 + h] = e4m3x2_to_f16x2(kb[2 * u + h] >> 16);
                             }
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) mma_16816<FP8>(x[mt][n], qa[u][mt], b0, b1);
-                        }
-                    }
-                }
-                // softmax: x becomes probabilities (times the value's scale for 8 bits)
-                float vs[FP8 ? KS / 8 : 1][2];
-#pragma unroll
-                for (int n = 0; n < KS / 8; ++n) {
-                    float2 k_sc = make_float2(1.f, 1.f);
-                    if (FP8) {
-                        k_sc = ld_shared_f32x2(sc_at + (key0 + n * 8 + 2 * j) * 4);
-                        const float2 v2 = ld_shared_f32x2(sc_at + 256 + (key0 + n * 8 + 2 * j) * 4);
-                        vs[FP8 ? n : 0][0] = v2.x;
-                        vs[FP8 ? n : 0][1] = v2.y;
                     }
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int nr = 0; nr < NR; ++nr) {
+                        uint32_t qb[4];
+                        if (kQRegs) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float v = x[mt][n][e] * row_scale[mt][e >> 1];
-                            if (FP8) v *= e & 1 ? k_sc.y : k_sc.x;
-                            if (!clean && at[n >> 1] + ((n & 1) * 8 + 2 * j + (e & 1)) >= sees[mt][e >> 1]) v = -INFINITY;
-                            x[mt][n][e] = v;
+                            for (int e = 0; e < 4; ++e) qb[e] = qf[kQRegs ? nr : 0][kQRegs ? c4 : 0][e];
+                        } else {
+                            q_frag(nr, c4, qb);
                         }
+                        mma_16816<FP8>(x[nr][0], ka[0], qb[0], qb[1]);
+                        mma_16816<FP8>(x[nr][1], ka[1], qb[2], qb[3]);
+                    }
                 }
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    float top[2] = {m[mt][0], m[mt][1]};
-#pragma unroll
-                    for (int n = 0; n < KS / 8; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) top[e >> 1] = fmaxf(top[e >> 1], FP8 ? x[mt][n][e] + log2_above(vs[FP8 ? n : 0][e & 1]) : x[mt][n][e]);
-                    float use[2];
-                    bool moved = false;
+                // softmax: element 2 h + e is key g + 8 h, row 2 j + e
+                float k_sc[2] = {1.f, 1.f}, v_sc[2] = {1.f, 1.f}, above[2] = {0.f, 0.f};
+                if (FP8) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        top[h] = fmaxf(top[h], __shfl_xor_sync(0xFFFFFFFFu, top[h], 1));
-                        top[h] = fmaxf(top[h], __shfl_xor_sync(0xFFFFFFFFu, top[h], 2));
-                        use[h] = top[h] == -INFINITY ? 0.f : top[h];
-                        moved |= top[h] != m[mt][h];
+                        k_sc[h] = ld_shared_f32(sc_at + (key0 + g + 8 * h) * 4);
+                        v_sc[h] = ld_shared_f32(sc_at + 256 + (key0 + g + 8 * h) * 4);
+                        above[h] = log2_above(v_sc[h]);
+                        v_sc[h] *= kF16Head;
                     }
-                    if (__any_sync(0xFFFFFFFFu, moved)) {
+                }
+                uint32_t pb[NR][2];
+                bool moved = false;
+                float top[NR][2], y[NR][4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float f = exp2_fast(m[mt][h] - use[h]);
-                            l[mt][h] *= f;
-                            m[mt][h] = top[h];
+                for (int nr = 0; nr < NR; ++nr) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float v = (x[nr][0][e] + x[nr][1][e]) * row_scale[nr][e & 1];
+                        if (FP8) v *= k_sc[e >> 1];
+                        if (!clean && at + g + 8 * (e >> 1) >= sees[nr][e & 1]) v = -INFINITY;
+                        y[nr][e] = v;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        top[nr][e] = FP8 ? fmaxf(y[nr][e] + above[0], y[nr][2 + e] + above[1]) : fmaxf(y[nr][e], y[nr][2 + e]);
+                        moved |= !(top[nr][e] <= m[nr][e] + kSlack);   // (no number: as one that moves)
+                    }
+                }
+                if (__any_sync(0xFFFFFFFFu, moved)) {      // (rare behind a segment's first keys)
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float v = fmaxf(m[nr][e], top[nr][e]);
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+                            const float f = exp2_fast(m[nr][e] - (v == -INFINITY ? 0.f : v));
+                            m[nr][e] = v;
+                            l[nr][e] *= f;
 #pragma unroll
                             for (int n = 0; n < NT; ++n) {
-                                o[mt][n][2 * h] *= f;
-                                o[mt][n][2 * h + 1] *= f;
+                                o[nr][n][e] *= f;
+                                o[nr][n][2 + e] *= f;
                             }
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < KS / 8; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float pr = exp2_fast(x[mt][n][e] - use[e >> 1]);
-                            l[mt][e >> 1] += pr;
-                            x[mt][n][e] = FP8 ? pr * (vs[FP8 ? n : 0][e & 1] * kF16Head) : pr;
                         }
                 }
-                // output
 #pragma unroll
-                for (int kk = 0; kk < KS / 16; ++kk) {
-                    uint32_t pa[MT][4];
+                for (int nr = 0; nr < NR; ++nr) {
+                    const float use[2] = {m[nr][0] == -INFINITY ? 0.f : m[nr][0], m[nr][1] == -INFINITY ? 0.f : m[nr][1]};
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int e = 0; e < 4; ++e) {
+                        y[nr][e] = exp2_fast(y[nr][e] - use[e & 1]);
+                        l[nr][e & 1] += y[nr][e];
+                        if (FP8) y[nr][e] *= v_sc[e >> 1];
+                    }
+                    pb[nr][0] = transpose_8x8(FP8 ? pack_f16(y[nr][0], y[nr][1]) : pack_bf16(y[nr][0], y[nr][1]));
+                    pb[nr][1] = transpose_8x8(FP8 ? pack_f16(y[nr][2], y[nr][3]) : pack_bf16(y[nr][2], y[nr][3]));
+                }
+                // output: A fragments are V's rows transposed
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float lo = x[mt][2 * kk + (e >> 1)][2 * (e & 1)], hi = x[mt][2 * kk + (e >> 1)][2 * (e & 1) + 1];
-                            pa[mt][e] = FP8 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
-                        }
-                    const int r = key0 + kk * 16 + (lane & 15);      // matrices (keys 0-7, 8-15) x two 16-byte chunks
+                for (int c2 = 0; c2 < ROWB / 32; ++c2) {
+                    uint32_t va[4];
+                    if (!FP8) {
+                        // (keys 0-7; columns 0-7, 8-15), then keys 8-15
+                        ldmatrix_x4_trans(v_at + chunk_at<ROWB>(key0 + (lane & 7) + (lane >> 4) * 8, 2 * c2 + (lane >> 3 & 1)), va);
 #pragma unroll
-                    for (int c2 = 0; c2 < ROWB / 32; ++c2) {
-                        uint32_t vb[4];
-                        ldmatrix_x4_trans(v_at + chunk_at<ROWB>(r, 2 * c2 + (lane >> 4)), vb);
-                        if (!FP8) {
+                        for (int nr = 0; nr < NR; ++nr) mma_16816<false>(o[nr][c2 % NT], va, pb[nr][0], pb[nr][1]);
+                    } else {
+                        uint32_t vb[4];                    // (keys 0-7, 8-15) of a 16-byte chunk, then of the next
+                        ldmatrix_x4_trans(v_at + chunk_at<ROWB>(key0 + (lane & 15), 2 * c2 + (lane >> 4)), vb);
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) {
-                                mma_16816<false>(o[mt][(2 * c2) % NT], pa[mt], vb[0], vb[1]);
-                                mma_16816<false>(o[mt][(2 * c2 + 1) % NT], pa[mt], vb[2], vb[3]);
-                            }
-                        } else {
-                            // A register holds columns 2 g, 2 g + 1 of keys 2 j, 2 j + 1: the even column's pair of keys, then the odd one's.
+                        for (int u = 0; u < 2; ++u) {
+                            // A register holds columns 2 g, 2 g + 1 of keys 2 j, 2 j + 1: the even column's two keys become row g of the fragment, the
+                            // odd one's row g + 8.
+                            const uint32_t w0 = __byte_perm(vb[2 * u], 0, 0x3120), w1 = __byte_perm(vb[2 * u + 1], 0, 0x3120);
+                            va[0] = e4m3x2_to_f16x2(w0 & 0xFFFFu);
+                            va[1] = e4m3x2_to_f16x2(w0 >> 16);
+                            va[2] = e4m3x2_to_f16x2(w1 & 0xFFFFu);
+                            va[3] = e4m3x2_to_f16x2(w1 >> 16);
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                const uint32_t w0 = __byte_perm(vb[2 * u], 0, 0x3120), w1 = __byte_perm(vb[2 * u + 1], 0, 0x3120);
-                                const uint32_t e0 = e4m3x2_to_f16x2(w0 & 0xFFFFu), e1 = e4m3x2_to_f16x2(w1 & 0xFFFFu);
-                                const uint32_t d0 = e4m3x2_to_f16x2(w0 >> 16), d1 = e4m3x2_to_f16x2(w1 >> 16);
-#pragma unroll
-                                for (int mt = 0; mt < MT; ++mt) {
-                                    mma_16816<true>(o[mt][(4 * c2 + 2 * u) % NT], pa[mt], e0, e1);
-                                    mma_16816<true>(o[mt][(4 * c2 + 2 * u + 1) % NT], pa[mt], d0, d1);
-                                }
-                            }
+                            for (int nr = 0; nr < NR; ++nr) mma_16816<true>(o[nr][(2 * c2 + u) % NT], va, pb[nr][0], pb[nr][1]);
                         }
                     }
                 }
@@ -613,89 +634,87 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             if (lane == 0) mbar_arrive(bars + 8 * (NS + st));
         }
         it += s.n;
+        more = walk.next(after);
+        if (kQRegs && more) load_q(after, q_next);         // (on the way while the warps' parts are joined)
 
         // ------------------------------------------------------------ the warps' parts of the segment joined
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                l[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][h], 1);
-                l[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][h], 2);
-                if (j == 0) st_shared_f32x2(ml_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * 8, m[mt][h], l[mt][h]);
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[nr][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nr][e], d);
+                if (g == 0) st_shared_f32x2(ml_s + (part * L::kRows + warp_row + nr * 8 + 2 * j + e) * 8, m[nr][e], l[nr][e]);
             }
         consumers_sync<W>();
-        const int64_t out_part = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * L::kRows;
-        auto joined = [&](int r, float& top, float& sum) {          // r: row of the CTA
-            const int of = r / (16 * MT), in = r % (16 * MT);
-            top = -INFINITY;
-            sum = 0.f;
+        const int64_t piece_row = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * L::kRows;
+        for (int r = threadIdx.x; r < n_rows; r += W * 32) {
             float2 v[L::kParts];
+            float best = -INFINITY, sum = 0.f;
 #pragma unroll
             for (int w = 0; w < L::kParts; ++w) {
-                v[w] = ld_shared_f32x2(ml_s + ((w * RG + of) * MT * 16 + in) * 8);
-                top = fmaxf(top, v[w].x);
+                v[w] = ld_shared_f32x2(ml_s + (w * L::kRows + r) * 8);
+                best = fmaxf(best, v[w].x);
             }
-            const float use = top == -INFINITY ? 0.f : top;
+            const float use = best == -INFINITY ? 0.f : best;
 #pragma unroll
-            for (int w = 0; w < L::kParts; ++w) sum += v[w].y * exp2_fast(v[w].x - use);
-        };
-        float f[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float top, sum;
-                joined((rg * MT + mt) * 16 + h * 8 + g, top, sum);
-                f[mt][h] = exp2_fast(m[mt][h] - (top == -INFINITY ? 0.f : top));
+            for (int w = 0; w < L::kParts; ++w) {
+                const float f = exp2_fast(v[w].x - use);
+                sum += v[w].y * f;
+                st_shared_f32(ml_s + (w * L::kRows + r) * 8, f);
             }
-        for (int r = threadIdx.x; r < n_rows; r += W * 32) {
-            float top, sum;
-            joined(r, top, sum);
-            const float over = sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum;
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(qs_s + r * 4), "f"(over) : "memory");      // (q's scales are in registers)
+            st_shared_f32(row_s + r * 4, whole ? (sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum) : 1.f);
             if (!whole) {
-                p.part_ml[out_part + r] = make_float2(top, sum);
+                p.part_ml[piece_row + r] = make_float2(best, sum);
             } else if (a.lse) {
                 const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
                 a.lse[(static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h] =
-                    sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+                    sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
             }
         }
+        consumers_sync<W>();
+        float f[NR][2];
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) f[nr][e] = ld_shared_f32(ml_s + (part * L::kRows + warp_row + nr * 8 + 2 * j + e) * 8);
 #pragma unroll
         for (int c0 = 0; c0 < D; c0 += L::kSlice) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-                for (int n0 = 0; n0 < L::kSlice / 8; ++n0)
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t row = red_s + ((part * L::kRows + warp_row + nr * 8 + 2 * j + e) * L::kPitch) * 4;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float v[2] = {o[mt][c0 / 8 + n0][2 * h] * f[mt][h], o[mt][c0 / 8 + n0][2 * h + 1] * f[mt][h]};
-                        const uint32_t row = red_s + ((part * RG + rg) * MT * 16 + mt * 16 + h * 8 + g) * (L::kPitch * 4);
-                        if (!FP8) {
-                            st_shared_f32x2(row + (n0 * 8 + 2 * j) * 4, v[0], v[1]);
-                        } else {                 // fragment 2 c + odd holds columns 16 c + 2 n + odd
-                            const uint32_t to = row + ((n0 >> 1) * 16 + 4 * j + (n0 & 1)) * 4;
-                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(v[0]) : "memory");
-                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(v[1]) : "memory");
+                    for (int n0 = 0; n0 < L::kSlice / 16; ++n0) {
+                        const float lo = o[nr][c0 / 16 + n0][e] * f[nr][e], hi = o[nr][c0 / 16 + n0][2 + e] * f[nr][e];
+                        if (FP8) {               // columns 16 n + 2 g, + 1
+                            st_shared_f32x2(row + (n0 * 16 + 2 * g) * 4, lo, hi);
+                        } else {                 // 16 n + g, + 8
+                            st_shared_f32(row + (n0 * 16 + g) * 4, lo);
+                            st_shared_f32(row + (n0 * 16 + 8 + g) * 4, hi);
                         }
                     }
+                }
             consumers_sync<W>();
-            for (int i = threadIdx.x; i < n_rows * (L::kSlice / 2); i += W * 32) {
-                const int r = i / (L::kSlice / 2), c = i % (L::kSlice / 2) * 2, of = r / (16 * MT), in = r % (16 * MT);
-                float2 v = make_float2(0.f, 0.f);
+            for (int i = threadIdx.x; i < n_rows * (L::kSlice / 4); i += W * 32) {
+                const int r = i / (L::kSlice / 4), c = i % (L::kSlice / 4) * 4;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < L::kParts; ++w) {
-                    const float2 y = ld_shared_f32x2(red_s + ((w * RG + of) * MT * 16 + in) * (L::kPitch * 4) + c * 4);
-                    v.x += y.x;
-                    v.y += y.y;
+                    const float4 z = ld_shared_f32x4(red_s + ((w * L::kRows + r) * L::kPitch + c) * 4);
+                    v.x += z.x;
+                    v.y += z.y;
+                    v.z += z.z;
+                    v.w += z.w;
                 }
                 if (!whole) {
-                    *reinterpret_cast<float2*>(p.part_o + (out_part + r) * D + c0 + c) = v;
+                    *reinterpret_cast<float4*>(p.part_o + (piece_row + r) * D + c0 + c) = v;
                 } else {
-                    const float over = ld_shared_f32(qs_s + r * 4);
+                    const float over = ld_shared_f32(row_s + r * 4);
                     const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
                     const int64_t to = ((static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h) * D + c0 + c;
-                    *reinterpret_cast<uint32_t*>(a.out + to) = pack_bf16(v.x * over, v.y * over);
+                    *reinterpret_cast<uint2*>(a.out + to) = make_uint2(pack_bf16(v.x * over, v.y * over), pack_bf16(v.z * over, v.w * over));
                 }
             }
             consumers_sync<W>();
@@ -732,7 +751,7 @@ paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) 
     int pieces;                                  // the segment's tiles after this run fill the runs that follow
     {
         const int n = min(grid, total);
-        const int last_tile = run_begin(total, cta + 1, grid) + (own.w - own.z) - 1;                    // end to end; in the run of
+        const int last_tile = run_begin(total, cta + 1, grid) + (own.w - own.z) - 1;                    // its place; it is in the run of
         const int last = static_cast<int>(((static_cast<int64_t>(last_tile) + 1) * n + total - 1) / total) - 1;      // the last c with total * c / n <= last_tile
         pieces = last - cta + 1;
     }
@@ -781,14 +800,14 @@ paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) 
     if (p.a.lse && lane == 0) p.a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
-int max_grid(int cta_rows) { return cta_rows <= 32 ? 2 * kPagedMaxSms : kPagedMaxSms; }
-int rows_of_cta(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128)); }
+int max_grid(int cta_rows) { return cta_rows <= 8 ? 3 * kPagedMaxSms : (cta_rows <= 32 ? 2 * kPagedMaxSms : kPagedMaxSms); }
+int rows_of_cta(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128))); }
 
-template <int D, bool FP8, int MT, int RG>
+template <int D, bool FP8, int NR, int RG>
 cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, int sm_count, cudaStream_t stream, int* launches) {
-    using L = Layout<D, FP8, MT, RG>;
+    using L = Layout<D, FP8, NR, RG>;
     const int grid = sm_count * L::kCtas < max_grid(L::kRows) ? sm_count * L::kCtas : max_grid(L::kRows);
-    auto kernel = paged_attn_kernel<D, FP8, MT, RG>;
+    auto kernel = paged_attn_kernel<D, FP8, NR, RG>;
     cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes);
     if (e != cudaSuccess) return e;
     e = launch_behind(kernel, dim3(grid), L::kThreads, L::kBytes, stream, k_map, v_map, p);
@@ -808,12 +827,12 @@ size_t paged_attn_workspace_bytes(int n_step, int group, int d) {
 }
 bool paged_attn_fits(const PagedAttnArgs& a) {
     const int64_t rows = static_cast<int64_t>(a.n_step) * a.group, cta = rows_of_cta(a.n_step * a.group);
-    int64_t keys = a.max_len + kTile;
+    int64_t keys = a.max_len + kTile;            // (a tile more than there are)
     if (a.pages) {
         const int64_t pages = (a.max_len + a.c.page_size - 1) / a.c.page_size;
         keys = (pages < a.n_sel ? pages : a.n_sel) * a.c.page_size + kTile;
     }
-    return static_cast<double>(a.B) * a.c.H_kv * ((rows + cta - 1) / cta) * (keys / kTile) < 2147483648.0;
+    return static_cast<double>(a.B) * a.c.H_kv * ((rows + cta - 1) / cta) * (keys / kTile + kSegmentTiles) < 2147483648.0;
 }
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
@@ -832,10 +851,11 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUt
     p.part_o = reinterpret_cast<float*>(w + grid * 16 + 256 + grid * 2 * cta_rows * 8);
     p.status = status;
 #define IDXC_RUN(D_, F_)                                                                                   \
-    (cta_rows == 16   ? run<D_, F_, 1, 1>(k_map, v_map, p, sm_count, stream, launches)                          \
-     : cta_rows == 32 ? run<D_, F_, 2, 1>(k_map, v_map, p, sm_count, stream, launches)                          \
-     : cta_rows == 64 ? run<D_, F_, 2, 2>(k_map, v_map, p, sm_count, stream, launches)                          \
-                      : run<D_, F_, 2, 4>(k_map, v_map, p, sm_count, stream, launches))
+    (cta_rows == 8    ? run<D_, F_, 1, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
+     : cta_rows == 16 ? run<D_, F_, 2, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
+     : cta_rows == 32 ? run<D_, F_, 4, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
+     : cta_rows == 64 ? run<D_, F_, 4, 2>(k_map, v_map, p, sm_count, stream, launches)                      \
+                      : run<D_, F_, 4, 4>(k_map, v_map, p, sm_count, stream, launches))
     if (a.c.d == 128) return a.c.fp8 ? IDXC_RUN(128, true) : IDXC_RUN(128, false);
     return a.c.fp8 ? IDXC_RUN(64, true) : IDXC_RUN(64, false);
 #undef IDXC_RUN
