@@ -33,6 +33,7 @@ struct ScoreArgsP {
     int64_t ld;
     int32_t* n_out;
     int groups_per_warp;         // of eight pages
+    int heads;                   // key heads of a CTA: 1, 2, 4 or 8
 };
 
 __device__ __forceinline__ uint32_t part_of(uint32_t x, bool positive) {
@@ -50,14 +51,18 @@ page_scores_kernel(const ScoreArgsP a) {
     let_next_start();
     wait_for_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, j = lane & 3;
-    const int b = blockIdx.z, head = blockIdx.y;
+    // The warps of a CTA take its heads of the same pages: a page's bounds lie side by side over the heads, and are read at about the same time.
+    const int b = blockIdx.z, head = blockIdx.y * a.heads + warp % a.heads, slices = kWarps / a.heads;
+    const int first = (blockIdx.x * a.groups_per_warp * slices + warp / a.heads) * 8, step = slices * 8;
+    const int32_t* table = a.table + b * a.ld_table;
+    auto page_of = [&](int p) -> int { return p < a.ld_table ? __ldg(table + p) : -1; };
+    int page_next = page_of(first + g);          // (on its way beside the length)
     const int64_t len = max(a.lens[b], 0);
     const int pages = static_cast<int>(min((len + a.P - 1) / a.P, a.ld_table));
     const int64_t out_row = static_cast<int64_t>(b) * a.H_kv + head;
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.n_out[out_row] = pages;
+    if (blockIdx.x == 0 && warp < a.heads && lane == 0) a.n_out[out_row] = pages;
     const int rows = a.n_step * a.group;
-    const int first = (blockIdx.x * kWarps + warp) * a.groups_per_warp * 8;
-    if (static_cast<int>(blockIdx.x) * kWarps * a.groups_per_warp * 8 >= pages) return;
+    if (static_cast<int>(blockIdx.x) * a.groups_per_warp * step >= pages) return;
     auto q_row = [&](int r) -> const uint4* {    // query row r: token r / group, head r % group of the key head's
         const int i = r / a.group;
         return reinterpret_cast<const uint4*>(a.q + (static_cast<int64_t>(b) * a.n_step + i) * a.q_stride +
@@ -73,6 +78,7 @@ page_scores_kernel(const ScoreArgsP a) {
         }
     }
     for (int r0 = 0; r0 < rows; r0 += kMaxRows) {
+        if (r0 > 0) page_next = page_of(first + g);
         const int n_rows = min(kMaxRows, rows - r0), tiles = FEW ? 1 : (n_rows + 15) / 16;
         if (!FEW) {
             __syncthreads();
@@ -82,17 +88,30 @@ page_scores_kernel(const ScoreArgsP a) {
             }
             __syncthreads();
         }
-        for (int p0 = first; p0 < min(first + a.groups_per_warp * 8, pages); p0 += 8) {
-            const int p = p0 + g;
-            const int64_t page = p < pages ? a.table[b * a.ld_table + p] : -1;
-            const bool valid = page >= 0 && page < a.n_pages;
-            const uint4* edge = reinterpret_cast<const uint4*>(a.bounds) + ((valid ? page : 0) * a.H_kv + head) * (D / 4) + j;
+        // The bounds of the next eight pages are on their way while these are worked on.
+        uint4 lo_next[KC], hi_next[KC];
+        bool valid_next = false;
+        auto fetch = [&](int p0) {
+            const int64_t page = p0 + g < pages ? page_next : -1;
+            valid_next = page >= 0 && page < a.n_pages;
+            const uint4* edge = reinterpret_cast<const uint4*>(a.bounds) + ((valid_next ? page : 0) * a.H_kv + head) * (D / 4) + j;
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                lo_next[c] = valid_next ? __ldg(edge + 4 * c) : none;
+                hi_next[c] = valid_next ? __ldg(edge + D / 8 + 4 * c) : none;
+            }
+            page_next = page_of(p0 + step + g);
+        };
+        fetch(first);
+        for (int i = 0, p0 = first; i < a.groups_per_warp && p0 < pages; ++i, p0 += step) {
+            const bool valid = valid_next;
             uint4 lo[KC], hi[KC];
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
-                lo[c] = valid ? __ldg(edge + 4 * c) : none;
-                hi[c] = valid ? __ldg(edge + D / 8 + 4 * c) : none;
+                lo[c] = lo_next[c];
+                hi[c] = hi_next[c];
             }
+            if (i + 1 < a.groups_per_warp) fetch(p0 + step);
             float best0 = -INFINITY, best1 = -INFINITY;          // pages p0 + 2 j, + 1
             for (int t = 0; t < tiles; ++t) {
                 float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -153,12 +172,16 @@ cudaError_t launch_page_scores(const void* bounds, int64_t n_pages, int P, int H
                                const int32_t* table, int64_t ld_table, const int32_t* lens, int B, int keep_first, int keep_last, float scale,
                                float* scores, int64_t ld, int32_t* n_out, int sm_count, cudaStream_t stream) {
     ScoreArgsP a{static_cast<const __nv_bfloat16*>(bounds), n_pages, P, H_kv, static_cast<const __nv_bfloat16*>(q), q_stride, n_step, group, table, ld_table,
-                 lens, keep_first, keep_last, scale, scores, ld, n_out, 1};
-    const int64_t groups = (ld_table + 7) / 8, ctas = (groups + kWarps - 1) / kWarps * B * H_kv;
-    while (a.groups_per_warp < 16 && ctas / (2 * a.groups_per_warp) >= 8 * sm_count) a.groups_per_warp *= 2;
-    const int64_t per_cta = static_cast<int64_t>(kWarps) * a.groups_per_warp;
-    const dim3 grid(static_cast<unsigned>((groups + per_cta - 1) / per_cta), static_cast<unsigned>(H_kv), static_cast<unsigned>(B));
+                 lens, keep_first, keep_last, scale, scores, ld, n_out, 1, 1};
     const bool few = n_step * group <= 16;
+    while (few && a.heads < 8 && H_kv % (2 * a.heads) == 0) a.heads *= 2;      // (more rows: q of one head in shared memory)
+    // As many groups of eight pages a warp as leave two CTAs for every SM a few times over: requests end anywhere in front of ld_table.
+    const int64_t most = ld_table < (1 << 27) ? ld_table : 1 << 27;                  // pages of 2^31 positions
+    const int64_t groups = (most + 7) / 8, slices = kWarps / a.heads;
+    const int64_t all = (groups + slices - 1) / slices * B * (H_kv / a.heads);      // CTAs with one group a warp
+    while (a.groups_per_warp < 8 && all / (a.groups_per_warp + 1) >= 2 * sm_count) ++a.groups_per_warp;
+    const int64_t per_cta = slices * a.groups_per_warp;
+    const dim3 grid(static_cast<unsigned>((groups + per_cta - 1) / per_cta), static_cast<unsigned>(H_kv / a.heads), static_cast<unsigned>(B));
     if (d == 128)
         return few ? launch_behind(page_scores_kernel<128, true>, grid, kWarps * 32, 0, stream, a)
                    : launch_behind(page_scores_kernel<128, false>, grid, kWarps * 32, 0, stream, a);

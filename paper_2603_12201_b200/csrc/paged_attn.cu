@@ -29,7 +29,6 @@
 namespace idxc {
 namespace {
 
-constexpr int kTile = 64;                       // keys of a tile
 constexpr int kProducerRegs = 40;
 constexpr int kSegmentTiles = 4;                // what a segment's beginning and end cost, in tiles
 constexpr float kSlack = 8.f;                   // log2 units by which a score may pass its row's reference before that moves
@@ -37,7 +36,10 @@ constexpr float kF16Head = 64.f;                // probabilities times scale rea
 
 struct Params {
     PagedAttnArgs a;
-    int row_blocks;              // blocks of MAXR query rows of a (request, key head)
+    int heads;                   // key heads that as many neighbouring CTAs walk through in step
+    int units;                   // (heads of a CTA, blocks of query rows) of a request
+    int row_blocks;              // blocks of a CTA's query rows of a (request, key head)
+    int tile_log2;               // keys of a tile
     int piece_log2;              // keys of a copy: 16, 32 or 64
     float scale_log2;            // scale * log2(e)
     float* part_o;               // [grid][2][MAXR][D]
@@ -104,13 +106,15 @@ __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;
 // Keys of request b that the call knows of.
 __device__ __forceinline__ int length_of(const PagedAttnArgs& a, int b) { return min(max(__ldg(a.lens + b), 0), static_cast<int>(a.max_len)); }
 // Tiles of one (key head, block of rows) of request b: of its keys, or of the first min(n_sel, pages of the request) entries of its selection.
-__device__ __forceinline__ int tiles_of(const PagedAttnArgs& a, int b) {
-    const int len = length_of(a, b);
-    if (!a.pages) return (len + kTile - 1) / kTile;
-    const int pages = (len + a.c.page_size - 1) / a.c.page_size;
-    return static_cast<int>((static_cast<int64_t>(min(a.n_sel, pages)) * a.c.page_size + kTile - 1) / kTile);
+__device__ __forceinline__ int tiles_of(const Params& p, int b) {
+    const int len = length_of(p.a, b), up = (1 << p.tile_log2) - 1;
+    if (!p.a.pages) return (len + up) >> p.tile_log2;
+    const int pages = (len + p.a.c.page_size - 1) / p.a.c.page_size;
+    return static_cast<int>((static_cast<int64_t>(min(p.a.n_sel, pages)) * p.a.c.page_size + up) >> p.tile_log2);
 }
-// The units (request, key head, block of rows) lie end to end, each kSegmentTiles and its tiles long, and are cut into runs of equal length: a
+// p.heads neighbouring CTAs take the same stretch of keys for as many key heads, so that the rows of one token, which lie side by side in a cache with
+// tokens in front of heads, are read at about the same time (128-byte rows of 8 heads: 5.3 TB/s when every head went its own way). The units
+// (request, its heads for this CTA, block of rows) lie end to end, each kSegmentTiles and its tiles long, and are cut into runs of equal length: a
 // run with many short segments gets fewer tiles. A run that ends among the first kSegmentTiles of a unit has none of its tiles.
 struct Run {
     int b, x;             // request, place among all of the request's units
@@ -126,11 +130,11 @@ __device__ __forceinline__ int run_begin(int total, int cta, int grid) {
     return static_cast<int>(each * cta + more * cta / n);
 }
 __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared, 16 words */) {
-    const int units = p.a.c.H_kv * p.row_blocks;
+    const int units = p.units, cta = blockIdx.x / p.heads, ctas = gridDim.x / p.heads;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_thr = blockDim.x, n_warps = n_thr >> 5;
     int sum = 0, mine = 0;
     for (int b = threadIdx.x; b < p.a.B; b += n_thr) {
-        const int n = length_of_unit(tiles_of(p.a, b)) * units;
+        const int n = length_of_unit(tiles_of(p, b)) * units;
         if (b < n_thr) mine = n;
         sum += n;
     }
@@ -139,13 +143,13 @@ __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared,
     __syncthreads();
     Run r{0, 0, 0, 0};
     for (int w = 0; w < n_warps; ++w) r.total += scratch[w];
-    const int first = run_begin(r.total, blockIdx.x, gridDim.x);
-    r.n = run_begin(r.total, blockIdx.x + 1, gridDim.x) - first;
+    const int first = run_begin(r.total, cta, ctas);
+    r.n = run_begin(r.total, cta + 1, ctas) - first;
     if (r.n > 0) {                               // (uniform over the CTA)
         int before_block = 0;
         for (int b0 = 0; b0 < p.a.B; b0 += n_thr) {
             const int b = b0 + threadIdx.x;
-            const int n = b0 == 0 ? mine : (b < p.a.B ? length_of_unit(tiles_of(p.a, b)) * units : 0);
+            const int n = b0 == 0 ? mine : (b < p.a.B ? length_of_unit(tiles_of(p, b)) * units : 0);
             int incl = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -174,24 +178,27 @@ __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared,
     return r;
 }
 struct Segment {
-    int b, unit;          // request; key head * row_blocks + block of rows
+    int b, head;          // request, key head
+    int rows;             // block of query rows
     int t0, n, nt;        // first tile, tiles here, tiles of the unit
 };
 struct Walk {
     const Params& p;
     int b, x, left, nt;
-    __device__ __forceinline__ Walk(const Params& q, const Run& r) : p(q), b(r.b), x(r.x), left(r.n), nt(r.n > 0 ? tiles_of(q.a, r.b) : 0) {}
+    __device__ __forceinline__ Walk(const Params& q, const Run& r) : p(q), b(r.b), x(r.x), left(r.n), nt(r.n > 0 ? tiles_of(q, r.b) : 0) {}
     __device__ __forceinline__ bool next(Segment& s) {
-        const int units = p.a.c.H_kv * p.row_blocks;
+        const int units = p.units;
         while (left > 0) {
             while (x == length_of_unit(nt) * units) {       // the request's end (or one without tiles); more follow
-                nt = tiles_of(p.a, ++b);
+                nt = tiles_of(p, ++b);
                 x = 0;
             }
             const int len = nt + kSegmentTiles;
             s.b = b;
-            s.unit = x / len;
-            const int from = x - s.unit * len, n = min(len - from, left);
+            const int unit = x / len, from = x - unit * len, n = min(len - from, left);
+            s.head = unit / p.row_blocks;
+            s.rows = unit - s.head * p.row_blocks;
+            s.head = s.head * p.heads + static_cast<int>(blockIdx.x) % p.heads;
             x += n;
             left -= n;
             s.t0 = max(from - kSegmentTiles, 0);
@@ -210,16 +217,19 @@ struct Walk {
 template <int D, bool FP8, int NR, int RG>
 struct Layout {
     static constexpr int kWarps = RG == 1 ? 4 : 8;                     // consumers
-    static constexpr bool kUneven = NR == 4;
+    static constexpr bool kUneven = NR * D == 512;
     static constexpr int kThreads = (kWarps + (kUneven ? 4 : 1)) * 32;
-    static constexpr int kCtas = RG > 1 ? 1 : (NR == 1 && (FP8 || D == 64) ? 3 : 2);      // of an SM
+    static constexpr int kCtas = RG > 1 ? 1 : (NR == 1 && FP8 ? 3 : 2);        // of an SM
     static constexpr int kConsumerRegs = RG == 1 ? 216 : 232;
     static_assert(128 * kProducerRegs + kWarps * 32 * kConsumerRegs <= (kWarps + 4) * 32 * (RG == 1 ? 128 : 168), "shares of the launch's registers");
+    // Keys of a tile: 18 to 36 KB, so that a tile's fixed costs (barriers, votes, the producer's turn) stay small beside its bytes, as far as a ring
+    // of three leaves room. (One request length of 32768 and 8 key heads, 8 rows: d = 64 in bf16 108 us with 64 keys and three CTAs, 91 with these.)
+    static constexpr int kTile = (D == 64 && (FP8 || NR < 4 || RG > 1)) || (FP8 && NR == 2) ? 128 : 64;
     static constexpr int kRows = 8 * NR * RG;                          // query rows of a CTA
     static constexpr int kParts = kWarps / RG;                         // warps that share a row; they share every tile
     static constexpr int kKeys = kTile / kParts;                       // keys of a tile that a warp takes
     static constexpr int kTileBytes = kTile * D * (FP8 ? 1 : 2);
-    static constexpr int kStageBytes = 2 * kTileBytes + (FP8 ? 1024 : 0);      // K, V, scales of K and of V (256 bytes each)
+    static constexpr int kStageBytes = 2 * kTileBytes + (FP8 ? 8 * kTile : 0);      // K, V, scales of K and of V
     static constexpr int kSlice = NR == 1 ? 64 : (NR == 2 ? 32 : 16);  // columns of the output that go through shared memory at a time
     static constexpr int kPitch = kSlice + 4;                          // floats between rows there: no bank conflicts
     static constexpr int kQBytes = kRows * D * 2;
@@ -234,13 +244,13 @@ struct Layout {
     static constexpr int kStages = kFit > 24 ? 24 : kFit;
     static constexpr int kBytes = kSmall + kStages * kStageBytes + kShared + kMlBytes;
     static_assert(kKeys % 16 == 0 && kStages >= 3, "whole steps of 16 keys, a ring of at least three tiles");
-    static_assert(kStages * (16 + 16) + kRows * 4 + 16 <= 1536, "small words");
+    static_assert(kStages * (16 + 32) + kRows * 4 + 16 <= 1536 && kTile <= 128, "small words");
 };
 
 // Byte offset of 16-byte chunk `c` of row `r` in a tile whose rows are at most 128 bytes (wider ones lie in blocks of 128).
-template <int ROW_BYTES>
+template <int ROW_BYTES, int TILE>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
-    if (ROW_BYTES >= 128) return (c >> 3) * (kTile * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+    if (ROW_BYTES >= 128) return (c >> 3) * (TILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
     return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
 }
 
@@ -257,8 +267,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const uint32_t red_s = q_s;
     const uint32_t ml_s = q_s + L::kShared;      // [parts][rows] (maximum, sum) of a warp, then (factor, -)
     const uint32_t bars = ml_s + L::kMlBytes;    // full[NS], empty[NS]
-    const uint32_t pos_s = bars + NS * 16;       // [NS][4] position of the first key of each piece, -1: none
-    const uint32_t row_s = pos_s + NS * 16;      // [rows] power of two taken out of a row of q; at the end what the row is multiplied by
+    const uint32_t pos_s = bars + NS * 16;       // [NS][8] position of the first key of each piece, -1: none
+    const uint32_t row_s = pos_s + NS * 32;      // [rows] power of two taken out of a row of q; at the end what the row is multiplied by
     const uint32_t flag_s = row_s + L::kRows * 4;
     __shared__ int scratch[16];
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(raw + (flag_s - base));
@@ -284,7 +294,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (L::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
         if (warp > W) return;
         // ------------------------------------------------------------ producer: pieces of pages into the ring
-        const int piece = 1 << p.piece_log2, per_tile_log2 = 6 - p.piece_log2, per_tile = 1 << per_tile_log2;
+        constexpr int kTileLog2 = L::kTile == 64 ? 6 : 7;
+        const int piece = 1 << p.piece_log2, per_tile_log2 = kTileLog2 - p.piece_log2, per_tile = 1 << per_tile_log2;
         const uint32_t piece_bytes = static_cast<uint32_t>(piece) * (2 * ROWB + (FP8 ? 8 : 0));
         const int P = a.c.page_size;
         int it = 0;
@@ -292,7 +303,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         Segment s;
         while (walk.next(s)) {
             const int len = length_of(a, s.b);
-            const int head = s.unit / p.row_blocks;
+            const int head = s.head;
             const int32_t* table = a.table + static_cast<int64_t>(s.b) * a.ld_table;
             const int32_t* sel = a.pages ? a.pages + (static_cast<int64_t>(s.b) * a.c.H_kv + head) * a.n_sel : nullptr;
             const int n_entries = (len + P - 1) / P;      // pages of the request; with a selection min(n_sel, that) entries are looked at
@@ -302,7 +313,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             auto locate = [&](int i) -> Where {           // piece i of the segment
                 Where w{0, 0, -1};
                 if (i < n_pieces) {
-                    const unsigned v = static_cast<unsigned>(s.t0) * kTile + (static_cast<unsigned>(i) << p.piece_log2);
+                    const unsigned v = static_cast<unsigned>(s.t0) * L::kTile + (static_cast<unsigned>(i) << p.piece_log2);
                     const unsigned e = v / static_cast<unsigned>(P);
                     w.off = static_cast<int>(v - e * P);
                     if (static_cast<int>(e) < most) {
@@ -333,7 +344,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     const bool mine = (lane >> per_tile_log2) == t;
                     const int in_tile = lane & (per_tile - 1);
                     const uint32_t who = __ballot_sync(0xFFFFFFFFu, mine && now.pos >= 0);
-                    if (mine) asm volatile("st.shared.b32 [%0], %1;" ::"r"(pos_s + st * 16 + in_tile * 4), "r"(now.pos) : "memory");
+                    if (mine) asm volatile("st.shared.b32 [%0], %1;" ::"r"(pos_s + st * 32 + in_tile * 4), "r"(now.pos) : "memory");
                     __syncwarp();
                     const uint32_t full = bars + 8 * st;
                     if (lane == 0) mbar_arrive_expect_tx(full, __popc(who) * piece_bytes);
@@ -344,14 +355,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         const uint32_t at = in_tile * piece * INNER;
 #pragma unroll
                         for (int h = 0; h < ROWB / INNER; ++h) {
-                            tma_load_4d(k_to + h * (kTile * INNER) + at, &k_map, full, h * 64, now.off, head, now.page);
-                            tma_load_4d(v_to + h * (kTile * INNER) + at, &v_map, full, h * 64, now.off, head, now.page);
+                            tma_load_4d(k_to + h * (L::kTile * INNER) + at, &k_map, full, h * 64, now.off, head, now.page);
+                            tma_load_4d(v_to + h * (L::kTile * INNER) + at, &v_map, full, h * 64, now.off, head, now.page);
                         }
                         if (FP8) {
                             const int64_t from = (static_cast<int64_t>(now.page) * a.c.H_kv + head) * P + now.off;
                             const uint32_t sc = v_to + L::kTileBytes + in_tile * piece * 4;
                             bulk_load_1d(sc, a.c.k_scale + from, piece * 4, full);
-                            bulk_load_1d(sc + 256, a.c.v_scale + from, piece * 4, full);
+                            bulk_load_1d(sc + 4 * L::kTile, a.c.v_scale + from, piece * 4, full);
                         }
                     }
                 }
@@ -376,12 +387,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const int warp_row = rg * NR * 8;            // first row of the CTA's that is this warp's
     const int rows_all = a.n_step * a.group;
     constexpr int NT = D / 16;                   // output fragments of 16 columns
-    constexpr bool kQRegs = NR < 4;              // q's fragments stay in registers, and the next segment's q is on its way early
+    constexpr int KB = NR <= 2 && L::kKeys >= 32 ? 2 : 1;      // blocks of 16 keys in a step
+    constexpr int CH = NR * KB == 1 ? 2 : 1;     // sums that a block's scores are formed in
+    constexpr bool kQRegs = NR * D <= 128;              // q's fragments stay in registers, and the next segment's q is on its way early
     constexpr int QV = L::kRows * (D / 8) / (W * 32) > 0 ? L::kRows * (D / 8) / (W * 32) : 1;      // vectors of q a thread brings
     constexpr int Q_THREADS = L::kRows * (D / 8) < W * 32 ? L::kRows * (D / 8) : W * 32;
 
     auto load_q = [&](const Segment& s, uint4(&q)[QV]) {              // zeros behind the last row
-        const int head = s.unit / p.row_blocks, row0 = (s.unit - head * p.row_blocks) * L::kRows;
+        const int head = s.head, row0 = s.rows * L::kRows;
 #pragma unroll
         for (int u = 0; u < QV; ++u) {
             const int i = threadIdx.x + u * W * 32, r = i / (D / 8), c = i - r * (D / 8);
@@ -405,7 +418,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         s = after;
         if (!kQRegs) load_q(s, q_next);
         const int len = length_of(a, s.b);
-        const int head = s.unit / p.row_blocks, row0 = (s.unit - head * p.row_blocks) * L::kRows;
+        const int head = s.head, row0 = s.rows * L::kRows;
         const int n_rows = min(rows_all - row0, L::kRows);
         const bool whole = s.t0 == 0 && s.n == s.nt;
         if (threadIdx.x < Q_THREADS) {
@@ -489,90 +502,105 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             if (!ok) break;
             const uint32_t k_at = stages + st * L::kStageBytes, v_at = k_at + L::kTileBytes, sc_at = v_at + L::kTileBytes;
 #pragma unroll
-            for (int step = 0; step < L::kKeys / 16; ++step) {
-                const int key0 = (part * (L::kKeys / 16) + step) * 16;
-                const int pc = key0 >> p.piece_log2;
-                int at = static_cast<int>(ld_shared_u32(pos_s + st * 16 + pc * 4));      // position of the first of the 16 keys
-                at = at < 0 ? INT32_MAX / 2 : at + (key0 - (pc << p.piece_log2));
-                const bool clean = at + 16 <= sees_least;
+            for (int step = 0; step < L::kKeys / (16 * KB); ++step) {
+                int key0[KB], at[KB];                      // first key of each 16, and its position
+                int first = INT32_MAX, last = 0;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    key0[kb] = part * L::kKeys + (step * KB + kb) * 16;
+                    const int pc = key0[kb] >> p.piece_log2;
+                    at[kb] = static_cast<int>(ld_shared_u32(pos_s + st * 32 + pc * 4));
+                    at[kb] = at[kb] < 0 ? INT32_MAX / 2 : at[kb] + (key0[kb] - (pc << p.piece_log2));
+                    first = min(first, at[kb]);
+                    last = max(last, at[kb] + 16);
+                }
+                if (L::kTile > 64 && first >= len) continue;           // none of them is there
+                const bool clean = last <= sees_least;
                 if (!clean) {
                     // Rows of V that no token sees meet probability 0 and may hold anything: they are cleared. (Warps that share keys clear them alike.)
-                    const int r = key0 + (lane & 15);
-                    if (at + (lane & 15) >= len) {
 #pragma unroll
-                        for (int c = 0; c < ROWB / 16; c += 2) st_shared_v4(v_at + chunk_at<ROWB>(r, c + (lane >> 4)), make_uint4(0u, 0u, 0u, 0u));
-                        if (FP8) st_shared_f32(sc_at + 256 + r * 4, 1.f);
-                        fence_proxy_async_smem();          // (the next copy into these rows comes from the asynchronous proxy)
-                    }
+                    for (int kb = 0; kb < KB; ++kb)
+                        if (at[kb] + (lane & 15) >= len) {
+                            const int r = key0[kb] + (lane & 15);
+#pragma unroll
+                            for (int c = 0; c < ROWB / 16; c += 2) st_shared_v4(v_at + chunk_at<ROWB, L::kTile>(r, c + (lane >> 4)), make_uint4(0u, 0u, 0u, 0u));
+                            if (FP8) st_shared_f32(sc_at + 4 * L::kTile + r * 4, 1.f);
+                            fence_proxy_async_smem();      // (the next copy into these rows comes from the asynchronous proxy)
+                        }
                     __syncwarp();
                 }
-                // scores of 16 keys: A fragments straight from K's rows, (keys 0-7, 8-15) x two 16-byte chunks an ldmatrix; two sums a block
-                // halve the chain of dependent instructions
-                float x[NR][2][4];
+                // scores: A fragments straight from K's rows, (keys 0-7, 8-15) x two 16-byte chunks an ldmatrix; with few independent sums each is
+                // formed in two, which halves the chain of dependent instructions
+                float x[KB][NR][CH][4];
 #pragma unroll
-                for (int nr = 0; nr < NR; ++nr)
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[nr][e >> 2][e & 3] = 0.f;
+                    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-                for (int c4 = 0; c4 < D / 32; ++c4) {                  // 32 columns: two steps of 16
-                    uint32_t ka[2][4];
-                    if (!FP8) {
+                        for (int e = 0; e < 4 * CH; ++e) x[kb][nr][e >> 2][e & 3] = 0.f;
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            ldmatrix_x4(k_at + chunk_at<ROWB>(key0 + (lane & 15), c4 * 4 + 2 * u + (lane >> 4)), ka[u]);
-                    } else {
-                        uint32_t kb[4];
-                        ldmatrix_x4(k_at + chunk_at<ROWB>(key0 + (lane & 15), c4 * 2 + (lane >> 4)), kb);
+                for (int c4 = 0; c4 < D / 32; ++c4)                    // 32 columns: two steps of 16
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)
+                    for (int kb = 0; kb < KB; ++kb) {
+                        uint32_t ka[2][4];
+                        if (!FP8) {
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {              // keys g and g + 8: four codes each
-                                ka[u][h] = e4m3x2_to_f16x2(kb[2 * u + h] & 0xFFFFu);
-                                ka[u][2 + h] = e4m3x2_to_f16x2(kb[2 * u + h] >> 16);
-                            }
-                    }
-#pragma unroll
-                    for (int nr = 0; nr < NR; ++nr) {
-                        uint32_t qb[4];
-                        if (kQRegs) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) qb[e] = qf[kQRegs ? nr : 0][kQRegs ? c4 : 0][e];
+                            for (int u = 0; u < 2; ++u)
+                                ldmatrix_x4(k_at + chunk_at<ROWB, L::kTile>(key0[kb] + (lane & 15), c4 * 4 + 2 * u + (lane >> 4)), ka[u]);
                         } else {
-                            q_frag(nr, c4, qb);
+                            uint32_t raw4[4];
+                            ldmatrix_x4(k_at + chunk_at<ROWB, L::kTile>(key0[kb] + (lane & 15), c4 * 2 + (lane >> 4)), raw4);
+#pragma unroll
+                            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {          // keys g and g + 8: four codes each
+                                    ka[u][h] = e4m3x2_to_f16x2(raw4[2 * u + h] & 0xFFFFu);
+                                    ka[u][2 + h] = e4m3x2_to_f16x2(raw4[2 * u + h] >> 16);
+                                }
                         }
-                        mma_16816<FP8>(x[nr][0], ka[0], qb[0], qb[1]);
-                        mma_16816<FP8>(x[nr][1], ka[1], qb[2], qb[3]);
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr) {
+                            uint32_t qb[4];
+                            if (kQRegs) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) qb[e] = qf[kQRegs ? nr : 0][kQRegs ? c4 : 0][e];
+                            } else {
+                                q_frag(nr, c4, qb);
+                            }
+                            mma_16816<FP8>(x[kb][nr][0], ka[0], qb[0], qb[1]);
+                            mma_16816<FP8>(x[kb][nr][CH - 1], ka[1], qb[2], qb[3]);
+                        }
                     }
-                }
                 // softmax: element 2 h + e is key g + 8 h, row 2 j + e
-                float k_sc[2] = {1.f, 1.f}, v_sc[2] = {1.f, 1.f}, above[2] = {0.f, 0.f};
-                if (FP8) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        k_sc[h] = ld_shared_f32(sc_at + (key0 + g + 8 * h) * 4);
-                        v_sc[h] = ld_shared_f32(sc_at + 256 + (key0 + g + 8 * h) * 4);
-                        above[h] = log2_above(v_sc[h]);
-                        v_sc[h] *= kF16Head;
-                    }
-                }
-                uint32_t pb[NR][2];
+                float v_sc[KB][2], y[KB][NR][4], top[NR][2];
                 bool moved = false;
-                float top[NR][2], y[NR][4];
 #pragma unroll
-                for (int nr = 0; nr < NR; ++nr) {
+                for (int nr = 0; nr < NR; ++nr) top[nr][0] = top[nr][1] = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v = (x[nr][0][e] + x[nr][1][e]) * row_scale[nr][e & 1];
-                        if (FP8) v *= k_sc[e >> 1];
-                        if (!clean && at + g + 8 * (e >> 1) >= sees[nr][e & 1]) v = -INFINITY;
-                        y[nr][e] = v;
+                for (int kb = 0; kb < KB; ++kb) {
+                    float k_sc[2] = {1.f, 1.f}, above[2] = {0.f, 0.f};
+                    if (FP8) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            k_sc[h] = ld_shared_f32(sc_at + (key0[kb] + g + 8 * h) * 4);
+                            v_sc[kb][h] = ld_shared_f32(sc_at + 4 * L::kTile + (key0[kb] + g + 8 * h) * 4);
+                            above[h] = log2_above(v_sc[kb][h]);
+                            v_sc[kb][h] *= kF16Head;
+                        }
                     }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        top[nr][e] = FP8 ? fmaxf(y[nr][e] + above[0], y[nr][2 + e] + above[1]) : fmaxf(y[nr][e], y[nr][2 + e]);
-                        moved |= !(top[nr][e] <= m[nr][e] + kSlack);   // (no number: as one that moves)
-                    }
+                    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float v = (CH == 2 ? x[kb][nr][0][e] + x[kb][nr][CH - 1][e] : x[kb][nr][0][e]) * row_scale[nr][e & 1];
+                            if (FP8) v *= k_sc[e >> 1];
+                            if (!clean && at[kb] + g + 8 * (e >> 1) >= sees[nr][e & 1]) v = -INFINITY;
+                            y[kb][nr][e] = v;
+                            top[nr][e & 1] = fmaxf(top[nr][e & 1], FP8 ? v + above[e >> 1] : v);
+                        }
                 }
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) moved |= !(top[nr][0] <= m[nr][0] + kSlack) | !(top[nr][1] <= m[nr][1] + kSlack);
                 if (__any_sync(0xFFFFFFFFu, moved)) {      // (rare behind a segment's first keys)
 #pragma unroll
                     for (int nr = 0; nr < NR; ++nr)
@@ -591,44 +619,51 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                             }
                         }
                 }
+                uint32_t pb[KB][NR][2];
 #pragma unroll
                 for (int nr = 0; nr < NR; ++nr) {
                     const float use[2] = {m[nr][0] == -INFINITY ? 0.f : m[nr][0], m[nr][1] == -INFINITY ? 0.f : m[nr][1]};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[nr][e] = exp2_fast(y[nr][e] - use[e & 1]);
-                        l[nr][e & 1] += y[nr][e];
-                        if (FP8) y[nr][e] *= v_sc[e >> 1];
+                    for (int kb = 0; kb < KB; ++kb) {
+                        float* v = y[kb][nr];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            v[e] = exp2_fast(v[e] - use[e & 1]);
+                            l[nr][e & 1] += v[e];
+                            if (FP8) v[e] *= v_sc[kb][e >> 1];
+                        }
+                        pb[kb][nr][0] = transpose_8x8(FP8 ? pack_f16(v[0], v[1]) : pack_bf16(v[0], v[1]));
+                        pb[kb][nr][1] = transpose_8x8(FP8 ? pack_f16(v[2], v[3]) : pack_bf16(v[2], v[3]));
                     }
-                    pb[nr][0] = transpose_8x8(FP8 ? pack_f16(y[nr][0], y[nr][1]) : pack_bf16(y[nr][0], y[nr][1]));
-                    pb[nr][1] = transpose_8x8(FP8 ? pack_f16(y[nr][2], y[nr][3]) : pack_bf16(y[nr][2], y[nr][3]));
                 }
                 // output: A fragments are V's rows transposed
 #pragma unroll
-                for (int c2 = 0; c2 < ROWB / 32; ++c2) {
-                    uint32_t va[4];
-                    if (!FP8) {
-                        // (keys 0-7; columns 0-7, 8-15), then keys 8-15
-                        ldmatrix_x4_trans(v_at + chunk_at<ROWB>(key0 + (lane & 7) + (lane >> 4) * 8, 2 * c2 + (lane >> 3 & 1)), va);
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                        for (int nr = 0; nr < NR; ++nr) mma_16816<false>(o[nr][c2 % NT], va, pb[nr][0], pb[nr][1]);
-                    } else {
-                        uint32_t vb[4];                    // (keys 0-7, 8-15) of a 16-byte chunk, then of the next
-                        ldmatrix_x4_trans(v_at + chunk_at<ROWB>(key0 + (lane & 15), 2 * c2 + (lane >> 4)), vb);
+                    for (int c2 = 0; c2 < ROWB / 32; ++c2) {
+                        uint32_t va[4];
+                        if (!FP8) {
+                            // (keys 0-7; columns 0-7, 8-15), then keys 8-15
+                            ldmatrix_x4_trans(v_at + chunk_at<ROWB, L::kTile>(key0[kb] + (lane & 7) + (lane >> 4) * 8, 2 * c2 + (lane >> 3 & 1)), va);
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            // A register holds columns 2 g, 2 g + 1 of keys 2 j, 2 j + 1: the even column's two keys become row g of the fragment, the
-                            // odd one's row g + 8.
-                            const uint32_t w0 = __byte_perm(vb[2 * u], 0, 0x3120), w1 = __byte_perm(vb[2 * u + 1], 0, 0x3120);
-                            va[0] = e4m3x2_to_f16x2(w0 & 0xFFFFu);
-                            va[1] = e4m3x2_to_f16x2(w0 >> 16);
-                            va[2] = e4m3x2_to_f16x2(w1 & 0xFFFFu);
-                            va[3] = e4m3x2_to_f16x2(w1 >> 16);
+                            for (int nr = 0; nr < NR; ++nr) mma_16816<false>(o[nr][c2 % NT], va, pb[kb][nr][0], pb[kb][nr][1]);
+                        } else {
+                            uint32_t vb[4];                // (keys 0-7, 8-15) of a 16-byte chunk, then of the next
+                            ldmatrix_x4_trans(v_at + chunk_at<ROWB, L::kTile>(key0[kb] + (lane & 15), 2 * c2 + (lane >> 4)), vb);
 #pragma unroll
-                            for (int nr = 0; nr < NR; ++nr) mma_16816<true>(o[nr][(2 * c2 + u) % NT], va, pb[nr][0], pb[nr][1]);
+                            for (int u = 0; u < 2; ++u) {
+                                // A register holds columns 2 g, 2 g + 1 of keys 2 j, 2 j + 1: the even column's two keys become row g of the fragment,
+                                // the odd one's row g + 8.
+                                const uint32_t w0 = __byte_perm(vb[2 * u], 0, 0x3120), w1 = __byte_perm(vb[2 * u + 1], 0, 0x3120);
+                                va[0] = e4m3x2_to_f16x2(w0 & 0xFFFFu);
+                                va[1] = e4m3x2_to_f16x2(w0 >> 16);
+                                va[2] = e4m3x2_to_f16x2(w1 & 0xFFFFu);
+                                va[3] = e4m3x2_to_f16x2(w1 >> 16);
+#pragma unroll
+                                for (int nr = 0; nr < NR; ++nr) mma_16816<true>(o[nr][(2 * c2 + u) % NT], va, pb[kb][nr][0], pb[kb][nr][1]);
+                            }
                         }
                     }
-                }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (NS + st));
@@ -719,13 +754,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
             consumers_sync<W>();
         }
-        if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.unit, s.n, s.nt);
+        if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.head * p.row_blocks + s.rows, s.n, s.nt);
     }
     if (threadIdx.x == 0) p.owners[blockIdx.x] = owner;
 
     // Requests without keys: zeros and -inf.
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        if (tiles_of(a, b) != 0) continue;
+        if (tiles_of(p, b) != 0) continue;
         const int64_t n_vec = static_cast<int64_t>(a.n_step) * a.H * (D / 8);
         uint4* to = reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(b) * a.n_step * a.H * D);
         for (int64_t i = threadIdx.x; i < n_vec; i += W * 32) to[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -740,8 +775,8 @@ __global__ void __launch_bounds__(128)
 paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) {
     let_next_start();
     wait_for_previous();
-    const int cta = blockIdx.x;
-    const int4 own = p.owners[cta];
+    const int cta = blockIdx.x / p.heads, ctas = grid / p.heads;
+    const int4 own = p.owners[blockIdx.x];
     if (own.x < 0) return;
     const int lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5);
     const int head = own.y / p.row_blocks, row0 = (own.y - head * p.row_blocks) * ROWS;
@@ -750,12 +785,12 @@ paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) 
     const int total = *p.total;
     int pieces;                                  // the segment's tiles after this run fill the runs that follow
     {
-        const int n = min(grid, total);
-        const int last_tile = run_begin(total, cta + 1, grid) + (own.w - own.z) - 1;                    // its place; it is in the run of
+        const int n = min(ctas, total);
+        const int last_tile = run_begin(total, cta + 1, ctas) + (own.w - own.z) - 1;                    // its place; it is in the run of
         const int last = static_cast<int>(((static_cast<int64_t>(last_tile) + 1) * n + total - 1) / total) - 1;      // the last c with total * c / n <= last_tile
         pieces = last - cta + 1;
     }
-    auto row_of = [&](int i) -> int64_t { return (static_cast<int64_t>(cta + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r; };
+    auto row_of = [&](int i) -> int64_t { return (static_cast<int64_t>(blockIdx.x + i * p.heads) * 2 + (i == 0 ? 1 : 0)) * ROWS + r; };
     float top = -INFINITY;
     for (int i = lane; i < pieces; i += 32) top = fmaxf(top, p.part_ml[row_of(i)].x);
 #pragma unroll
@@ -806,7 +841,13 @@ int rows_of_cta(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 3
 template <int D, bool FP8, int NR, int RG>
 cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, int sm_count, cudaStream_t stream, int* launches) {
     using L = Layout<D, FP8, NR, RG>;
-    const int grid = sm_count * L::kCtas < max_grid(L::kRows) ? sm_count * L::kCtas : max_grid(L::kRows);
+    // Heads in step: all of up to 8, else the largest divisor of their number up to 8.
+    p.heads = p.a.c.H_kv < 8 ? p.a.c.H_kv : 8;
+    while (p.a.c.H_kv % p.heads) --p.heads;
+    p.units = p.a.c.H_kv / p.heads * p.row_blocks;
+    p.tile_log2 = L::kTile == 64 ? 6 : 7;
+    const int most = sm_count * L::kCtas < max_grid(L::kRows) ? sm_count * L::kCtas : max_grid(L::kRows);
+    const int grid = most / p.heads * p.heads;
     auto kernel = paged_attn_kernel<D, FP8, NR, RG>;
     cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes);
     if (e != cudaSuccess) return e;
@@ -827,7 +868,8 @@ size_t paged_attn_workspace_bytes(int n_step, int group, int d) {
 }
 bool paged_attn_fits(const PagedAttnArgs& a) {
     const int64_t rows = static_cast<int64_t>(a.n_step) * a.group, cta = rows_of_cta(a.n_step * a.group);
-    int64_t keys = a.max_len + kTile;            // (a tile more than there are)
+    constexpr int kTile = 64;                    // (of the smallest tiles)
+    int64_t keys = a.max_len + kTile;
     if (a.pages) {
         const int64_t pages = (a.max_len + a.c.page_size - 1) / a.c.page_size;
         keys = (pages < a.n_sel ? pages : a.n_sel) * a.c.page_size + kTile;
