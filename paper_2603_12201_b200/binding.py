@@ -675,7 +675,8 @@ class PagedCache:
                 raise ValueError(f"{name} must be contiguous")
         self.k, self.v, self.k_scale, self.v_scale, self.bounds = k, v, k_scale, v_scale, bounds
         self.n_pages, self.page_size, self.H_kv, self.d = n_pages, page_size, H_kv, d
-        self.device_index = k.get_device()
+        self.device, self.device_index = k.device, k.get_device()
+        self._workspace_bytes = {}               # by (n_step, H)
         self._c = _PagedCacheStruct(_at(k), _at(v), _at(k_scale), _at(v_scale), _at(bounds), n_pages, *strides[0][:3], page_size, H_kv, d, dt)
         self._p = ctypes.addressof(self._c)
 
@@ -762,12 +763,17 @@ def paged_attention(cache, q, table, lens, max_len, scale, pages=None, want_lse=
         _typed(pages, "pages", torch.int32, (B, cache.H_kv, n_sel) if pages.dim() == 3 else (B * cache.H_kv, n_sel))
     with guard:
         if out is None:
-            out = torch.empty_strided((B, n_step, H, d), (n_step * H * d, H * d, d, 1), dtype=torch.bfloat16, device=q.device)
-        lse = _new3(B, n_step, H, torch.float32, q.device) if want_lse else None
+            out = torch.empty_strided((B, n_step, H, d), (n_step * H * d, H * d, d, 1), dtype=torch.bfloat16, device=cache.device)
+        lse = _new3(B, n_step, H, torch.float32, cache.device) if want_lse else None
         if workspace is None:
-            workspace = torch.empty_strided((max(paged_attention_workspace_bytes(n_step, H, cache.H_kv, d), 256),), (1,), dtype=torch.uint8, device=q.device)
+            need = cache._workspace_bytes.get((n_step, H))
+            if need is None:
+                need = cache._workspace_bytes[n_step, H] = max(paged_attention_workspace_bytes(n_step, H, cache.H_kv, d), 256)
+            workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=cache.device)
+        else:
+            need = workspace.nbytes
         _check(lib().idxc_paged_attention(cache._p, _at(q), q_stride, _at(table), ld, _at(lens), B, n_step, int(max_len), H, _at(pages), n_sel, float(scale),
-                                          _at(out), _at(lse), _at(workspace), workspace.nbytes, stream), "idxc_paged_attention")
+                                          _at(out), _at(lse), _at(workspace), need, stream), "idxc_paged_attention")
     return out, lse
 
 

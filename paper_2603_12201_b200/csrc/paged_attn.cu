@@ -44,8 +44,7 @@ struct Params {
     float scale_log2;            // scale * log2(e)
     float* part_o;               // [grid][2][MAXR][D]
     float2* part_ml;             // [grid][2][MAXR] (maximum in log2 units, sum)
-    int4* owners;                // [grid] the segment that begins in a CTA's run and does not end in it: (request, unit, its tiles in the run, all), request -1: none
-    int* total;                  // tiles of the call
+    int4* owners;                // [grid] the segment that begins in a CTA's run and does not end in it: (request, key head * row_blocks + block of rows, pieces); -1: none
     unsigned int* status;
 };
 
@@ -182,6 +181,13 @@ struct Segment {
     int rows;             // block of query rows
     int t0, n, nt;        // first tile, tiles here, tiles of the unit
 };
+// Runs over which a segment goes that begins in this CTA's and does not end in it: the tiles that are left lie in the runs that follow.
+__device__ __forceinline__ int pieces_of(const Run& run, const Segment& s, int heads) {
+    const int cta = blockIdx.x / heads, ctas = min(static_cast<int>(gridDim.x) / heads, run.total);
+    const int last_tile = run_begin(run.total, cta + 1, ctas) + (s.nt - s.n) - 1;                              // its place; it is in the run of the
+    const int last = static_cast<int>(((static_cast<int64_t>(last_tile) + 1) * ctas + run.total - 1) / run.total) - 1;      // last c with total * c / ctas <= last_tile
+    return last - cta + 1;
+}
 struct Walk {
     const Params& p;
     int b, x, left, nt;
@@ -288,7 +294,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     wait_for_previous();
     const Run run = find_run(p, scratch);        // (its barriers publish the mbarriers too)
     const PagedAttnArgs& a = p.a;
-    if (threadIdx.x == 0 && blockIdx.x == 0) *p.total = run.total;
 
     if (warp >= W) {
         if (L::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
@@ -754,7 +759,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
             consumers_sync<W>();
         }
-        if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.head * p.row_blocks + s.rows, s.n, s.nt);
+        if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.head * p.row_blocks + s.rows, pieces_of(run, s, p.heads), 0);
     }
     if (threadIdx.x == 0) p.owners[blockIdx.x] = owner;
 
@@ -769,39 +774,50 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 }
 
-// Joins the pieces of a segment that runs cut. blockIdx.x: the CTA in whose run the segment begins; a warp a row.
+// Joins the pieces of a segment that runs cut. blockIdx.x: the CTA in whose run the segment begins; a warp a row. Two round trips to memory: the
+// owner's word, then maxima, sums and the first pieces together.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(128)
-paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) {
+paged_merge_kernel(const __grid_constant__ Params p, float out_scale) {
     let_next_start();
     wait_for_previous();
-    const int cta = blockIdx.x / p.heads, ctas = grid / p.heads;
     const int4 own = p.owners[blockIdx.x];
     if (own.x < 0) return;
     const int lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5);
-    const int head = own.y / p.row_blocks, row0 = (own.y - head * p.row_blocks) * ROWS;
+    const int head = own.y / p.row_blocks, row0 = (own.y - head * p.row_blocks) * ROWS, pieces = own.z;
     const int n_rows = min(p.a.n_step * p.a.group - row0, ROWS);
     if (r >= n_rows) return;
-    const int total = *p.total;
-    int pieces;                                  // the segment's tiles after this run fill the runs that follow
-    {
-        const int n = min(ctas, total);
-        const int last_tile = run_begin(total, cta + 1, ctas) + (own.w - own.z) - 1;                    // its place; it is in the run of
-        const int last = static_cast<int>(((static_cast<int64_t>(last_tile) + 1) * n + total - 1) / total) - 1;      // the last c with total * c / n <= last_tile
-        pieces = last - cta + 1;
-    }
+    constexpr int V = D / 32, AHEAD = 4;         // columns of a lane; pieces on their way at a time
     auto row_of = [&](int i) -> int64_t { return (static_cast<int64_t>(blockIdx.x + i * p.heads) * 2 + (i == 0 ? 1 : 0)) * ROWS + r; };
-    float top = -INFINITY;
-    for (int i = lane; i < pieces; i += 32) top = fmaxf(top, p.part_ml[row_of(i)].x);
+    auto load = [&](int i, float(&y)[V]) {
+        const float* from = p.part_o + row_of(i) * D + lane * V;
+        if (V == 4) {
+            const float4 z = *reinterpret_cast<const float4*>(from);
+            y[0] = z.x;
+            y[1] = z.y;
+            y[2 % V] = z.z;
+            y[3 % V] = z.w;
+        } else {
+            const float2 z = *reinterpret_cast<const float2*>(from);
+            y[0] = z.x;
+            y[1] = z.y;
+        }
+    };
+    float y[AHEAD][V];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (u < pieces) load(u, y[u]);
+    const float2 first = lane < pieces ? p.part_ml[row_of(lane)] : make_float2(-INFINITY, 0.f);
+    float top = first.x;
+    for (int i = 32 + lane; i < pieces; i += 32) top = fmaxf(top, p.part_ml[row_of(i)].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const float use = top == -INFINITY ? 0.f : top;
-    constexpr int V = D / 32;                    // columns of a lane
     float acc[V] = {}, sum = 0.f;
     for (int i0 = 0; i0 < pieces; i0 += 32) {
         float w = 0.f, lw = 0.f;
         if (i0 + lane < pieces) {
-            const float2 ml = p.part_ml[row_of(i0 + lane)];
+            const float2 ml = i0 == 0 ? first : p.part_ml[row_of(i0 + lane)];
             w = exp2_fast(ml.x - use);
             lw = w * ml.y;
         }
@@ -809,20 +825,21 @@ paged_merge_kernel(const __grid_constant__ Params p, int grid, float out_scale) 
         for (int o = 16; o > 0; o >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, o);
         sum += lw;
         const int n = min(32, pieces - i0);
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float wi = __shfl_sync(0xFFFFFFFFu, w, i);
-            const float* from = p.part_o + row_of(i0 + i) * D + lane * V;
-            if (V == 4) {
-                const float4 y = *reinterpret_cast<const float4*>(from);
-                acc[0] += wi * y.x;
-                acc[1] += wi * y.y;
-                acc[2 % V] += wi * y.z;
-                acc[3 % V] += wi * y.w;
-            } else {
-                const float2 y = *reinterpret_cast<const float2*>(from);
-                acc[0] += wi * y.x;
-                acc[1] += wi * y.y;
+        for (int i = 0; i < n; i += AHEAD) {
+            float z[AHEAD][V];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) z[u][v] = y[u][v];
+                if (i0 + i + AHEAD + u < pieces) load(i0 + i + AHEAD + u, y[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const float wi = __shfl_sync(0xFFFFFFFFu, w, i + u);
+                if (i + u < n) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[v] += wi * z[u][v];
+                }
             }
         }
     }
@@ -856,15 +873,15 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
     if (e != cudaSuccess) return e;
     const int rows = p.a.n_step * p.a.group < L::kRows ? p.a.n_step * p.a.group : L::kRows;
     *launches += 1;
-    return launch_behind(paged_merge_kernel<D, L::kRows>, dim3(grid, (rows + 3) / 4), 128, 0, stream, p, grid, FP8 ? 1.f / kF16Head : 1.f);
+    return launch_behind(paged_merge_kernel<D, L::kRows>, dim3(grid, (rows + 3) / 4), 128, 0, stream, p, FP8 ? 1.f / kF16Head : 1.f);
 }
 
 }  // namespace
 
-// owners and total, the pieces' maxima and sums, the pieces
+// owners, the pieces' maxima and sums, the pieces
 size_t paged_attn_workspace_bytes(int n_step, int group, int d) {
     const size_t rows = static_cast<size_t>(rows_of_cta(n_step * group)), grid = static_cast<size_t>(max_grid(static_cast<int>(rows)));
-    return grid * 16 + 256 + grid * 2 * rows * (8 + static_cast<size_t>(d) * 4);
+    return grid * 16 + grid * 2 * rows * (8 + static_cast<size_t>(d) * 4);
 }
 bool paged_attn_fits(const PagedAttnArgs& a) {
     const int64_t rows = static_cast<int64_t>(a.n_step) * a.group, cta = rows_of_cta(a.n_step * a.group);
@@ -888,9 +905,8 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUt
     uint8_t* w = static_cast<uint8_t*>(workspace);
     p.owners = reinterpret_cast<int4*>(w);
     const size_t grid = static_cast<size_t>(max_grid(cta_rows));
-    p.total = reinterpret_cast<int*>(w + grid * 16);
-    p.part_ml = reinterpret_cast<float2*>(w + grid * 16 + 256);
-    p.part_o = reinterpret_cast<float*>(w + grid * 16 + 256 + grid * 2 * cta_rows * 8);
+    p.part_ml = reinterpret_cast<float2*>(w + grid * 16);
+    p.part_o = reinterpret_cast<float*>(w + grid * 16 + grid * 2 * cta_rows * 8);
     p.status = status;
 #define IDXC_RUN(D_, F_)                                                                                   \
     (cta_rows == 8    ? run<D_, F_, 1, 1>(k_map, v_map, p, sm_count, stream, launches)                      \

@@ -52,6 +52,8 @@ struct AppendArgs {
     int chunk;                   // tokens a CTA looks at for the beginnings of runs: at most 32
 };
 
+// x / 448, correctly rounded (as div_by_scale; x normal and, but for an infinite one, below 2^128).
+__device__ __forceinline__ float over_448(float x) { return x <= 3.4e38f ? div_by_scale(x, kE4m3Max, 1.f / kE4m3Max) : x; }
 // Largest magnitudes of a key's and of a value's 8 elements, as two bf16 (a number that is none counts as 0).
 __device__ __forceinline__ uint32_t two_maxima(uint4 k, uint4 v) {
     auto one = [](uint4 x) -> __nv_bfloat162 {
@@ -155,7 +157,7 @@ paged_append_kernel(const AppendArgs a) {
                 }
                 const float k_max = __uint_as_float(m << 16), v_max = __uint_as_float(m & 0xFFFF0000u);
                 if (in) {
-                    const float ks = __fdiv_rn(fmaxf(k_max, 1e-12f), kE4m3Max), vs = __fdiv_rn(fmaxf(v_max, 1e-12f), kE4m3Max);
+                    const float ks = over_448(fmaxf(k_max, 1e-12f)), vs = over_448(fmaxf(v_max, 1e-12f));
                     const uint2 kc = quantize8(k[u], ks);
                     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.k) + at) = kc;
                     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.v) + at) = quantize8(v[u], vs);
