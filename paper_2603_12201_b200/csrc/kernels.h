@@ -13,6 +13,8 @@ namespace idxc {
 cudaError_t ensure_max_dynamic_smem(const void* kernel, int bytes);
 
 // Launches a kernel that may start while the kernel before it in the stream still runs, and waits for it itself (wait_for_previous).
+// What earlier kernels may have written is then read with plain loads: a read-only load (__ldg) may find a line that an even earlier kernel left in this
+// SM's L1 after this one had started.
 template <typename... Params, typename... Args>
 cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const Args&... args) {
     cudaLaunchAttribute attr{};

@@ -103,7 +103,7 @@ __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;
 
 // ---------------------------------------------------------------- work
 // Keys of request b that the call knows of.
-__device__ __forceinline__ int length_of(const PagedAttnArgs& a, int b) { return min(max(__ldg(a.lens + b), 0), static_cast<int>(a.max_len)); }
+__device__ __forceinline__ int length_of(const PagedAttnArgs& a, int b) { return min(max(a.lens[b], 0), static_cast<int>(a.max_len)); }
 // Tiles of one (key head, block of rows) of request b: of its keys, or of the first min(n_sel, pages of the request) entries of its selection.
 __device__ __forceinline__ int tiles_of(const Params& p, int b) {
     const int len = length_of(p.a, b), up = (1 << p.tile_log2) - 1;
@@ -322,10 +322,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     const unsigned e = v / static_cast<unsigned>(P);
                     w.off = static_cast<int>(v - e * P);
                     if (static_cast<int>(e) < most) {
-                        const int logical = sel ? __ldg(sel + e) : static_cast<int>(e);
+                        const int logical = sel ? sel[e] : static_cast<int>(e);
                         if (logical >= 0 && logical < n_entries) {
                             const int pos = logical * P + w.off;
-                            w.page = __ldg(table + logical);
+                            w.page = table[logical];
                             if (pos < len && w.page >= 0 && w.page < a.c.n_pages) w.pos = pos;
                         }
                     }
@@ -406,8 +406,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             q[u] = make_uint4(0u, 0u, 0u, 0u);
             if (threadIdx.x < Q_THREADS && row0 + r < rows_all) {
                 const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
-                q[u] = __ldg(reinterpret_cast<const uint4*>(a.q + (static_cast<int64_t>(s.b) * a.n_step + step) * a.q_stride +
-                                                            static_cast<int64_t>(head * a.group + h) * D) + c);
+                q[u] = reinterpret_cast<const uint4*>(a.q + (static_cast<int64_t>(s.b) * a.n_step + step) * a.q_stride +
+                                                      static_cast<int64_t>(head * a.group + h) * D)[c];
             }
         }
     };

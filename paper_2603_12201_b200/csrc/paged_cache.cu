@@ -133,8 +133,8 @@ paged_append_kernel(const AppendArgs a) {
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * lanes + lane;
                 const bool in = works && i < n_new;
-                k[u].raw = in ? __ldg(a.k + (t0 + i) * a.k_stride + col) : make_uint4(0u, 0u, 0u, 0u);
-                v[u].raw = in ? __ldg(a.v + (t0 + i) * a.v_stride + col) : make_uint4(0u, 0u, 0u, 0u);
+                k[u].raw = in ? a.k[(t0 + i) * a.k_stride + col] : make_uint4(0u, 0u, 0u, 0u);
+                v[u].raw = in ? a.v[(t0 + i) * a.v_stride + col] : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
