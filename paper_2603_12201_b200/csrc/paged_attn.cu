@@ -235,7 +235,8 @@ struct Layout {
     static constexpr int kParts = kWarps / RG;                         // warps that share a row; they share every tile
     static constexpr int kKeys = kTile / kParts;                       // keys of a tile that a warp takes
     static constexpr int kTileBytes = kTile * D * (FP8 ? 1 : 2);
-    static constexpr int kStageBytes = 2 * kTileBytes + (FP8 ? 8 * kTile : 0);      // K, V, scales of K and of V
+    static constexpr int kStageBytes = (2 * kTileBytes + (FP8 ? 8 * kTile : 0) + 1023) / 1024 * 1024;      // K, V, scales of K and of V: swizzled rows
+                                                                                                           // begin on multiples of 1024 bytes
     static constexpr int kSlice = NR == 1 ? 64 : (NR == 2 ? 32 : 16);  // columns of the output that go through shared memory at a time
     static constexpr int kPitch = kSlice + 4;                          // floats between rows there: no bank conflicts
     static constexpr int kQBytes = kRows * D * 2;
@@ -249,6 +250,7 @@ struct Layout {
     // before its own is still on the way, and take the parity of the one before that for its own.)
     static constexpr int kStages = kFit > 24 ? 24 : kFit;
     static constexpr int kBytes = kSmall + kStages * kStageBytes + kShared + kMlBytes;
+    static_assert(kStageBytes % 1024 == 0 && kTileBytes % 1024 == 0, "the swizzle goes by the address");
     static_assert(kKeys % 16 == 0 && kStages >= 3, "whole steps of 16 keys, a ring of at least three tiles");
     static_assert(kStages * (16 + 32) + kRows * 4 + 16 <= 1536 && kTile <= 128, "small words");
 };

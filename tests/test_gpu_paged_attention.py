@@ -56,6 +56,17 @@ def test_one_long_request_over_all_ctas():
     check_call(cache, q, table, [30011], 0.088, out, lse)
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group,n_step", [(8, 1), (16, 1), (8, 4), (60, 1), (32, 4), (100, 2)])
+def test_rings_that_go_round(eight, d, group, n_step):
+    """Runs of many tiles, so that every stage of the ring is used several times, for every number of rows a CTA takes."""
+    lens, H_kv = [21011, 9000], 8
+    cache, q, table, n, _ = setup(lens, 64, group * H_kv, H_kv, d, eight, n_step)
+    out, lse = run(cache, q, table, n, 21011, d ** -0.5)
+    check_call(cache, q, table, lens, d ** -0.5, out, lse, only=[(0, 0), (0, 5), (1, 7)])
+
+
 def test_more_requests_than_threads():
     rng = np.random.default_rng(2)
     lens = [int(x) for x in rng.integers(0, 40, 1000)]
