@@ -708,13 +708,19 @@ def _token_stride(t, name, heads, d, index):
 
 def _on_cache(cache, stream, **tensors):
     """_launch_on for calls whose device is the cache's."""
-    guard, stream = _launch_on(stream, **tensors)
-    for name, t in tensors.items():
-        if t is not None:
-            if t.get_device() != cache.device_index:
-                raise ValueError(f"{name} is on {t.device}, the cache is on cuda:{cache.device_index}")
-            break
-    return guard, stream
+    index = cache.device_index
+    for t in tensors.values():
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            for name, t in tensors.items():
+                _dev(t, name)
+                if t is not None and t.get_device() != index:
+                    raise ValueError(f"{name} is on {t.device}, the cache is on cuda:{index}")
+    if stream is not None:
+        if stream.device.index != index:
+            raise ValueError(f"the stream is on {stream.device}, the cache is on cuda:{index}")
+        return torch.cuda.stream(stream), stream.cuda_stream
+    raw = torch._C._cuda_getCurrentRawStream(index)
+    return (_NO_GUARD if torch.cuda.current_device() == index else torch.cuda.device(index)), raw
 
 
 def paged_append(cache, k, v, slots, stream=None):

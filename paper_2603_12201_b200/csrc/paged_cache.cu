@@ -68,7 +68,7 @@ __device__ __forceinline__ uint32_t two_maxima(uint4 k, uint4 v) {
     return *reinterpret_cast<const uint32_t*>(&m);
 }
 
-template <bool FP8>
+template <bool FP8, int D>
 __global__ void __launch_bounds__(kAppendThreads, 3)
 paged_append_kernel(const AppendArgs a) {
     __shared__ int run_len;
@@ -76,7 +76,8 @@ paged_append_kernel(const AppendArgs a) {
     let_next_start();
     wait_for_previous();
     const PagedCache& c = a.c;
-    const int vecs = c.H_kv * (c.d / 8), per_head = c.d / 8;
+    constexpr int per_head = D / 8;
+    const int vecs = c.H_kv * per_head;
     const int cols = min(vecs, kAppendThreads), lanes = kAppendThreads / cols;       // threads of a row, rows at a time
     const int lane = threadIdx.x / cols;
     const int col = blockIdx.y * kAppendThreads + threadIdx.x % cols;
@@ -109,12 +110,28 @@ paged_append_kernel(const AppendArgs a) {
         uint4 hi = make_uint4(kBf16NegInf2, kBf16NegInf2, kBf16NegInf2, kBf16NegInf2);
         const int64_t base = page * c.page_stride + head * c.head_stride + d0;        // elements
         const int64_t scale_base = (page * c.H_kv + head) * c.page_size;
-        constexpr int U = FP8 ? 2 : 4;                                                // rows in flight a thread
-        if (c.bounds)
-            for (int r0 = lane; r0 < off; r0 += U * lanes) {                          // rows that are there
-                uint4 x[U];
+        constexpr int U = 2, U_OLD = FP8 ? 2 : 4;                                               // rows of a thread on their way
+        // new rows: the next U of a thread are on their way while these are worked on
+        const uint4 *k_from = a.k + (t0 + lane) * a.k_stride + col, *v_from = a.v + (t0 + lane) * a.v_stride + col;
+        const int64_t k_step = lanes * a.k_stride, v_step = lanes * a.v_stride, to_step = lanes * c.token_stride;
+        int64_t to = base + (off + lane) * c.token_stride;
+        uint4 k_next[U], v_next[U];
+        auto fetch = [&](int i0) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u) {
+                const bool in = works && i0 + u * lanes + lane < n_new;
+                k_next[u] = in ? *k_from : make_uint4(0u, 0u, 0u, 0u);
+                v_next[u] = in ? *v_from : make_uint4(0u, 0u, 0u, 0u);
+                k_from += k_step;
+                v_from += v_step;
+            }
+        };
+        fetch(0);
+        if (c.bounds)
+            for (int r0 = lane; r0 < off; r0 += U_OLD * lanes) {                          // rows that are there
+                uint4 x[U_OLD];
+#pragma unroll
+                for (int u = 0; u < U_OLD; ++u) {
                     const int r = r0 + u * lanes;
                     if (!works || r >= off) continue;
                     const int64_t at = base + r * c.token_stride;
@@ -124,32 +141,31 @@ paged_append_kernel(const AppendArgs a) {
                         x[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + at);
                 }
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U_OLD; ++u)
                     if (works && r0 + u * lanes < off) widen(x[u], lo, hi);
             }
         for (int i0 = 0; i0 < n_new; i0 += U * lanes) {                               // (all threads: they shuffle)
             Vec8 k[U], v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int i = i0 + u * lanes + lane;
-                const bool in = works && i < n_new;
-                k[u].raw = in ? a.k[(t0 + i) * a.k_stride + col] : make_uint4(0u, 0u, 0u, 0u);
-                v[u].raw = in ? a.v[(t0 + i) * a.v_stride + col] : make_uint4(0u, 0u, 0u, 0u);
+                k[u].raw = k_next[u];
+                v[u].raw = v_next[u];
             }
+            if (i0 + U * lanes < n_new) fetch(i0 + U * lanes);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u, to += to_step) {
                 const int i = i0 + u * lanes + lane;
                 const bool in = works && i < n_new;
-                const int64_t at = base + (off + i) * c.token_stride;
                 if (!FP8) {
                     if (in) {
-                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(c.k) + at) = k[u].raw;
-                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(c.v) + at) = v[u].raw;
+                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(c.k) + to) = k[u].raw;
+                        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(c.v) + to) = v[u].raw;
                         widen(k[u].raw, lo, hi);
                     }
                     continue;
                 }
                 uint32_t m = two_maxima(k[u].raw, v[u].raw);
+#pragma unroll
                 for (int o = per_head / 2; o > 0; o >>= 1) {                          // (a head's threads are aligned within a warp)
                     const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, m, o);
                     const __nv_bfloat162 z = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&y));
@@ -159,8 +175,8 @@ paged_append_kernel(const AppendArgs a) {
                 if (in) {
                     const float ks = over_448(fmaxf(k_max, 1e-12f)), vs = over_448(fmaxf(v_max, 1e-12f));
                     const uint2 kc = quantize8(k[u], ks);
-                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.k) + at) = kc;
-                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.v) + at) = quantize8(v[u], vs);
+                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.k) + to) = kc;
+                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(c.v) + to) = quantize8(v[u], vs);
                     if (d0 == 0) {
                         c.k_scale[scale_base + off + i] = ks;
                         c.v_scale[scale_base + off + i] = vs;
@@ -183,9 +199,9 @@ paged_append_kernel(const AppendArgs a) {
                 }
         }
         if (works && lane == 0 && rows > 0) {
-            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(c.bounds) + (page * c.H_kv + head) * 2 * c.d + d0;
-            *reinterpret_cast<uint4*>(to) = lo;
-            *reinterpret_cast<uint4*>(to + c.d) = hi;
+            __nv_bfloat16* edge = static_cast<__nv_bfloat16*>(c.bounds) + (page * c.H_kv + head) * 2 * D + d0;
+            *reinterpret_cast<uint4*>(edge) = lo;
+            *reinterpret_cast<uint4*>(edge + D) = hi;
         }
     }
 }
@@ -243,8 +259,11 @@ cudaError_t launch_paged_append(const PagedCache& c, const void* k, int64_t k_st
     const AppendArgs a{c, static_cast<const uint4*>(k), static_cast<const uint4*>(v), k_stride / 8, v_stride / 8, slots, n, chunk};
     const int vecs = c.H_kv * (c.d / 8);
     const dim3 grid(static_cast<unsigned>((n + chunk - 1) / chunk), static_cast<unsigned>((vecs + kAppendThreads - 1) / kAppendThreads));
-    return c.fp8 ? launch_behind(paged_append_kernel<true>, grid, kAppendThreads, 0, stream, a)
-                 : launch_behind(paged_append_kernel<false>, grid, kAppendThreads, 0, stream, a);
+    if (c.d == 128)
+        return c.fp8 ? launch_behind(paged_append_kernel<true, 128>, grid, kAppendThreads, 0, stream, a)
+                     : launch_behind(paged_append_kernel<false, 128>, grid, kAppendThreads, 0, stream, a);
+    return c.fp8 ? launch_behind(paged_append_kernel<true, 64>, grid, kAppendThreads, 0, stream, a)
+                 : launch_behind(paged_append_kernel<false, 64>, grid, kAppendThreads, 0, stream, a);
 }
 
 cudaError_t launch_paged_gather(const PagedCache& c, const int64_t* slots, int64_t n, void* k_out, void* v_out, cudaStream_t stream) {
