@@ -879,10 +879,12 @@ idxc_status idxc_page_scores(const void* bounds, int64_t n_pages, int page_size,
         return IDXC_ERR_INVALID_ARG;
     DeviceInfo& di = device_info();
     if (!di.ok) return IDXC_ERR_CUDA;
-    g_launches += 1;
-    return launch_page_scores(bounds, n_pages, page_size, H_kv, d, q, q_stride, n_step, H / H_kv, table, ld_table, lens, static_cast<int>(B), keep_first,
-                              keep_last, scale, scores, ld_scores, n_pages_out, di.sm_count, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
-               ? IDXC_OK : IDXC_ERR_CUDA;
+    int n_l = 0;
+    const cudaError_t e = launch_page_scores(bounds, n_pages, page_size, H_kv, d, q, q_stride, n_step, H / H_kv, table, ld_table, lens, static_cast<int>(B),
+                                             keep_first, keep_last, scale, scores, ld_scores, n_pages_out, di.status_ptr, di.sm_count,
+                                             static_cast<cudaStream_t>(cuda_stream), &n_l);
+    g_launches += n_l;
+    return e == cudaSuccess ? IDXC_OK : IDXC_ERR_CUDA;
 }
 
 idxc_status idxc_selftest_bounded_wait(uint32_t wait_cycles, void* cuda_stream) {

@@ -207,7 +207,7 @@ cudaError_t launch_paged_gather(const PagedCache& c, const int64_t* slots, int64
 // page_scores.cu
 cudaError_t launch_page_scores(const void* bounds, int64_t n_pages, int P, int H_kv, int d, const void* q, int64_t q_stride, int n_step, int group,
                                const int32_t* table, int64_t ld_table, const int32_t* lens, int B, int keep_first, int keep_last, float scale,
-                               float* scores, int64_t ld, int32_t* n_out, int sm_count, cudaStream_t stream);
+                               float* scores, int64_t ld, int32_t* n_out, unsigned int* status, int sm_count, cudaStream_t stream, int* launches);
 // paged_attn.cu. k_map, v_map: the cache as [n_pages][H_kv][page_size][d], boxes of 128 bytes (d = 64 in 8 bits: 64) x 64, 32 or 16 tokens
 // (the most that divides page_size), swizzled over their own width.
 struct PagedAttnArgs {
