@@ -6,7 +6,7 @@
 // those of up to eight heads of a page (4 KB) into a ring in shared memory, 64 (page, head) pairs a stage; eight warps take eight pages of a head each
 // with warp-level MMAs (rows as M, pages as N). The columns are permuted alike in both operands, so that a lane's share of four fragments is 16
 // contiguous bytes, and slots lie 64 bytes farther apart than they are long, so that the reads meet no bank twice. 32 requests of 8K to 64K positions
-// (74455 pages of 8 heads, d = 128): 53 us, 5.7 TB/s; with fragments straight from global memory, 64 bytes of eight pages an instruction, 58.
+// (73702 pages of 8 heads, d = 128): 53 us, 5.7 TB/s; with fragments straight from global memory, 64 bytes of eight pages an instruction, 58.
 #include <cuda_bf16.h>
 
 #include "kernels.h"
