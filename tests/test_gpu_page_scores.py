@@ -15,7 +15,8 @@ FORCED = float(np.float32(3e38))
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("lens,P,H,H_kv,n_step,first,last", [
     ([1], 16, 1, 1, 1, 0, 0), ([777, 0, 16], 16, 32, 8, 1, 1, 1), ([3000], 48, 16, 1, 1, 0, 2), ([100, 2000, 17], 16, 34, 2, 1, 2, 0), ([900, 5], 32, 64, 1, 1, 0, 0),
-    ([500], 16, 128, 1, 1, 1, 1), ([333, 1500], 64, 12, 4, 4, 1, 1), ([600], 16, 100, 1, 3, 5, 5), ([40000], 16, 8, 2, 1, 1, 1)])
+    ([500], 16, 128, 1, 1, 1, 1), ([333, 1500], 64, 12, 4, 4, 1, 1), ([600], 16, 100, 1, 3, 5, 5), ([40000], 16, 8, 2, 1, 1, 1),
+    ([900, 33], 16, 24, 12, 1, 1, 1), ([500], 32, 18, 6, 1, 0, 0), ([700], 16, 22, 11, 1, 1, 0), ([300], 16, 256, 2, 1, 1, 1), ([2000], 1024, 16, 16, 1, 0, 1)])
 def test_against_the_oracle(d, lens, P, H, H_kv, n_step, first, last):
     g = gen(sum(lens) + H + d)
     table, n_pages = tables(lens, P, g)

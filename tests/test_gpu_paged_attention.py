@@ -30,7 +30,8 @@ def run(cache, q, table, lens, max_len, scale, **kw):
     ([1], 16, 1, 1, 1, "tokens"), ([64], 64, 8, 8, 1, "heads"), ([777], 16, 32, 8, 1, "tokens"), ([5, 0, 130, 64, 63, 65], 16, 6, 2, 1, "pair"),
     ([300, 1, 2], 48, 16, 1, 1, "tokens"), ([500, 3, 90], 32, 34, 2, 1, "heads"), ([200, 700], 64, 35, 1, 1, "tokens"), ([900], 128, 128, 2, 1, "pair"),
     ([150, 333], 16, 128, 1, 1, "tokens"), ([400, 2, 1], 16, 8, 2, 4, "tokens"), ([129, 40], 32, 40, 4, 3, "pair"), ([70, 1000], 16, 100, 1, 3, "tokens"),
-    ([2500], 96, 7, 7, 2, "tokens"), ([10, 260], 16, 4, 2, 33, "heads")])
+    ([2500], 96, 7, 7, 2, "tokens"), ([10, 260], 16, 4, 2, 33, "heads"), ([1100], 64, 2, 1, 1024, "tokens"), ([2100, 40], 1024, 8, 2, 1, "pair"),
+    ([70, 200], 16, 22, 11, 1, "tokens"), ([70, 500], 32, 24, 12, 1, "heads"), ([333], 16, 48, 16, 2, "tokens"), ([600, 1], 80, 260, 4, 1, "tokens")])
 def test_against_the_oracle(eight, d, lens, P, H, H_kv, n_step, layout):
     cache, q, table, n, _ = setup(lens, P, H, H_kv, d, eight, n_step, layout)
     scale = d ** -0.5
@@ -74,6 +75,27 @@ def test_more_requests_than_threads():
     cache, q, table, n, _ = setup(lens, 16, 2, 1, 64, False)
     out, lse = run(cache, q, table, n, 40, 0.2)
     check_call(cache, q, table, lens, 0.2, out, lse)
+
+
+def test_the_most_requests():
+    B, P, g = 65535, 16, gen(6)
+    lens = torch.randint(0, 2, (B,), generator=g)
+    lens[::4099] = 16
+    n_pages = 300
+    cache = Cache(n_pages, P, 1, 64, False, g)
+    table = torch.randint(0, n_pages, (B, 1), generator=g).to(torch.int32).to(DEV)
+    q = bf16((B, 1, 1, 64), g).to(DEV)
+    out, lse = run(cache, q, table, lens.to(torch.int32).to(DEV), 16, 0.2)
+    k, v = cache.k[:, 0, 0].double(), cache.v[:, 0, 0]
+    one = (lens == 1).to(DEV)
+    page = table[one, 0].long()
+    assert torch.equal(out[one, 0, 0], v[page])                       # a single key: its value
+    x = 0.2 * (q[one, 0, 0].double() * k[page]).sum(dim=1)
+    assert torch.all((lse[one, 0, 0].double() - x).abs() <= 2.0 ** -16 * 0.2 * (q[one, 0, 0].double() * k[page]).abs().sum(dim=1) + 2.0 ** -19 * (1 + x.abs()))
+    none = (lens == 0).to(DEV)
+    assert not out[none].any() and torch.isneginf(lse[none]).all()
+    some = torch.arange(0, B, 4099)
+    check_call(cache, q[some.to(DEV)], table[some.to(DEV)], [16] * some.numel(), 0.2, out[some.to(DEV)], lse[some.to(DEV)])
 
 
 def test_all_requests_empty():

@@ -86,10 +86,11 @@ def test_append_and_gather(eight, lens, new, P, H_kv, d, layout):
 
 
 @pytest.mark.parametrize("eight", [False, True])
-def test_long_prompts(eight):
+@pytest.mark.parametrize("P,H_kv,d", [(64, 2, 64), (16, 1, 128), (1024, 1, 64), (48, 3, 64)])
+def test_long_prompts(eight, P, H_kv, d):
     """More tokens than the threshold of one CTA a token; runs that begin and end inside the CTAs' chunks."""
     g = gen(11)
-    lens, new, P, H_kv, d = [9, 0, 70], [3001, 17, 1500], 64, 2, 64
+    lens, new = [9, 0, 70], [3001, 17, 1500]
     table, n_pages = tables([n + m for n, m in zip(lens, new)], P, g)
     cache = Cache(n_pages, P, H_kv, d, eight, g, bounds=True)
     slots = slots_of(table, lens, new, P)
