@@ -2,8 +2,11 @@
 //     x[s] = scale <q, k_s> over the visible keys s,   out = sum_s softmax(x)[s] v_s,   lse = log sum_s exp(x[s])
 // over all pages of a request, or over the pages that a selection names for each (request, key head).
 //
+// A unit is a (request, key head, block of rows). Few units of few tiles: a cluster of up to 8 CTAs takes a unit and joins its parts over distributed shared
+// memory, one launch in all.
+//
 // Measured (graph replays, one B200): 32 requests of 4K to 32K bf16 keys, 64 heads over 8: 352 us, 6.9 TB/s of what has to be read; 8 requests of 131072
-// 8-bit keys: 352 us, 6.3 TB/s; 8 x 32768 with 16 / 32 rows a key head: bf16 6.4 / 6.2, 8 bits 5.4 / 3.4 TB/s; one request of 777 keys: 9.3 us with the merge.
+// 8-bit keys: 352 us, 6.3 TB/s; 8 x 32768 with 16 / 32 rows a key head: bf16 6.4 / 6.2, 8 bits 5.4 / 3.4 TB/s; one request of 777 keys: 6.1 us.
 //
 // What bounds it: a key and a value of d columns are 4 d bytes (bf16) and 4 d flops a query row; with the 1 to 32 rows that share a key head
 // in a decode step that is 1 to 32 flops a byte, far below the tensor cores' 200: HBM. So the design serves the copies: a ring of 64- or 128-key tiles
@@ -16,7 +19,7 @@
 //
 // Up to 32 rows: 4 warps, each 16 or 32 keys of a tile with its own running reference and sum; 2 or 3 CTAs an SM hide each other's segment ends. More rows:
 // 8 warps, of which 2 or 4 share the keys and take 32 rows each. The warps' parts meet once at a segment's end, in shared memory. The tiles of all
-// (request, key head, block of rows), end to end, are cut into runs of equal cost, a run a CTA, which finds it from the lengths on the device;
+// units, end to end, are cut into runs of equal cost, a run a CTA, which finds it from the lengths on the device;
 // segments cut by a run's end go to the workspace in fp32 and through a merge kernel. All sums have an order fixed by the sizes, so results
 // repeat bit for bit.
 //
@@ -33,6 +36,9 @@ namespace idxc {
 namespace {
 
 constexpr int kProducerRegs = 40;
+// Tiles of a CTA up to which few units are given to clusters. (bf16, 8 key heads, d = 128, one request of 777 / 2000 / 4000 / 8000 keys: 9.3 / 11.1 / 12.7 /
+// 13.9 us by runs and a merge, 6.1 / 7.5 / 10.4 / 16.4 by clusters, with 2, 4, 8 and 16 tiles a CTA.)
+constexpr int kJoinTiles = 8;
 constexpr int kSegmentTiles = 4;                // what a segment's beginning and end cost, in tiles
 // Log2 units by which a score may pass its row's reference before that moves. In bf16 up to 16 rows the reference is the maximum: the largest
 // probability is then 1, which bf16 holds exactly (error of out against 64 bits for 16 requests over 64 pages: 2.2e-3 with 8, 1.8e-3 with 0, of which
@@ -48,6 +54,7 @@ struct Params {
     int units;                   // (heads of a CTA, blocks of query rows) of a request
     int row_blocks;              // blocks of a CTA's query rows of a (request, key head)
     int tile_log2;               // keys of a tile
+    int join;                    // 0: runs over all units; else a unit is a cluster's of so many CTAs, which join their parts themselves
     int piece_log2;              // keys of a copy: 16, 32 or 64
     float scale_log2;            // scale * log2(e)
     float* part_o;               // [grid][2][MAXR][D]
@@ -105,6 +112,16 @@ __device__ __forceinline__ void st_shared_v2(uint32_t addr, uint32_t x, uint32_t
 // log2 of a positive scale, rounded up, as a number between -60 and 60.
 __device__ __forceinline__ float log2_above(float scale) {
     return static_cast<float>(min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 126, -60), 60));
+}
+// The two barriers of a cluster that joins its parts, for the warps that have no share in that: parts are there; parts have been read.
+__device__ __forceinline__ void leave_cluster() {
+    cluster_sync();
+    cluster_sync();
+}
+__device__ __forceinline__ float2 ld_cluster_f32x2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
 }
 template <int WARPS>
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
@@ -199,8 +216,20 @@ __device__ __forceinline__ int pieces_of(const Run& run, const Segment& s, int h
 struct Walk {
     const Params& p;
     int b, x, left, nt;
-    __device__ __forceinline__ Walk(const Params& q, const Run& r) : p(q), b(r.b), x(r.x), left(r.n), nt(r.n > 0 ? tiles_of(q, r.b) : 0) {}
+    __device__ __forceinline__ Walk(const Params& q, const Run& r) : p(q), b(r.b), x(r.x), left(r.n), nt(r.n > 0 && !q.join ? tiles_of(q, r.b) : 0) {}
     __device__ __forceinline__ bool next(Segment& s) {
+        if (p.join) {                            // this CTA's share of its cluster's unit, which may be none; once
+            if (left == 0) return false;
+            left = 0;
+            const int per_request = p.a.c.H_kv * p.row_blocks, unit = blockIdx.x / p.join, rank = blockIdx.x % p.join;
+            s.b = unit / per_request;
+            s.head = (unit - s.b * per_request) / p.row_blocks;
+            s.rows = unit - s.b * per_request - s.head * p.row_blocks;
+            s.nt = tiles_of(p, s.b);
+            s.t0 = static_cast<int>(static_cast<unsigned>(s.nt) * rank / p.join);
+            s.n = static_cast<int>(static_cast<unsigned>(s.nt) * (rank + 1) / p.join) - s.t0;
+            return true;
+        }
         const int units = p.units;
         while (left > 0) {
             while (x == length_of_unit(nt) * units) {       // the request's end (or one without tiles); more follow
@@ -260,6 +289,7 @@ struct Layout {
     static constexpr int kBytes = kSmall + kStages * kStageBytes + kShared + kMlBytes;
     static_assert(kStageBytes % 1024 == 0 && kTileBytes % 1024 == 0, "the swizzle goes by the address");
     static_assert(kKeys % 16 == 0 && kStages >= 3, "whole steps of 16 keys, a ring of at least three tiles");
+    static_assert(kRows * (D * 4 + 8) <= kStages * kStageBytes, "a CTA's part of a cluster's unit");
     static_assert(kStages * (16 + 32) + kRows * 4 + 16 <= 1536 && kTile <= 128, "small words");
 };
 
@@ -281,6 +311,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const uint32_t stages = (base + 1023u) & ~1023u;
     const uint32_t q_s = stages + NS * L::kStageBytes;
     const uint32_t red_s = q_s;
+    const uint32_t join_s = stages;              // [rows][D] output and [rows] (maximum, sum) of a CTA whose cluster joins them, when its tiles are done with
     const uint32_t ml_s = q_s + L::kShared;      // [parts][rows] (maximum, sum) of a warp, then (factor, -)
     const uint32_t bars = ml_s + L::kMlBytes;    // full[NS], empty[NS]
     const uint32_t pos_s = bars + NS * 16;       // [NS][8] position of the first key of each piece, -1: none
@@ -302,12 +333,17 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
     let_next_start();
     wait_for_previous();
-    const Run run = find_run(p, scratch);        // (its barriers publish the mbarriers too)
+    Run run{0, 0, 1, 0};
+    if (p.join) __syncthreads();
+    else run = find_run(p, scratch);             // (its barriers publish the mbarriers too)
     const PagedAttnArgs& a = p.a;
 
     if (warp >= W) {
         if (L::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
-        if (warp > W) return;
+        if (warp > W) {
+            if (p.join > 1) leave_cluster();
+            return;
+        }
         // ------------------------------------------------------------ producer: pieces of pages into the ring
         constexpr int kTileLog2 = L::kTile == 64 ? 6 : 7;
         const int piece = 1 << p.piece_log2, per_tile_log2 = kTileLog2 - p.piece_log2, per_tile = 1 << per_tile_log2;
@@ -392,6 +428,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 while (!mbar_try_wait(bars + 8 * (i % NS), (i / NS) & 1) && clock64() - t0 < kWaitCycleBudget) {}
             }
         }
+        __syncwarp();
+        if (p.join > 1) leave_cluster();
         return;
     }
 
@@ -435,7 +473,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         const int len = length_of(a, s.b);
         const int head = s.head, row0 = s.rows * L::kRows;
         const int n_rows = min(rows_all - row0, L::kRows);
-        const bool whole = s.t0 == 0 && s.n == s.nt;
+        const bool whole = s.t0 == 0 && s.n == s.nt && p.join <= 1;
         if (threadIdx.x < Q_THREADS) {
 #pragma unroll
             for (int u = 0; u < QV; ++u) {
@@ -715,7 +753,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
             st_shared_f32(row_s + r * 4, whole ? (sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum) : 1.f);
             if (!whole) {
-                p.part_ml[piece_row + r] = make_float2(best, sum);
+                if (p.join) st_shared_f32x2(join_s + L::kRows * D * 4 + r * 8, best, sum);
+                else p.part_ml[piece_row + r] = make_float2(best, sum);
             } else if (a.lse) {
                 const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
                 a.lse[(static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h] =
@@ -759,7 +798,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     v.w += z.w;
                 }
                 if (!whole) {
-                    *reinterpret_cast<float4*>(p.part_o + (piece_row + r) * D + c0 + c) = v;
+                    if (p.join) st_shared_v4(join_s + (r * D + c0 + c) * 4, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+                    else *reinterpret_cast<float4*>(p.part_o + (piece_row + r) * D + c0 + c) = v;
                 } else {
                     const float over = ld_shared_f32(row_s + r * 4);
                     const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
@@ -769,8 +809,44 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
             consumers_sync<W>();
         }
+        if (p.join > 1) {
+            // The cluster's parts: every CTA joins some of the rows, D / 2 threads each.
+            cluster_sync();
+            constexpr int T = D / 2;
+            const int rank = blockIdx.x % p.join, c = threadIdx.x % T * 2;
+            for (int r = rank + p.join * static_cast<int>(threadIdx.x / T); r < n_rows; r += p.join * (W * 32 / T)) {
+                float2 ml[8], of[8];
+                float best = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < p.join) {
+                        const uint32_t at = map_to_cta(join_s, k);
+                        ml[k] = ld_cluster_f32x2(at + L::kRows * D * 4 + r * 8);
+                        of[k] = ld_cluster_f32x2(at + (r * D + c) * 4);
+                        best = fmaxf(best, ml[k].x);
+                    }
+                const float use = best == -INFINITY ? 0.f : best;
+                float sum = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < p.join) {
+                        const float w = exp2_fast(ml[k].x - use);
+                        sum += ml[k].y * w;
+                        x += of[k].x * w;
+                        y += of[k].y * w;
+                    }
+                const float over = sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum;
+                const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
+                const int64_t row = (static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h;
+                *reinterpret_cast<uint32_t*>(a.out + row * D + c) = pack_bf16(x * over, y * over);
+                if (a.lse && c == 0) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
+            }
+            cluster_sync();
+            return;
+        }
         if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.head * p.row_blocks + s.rows, pieces_of(run, s, p.heads), 0);
     }
+    if (p.join) return;
     if (threadIdx.x == 0) p.owners[blockIdx.x] = owner;
 
     // Requests without keys: zeros and -inf.
@@ -873,13 +949,42 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
     while (p.a.c.H_kv % p.heads) --p.heads;
     p.units = p.a.c.H_kv / p.heads * p.row_blocks;
     p.tile_log2 = L::kTile == 64 ? 6 : 7;
-    const int most = sm_count * L::kCtas < max_grid(L::kRows) ? sm_count * L::kCtas : max_grid(L::kRows);
-    const int grid = most / p.heads * p.heads;
     auto kernel = paged_attn_kernel<D, FP8, NR, RG>;
     cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes);
     if (e != cudaSuccess) return e;
-    e = launch_behind(kernel, dim3(grid), L::kThreads, L::kBytes, stream, k_map, v_map, p);
+    // Few units of few tiles: a unit a cluster, cut among as many CTAs (8 at most) as all have room at once, which join their parts over distributed
+    // shared memory. One launch, and no scan over the requests; but every unit is cut alike, whatever its length, so only where that is at most
+    // kJoinTiles tiles a CTA.
+    const int64_t units = static_cast<int64_t>(p.a.B) * p.a.c.H_kv * p.row_blocks;
+    int64_t keys = p.a.max_len;
+    if (p.a.pages) {
+        const int64_t pages = (keys + p.a.c.page_size - 1) / p.a.c.page_size;
+        keys = (pages < p.a.n_sel ? pages : p.a.n_sel) * p.a.c.page_size;
+    }
+    const int64_t tiles = (keys + L::kTile - 1) / L::kTile;
+    int join = 8;
+    while (join > 1 && (units * join > sm_count * L::kCtas || join / 2 >= tiles)) join /= 2;
+    p.join = units * join <= sm_count * L::kCtas && tiles <= join * kJoinTiles ? join : 0;
     *launches += 1;
+    if (p.join) {
+        cudaLaunchAttribute attr[2]{};
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = static_cast<unsigned>(join);
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(static_cast<unsigned>(units * join));
+        cfg.blockDim = dim3(L::kThreads);
+        cfg.dynamicSmemBytes = L::kBytes;
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        return cudaLaunchKernelEx(&cfg, kernel, k_map, v_map, p);
+    }
+    const int most = sm_count * L::kCtas < max_grid(L::kRows) ? sm_count * L::kCtas : max_grid(L::kRows);
+    const int grid = most / p.heads * p.heads;
+    e = launch_behind(kernel, dim3(grid), L::kThreads, L::kBytes, stream, k_map, v_map, p);
     if (e != cudaSuccess) return e;
     const int rows = p.a.n_step * p.a.group < L::kRows ? p.a.n_step * p.a.group : L::kRows;
     *launches += 1;

@@ -24,19 +24,46 @@ def run(cache, q, table, lens, max_len, scale, **kw):
     return out, lse
 
 
-@pytest.mark.parametrize("eight", [False, True])
-@pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("lens,P,H,H_kv,n_step,layout", [
+SHAPES = [
     ([1], 16, 1, 1, 1, "tokens"), ([64], 64, 8, 8, 1, "heads"), ([777], 16, 32, 8, 1, "tokens"), ([5, 0, 130, 64, 63, 65], 16, 6, 2, 1, "pair"),
     ([300, 1, 2], 48, 16, 1, 1, "tokens"), ([500, 3, 90], 32, 34, 2, 1, "heads"), ([200, 700], 64, 35, 1, 1, "tokens"), ([900], 128, 128, 2, 1, "pair"),
     ([150, 333], 16, 128, 1, 1, "tokens"), ([400, 2, 1], 16, 8, 2, 4, "tokens"), ([129, 40], 32, 40, 4, 3, "pair"), ([70, 1000], 16, 100, 1, 3, "tokens"),
     ([2500], 96, 7, 7, 2, "tokens"), ([10, 260], 16, 4, 2, 33, "heads"), ([1100], 64, 2, 1, 1024, "tokens"), ([2100, 40], 1024, 8, 2, 1, "pair"),
-    ([70, 200], 16, 22, 11, 1, "tokens"), ([70, 500], 32, 24, 12, 1, "heads"), ([333], 16, 48, 16, 2, "tokens"), ([600, 1], 80, 260, 4, 1, "tokens")])
+    ([70, 200], 16, 22, 11, 1, "tokens"), ([70, 500], 32, 24, 12, 1, "heads"), ([333], 16, 48, 16, 2, "tokens"), ([600, 1], 80, 260, 4, 1, "tokens")]
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,P,H,H_kv,n_step,layout", SHAPES)
 def test_against_the_oracle(eight, d, lens, P, H, H_kv, n_step, layout):
     cache, q, table, n, _ = setup(lens, P, H, H_kv, d, eight, n_step, layout)
     scale = d ** -0.5
     out, lse = run(cache, q, table, n, max(lens) + 5 if max(lens) + 5 <= table.shape[1] * P else max(lens), scale)
     check_call(cache, q, table, lens, scale, out, lse)
+
+
+@pytest.mark.parametrize("eight,d", [(False, 64), (False, 128), (True, 64), (True, 128)])
+@pytest.mark.parametrize("lens,P,H,H_kv,n_step,layout", SHAPES)
+def test_short_requests_under_a_high_bound(eight, d, lens, P, H, H_kv, n_step, layout):
+    """Where max_len allows long requests the work is cut into runs over all units, and segments go through the merge, however short the requests are."""
+    cache, q, table, n, _ = setup(lens, P, H, H_kv, d, eight, n_step, layout)
+    wide = torch.full((len(lens), 1 + 100000 // P), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    scale = d ** -0.5
+    out, lse = run(cache, q, wide, n, 100000, scale)
+    check_call(cache, q, table, lens, scale, out, lse)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("B,H_kv,top", [(1, 1, 64), (1, 1, 5000), (3, 8, 1000), (9, 4, 600), (18, 8, 700), (37, 8, 300), (140, 2, 500), (20, 2, 129)])
+def test_units_of_clusters(eight, B, H_kv, top):
+    """Every size of cluster, units whose CTAs have no tile, and requests without keys among them."""
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(0, top + 1, B)]
+    lens[0] = top
+    cache, q, table, n, _ = setup(lens, 16, 8 * H_kv, H_kv, 128, eight)
+    out, lse = run(cache, q, table, n, top, 0.09)
+    check_call(cache, q, table, lens, 0.09, out, lse)
 
 
 @pytest.mark.parametrize("eight", [False, True])
