@@ -39,6 +39,9 @@ constexpr int kProducerRegs = 40;
 // Tiles of a CTA up to which few units are given to clusters. (bf16, 8 key heads, d = 128, one request of 777 / 2000 / 4000 / 8000 keys: 9.3 / 11.1 / 12.7 /
 // 13.9 us by runs and a merge, 6.1 / 7.5 / 10.4 / 16.4 by clusters, with 2, 4, 8 and 16 tiles a CTA.)
 constexpr int kJoinTiles = 8;
+// Tiles above an equal share that a cut and the merge cost. (64 pages of 32 for 16 requests and 8 key heads, 8 rows: bf16, 16 tiles a CTA where 14 are a share, 30
+// us by runs, 26.6 by clusters of two; 8 bits, 16 where 9 are, 20.4 and 23.0. 32 pages of 64 in 8 bits for 100 requests and 4 heads, 32 and 29: 53 and 40.)
+constexpr int kJoinSlack = 5;
 constexpr int kSegmentTiles = 4;                // what a segment's beginning and end cost, in tiles
 // Log2 units by which a score may pass its row's reference before that moves. In bf16 up to 16 rows the reference is the maximum: the largest
 // probability is then 1, which bf16 holds exactly (error of out against 64 bits for 16 requests over 64 pages: 2.2e-3 with 8, 1.8e-3 with 0, of which
@@ -954,7 +957,7 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
     if (e != cudaSuccess) return e;
     // Few units of few tiles: a unit a cluster, cut among as many CTAs (8 at most) as all have room at once, which join their parts over distributed
     // shared memory. One launch, and no scan over the requests; but every unit is cut alike, whatever its length, so only where that is at most
-    // kJoinTiles tiles a CTA.
+    // kJoinTiles tiles a CTA, or where the units are alike (selections) and a CTA has hardly more than an equal share of all tiles.
     const int64_t units = static_cast<int64_t>(p.a.B) * p.a.c.H_kv * p.row_blocks;
     int64_t keys = p.a.max_len;
     if (p.a.pages) {
@@ -964,7 +967,9 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
     const int64_t tiles = (keys + L::kTile - 1) / L::kTile;
     int join = 8;
     while (join > 1 && (units * join > sm_count * L::kCtas || join / 2 >= tiles)) join /= 2;
-    p.join = units * join <= sm_count * L::kCtas && tiles <= join * kJoinTiles ? join : 0;
+    const int64_t room = sm_count * L::kCtas;
+    const bool alike = p.a.pages && tiles <= join * (units * tiles / room + kJoinSlack);
+    p.join = units * join <= room && (tiles <= join * kJoinTiles || alike) ? join : 0;
     *launches += 1;
     if (p.join) {
         cudaLaunchAttribute attr[2]{};
