@@ -863,19 +863,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 }
 
-// Joins the pieces of a segment that runs cut. blockIdx.x: the CTA in whose run the segment begins; a warp a row. Two round trips to memory: the
-// owner's word, then maxima, sums and the first pieces together.
-template <int D, int ROWS>
-__global__ void __launch_bounds__(128)
+// Joins the pieces of a segment that runs cut. blockIdx.x: the CTA in whose run the segment begins; kMergeWarps warps a row, which take its pieces in turn. Two
+// round trips to memory: the owner's word, then maxima, sums and the first pieces together. Units of many pieces get four warps a row (a request of 36392
+// keys and one key head has 296: 37 us in all with one warp, 18 with four), others one (96 requests of 2000 positions, 36 us in all, and 47 with four).
+template <int D, int ROWS, int kMergeWarps, int kMergeRows>
+__global__ void __launch_bounds__(32 * kMergeWarps * kMergeRows)
 paged_merge_kernel(const __grid_constant__ Params p, float out_scale) {
+    __shared__ float acc_s[kMergeRows][kMergeWarps][D], sum_s[kMergeRows][kMergeWarps];
     let_next_start();
     wait_for_previous();
     const int4 own = p.owners[blockIdx.x];
     if (own.x < 0) return;
-    const int lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, sub = (threadIdx.x >> 5) % kMergeWarps, in = (threadIdx.x >> 5) / kMergeWarps, r = blockIdx.y * kMergeRows + in;
     const int head = own.y / p.row_blocks, row0 = (own.y - head * p.row_blocks) * ROWS, pieces = own.z;
     const int n_rows = min(p.a.n_step * p.a.group - row0, ROWS);
-    if (r >= n_rows) return;
+    const bool works = r < n_rows;
     constexpr int V = D / 32, AHEAD = 4;         // columns of a lane; pieces on their way at a time
     auto row_of = [&](int i) -> int64_t { return (static_cast<int64_t>(blockIdx.x + i * p.heads) * 2 + (i == 0 ? 1 : 0)) * ROWS + r; };
     auto load = [&](int i, float(&y)[V]) {
@@ -892,35 +894,36 @@ paged_merge_kernel(const __grid_constant__ Params p, float out_scale) {
             y[1] = z.y;
         }
     };
+    const int mine = works && sub < pieces ? (pieces - sub + kMergeWarps - 1) / kMergeWarps : 0;      // this warp's: sub, sub + kMergeWarps, ...
     float y[AHEAD][V];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-        if (u < pieces) load(u, y[u]);
-    const float2 first = lane < pieces ? p.part_ml[row_of(lane)] : make_float2(-INFINITY, 0.f);
-    float top = first.x;
-    for (int i = 32 + lane; i < pieces; i += 32) top = fmaxf(top, p.part_ml[row_of(i)].x);
+        if (u < mine) load(sub + u * kMergeWarps, y[u]);
+    float top = -INFINITY;
+    if (works)
+        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, p.part_ml[row_of(i)].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const float use = top == -INFINITY ? 0.f : top;
     float acc[V] = {}, sum = 0.f;
-    for (int i0 = 0; i0 < pieces; i0 += 32) {
+    for (int i0 = 0; i0 < mine; i0 += 32) {
         float w = 0.f, lw = 0.f;
-        if (i0 + lane < pieces) {
-            const float2 ml = i0 == 0 ? first : p.part_ml[row_of(i0 + lane)];
+        if (i0 + lane < mine) {
+            const float2 ml = p.part_ml[row_of(sub + (i0 + lane) * kMergeWarps)];
             w = exp2_fast(ml.x - use);
             lw = w * ml.y;
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, o);
         sum += lw;
-        const int n = min(32, pieces - i0);
+        const int n = min(32, mine - i0);
         for (int i = 0; i < n; i += AHEAD) {
             float z[AHEAD][V];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) z[u][v] = y[u][v];
-                if (i0 + i + AHEAD + u < pieces) load(i0 + i + AHEAD + u, y[u]);
+                if (i0 + i + AHEAD + u < mine) load(sub + (i0 + i + AHEAD + u) * kMergeWarps, y[u]);
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
@@ -931,6 +934,18 @@ paged_merge_kernel(const __grid_constant__ Params p, float out_scale) {
                 }
             }
         }
+    }
+    if (kMergeWarps > 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc_s[in][sub][lane * V + v] = acc[v];
+        if (lane == 0) sum_s[in][sub] = sum;
+        __syncthreads();
+    }
+    if (sub != 0 || !works) return;
+    for (int w = 1; w < kMergeWarps; ++w) {
+        sum += sum_s[in][w];
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[v] += acc_s[in][w][lane * V + v];
     }
     const float over = sum == 0.f ? 0.f : out_scale / sum;
     const int step = (row0 + r) / p.a.group, h = row0 + r - step * p.a.group;
@@ -993,7 +1008,10 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
     if (e != cudaSuccess) return e;
     const int rows = p.a.n_step * p.a.group < L::kRows ? p.a.n_step * p.a.group : L::kRows;
     *launches += 1;
-    return launch_behind(paged_merge_kernel<D, L::kRows>, dim3(grid, (rows + 3) / 4), 128, 0, stream, p, FP8 ? 1.f / kF16Head : 1.f);
+    const float out_scale = FP8 ? 1.f / kF16Head : 1.f;
+    if (grid / p.heads > 12 * static_cast<int64_t>(p.a.B) * p.units)       // runs per unit, and so pieces: more than a warp's three batches in flight
+        return launch_behind(paged_merge_kernel<D, L::kRows, 4, 2>, dim3(grid, (rows + 1) / 2), 256, 0, stream, p, out_scale);
+    return launch_behind(paged_merge_kernel<D, L::kRows, 1, 4>, dim3(grid, (rows + 3) / 4), 128, 0, stream, p, out_scale);
 }
 
 }  // namespace
