@@ -12,7 +12,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libidxc.so"
 SOURCES = ["api.cu", "topk.cu", "topk_cluster.cu", "topk_stream.cu", "scorer_simt.cu", "scorer_tc.cu", "noalloc.cu", "selftest.cu", "quantize.cu", "pattern_tools.cu", "distill.cu", "sparse_attn.cu",
            "latent_cache.cu", "latent_attn.cu", "latent_attn_pair.cu", "attn_weights.cu", "evict.cu",
-           "page_tables.cu", "paged_cache.cu", "page_scores.cu", "paged_attn.cu"]
+           "page_tables.cu", "paged_cache.cu", "page_scores.cu", "paged_attn.cu", "paged_attn_rows.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",

@@ -232,6 +232,10 @@ bool paged_attn_fits(const PagedAttnArgs& a);           // the tile count of the
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
                               int sm_count, cudaStream_t stream, int* launches);
 
+// paged_attn_rows.cu: the same for many rows of a key head, bf16; launch_paged_attn goes there.
+cudaError_t launch_paged_attn_rows(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
+                                   int sm_count, cudaStream_t stream, int* launches);
+
 // selftest.cu: one tiny kernel whose only wait can never be satisfied; it must record a time-out in
 // `status` after `budget_cycles` and return.
 cudaError_t launch_selftest_bounded_wait(unsigned int* status, long long budget_cycles, cudaStream_t stream);

@@ -17,7 +17,7 @@
 // padding, and 64 keys in 8 bits took 1740 instructions instead of 1390. tcgen05's M = 64 or 128 with rows as N would fit too, but its scores would cross
 // tensor memory twice a tile, a latency that several resident CTAs would have to hide.) P^T comes out of the scores' registers by an 8 x 8 transposition.
 //
-// Up to 32 rows: 4 warps, each 16 or 32 keys of a tile with its own running reference and sum; 2 or 3 CTAs an SM hide each other's segment ends. More rows:
+// (More than kRowsOfRegisters bf16 rows: paged_attn_rows.cu.) Up to 32 rows: 4 warps, each 16 or 32 keys of a tile with its own running reference and sum; 2 or 3 CTAs an SM hide each other's segment ends. More rows:
 // 8 warps, of which 2 or 4 share the keys and take 32 rows each. The warps' parts meet once at a segment's end, in shared memory. The tiles of all
 // units, end to end, are cut into runs of equal cost, a run a CTA, which finds it from the lengths on the device;
 // segments cut by a run's end go to the workspace in fp32 and through a merge kernel. All sums have an order fixed by the sizes, so results
@@ -30,55 +30,29 @@
 #include <cuda_fp16.h>
 
 #include "kernels.h"
+#include "paged_attn.cuh"
 #include "ptx_sm100.cuh"
 
 namespace idxc {
+using namespace paged;
 namespace {
 
 constexpr int kProducerRegs = 40;
+// bf16 rows of a key head up to which this file's kernel is taken. (8 x 32768 keys, 8 key heads, d = 128 / 64: 64 rows 240 / 181 us, and 242 / 212 with
+// paged_attn_rows.cu, which takes 128 alike; 128 rows 477 / 347 here.)
+constexpr int kRowsOfRegisters = 64;
 // Tiles of a CTA up to which few units are given to clusters. (bf16, 8 key heads, d = 128, one request of 777 / 2000 / 4000 / 8000 keys: 9.3 / 11.1 / 12.7 /
 // 13.9 us by runs and a merge, 6.1 / 7.5 / 10.4 / 16.4 by clusters, with 2, 4, 8 and 16 tiles a CTA.)
 constexpr int kJoinTiles = 8;
 // Tiles above an equal share that a cut and the merge cost. (64 pages of 32 for 16 requests and 8 key heads, 8 rows: bf16, 16 tiles a CTA where 14 are a share, 30
 // us by runs, 26.6 by clusters of two; 8 bits, 16 where 9 are, 20.4 and 23.0. 32 pages of 64 in 8 bits for 100 requests and 4 heads, 32 and 29: 53 and 40.)
 constexpr int kJoinSlack = 5;
-constexpr int kSegmentTiles = 4;                // what a segment's beginning and end cost, in tiles
 // Log2 units by which a score may pass its row's reference before that moves. In bf16 up to 16 rows the reference is the maximum: the largest
 // probability is then 1, which bf16 holds exactly (error of out against 64 bits for 16 requests over 64 pages: 2.2e-3 with 8, 1.8e-3 with 0, of which
 // 1.7e-3 are the output's own rounding). With 32 rows a warp some reference moves at most steps, and that costs an eighth of the time (96 requests
 // of 16 heads and 4 tokens: 33.5 us with 8, 37.4 with 0). f16 of 8-bit rows is exact enough either way.
 template <bool FP8, int NR>
 constexpr float kSlack = FP8 || NR == 4 ? 8.f : 0.f;
-constexpr float kF16Head = 64.f;                // probabilities times scale reach 2^8; f16 holds them times 2^6
-
-struct Params {
-    PagedAttnArgs a;
-    int heads;                   // key heads that as many neighbouring CTAs walk through in step
-    int units;                   // (heads of a CTA, blocks of query rows) of a request
-    int row_blocks;              // blocks of a CTA's query rows of a (request, key head)
-    int tile_log2;               // keys of a tile
-    int join;                    // 0: runs over all units; else a unit is a cluster's of so many CTAs, which join their parts themselves
-    int piece_log2;              // keys of a copy: 16, 32 or 64
-    float scale_log2;            // scale * log2(e)
-    float* part_o;               // [grid][2][MAXR][D]
-    float2* part_ml;             // [grid][2][MAXR] (maximum in log2 units, sum)
-    int4* owners;                // [grid] the segment that begins in a CTA's run and does not end in it: (request, key head * row_blocks + block of rows, pieces); -1: none
-    unsigned int* status;
-};
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
 __device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
     float v;
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
@@ -130,92 +104,6 @@ template <int WARPS>
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
 
 // ---------------------------------------------------------------- work
-// Keys of request b that the call knows of.
-__device__ __forceinline__ int length_of(const PagedAttnArgs& a, int b) { return min(max(a.lens[b], 0), static_cast<int>(a.max_len)); }
-// Tiles of one (key head, block of rows) of request b: of its keys, or of the first min(n_sel, pages of the request) entries of its selection.
-__device__ __forceinline__ int tiles_of(const Params& p, int b) {
-    const int len = length_of(p.a, b), up = (1 << p.tile_log2) - 1;
-    if (!p.a.pages) return (len + up) >> p.tile_log2;
-    const int pages = (len + p.a.c.page_size - 1) / p.a.c.page_size;
-    return static_cast<int>((static_cast<int64_t>(min(p.a.n_sel, pages)) * p.a.c.page_size + up) >> p.tile_log2);
-}
-// p.heads neighbouring CTAs take the same stretch of keys for as many key heads, so that the rows of one token, which lie side by side in a cache with
-// tokens in front of heads, are read at about the same time (128-byte rows of 8 heads: 5.3 TB/s when every head went its own way). The units
-// (request, its heads for this CTA, block of rows) lie end to end, each kSegmentTiles and its tiles long, and are cut into runs of equal length: a
-// run with many short segments gets fewer tiles. A run that ends among the first kSegmentTiles of a unit has none of its tiles.
-struct Run {
-    int b, x;             // request, place among all of the request's units
-    int n;                // length
-    int total;            // of all units
-};
-__device__ __forceinline__ int length_of_unit(int tiles) { return tiles > 0 ? tiles + kSegmentTiles : 0; }
-// Beginning of a CTA's run: total * cta / n, cut among n = min(grid, total) CTAs so that no run in front of another is empty.
-__device__ __forceinline__ int run_begin(int total, int cta, int grid) {
-    const int n = min(grid, total);
-    if (cta >= n) return total;
-    const unsigned each = static_cast<unsigned>(total) / n, more = total - each * n;
-    return static_cast<int>(each * cta + more * cta / n);
-}
-__device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared, 16 words */) {
-    const int units = p.units, cta = blockIdx.x / p.heads, ctas = gridDim.x / p.heads;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_thr = blockDim.x, n_warps = n_thr >> 5;
-    int sum = 0, mine = 0;
-    for (int b = threadIdx.x; b < p.a.B; b += n_thr) {
-        const int n = length_of_unit(tiles_of(p, b)) * units;
-        if (b < n_thr) mine = n;
-        sum += n;
-    }
-    sum = __reduce_add_sync(0xFFFFFFFFu, sum);
-    if (lane == 0) scratch[warp] = sum;
-    __syncthreads();
-    Run r{0, 0, 0, 0};
-    for (int w = 0; w < n_warps; ++w) r.total += scratch[w];
-    const int first = run_begin(r.total, cta, ctas);
-    r.n = run_begin(r.total, cta + 1, ctas) - first;
-    if (r.n > 0) {                               // (uniform over the CTA)
-        int before_block = 0;
-        for (int b0 = 0; b0 < p.a.B; b0 += n_thr) {
-            const int b = b0 + threadIdx.x;
-            const int n = b0 == 0 ? mine : (b < p.a.B ? length_of_unit(tiles_of(p, b)) * units : 0);
-            int incl = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += y;
-            }
-            __syncthreads();
-            if (lane == 31) scratch[warp] = incl;
-            __syncthreads();
-            int before = before_block + incl - n, all = 0;
-            for (int w = 0; w < n_warps; ++w) {
-                if (w < warp) before += scratch[w];
-                all += scratch[w];
-            }
-            if (first >= before && first < before + n) {
-                scratch[12] = b;
-                scratch[13] = first - before;
-            }
-            before_block += all;
-            if (first < before_block) break;
-        }
-        __syncthreads();
-        r.b = scratch[12];
-        r.x = scratch[13];
-    }
-    return r;
-}
-struct Segment {
-    int b, head;          // request, key head
-    int rows;             // block of query rows
-    int t0, n, nt;        // first tile, tiles here, tiles of the unit
-};
-// Runs over which a segment goes that begins in this CTA's and does not end in it: the tiles that are left lie in the runs that follow.
-__device__ __forceinline__ int pieces_of(const Run& run, const Segment& s, int heads) {
-    const int cta = blockIdx.x / heads, ctas = min(static_cast<int>(gridDim.x) / heads, run.total);
-    const int last_tile = run_begin(run.total, cta + 1, ctas) + (s.nt - s.n) - 1;                              // its place; it is in the run of the
-    const int last = static_cast<int>(((static_cast<int64_t>(last_tile) + 1) * ctas + run.total - 1) / run.total) - 1;      // last c with total * c / ctas <= last_tile
-    return last - cta + 1;
-}
 struct Walk {
     const Params& p;
     int b, x, left, nt;
@@ -338,7 +226,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     wait_for_previous();
     Run run{0, 0, 1, 0};
     if (p.join) __syncthreads();
-    else run = find_run(p, scratch);             // (its barriers publish the mbarriers too)
+    else run = find_run(p, scratch, [&](int b) { return length_of_unit(tiles_of(p, b)) * p.units; });      // (its barriers publish the mbarriers too)
     const PagedAttnArgs& a = p.a;
 
     if (warp >= W) {
@@ -863,99 +751,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 }
 
-// Joins the pieces of a segment that runs cut. blockIdx.x: the CTA in whose run the segment begins; kMergeWarps warps a row, which take its pieces in turn. Two
-// round trips to memory: the owner's word, then maxima, sums and the first pieces together. Units of many pieces get four warps a row (a request of 36392
-// keys and one key head has 296: 37 us in all with one warp, 18 with four), others one (96 requests of 2000 positions, 36 us in all, and 47 with four).
-template <int D, int ROWS, int kMergeWarps, int kMergeRows>
-__global__ void __launch_bounds__(32 * kMergeWarps * kMergeRows)
-paged_merge_kernel(const __grid_constant__ Params p, float out_scale) {
-    __shared__ float acc_s[kMergeRows][kMergeWarps][D], sum_s[kMergeRows][kMergeWarps];
-    let_next_start();
-    wait_for_previous();
-    const int4 own = p.owners[blockIdx.x];
-    if (own.x < 0) return;
-    const int lane = threadIdx.x & 31, sub = (threadIdx.x >> 5) % kMergeWarps, in = (threadIdx.x >> 5) / kMergeWarps, r = blockIdx.y * kMergeRows + in;
-    const int head = own.y / p.row_blocks, row0 = (own.y - head * p.row_blocks) * ROWS, pieces = own.z;
-    const int n_rows = min(p.a.n_step * p.a.group - row0, ROWS);
-    const bool works = r < n_rows;
-    constexpr int V = D / 32, AHEAD = 4;         // columns of a lane; pieces on their way at a time
-    auto row_of = [&](int i) -> int64_t { return (static_cast<int64_t>(blockIdx.x + i * p.heads) * 2 + (i == 0 ? 1 : 0)) * ROWS + r; };
-    auto load = [&](int i, float(&y)[V]) {
-        const float* from = p.part_o + row_of(i) * D + lane * V;
-        if (V == 4) {
-            const float4 z = *reinterpret_cast<const float4*>(from);
-            y[0] = z.x;
-            y[1] = z.y;
-            y[2 % V] = z.z;
-            y[3 % V] = z.w;
-        } else {
-            const float2 z = *reinterpret_cast<const float2*>(from);
-            y[0] = z.x;
-            y[1] = z.y;
-        }
-    };
-    const int mine = works && sub < pieces ? (pieces - sub + kMergeWarps - 1) / kMergeWarps : 0;      // this warp's: sub, sub + kMergeWarps, ...
-    float y[AHEAD][V];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-        if (u < mine) load(sub + u * kMergeWarps, y[u]);
-    float top = -INFINITY;
-    if (works)
-        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, p.part_ml[row_of(i)].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float use = top == -INFINITY ? 0.f : top;
-    float acc[V] = {}, sum = 0.f;
-    for (int i0 = 0; i0 < mine; i0 += 32) {
-        float w = 0.f, lw = 0.f;
-        if (i0 + lane < mine) {
-            const float2 ml = p.part_ml[row_of(sub + (i0 + lane) * kMergeWarps)];
-            w = exp2_fast(ml.x - use);
-            lw = w * ml.y;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) lw += __shfl_xor_sync(0xFFFFFFFFu, lw, o);
-        sum += lw;
-        const int n = min(32, mine - i0);
-        for (int i = 0; i < n; i += AHEAD) {
-            float z[AHEAD][V];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) z[u][v] = y[u][v];
-                if (i0 + i + AHEAD + u < mine) load(sub + (i0 + i + AHEAD + u) * kMergeWarps, y[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const float wi = __shfl_sync(0xFFFFFFFFu, w, i + u);
-                if (i + u < n) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[v] += wi * z[u][v];
-                }
-            }
-        }
-    }
-    if (kMergeWarps > 1) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) acc_s[in][sub][lane * V + v] = acc[v];
-        if (lane == 0) sum_s[in][sub] = sum;
-        __syncthreads();
-    }
-    if (sub != 0 || !works) return;
-    for (int w = 1; w < kMergeWarps; ++w) {
-        sum += sum_s[in][w];
-#pragma unroll
-        for (int v = 0; v < V; ++v) acc[v] += acc_s[in][w][lane * V + v];
-    }
-    const float over = sum == 0.f ? 0.f : out_scale / sum;
-    const int step = (row0 + r) / p.a.group, h = row0 + r - step * p.a.group;
-    const int64_t row = (static_cast<int64_t>(own.x) * p.a.n_step + step) * p.a.H + head * p.a.group + h;
-    __nv_bfloat16* to = p.a.out + row * D + lane * V;
-    if (V == 4) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(acc[0] * over, acc[1] * over), pack_bf16(acc[2 % V] * over, acc[3 % V] * over));
-    else *reinterpret_cast<uint32_t*>(to) = pack_bf16(acc[0] * over, acc[1] * over);
-    if (p.a.lse && lane == 0) p.a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-}
-
 int max_grid(int cta_rows) { return cta_rows <= 8 ? 3 * kPagedMaxSms : (cta_rows <= 32 ? 2 * kPagedMaxSms : kPagedMaxSms); }
 int rows_of_cta(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128))); }
 
@@ -1016,9 +811,9 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
 
 }  // namespace
 
-// owners, the pieces' maxima and sums, the pieces
+// owners, the pieces' maxima and sums, the pieces (of 256 rows for more than 128: paged_attn_rows.cu)
 size_t paged_attn_workspace_bytes(int n_step, int group, int d) {
-    const size_t rows = static_cast<size_t>(rows_of_cta(n_step * group)), grid = static_cast<size_t>(max_grid(static_cast<int>(rows)));
+    const size_t rows = n_step * group > 128 ? 256 : static_cast<size_t>(rows_of_cta(n_step * group)), grid = static_cast<size_t>(max_grid(static_cast<int>(rows)));
     return grid * 16 + grid * 2 * rows * (8 + static_cast<size_t>(d) * 4);
 }
 bool paged_attn_fits(const PagedAttnArgs& a) {
@@ -1034,6 +829,7 @@ bool paged_attn_fits(const PagedAttnArgs& a) {
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
                               int sm_count, cudaStream_t stream, int* launches) {
+    if (!a.c.fp8 && a.n_step * a.group > kRowsOfRegisters) return launch_paged_attn_rows(a, workspace, k_map, v_map, status, sm_count, stream, launches);
     Params p;
     p.a = a;
     const int rows = a.n_step * a.group, cta_rows = rows_of_cta(rows);
@@ -1050,8 +846,9 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUt
     (cta_rows == 8    ? run<D_, F_, 1, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
      : cta_rows == 16 ? run<D_, F_, 2, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
      : cta_rows == 32 ? run<D_, F_, 4, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
-     : cta_rows == 64 ? run<D_, F_, 4, 2>(k_map, v_map, p, sm_count, stream, launches)                      \
-                      : run<D_, F_, 4, 4>(k_map, v_map, p, sm_count, stream, launches))
+                      : run<D_, F_, 4, 2>(k_map, v_map, p, sm_count, stream, launches))
+    if (cta_rows == 128)
+        return a.c.d == 128 ? run<128, true, 4, 4>(k_map, v_map, p, sm_count, stream, launches) : run<64, true, 4, 4>(k_map, v_map, p, sm_count, stream, launches);
     if (a.c.d == 128) return a.c.fp8 ? IDXC_RUN(128, true) : IDXC_RUN(128, false);
     return a.c.fp8 ? IDXC_RUN(64, true) : IDXC_RUN(64, false);
 #undef IDXC_RUN

@@ -69,12 +69,12 @@ def tables(lens, P, g, spare=5, extra=2):
     return table, n_pages
 
 
-def check(out, lse, want, eight, keys, what="", q_size=0.0):
+def check(out, lse, want, eight, keys, what="", q_size=0.0, under=0.0):
     """out [R, d] bf16, lse [R] against the oracle's (out, lse, spread, reach). Scores: products are exact in fp32 and summed in d / 16 <= 8 matrix
     steps of relative error at most 2^-21 each, then scaled: within 2^-17 of reach. In 8 bits q is f16 after a power of two that
     brings its largest element to [1, 2): off by at most 2^-25 of that element (q_size: scale * max|q| * max_s sum|k_s|), and two more
     scalings, 2^-23 of reach. Sums of probabilities and of values: at most 2^-23 a term. Probabilities are rounded to bf16 (half a step 2^-8) or f16 (2^-11),
-    exp2 is off by 2^-21. The output is rounded to bf16, half a step of which is 2^-8."""
+    exp2 is off by 2^-21. The output is rounded to bf16, half a step of which is 2^-8. under: what f16's smallest steps add in 8 bits (underflow())."""
     o_out, o_lse, spread, reach = want
     out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
     empty = np.isneginf(o_lse)
@@ -83,7 +83,7 @@ def check(out, lse, want, eight, keys, what="", q_size=0.0):
     e = (2.0 ** -17 + 2.0 ** -23) * reach + (2.0 ** -24 * q_size if eight else 0.0)
     total = keys * 2.0 ** -23 + 2.0 ** -20
     rounding = 2.0 ** -11 if eight else 2.0 ** -8
-    bound = spread * (rounding + 2 * e[:, None] + 2 * total) * (1 + 2.0 ** -7) + np.abs(o_out) * 2.0 ** -8
+    bound = spread * (rounding + 2 * e[:, None] + 2 * total) * (1 + 2.0 ** -7) + np.abs(o_out) * 2.0 ** -8 + under
     err = np.abs(out - o_out)
     assert np.all(err <= bound), f"{what}: out off by {(err / np.maximum(bound, 1e-300)).max():.2f} bounds"
     ok = ~empty
@@ -91,8 +91,17 @@ def check(out, lse, want, eight, keys, what="", q_size=0.0):
     assert np.all(np.abs(lse[ok] - o_lse[ok]) <= l_bound), f"{what}: lse off by {(np.abs(lse[ok] - o_lse[ok]) / l_bound).max():.2f} bounds"
 
 
-def oracle_attention(cache_values, q, table, lens, P, H_kv, scale, n_pages, pages=None, only=None):
-    """For every (request, key head) of `only` (all): (b, head, rows [n_step, group], oracle.attention's results, keys, q_size)."""
+def underflow(rows, k, codes, v_scale, scale, mask, lse):
+    """[R, d]. In 8 bits probability times scale times 2^6 is an f16, below 2^-14 off by up to 2^-25 whatever its size: 2^-31 |code| a key, over the sum of
+    probabilities 2^(x - m). The reference m is at most the largest x + log2(v_scale), rounded up, so 2^m over that sum is at most twice the
+    largest softmax * v_scale: in all 2^-30 max_s(softmax_s v_scale_s) sum_s |code_s|."""
+    x = np.where(mask, scale * (rows @ k.T), -np.inf)
+    w = np.exp(x - np.where(np.isneginf(lse), 0.0, lse)[:, None]) * v_scale
+    return 2.0 ** -30 * w.max(axis=1, initial=0.0)[:, None] * (mask.astype(np.float64) @ np.abs(codes))
+
+
+def oracle_attention(cache_values, q, table, lens, P, H_kv, scale, n_pages, pages=None, only=None, v_scale=None):
+    """For every (request, key head) of `only` (all): (b, head, rows [n_step, group], oracle.attention's results, keys, q_size, underflow in 8 bits)."""
     k_all, v_all = cache_values
     B, n_step, H, d = q.shape
     group = H // H_kv
@@ -118,13 +127,19 @@ def oracle_attention(cache_values, q, table, lens, P, H_kv, scale, n_pages, page
             mask = inside[None, :] & (pos[None, :] < sees[:, None])
             used = mask.any(axis=0)
             size = abs(scale) * np.abs(rows).max() * np.abs(k[used]).sum(axis=1).max() if used.any() else 0.0
-            yield b, head, oracle.attention(rows, k, v, scale, mask), pos.size, size
+            want = oracle.attention(rows, k, v, scale, mask)
+            under = 0.0
+            if v_scale is not None and used.any():
+                s = v_scale[at, head, pos % P][used]
+                under = underflow(rows, k[used], v[used] / s[:, None], s, scale, mask[:, used], want[1])
+            yield b, head, want, pos.size, size, under
 
 
 def check_call(cache, q, table, lens, scale, out, lse, pages=None, only=None, what=""):
     n_pages, P, H_kv, d = cache.shape
     B, n_step, H, _ = q.shape
     group = H // H_kv
-    for b, head, want, keys, size in oracle_attention(cache.values(), q, table, lens, P, H_kv, scale, n_pages, pages, only):
+    v_scale = None if cache.v_scale is None else cache.v_scale.double().cpu().numpy()
+    for b, head, want, keys, size, under in oracle_attention(cache.values(), q, table, lens, P, H_kv, scale, n_pages, pages, only, v_scale):
         part = slice(head * group, (head + 1) * group)
-        check(out[b, :, part].reshape(n_step * group, d), lse[b, :, part].reshape(-1), want, cache.scale is not None, keys, f"{what} request {b} head {head}", size)
+        check(out[b, :, part].reshape(n_step * group, d), lse[b, :, part].reshape(-1), want, cache.scale is not None, keys, f"{what} request {b} head {head}", size, under)
