@@ -232,7 +232,7 @@ bool paged_attn_fits(const PagedAttnArgs& a);           // the tile count of the
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
                               int sm_count, cudaStream_t stream, int* launches);
 
-// paged_attn_rows.cu: the same for many rows of a key head, bf16; launch_paged_attn goes there.
+// paged_attn_rows.cu: the same for many rows of a key head; launch_paged_attn goes there.
 cudaError_t launch_paged_attn_rows(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
                                    int sm_count, cudaStream_t stream, int* launches);
 

@@ -2,7 +2,7 @@
 //     x[s] = scale <q, k_s> over the visible keys s,   out = sum_s softmax(x)[s] v_s,   lse = log sum_s exp(x[s])
 // over all pages of a request, or over the pages that a selection names for each (request, key head).
 //
-// A unit is a (request, key head, block of rows). Few units of few tiles: a cluster of up to 8 CTAs takes a unit and joins its parts over distributed shared
+// A unit is a (request, key head). Few units of few tiles: a cluster of up to 8 CTAs takes a unit and joins its parts over distributed shared
 // memory, one launch in all.
 //
 // Measured (graph replays, one B200): 32 requests of 4K to 32K bf16 keys, 64 heads over 8: 352 us, 6.9 TB/s of what has to be read; 8 requests of 131072
@@ -17,8 +17,8 @@
 // padding, and 64 keys in 8 bits took 1740 instructions instead of 1390. tcgen05's M = 64 or 128 with rows as N would fit too, but its scores would cross
 // tensor memory twice a tile, a latency that several resident CTAs would have to hide.) P^T comes out of the scores' registers by an 8 x 8 transposition.
 //
-// (More than kRowsOfRegisters bf16 rows: paged_attn_rows.cu.) Up to 32 rows: 4 warps, each 16 or 32 keys of a tile with its own running reference and sum; 2 or 3 CTAs an SM hide each other's segment ends. More rows:
-// 8 warps, of which 2 or 4 share the keys and take 32 rows each. The warps' parts meet once at a segment's end, in shared memory. The tiles of all
+// Up to 32 rows (more: paged_attn_rows.cu): 4 warps, each 16 or 32 keys of a tile with its own running reference and sum; 2 or 3 CTAs an SM hide each
+// other's segment ends. The warps' parts meet once at a segment's end, in shared memory. The tiles of all
 // units, end to end, are cut into runs of equal cost, a run a CTA, which finds it from the lengths on the device;
 // segments cut by a run's end go to the workspace in fp32 and through a merge kernel. All sums have an order fixed by the sizes, so results
 // repeat bit for bit.
@@ -38,9 +38,9 @@ using namespace paged;
 namespace {
 
 constexpr int kProducerRegs = 40;
-// bf16 rows of a key head up to which this file's kernel is taken. (8 x 32768 keys, 8 key heads, d = 128 / 64: 64 rows 240 / 181 us, and 242 / 212 with
-// paged_attn_rows.cu, which takes 128 alike; 128 rows 477 / 347 here.)
-constexpr int kRowsOfRegisters = 64;
+// Rows of a key head up to which this kernel is the faster one. (8 x 32768 keys, 8 key heads, d = 128 / 64. bf16: 32 rows 173 / 99 us here, 64 rows, with 8 warps
+// of which two shared keys, 240 / 183, and 186 / 134 by paged_attn_rows.cu. 8 bits: 32 rows 159 / 111 here and 271 / 207 there, 64 rows 305 / 227 and 273 / 210.)
+constexpr int kRowsHere = 32;
 // Tiles of a CTA up to which few units are given to clusters. (bf16, 8 key heads, d = 128, one request of 777 / 2000 / 4000 / 8000 keys: 9.3 / 11.1 / 12.7 /
 // 13.9 us by runs and a merge, 6.1 / 7.5 / 10.4 / 16.4 by clusters, with 2, 4, 8 and 16 tiles a CTA.)
 constexpr int kJoinTiles = 8;
@@ -53,42 +53,19 @@ constexpr int kJoinSlack = 5;
 // of 16 heads and 4 tokens: 33.5 us with 8, 37.4 with 0). f16 of 8-bit rows is exact enough either way.
 template <bool FP8, int NR>
 constexpr float kSlack = FP8 || NR == 4 ? 8.f : 0.f;
-__device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float2 ld_shared_f32x2(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 ld_shared_f32x4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint32_t ld_shared_u32(uint32_t addr) {
     uint32_t v;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ void st_shared_f32(uint32_t addr, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory"); }
 // An 8 x 8 matrix of 16-bit elements, lane 4 g + j holding elements 2 j, + 1 of row g, transposed.
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-__device__ __forceinline__ void st_shared_f32x2(uint32_t addr, float x, float y) {
-    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y) : "memory");
-}
 __device__ __forceinline__ void st_shared_v2(uint32_t addr, uint32_t x, uint32_t y) {
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
-}
-// log2 of a positive scale, rounded up, as a number between -60 and 60.
-__device__ __forceinline__ float log2_above(float scale) {
-    return static_cast<float>(min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 126, -60), 60));
 }
 // The two barriers of a cluster that joins its parts, for the warps that have no share in that: parts are there; parts have been read.
 __device__ __forceinline__ void leave_cluster() {
@@ -112,10 +89,9 @@ struct Walk {
         if (p.join) {                            // this CTA's share of its cluster's unit, which may be none; once
             if (left == 0) return false;
             left = 0;
-            const int per_request = p.a.c.H_kv * p.row_blocks, unit = blockIdx.x / p.join, rank = blockIdx.x % p.join;
-            s.b = unit / per_request;
-            s.head = (unit - s.b * per_request) / p.row_blocks;
-            s.rows = unit - s.b * per_request - s.head * p.row_blocks;
+            const int unit = blockIdx.x / p.join, rank = blockIdx.x % p.join;
+            s.b = unit / p.a.c.H_kv;
+            s.head = unit - s.b * p.a.c.H_kv;
             s.nt = tiles_of(p, s.b);
             s.t0 = static_cast<int>(static_cast<unsigned>(s.nt) * rank / p.join);
             s.n = static_cast<int>(static_cast<unsigned>(s.nt) * (rank + 1) / p.join) - s.t0;
@@ -130,9 +106,7 @@ struct Walk {
             const int len = nt + kSegmentTiles;
             s.b = b;
             const int unit = x / len, from = x - unit * len, n = min(len - from, left);
-            s.head = unit / p.row_blocks;
-            s.rows = unit - s.head * p.row_blocks;
-            s.head = s.head * p.heads + static_cast<int>(blockIdx.x) % p.heads;
+            s.head = unit * p.heads + static_cast<int>(blockIdx.x) % p.heads;
             x += n;
             left -= n;
             s.t0 = max(from - kSegmentTiles, 0);
@@ -145,32 +119,31 @@ struct Walk {
 };
 
 // ---------------------------------------------------------------- shared memory
-// NR blocks of 8 query rows a warp, RG warps side by side over the rows.
+// NR blocks of 8 query rows.
 // With 32 rows a warp the output alone is 128 registers of d = 128: registers are then handed out unevenly, by warpgroups (three idle warps fill
-// up the producer's): the launch's 128 (168) a thread, of which the producer's warpgroup keeps 40.
-template <int D, bool FP8, int NR, int RG>
+// up the producer's): the launch's 128 a thread, of which the producer's warpgroup keeps 40.
+template <int D, bool FP8, int NR>
 struct Layout {
-    static constexpr int kWarps = RG == 1 ? 4 : 8;                     // consumers
+    static constexpr int kWarps = 4;                                   // consumers; they share every tile
     static constexpr bool kUneven = NR * D == 512;
     static constexpr int kThreads = (kWarps + (kUneven ? 4 : 1)) * 32;
-    static constexpr int kCtas = RG > 1 ? 1 : (NR == 1 && FP8 ? 3 : 2);        // of an SM
-    static constexpr int kConsumerRegs = RG == 1 ? 216 : 232;
-    static_assert(128 * kProducerRegs + kWarps * 32 * kConsumerRegs <= (kWarps + 4) * 32 * (RG == 1 ? 128 : 168), "shares of the launch's registers");
+    static constexpr int kCtas = NR == 1 && FP8 ? 3 : 2;               // of an SM
+    static constexpr int kConsumerRegs = 216;
+    static_assert(128 * kProducerRegs + kWarps * 32 * kConsumerRegs <= (kWarps + 4) * 32 * 128, "shares of the launch's registers");
     // Keys of a tile: 18 to 36 KB, so that a tile's fixed costs (barriers, votes, the producer's turn) stay small beside its bytes, as far as a ring
     // of three leaves room. (One request length of 32768 and 8 key heads, 8 rows: d = 64 in bf16 108 us with 64 keys and three CTAs, 91 with these.)
-    static constexpr int kTile = (D == 64 && (FP8 || NR < 4 || RG > 1)) || (FP8 && NR == 2) ? 128 : 64;
-    static constexpr int kRows = 8 * NR * RG;                          // query rows of a CTA
-    static constexpr int kParts = kWarps / RG;                         // warps that share a row; they share every tile
-    static constexpr int kKeys = kTile / kParts;                       // keys of a tile that a warp takes
+    static constexpr int kTile = (D == 64 && (FP8 || NR < 4)) || (FP8 && NR == 2) ? 128 : 64;
+    static constexpr int kRows = 8 * NR;                               // query rows of a CTA
+    static constexpr int kKeys = kTile / kWarps;                       // keys of a tile that a warp takes
     static constexpr int kTileBytes = kTile * D * (FP8 ? 1 : 2);
     static constexpr int kStageBytes = (2 * kTileBytes + (FP8 ? 8 * kTile : 0) + 1023) / 1024 * 1024;      // K, V, scales of K and of V: swizzled rows
                                                                                                            // begin on multiples of 1024 bytes
     static constexpr int kSlice = NR == 1 ? 64 : (NR == 2 ? 32 : 16);  // columns of the output that go through shared memory at a time
     static constexpr int kPitch = kSlice + 4;                          // floats between rows there: no bank conflicts
     static constexpr int kQBytes = kRows * D * 2;
-    static constexpr int kRedBytes = kParts * kRows * kPitch * 4;
+    static constexpr int kRedBytes = kWarps * kRows * kPitch * 4;
     static constexpr int kShared = kQBytes > kRedBytes ? kQBytes : kRedBytes;  // q, and the output's slices when q is done with
-    static constexpr int kMlBytes = kParts * kRows * 8;
+    static constexpr int kMlBytes = kWarps * kRows * 8;
     static constexpr int kSmall = 1024 + 1536;                         // alignment of the stages; barriers, positions, a number per row
     static constexpr int kLimit = (233472 - kCtas * (1024 + 128)) / kCtas;     // an SM's, without what the system and static arrays take
     static constexpr int kFit = (kLimit - kSmall - kShared - kMlBytes) / kStageBytes;
@@ -191,10 +164,10 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
     return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
 }
 
-template <int D, bool FP8, int NR, int RG>
-__global__ void __launch_bounds__((Layout<D, FP8, NR, RG>::kThreads), (Layout<D, FP8, NR, RG>::kCtas))
+template <int D, bool FP8, int NR>
+__global__ void __launch_bounds__((Layout<D, FP8, NR>::kThreads), (Layout<D, FP8, NR>::kCtas))
 paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ Params p) {
-    using L = Layout<D, FP8, NR, RG>;
+    using L = Layout<D, FP8, NR>;
     constexpr int ROWB = D * (FP8 ? 1 : 2);      // bytes of a cached row
     constexpr int NS = L::kStages, W = L::kWarps;
     extern __shared__ uint8_t raw[];
@@ -208,7 +181,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const uint32_t pos_s = bars + NS * 16;       // [NS][8] position of the first key of each piece, -1: none
     const uint32_t row_s = pos_s + NS * 32;      // [rows] power of two taken out of a row of q; at the end what the row is multiplied by
     const uint32_t flag_s = row_s + L::kRows * 4;
-    __shared__ int scratch[16];
+    __shared__ int scratch[18];
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(raw + (flag_s - base));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -326,9 +299,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
     // ---------------------------------------------------------------- consumers
     if (L::kUneven) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kConsumerRegs));
-    const int rg = warp % RG, part = warp / RG;
     const int g = lane >> 2, j = lane & 3;       // of a fragment: key (or output column) g and g + 8, query rows 2 j and 2 j + 1
-    const int warp_row = rg * NR * 8;            // first row of the CTA's that is this warp's
     const int rows_all = a.n_step * a.group;
     constexpr int NT = D / 16;                   // output fragments of 16 columns
     constexpr int KB = NR <= 2 && L::kKeys >= 32 ? 2 : 1;      // blocks of 16 keys in a step
@@ -338,13 +309,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     constexpr int Q_THREADS = L::kRows * (D / 8) < W * 32 ? L::kRows * (D / 8) : W * 32;
 
     auto load_q = [&](const Segment& s, uint4(&q)[QV]) {              // zeros behind the last row
-        const int head = s.head, row0 = s.rows * L::kRows;
+        const int head = s.head;
 #pragma unroll
         for (int u = 0; u < QV; ++u) {
             const int i = threadIdx.x + u * W * 32, r = i / (D / 8), c = i - r * (D / 8);
             q[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (threadIdx.x < Q_THREADS && row0 + r < rows_all) {
-                const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
+            if (threadIdx.x < Q_THREADS && r < rows_all) {
+                const int step = r / a.group, h = r - step * a.group;
                 q[u] = reinterpret_cast<const uint4*>(a.q + (static_cast<int64_t>(s.b) * a.n_step + step) * a.q_stride +
                                                       static_cast<int64_t>(head * a.group + h) * D)[c];
             }
@@ -362,8 +333,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         s = after;
         if (!kQRegs) load_q(s, q_next);
         const int len = length_of(a, s.b);
-        const int head = s.head, row0 = s.rows * L::kRows;
-        const int n_rows = min(rows_all - row0, L::kRows);
+        const int head = s.head, n_rows = rows_all;
         const bool whole = s.t0 == 0 && s.n == s.nt && p.join <= 1;
         if (threadIdx.x < Q_THREADS) {
 #pragma unroll
@@ -402,7 +372,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
         // B fragments of q for two steps of 16 columns and a block of 8 rows: matrices of 8 rows x 8 columns side by side.
         auto q_frag = [&](int nr, int c4, uint32_t(&f)[4]) {
-            const int r = warp_row + nr * 8 + (lane & 7), c = c4 * 4 + (lane >> 3);
+            const int r = nr * 8 + (lane & 7), c = c4 * 4 + (lane >> 3);
             ldmatrix_x4(q_s + r * (D * 2) + ((c ^ (r & 7)) << 4), f);
         };
         uint32_t qf[kQRegs ? NR : 1][kQRegs ? D / 32 : 1][4];
@@ -419,8 +389,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int r = warp_row + nr * 8 + 2 * j + e;
-                sees[nr][e] = len - (a.n_step - 1 - min((row0 + r) / a.group, a.n_step - 1));
+                const int r = nr * 8 + 2 * j + e;
+                sees[nr][e] = len - (a.n_step - 1 - min(r / a.group, a.n_step - 1));
                 row_scale[nr][e] = FP8 ? p.scale_log2 * ld_shared_f32(row_s + r * 4) : p.scale_log2;
                 m[nr][e] = -INFINITY;
                 l[nr][e] = 0.f;
@@ -451,7 +421,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 int first = INT32_MAX, last = 0;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
-                    key0[kb] = part * L::kKeys + (step * KB + kb) * 16;
+                    key0[kb] = warp * L::kKeys + (step * KB + kb) * 16;
                     const int pc = key0[kb] >> p.piece_log2;
                     at[kb] = static_cast<int>(ld_shared_u32(pos_s + st * 32 + pc * 4));
                     at[kb] = at[kb] < 0 ? INT32_MAX / 2 : at[kb] + (key0[kb] - (pc << p.piece_log2));
@@ -461,7 +431,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 if (L::kTile > 64 && first >= len) continue;           // none of them is there
                 const bool clean = last <= sees_least;
                 if (!clean) {
-                    // Rows of V that no token sees meet probability 0 and may hold anything: they are cleared. (Warps that share keys clear them alike.)
+                    // Rows of V that no token sees meet probability 0 and may hold anything: they are cleared.
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb)
                         if (at[kb] + (lane & 15) >= len) {
@@ -623,21 +593,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nr][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nr][e], d);
-                if (g == 0) st_shared_f32x2(ml_s + (part * L::kRows + warp_row + nr * 8 + 2 * j + e) * 8, m[nr][e], l[nr][e]);
+                if (g == 0) st_shared_f32x2(ml_s + (warp * L::kRows + nr * 8 + 2 * j + e) * 8, m[nr][e], l[nr][e]);
             }
         consumers_sync<W>();
         const int64_t piece_row = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * L::kRows;
         for (int r = threadIdx.x; r < n_rows; r += W * 32) {
-            float2 v[L::kParts];
+            float2 v[W];
             float best = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < L::kParts; ++w) {
+            for (int w = 0; w < W; ++w) {
                 v[w] = ld_shared_f32x2(ml_s + (w * L::kRows + r) * 8);
                 best = fmaxf(best, v[w].x);
             }
             const float use = best == -INFINITY ? 0.f : best;
 #pragma unroll
-            for (int w = 0; w < L::kParts; ++w) {
+            for (int w = 0; w < W; ++w) {
                 const float f = exp2_fast(v[w].x - use);
                 sum += v[w].y * f;
                 st_shared_f32(ml_s + (w * L::kRows + r) * 8, f);
@@ -647,7 +617,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 if (p.join) st_shared_f32x2(join_s + L::kRows * D * 4 + r * 8, best, sum);
                 else p.part_ml[piece_row + r] = make_float2(best, sum);
             } else if (a.lse) {
-                const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
+                const int step = r / a.group, h = r - step * a.group;
                 a.lse[(static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h] =
                     sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
             }
@@ -657,14 +627,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) f[nr][e] = ld_shared_f32(ml_s + (part * L::kRows + warp_row + nr * 8 + 2 * j + e) * 8);
+            for (int e = 0; e < 2; ++e) f[nr][e] = ld_shared_f32(ml_s + (warp * L::kRows + nr * 8 + 2 * j + e) * 8);
 #pragma unroll
         for (int c0 = 0; c0 < D; c0 += L::kSlice) {
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t row = red_s + ((part * L::kRows + warp_row + nr * 8 + 2 * j + e) * L::kPitch) * 4;
+                    const uint32_t row = red_s + ((warp * L::kRows + nr * 8 + 2 * j + e) * L::kPitch) * 4;
 #pragma unroll
                     for (int n0 = 0; n0 < L::kSlice / 16; ++n0) {
                         const float lo = o[nr][c0 / 16 + n0][e] * f[nr][e], hi = o[nr][c0 / 16 + n0][2 + e] * f[nr][e];
@@ -681,7 +651,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 const int r = i / (L::kSlice / 4), c = i % (L::kSlice / 4) * 4;
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < L::kParts; ++w) {
+                for (int w = 0; w < W; ++w) {
                     const float4 z = ld_shared_f32x4(red_s + ((w * L::kRows + r) * L::kPitch + c) * 4);
                     v.x += z.x;
                     v.y += z.y;
@@ -693,7 +663,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     else *reinterpret_cast<float4*>(p.part_o + (piece_row + r) * D + c0 + c) = v;
                 } else {
                     const float over = ld_shared_f32(row_s + r * 4);
-                    const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
+                    const int step = r / a.group, h = r - step * a.group;
                     const int64_t to = ((static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h) * D + c0 + c;
                     *reinterpret_cast<uint2*>(a.out + to) = make_uint2(pack_bf16(v.x * over, v.y * over), pack_bf16(v.z * over, v.w * over));
                 }
@@ -727,7 +697,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         y += of[k].y * w;
                     }
                 const float over = sum == 0.f ? 0.f : (FP8 ? 1.f / kF16Head : 1.f) / sum;
-                const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
+                const int step = r / a.group, h = r - step * a.group;
                 const int64_t row = (static_cast<int64_t>(s.b) * a.n_step + step) * a.H + head * a.group + h;
                 *reinterpret_cast<uint32_t*>(a.out + row * D + c) = pack_bf16(x * over, y * over);
                 if (a.lse && c == 0) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
@@ -735,7 +705,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             cluster_sync();
             return;
         }
-        if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.head * p.row_blocks + s.rows, pieces_of(run, s, p.heads), 0);
+        if (s.t0 == 0 && !whole) owner = make_int4(s.b, s.head, pieces_of(run, s, p.heads), 0);
     }
     if (p.join) return;
     if (threadIdx.x == 0) p.owners[blockIdx.x] = owner;
@@ -752,23 +722,24 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 }
 
 int max_grid(int cta_rows) { return cta_rows <= 8 ? 3 * kPagedMaxSms : (cta_rows <= 32 ? 2 * kPagedMaxSms : kPagedMaxSms); }
-int rows_of_cta(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128))); }
+// of a block of rows: here up to 32, in paged_attn_rows.cu 128 or 256
+int rows_of_cta(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 128 ? 128 : 256))); }
 
-template <int D, bool FP8, int NR, int RG>
+template <int D, bool FP8, int NR>
 cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, int sm_count, cudaStream_t stream, int* launches) {
-    using L = Layout<D, FP8, NR, RG>;
+    using L = Layout<D, FP8, NR>;
     // Heads in step: all of up to 8, else the largest divisor of their number up to 8.
     p.heads = p.a.c.H_kv < 8 ? p.a.c.H_kv : 8;
     while (p.a.c.H_kv % p.heads) --p.heads;
-    p.units = p.a.c.H_kv / p.heads * p.row_blocks;
+    p.units = p.a.c.H_kv / p.heads;
     p.tile_log2 = L::kTile == 64 ? 6 : 7;
-    auto kernel = paged_attn_kernel<D, FP8, NR, RG>;
+    auto kernel = paged_attn_kernel<D, FP8, NR>;
     cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes);
     if (e != cudaSuccess) return e;
     // Few units of few tiles: a unit a cluster, cut among as many CTAs (8 at most) as all have room at once, which join their parts over distributed
     // shared memory. One launch, and no scan over the requests; but every unit is cut alike, whatever its length, so only where that is at most
     // kJoinTiles tiles a CTA, or where the units are alike (selections) and a CTA has hardly more than an equal share of all tiles.
-    const int64_t units = static_cast<int64_t>(p.a.B) * p.a.c.H_kv * p.row_blocks;
+    const int64_t units = static_cast<int64_t>(p.a.B) * p.a.c.H_kv;
     int64_t keys = p.a.max_len;
     if (p.a.pages) {
         const int64_t pages = (keys + p.a.c.page_size - 1) / p.a.c.page_size;
@@ -811,9 +782,9 @@ cudaError_t run(const CUtensorMap& k_map, const CUtensorMap& v_map, Params& p, i
 
 }  // namespace
 
-// owners, the pieces' maxima and sums, the pieces (of 256 rows for more than 128: paged_attn_rows.cu)
+// owners, the pieces' maxima and sums, the pieces
 size_t paged_attn_workspace_bytes(int n_step, int group, int d) {
-    const size_t rows = n_step * group > 128 ? 256 : static_cast<size_t>(rows_of_cta(n_step * group)), grid = static_cast<size_t>(max_grid(static_cast<int>(rows)));
+    const size_t rows = static_cast<size_t>(rows_of_cta(n_step * group)), grid = static_cast<size_t>(max_grid(static_cast<int>(rows)));
     return grid * 16 + grid * 2 * rows * (8 + static_cast<size_t>(d) * 4);
 }
 bool paged_attn_fits(const PagedAttnArgs& a) {
@@ -829,11 +800,11 @@ bool paged_attn_fits(const PagedAttnArgs& a) {
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUtensorMap& k_map, const CUtensorMap& v_map, unsigned int* status,
                               int sm_count, cudaStream_t stream, int* launches) {
-    if (!a.c.fp8 && a.n_step * a.group > kRowsOfRegisters) return launch_paged_attn_rows(a, workspace, k_map, v_map, status, sm_count, stream, launches);
-    Params p;
+    if (a.n_step * a.group > kRowsHere) return launch_paged_attn_rows(a, workspace, k_map, v_map, status, sm_count, stream, launches);
+    Params p{};
     p.a = a;
-    const int rows = a.n_step * a.group, cta_rows = rows_of_cta(rows);
-    p.row_blocks = (rows + cta_rows - 1) / cta_rows;
+    const int cta_rows = rows_of_cta(a.n_step * a.group);
+    p.row_blocks = 1;
     p.piece_log2 = a.c.page_size % 64 == 0 ? 6 : (a.c.page_size % 32 == 0 ? 5 : 4);
     p.scale_log2 = a.scale * 1.4426950408889634f;
     uint8_t* w = static_cast<uint8_t*>(workspace);
@@ -842,13 +813,10 @@ cudaError_t launch_paged_attn(const PagedAttnArgs& a, void* workspace, const CUt
     p.part_ml = reinterpret_cast<float2*>(w + grid * 16);
     p.part_o = reinterpret_cast<float*>(w + grid * 16 + grid * 2 * cta_rows * 8);
     p.status = status;
-#define IDXC_RUN(D_, F_)                                                                                   \
-    (cta_rows == 8    ? run<D_, F_, 1, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
-     : cta_rows == 16 ? run<D_, F_, 2, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
-     : cta_rows == 32 ? run<D_, F_, 4, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
-                      : run<D_, F_, 4, 2>(k_map, v_map, p, sm_count, stream, launches))
-    if (cta_rows == 128)
-        return a.c.d == 128 ? run<128, true, 4, 4>(k_map, v_map, p, sm_count, stream, launches) : run<64, true, 4, 4>(k_map, v_map, p, sm_count, stream, launches);
+#define IDXC_RUN(D_, F_)                                                                                \
+    (cta_rows == 8    ? run<D_, F_, 1>(k_map, v_map, p, sm_count, stream, launches)                      \
+     : cta_rows == 16 ? run<D_, F_, 2>(k_map, v_map, p, sm_count, stream, launches)                      \
+                      : run<D_, F_, 4>(k_map, v_map, p, sm_count, stream, launches))
     if (a.c.d == 128) return a.c.fp8 ? IDXC_RUN(128, true) : IDXC_RUN(128, false);
     return a.c.fp8 ? IDXC_RUN(64, true) : IDXC_RUN(64, false);
 #undef IDXC_RUN

@@ -15,8 +15,8 @@ constexpr float kF16Head = 64.f;                // probabilities times scale rea
 struct Params {
     PagedAttnArgs a;
     int heads;                   // key heads that as many neighbouring CTAs walk through in step
-    int units;                   // (heads of a CTA, blocks of query rows) of a request
-    int row_blocks;              // blocks of a CTA's query rows of a (request, key head)
+    int units;                   // of a request for a CTA: key heads / heads
+    int row_blocks;              // blocks of query rows of a (request, key head)
     int tile_log2;               // keys of a tile
     int ways;                    // blocks of 128 rows that share a CTA's tiles (paged_attn_rows.cu)
     int join;                    // 0: runs over all units; else a unit is a cluster's of so many CTAs, which join their parts themselves
@@ -24,7 +24,8 @@ struct Params {
     float scale_log2;            // scale * log2(e)
     float* part_o;               // [grid][2][MAXR][D]
     float2* part_ml;             // [grid][2][MAXR] (maximum in log2 units, sum)
-    int4* owners;                // [grid] the segment that begins in a CTA's run and does not end in it: (request, key head * row_blocks + block of rows, pieces); -1: none
+    int4* owners;                // [grid] the segment that begins in a CTA's run and does not end in it: (request, key head * row_blocks + block of rows,
+                                 // pieces); -1: none
     unsigned int* status;
 };
 
@@ -40,6 +41,29 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 ld_shared_f32x2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_shared_f32x4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_shared_f32(uint32_t addr, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory"); }
+__device__ __forceinline__ void st_shared_f32x2(uint32_t addr, float x, float y) {
+    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y) : "memory");
+}
+// log2 of a positive scale, rounded up, as a number between -60 and 60.
+__device__ __forceinline__ float log2_above(float scale) {
+    return static_cast<float>(min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 126, -60), 60));
 }
 // Keys of request b that the call knows of.
 __device__ __forceinline__ int length_of(const PagedAttnArgs& a, int b) { return min(max(a.lens[b], 0), static_cast<int>(a.max_len)); }
@@ -67,9 +91,9 @@ __device__ __forceinline__ int run_begin(int total, int cta, int grid) {
     const unsigned each = static_cast<unsigned>(total) / n, more = total - each * n;
     return static_cast<int>(each * cta + more * cta / n);
 }
-// length(b): of all of request b's units. (At most 12 warps.)
+// length(b): of all of request b's units. (At most 16 warps.)
 template <class F>
-__device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared, 16 words */, const F& length) {
+__device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared, 18 words */, const F& length) {
     const int cta = blockIdx.x / p.heads, ctas = gridDim.x / p.heads;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_thr = blockDim.x, n_warps = n_thr >> 5;
     int sum = 0, mine = 0;
@@ -105,15 +129,15 @@ __device__ __forceinline__ Run find_run(const Params& p, int* scratch /* shared,
                 all += scratch[w];
             }
             if (first >= before && first < before + n) {
-                scratch[12] = b;
-                scratch[13] = first - before;
+                scratch[16] = b;
+                scratch[17] = first - before;
             }
             before_block += all;
             if (first < before_block) break;
         }
         __syncthreads();
-        r.b = scratch[12];
-        r.x = scratch[13];
+        r.b = scratch[16];
+        r.x = scratch[17];
     }
     return r;
 }
