@@ -8,6 +8,7 @@ from oracle import paged as oracle
 from paper_2603_12201_b200 import binding as idxc
 from tests.paged_util import DEV, check_call, int32
 from tests.test_gpu_paged_attention import run, setup
+from tests.test_gpu_paged_guard_bands import test_attention as guarded_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -147,3 +148,41 @@ def test_captured_and_replayed_over_other_lengths():
         torch.cuda.synchronize()
         idxc.poll_device_status()
         check_call(cache, q, table, lens, 0.1, out, lse)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("lens,P,H,H_kv,d,n_step,k", [([1], 16, 33, 1, 64, 1, 0), ([700, 0, 65, 3], 16, 10, 2, 128, 40, 0), ([3000], 48, 64, 1, 64, 1, 0),
+                                                      ([257, 31], 64, 26, 2, 128, 11, 0), ([63] * 40, 16, 16, 8, 64, 9, 0), ([2000, 90, 0], 16, 16, 2, 128, 5, 7)])
+def test_nothing_is_written_beside_the_outputs(lens, P, H, H_kv, d, n_step, k, eight):
+    guarded_attention(lens, P, H, H_kv, d, n_step, k, eight)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("n_step", [6, 40])
+def test_selections_that_name_nothing_and_no_lse(eight, n_step):
+    lens, P = [500, 0, 77], 32
+    cache, q, table, n, _ = setup(lens, P, 20, 2, 64, eight, n_step)
+    sel = torch.full((3, 2, 5), -1, dtype=torch.int32)
+    sel[2, 1] = torch.tensor([2, 1, 0, 9, 2 ** 31 - 1], dtype=torch.int32)
+    out, lse = run(cache, q, table, n, 500, 0.1, pages=sel.to(DEV))
+    check_call(cache, q, table, lens, 0.1, out, lse, pages=sel)
+    assert torch.isneginf(lse[:2]).all() and not out[:2].any()
+    again, none = run(cache, q, table, n, 500, 0.1, pages=sel.to(DEV), want_lse=False)
+    assert none is None and torch.equal(again, out)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_calls_on_two_streams_at_once(eight):
+    jobs = []
+    for seed, (lens, n_step) in enumerate([([2000, 90], 33), ([1500], 5)]):
+        cache, q, table, n, _ = setup(lens, 16, 16, 2, 128, eight, n_step, seed=seed)
+        jobs.append((cache, q, table, n, max(lens), run(cache, q, table, n, max(lens), 0.09), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for cache, q, table, n, top, want, stream in jobs:
+            got.append((idxc.paged_attention(cache.handle, q, table, n, top, 0.09, stream=stream), want))
+    torch.cuda.synchronize()
+    idxc.poll_device_status()
+    for (out, lse), want in got:
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
