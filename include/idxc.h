@@ -506,9 +506,9 @@ idxc_status idxc_paged_gather(const idxc_paged_cache* cache /* HOST */, const in
  *   workspace DEVICE, 256-byte aligned, idxc_paged_attention_workspace_bytes(n_step, H, H_kv, d) bytes; scratch, one per call in flight
  * H a multiple of H_kv, H / H_kv <= 128, n_step <= 1024. Rows of a page that no token sees do not influence the result, whatever they hold. A
  * request's newest n_step - 1 rows, which some of its tokens see and others do not, meet the others with weight 0 and have to be finite. A visible
- * score that is no number makes its row of out and lse none; a token all of whose visible scores are -inf is as one that sees nothing. Arithmetic: bf16
- * products (8-bit rows: f16, exact codes, q as f16 times a power of two) with fp32 accumulation, fp32 softmax, probabilities rounded to bf16 (f16) for the
- * second product, bf16 output. How the work is cut follows from the sizes, max_len and lens; the result does not depend on what else runs.
+ * score that is no number makes its row of out and lse none; a token all of whose visible scores are -inf is as one that sees nothing. An
+ * infinite value makes the rows that see it infinite or no numbers. Arithmetic: bf16 products (8-bit rows: f16, exact codes, q as f16 times a power of
+ * two) with fp32 accumulation, fp32 softmax, probabilities rounded to bf16 (f16) for the second product, bf16 output. How the work is cut follows from the sizes, max_len and lens; the result does not depend on what else runs.
  *
  * idxc_page_scores -- the largest score that any key between a page's bounds could reach, for choosing pages:
  *     scores[b * H_kv + g, p] = scale * max over i and the heads h of key head g of  sum_d max(q[b,i,h,d] * lo[d], q[b,i,h,d] * hi[d])

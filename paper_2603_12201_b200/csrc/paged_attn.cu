@@ -39,7 +39,7 @@ namespace {
 
 constexpr int kProducerRegs = 40;
 // Rows of a key head up to which this kernel is the faster one. (8 x 32768 keys, 8 key heads, d = 128 / 64. bf16: 32 rows 173 / 99 us here, 64 rows, with 8 warps
-// of which two shared keys, 240 / 183, and 186 / 134 by paged_attn_rows.cu. 8 bits: 32 rows 159 / 111 here and 271 / 207 there, 64 rows 305 / 227 and 273 / 210.)
+// of which two shared keys, 240 / 183, and 183 / 111 by paged_attn_rows.cu. 8 bits: 32 rows 159 / 111 here and 215 / 161 there, 64 rows 305 / 227 and 232 / 182.)
 constexpr int kRowsHere = 32;
 // Tiles of a CTA up to which few units are given to clusters. (bf16, 8 key heads, d = 128, one request of 777 / 2000 / 4000 / 8000 keys: 9.3 / 11.1 / 12.7 /
 // 13.9 us by runs and a merge, 6.1 / 7.5 / 10.4 / 16.4 by clusters, with 2, 4, 8 and 16 tiles a CTA.)

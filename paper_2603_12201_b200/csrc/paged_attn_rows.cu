@@ -9,7 +9,8 @@
 // While it does, the tensor cores work for the other way; one warp issues everything, PV of a way's tile before S of its next, so that scores arriving
 // mean that the output is at rest. A row's reference moves, and the output with it, only when a score passes it by 2^8. More than 128 rows: each way has
 // a block of 128 rows, and both share every tile. Fewer: both have the same rows and take tiles in turn, and their outputs meet in shared memory at the end
-// (8 x 32768 keys, 8 key heads, 128 rows, d = 128 / 64: 196 / 137 us, 242 / 212 with one way).
+// (8 x 32768 keys, 8 key heads, 128 rows, d = 128 / 64: 196 / 137 us, 242 / 212 with one way). Up to 64 rows: the 128 rows are two copies, each with the
+// probabilities of half of a tile's keys and zeros for the others, which halves a thread's share (64 rows 186 / 134 -> 183 / 111 us, 8 bits 273 / 210 -> 232 / 182).
 //
 // A warp fills a ring of tiles, K and V in turn, by TMA from pages or 16- to 64-key pieces of them. 8 bits: the ring holds codes, which four warps turn into f16
 // (exact) in a second ring, with q as f16 times a power of two a row and the value's scale in the probability, whose reference is the running
@@ -18,12 +19,13 @@
 //
 // Measured (graph replays, one B200; 8 requests, 8 key heads, d = 128 / 64; in brackets with the warp-level instructions of paged_attn.cu, 8 warps a CTA):
 //     rows   keys     bf16 us                   8 bits us
-//       64  32768     186 / 134 (240 / 183)      273 / 210 (305 / 227)
-//      128  32768     196 / 137 (477 / 347)      282 / 217 (540 / 424)
+//       64  32768     183 / 111 (240 / 183)      232 / 182 (305 / 227)
+//      128  32768     196 / 137 (477 / 347)      299 / 217 (540 / 424)
 //      512   8192     171 / 147 (492 / 358)      276 / 236 (560 / 436)
-//     4096   8192    1053 / 928 (3760 / 2695)   1769 / 1567 (4311 / 3322)
-// so up to 1045 / 595 TFLOP/s in bf16, 620 / 350 in 8 bits. A request's first 1024 tokens at once (8192 rows, half of the tiles): 317 / 254 us. What is left in
-// bf16: with d = 64 the exponentials (twice as many a flop); in 8 bits the softmax threads' instructions, two products and a sum more a score.
+//     4096   8192    1038 / 925 (3760 / 2695)   1770 / 1570 (4311 / 3322)
+// so up to 1060 / 595 TFLOP/s in bf16, 620 / 350 in 8 bits (bf16 of d = 128 under the power cap: 945 to 1060). A request's first 1024 tokens at once (8192 rows, half of the tiles): 317 / 254 us. What is left in
+// bf16: with d = 64 the exponentials (twice as many a flop); in 8 bits the softmax threads' instructions, two products and a sum more a score, and up
+// to 64 rows the four warps that convert.
 // Tried: 208 and 80 registers come without spills only if each role's code begins with its own setmaxnreg (scores spilled to local memory cost two thirds);
 // a thread's vectors of q loaded one after the other cost 10 us a segment; rows of the output written by their threads 317 -> 356 us.
 #include <cuda_bf16.h>
@@ -55,18 +57,20 @@ struct Layout {
     static constexpr int kRaws = FP8 ? (D == 64 ? 8 : 3) : 0;          // tiles of codes and scales
     static constexpr int kCodes = kTile * D;
     static constexpr int kRawBytes = FP8 ? kCodes + 1024 : 0;
-    static constexpr int kQBytes = WAYS * kWayRows * D * 2;            // WAYS == 1: half an output in fp32 as well
+    static constexpr int kQBytes = WAYS * kWayRows * D * 2;            // WAYS == 1: a quarter of both ways' outputs in fp32 as well
     static constexpr int kScaleBytes = FP8 ? kScaleTiles * 3 * kTile * 4 : 0;
     static constexpr int kPowerBytes = FP8 ? WAYS * kWayRows * 4 : 0;  // of two, taken out of a row of q
-    static constexpr int kRowBytes = kPowerBytes + (WAYS == 1 ? kWayRows * 8 : 0);              // and the second way's (maximum, sum)
     static constexpr int kSmall = 1024;
-    static constexpr int kBytes = 1024 + kSlots * kSlotBytes + kRaws * kRawBytes + kQBytes + kScaleBytes + kRowBytes + kSmall;
+    static constexpr int kBytes = 1024 + kSlots * kSlotBytes + kRaws * kRawBytes + kQBytes + kScaleBytes + kPowerBytes + kSmall;
     static constexpr uint32_t kColO = 256;                             // tensor memory: scores of way w at 128 w, output at kColO + D w
     static_assert(kBytes <= 232448, "shared memory of a CTA");
     static_assert((kSlots + kRaws) * 16 + 8 * 8 + kPosTiles * 32 + 128 <= kSmall, "small words");
 };
 
 __device__ __forceinline__ void threads_sync(int barrier, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory"); }
+
+__device__ __forceinline__ void tmem_ld_columns(uint32_t at, uint32_t (&o)[32]) { tmem_ld_32x32b_x32(at, o); }
+__device__ __forceinline__ void tmem_ld_columns(uint32_t at, uint32_t (&o)[16]) { tmem_ld_32x32b_x16(at, o); }
 
 // Tiles of block r of a request's rows: of the keys that its last row sees, or of the selection.
 __device__ __forceinline__ int tiles_of_block(const Params& p, int b, int r) {
@@ -117,12 +121,14 @@ struct Walk {
     }
 };
 
-template <int D, bool FP8, int WAYS>
+template <int D, bool FP8, int WAYS, int R>
 __global__ void __launch_bounds__((Layout<D, FP8, WAYS>::kThreads), 1)
 paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ Params p) {
     using L = Layout<D, FP8, WAYS>;
     constexpr int NS = L::kSlots, NR = FP8 ? L::kRaws : NS;            // tiles of 16-bit elements; what the producer fills
-    constexpr int kBlockRows = WAYS * kWayRows;
+    constexpr int kBlockRows = WAYS == 1 ? R : 2 * kWayRows;
+    constexpr int COPIES = kWayRows / R, NX = R / 32;                  // of the rows; a copy takes R of a tile's keys
+    static_assert(WAYS == 1 || R == kWayRows, "copies with one block of rows only");
     constexpr float kHead = FP8 ? kF16Head : 1.f;
     extern __shared__ uint8_t raw[];
     const uint32_t base = smem_u32(raw);
@@ -131,7 +137,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const uint32_t q_s = slots + NS * L::kSlotBytes + L::kRaws * L::kRawBytes;
     const uint32_t scale_s = q_s + L::kQBytes;   // [kScaleTiles][scales of K, log2 of V's, V's times 2^6][keys]
     const uint32_t row_s = scale_s + L::kScaleBytes;
-    const uint32_t bar_full = row_s + L::kRowBytes, bar_empty = bar_full + NS * 8;
+    const uint32_t bar_full = row_s + L::kPowerBytes, bar_empty = bar_full + NS * 8;
     const uint32_t bar_raw = FP8 ? bar_empty + NS * 8 : bar_full, bar_raw_empty = FP8 ? bar_raw + NR * 8 : bar_empty;
     const uint32_t bar_q = bar_empty + NS * 8 + L::kRaws * 16, bar_s = bar_q + 16, bar_p = bar_s + 16, bar_o = bar_p + 16;      // of two ways each
     const uint32_t pos_s = bar_o + 16;           // [kPosTiles][8] position of the first key of each piece, -1: none
@@ -214,7 +220,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             uint4 q_v[QV];
 #pragma unroll
             for (int u = 0; u < QV; ++u) {
-                const int i = (WAYS == 1 ? threadIdx.x : tid) + u * Q_THREADS, r = i / (D / 8), c = i % (D / 8);
+                const int i = (WAYS == 1 ? threadIdx.x : tid) + u * Q_THREADS, r = i / (D / 8) % R, c = i % (D / 8);
                 q_v[u] = make_uint4(0u, 0u, 0u, 0u);
                 if (row0 + r < rows_all) {
                     const int step = (row0 + r) / a.group, h = row0 + r - step * a.group;
@@ -248,7 +254,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             mbar_arrive(bar_q + 8 * q_block);
             if (FP8) threads_sync(WAYS == 1 ? 1 : 1 + w, Q_THREADS);
 
-            const int row = row0 + tid, step = min(row / a.group, a.n_step - 1);
+            const int row = row0 + tid % R, step = min(row / a.group, a.n_step - 1), key0 = tid / R * R;      // first key of the copy's (of a warp)
             const int sees = len - (a.n_step - 1 - step), sees_least = len - (a.n_step - 1 - row0 / a.group);
             const float row_scale = FP8 ? p.scale_log2 * ld_shared_f32(row_s + (q_block * kWayRows + tid) * 4) : p.scale_log2;
             constexpr int T0 = WAYS == 1 ? 1 : 0, STEP = WAYS == 1 ? 2 : 1;    // WAYS == 1: the ways take tiles in turn
@@ -273,15 +279,15 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         fence_proxy_async_smem();
                     }
                 }
-                const uint32_t sc_at = scale_s + ((it + t) % kScaleTiles) * (3 * kTile * 4);
-                uint32_t x[4][32];
+                const uint32_t sc_at = scale_s + ((it + t) % kScaleTiles) * (3 * kTile * 4) + key0 * 4;
+                uint32_t x[NX][32];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(s_col + 32 * c, x[c]);
+                for (int c = 0; c < NX; ++c) tmem_ld_32x32b_x32(s_col + key0 + 32 * c, x[c]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_wait(x[c]);
+                for (int c = 0; c < NX; ++c) tmem_ld_wait(x[c]);
                 if (FP8) {
 #pragma unroll
-                    for (int g = 0; g < 32; ++g) {                            // four keys
+                    for (int g = 0; g < R / 4; ++g) {                            // four keys
                         const float4 k_sc = ld_shared_f32x4(sc_at + g * 16);
                         uint32_t* y = &x[g / 8][g % 8 * 4];
                         y[0] = __float_as_uint(__uint_as_float(y[0]) * k_sc.x);
@@ -293,9 +299,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 float scale = row_scale;
                 if (!clean || (!FP8 && !(scale > 0.f))) {
 #pragma unroll
-                    for (int g = 0; g < 8; ++g) {                             // 16 keys
-                        const int first = __shfl_sync(0xFFFFFFFFu, pos, g * 16 >> piece_log2);
-                        const int n = first < 0 ? 0 : sees - first - (g * 16 & (piece - 1));
+                    for (int g = 0; g < R / 16; ++g) {                        // 16 keys
+                        const int k = key0 + g * 16, first = __shfl_sync(0xFFFFFFFFu, pos, k >> piece_log2);
+                        const int n = first < 0 ? 0 : sees - first - (k & (piece - 1));
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             uint32_t& y = x[g / 2][g % 2 * 16 + e];
@@ -307,7 +313,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 if (FP8) {
 #pragma unroll
-                    for (int g = 0; g < 32; ++g) {
+                    for (int g = 0; g < R / 4; ++g) {
                         const float4 above = ld_shared_f32x4(sc_at + kTile * 4 + g * 16);
                         const uint32_t* y = &x[g / 8][g % 8 * 4];
                         top4[0] = fmaxf(top4[0], fmaf(__uint_as_float(y[0]), scale, above.x));
@@ -317,7 +323,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     }
                 } else {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < NX; ++c)
 #pragma unroll
                         for (int e = 0; e < 32; ++e) top4[e & 3] = fmaxf(top4[e & 3], __uint_as_float(x[c][e]));
                 }
@@ -342,7 +348,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 const float use = m == -INFINITY ? 0.f : m;
                 float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {                                 // 16 keys
+                for (int c = 0; c < R / 16; ++c) {                            // 16 keys
                     uint32_t y[8];
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
@@ -361,7 +367,13 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                             y[e + 1] = pack_bf16(v[2], v[3]);
                         }
                     }
-                    tmem_st_32x32b_x8(s_col + 8 * c, y);
+                    tmem_st_32x32b_x8(s_col + key0 / 2 + 8 * c, y);
+                }
+                if (COPIES > 1) {                                             // the other copies' keys
+                    const uint32_t none[8] = {};
+#pragma unroll
+                    for (int c = 0; c < kTile / 16; ++c)
+                        if (8 * c < key0 / 2 || 8 * c >= (key0 + R) / 2) tmem_st_32x32b_x8(s_col + 8 * c, none);
                 }
                 l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 tmem_st_wait();
@@ -376,7 +388,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             // ---- output
             const bool writes = ok && row < rows_all;
             const int64_t out_row = (static_cast<int64_t>(s.b) * a.n_step + step) * a.H + s.head * a.group + (row - step * a.group);
-            const int64_t piece_row = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * kBlockRows + q_block * kWayRows + tid;
+            const int64_t piece_row = (static_cast<int64_t>(blockIdx.x) * 2 + (s.t0 == 0 ? 1 : 0)) * kBlockRows + q_block * kWayRows + tid % R;
             float over = 1.f;
             auto put = [&](int c, const uint32_t(&o)[32]) {                   // columns c .. c + 31 of the row
                 if (!writes) return;
@@ -434,50 +446,57 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     threads_sync(1 + w, 128);
                 }
             } else {
-                // The second way's part goes through shared memory, half of the columns at a time, in place of q, which both ways' products are done with.
-                if (w == 1) st_shared_f32x2(row_s + L::kPowerBytes + tid * 8, m, l);
+                // All parts of a row, two ways' and the copies', go through shared memory, a quarter of the columns at a time, in place of q, which the
+                // products are done with: [column][thread], so that neighbours meet in no bank.
                 threads_sync(1, 256);
-                float f = 1.f, f1 = 0.f;
-                if (w == 0) {
-                    const float2 other = ld_shared_f32x2(row_s + L::kPowerBytes + tid * 8);
-                    const float best = fmaxf(m, other.x), use = best == -INFINITY ? 0.f : best;
-                    f = exp2_fast(m - use);
-                    f1 = exp2_fast(other.x - use);
-                    m = best;
-                    l = l * f + other.y * f1;
-                    if (whole) over = l == 0.f ? 0.f : 1.f / (kHead * l);
-                }
-#pragma unroll 1
-                for (int half = 0; half < D; half += D / 2) {
-                    if (w == 1 && any) {
-#pragma unroll 1
-                        for (int c = 0; c < D / 2; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32b_x32(o_col + half + c, o);
-                            tmem_ld_wait(o);
+                st_shared_f32x2(q_s + threadIdx.x * 8, m, l);
+                threads_sync(1, 256);
+                const int r = threadIdx.x % R;
+                float best = -INFINITY;
+                l = 0.f;
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) st_shared_f32(q_s + ((c + e) * kWayRows + tid) * 4, __uint_as_float(o[e]));
+                for (int part = 0; part < 2 * COPIES; ++part) best = fmaxf(best, ld_shared_f32x2(q_s + (part * R + r) * 8).x);
+                const float use = best == -INFINITY ? 0.f : best, f = exp2_fast(m - use);
+#pragma unroll
+                for (int part = 0; part < 2 * COPIES; ++part) {
+                    const float2 ml = ld_shared_f32x2(q_s + (part * R + r) * 8);
+                    l = fmaf(ml.y, exp2_fast(ml.x - use), l);
+                }
+                m = best;
+                if (whole) over = l == 0.f ? 0.f : 1.f / (kHead * l);
+                threads_sync(1, 256);
+                constexpr int CW = D / 4, CT = CW / (2 * COPIES);             // columns of a turn; of a thread that sums
+                const int c0 = static_cast<int>(threadIdx.x) / R * CT;
+#pragma unroll 1
+                for (int c = 0; c < D; c += CW) {
+                    if (any) {
+                        uint32_t o[CW];
+                        tmem_ld_columns(o_col + c, o);
+                        tmem_ld_wait(o);
+#pragma unroll
+                        for (int e = 0; e < CW; ++e) st_shared_f32(q_s + (e * 256 + threadIdx.x) * 4, __uint_as_float(o[e]) * f);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < CW; ++e) st_shared_f32(q_s + (e * 256 + threadIdx.x) * 4, 0.f);
+                    }
+                    threads_sync(1, 256);
+                    float v[CT];
+#pragma unroll
+                    for (int e = 0; e < CT; ++e) {
+                        v[e] = 0.f;
+#pragma unroll
+                        for (int part = 0; part < 2 * COPIES; ++part) v[e] += ld_shared_f32(q_s + ((c0 + e) * 256 + part * R + r) * 4);
+                    }
+                    if (writes) {
+#pragma unroll
+                        for (int e = 0; e < CT; e += 2) {
+                            if (whole) *reinterpret_cast<uint32_t*>(a.out + out_row * D + c + c0 + e) = pack_bf16(v[e] * over, v[e + 1] * over);
+                            else *reinterpret_cast<float2*>(p.part_o + piece_row * D + c + c0 + e) = make_float2(v[e], v[e + 1]);
                         }
                     }
                     threads_sync(1, 256);
-                    if (w == 0) {
-#pragma unroll 1
-                        for (int c = 0; c < D / 2; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32b_x32(o_col + half + c, o);
-                            tmem_ld_wait(o);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                float v = __uint_as_float(o[e]) * f;
-                                if (s.n > 1) v = fmaf(ld_shared_f32(q_s + ((c + e) * kWayRows + tid) * 4), f1, v);
-                                o[e] = __float_as_uint(v);
-                            }
-                            put(half + c, o);
-                        }
-                    }
-                    threads_sync(1, 256);
                 }
-                if (w == 0) put_sums();
+                if (threadIdx.x < R) put_sums();
             }
             tcgen05_fence_before_sync();         // (the next segment's first product follows this thread's next arrival)
         }
@@ -718,21 +737,22 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 }
 
-template <int D, bool FP8, int WAYS>
+template <int D, bool FP8, int WAYS, int R>
 cudaError_t run_rows(const CUtensorMap& k_map, const CUtensorMap& v_map, const Params& p, int grid, cudaStream_t stream, int* launches) {
     using L = Layout<D, FP8, WAYS>;
-    const auto kernel = paged_rows_kernel<D, FP8, WAYS>;
+    const auto kernel = paged_rows_kernel<D, FP8, WAYS, R>;
     cudaError_t e = ensure_max_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes);
     if (e != cudaSuccess) return e;
     *launches += 1;
     e = launch_behind(kernel, dim3(grid), L::kThreads, L::kBytes, stream, k_map, v_map, p);
     if (e != cudaSuccess) return e;
-    const int all = p.a.n_step * p.a.group, rows = all < WAYS * kWayRows ? all : WAYS * kWayRows;
+    constexpr int kBlockRows = WAYS == 1 ? R : 2 * kWayRows;
+    const int all = p.a.n_step * p.a.group, rows = all < kBlockRows ? all : kBlockRows;
     *launches += 1;
     const float out_scale = FP8 ? 1.f / kF16Head : 1.f;
     if (grid > 12 * static_cast<int64_t>(p.a.B) * p.a.c.H_kv * p.row_blocks)      // many pieces a unit, as in paged_attn.cu
-        return launch_behind(paged_merge_kernel<D, WAYS * kWayRows, 4, 2>, dim3(grid, (rows + 1) / 2), 256, 0, stream, p, out_scale);
-    return launch_behind(paged_merge_kernel<D, WAYS * kWayRows, 1, 4>, dim3(grid, (rows + 3) / 4), 128, 0, stream, p, out_scale);
+        return launch_behind(paged_merge_kernel<D, kBlockRows, 4, 2>, dim3(grid, (rows + 1) / 2), 256, 0, stream, p, out_scale);
+    return launch_behind(paged_merge_kernel<D, kBlockRows, 1, 4>, dim3(grid, (rows + 3) / 4), 128, 0, stream, p, out_scale);
 }
 
 }  // namespace
@@ -742,8 +762,8 @@ cudaError_t launch_paged_attn_rows(const PagedAttnArgs& a, void* workspace, cons
     Params p{};
     p.a = a;
     p.ways = a.n_step * a.group > kWayRows ? 2 : 1;
-    const int block = p.ways * kWayRows;
-    p.row_blocks = (a.n_step * a.group + block - 1) / block;
+    const int rows = a.n_step * a.group, block = rows <= 64 ? 64 : p.ways * kWayRows;
+    p.row_blocks = (rows + block - 1) / block;
     p.heads = 1;
     p.tile_log2 = 7;
     p.piece_log2 = a.c.page_size % 64 == 0 ? 6 : (a.c.page_size % 32 == 0 ? 5 : 4);
@@ -755,8 +775,10 @@ cudaError_t launch_paged_attn_rows(const PagedAttnArgs& a, void* workspace, cons
     p.part_ml = reinterpret_cast<float2*>(w + most * 16);
     p.part_o = reinterpret_cast<float*>(w + most * 16 + most * 2 * block * 8);
     const int grid = sm_count < kPagedMaxSms ? sm_count : kPagedMaxSms;
-#define IDXC_RUN(D_, F_) \
-    (p.ways == 1 ? run_rows<D_, F_, 1>(k_map, v_map, p, grid, stream, launches) : run_rows<D_, F_, 2>(k_map, v_map, p, grid, stream, launches))
+#define IDXC_RUN(D_, F_)                                                                    \
+    (block == 64    ? run_rows<D_, F_, 1, 64>(k_map, v_map, p, grid, stream, launches)       \
+     : block == 128 ? run_rows<D_, F_, 1, 128>(k_map, v_map, p, grid, stream, launches)      \
+                    : run_rows<D_, F_, 2, 128>(k_map, v_map, p, grid, stream, launches))
     if (a.c.d == 128) return a.c.fp8 ? IDXC_RUN(128, true) : IDXC_RUN(128, false);
     return a.c.fp8 ? IDXC_RUN(64, true) : IDXC_RUN(64, false);
 #undef IDXC_RUN
