@@ -23,11 +23,11 @@
 //      128  32768     196 / 137 (477 / 347)      299 / 217 (540 / 424)
 //      512   8192     171 / 147 (492 / 358)      276 / 236 (560 / 436)
 //     4096   8192    1038 / 925 (3760 / 2695)   1770 / 1570 (4311 / 3322)
-// so up to 1060 / 595 TFLOP/s in bf16, 620 / 350 in 8 bits (bf16 of d = 128 under the power cap: 945 to 1060). A request's first 1024 tokens at once (8192 rows, half of the tiles): 317 / 254 us. What is left in
-// bf16: with d = 64 the exponentials (twice as many a flop); in 8 bits the softmax threads' instructions, two products and a sum more a score, and up
-// to 64 rows the four warps that convert.
-// Tried: 208 and 80 registers come without spills only if each role's code begins with its own setmaxnreg (scores spilled to local memory cost two thirds);
-// a thread's vectors of q loaded one after the other cost 10 us a segment; rows of the output written by their threads 317 -> 356 us.
+// so up to 1060 / 595 TFLOP/s in bf16 (d = 128: 945 to 1060 from run to run), 620 / 350 in 8 bits. A request's first 1024 tokens at once (8192 rows, half of
+// the tiles): 317 / 254 us. What is left in bf16: with d = 64 the exponentials (twice as many a flop); in 8 bits the softmax threads' instructions, two
+// products and a sum more a score, and up to 64 rows the four warps that convert.
+// Tried: 208 and 80 registers come without spills only if each role's code begins with its own setmaxnreg (3142 us with scores spilled to local memory, 1105
+// without); a thread's vectors of q loaded one after the other, and rows of the output written by their threads, 415 us for those first tokens.
 #include <cuda_bf16.h>
 
 #include "kernels.h"
