@@ -486,7 +486,10 @@ latent_attn_pair_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_
                 raw_ph ^= 1u;
             }
         };
+        // The ring is filled by bulk copies, of the asynchronous proxy, and read by plain loads, which may still be under way here: the arrival alone does
+        // not keep them in front of the next copy into the slot. (Without the fence about one call in 200 with tiles for all pairs read a row too late.)
         auto done_with = [&](uint32_t s) {
+            fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_raw_empty + 8 * s);
         };

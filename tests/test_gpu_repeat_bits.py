@@ -1,0 +1,57 @@
+"""The order of all sums is fixed by the sizes, so a call on the same inputs gives the same bits however often it is made. What varies from call to call is
+when copies land and warps run, so many calls in a row find what a comparison of one call with the oracle passes over: a slot of a ring that is
+refilled while it is still read."""
+import numpy as np
+import pytest
+import torch
+
+from tests.latent_util import bf16_rows, cache_rows
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def idxc():
+    from paper_2603_12201_b200 import binding
+    binding.lib()
+    return binding
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def same_every_time(call, n):
+    """call() -> tensors; n calls, the first's outputs bit for bit."""
+    words = lambda t: t.view({2: torch.int16, 4: torch.int32}[t.element_size()])
+    first = [t.clone() for t in call()]
+    differ = torch.zeros((), dtype=torch.int64, device=DEV)
+    for _ in range(n):
+        got = call()
+        differ += torch.stack([(words(a) != words(b)).any() for a, b in zip(got, first)]).any()
+    assert int(differ) == 0, f"{int(differ)} of {n} calls differ from the first"
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("lens,H,n_step", [([260], 128, 200), ([9000] * 40, 128, 1), ([5000, 3000, 777], 128, 1), ([77, 400], 20, 77), ([900] * 90, 16, 3)])
+def test_latent_attention(idxc, lens, H, n_step, four):
+    g, B = gen(n_step + H), len(lens)
+    kv = cache_rows(sum(lens), four, g).to(DEV)
+    q = bf16_rows(B * n_step * H, g, 0.5).view(B, n_step, H, 576).to(DEV)
+    base = torch.tensor(np.concatenate([[0], np.cumsum(lens)[:-1]]), device=DEV)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    same_every_time(lambda: idxc.latent_attention(q, kv, base, n, max(lens) + 9, 512, 1 / 24), 1000)
+    idxc.poll_device_status()
+
+
+@pytest.mark.parametrize("H", [16, 128])
+def test_selected_latent_rows(idxc, H):
+    g, n_q, n_kv, k = gen(H), 300, 5000, 700
+    kv = cache_rows(n_kv, True, g).to(DEV)
+    q = bf16_rows(n_q * H, g, 0.5).view(n_q, H, 576).to(DEV)
+    topk = torch.stack([torch.randperm(n_kv, generator=g)[:k] for _ in range(n_q)]).to(torch.int32).to(DEV)
+    same_every_time(lambda: idxc.sparse_attention_q4(q, kv, topk, 512, 1 / 24), 500)
+    idxc.poll_device_status()
