@@ -173,6 +173,7 @@ page_scores_kernel(const ScoreArgsP a) {
             lo[c] = ld_shared_v4(at + c * 64);
             hi[c] = ld_shared_v4(at + 2 * D + c * 64);
         }
+        fence_proxy_async_smem();                // (the loads may still be under way, and the next copy is the asynchronous proxy's)
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + 8 * st);
         float best0 = -INFINITY, best1 = -INFINITY;                // pages p0 + 2 j, + 1

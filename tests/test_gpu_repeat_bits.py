@@ -55,3 +55,34 @@ def test_selected_latent_rows(idxc, H):
     topk = torch.stack([torch.randperm(n_kv, generator=g)[:k] for _ in range(n_q)]).to(torch.int32).to(DEV)
     same_every_time(lambda: idxc.sparse_attention_q4(q, kv, topk, 512, 1 / 24), 500)
     idxc.poll_device_status()
+
+
+def tables(lens, P, g):
+    """Pages of all requests in no order: table, number of pages."""
+    pages = [-(-n // P) for n in lens]
+    perm = torch.randperm(sum(pages) + 5, generator=g).to(torch.int32)
+    table, at = torch.full((len(lens), max(pages) + 1), -1, dtype=torch.int32), 0
+    for b, n in enumerate(pages):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    return table.to(DEV), sum(pages) + 5
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv,n_step", [(64, 8, 1), (10, 5, 1), (64, 2, 4)])
+def test_page_scores(idxc, H, Hkv, n_step, d):
+    g, P = gen(H + d), 16
+    lens = [3000 + 1777 * b for b in range(24)]
+    table, n_pages = tables(lens, P, g)
+    bounds = (torch.randn((n_pages, Hkv, 2, d), generator=g)).sort(dim=2).values.to(torch.bfloat16).to(DEV).contiguous()
+    q = torch.randn((len(lens), n_step, H, d), generator=g).to(torch.bfloat16).to(DEV)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    scores = torch.zeros((len(lens) * Hkv, (table.shape[1] + 3) // 4 * 4), device=DEV)
+    count = torch.empty((len(lens) * Hkv,), dtype=torch.int32, device=DEV)
+
+    def call():
+        idxc.page_scores(bounds, q, table, n, P, d ** -0.5, scores, count)
+        return scores, count
+
+    same_every_time(call, 1000)
+    idxc.poll_device_status()
