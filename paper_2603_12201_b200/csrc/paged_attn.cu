@@ -579,6 +579,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         }
                     }
             }
+            fence_proxy_async_smem();                      // (this warp's loads before the copies that refill the stage)
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (NS + st));
         }

@@ -86,3 +86,20 @@ def test_page_scores(idxc, H, Hkv, n_step, d):
 
     same_every_time(call, 1000)
     idxc.poll_device_status()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("H,Hkv,n_step", [(32, 8, 1), (32, 4, 2), (32, 2, 2), (32, 2, 5), (16, 2, 80)])
+def test_paged_attention(idxc, H, Hkv, n_step, eight, d):
+    """8, 16, 32, 80 and 640 rows of a key head."""
+    g, P = gen(H + d), 32
+    lens = [200 + 333 * b for b in range(24)]
+    table, n_pages = tables(lens, P, g)
+    k, v = [torch.randn((n_pages, P, Hkv, d), generator=g).to(torch.float8_e4m3fn if eight else torch.bfloat16).to(DEV) for _ in range(2)]
+    scales = [torch.rand((n_pages, Hkv, P), generator=g).to(DEV) + 0.5 if eight else None for _ in range(2)]
+    cache = idxc.PagedCache(k, v, *scales)
+    q = torch.randn((len(lens), n_step, H, d), generator=g).to(torch.bfloat16).to(DEV)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    same_every_time(lambda: idxc.paged_attention(cache, q, table, n, max(lens), d ** -0.5), 500)
+    idxc.poll_device_status()
