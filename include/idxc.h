@@ -513,7 +513,9 @@ idxc_status idxc_paged_gather(const idxc_paged_cache* cache /* HOST */, const in
  * idxc_page_scores -- the largest score that any key between a page's bounds could reach, for choosing pages:
  *     scores[b * H_kv + g, p] = scale * max over i and the heads h of key head g of  sum_d max(q[b,i,h,d] * lo[d], q[b,i,h,d] * hi[d])
  * for the pages p < n_pages_out[b * H_kv + g] = min(ceil(lens[b] / P), ld_table) of the request; other entries of the row are left as they are. The first keep_first
- * and the last keep_last pages get 3e38, pages that are none of the cache's -3e38. With k_top pages wanted,
+ * and the last keep_last pages get 3e38, other pages that are none of the cache's -3e38. Bounds and q may be infinite (the keys of a page may): a product of 0 and
+ * an infinity counts as 0, so a key of -inf does not hide the others of its page. A row (i, h) whose sum is no number, because q holds one or infinities of both signs
+ * meet, scores 3e38. With k_top pages wanted,
  * idxc_topk_rows(scores, ld_scores, B * H_kv, 0, 0, n_pages_out, k_top, pages) gives the selection that idxc_paged_attention takes (it wants ld_scores a
  * multiple of 4 and scores 16-byte aligned).
  *   bounds   DEVICE bf16 [n_pages, H_kv, 2, d], 16-byte aligned; scores DEVICE fp32 [B * H_kv, ld_scores], ld_scores >= ld_table

@@ -113,6 +113,19 @@ def page_score(q, edge, scale: float):
     return scale * terms.sum(axis=1).max(), abs(scale) * np.abs(terms).sum(axis=1).max()
 
 
+def page_score_any(q, edge, scale: float) -> float:
+    """page_score for any bit patterns: a product of 0 and an infinity counts as 0, a row whose sum is no number as 3e38."""
+    def product(x, y):
+        with np.errstate(invalid="ignore"):
+            return np.where(((x == 0) & np.isinf(y)) | ((y == 0) & np.isinf(x)), 0.0, x * y)
+    best = -np.inf
+    for row in q:
+        with np.errstate(invalid="ignore"):
+            total = scale * np.maximum(product(row, edge[0]), product(row, edge[1])).sum()
+        best = max(best, float(np.float32(3e38)) if np.isnan(total) else total)
+    return best
+
+
 def attention(q, k, v, scale: float, mask):
     """q [R, d], k, v [n, d] float64, mask [R, n]. Returns out [R, d], lse [R], spread [R, d] = sum p |v|, reach [R] = scale * max_s sum |q||k|."""
     R, n = q.shape[0], k.shape[0]

@@ -6,7 +6,10 @@
 // those of up to eight heads of a page (4 KB) into a ring in shared memory, 64 (page, head) pairs a stage; eight warps take eight pages of a head each
 // with warp-level MMAs (rows as M, pages as N). The columns are permuted alike in both operands, so that a lane's share of four fragments is 16
 // contiguous bytes, and slots lie 64 bytes farther apart than they are long, so that the reads meet no bank twice. 32 requests of 8K to 64K positions
-// (73702 pages of 8 heads, d = 128): 53 us, 5.7 TB/s; with fragments straight from global memory, 64 bytes of eight pages an instruction, 58.
+// (73702 pages of 8 heads, d = 128): 54 us, 5.6 TB/s; with fragments straight from global memory, 64 bytes of eight pages an instruction, 58 where this took 53.
+//
+// A key of -inf in a column where q is positive must not hide its page: the products with the part of q that is 0 are 0 * -inf then, and the sum is no
+// number. So are sums with a q that holds none. Such sums are carried through every maximum, and those pages (none, as a rule) are scored again column by column.
 #include <cuda_bf16.h>
 
 #include "kernels.h"
@@ -36,7 +39,7 @@ struct ScoreArgsP {
     float* scores;
     int64_t ld;
     int32_t* n_out;
-    int steps;                   // stages' worth of pages a CTA takes
+    int steps;                   // stages' worth of pages a CTA takes: at most 8
     int heads;                   // key heads of a CTA: 1, 2, 4 or 8
     unsigned int* status;
 };
@@ -44,9 +47,41 @@ struct ScoreArgsP {
 template <bool POSITIVE>
 __device__ __forceinline__ uint32_t part_of(uint32_t x) {
     uint32_t r;
-    if (POSITIVE) asm volatile("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0u));
-    else asm volatile("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0u));
+    if (POSITIVE) asm volatile("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0u));
+    else asm volatile("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0u));
     return r;
+}
+// The larger one; none if either is none.
+__device__ __forceinline__ float max_or_none(float x, float y) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+// One page's score by its definition, for a warp: `edge` the bounds of a page and head, `first` the token of the launch's first query row, `h` that row's place among
+// the key head's, whose first head q points to. A product of 0 and an infinity is 0; a row whose sum is no number scores kForced.
+template <int D>
+__device__ __noinline__ float score_by_columns(const __nv_bfloat16* edge, const __nv_bfloat16* q, int64_t q_stride, int group, int first, int h, int rows,
+                                               float scale) {
+    constexpr int V = D / 32;
+    const int at = (threadIdx.x & 31) * V;
+    auto product = [](float x, float y) { return (x == 0.f && fabsf(y) == INFINITY) || (y == 0.f && fabsf(x) == INFINITY) ? 0.f : x * y; };
+    float best = -INFINITY;
+    for (int r = 0; r < rows; ++r) {
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float x = __bfloat162float(q[first * q_stride + h * D + at + v]);
+            sum += max_or_none(product(x, __bfloat162float(edge[at + v])), product(x, __bfloat162float(edge[D + at + v])));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        best = fmaxf(best, sum == sum ? sum * scale : kForced);
+        if (++h == group) {
+            h = 0;
+            ++first;
+        }
+    }
+    return best;
 }
 
 template <int D>
@@ -156,6 +191,7 @@ page_scores_kernel(const ScoreArgsP a) {
         }
         asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
     }
+    uint32_t again = 0;                          // steps whose page of this lane has to be scored column by column
     for (int i = 0; i < n; ++i) {
         const int st = i % kStages, p0 = first + i * per_step + slice * 8;
         if (!mbar_wait(full + 8 * st, (i / kStages) & 1, abort_flag)) {
@@ -201,18 +237,18 @@ page_scores_kernel(const ScoreArgsP a) {
             }
             const int r = t * 16 + g;
             if (r < a.rows) {
-                best0 = fmaxf(best0, acc[0] + more[0]);
-                best1 = fmaxf(best1, acc[1] + more[1]);
+                best0 = max_or_none(best0, acc[0] + more[0]);
+                best1 = max_or_none(best1, acc[1] + more[1]);
             }
             if (r + 8 < a.rows) {
-                best0 = fmaxf(best0, acc[2] + more[2]);
-                best1 = fmaxf(best1, acc[3] + more[3]);
+                best0 = max_or_none(best0, acc[2] + more[2]);
+                best1 = max_or_none(best1, acc[3] + more[3]);
             }
         }
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
-            best0 = fmaxf(best0, __shfl_xor_sync(0xFFFFFFFFu, best0, o));
-            best1 = fmaxf(best1, __shfl_xor_sync(0xFFFFFFFFu, best1, o));
+            best0 = max_or_none(best0, __shfl_xor_sync(0xFFFFFFFFu, best0, o));
+            best1 = max_or_none(best1, __shfl_xor_sync(0xFFFFFFFFu, best1, o));
         }
         const float mine = __shfl_sync(0xFFFFFFFFu, best0, (lane >> 1) & 3), other = __shfl_sync(0xFFFFFFFFu, best1, (lane >> 1) & 3);
         const int p = p0 + lane;
@@ -220,9 +256,20 @@ page_scores_kernel(const ScoreArgsP a) {
             float u = (lane & 1 ? other : mine) * a.scale;
             if (!(ok >> lane & 1)) u = -kForced;
             if (p < a.keep_first || p >= pages - a.keep_last) u = kForced;
-            out[p] = a.row0 > 0 ? fmaxf(out[p], u) : u;
+            if (u != u) again |= 1u << i;
+            else out[p] = a.row0 > 0 ? fmaxf(out[p], u) : u;
         }
     }
+    if (!__any_sync(0xFFFFFFFFu, again != 0u)) return;
+    for (int i = 0; i < n; ++i)
+        for (uint32_t none = __ballot_sync(0xFFFFFFFFu, again >> i & 1u); none; none &= none - 1) {
+            const int p = first + i * per_step + slice * 8 + __ffs(none) - 1, token = a.row0 / a.group;
+            const int64_t page = a.table[b * a.ld_table + p];
+            const float u = score_by_columns<D>(a.bounds + (page * a.H_kv + head) * 2 * D,
+                                                a.q + static_cast<int64_t>(b) * a.n_step * a.q_stride + static_cast<int64_t>(head) * a.group * D, a.q_stride, a.group, token,
+                                                a.row0 - token * a.group, a.rows, a.scale);
+            if (lane == 0) out[p] = a.row0 > 0 ? fmaxf(out[p], u) : u;
+        }
 }
 
 template <int D, bool FEW>
