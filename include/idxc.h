@@ -440,13 +440,14 @@ idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t
  * requests and of their pages, free_pages[count - 1] first. A request is refused, and all behind it, when the stack does not hold what it and
  * those in front of it want, when its pages would not fit ld_table, or its tokens not n_slots. For a request that is served, the table gets its pages, lens[b]
  * grows by n, and start_out[b] is its length before; for one that is refused start_out[b] = -1 and nothing changes.
- *   free_pages DEVICE int32 [free_capacity] (read), free_count DEVICE int32 [1] (taken as at most free_capacity; lowered by the pages taken)
+ *   free_pages DEVICE int32 [free_capacity] (read; pages, so none below 0), free_count DEVICE int32 [1] (taken as at most free_capacity; lowered by the pages taken)
  *   token_begin_out DEVICE int32 [B + 1]: tokens in front of each request, refused ones included (sums above 2^31 - 1 are given as that)
  *   slots_out DEVICE int64 [n_slots]: token j of request b at token_begin_out[b] + j; -1 for tokens of refused requests and behind the last token
  *   seq_out   NULL or DEVICE int32 [n_slots]: the token's request, -1 behind the last token
  * idxc_page_release -- requests cut to their first keep_lens[b] positions (NULL or negative: 0, finished requests): lens[b] = min(lens[b], keep_lens[b]), and the pages that
  * hold none of them return to the stack, in the reverse of the order above, so that giving back what idxc_page_tables has just handed out leaves the
- * stack as it was. Their table entries become -1. Pages for which the stack has no room (free_capacity) are dropped.
+ * stack as it was. Their table entries become -1. Entries below 0 (no page) stay off the stack, pages for which it has no room (free_capacity) are dropped.
+ * A page goes on the stack once for every entry that names it: where requests share pages, the caller sets all but one entry to -1 beforehand.
  * idxc_page_rows -- positions (such as topk_out) as rows of a paged cache: out[r, j] = the slot of positions[r, j] in the request of row r, which is seq[r] (NULL: r);
  * -1 for positions below 0 or behind the table, for table entries below 0 and for requests outside [0, B). The rows serve idxc_sparse_attention
  * and idxc_sparse_attention_q4 over a paged latent cache with kv_base = NULL. positions, out: DEVICE int32 [n_rows, k]; out may be positions.

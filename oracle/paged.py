@@ -45,13 +45,14 @@ def page_tables(table, lens, new_tokens, free_pages, free_count: int, P: int, n_
 
 
 def page_release(table, lens, keep, free_pages, free_count: int, P: int):
-    """Returns (table, lens, free_pages, free_count) after every request has been cut to keep[b] positions."""
+    """Returns (table, lens, free_pages, free_count) after every request has been cut to keep[b] positions; entries that are no page (below 0) stay off the stack."""
     table, lens, free_pages = np.array(table, dtype=np.int64), np.array(lens, dtype=np.int64), np.array(free_pages, dtype=np.int64)
     back = []
     for b in range(table.shape[0]):
         kept = min(int(lens[b]), max(int(keep[b]), 0))
         for p in range(ceil_div(kept, P), min(ceil_div(int(lens[b]), P), table.shape[1])):
-            back.append(int(table[b, p]))
+            if table[b, p] >= 0:
+                back.append(int(table[b, p]))
             table[b, p] = -1
         lens[b] = kept
     for page in reversed(back):
