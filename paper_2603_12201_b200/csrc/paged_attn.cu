@@ -192,8 +192,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         }
         *abort_flag = 0;
         fence_mbar_init();
-        tma_prefetch_desc(&k_map);
-        tma_prefetch_desc(&v_map);
+        if (p.a.c.n_pages > 0) {                 // (a cache without pages has no maps)
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&v_map);
+        }
     }
     let_next_start();
     wait_for_previous();

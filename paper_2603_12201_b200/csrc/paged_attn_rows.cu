@@ -163,8 +163,10 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         }
         *abort_flag = 0;
         fence_mbar_init();
-        tma_prefetch_desc(&k_map);
-        tma_prefetch_desc(&v_map);
+        if (p.a.c.n_pages > 0) {                 // (a cache without pages has no maps)
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&v_map);
+        }
     }
     if (warp == kProductsWarp) {
         tmem_alloc(tmem_s, 512);
