@@ -464,7 +464,7 @@ idxc_status idxc_page_rows(const int32_t* table, int64_t ld_table, int64_t B, co
  * by side in one array). HOST struct of DEVICE pointers.
  *   IDXC_BF16      k, v bf16; no scales
  *   IDXC_FP8_E4M3  k, v e4m3 codes; k_scale, v_scale fp32 [n_pages, H_kv, page_size], value = code * scale (16-byte aligned). Value scales are
- *                  positive and at most 2^60.
+ *                  not negative and at most 2^100; rows with scales below 2^-60 lose digits in the attention.
  *   bounds         NULL, or bf16 [n_pages, H_kv, 2, d], 16-byte aligned: the smallest (0) and largest (1) value of every key column of a page
  * d in {64, 128}; k, v 16-byte aligned, strides multiples of 16 bytes, at least 16 bytes and below 2^39 bytes; 1 <= H_kv <= 1024; n_pages * page_size < 2^31. */
 typedef struct {
@@ -481,7 +481,8 @@ typedef struct {
 
 /* ---------------------------------------------------------------------------
  * idxc_paged_append -- keys and values of n tokens written to their slots (a slot outside the cache: not written; slots distinct). In 8 bits every
- * (token, head) gets scale = max(max|x|, 1e-12) / 448 and codes as idxc_quantize_e4m3 writes them. With bounds, those of every page written to
+ * (token, head) gets scale = max(max|x|, 1e-12) / 448 and codes as idxc_quantize_e4m3 writes them (elements of v above 5e32 get scales that
+ * idxc_paged_attention does not take). With bounds, those of every page written to
  * become the bounds of its rows 0 .. the last one written, as they read back in bf16. For that, the tokens of one page follow each other, in ascending slots
  * without gaps (as idxc_page_tables gives them), and its rows in front of them hold the request's earlier tokens.
  *   k, v     DEVICE bf16 [n, H_kv, d], 16-byte aligned, k_stride and v_stride elements between tokens (multiples of 8, at least H_kv * d: a projection's

@@ -61,9 +61,10 @@ __device__ __forceinline__ void st_shared_f32(uint32_t addr, float x) { asm vola
 __device__ __forceinline__ void st_shared_f32x2(uint32_t addr, float x, float y) {
     asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y) : "memory");
 }
-// log2 of a positive scale, rounded up, as a number between -60 and 60.
+// log2 of a positive scale, rounded up, as a number between -60 and 100. (A row's largest probability is 2 to minus that, against the reference that it goes into:
+// with 100, probabilities down to 2^-26 of it are normal numbers; with -60, sums of 2^30 of them and the reference's lag stay below 2^98.)
 __device__ __forceinline__ float log2_above(float scale) {
-    return static_cast<float>(min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 126, -60), 60));
+    return static_cast<float>(min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 126, -60), 100));
 }
 // Keys of request b that the call knows of.
 __device__ __forceinline__ int length_of(const PagedAttnArgs& a, int b) { return min(max(a.lens[b], 0), static_cast<int>(a.max_len)); }
