@@ -430,7 +430,9 @@ idxc_status idxc_compact_rows(const void* src, void* dst, int row_bytes, int64_t
  *
  * A page holds P = page_size positions of a request. Request b's logical page p is physical page table[b, p]; the slot of a position s is
  * table[b, s / P] * P + s % P: the row of that position in a cache of n_pages * P rows. Slots are the dst_rows of idxc_quantize_e4m3 and
- * idxc_quantize_q4, so indexer keys and latent rows are appended to paged caches by the calls that are there.
+ * idxc_quantize_q4, so indexer keys and latent rows can be written to pages by the calls that are there. Of the calls that read these two caches
+ * only the sparse attention takes pages (idxc_page_rows): idxc_indexer_decode, idxc_latent_attention and idxc_attention_weights over whole sequences want a
+ * sequence's rows one after the other.
  *   table    DEVICE int32 [B, ld_table]; entries behind a request's pages are not looked at
  *   lens     DEVICE int32 [B], positions of every request (negative: 0)
  *   page_size a multiple of 16, 16 .. 1024; B <= 65535; B * ld_table < 2^31
@@ -464,7 +466,7 @@ idxc_status idxc_page_rows(const int32_t* table, int64_t ld_table, int64_t B, co
  * by side in one array). HOST struct of DEVICE pointers.
  *   IDXC_BF16      k, v bf16; no scales
  *   IDXC_FP8_E4M3  k, v e4m3 codes; k_scale, v_scale fp32 [n_pages, H_kv, page_size], value = code * scale (16-byte aligned). Value scales are
- *                  not negative and at most 2^100; rows with scales below 2^-60 lose digits in the attention.
+ *                  not negative; scales are at most 2^100, and rows with value scales below 2^-60 lose digits in the attention.
  *   bounds         NULL, or bf16 [n_pages, H_kv, 2, d], 16-byte aligned: the smallest (0) and largest (1) value of every key column of a page
  * d in {64, 128}; k, v 16-byte aligned, strides multiples of 16 bytes, at least 16 bytes and below 2^39 bytes; 1 <= H_kv <= 1024; n_pages * page_size < 2^31. */
 typedef struct {
@@ -484,7 +486,8 @@ typedef struct {
  * (token, head) gets scale = max(max|x|, 1e-12) / 448 and codes as idxc_quantize_e4m3 writes them (elements of v above 5e32 get scales that
  * idxc_paged_attention does not take). With bounds, those of every page written to
  * become the bounds of its rows 0 .. the last one written, as they read back in bf16. For that, the tokens of one page follow each other, in ascending slots
- * without gaps (as idxc_page_tables gives them), and its rows in front of them hold the request's earlier tokens.
+ * without gaps (as idxc_page_tables gives them), and its rows in front of them hold the request's earlier tokens. The tokens of a page are one thread block's
+ * work for every 2048 columns of a row: a long prompt is written at the memory's rate in many pages, not in one or two of 1024.
  *   k, v     DEVICE bf16 [n, H_kv, d], 16-byte aligned, k_stride and v_stride elements between tokens (multiples of 8, at least H_kv * d: a projection's
  *            output may hold queries, keys and values side by side)
  * idxc_paged_gather -- rows read back: k_out, v_out DEVICE bf16 [n, H_kv, d] without gaps, 16-byte aligned; zeros for slots outside the cache.
@@ -520,6 +523,7 @@ idxc_status idxc_paged_gather(const idxc_paged_cache* cache /* HOST */, const in
  * meet, scores 3e38. With k_top pages wanted,
  * idxc_topk_rows(scores, ld_scores, B * H_kv, 0, 0, n_pages_out, k_top, pages) gives the selection that idxc_paged_attention takes (it wants ld_scores a
  * multiple of 4 and scores 16-byte aligned).
+ * Made for decode steps and drafted tokens: the n_step * H / H_kv query rows of a key head are taken 64 at a time, a launch each, which reads all bounds again.
  *   bounds   DEVICE bf16 [n_pages, H_kv, 2, d], 16-byte aligned; scores DEVICE fp32 [B * H_kv, ld_scores], ld_scores >= ld_table
  *   scale    positive and finite
  * ------------------------------------------------------------------------- */

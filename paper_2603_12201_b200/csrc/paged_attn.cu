@@ -6,7 +6,8 @@
 // memory, one launch in all.
 //
 // Measured (graph replays, one B200): 32 requests of 4K to 32K bf16 keys, 64 heads over 8: 352 us, 6.9 TB/s of what has to be read; 8 requests of 131072
-// 8-bit keys: 352 us, 6.3 TB/s; 8 x 32768 with 16 / 32 rows a key head: bf16 6.4 / 6.2, 8 bits 5.4 / 3.4 TB/s; one request of 777 keys: 6.1 us.
+// 8-bit keys: 352 to 371 us from run to run, 6.3 to 6.0 TB/s; 8 x 32768 with 16 / 32 rows a key head: bf16 6.4 / 6.2, 8 bits 5.4 / 3.4 TB/s; one request of 777
+// keys: 6.5 us.
 //
 // What bounds it: a key and a value of d columns are 4 d bytes (bf16) and 4 d flops a query row; with the 1 to 32 rows that share a key head
 // in a decode step that is 1 to 32 flops a byte, far below the tensor cores' 200: HBM. So the design serves the copies: a ring of 64- or 128-key tiles

@@ -6,7 +6,9 @@
 // (never from what they were), one thread owns a column's bounds, and nothing is read twice. A thread owns 8 columns (16 bytes) of a head; what
 // a head's 8 or 16 threads share is only the row's maximum in front of the e4m3 codes. HBM-bound: 8 bytes moved per element of k and v in bf16
 // (read, written), 6 in e4m3, and for a decode step the latency of one page's rows. Measured: 70299 tokens of 8 heads with d = 128 in e4m3 105 us (4.1 TB/s
-// of what is read and written; bound by its instructions, 75 % of the issue slots), 32 tokens in bf16 6.2 us; the same read back 78 and 5 us.
+// of what is read and written; bound by its instructions, 75 % of the issue slots), in bf16 97 us (5.9 TB/s), 32 tokens in bf16 6.2 us; the same read back 78 to 84, 88
+// and 5 us. Few long pages leave most of the GPU idle: 1000 tokens of 8 heads, d = 128, bf16 / e4m3, take 7 / 10 us in pages of 16, 12 / 23 in pages of 64, and 89 / 255
+// in one of 1024, which is one CTA's.
 #include "e4m3_rows.cuh"
 #include "kernels.h"
 #include "ptx_sm100.cuh"
